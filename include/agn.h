@@ -51,6 +51,8 @@ extern "C" {
 #define AGN_PREC_FP32 0        /* fp32 parameters, activations and GEMMs    */
 #define AGN_PREC_BF16 1        /* bf16 GEMM operands, fp32 accumulation, fp32
                                   master replicas and accumulators            */
+#define AGN_PREC_MX4 2         /* microscaled 4-bit codes and scales: only where a
+                                  call says so (agn_mx4_linear's output)      */
 
 #define AGN_DIST_UNIFORM 0     /* x ~ U[0,1)^d0 */
 #define AGN_DIST_NORMAL 1      /* x ~ N(0,1)^d0 */
@@ -394,6 +396,109 @@ int agn_commit_pull_noalloc(float* theta_c, float* acc, float* replicas, void* r
                             const int32_t* commit_worker, const int32_t* pull_offsets,
                             const int32_t* pull_workers, double eta, int32_t lambda,
                             int32_t normalize, float* delta_norm, void* stream);
+
+/*
+ * Dropout of a layer's activations, with the layer's bias and ReLU before it and
+ * a residual after it in the same pass (the paper's experiments leave their
+ * model open, Section 4; no counterpart call).  Per element of x [rows][cols]
+ *     v = x + bias[c] (fp32);  v = 0 where relu and v <= 0;
+ *     y = (keep(r, c) ? v * scale : 0) + residual, rounded once to dtype.
+ * keep comes from a counter-based generator and is stored nowhere: with
+ * T = round(65536 p) (ties to even, at most 65535), element (r, c) is kept iff its 16 bits of
+ * the library's splitmix64 generator are >= T: number
+ * offset + r ceil(cols / 4) + floor(c / 4) (mod 2^64) of stream 8 of `seed`,
+ * bits 16 (c mod 4) and up.  scale = 65536 / (65536 - T), so that kept values
+ * make up for the dropped ones exactly at the probability T / 65536 that is
+ * used.  A call uses rows ceil(cols / 4) numbers: a caller that wants other
+ * masks at every step adds that to offset.  agn_run's option `dropout` uses this
+ * mask.  A dropped element is 0 (the residual) whatever x holds, NaN and
+ * infinities too; a NaN that is kept stays one.
+ *   dtype     : AGN_PREC_FP32 or AGN_PREC_BF16, of x, residual and y;
+ *   bias      : device fp32 [cols], NULL = none;  residual: NULL = none;
+ *   ldx, ldr, ldy: row strides in elements, >= cols (ldr unused without a
+ *               residual); rows that start on 16-byte boundaries are faster;
+ *   y         : may be x or the residual itself with the same stride (in place);
+ *               any other overlap is AGN_E_INVALID.  Bytes between the rows are
+ *               left alone.
+ *   p         : in [0, 1).  rows or cols 0: nothing to do.
+ * This call and the ones after it queue their work on `stream` and return
+ * without waiting; they allocate nothing, keep nothing between calls, may be
+ * captured into a graph, and need every buffer in memory of the current
+ * device, to which the stream belongs (else AGN_E_INVALID or AGN_E_CUDA).
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_dropout(const void* x, const float* bias, const void* residual, void* y, int32_t dtype,
+                int32_t relu, int64_t rows, int64_t cols, int64_t ldx, int64_t ldr, int64_t ldy,
+                double p, uint64_t seed, uint64_t offset, void* stream);
+
+/*
+ * Gradient of agn_dropout: from dy = dL/dy,
+ *     dx = keep(r, c) and not (relu and x + bias <= 0) ? dy * scale : 0
+ * (rounded once to dtype) with the mask of (p, seed, offset), computed anew, and
+ *     dbias[c] = sum_r of dx[r][c] before its rounding, fp32, in a fixed order
+ * (the same bits each time).  The residual's gradient is dy itself.
+ *   x, bias   : the forward call's, read only with relu (bias NULL = none there);
+ *   dx        : may be dy or x itself with the same stride;
+ *   dbias     : device fp32 [cols], NULL = not wanted; with rows = 0 it is zeroed.
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_dropout_backward(const void* dy, const void* x, const float* bias, void* dx, float* dbias,
+                         int32_t dtype, int32_t relu, int64_t rows, int64_t cols, int64_t lddy,
+                         int64_t ldx, int64_t lddx, double p, uint64_t seed, uint64_t offset,
+                         void* stream);
+
+/*
+ * Microscaled 4-bit matrices (OCP Microscaling Formats 1.0, MXFP4; no
+ * counterpart in the paper).  A [rows][cols] matrix is two device buffers,
+ * 16-byte aligned, whose sizes agn_mx4_bytes gives:
+ *   codes : [rows][16 ceil(cols / 32)] bytes, element 2i of a row in the low and
+ *           2i + 1 in the high half of byte i.  A code is E2M1: a sign bit (8) and
+ *           one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; codes past cols are 0.
+ *   scales: a power of two for 32 consecutive elements of a row, E8M0 (2^(code - 127);
+ *           255 is NaN).  Blocks kb = 0 .. ceil(cols / 32) - 1 of row r are bytes
+ *             ((r / 128) K + kb / 4) 512 + (r mod 32) 16 + ((r / 32) mod 4) 4 + kb mod 4,
+ *           K = ceil(ceil(cols / 32) / 4): tiles of 128 rows x 4 blocks, as the
+ *           tensor cores read them.  Blocks past the row's last in its last tile
+ *           are 0; rows past the last one are never written and never matter.
+ * agn_mx4_bytes: either pointer may be NULL; needs no GPU.
+ */
+int agn_mx4_bytes(int64_t rows, int64_t cols, int64_t* codes, int64_t* scales);
+
+/*
+ * Quantise the rows of x: a block's scale is 2^e, e = floor(log2 max|x|) - 2,
+ * at least -127 (blocks of zeros too); its codes are x 2^-e rounded to the nearest
+ * E2M1 value (ties to the even code), saturating at 6.  A block that holds a
+ * NaN or an infinity gets the scale NaN (codes 0): every value of it is NaN.
+ *   x: device [rows][ldx] of dtype (AGN_PREC_FP32 or AGN_PREC_BF16), ldx >= cols.
+ * rows or cols 0: nothing to do.  Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_mx4_quantize(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx,
+                     void* codes, void* scales, void* stream);
+
+/* The values that codes and scales stand for, exact in either dtype, into y
+ * [rows][ldy] (bytes between the rows are left alone).  Errors as above. */
+int agn_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, void* y,
+                       int32_t dtype, int64_t ldy, void* stream);
+
+/*
+ * A layer on microscaled operands, on the tensor cores:
+ *     y[r][f] = act(sum_k x[r][k] w[f][k] + bias[f]),  act = ReLU with relu, else none
+ * x [rows][in] and w [out][in] in 4-bit form, fp32 sums, any rows >= 0, in >= 1,
+ * out >= 1 (below 2^31 - 256).  A NaN passes the ReLU.
+ *   y     : dtype AGN_PREC_FP32 or AGN_PREC_BF16: device [rows][ldy], ldy >= out, rounded
+ *           once from the fp32 value.  AGN_PREC_MX4: y and y_scales are the codes
+ *           and scales of a [rows][out] matrix, quantised from the fp32 values as
+ *           agn_mx4_quantize does: the next layer's x (ldy unused).
+ *   bias  : device fp32 [out], NULL = none.
+ *   err   : device int32, NULL = none: set to 1 (never cleared) when a bounded wait of the kernel
+ *           gave up (2 s); the values that it could not compute are NaN.
+ * The order of the sums depends on the sizes alone: equal calls give equal bits.
+ * Errors: AGN_E_INVALID, AGN_E_UNSUPPORTED (more than 16776960 rows), AGN_E_CUDA.
+ */
+int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_codes,
+                   const void* w_scales, const float* bias, int64_t rows, int64_t in, int64_t out,
+                   int32_t relu, void* y, int32_t dtype, int64_t ldy, void* y_scales, int32_t* err,
+                   void* stream);
 
 /*
  * Test hook of the failure path of the bounded device waits (the paper has no

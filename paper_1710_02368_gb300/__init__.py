@@ -16,7 +16,7 @@ import numpy as np
 from . import _lib
 from ._lib import (AGN_COMMIT_AGN, AGN_COMMIT_DYNSGD, AGN_OPT_ADAM, AGN_OPT_SGD,  # noqa: F401
                    AGN_DIST_NORMAL, AGN_DIST_UNIFORM, AGN_GEMM_AUTO, AGN_GEMM_SIMT,  # noqa: F401
-                   AGN_GEMM_TCGEN05, AGN_PREC_BF16, AGN_PREC_FP32, AGN_OK, AGN_E_INVALID,
+                   AGN_GEMM_TCGEN05, AGN_PREC_BF16, AGN_PREC_FP32, AGN_PREC_MX4, AGN_OK, AGN_E_INVALID,
                    AGN_E_SCHEDULE, AGN_E_OOM, AGN_E_CUDA, AGN_E_TIMEOUT, AGN_E_NONFINITE,
                    AGN_E_UNSUPPORTED, AGN_E_BOUNDS, agn_options)
 
@@ -26,7 +26,8 @@ __all__ = [
     "agn_last_run_stats", "agn_profile", "agn_kernel_stats", "agn_generate_inputs", "agn_export_inputs", "agn_last_error",
     "agn_destroy", "agn_make_schedule", "agn_plan_waves", "agn_commit_pull",
     "agn_commit_pull_noalloc",
-    "agn_fill_commit_inputs", "agn_debug_waits",
+    "agn_fill_commit_inputs", "agn_debug_waits", "agn_dropout", "agn_dropout_backward",
+    "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
     "library_path",
 ]
 
@@ -281,6 +282,64 @@ def agn_debug_waits(h, wait_ns, withhold_rank=-1):
 def agn_fill_commit_inputs(theta_c, acc, replicas, P, ld, n, seed, stream=None):
     _check(_L().agn_fill_commit_inputs(_ptr(theta_c), _ptr(acc), _ptr(replicas), int(P), int(ld),
                                        int(n), int(seed), _ptr(stream)))
+
+
+def _addr(x):
+    """A device pointer argument (a tensor or an int) as ctypes takes it."""
+    if x is None:
+        return None
+    return x.data_ptr() if hasattr(x, "data_ptr") else int(x)
+
+
+_U64 = (1 << 64) - 1
+
+
+def agn_dropout(x, y, dtype, rows, cols, p, seed, offset=0, bias=None, residual=None, relu=0,
+                ldx=None, ldr=None, ldy=None, stream=None):
+    """y = dropout(act(x + bias)) + residual on device buffers; row strides
+    default to cols.  The mask is a function of (p, seed, offset) and the
+    element's place (include/agn.h)."""
+    _check(_L().agn_dropout(_addr(x), _addr(bias), _addr(residual), _addr(y), dtype, bool(relu),
+                            rows, cols, cols if ldx is None else ldx, cols if ldr is None else ldr,
+                            cols if ldy is None else ldy, p, seed & _U64, offset & _U64,
+                            _addr(stream)))
+
+
+def agn_dropout_backward(dy, dx, dtype, rows, cols, p, seed, offset=0, x=None, bias=None,
+                         dbias=None, relu=0, lddy=None, ldx=None, lddx=None, stream=None):
+    """Gradient of agn_dropout with the same (p, seed, offset): dx, and dbias [cols]
+    (fp32) when given.  With relu, x and bias are the forward call's."""
+    _check(_L().agn_dropout_backward(_addr(dy), _addr(x), _addr(bias), _addr(dx), _addr(dbias),
+                                     dtype, bool(relu), rows, cols, cols if lddy is None else lddy,
+                                     cols if ldx is None else ldx, cols if lddx is None else lddx,
+                                     p, seed & _U64, offset & _U64, _addr(stream)))
+
+
+def agn_mx4_bytes(rows, cols):
+    """(bytes of the codes, bytes of the scales) of a [rows][cols] 4-bit matrix."""
+    c, s = C.c_int64(), C.c_int64()
+    _check(_L().agn_mx4_bytes(rows, cols, C.byref(c), C.byref(s)))
+    return c.value, s.value
+
+
+def agn_mx4_quantize(x, dtype, rows, cols, codes, scales, ldx=None, stream=None):
+    _check(_L().agn_mx4_quantize(_addr(x), dtype, rows, cols, cols if ldx is None else ldx,
+                                 _addr(codes), _addr(scales), _addr(stream)))
+
+
+def agn_mx4_dequantize(codes, scales, rows, cols, y, dtype, ldy=None, stream=None):
+    _check(_L().agn_mx4_dequantize(_addr(codes), _addr(scales), rows, cols, _addr(y), dtype,
+                                   cols if ldy is None else ldy, _addr(stream)))
+
+
+def agn_mx4_linear(x_codes, x_scales, w_codes, w_scales, rows, inner, out, y, dtype, bias=None,
+                   relu=0, ldy=None, y_scales=None, err=None, stream=None):
+    """y [rows][out] = act(x w^T + bias) on 4-bit x [rows][inner] and w [out][inner];
+    dtype AGN_PREC_MX4: y and y_scales receive 4-bit rows."""
+    _check(_L().agn_mx4_linear(_addr(x_codes), _addr(x_scales), _addr(w_codes), _addr(w_scales),
+                               _addr(bias), rows, inner, out, bool(relu), _addr(y), dtype,
+                               out if ldy is None else ldy, _addr(y_scales), _addr(err),
+                               _addr(stream)))
 
 
 class AGN:

@@ -27,6 +27,7 @@ AGN_E_BOUNDS = -8
 
 AGN_PREC_FP32 = 0
 AGN_PREC_BF16 = 1
+AGN_PREC_MX4 = 2
 AGN_DIST_UNIFORM = 0
 AGN_DIST_NORMAL = 1
 AGN_OPT_SGD = 0
@@ -75,6 +76,7 @@ class agn_options(C.Structure):
     ]
 
 
+_PTR = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _I64P = C.POINTER(C.c_int64)
 _F32P = C.POINTER(C.c_float)
@@ -115,6 +117,17 @@ SIGNATURES = {
                                           C.c_int64, C.c_int64, C.c_int32, C.c_int32, _I32P,
                                           _I32P, _I32P, C.c_double, C.c_int32, C.c_int32,
                                           C.c_void_p, C.c_void_p]),
+    "agn_dropout": (C.c_int, [_PTR] * 4 + [C.c_int32] * 2 + [C.c_int64] * 5 +
+                    [C.c_double, C.c_uint64, C.c_uint64, _PTR]),
+    "agn_dropout_backward": (C.c_int, [_PTR] * 5 + [C.c_int32] * 2 + [C.c_int64] * 5 +
+                             [C.c_double, C.c_uint64, C.c_uint64, _PTR]),
+    "agn_mx4_bytes": (C.c_int, [C.c_int64, C.c_int64, _I64P, _I64P]),
+    "agn_mx4_quantize": (C.c_int, [_PTR, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _PTR, _PTR,
+                                   _PTR]),
+    "agn_mx4_dequantize": (C.c_int, [_PTR, _PTR, C.c_int64, C.c_int64, _PTR, C.c_int32, C.c_int64,
+                                     _PTR]),
+    "agn_mx4_linear": (C.c_int, [_PTR] * 5 + [C.c_int64] * 3 + [C.c_int32, _PTR, C.c_int32,
+                                                                C.c_int64, _PTR, _PTR, _PTR]),
     "agn_debug_waits": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32]),
     "agn_fill_commit_inputs": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                          C.c_int64, C.c_int32, C.c_uint64, C.c_void_p]),

@@ -29,7 +29,8 @@ BUILD_CHECK = os.path.join(HERE, "_build_check")
 LIB_CHECK_PATH = os.path.join(BUILD_CHECK, "libagn_gb300_check.so")
 
 SOURCES = ["agn_api.cu", "commit_pull.cu", "commit_pull_noalloc.cu", "mlp_simt.cu", "mlp_head.cu",
-           "mlp_tc.cu", "mlp_tc_dw.cu", "mlp_eval.cu", "optim.cu", "host_inputs.cu"]
+           "mlp_tc.cu", "mlp_tc_dw.cu", "mlp_eval.cu", "optim.cu", "host_inputs.cu", "dropout.cu",
+           "mx4.cu", "mx4_linear.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr",
               "-Xcompiler", "-fPIC,-ffp-contract=off,-O3", "-I", INCLUDE]

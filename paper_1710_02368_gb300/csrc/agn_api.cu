@@ -80,6 +80,9 @@ AGN_BOUNDS_DECL(simt)
 AGN_BOUNDS_DECL(tc)
 AGN_BOUNDS_DECL(dw)
 AGN_BOUNDS_DECL(optim)
+AGN_BOUNDS_DECL(dropout)
+AGN_BOUNDS_DECL(mx4)
+AGN_BOUNDS_DECL(mx4_linear)
 #undef AGN_BOUNDS_DECL
 
 namespace {
@@ -133,7 +136,8 @@ Status bounds_upload(cudaStream_t st) {
   }
   using SetFn = cudaError_t (*)(const BoundsTable&, cudaStream_t);
   for (SetFn f : {bounds_set_commit, bounds_set_eval, bounds_set_head, bounds_set_simt,
-                  bounds_set_tc, bounds_set_dw, bounds_set_optim})
+                  bounds_set_tc, bounds_set_dw, bounds_set_optim, bounds_set_dropout,
+                  bounds_set_mx4, bounds_set_mx4_linear})
     AGN_TRY_CUDA(f(t, st));
   return Status::Ok();
 }
@@ -143,7 +147,8 @@ Status bounds_collect(cudaStream_t st) {
   unsigned long long first = 0;
   unsigned long long total = 0;
   for (GetFn f : {bounds_get_commit, bounds_get_eval, bounds_get_head, bounds_get_simt,
-                  bounds_get_tc, bounds_get_dw, bounds_get_optim}) {
+                  bounds_get_tc, bounds_get_dw, bounds_get_optim, bounds_get_dropout,
+                  bounds_get_mx4, bounds_get_mx4_linear}) {
     unsigned long long a = 0;
     unsigned int c = 0;
     AGN_TRY_CUDA(f(&a, &c, st));

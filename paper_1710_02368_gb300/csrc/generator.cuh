@@ -35,6 +35,7 @@ enum Stream : uint64_t {
   kCommitAcc = 5,
   kCommitTheta = 6,
   kCommitOrder = 7,
+  kDropout = 8,
 };
 
 AGN_HD uint64_t mix(uint64_t z) {

@@ -163,6 +163,28 @@ struct AdamArgs {
 };
 Status adam_step(const AdamArgs& a, int slots, int num_sms, cudaStream_t st);
 
+// Dropout of a hidden layer's activations (dropout.cu), in place: H [slots][m][d]
+// after its ReLU, with the mask that agn_dropout gives worker w's layer at its
+// step counter t (seed number w layers + layer of the handle's dropout stream,
+// offset t m ceil(d / 4)); fp32 T: also its three exact bf16 pieces, planes
+// `plane` apart (null: none).
+struct HiddenDropArgs {
+  void* H;
+  int m, d;
+  double p;
+  uint64_t seed;           // the handle's
+  const int* slot_worker;
+  const long long* slot_t0;
+  int step;                // t = slot_t0[slot] + step
+  int layers, layer;       // hidden layers, and which (from 0)
+  bf16* pieces;
+  int64_t plane;
+};
+template <typename T>
+Status dropout_hidden(const HiddenDropArgs& a, int slots, cudaStream_t st);
+// T = round(65536 p) and the kept values' scale 65536 / (65536 - T); false: p not in [0, 1).
+bool dropout_threshold(double p, uint32_t* t, float* scale);
+
 // Evaluation (mlp_eval.cu): per-sample loss / correctness / prediction of
 // fp32 logits Z [rows][C] against labels y, and their fixed-order means
 // (out[0] loss, out[1] accuracy).

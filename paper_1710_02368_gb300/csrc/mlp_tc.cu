@@ -1300,6 +1300,14 @@ Status make_tmap_f32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint
                 swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
+                       uint64_t row_stride, uint32_t box_rows) {
+  cuuint64_t dims[2] = {inner, rows};
+  cuuint64_t strides[1] = {row_stride};
+  cuuint32_t box[2] = {128, box_rows};
+  return encode(map, 2, base, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1);
+}
+
 // More than one round of one-tile CTAs on the SMs (full waves).
 bool full_wave(const TcArgs& args, int slots, int bn) {
   static const int sms = [] {

@@ -139,6 +139,9 @@ Status make_tmap_bf16_3d(CUtensorMap* map, const void* base, uint64_t inner, uin
 Status make_tmap_f32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                         uint64_t batch, uint64_t row_stride_elems, uint64_t batch_stride_elems,
                         uint32_t box_inner, uint32_t box_rows, bool swizzle128 = false);
+// Bytes in rows (inner and row_stride multiples of 16), boxes of 128 bytes, 128-byte swizzle.
+Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
+                       uint64_t row_stride, uint32_t box_rows);
 // 4D bf16 tensor map (inner, rows, batch, piece) over three piece planes.
 Status make_tmap_bf16_4d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                          uint64_t batch, uint64_t row_stride_elems, uint64_t batch_stride_elems,

@@ -1,0 +1,403 @@
+// Product of microscaled 4-bit matrices on the tensor cores: rows of x and rows
+// of w (both along K) quantised as in mx4.cu,
+//   y[r][f] = act(sum_k x[r][k] w[f][k] + b[f]),
+// tcgen05.mma kind::mxf4 (products of E2M1 values scaled by both blocks'
+// powers of two, f32 sums in TMEM), output fp32, bf16 or 4-bit codes again.
+//
+// The features are the MMA's M (128 TMEM lanes), the rows of x its N (BN
+// columns): few rows take narrow tiles that read each weight once, and a lane's
+// features are contiguous in every output row.  A stage is 256 k: 128-byte rows
+// of codes (TMA, 128-byte swizzle) and two scale tiles of 512 bytes (bulk copies;
+// the scales are stored as the tensor core wants them), copied to TMEM by the
+// thread that issues the MMAs.  K past the last element costs nothing: codes and
+// scales are zero there.  Few output tiles split K over a cluster: every CTA
+// leaves its sums in its shared memory, and each finishes a share of the columns,
+// adding the others' in rank order through distributed shared memory (no
+// workspace, no atomics, the same bits each time).
+// Every wait on an mbarrier is bounded (2 s): a tile that gives up is stored as
+// NaN and sets *err.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "mlp.cuh"
+#include "mlp_tc.cuh"
+#include "mx4.cuh"
+#include "ops.cuh"
+#include "tc_ptx.cuh"
+
+namespace agn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr int kABytes = 128 * 128;
+constexpr int kSfBytes = 2 * kMxTileBytes; // a stage's scales of 128 rows
+constexpr int kMaxSplit = 8;               // portable cluster size
+
+template <int BN>
+struct Tile {
+  static constexpr int kBBytes = BN * 128;
+  static constexpr int kSfTiles = BN > 128 ? 2 : 1;   // 128-row scale tiles of the rows of x
+  static constexpr int kStageBytes = kABytes + kBBytes + kSfBytes * (1 + kSfTiles);
+  static constexpr int kStages = BN <= 32 ? 8 : BN == 64 ? 7 : BN == 128 ? 6 : 4;
+  static constexpr uint32_t kSfCol = BN < 32 ? 32 : BN;   // first TMEM column of the scales
+  static constexpr uint32_t kCols = kSfCol + 8 + 8 * kSfTiles;
+  static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + 256;
+  static_assert(kStageBytes % 1024 == 0, "tiles of the 128-byte swizzle");
+  static_assert(kSmem <= 232448, "shared memory");
+  static_assert(BN * 128 * 4 <= kStages * kStageBytes, "the sums fit into the ring");
+};
+
+struct LinearArgs {
+  const uint8_t *w_scales, *x_scales;
+  int64_t rows, out;
+  int64_t tiles_k;          // scale tiles along K
+  int64_t row_tiles;        // 128-row scale tiles of x
+  int k_steps;              // ceil(in / 64)
+  int split;                // CTAs of a cluster, along K
+  const float* bias;
+  int relu, dtype, vec;     // vec: four features of a row are one aligned store
+  void* y;
+  int64_t ldy;
+  uint8_t* y_scales;
+  int64_t y_tiles_k;
+  int* err;
+};
+
+__device__ __forceinline__ float4 ld_cluster4(const float* p, uint32_t rank) {
+  const uint32_t own = tc::smem_u32(p);
+  uint32_t at;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+// Four features f .. f + 3 (n of them exist) of row r: bias, ReLU, store.  A warp
+// calls it for one row, lane by lane along 128 features: in the 4-bit form
+// eight lanes are a block and the warp's four scales one word.
+__device__ __forceinline__ void finish(const LinearArgs& a, int64_t r, int64_t f, int n,
+                                       const float (&b)[4], float4 s) {
+  float v[4] = {s.x + b[0], s.y + b[1], s.z + b[2], s.w + b[3]};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (a.relu && v[e] <= 0.f) v[e] = 0.f;
+  if (a.dtype == AGN_PREC_MX4) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= n) v[e] = 0.f;
+      amax = max(amax, __float_as_uint(v[e]) & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const uint32_t code = mx_scale_code(amax);
+    const float inv = mx_inverse(code);
+    uint32_t q = code == 255 ? 0u
+                             : mx_pair(v[0] * inv, v[1] * inv) | mx_pair(v[2] * inv, v[3] * inv) << 8;
+    const uint32_t hi = __shfl_down_sync(0xffffffffu, q, 1);
+    const int lane = threadIdx.x & 31;
+    const int64_t row_bytes = mx_row_bytes(a.out);
+    if ((lane & 1) == 0 && f / 2 < row_bytes)
+      AGN_ST(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.y) + r * row_bytes + f / 2),
+             q | hi << 16);
+    uint32_t word = code << (8 * (lane >> 3));
+    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+    word |= __shfl_xor_sync(0xffffffffu, word, 16);
+    if (lane == 0)
+      AGN_ST(reinterpret_cast<uint32_t*>(a.y_scales + mx_scale_at(r, f / kMxBlock, a.y_tiles_k)),
+             word);
+  } else if (a.dtype == AGN_PREC_BF16) {
+    bf16* p = static_cast<bf16*>(a.y) + r * a.ldy + f;
+    if (a.vec && n == 4) {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+      AGN_ST(reinterpret_cast<uint2*>(p), make_uint2(*reinterpret_cast<const uint32_t*>(&lo),
+                                                     *reinterpret_cast<const uint32_t*>(&hi)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < n) AGN_ST(p + e, __float2bfloat16_rn(v[e]));
+    }
+  } else {
+    float* p = static_cast<float*>(a.y) + r * a.ldy + f;
+    if (a.vec && n == 4) {
+      AGN_ST(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < n) AGN_ST(p + e, v[e]);
+    }
+  }
+}
+
+// One bulk copy (or, in the bounds-checked build, its bytes alone).
+__device__ __forceinline__ void load_scales(void* dst, const uint8_t* src, uint32_t bytes,
+                                            uint64_t* bar) {
+  if (AGN_BOUNDS_OK(src, bytes)) {
+    tc::bulk_load(dst, src, bytes, bar);
+  } else {
+    AGN_BOUNDS_FAIL(src);
+    tc::mbar_complete_tx(bar, bytes);
+  }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kThreads, 1)
+mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+                  const LinearArgs a) {
+  using Cfg = Tile<BN>;
+  constexpr int kStages = Cfg::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * Cfg::kStageBytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* done = empty + kStages;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t f0 = (int64_t)blockIdx.x * 128, n0 = (int64_t)blockIdx.y * BN;
+  const int rank = blockIdx.z;
+  const int KT_all = (a.k_steps + 3) / 4, kt_per = (KT_all + a.split - 1) / a.split;
+  const int kt0 = rank * kt_per, KT = min(KT_all, kt0 + kt_per) - kt0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    tc::mbar_init(done, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+    tc::tma_prefetch_desc(&tmW);
+    tc::tma_prefetch_desc(&tmX);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tmem_holder, Cfg::kTmemCols);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  pdl_begin();
+
+  if (warp == 0 && lane == 0) {
+    const int64_t xt0 = n0 >> 7;   // first 128-row scale tile of x
+    const int xt = (int)min((int64_t)Cfg::kSfTiles, a.row_tiles - xt0);
+    int kt = 0;
+    for (; kt < KT; ++kt) {
+      const int s = kt % kStages;
+      if (kt >= kStages && !tc::wait_or_abort(&empty[s], ((kt / kStages) - 1) & 1, abort_flag, kWaitNs)) {
+        *abort_flag = 1;
+        break;
+      }
+      if (*abort_flag) break;
+      uint8_t* st = smem + s * Cfg::kStageBytes;
+      uint8_t* sf = st + kABytes + Cfg::kBBytes;
+      const int kg = kt0 + kt;   // stage along the whole K
+      const uint32_t sfb = (uint32_t)min((int64_t)2, a.tiles_k - 2 * kg) * kMxTileBytes;
+      tc::mbar_arrive_expect_tx(&full[s], kABytes + Cfg::kBBytes + sfb * (1 + xt));
+      tc::tma_load_2d(st, &tmW, &full[s], kg * 128, (int)f0);
+      tc::tma_load_2d(st + kABytes, &tmX, &full[s], kg * 128, (int)n0);
+      load_scales(sf, a.w_scales + ((int64_t)blockIdx.x * a.tiles_k + 2 * kg) * kMxTileBytes, sfb,
+                  &full[s]);
+      for (int t = 0; t < xt; ++t)
+        load_scales(sf + kSfBytes * (1 + t),
+                    a.x_scales + ((xt0 + t) * a.tiles_k + 2 * kg) * kMxTileBytes, sfb, &full[s]);
+    }
+    if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
+      for (int j = kt - 1; j >= 0 && j >= kt - kStages; --j)
+        tc::mbar_wait_bounded(&full[j % kStages], (j / kStages) & 1, kWaitNs);
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t sfa = tmem + Cfg::kSfCol, sfb = sfa + 8;
+    const uint32_t shift = (uint32_t)(n0 & 127) / 32;   // BN = 64: the tile's half of 128 rows
+    for (int kt = 0; kt < KT; ++kt) {
+      const int s = kt % kStages;
+      if (!tc::wait_or_abort(&full[s], (kt / kStages) & 1, abort_flag, kWaitNs)) {
+        *abort_flag = 1;
+        break;
+      }
+      tc::tc_fence_after();
+      const uint32_t sa = tc::smem_u32(smem + s * Cfg::kStageBytes), sb = sa + kABytes;
+      const uint32_t ss = sb + Cfg::kBBytes;
+      const int steps = min(4, a.k_steps - 4 * (kt0 + kt));
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {   // scale words: blocks 4 q .. 4 q + 3 of the stage
+        if (2 * q >= steps) break;
+        tc::cp_32x128b_warpx4(sfa + 4 * q, tc::smem_desc_rows16(ss + q * kMxTileBytes, 128));
+#pragma unroll
+        for (int t = 0; t < Cfg::kSfTiles; ++t)
+          tc::cp_32x128b_warpx4(sfb + 4 * (Cfg::kSfTiles * q + t),
+                                tc::smem_desc_rows16(ss + kSfBytes * (1 + t) + q * kMxTileBytes, 128));
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        if (kk >= steps) break;
+        const int q = kk >> 1;
+        tc::mma_mxf4(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
+                     tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
+                     (kk & 1) ? tc::idesc_mxf4(128, BN, 2) : tc::idesc_mxf4(128, BN, 0),
+                     sfa + 4 * q, sfb + 4 * Cfg::kSfTiles * q + shift, (kt | kk) != 0);
+      }
+      tc::mma_commit(&empty[s]);
+    }
+    tc::mma_commit(done);
+  }
+  __syncwarp();
+  const bool ok =
+      __syncthreads_and(tc::wait_or_abort(done, 0, abort_flag, kWaitNs) && !*abort_flag) != 0;
+  tc::tc_fence_after();
+  if (!ok && threadIdx.x == 0 && a.err) atomicExch(a.err, 1);
+
+  // the sums to shared memory (the ring is free): [column][128 features]
+  float* sums = reinterpret_cast<float*>(smem);
+  {
+    constexpr int kPer = BN == 16 ? 16 : BN / 2;   // columns of this warp
+    const int g = warp & 3, c0 = (warp >> 2) * kPer;
+    if (c0 < BN) {
+#pragma unroll 1
+      for (int c = c0; c < c0 + kPer; c += 16) {
+        uint32_t r[16];
+        tc::tmem_ld_32x32b_x16(tmem + ((uint32_t)(32 * g) << 16) + (uint32_t)c, r);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sums[(c + i) * 128 + 32 * g + lane] = ok ? __uint_as_float(r[i]) : NAN;
+      }
+    }
+  }
+  tc::tc_fence_before();
+  if (a.split > 1) cluster_sync();
+  else __syncthreads();
+  if (warp == 1) tc::tmem_dealloc(tmem, Cfg::kTmemCols);
+
+  // finish this CTA's columns: a warp a row of y, a lane four features
+  {
+    const int64_t f = f0 + 4 * lane;
+    const int n = (int)max((int64_t)0, min((int64_t)4, a.out - f));
+    float b[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = a.bias && e < n ? AGN_LD(a.bias + f + e) : 0.f;
+    const int own1 = BN * (rank + 1) / a.split;
+    for (int j = BN * rank / a.split + warp; j < own1; j += kThreads / 32) {
+      if (n0 + j >= a.rows) break;   // (warp-uniform)
+      const float* p = sums + j * 128 + 4 * lane;
+      float4 s;
+      if (a.split == 1) {
+        s = *reinterpret_cast<const float4*>(p);
+      } else {
+        s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < a.split; ++k) {
+          const float4 t = ld_cluster4(p, k);
+          s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+        }
+      }
+      finish(a, n0 + j, f, n, b, s);
+    }
+  }
+  if (a.split > 1) cluster_sync();   // the others' reads, before this CTA's memory goes
+}
+
+template <int BN>
+Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
+  CUtensorMap tw, tx;
+  AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, mx_row_bytes(m.in), m.out, mx_row_bytes(m.in), 128));
+  AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, mx_row_bytes(m.in), m.rows, mx_row_bytes(m.in), BN));
+  auto kern = mx4_linear_kernel<BN>;
+  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)Tile<BN>::kSmem));
+  const dim3 grid((unsigned)ceil_div(m.out, 128), (unsigned)ceil_div(m.rows, BN), (unsigned)a.split);
+  if (a.split > 1)
+    AGN_TRY_CUDA(launch_pdl_cluster(kern, grid, kThreads, Tile<BN>::kSmem,
+                                    dim3(1, 1, (unsigned)a.split), st, tw, tx, a));
+  else
+    AGN_TRY_CUDA(launch_pdl(kern, grid, kThreads, Tile<BN>::kSmem, st, tw, tx, a));
+  AGN_TRY_CUDA(cudaGetLastError());
+  return Status::Ok();
+}
+
+}  // namespace
+
+Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
+  const size_t es = m.dtype == AGN_PREC_MX4 ? 1 : dtype_size(m.dtype);
+  if (!es) return Status::Err(AGN_E_INVALID, "unknown dtype");
+  if (m.rows < 0 || m.in < 1 || m.out < 1 || m.rows > INT32_MAX - 256 || m.in > INT32_MAX - 256 ||
+      m.out > INT32_MAX - 256)
+    return Status::Err(AGN_E_INVALID, "need rows >= 0, in >= 1, out >= 1, below 2^31");
+  if (m.dtype != AGN_PREC_MX4) AGN_TRY(check_matrix("y", m.rows, m.out, m.ldy));
+  if (m.rows == 0) return Status::Ok();
+  if (!m.x_codes || !m.x_scales || !m.w_codes || !m.w_scales || !m.y ||
+      (m.dtype == AGN_PREC_MX4 && !m.y_scales))
+    return Status::Err(AGN_E_INVALID, "null pointer");
+  if (ceil_div(m.rows, 256) > 65535)
+    return Status::Err(AGN_E_UNSUPPORTED, "more than 16776960 rows");
+  const bool mx = m.dtype == AGN_PREC_MX4;
+  const CallBuffer xc{"x codes", m.x_codes, (size_t)mx_code_bytes(m.rows, m.in), 16},
+      xs{"x scales", m.x_scales, (size_t)mx_scale_bytes(m.rows, m.in), 16},
+      wc{"w codes", m.w_codes, (size_t)mx_code_bytes(m.out, m.in), 16},
+      ws{"w scales", m.w_scales, (size_t)mx_scale_bytes(m.out, m.in), 16},
+      bb{"bias", m.bias, m.bias ? (size_t)m.out * 4 : 0, 4},
+      y{"y", m.y, mx ? (size_t)mx_code_bytes(m.rows, m.out) : matrix_bytes(m.rows, m.out, m.ldy, es),
+        mx ? 16 : es},
+      ys{"y scales", mx ? m.y_scales : nullptr, mx ? (size_t)mx_scale_bytes(m.rows, m.out) : 0, 16},
+      er{"err", m.err, m.err ? sizeof(int) : 0, 4};
+  AGN_TRY(check_apart(y, {xc, xs, wc, ws, bb, ys, er}));
+  AGN_TRY(check_apart(ys, {xc, xs, wc, ws, bb, er}));
+  AGN_TRY(check_apart(er, {xc, xs, wc, ws, bb}));
+  AGN_TRY(check_buffers({xc, xs, wc, ws, bb, y, ys, er}));
+  LinearArgs a{};
+  a.w_scales = static_cast<const uint8_t*>(m.w_scales);
+  a.x_scales = static_cast<const uint8_t*>(m.x_scales);
+  a.rows = m.rows; a.out = m.out;
+  a.tiles_k = mx_tiles_k(m.in);
+  a.row_tiles = ceil_div(m.rows, kMxTileRows);
+  a.k_steps = (int)ceil_div(m.in, 64);
+  a.bias = m.bias;
+  a.relu = m.relu != 0; a.dtype = m.dtype;
+  a.y = m.y; a.ldy = m.ldy;
+  a.y_scales = static_cast<uint8_t*>(m.y_scales);
+  a.y_tiles_k = mx_tiles_k(m.out);
+  a.err = m.err;
+  a.vec = !mx && reinterpret_cast<uintptr_t>(m.y) % (4 * es) == 0 && m.ldy % 4 == 0;
+  const int bn = m.rows <= 16 ? 16 : m.rows <= 32 ? 32 : m.rows <= 64 ? 64 : m.rows <= 1024 ? 128 : 256;
+  const int64_t tiles = ceil_div(m.out, 128) * ceil_div(m.rows, bn);
+  const int kt = (a.k_steps + 3) / 4;
+  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, kt, current_sms() / tiles}));
+  a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
+  KnownBuffers known({xc, xs, wc, ws, bb, y, ys, er});
+  AGN_TRY(bounds_upload(st));
+  switch (bn) {
+    case 16: AGN_TRY(launch_linear<16>(m, a, st)); break;
+    case 32: AGN_TRY(launch_linear<32>(m, a, st)); break;
+    case 64: AGN_TRY(launch_linear<64>(m, a, st)); break;
+    case 128: AGN_TRY(launch_linear<128>(m, a, st)); break;
+    default: AGN_TRY(launch_linear<256>(m, a, st)); break;
+  }
+  return bounds_collect(st);
+}
+
+AGN_BOUNDS_UNIT(mx4_linear)
+
+}  // namespace agn
+
+extern "C" int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_codes,
+                              const void* w_scales, const float* bias, int64_t rows, int64_t in,
+                              int64_t out, int32_t relu, void* y, int32_t dtype, int64_t ldy,
+                              void* y_scales, int32_t* err, void* stream) {
+  return agn::guarded([&] {
+    agn::Mx4LinearArgs m{};
+    m.x_codes = x_codes; m.x_scales = x_scales;
+    m.w_codes = w_codes; m.w_scales = w_scales;
+    m.bias = bias;
+    m.rows = rows; m.in = in; m.out = out;
+    m.relu = relu;
+    m.y = y; m.dtype = dtype; m.ldy = ldy; m.y_scales = y_scales;
+    m.err = err;
+    return agn::mx4_linear(m, static_cast<cudaStream_t>(stream));
+  });
+}

@@ -87,6 +87,14 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity,
 __device__ __forceinline__ void tma_prefetch_desc(const void* tmap) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
 }
+__device__ __forceinline__ void tma_load_2d(void* dst, const void* tmap, uint64_t* bar, int x,
+                                            int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y)
+      : "memory");
+}
 __device__ __forceinline__ void tma_load_3d(void* dst, const void* tmap, uint64_t* bar, int x,
                                             int y, int z) {
   asm volatile(
@@ -211,6 +219,29 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// D[tmem] (+)= (A scaled) (B scaled)^T, kind::mxf4: E2M1 operands in shared memory
+// (K = 64, two to a byte), one E8M0 scale for 32 along K.  The scales lie in
+// TMEM: a 32-bit column holds four consecutive blocks of a row, row r of 128 in
+// lane r mod 32 (the same in all four lane quadrants) and column r / 32;
+// the instruction descriptor says which two of the four (idesc_mxf4).
+__device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                         uint32_t idesc, uint32_t sfa_tmem, uint32_t sfb_tmem,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
+      "[%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes (rows contiguous) from shared memory to TMEM lanes 0-31,
+// four 32-bit columns, and the same to lanes 32-63, 64-95 and 96-127.  Ordered
+// before later MMAs of the issuing thread.
+__device__ __forceinline__ void cp_32x128b_warpx4(uint32_t taddr, uint64_t s_desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(s_desc)
+               : "memory");
+}
 // Arrive on `bar` once every tcgen05.mma issued so far by this thread completes.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile(
@@ -294,6 +325,24 @@ __device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t saddr, uint32_t lbo_
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)4 << 61;
   return d;
+}
+
+// No swizzle: rows of 16 bytes in groups of eight, sbo_bytes from group to group.
+__device__ __forceinline__ uint64_t smem_desc_rows16(uint32_t saddr, uint32_t sbo_bytes) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+  d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32;
+  d |= (uint64_t)1 << 46;
+  return d;
+}
+
+// Instruction descriptor of kind::mxf4 with E2M1 A and B (K-major), f32 D, E8M0
+// scales: B's scale id bits 4-5, A format (1 = E2M1) bits 7-9, B format bits 10-12,
+// N >> 3 in 17-22, scale format (1 = E8M0) bit 23, M >> 4 in 24-28, A's scale id
+// bits 29-30 (0 or 2: the first or the last two blocks of a scale word).
+__host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int scale_id) {
+  return ((uint32_t)scale_id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) |
+         (1u << 23) | ((uint32_t)(M >> 4) << 24) | ((uint32_t)scale_id << 29);
 }
 
 // Instruction descriptor of kind::f16 with bf16 A and B, f32 D, dense:
