@@ -149,6 +149,18 @@ typedef struct agn_options {
      tc_mask bit 3. */
   int32_t local_optimizer;
   float adam_beta1, adam_beta2, adam_eps;
+  /* Dropout of every hidden layer's activations while training (after the ReLU;
+     inverted: kept values are scaled, evaluation uses all of them), with
+     probability dropout in [0, 1), 0 = none.  The mask of hidden layer l
+     (1 .. L - 1) of worker w at its step counter t (never reset) is that of
+     agn_dropout on the minibatch's [batch][d_l] activations with the seed
+     number w (L - 1) + l - 1 of stream 8 of the handle's seed and the offset
+     t batch ceil(d_l / 4).  The losses are those of the masked net.  One more launch a
+     hidden layer and local step, and the output layer is a launch of its own. */
+  double dropout;
+  /* 1: keep the held-out rows in microscaled 4 bits too, for agn_evaluate_mx4
+     (needs n_eval and a hidden layer). */
+  int32_t eval_mx4;
 } agn_options;
 
 void agn_default_options(agn_options* opt);
@@ -229,6 +241,18 @@ int agn_loss(agn_handle* h, float* out, int64_t cap);
 int agn_evaluate(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int64_t cap);
 
 /*
+ * agn_evaluate with the hidden layers on microscaled 4-bit operands: what theta~
+ * answers when it is served that way (no counterpart in the paper).  The call quantises each
+ * hidden layer's weights (agn_mx4_quantize); the rows, in 4 bits since
+ * agn_create, pass through agn_mx4_linear layer by layer with bias and ReLU, each
+ * hidden layer's output in 4 bits again, the last one's in fp32; the output
+ * layer, the loss and the predictions are fp32 as in agn_evaluate.  Needs a
+ * handle created with eval_mx4 (else AGN_E_INVALID); arguments and other errors
+ * as agn_evaluate.
+ */
+int agn_evaluate_mx4(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int64_t cap);
+
+/*
  * Temporal efficiency, Eq. 4: E(a, b) = int_0^m f_a dt / int_0^m f_b dt with m
  * the shorter of the two curves' end times.  Curve x is sampled at times
  * tx[0..nx) (non-decreasing, >= 0) with values fx; it is the piecewise-linear
@@ -280,7 +304,7 @@ int agn_generate_inputs(const int32_t* dims, int32_t n_dims, int32_t input_dist,
 #define AGN_K_BACKWARD_DW 4  /* dW GEMM + local step + accumulation              */
 #define AGN_K_COMMIT 5       /* fused commit + pull                              */
 #define AGN_K_NORMS 6        /* per-commit norm reduction                        */
-#define AGN_K_OTHER 7        /* pulls outside commits, loss means                */
+#define AGN_K_OTHER 7        /* pulls outside commits, loss means, dropout       */
 #define AGN_K_FORWARD_HEAD 8 /* the last hidden layer's forward GEMM with the
                                 output layer in its epilogue (forward,
                                 softmax-CE, dX of the last hidden layer)         */

@@ -27,7 +27,7 @@ __all__ = [
     "agn_destroy", "agn_make_schedule", "agn_plan_waves", "agn_commit_pull",
     "agn_commit_pull_noalloc",
     "agn_fill_commit_inputs", "agn_debug_waits", "agn_dropout", "agn_dropout_backward",
-    "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
+    "agn_evaluate_mx4", "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
     "library_path",
 ]
 
@@ -125,17 +125,27 @@ def agn_delta_norm(h) -> np.ndarray:
     return _read_commits(_L().agn_delta_norm, h)
 
 
-def agn_evaluate(h, pred=None):
-    """(loss, accuracy) of theta~ on the handle's held-out set; `pred`, an int32
-    array of n_eval entries, also receives the predictions."""
+def _evaluate(fn, h, pred):
     loss, acc = C.c_float(), C.c_float()
     pp, cap = None, 0
     if pred is not None:
         if pred.dtype != np.int32 or not pred.flags.c_contiguous:
             raise ValueError("pred must be a contiguous int32 array")
         pp, cap = pred.ctypes.data_as(_lib._I32P), len(pred)
-    _check(_L().agn_evaluate(h, C.byref(loss), C.byref(acc), pp, cap), h)
+    _check(fn(h, C.byref(loss), C.byref(acc), pp, cap), h)
     return loss.value, acc.value
+
+
+def agn_evaluate(h, pred=None):
+    """(loss, accuracy) of theta~ on the handle's held-out set; `pred`, an int32
+    array of n_eval entries, also receives the predictions."""
+    return _evaluate(_L().agn_evaluate, h, pred)
+
+
+def agn_evaluate_mx4(h, pred=None):
+    """agn_evaluate with the hidden layers on microscaled 4-bit operands (a handle
+    created with eval_mx4)."""
+    return _evaluate(_L().agn_evaluate_mx4, h, pred)
 
 
 def agn_temporal_efficiency(ta, fa, tb, fb) -> float:
@@ -349,7 +359,8 @@ class AGN:
                  n_samples=2048, input_dist=AGN_DIST_UNIFORM, teacher_dims=None, normalize=1,
                  gemm=AGN_GEMM_AUTO, tau_lo=0, tau_hi=0, stream=None, x=None, y=None,
                  theta0=None, tc_mask=0, commit_rule=AGN_COMMIT_AGN, elide_accumulator=0,
-                 n_eval=0, local_optimizer=AGN_OPT_SGD, adam=(0.0, 0.0, 0.0)):
+                 n_eval=0, local_optimizer=AGN_OPT_SGD, adam=(0.0, 0.0, 0.0), dropout=0.0,
+                 eval_mx4=0):
         o = agn_default_options()
         o.precision, o.batch, o.n_samples = int(precision), int(batch), int(n_samples)
         o.input_dist, o.normalize, o.gemm = int(input_dist), int(normalize), int(gemm)
@@ -360,6 +371,8 @@ class AGN:
         o.n_eval = int(n_eval)
         o.local_optimizer = int(local_optimizer)
         o.adam_beta1, o.adam_beta2, o.adam_eps = (float(x) for x in adam)
+        o.dropout = float(dropout)
+        o.eval_mx4 = int(eval_mx4)
         self.n_eval = int(n_eval)
         keep = []
         if teacher_dims is not None:
@@ -381,10 +394,17 @@ class AGN:
 
     def evaluate(self, with_pred=False):
         """(loss, accuracy[, predictions]) of theta~ on the held-out set."""
+        return self._evaluate(agn_evaluate, with_pred)
+
+    def evaluate_mx4(self, with_pred=False):
+        """The same with the hidden layers in microscaled 4 bits (eval_mx4)."""
+        return self._evaluate(agn_evaluate_mx4, with_pred)
+
+    def _evaluate(self, fn, with_pred):
         if not with_pred:
-            return agn_evaluate(self.h)
+            return fn(self.h)
         pred = np.empty(self.n_eval, dtype=np.int32)
-        loss, acc = agn_evaluate(self.h, pred)
+        loss, acc = fn(self.h, pred)
         return loss, acc, pred
 
     def run(self, n_commits, worker=None, staleness=None):

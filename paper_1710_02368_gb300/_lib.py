@@ -73,6 +73,8 @@ class agn_options(C.Structure):
         ("adam_beta1", C.c_float),
         ("adam_beta2", C.c_float),
         ("adam_eps", C.c_float),
+        ("dropout", C.c_double),
+        ("eval_mx4", C.c_int32),
     ]
 
 
@@ -93,6 +95,7 @@ SIGNATURES = {
     "agn_loss": (C.c_int, [C.c_void_p, _F32P, C.c_int64]),
     "agn_delta_norm": (C.c_int, [C.c_void_p, _F32P, C.c_int64]),
     "agn_evaluate": (C.c_int, [C.c_void_p, _F32P, _F32P, _I32P, C.c_int64]),
+    "agn_evaluate_mx4": (C.c_int, [C.c_void_p, _F32P, _F32P, _I32P, C.c_int64]),
     "agn_temporal_efficiency": (C.c_int, [_F64P, _F64P, C.c_int64, _F64P, _F64P, C.c_int64,
                                           _F64P]),
     "agn_num_params": (C.c_int64, [C.c_void_p]),

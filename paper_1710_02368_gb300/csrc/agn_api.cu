@@ -30,6 +30,7 @@
 #include "last_pulls.h"
 #include "mlp.cuh"
 #include "mlp_tc.cuh"
+#include "mx4.cuh"
 
 using agn::bf16;
 using agn::CommitPlan;
@@ -178,6 +179,9 @@ struct agn_handle {
   bool elide = false;
   // Adam as the local optimizer: raw gradients go to grad, the moments m, v
   // persist per worker, the accumulator (if kept) sums the steps
+  // dropout of the hidden layers (0: none) and the scale of what it keeps
+  double dropout = 0.0;
+  float drop_scale = 1.f;
   bool adam = false;
   float beta1 = 0.9f, beta2 = 0.999f, eps = 1e-8f;
   float* grad = nullptr;      // [n][P_pad]
@@ -201,6 +205,15 @@ struct agn_handle {
   };
   std::vector<EvalMaps> emaps;
   float* Ze = nullptr;        // [eval_chunk][d_L]
+  // agn_evaluate_mx4: the rows, the hidden layers' weights and a chunk's
+  // activations in microscaled 4 bits
+  struct Mx4 {
+    uint8_t* codes = nullptr;
+    uint8_t* scales = nullptr;
+  };
+  bool eval_mx4 = false;
+  Mx4 xe4, h4[2];
+  std::vector<Mx4> w4;
   float* e_loss = nullptr;    // [n_eval]
   int* e_correct = nullptr;   // [n_eval]
   int* e_pred = nullptr;      // [n_eval]
@@ -761,6 +774,7 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
         a.dH = L > 1 ? dZl(L - 1) : nullptr;
         a.dH_pieces = L > 1 ? dz_pieces(L - 1) : nullptr;
         a.dH_plane = L > 1 ? dz_plane(L - 1) : 0;
+        a.mask_scale = h->drop_scale;
         a.ce_partial = h->ce_partial; a.counter = h->head_counter;
         a.loss_parts = h->loss_parts; a.loss_q = h->loss_q; a.slot_commit = sc; a.lam = h->lam; a.step = i;
         a.flag = h->flag;
@@ -786,6 +800,7 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
       bf16* h_pieces =
           (h->split && (l + 1 < L || (h->fuse_out_dw && l + 1 == L))) ? h->Hs[l] : nullptr;
       bool pieces_done = false;
+      const bool drop = l < L && h->dropout > 0.0;   // (then the head is not fused)
       const bool fuse = fuse_head_now && l == L - 1;
       {
         // with the output layer fused: its forward and dX flops, W_L, dZ_L
@@ -845,7 +860,7 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
           t.ldo = fo; t.out_bstride = (int64_t)m * fo;
           t.theta = bias_base; t.ld_param = bias_ld;
           t.relu = 1; t.boff = bias_off(l);
-          t.out_pieces = h_pieces; t.out_plane = (int64_t)n * m * fo;
+          t.out_pieces = drop ? nullptr : h_pieces; t.out_plane = (int64_t)n * m * fo;
           const auto& mp = maps_of(l);
           t.x_b_direct = l == 1;
           t.no_a_prefetch = l == 1 && (h->tc_mask & 512) ? 1 : 0;
@@ -858,6 +873,18 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
         } else {
           AGN_TRY(agn::simt_forward<T>(g, l == L, s, h->stream));
         }
+      }
+      if (drop) {   // in place, with the pieces that the next GEMMs read
+        const int64_t count = (int64_t)s * m * fo;
+        Launch k(h, AGN_K_OTHER, 0.0, (double)count * (2.0 * es + (h_pieces ? 6.0 : 0.0)), launches);
+        agn::HiddenDropArgs d{};
+        d.H = Hl(l); d.m = m; d.d = fo;
+        d.p = h->dropout; d.seed = h->seed;
+        d.slot_worker = sw; d.slot_t0 = st0; d.step = i;
+        d.layers = L - 1; d.layer = l - 1;
+        d.pieces = h_pieces; d.plane = (int64_t)n * m * fo;
+        AGN_TRY(agn::dropout_hidden<T>(d, s, h->stream));
+        pieces_done = true;
       }
       if (h_pieces && !pieces_done) AGN_TRY(split_act(h, Hl(l), h_pieces, fo, s, launches));
     }
@@ -898,7 +925,7 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
         t.M = fi; t.N = m; t.K = fo;
         t.a_by_worker = 1;
         t.out = dZl(l - 1); t.ldo = fi; t.out_bstride = (int64_t)m * fi;
-        t.mask = Hprev; t.mask_bstride = (int64_t)m * fi;
+        t.mask = Hprev; t.mask_bstride = (int64_t)m * fi; t.mask_scale = h->drop_scale;
         t.out_pieces = next_pieces; t.out_plane = dz_plane(l - 1);
         const auto& mp = maps_of(l);
         const int bn = tc_bn(h, h->split, fi, m, s);
@@ -913,7 +940,7 @@ Status run_wave_steps(agn_handle* h, const Wave& wv, int64_t* launches) {
         g.b = W + h->woff[l - 1]; g.ldb = fi; g.b_bstride = h->P_pad; g.b_by_worker = 1;
         g.slot_worker = sw;
         g.out = dZl(l - 1); g.ldo = fi; g.out_bstride = (int64_t)m * fi;
-        g.mask = Hprev; g.mask_bstride = (int64_t)m * fi;
+        g.mask = Hprev; g.mask_bstride = (int64_t)m * fi; g.mask_scale = h->drop_scale;
         g.theta = h->rep; g.ld_param = h->P_pad;
         AGN_TRY(agn::simt_backward_dx<T>(g, s, h->stream));
       }
@@ -1410,6 +1437,14 @@ Status create(agn_handle* h, const int32_t* dims, int32_t n_dims, int32_t n_work
   if (o.elide_accumulator && (o.tc_mask & 8))
     return Status::Err(AGN_E_UNSUPPORTED,
                        "the one-tile-per-CTA dW kernel (tc_mask bit 3) keeps the accumulator");
+  uint32_t drop_t = 0;
+  float drop_scale = 1.f;
+  if (!agn::dropout_threshold(o.dropout, &drop_t, &drop_scale))
+    return Status::Err(AGN_E_INVALID, "dropout must be in [0, 1)");
+  if (o.eval_mx4 && o.n_eval == 0)
+    return Status::Err(AGN_E_INVALID, "eval_mx4 needs an evaluation set (n_eval)");
+  if (o.eval_mx4 && n_dims < 3)
+    return Status::Err(AGN_E_UNSUPPORTED, "eval_mx4 needs a hidden layer");
   h->dims.assign(dims, dims + n_dims);
   h->L = n_dims - 1;
   h->n = n_workers;
@@ -1424,6 +1459,8 @@ Status create(agn_handle* h, const int32_t* dims, int32_t n_dims, int32_t n_work
   h->normalize = o.normalize ? 1 : 0;
   h->commit_rule = o.commit_rule;
   h->elide = o.elide_accumulator != 0;
+  h->dropout = o.dropout;
+  h->drop_scale = drop_scale;
   h->adam = o.local_optimizer == AGN_OPT_ADAM;
   if (o.adam_beta1 > 0.f) h->beta1 = o.adam_beta1;
   if (o.adam_beta2 > 0.f) h->beta2 = o.adam_beta2;
@@ -1543,7 +1580,8 @@ Status create(agn_handle* h, const int32_t* dims, int32_t n_dims, int32_t n_work
                  !h->elide && agn::commit_low_pulls(h->P_pad);
   h->ldz_out = h->fuse_out_dw ? (int)round_up(dims[h->L], 8) : dims[h->L];
   h->fuse_head = h->use_tc && h->use_head && (h->tc_mask & 1) &&
-                 !(h->tc_mask & 32) && dims[h->L] <= agn::kHeadMaxClasses;
+                 !(h->tc_mask & 32) && dims[h->L] <= agn::kHeadMaxClasses &&
+                 h->dropout == 0.0;   // (it would read the last hidden layer before its dropout)
   if (h->split) {   // three piece planes of the activations (the weights stay fp32)
     h->Hs.assign(h->L, nullptr);
     for (int l = 0; l + 1 < h->L + (h->fuse_out_dw ? 1 : 0); ++l)
@@ -1659,6 +1697,24 @@ Status create(agn_handle* h, const int32_t* dims, int32_t n_dims, int32_t n_work
       AGN_TRY_CUDA(cudaMemcpy(h->Xe, hXe.data(), hXe.size() * sizeof(float), cudaMemcpyHostToDevice));
     AGN_TRY_CUDA(cudaMemcpy(h->ye, hye.data(), hye.size() * sizeof(int32_t), cudaMemcpyHostToDevice));
     AGN_TRY_CUDA(cudaMemset(h->e_sw, 0, sizeof(int)));
+    if (o.eval_mx4) {   // the rows in 4 bits, room for a chunk's hidden layers and the weights
+      auto matrix = [&](agn_handle::Mx4* q, int64_t r, int64_t c) -> Status {
+        AGN_TRY(dalloc_t(h, &q->codes, (size_t)agn::mx_code_bytes(r, c)));
+        AGN_TRY(dalloc_t(h, &q->scales, (size_t)agn::mx_scale_bytes(r, c)));
+        return Status::Ok();
+      };
+      h->eval_mx4 = true;
+      AGN_TRY(matrix(&h->xe4, E, d0));
+      h->w4.resize(h->L - 1);
+      for (int l = 1; l < h->L; ++l) AGN_TRY(matrix(&h->w4[l - 1], dims[l], dims[l - 1]));
+      if (h->L > 2)
+        for (auto& q : h->h4) AGN_TRY(matrix(&q, h->eval_chunk, maxh));
+      if (!h->eval_tc) {
+        AGN_TRY(agn::bounds_upload(h->stream));
+        AGN_TRY(agn::mx4_quantize(h->Xe, AGN_PREC_FP32, E, d0, d0, h->xe4.codes, h->xe4.scales,
+                                  h->stream));
+      }
+    }
     if (h->eval_tc) {
       AGN_TRY(dalloc_t(h, &h->Xe_p, (size_t)(3 * E * d0)));
       h->eval_plane = h->eval_chunk * maxh;
@@ -1669,6 +1725,10 @@ Status create(agn_handle* h, const int32_t* dims, int32_t n_dims, int32_t n_work
         AGN_TRY_CUDA(cudaMemcpyAsync(h->Xe, hXe.data() + r0 * d0, (size_t)count * sizeof(float),
                                      cudaMemcpyHostToDevice, h->stream));
         AGN_TRY(agn::split_pieces(h->Xe, h->Xe_p + r0 * d0, count, E * d0, h->stream));
+        if (h->eval_mx4)   // (r0 is a multiple of 128)
+          AGN_TRY(agn::mx4_quantize(h->Xe, AGN_PREC_FP32, std::min(up, E - r0), d0, d0,
+                                    h->xe4.codes + agn::mx_code_bytes(r0, d0),
+                                    h->xe4.scales + agn::mx_scale_bytes(r0, d0), h->stream));
         AGN_TRY_CUDA(cudaStreamSynchronize(h->stream));
       }
       dfree(h, h->Xe);
@@ -1824,16 +1884,56 @@ Status eval_chunk_tc(agn_handle* h, int64_t r0, int rows) {
                           h->e_correct + r0, h->e_pred + r0, h->stream);
 }
 
+// The hidden layers on microscaled 4-bit operands: the layer's weights (quantised
+// at the start of the call) times the chunk's rows, each layer's output 4 bits again, the
+// last hidden one's fp32; the output layer in fp32 as in the other forms.
+Status eval_chunk_mx4(agn_handle* h, int64_t r0, int rows) {
+  const int L = h->L, K = h->dims[L - 1], C = h->dims[L];
+  const int64_t d0 = h->dims[0];
+  for (int l = 1; l < L; ++l) {
+    agn::Mx4LinearArgs a{};
+    a.x_codes = l == 1 ? h->xe4.codes + agn::mx_code_bytes(r0, d0) : h->h4[l % 2].codes;
+    a.x_scales = l == 1 ? h->xe4.scales + agn::mx_scale_bytes(r0, d0) : h->h4[l % 2].scales;
+    a.w_codes = h->w4[l - 1].codes;
+    a.w_scales = h->w4[l - 1].scales;
+    a.bias = h->theta_c + h->boff[l - 1];
+    a.rows = rows; a.in = h->dims[l - 1]; a.out = h->dims[l];
+    a.relu = 1;
+    const bool last = l == L - 1;
+    a.dtype = last ? AGN_PREC_FP32 : AGN_PREC_MX4;
+    a.y = last ? static_cast<void*>(h->He[0]) : h->h4[(l + 1) % 2].codes;
+    a.y_scales = last ? nullptr : h->h4[(l + 1) % 2].scales;
+    a.ldy = h->dims[l];
+    a.err = h->flag + 1;
+    AGN_TRY(agn::mx4_linear(a, h->stream));
+  }
+  if (C <= agn::kHeadMaxClasses && K % 4 == 0)
+    return agn::eval_head(h->He[0], h->theta_c + h->woff[L - 1], h->theta_c + h->boff[L - 1],
+                          h->ye + r0, rows, K, C, h->e_loss + r0, h->e_correct + r0,
+                          h->e_pred + r0, h->stream);
+  AGN_TRY(eval_layer_simt(h, L, h->He[0], h->Ze, rows));
+  return agn::eval_logits(h->Ze, h->ye + r0, rows, C, h->e_loss + r0, h->e_correct + r0,
+                          h->e_pred + r0, h->stream);
+}
+
 // Loss and accuracy of theta~ on the held-out set: the forward pass in chunks
 // of rows, per-sample log-sum-exp / argmax, fixed-order means.
-Status evaluate(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int64_t cap) {
+Status evaluate(agn_handle* h, bool mx4, float* loss, float* accuracy, int32_t* pred, int64_t cap) {
   if (h->n_eval <= 0)
     return Status::Err(AGN_E_INVALID, "the handle has no evaluation set (agn_options.n_eval)");
+  if (mx4 && !h->eval_mx4)
+    return Status::Err(AGN_E_INVALID, "the handle was created without eval_mx4");
   if (pred && cap < h->n_eval) return Status::Err(AGN_E_INVALID, "pred shorter than n_eval");
   AGN_TRY(agn::bounds_upload(h->stream));   // bounds-checked build only
+  if (mx4)
+    for (int l = 1; l < h->L; ++l)
+      AGN_TRY(agn::mx4_quantize(h->theta_c + h->woff[l - 1], AGN_PREC_FP32, h->dims[l],
+                                h->dims[l - 1], h->dims[l - 1], h->w4[l - 1].codes,
+                                h->w4[l - 1].scales, h->stream));
   for (int64_t r0 = 0; r0 < h->n_eval; r0 += h->eval_chunk) {
     const int rows = (int)std::min<int64_t>(h->eval_chunk, h->n_eval - r0);
-    if (h->eval_tc) AGN_TRY(eval_chunk_tc(h, r0, rows));
+    if (mx4) AGN_TRY(eval_chunk_mx4(h, r0, rows));
+    else if (h->eval_tc) AGN_TRY(eval_chunk_tc(h, r0, rows));
     else AGN_TRY(eval_chunk_simt(h, r0, rows));
   }
   AGN_TRY(agn::eval_reduce(h->e_loss, h->e_correct, h->n_eval, h->e_out, h->stream));
@@ -1843,7 +1943,7 @@ Status evaluate(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int6
     AGN_TRY_CUDA(cudaMemcpyAsync(pred, h->e_pred, (size_t)h->n_eval * sizeof(int32_t),
                                  cudaMemcpyDeviceToHost, h->stream));
   int flags[2] = {0, 0};
-  if (h->eval_tc)
+  if (h->eval_tc || mx4)
     AGN_TRY_CUDA(cudaMemcpyAsync(flags, h->flag, 2 * sizeof(int), cudaMemcpyDeviceToHost, h->stream));
   AGN_TRY_CUDA(cudaStreamSynchronize(h->stream));
   AGN_TRY(agn::bounds_collect(h->stream));
@@ -2156,8 +2256,19 @@ int agn_loss(agn_handle* h, float* out, int64_t cap) {
 int agn_evaluate(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int64_t cap) {
   if (!h) return fail(nullptr, AGN_E_INVALID, "null handle");
   DeviceGuard g(h->device);
-  Status s = evaluate(h, loss, accuracy, pred, cap);
+  Status s = evaluate(h, false, loss, accuracy, pred, cap);
   return s.ok() ? AGN_OK : fail(h, s);
+}
+
+int agn_evaluate_mx4(agn_handle* h, float* loss, float* accuracy, int32_t* pred, int64_t cap) {
+  if (!h) return fail(nullptr, AGN_E_INVALID, "null handle");
+  DeviceGuard g(h->device);
+  try {
+    Status s = evaluate(h, true, loss, accuracy, pred, cap);
+    return s.ok() ? AGN_OK : fail(h, s);
+  } catch (const std::bad_alloc&) {
+    return fail(h, AGN_E_OOM, "host allocation failed");
+  }
 }
 
 int agn_temporal_efficiency(const double* ta, const double* fa, int64_t na, const double* tb,

@@ -33,6 +33,7 @@ struct GemmArgs {
   int64_t ldo, out_bstride;
   const void* mask;      // dX: H_{l-1}
   int64_t mask_bstride;
+  float mask_scale;      // dX: factor of the unmasked values (dropout's; 1 without)
   int relu;
   float* theta;          // fp32 master replicas [n][ld_param]
   float* acc;            // accumulators [n][ld_param], or null (accumulator elided)
@@ -94,6 +95,7 @@ struct HeadArgs {
   bf16* dZL_pieces;        // fp32 T only: also dZ_L's three exact bf16 pieces (planes
   int64_t dZL_plane;       // dZL_plane apart, same layout) for the tensor-core dW; null = no
   void* dH;                // out: dZ_{L-1} [slots][m][K] (T)
+  float mask_scale;        // factor of dZ_{L-1} (dropout's; 1 without)
   bf16* dH_pieces;         // fp32 T only: also its three exact bf16 pieces (planes
   int64_t dH_plane;        // dH_plane apart) for tensor-core GEMMs; null = no
   float* ce_partial;       // [slots][ceil(m / kHeadSamples)] scratch

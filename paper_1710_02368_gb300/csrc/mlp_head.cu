@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const HeadArgs a) {
       float hv[8], o[8];
       ld8(h + k0, hv);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = cvt(st_f<T>(hv[i] > 0.f ? v[i] : 0.f));
+      for (int i = 0; i < 8; ++i) o[i] = cvt(st_f<T>(hv[i] > 0.f ? v[i] * a.mask_scale : 0.f));
       st8(dh + k0, o);
       if (dp) {   // (fp32 mode: o holds the stored floats themselves)
         float q0[8], q1[8], q2[8];
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const HeadArgs a) {
         if (c + 1 < C && c + 1 < kMaxC) v1 = fmaf(g[c + 1], cvt(Ws[(int64_t)(c + 1) * Kp + k]), v1);
       }
       const float v = v0 + v1;
-      const T out = st_f<T>(cvt(h[k]) > 0.f ? v : 0.f);
+      const T out = st_f<T>(cvt(h[k]) > 0.f ? v * a.mask_scale : 0.f);
       AGN_ST(dh + k, out);
       if (dp) {
         bf16 q0, q1, q2;

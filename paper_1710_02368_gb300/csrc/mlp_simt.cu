@@ -199,7 +199,7 @@ __device__ __forceinline__ void gemm_simt_tile(const GemmArgs& g, int tile_x, in
         const int64_t n = n0 + tx + 16 * j;
         if (n >= g.N) continue;
         const float h = to_f(AGN_LD(mask + m * g.ldo + n));
-        AGN_ST(out + m * g.ldo + n, from_f<TO>(h > 0.f ? acc[i][j] : 0.f));
+        AGN_ST(out + m * g.ldo + n, from_f<TO>(h > 0.f ? acc[i][j] * g.mask_scale : 0.f));
       }
     }
   } else if (g.grad_out) {   // kEpiDW, raw gradient out (the optimizer runs after)

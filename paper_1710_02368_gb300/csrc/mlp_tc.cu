@@ -852,7 +852,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 } else {
                   const float hv[4] = {hm[u].x, hm[u].y, hm[u].z, hm[u].w};
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) v[e] = hv[e] > 0.f ? v[e] : 0.f;
+                  for (int e = 0; e < 4; ++e) v[e] = hv[e] > 0.f ? v[e] * args.mask_scale : 0.f;
                 }
                 const int64_t o4 = (int64_t)j * args.ldo + row4;
                 if (kSplit == 1 || args.out) store4(out + o4, v);

@@ -20,6 +20,7 @@ struct TcArgs {
   int64_t ldo, out_bstride;
   const void* mask;        // dX: H_{l-1}, same layout and type as out
   int64_t mask_bstride;
+  float mask_scale;        // dX: factor of the unmasked values (dropout's; 1 without)
   int relu;
   float* theta;            // fp32 master replicas [n][ld_param]
   float* acc;              // accumulators [n][ld_param]

@@ -186,35 +186,44 @@ bool rows_aligned(const void* p, int64_t ld, size_t es) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (size_t)ld * es % 16 == 0;
 }
 
-Status mx_call(bool quantize, const void* x, void* y, const void* codes, const void* scales,
-               int dtype, int64_t rows, int64_t cols, int64_t ld, cudaStream_t st) {
+// Quantise (y null) or dequantise (x null).
+Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, int64_t rows,
+                 int64_t cols, int64_t ld, cudaStream_t st) {
+  MxArgs a{};
+  a.x = x; a.y = y;
+  a.codes = static_cast<uint8_t*>(codes);
+  a.scales = static_cast<uint8_t*>(scales);
+  a.rows = rows; a.cols = cols; a.ld = ld;
+  a.row_bytes = mx_row_bytes(cols);
+  a.tiles_k = mx_tiles_k(cols);
+  const bool f32 = dtype == AGN_PREC_FP32;
+  a.vec = rows_aligned(x ? x : y, ld, f32 ? 4 : 2);
+  const dim3 grid = geometry(&a);
+  auto k = x ? (f32 ? mx4_quantize_kernel<float> : mx4_quantize_kernel<bf16>)
+             : (f32 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>);
+  AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
+  AGN_TRY_CUDA(cudaGetLastError());
+  return Status::Ok();
+}
+
+Status mx_call(const char* name, const void* x, void* y, const void* codes, const void* scales,
+               int dtype, int64_t rows, int64_t cols, int64_t ld, bool quantize, cudaStream_t st) {
   const size_t es = dtype_size(dtype);
   if (!es) return Status::Err(AGN_E_INVALID, "unknown dtype");
-  AGN_TRY(check_matrix(quantize ? "x" : "y", rows, cols, ld));
+  AGN_TRY(check_matrix(name, rows, cols, ld));
   if (rows == 0 || cols == 0) return Status::Ok();
   const void* m = quantize ? x : y;
   if (!m || !codes || !scales) return Status::Err(AGN_E_INVALID, "null pointer");
-  const CallBuffer bm{quantize ? "x" : "y", m, matrix_bytes(rows, cols, ld, es), es},
+  const CallBuffer bm{name, m, matrix_bytes(rows, cols, ld, es), es},
       bc{"codes", codes, (size_t)mx_code_bytes(rows, cols), 16},
       bs{"scales", scales, (size_t)mx_scale_bytes(rows, cols), 16};
   AGN_TRY(check_apart(bm, {bc, bs}));
   AGN_TRY(check_apart(bc, {bs}));
   AGN_TRY(check_buffers({bm, bc, bs}));
-  MxArgs a{};
-  a.x = x; a.y = y;
-  a.codes = static_cast<uint8_t*>(const_cast<void*>(codes));
-  a.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
-  a.rows = rows; a.cols = cols; a.ld = ld;
-  a.row_bytes = mx_row_bytes(cols);
-  a.tiles_k = mx_tiles_k(cols);
-  a.vec = rows_aligned(m, ld, es);
-  const dim3 grid = geometry(&a);
   KnownBuffers known({bm, bc, bs});
   AGN_TRY(bounds_upload(st));
-  auto k = quantize ? (es == 4 ? mx4_quantize_kernel<float> : mx4_quantize_kernel<bf16>)
-                    : (es == 4 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>);
-  AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
-  AGN_TRY_CUDA(cudaGetLastError());
+  AGN_TRY(launch_mx(x, y, const_cast<void*>(codes), const_cast<void*>(scales), dtype, rows, cols,
+                    ld, st));
   return bounds_collect(st);
 }
 
@@ -222,7 +231,7 @@ Status mx_call(bool quantize, const void* x, void* y, const void* codes, const v
 
 Status mx4_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
                     void* codes, void* scales, cudaStream_t st) {
-  return mx_call(true, x, nullptr, codes, scales, dtype, rows, cols, ldx, st);
+  return launch_mx(x, nullptr, codes, scales, dtype, rows, cols, ldx, st);
 }
 
 AGN_BOUNDS_UNIT(mx4)
@@ -241,8 +250,8 @@ extern "C" int agn_mx4_bytes(int64_t rows, int64_t cols, int64_t* codes, int64_t
 extern "C" int agn_mx4_quantize(const void* x, int32_t dtype, int64_t rows, int64_t cols,
                                 int64_t ldx, void* codes, void* scales, void* stream) {
   return agn::guarded([&] {
-    return agn::mx4_quantize(x, dtype, rows, cols, ldx, codes, scales,
-                             static_cast<cudaStream_t>(stream));
+    return agn::mx_call("x", x, nullptr, codes, scales, dtype, rows, cols, ldx, true,
+                        static_cast<cudaStream_t>(stream));
   });
 }
 
@@ -250,7 +259,7 @@ extern "C" int agn_mx4_dequantize(const void* codes, const void* scales, int64_t
                                   int64_t cols, void* y, int32_t dtype, int64_t ldy,
                                   void* stream) {
   return agn::guarded([&] {
-    return agn::mx_call(false, nullptr, y, codes, scales, dtype, rows, cols, ldy,
+    return agn::mx_call("y", nullptr, y, codes, scales, dtype, rows, cols, ldy, false,
                         static_cast<cudaStream_t>(stream));
   });
 }

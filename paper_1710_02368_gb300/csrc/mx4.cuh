@@ -65,6 +65,7 @@ struct Mx4LinearArgs {
   void* y_scales;         // AGN_PREC_MX4
   int* err;               // set to 1 when a bounded wait gives up (null: none)
 };
+// The launches alone (the entry points check their arguments first).
 Status mx4_linear(const Mx4LinearArgs& a, cudaStream_t st);
 Status mx4_quantize(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
                     void* codes, void* scales, cudaStream_t st);

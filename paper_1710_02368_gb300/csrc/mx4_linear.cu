@@ -324,32 +324,6 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
 }  // namespace
 
 Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
-  const size_t es = m.dtype == AGN_PREC_MX4 ? 1 : dtype_size(m.dtype);
-  if (!es) return Status::Err(AGN_E_INVALID, "unknown dtype");
-  if (m.rows < 0 || m.in < 1 || m.out < 1 || m.rows > INT32_MAX - 256 || m.in > INT32_MAX - 256 ||
-      m.out > INT32_MAX - 256)
-    return Status::Err(AGN_E_INVALID, "need rows >= 0, in >= 1, out >= 1, below 2^31");
-  if (m.dtype != AGN_PREC_MX4) AGN_TRY(check_matrix("y", m.rows, m.out, m.ldy));
-  if (m.rows == 0) return Status::Ok();
-  if (!m.x_codes || !m.x_scales || !m.w_codes || !m.w_scales || !m.y ||
-      (m.dtype == AGN_PREC_MX4 && !m.y_scales))
-    return Status::Err(AGN_E_INVALID, "null pointer");
-  if (ceil_div(m.rows, 256) > 65535)
-    return Status::Err(AGN_E_UNSUPPORTED, "more than 16776960 rows");
-  const bool mx = m.dtype == AGN_PREC_MX4;
-  const CallBuffer xc{"x codes", m.x_codes, (size_t)mx_code_bytes(m.rows, m.in), 16},
-      xs{"x scales", m.x_scales, (size_t)mx_scale_bytes(m.rows, m.in), 16},
-      wc{"w codes", m.w_codes, (size_t)mx_code_bytes(m.out, m.in), 16},
-      ws{"w scales", m.w_scales, (size_t)mx_scale_bytes(m.out, m.in), 16},
-      bb{"bias", m.bias, m.bias ? (size_t)m.out * 4 : 0, 4},
-      y{"y", m.y, mx ? (size_t)mx_code_bytes(m.rows, m.out) : matrix_bytes(m.rows, m.out, m.ldy, es),
-        mx ? 16 : es},
-      ys{"y scales", mx ? m.y_scales : nullptr, mx ? (size_t)mx_scale_bytes(m.rows, m.out) : 0, 16},
-      er{"err", m.err, m.err ? sizeof(int) : 0, 4};
-  AGN_TRY(check_apart(y, {xc, xs, wc, ws, bb, ys, er}));
-  AGN_TRY(check_apart(ys, {xc, xs, wc, ws, bb, er}));
-  AGN_TRY(check_apart(er, {xc, xs, wc, ws, bb}));
-  AGN_TRY(check_buffers({xc, xs, wc, ws, bb, y, ys, er}));
   LinearArgs a{};
   a.w_scales = static_cast<const uint8_t*>(m.w_scales);
   a.x_scales = static_cast<const uint8_t*>(m.x_scales);
@@ -363,23 +337,57 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.y_scales = static_cast<uint8_t*>(m.y_scales);
   a.y_tiles_k = mx_tiles_k(m.out);
   a.err = m.err;
-  a.vec = !mx && reinterpret_cast<uintptr_t>(m.y) % (4 * es) == 0 && m.ldy % 4 == 0;
+  a.vec = m.dtype != AGN_PREC_MX4 && m.ldy % 4 == 0 &&
+          reinterpret_cast<uintptr_t>(m.y) % (4 * dtype_size(m.dtype)) == 0;
   const int bn = m.rows <= 16 ? 16 : m.rows <= 32 ? 32 : m.rows <= 64 ? 64 : m.rows <= 1024 ? 128 : 256;
   const int64_t tiles = ceil_div(m.out, 128) * ceil_div(m.rows, bn);
   const int kt = (a.k_steps + 3) / 4;
   a.split = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, kt, current_sms() / tiles}));
   a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
+  switch (bn) {
+    case 16: return launch_linear<16>(m, a, st);
+    case 32: return launch_linear<32>(m, a, st);
+    case 64: return launch_linear<64>(m, a, st);
+    case 128: return launch_linear<128>(m, a, st);
+    default: return launch_linear<256>(m, a, st);
+  }
+}
+
+namespace {
+
+Status linear_call(const Mx4LinearArgs& m, cudaStream_t st) {
+  const bool mx = m.dtype == AGN_PREC_MX4;
+  const size_t es = mx ? 1 : dtype_size(m.dtype);
+  constexpr int64_t kMost = INT32_MAX - 256;
+  if (!es) return Status::Err(AGN_E_INVALID, "unknown dtype");
+  if (m.rows < 0 || m.in < 1 || m.out < 1 || m.rows > kMost || m.in > kMost || m.out > kMost)
+    return Status::Err(AGN_E_INVALID, "need rows >= 0, in >= 1, out >= 1, below 2^31 - 256");
+  if (!mx) AGN_TRY(check_matrix("y", m.rows, m.out, m.ldy));
+  if (m.rows == 0) return Status::Ok();
+  if (!m.x_codes || !m.x_scales || !m.w_codes || !m.w_scales || !m.y || (mx && !m.y_scales))
+    return Status::Err(AGN_E_INVALID, "null pointer");
+  if (ceil_div(m.rows, 256) > 65535)
+    return Status::Err(AGN_E_UNSUPPORTED, "more than 16776960 rows");
+  const CallBuffer xc{"x codes", m.x_codes, (size_t)mx_code_bytes(m.rows, m.in), 16},
+      xs{"x scales", m.x_scales, (size_t)mx_scale_bytes(m.rows, m.in), 16},
+      wc{"w codes", m.w_codes, (size_t)mx_code_bytes(m.out, m.in), 16},
+      ws{"w scales", m.w_scales, (size_t)mx_scale_bytes(m.out, m.in), 16},
+      bb{"bias", m.bias, m.bias ? (size_t)m.out * 4 : 0, 4},
+      y{"y", m.y, mx ? (size_t)mx_code_bytes(m.rows, m.out) : matrix_bytes(m.rows, m.out, m.ldy, es),
+        mx ? 16 : es},
+      ys{"y scales", mx ? m.y_scales : nullptr, mx ? (size_t)mx_scale_bytes(m.rows, m.out) : 0, 16},
+      er{"err", m.err, m.err ? sizeof(int) : 0, 4};
+  AGN_TRY(check_apart(y, {xc, xs, wc, ws, bb, ys, er}));
+  AGN_TRY(check_apart(ys, {xc, xs, wc, ws, bb, er}));
+  AGN_TRY(check_apart(er, {xc, xs, wc, ws, bb}));
+  AGN_TRY(check_buffers({xc, xs, wc, ws, bb, y, ys, er}));
   KnownBuffers known({xc, xs, wc, ws, bb, y, ys, er});
   AGN_TRY(bounds_upload(st));
-  switch (bn) {
-    case 16: AGN_TRY(launch_linear<16>(m, a, st)); break;
-    case 32: AGN_TRY(launch_linear<32>(m, a, st)); break;
-    case 64: AGN_TRY(launch_linear<64>(m, a, st)); break;
-    case 128: AGN_TRY(launch_linear<128>(m, a, st)); break;
-    default: AGN_TRY(launch_linear<256>(m, a, st)); break;
-  }
+  AGN_TRY(mx4_linear(m, st));
   return bounds_collect(st);
 }
+
+}  // namespace
 
 AGN_BOUNDS_UNIT(mx4_linear)
 
@@ -398,6 +406,6 @@ extern "C" int agn_mx4_linear(const void* x_codes, const void* x_scales, const v
     m.relu = relu;
     m.y = y; m.dtype = dtype; m.ldy = ldy; m.y_scales = y_scales;
     m.err = err;
-    return agn::mx4_linear(m, static_cast<cudaStream_t>(stream));
+    return agn::linear_call(m, static_cast<cudaStream_t>(stream));
   });
 }
