@@ -1308,6 +1308,15 @@ Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint6
   return encode(map, 2, base, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1);
 }
 
+Status make_tmap_u32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
+                        uint64_t batch, uint32_t box_rows, uint32_t box_batch) {
+  cuuint64_t dims[3] = {inner, rows, batch};
+  cuuint64_t strides[2] = {inner * 4, inner * rows * 4};
+  cuuint32_t box[3] = {(cuuint32_t)inner, box_rows, box_batch};
+  return encode(map, 3, base, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4,
+                CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 // More than one round of one-tile CTAs on the SMs (full waves).
 bool full_wave(const TcArgs& args, int slots, int bn) {
   static const int sms = [] {

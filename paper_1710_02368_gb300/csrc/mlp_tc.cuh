@@ -143,6 +143,9 @@ Status make_tmap_f32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint
 // Bytes in rows (inner and row_stride multiples of 16), boxes of 128 bytes, 128-byte swizzle.
 Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                        uint64_t row_stride, uint32_t box_rows);
+// Contiguous 32-bit words [batch][rows][inner], boxes of whole rows, no swizzle.
+Status make_tmap_u32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
+                        uint64_t batch, uint32_t box_rows, uint32_t box_batch);
 // 4D bf16 tensor map (inner, rows, batch, piece) over three piece planes.
 Status make_tmap_bf16_4d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                          uint64_t batch, uint64_t row_stride_elems, uint64_t batch_stride_elems,

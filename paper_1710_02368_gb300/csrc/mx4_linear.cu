@@ -321,6 +321,259 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
   return Status::Ok();
 }
 
+// ---------------------------------------------------------------------------
+// Many rows: pairs of CTAs
+// ---------------------------------------------------------------------------
+
+// Two SMs share a tile of 256 features x 256 rows (tcgen05 cta_group::2): each
+// holds its 128 features and half of the rows, 64 bytes of operands a clock of MMA
+// time where a CTA alone would need 96, and the L2 gives an SM about 64.  One
+// pair for every two SMs walks over the tiles; roles by warp: 0 loads (in both
+// CTAs, all on the first one's barriers), 1 issues the MMAs (first CTA), 4-11 finish:
+// they take the sums into registers at once, so that the next tile's MMAs start
+// while they add, round and store (a second accumulator leaves no TMEM columns for
+// the scales).
+constexpr int kPairThreads = 384;
+constexpr int kPairStages = 6;
+constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows
+constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // W, X, and the scales of 128 + 256 rows
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 1024 + 256;
+static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448, "shared memory");
+constexpr uint32_t kPairSfa = 256, kPairSfb = 264;         // TMEM columns of the scales
+
+// wait_or_abort whose acquire covers the other CTA's arrivals.
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity,
+                                             volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 0;; ++it) {
+    uint32_t got;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    if (got) return true;
+    if ((it & 63) == 0) {
+      const uint64_t now = tc::globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (*abort_flag || now - t0 > kWaitNs) return false;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1)
+mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+                       const __grid_constant__ CUtensorMap tmWs,
+                       const __grid_constant__ CUtensorMap tmXs, const LinearArgs a, int tiles_f,
+                       int tiles) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kPairStages * kPairStage);
+  uint64_t* empty = full + kPairStages;
+  uint64_t* sums_full = empty + kPairStages;
+  uint64_t* sums_empty = sums_full + 1;
+  uint64_t* drained = sums_empty + 1;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drained + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = (int)cluster_rank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int KT = (a.k_steps + 3) / 4;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    tc::mbar_init(sums_full, 1);
+    tc::mbar_init(sums_empty, 16);   // the finishing warps of both CTAs
+    tc::mbar_init(drained, 1);
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+    tc::tma_prefetch_desc(&tmW);
+    tc::tma_prefetch_desc(&tmX);
+    tc::tma_prefetch_desc(&tmWs);
+    tc::tma_prefetch_desc(&tmXs);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc_pair(tmem_holder, 512);
+    tc::tmem_relinquish_pair();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  pdl_begin();
+
+  if (warp == 0 && lane == 0) {
+    int it = 0;
+    for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
+      const int f = (t % tiles_f) * 256 + 128 * cta, n = (t / tiles_f) * 256;
+      for (int kt = 0; kt < KT; ++kt, ++it) {
+        const int s = it % kPairStages;
+        if (it >= kPairStages &&
+            !wait_cluster(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
+          *abort_flag = 1;
+          break;
+        }
+        uint8_t* st = smem + s * kPairStage;
+        const uint32_t bar = tc::map_cluster(&full[s], 0);
+        if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
+        tc::tma_load_2d_pair(st, &tmW, bar, kt * 128, f);
+        tc::tma_load_2d_pair(st + kPairHalf, &tmX, bar, kt * 128, n + 128 * cta);
+        tc::tma_load_3d_pair(st + 2 * kPairHalf, &tmWs, bar, 0, 2 * kt, f >> 7);
+        tc::tma_load_3d_pair(st + 2 * kPairHalf + kSfBytes, &tmXs, bar, 0, 2 * kt, n >> 7);
+      }
+    }
+    if (*abort_flag && cta == 0)   // wait (bounded) for the copies of the stages armed last
+      for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j)
+        tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+  } else if (warp == 1 && lane == 0 && cta == 0) {
+    int it = 0, done = 0;
+    for (int t = pair; t < tiles; t += pairs, ++done) {
+      if (done > 0 && !wait_cluster(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
+      tc::tc_fence_after();
+      for (int kt = 0; kt < KT && !*abort_flag; ++kt, ++it) {
+        const int s = it % kPairStages;
+        if (!wait_cluster(&full[s], (it / kPairStages) & 1, abort_flag)) {
+          *abort_flag = 1;
+          break;
+        }
+        tc::tc_fence_after();
+        const uint32_t sa = tc::smem_u32(smem + s * kPairStage), sb = sa + kPairHalf;
+        const uint32_t ss = sb + kPairHalf;
+        const int steps = min(4, a.k_steps - 4 * kt);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (2 * q >= steps) break;
+          tc::cp_32x128b_warpx4_pair(tmem + kPairSfa + 4 * q,
+                                     tc::smem_desc_rows16(ss + q * kMxTileBytes, 128));
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            tc::cp_32x128b_warpx4_pair(
+                tmem + kPairSfb + 8 * q + 4 * h,
+                tc::smem_desc_rows16(ss + kSfBytes * (1 + h) + q * kMxTileBytes, 128));
+        }
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          if (kk >= steps) break;
+          const int q = kk >> 1;
+          tc::mma_mxf4_pair(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
+                            tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
+                            (kk & 1) ? tc::idesc_mxf4(256, 256, 2) : tc::idesc_mxf4(256, 256, 0),
+                            tmem + kPairSfa + 4 * q, tmem + kPairSfb + 8 * q, (kt | kk) != 0);
+        }
+        tc::mma_commit_pair(&empty[s]);
+      }
+      if (*abort_flag) {
+        // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
+        // end before any memory goes
+        tc::mma_commit_pair(drained);
+        tc::mbar_wait_bounded(drained, 0, kWaitNs);
+        break;
+      }
+      tc::mma_commit_pair(sums_full);
+    }
+  } else if (warp >= 4) {
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
+    bool ok = true;
+    int done = 0;
+    for (int t = pair; t < tiles; t += pairs, ++done) {
+      ok = ok && wait_cluster(sums_full, done & 1, abort_flag) && !*abort_flag;
+      ok = __all_sync(0xffffffffu, ok);
+      tc::tc_fence_after();
+      uint32_t v[4][32];
+      if (ok) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          tc::tmem_ld_32x32b_x32(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half + 32 * c),
+                                 v[c]);
+        tc::tmem_ld_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_cluster(empty_at);
+      } else {
+        if (lane == 0) {
+          *abort_flag = 1;
+          if (a.err) atomicExch(a.err, 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0x7fc00000u;
+      }
+      const int64_t f = (int64_t)(t % tiles_f) * 256 + 128 * cta + 32 * q + lane;
+      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * half;
+      const bool live = f < a.out;
+      const float b = a.bias && live ? AGN_LD(a.bias + f) : 0.f;
+      const int n = (int)min((int64_t)128, a.rows - r0);
+      auto value = [&](int i) {
+        float x = __uint_as_float(v[i / 32][i % 32]) + b;
+        if (a.relu && x <= 0.f) x = 0.f;
+        return x;
+      };
+      if (a.dtype == AGN_PREC_FP32) {
+        float* p = static_cast<float*>(a.y) + r0 * a.ldy + f;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (live && i < n) AGN_ST(p + i * a.ldy, value(i));
+      } else if (a.dtype == AGN_PREC_BF16) {
+        bf16* p = static_cast<bf16*>(a.y) + r0 * a.ldy + f;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (live && i < n) AGN_ST(p + i * a.ldy, __float2bfloat16_rn(value(i)));
+      } else {
+        // the warp's 32 features are a block: one row after another
+        const int64_t row_bytes = mx_row_bytes(a.out), kb = (f - lane) / kMxBlock;
+        uint8_t* codes = static_cast<uint8_t*>(a.y);
+#pragma unroll
+        for (int i = 0; i < 128; ++i) {
+          if (i < n) {   // (warp-uniform)
+            const float x = live ? value(i) : 0.f;
+            const uint32_t code = mx_scale_code(
+                __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu));
+            uint32_t w = code == 255 ? 0u : (mx_pair(x * mx_inverse(code), 0.f) & 15u) << (4 * (lane & 7));
+            w |= __shfl_xor_sync(0xffffffffu, w, 1);
+            w |= __shfl_xor_sync(0xffffffffu, w, 2);
+            w |= __shfl_xor_sync(0xffffffffu, w, 4);
+            const int64_t r = r0 + i;
+            if ((lane & 7) == 0 && kb * 16 < row_bytes)
+              AGN_ST(reinterpret_cast<uint32_t*>(codes + r * row_bytes + kb * 16) + (lane >> 3), w);
+            if (lane == 0 && (kb >> 2) < a.y_tiles_k)
+              AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
+          }
+        }
+      }
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers
+  if (warp == 1) tc::tmem_dealloc_pair(tmem, 512);
+}
+
+Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStream_t st) {
+  CUtensorMap tw, tx, tws, txs;
+  const int64_t rb = mx_row_bytes(m.in);
+  AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, rb, m.out, rb, 128));
+  AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, rb, m.rows, rb, 128));
+  // the scales: words of a tile, tiles along K, tiles of rows
+  AGN_TRY(make_tmap_u32_3d(&tws, m.w_scales, kMxTileBytes / 4, a.tiles_k,
+                           ceil_div(m.out, kMxTileRows), 2, 1));
+  AGN_TRY(make_tmap_u32_3d(&txs, m.x_scales, kMxTileBytes / 4, a.tiles_k, a.row_tiles, 2, 2));
+  auto kern = mx4_linear_pair_kernel;
+  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)kPairSmem));
+  const int64_t tiles_f = ceil_div(m.out, 256), tiles = tiles_f * ceil_div(m.rows, 256);
+  const int64_t pairs = std::min<int64_t>(tiles, sms / 2);
+  AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem,
+                                  dim3(2, 1, 1), st, tw, tx, tws, txs, a, (int)tiles_f, (int)tiles));
+  AGN_TRY_CUDA(cudaGetLastError());
+  return Status::Ok();
+}
+
 }  // namespace
 
 Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
@@ -339,10 +592,13 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.err = m.err;
   a.vec = m.dtype != AGN_PREC_MX4 && m.ldy % 4 == 0 &&
           reinterpret_cast<uintptr_t>(m.y) % (4 * dtype_size(m.dtype)) == 0;
+  const int sms = current_sms();
+  if (m.rows > 256 && m.out > 128 && ceil_div(m.out, 256) * ceil_div(m.rows, 256) * 4 >= sms)
+    return launch_pair(m, a, sms, st);
   const int bn = m.rows <= 16 ? 16 : m.rows <= 32 ? 32 : m.rows <= 64 ? 64 : m.rows <= 1024 ? 128 : 256;
   const int64_t tiles = ceil_div(m.out, 128) * ceil_div(m.rows, bn);
   const int kt = (a.k_steps + 3) / 4;
-  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, kt, current_sms() / tiles}));
+  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, kt, sms / tiles}));
   a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
   switch (bn) {
     case 16: return launch_linear<16>(m, a, st);

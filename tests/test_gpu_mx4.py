@@ -141,23 +141,21 @@ def linear(agn, torch, x, w, rows, inner, out, dtype=0, ldy=None, fill=7.0, **kw
 
 
 def units(x, w):
-    """Every product is a multiple of a quarter of the smallest scales' product; whether sums of the
-    magnitudes stay below 2^24 of it, where fp32 sums are exact in any order."""
+    """Every product of a row of x and one of w is a multiple of the smallest last bits of the two; whether
+    the sum of the magnitudes stays below 2^24 of it, where fp32 sums are exact in any order."""
     def unit(m):
-        nz = np.abs(m[m != 0])
-        if nz.size == 0:
-            return 1.0
-        frac, ex = np.frexp(nz)
-        # a value is 1, 1.5 times a power of two (or half the scale): its last bit is half its leading one at most
-        return float(np.min(np.exp2(ex - 2.0)))
-    u = unit(x) * unit(w)
+        # a value is 1 or 1.5 times a power of two: its last bit is at least half its leading one
+        _, ex = np.frexp(np.where(m == 0, np.inf, m))
+        return np.where(m == 0, np.inf, np.exp2(ex - 2.0)).min(1)
+    ux, uw = (np.where(np.isinf(u), 1.0, u) for u in (unit(x), unit(w)))
+    u = np.outer(ux, uw)
     return u, np.abs(x) @ np.abs(w).T / u < 2 ** 24
 
 
 LINEAR = [(1, 32, 1), (1, 1, 4), (2, 33, 10), (1, 784, 128), (5, 100, 31), (16, 256, 129), (17, 257, 128),
           (32, 64, 33), (33, 1000, 127), (64, 320, 300), (65, 784, 96), (128, 128, 128), (129, 65, 257),
           (200, 2048, 100), (257, 512, 260), (300, 96, 520), (1, 8192, 64), (3, 4096, 1000), (1030, 160, 140),
-          (1100, 300, 388), (70, 5000, 40)]
+          (1100, 300, 388), (70, 5000, 40), (9800, 65, 257), (2500, 640, 1030), (2433, 1100, 1111)]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
@@ -179,7 +177,7 @@ def test_linear_exact(agn, torch, rows, inner, out, dtype):
     assert np.all(np.abs(got - want) <= 1.01 * tol)
 
 
-@pytest.mark.parametrize("rows,inner,out", [(3, 200, 70), (40, 1000, 130), (150, 600, 260), (1500, 500, 200)])
+@pytest.mark.parametrize("rows,inner,out", [(3, 200, 70), (40, 1000, 130), (150, 600, 260), (1500, 500, 200), (2433, 500, 1030)])
 def test_linear_spread(agn, torch, rows, inner, out):
     """Rows 20 binades apart."""
     x, w = operands(agn, torch, np.random.default_rng(3), rows, inner, out, spread=20)
@@ -189,7 +187,7 @@ def test_linear_spread(agn, torch, rows, inner, out):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,inner,out", [(1, 64, 10), (20, 300, 131), (100, 257, 130), (1200, 128, 72)])
+@pytest.mark.parametrize("rows,inner,out", [(1, 64, 10), (20, 300, 131), (100, 257, 130), (1200, 128, 72), (9800, 65, 140)])
 def test_bias_relu_strides(agn, torch, rows, inner, out, dtype):
     rng = np.random.default_rng(4)
     x, w = operands(agn, torch, rng, rows, inner, out)
@@ -204,7 +202,7 @@ def test_bias_relu_strides(agn, torch, rows, inner, out, dtype):
 
 
 @pytest.mark.parametrize("rows,inner,out", [(1, 64, 10), (7, 1024, 32), (20, 300, 131), (100, 257, 130),
-                                            (200, 784, 1000), (1200, 128, 72), (1030, 1000, 388)])
+                                            (200, 784, 1000), (1200, 128, 72), (1030, 1000, 388), (9800, 96, 130), (2433, 300, 1111)])
 def test_four_bit_output(agn, torch, rows, inner, out):
     """The 4-bit output is the quantisation of the fp32 one, byte for byte, and nothing else is written."""
     rng = np.random.default_rng(5)
