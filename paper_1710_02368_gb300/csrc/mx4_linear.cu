@@ -58,7 +58,7 @@ struct LinearArgs {
   int k_steps;              // ceil(in / 64)
   int split;                // CTAs of a cluster, along K
   const float* bias;
-  int relu, dtype, vec;     // vec: four features of a row are one aligned store
+  int relu, dtype, vec;     // vec: rows of y start 16-byte aligned
   void* y;
   int64_t ldy;
   uint8_t* y_scales;
@@ -328,36 +328,116 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
 // Two SMs share a tile of 256 features x 256 rows (tcgen05 cta_group::2): each
 // holds its 128 features and half of the rows, 64 bytes of operands a clock of MMA
 // time where a CTA alone would need 96, and the L2 gives an SM about 64.  One
-// pair for every two SMs walks over the tiles; roles by warp: 0 loads (in both
-// CTAs, all on the first one's barriers), 1 issues the MMAs (first CTA), 4-11 finish:
-// they take the sums into registers at once, so that the next tile's MMAs start
-// while they add, round and store (a second accumulator leaves no TMEM columns for
-// the scales).
-constexpr int kPairThreads = 384;
-constexpr int kPairStages = 6;
+// pair for every two SMs walks over the tiles; roles by warp:
+//   4     loads: codes complete on the first CTA's barriers, each CTA's scales on its own
+//   0-3   bring a stage's scales from shared memory into TMEM (tcgen05.st, each warp
+//         its lane quadrant): tcgen05.cp runs between the MMAs, about 53 clocks for each
+//         512 bytes, six of them a stage (16384 x 8192 x 4096: 296 us with it, 223 without)
+//   5     issues the MMAs (first CTA)
+//   8-15  finish: 64 columns at a time into registers, bias and ReLU there, then through
+//         shared memory so that a warp stores whole 64- or 128-byte pieces of rows
+// A second accumulator would leave no TMEM columns for the scales: the next tile's
+// MMAs start once the last 64 columns are in registers.
+constexpr int kPairThreads = 512;
+constexpr int kPairStages = 5;
 constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows
 constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // W, X, and the scales of 128 + 256 rows
-constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 1024 + 256;
+constexpr int kPairPad = 36;                               // floats of a staged row: no bank conflicts
+constexpr int kPairStaged = 32 * kPairPad;                 // a warp's 32 rows x 32 features
+constexpr size_t kPairRing = (size_t)kPairStages * kPairStage;
+constexpr size_t kPairSmem = kPairRing + 8 * kPairStaged * 4 + 1024 + 256;
 static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448, "shared memory");
-constexpr uint32_t kPairSfa = 256, kPairSfb = 264;         // TMEM columns of the scales
+constexpr uint32_t kPairSf = 256, kPairSfCols = 24;        // a stage's scales in TMEM: W's 8, X's 16
+static_assert(kPairSf + kPairStages * kPairSfCols <= 512, "TMEM");
 
-// wait_or_abort whose acquire covers the other CTA's arrivals.
-__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity,
-                                             volatile int* abort_flag) {
+// Bounded waits that give up when another role of the CTA has: kTmem for barriers
+// that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
+template <bool kTmem>
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
-  for (uint32_t it = 0;; ++it) {
+  for (uint32_t it = 1;; ++it) {
     uint32_t got;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    if (kTmem)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    else
+      got = tc::mbar_try_wait(bar, parity);
     if (got) return true;
     if ((it & 63) == 0) {
       const uint64_t now = tc::globaltimer_ns();
       if (t0 == 0) t0 = now;
       if (*abort_flag || now - t0 > kWaitNs) return false;
     }
+  }
+}
+
+// 32 rows (from r0, n of them exist) x 32 features (from f0) of finished values, staged
+// by a warp as [row][kPairPad] floats, to y.
+__device__ __forceinline__ void store_staged(const LinearArgs& a, const float* t, int64_t r0, int n,
+                                             int64_t f0, int lane) {
+  if (a.dtype == AGN_PREC_MX4) {   // a lane a row: the 32 features are a block
+    const int64_t kb = f0 / kMxBlock, r = r0 + lane;
+    const float4* p = reinterpret_cast<const float4*>(t + lane * kPairPad);
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float4 v = p[i];
+      const uint32_t x = max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu);
+      const uint32_t y = max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu);
+      amax = max(amax, max(x, y));
+    }
+    const uint32_t code = mx_scale_code(amax);
+    const float inv = mx_inverse(code);
+    uint32_t q[4] = {0, 0, 0, 0};
+    if (code != 255) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 v = p[i];
+        q[i >> 1] |= (mx_pair(v.x * inv, v.y * inv) | mx_pair(v.z * inv, v.w * inv) << 8) << (16 * (i & 1));
+      }
+    }
+    if (lane < n) {
+      if (f0 < a.out)
+        AGN_ST(reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.y) + r * mx_row_bytes(a.out) + kb * 16),
+               make_uint4(q[0], q[1], q[2], q[3]));
+      if ((kb >> 2) < a.y_tiles_k)
+        AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
+    }
+    return;
+  }
+  if (a.vec && f0 + 32 <= a.out) {
+    if (a.dtype == AGN_PREC_BF16) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int row = 8 * g + (lane >> 2), f = 8 * (lane & 3);
+        const float4 u = *reinterpret_cast<const float4*>(t + row * kPairPad + f);
+        const float4 v = *reinterpret_cast<const float4*>(t + row * kPairPad + f + 4);
+        const __nv_bfloat162 o[4] = {__floats2bfloat162_rn(u.x, u.y), __floats2bfloat162_rn(u.z, u.w),
+                                     __floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+        if (row < n)
+          AGN_ST(reinterpret_cast<uint4*>(static_cast<bf16*>(a.y) + (r0 + row) * a.ldy + f0 + f),
+                 *reinterpret_cast<const uint4*>(o));
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const int row = 4 * g + (lane >> 3), f = 4 * (lane & 7);
+        const float4 v = *reinterpret_cast<const float4*>(t + row * kPairPad + f);
+        if (row < n)
+          AGN_ST(reinterpret_cast<float4*>(static_cast<float*>(a.y) + (r0 + row) * a.ldy + f0 + f), v);
+      }
+    }
+    return;
+  }
+  if (f0 + lane >= a.out) return;   // rows that are not aligned, or the last features: one by one
+  for (int row = 0; row < n; ++row) {
+    const float v = t[row * kPairPad + lane];
+    const int64_t at = (r0 + row) * a.ldy + f0 + lane;
+    if (a.dtype == AGN_PREC_BF16) AGN_ST(static_cast<bf16*>(a.y) + at, __float2bfloat16_rn(v));
+    else AGN_ST(static_cast<float*>(a.y) + at, v);
   }
 }
 
@@ -369,10 +449,13 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kPairStages * kPairStage);
+  float* staged = reinterpret_cast<float*>(smem + kPairRing);
+  uint64_t* full = reinterpret_cast<uint64_t*>(staged + 8 * kPairStaged);   // codes of both CTAs (first CTA's)
   uint64_t* empty = full + kPairStages;
-  uint64_t* sums_full = empty + kPairStages;
-  uint64_t* sums_empty = sums_full + 1;
+  uint64_t* scales_in = empty + kPairStages;        // this CTA's scales in shared memory
+  uint64_t* scales_up = scales_in + kPairStages;    // both CTAs' in TMEM (first CTA's)
+  uint64_t* sums_full = scales_up + kPairStages;
+  uint64_t* sums_empty = sums_full + 1;             // (first CTA's)
   uint64_t* drained = sums_empty + 1;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drained + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
@@ -386,9 +469,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     for (int s = 0; s < kPairStages; ++s) {
       tc::mbar_init(&full[s], 1);
       tc::mbar_init(&empty[s], 1);
+      tc::mbar_init(&scales_in[s], 1);
+      tc::mbar_init(&scales_up[s], 8);   // four warps of each CTA
     }
     tc::mbar_init(sums_full, 1);
-    tc::mbar_init(sums_empty, 16);   // the finishing warps of both CTAs
+    tc::mbar_init(sums_empty, 16);       // the finishing warps of both CTAs
     tc::mbar_init(drained, 1);
     *abort_flag = 0;
     tc::fence_mbar_init();
@@ -397,7 +482,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     tc::tma_prefetch_desc(&tmWs);
     tc::tma_prefetch_desc(&tmXs);
   }
-  if (warp == 1) {
+  if (warp == 5) {
     tc::tmem_alloc_pair(tmem_holder, 512);
     tc::tmem_relinquish_pair();
   }
@@ -408,55 +493,81 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 4 && lane == 0) {
     int it = 0;
     for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
       const int f = (t % tiles_f) * 256 + 128 * cta, n = (t / tiles_f) * 256;
       for (int kt = 0; kt < KT; ++kt, ++it) {
         const int s = it % kPairStages;
         if (it >= kPairStages &&
-            !wait_cluster(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
+            !wait_pair<false>(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
           *abort_flag = 1;
           break;
         }
         uint8_t* st = smem + s * kPairStage;
         const uint32_t bar = tc::map_cluster(&full[s], 0);
-        if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 2 * kPairStage);
+        tc::mbar_arrive_expect_tx(&scales_in[s], 3 * kSfBytes);
+        tc::tma_load_3d(st + 2 * kPairHalf, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
+        tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
+        if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
         tc::tma_load_2d_pair(st, &tmW, bar, kt * 128, f);
         tc::tma_load_2d_pair(st + kPairHalf, &tmX, bar, kt * 128, n + 128 * cta);
-        tc::tma_load_3d_pair(st + 2 * kPairHalf, &tmWs, bar, 0, 2 * kt, f >> 7);
-        tc::tma_load_3d_pair(st + 2 * kPairHalf + kSfBytes, &tmXs, bar, 0, 2 * kt, n >> 7);
       }
     }
-    if (*abort_flag && cta == 0)   // wait (bounded) for the copies of the stages armed last
-      for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j)
-        tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
-  } else if (warp == 1 && lane == 0 && cta == 0) {
+    if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
+      for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j) {
+        tc::mbar_wait_bounded(&scales_in[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+        if (cta == 0) tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+      }
+  } else if (warp < 4) {
+    // a stage's scales: lane l holds words j (rows 32 j + l) of every tile; the
+    // stage was loaded again only after the MMAs that read its TMEM columns
+    const uint32_t quadrant = (uint32_t)(32 * warp) << 16;
+    int it = 0;
+    bool ok = true;
+    for (int t = pair; t < tiles && ok; t += pairs) {
+      for (int kt = 0; kt < KT; ++kt, ++it) {
+        const int s = it % kPairStages;
+        ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], (it / kPairStages) & 1, abort_flag));
+        if (!ok) break;
+        const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
+        uint32_t w[8], x[16];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint4 v = src[32 * q];
+          w[4 * q] = v.x; w[4 * q + 1] = v.y; w[4 * q + 2] = v.z; w[4 * q + 3] = v.w;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 u = src[64 * (1 + h) + 32 * q];
+            x[8 * q + 4 * h] = u.x; x[8 * q + 4 * h + 1] = u.y;
+            x[8 * q + 4 * h + 2] = u.z; x[8 * q + 4 * h + 3] = u.w;
+          }
+        }
+        const uint32_t col = tmem + quadrant + kPairSf + (uint32_t)s * kPairSfCols;
+        tc::tmem_st_32x32b_x8(col, w);
+        tc::tmem_st_32x32b_x16(col + 8, x);
+        tc::tmem_st_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_relaxed(tc::map_cluster(&scales_up[s], 0));
+      }
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
+  } else if (warp == 5 && lane == 0 && cta == 0) {
     int it = 0, done = 0;
     for (int t = pair; t < tiles; t += pairs, ++done) {
-      if (done > 0 && !wait_cluster(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
-      tc::tc_fence_after();
+      if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
       for (int kt = 0; kt < KT && !*abort_flag; ++kt, ++it) {
         const int s = it % kPairStages;
-        if (!wait_cluster(&full[s], (it / kPairStages) & 1, abort_flag)) {
+        if (!wait_pair<true>(&scales_up[s], (it / kPairStages) & 1, abort_flag) ||
+            !wait_pair<false>(&full[s], (it / kPairStages) & 1, abort_flag)) {
           *abort_flag = 1;
           break;
         }
         tc::tc_fence_after();
         const uint32_t sa = tc::smem_u32(smem + s * kPairStage), sb = sa + kPairHalf;
-        const uint32_t ss = sb + kPairHalf;
+        const uint32_t sf = tmem + kPairSf + (uint32_t)s * kPairSfCols;
         const int steps = min(4, a.k_steps - 4 * kt);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          if (2 * q >= steps) break;
-          tc::cp_32x128b_warpx4_pair(tmem + kPairSfa + 4 * q,
-                                     tc::smem_desc_rows16(ss + q * kMxTileBytes, 128));
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            tc::cp_32x128b_warpx4_pair(
-                tmem + kPairSfb + 8 * q + 4 * h,
-                tc::smem_desc_rows16(ss + kSfBytes * (1 + h) + q * kMxTileBytes, 128));
-        }
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           if (kk >= steps) break;
@@ -464,7 +575,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           tc::mma_mxf4_pair(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
                             tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
                             (kk & 1) ? tc::idesc_mxf4(256, 256, 2) : tc::idesc_mxf4(256, 256, 0),
-                            tmem + kPairSfa + 4 * q, tmem + kPairSfb + 8 * q, (kt | kk) != 0);
+                            sf + 4 * q, sf + 8 + 8 * q, (kt | kk) != 0);
         }
         tc::mma_commit_pair(&empty[s]);
       }
@@ -477,73 +588,51 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
       tc::mma_commit_pair(sums_full);
     }
-  } else if (warp >= 4) {
-    const int q = warp & 3, half = (warp - 4) >> 2;
+  } else if (warp >= 8) {
+    const int q = warp & 3, half = (warp - 8) >> 2;
     const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
+    float* stage = staged + (warp - 8) * kPairStaged;
     bool ok = true;
     int done = 0;
     for (int t = pair; t < tiles; t += pairs, ++done) {
-      ok = ok && wait_cluster(sums_full, done & 1, abort_flag) && !*abort_flag;
+      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * cta + 32 * q;
+      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * half;
+      const bool live = f0 + lane < a.out;
+      const float b = a.bias && live ? AGN_LD(a.bias + f0 + lane) : 0.f;
+      ok = ok && wait_pair<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
       ok = __all_sync(0xffffffffu, ok);
       tc::tc_fence_after();
-      uint32_t v[4][32];
-      if (ok) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          tc::tmem_ld_32x32b_x32(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half + 32 * c),
-                                 v[c]);
-        tc::tmem_ld_wait();
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive_cluster(empty_at);
-      } else {
-        if (lane == 0) {
-          *abort_flag = 1;
-          if (a.err) atomicExch(a.err, 1);
+      if (!ok && lane == 0) {
+        *abort_flag = 1;
+        if (a.err) atomicExch(a.err, 1);
+      }
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {   // 64 columns (rows of y) at a time
+        uint32_t v[2][32];
+        if (ok) {
+          const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half + 64 * h);
+          tc::tmem_ld_32x32b_x32(col, v[0]);
+          tc::tmem_ld_32x32b_x32(col + 32, v[1]);
+          tc::tmem_ld_wait();
+          if (h == 1) {
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive_relaxed(empty_at);
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0x7fc00000u;
-      }
-      const int64_t f = (int64_t)(t % tiles_f) * 256 + 128 * cta + 32 * q + lane;
-      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * half;
-      const bool live = f < a.out;
-      const float b = a.bias && live ? AGN_LD(a.bias + f) : 0.f;
-      const int n = (int)min((int64_t)128, a.rows - r0);
-      auto value = [&](int i) {
-        float x = __uint_as_float(v[i / 32][i % 32]) + b;
-        if (a.relu && x <= 0.f) x = 0.f;
-        return x;
-      };
-      if (a.dtype == AGN_PREC_FP32) {
-        float* p = static_cast<float*>(a.y) + r0 * a.ldy + f;
+        for (int c = 0; c < 2; ++c) {
+          const int64_t rc = r0 + 64 * h + 32 * c;
+          if (rc >= a.rows) break;   // (warp-uniform)
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-          if (live && i < n) AGN_ST(p + i * a.ldy, value(i));
-      } else if (a.dtype == AGN_PREC_BF16) {
-        bf16* p = static_cast<bf16*>(a.y) + r0 * a.ldy + f;
-#pragma unroll
-        for (int i = 0; i < 128; ++i)
-          if (live && i < n) AGN_ST(p + i * a.ldy, __float2bfloat16_rn(value(i)));
-      } else {
-        // the warp's 32 features are a block: one row after another
-        const int64_t row_bytes = mx_row_bytes(a.out), kb = (f - lane) / kMxBlock;
-        uint8_t* codes = static_cast<uint8_t*>(a.y);
-#pragma unroll
-        for (int i = 0; i < 128; ++i) {
-          if (i < n) {   // (warp-uniform)
-            const float x = live ? value(i) : 0.f;
-            const uint32_t code = mx_scale_code(
-                __reduce_max_sync(0xffffffffu, __float_as_uint(x) & 0x7fffffffu));
-            uint32_t w = code == 255 ? 0u : (mx_pair(x * mx_inverse(code), 0.f) & 15u) << (4 * (lane & 7));
-            w |= __shfl_xor_sync(0xffffffffu, w, 1);
-            w |= __shfl_xor_sync(0xffffffffu, w, 2);
-            w |= __shfl_xor_sync(0xffffffffu, w, 4);
-            const int64_t r = r0 + i;
-            if ((lane & 7) == 0 && kb * 16 < row_bytes)
-              AGN_ST(reinterpret_cast<uint32_t*>(codes + r * row_bytes + kb * 16) + (lane >> 3), w);
-            if (lane == 0 && (kb >> 2) < a.y_tiles_k)
-              AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
+          for (int i = 0; i < 32; ++i) {
+            float x = ok ? __uint_as_float(v[c][i]) + b : NAN;
+            if (a.relu && x <= 0.f) x = 0.f;
+            stage[i * kPairPad + lane] = live ? x : 0.f;
           }
+          __syncwarp();
+          store_staged(a, stage, rc, (int)min((int64_t)32, a.rows - rc), f0, lane);
+          __syncwarp();
         }
       }
     }
@@ -551,7 +640,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   tc::tc_fence_before();
   __syncthreads();
   cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers
-  if (warp == 1) tc::tmem_dealloc_pair(tmem, 512);
+  if (warp == 5) tc::tmem_dealloc_pair(tmem, 512);
 }
 
 Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStream_t st) {
@@ -590,8 +679,8 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.y_scales = static_cast<uint8_t*>(m.y_scales);
   a.y_tiles_k = mx_tiles_k(m.out);
   a.err = m.err;
-  a.vec = m.dtype != AGN_PREC_MX4 && m.ldy % 4 == 0 &&
-          reinterpret_cast<uintptr_t>(m.y) % (4 * dtype_size(m.dtype)) == 0;
+  a.vec = m.dtype != AGN_PREC_MX4 && m.ldy * (int64_t)dtype_size(m.dtype) % 16 == 0 &&
+          reinterpret_cast<uintptr_t>(m.y) % 16 == 0;
   const int sms = current_sms();
   if (m.rows > 256 && m.out > 128 && ceil_div(m.out, 256) * ceil_div(m.rows, 256) * 4 >= sms)
     return launch_pair(m, a, sms, st);

@@ -255,11 +255,6 @@ __device__ __forceinline__ void mma_mxf4_pair(uint32_t d_tmem, uint64_t a_desc, 
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(accumulate)
       : "memory");
 }
-// (each CTA's own shared memory to its own TMEM)
-__device__ __forceinline__ void cp_32x128b_warpx4_pair(uint32_t taddr, uint64_t s_desc) {
-  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(s_desc)
-               : "memory");
-}
 // Arrive on the barriers at `bar`'s address in both CTAs of the pair once every
 // tcgen05 operation issued so far by this thread completes.
 __device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
@@ -286,7 +281,7 @@ __device__ __forceinline__ uint32_t map_cluster(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
   return at;
 }
-// TMA loads into this CTA's shared memory that complete on a barrier of either
+// TMA load into this CTA's shared memory that completes on a barrier of either
 // CTA of the pair (bar: its shared::cluster address).
 __device__ __forceinline__ void tma_load_2d_pair(void* dst, const void* tmap, uint32_t bar, int x,
                                                  int y) {
@@ -296,17 +291,11 @@ __device__ __forceinline__ void tma_load_2d_pair(void* dst, const void* tmap, ui
       "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y)
       : "memory");
 }
-__device__ __forceinline__ void tma_load_3d_pair(void* dst, const void* tmap, uint32_t bar, int x,
-                                                 int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-// Arrive on a barrier of the cluster (its shared::cluster address), release at cluster scope.
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+// Arrive on a barrier of the cluster (its shared::cluster address).  Relaxed: it
+// orders TMEM accesses alone, with tcgen05.fence::before_thread_sync before it and
+// ::after_thread_sync after the wait (a release at cluster scope costs about 1000 clocks).
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
                : "memory");
 }
 
