@@ -58,7 +58,8 @@ struct LinearArgs {
   int k_steps;              // ceil(in / 64)
   int split;                // CTAs of a cluster, along K
   const float* bias;
-  int relu, dtype, vec;     // vec: rows of y start 16-byte aligned
+  int relu, dtype;
+  int vec;                  // rows of y start 16-byte aligned (1), 32-byte (2)
   void* y;
   int64_t ldy;
   uint8_t* y_scales;
@@ -325,29 +326,29 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
 // Many rows: pairs of CTAs
 // ---------------------------------------------------------------------------
 
-// Two SMs share a tile of 256 features x 256 rows (tcgen05 cta_group::2): each
-// holds its 128 features and half of the rows, 64 bytes of operands a clock of MMA
-// time where a CTA alone would need 96, and the L2 gives an SM about 64.  One
+// Two SMs share a tile of 256 rows x 256 features (tcgen05 cta_group::2): each
+// holds its 128 rows and half of the features, 64 bytes of operands a clock of MMA
+// time where a CTA alone would need 96, and the L2 gives an SM about 64.  Here the
+// rows are the MMA's M: a lane holds a row's consecutive features, which it
+// stores 32 bytes at a time and which are whole blocks of a 4-bit output; nothing
+// passes through shared memory, whose bandwidth the MMAs and the loads use up
+// (128 of 128 bytes a clock at the full rate).  One
 // pair for every two SMs walks over the tiles; roles by warp:
 //   4     loads: codes complete on the first CTA's barriers, each CTA's scales on its own
 //   0-3   bring a stage's scales from shared memory into TMEM (tcgen05.st, each warp
-//         its lane quadrant): tcgen05.cp runs between the MMAs, about 53 clocks for each
-//         512 bytes, six of them a stage (16384 x 8192 x 4096: 296 us with it, 223 without)
+//         its lane quadrant): tcgen05.cp takes 97 clocks for 512 bytes, six of them a stage,
+//         and little of it beside the MMAs (four MMAs 513 clocks, with six copies 860)
 //   5     issues the MMAs (first CTA)
-//   8-15  finish: 64 columns at a time into registers, bias and ReLU there, then through
-//         shared memory so that a warp stores whole 64- or 128-byte pieces of rows
+//   8-15  finish: 64 columns at a time into registers, bias, ReLU, rounding, stores
 // A second accumulator would leave no TMEM columns for the scales: the next tile's
 // MMAs start once the last 64 columns are in registers.
 constexpr int kPairThreads = 512;
-constexpr int kPairStages = 5;
-constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows
-constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // W, X, and the scales of 128 + 256 rows
-constexpr int kPairPad = 36;                               // floats of a staged row: no bank conflicts
-constexpr int kPairStaged = 32 * kPairPad;                 // a warp's 32 rows x 32 features
-constexpr size_t kPairRing = (size_t)kPairStages * kPairStage;
-constexpr size_t kPairSmem = kPairRing + 8 * kPairStaged * 4 + 1024 + 256;
+constexpr int kPairStages = 6;
+constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows or features
+constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // x, w, scales of 128 rows and 256 features
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 8 * 512 + 1024 + 512;   // + biases
 static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448, "shared memory");
-constexpr uint32_t kPairSf = 256, kPairSfCols = 24;        // a stage's scales in TMEM: W's 8, X's 16
+constexpr uint32_t kPairSf = 256, kPairSfCols = 24;        // a stage's scales in TMEM: x's 8, w's 16
 static_assert(kPairSf + kPairStages * kPairSfCols <= 512, "TMEM");
 
 // Bounded waits that give up when another role of the CTA has: kTmem for barriers
@@ -374,70 +375,102 @@ __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volati
   }
 }
 
-// 32 rows (from r0, n of them exist) x 32 features (from f0) of finished values, staged
-// by a warp as [row][kPairPad] floats, to y.
-__device__ __forceinline__ void store_staged(const LinearArgs& a, const float* t, int64_t r0, int n,
-                                             int64_t f0, int lane) {
-  if (a.dtype == AGN_PREC_MX4) {   // a lane a row: the 32 features are a block
-    const int64_t kb = f0 / kMxBlock, r = r0 + lane;
-    const float4* p = reinterpret_cast<const float4*>(t + lane * kPairPad);
+__device__ __forceinline__ float relu_nan(float x) {   // max(x, 0), NaN stays
+  float r;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// 32 bytes of a row in one store (the address 32-byte aligned) or two (16).
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8], bool whole) {
+  if (!AGN_BOUNDS_OK(p, 32)) {
+    AGN_BOUNDS_FAIL(p);
+  } else if (whole) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]),
+                 "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
+// Features f .. f + 31 of row r from their sums: bias (theirs, in shared memory; null:
+// none), ReLU, rounding, store.  `row`: the row exists.  f < out (4-bit outputs: or
+// in its last scale tile).
+__device__ __forceinline__ void finish_row(const LinearArgs& a, const float* bias, int64_t r, bool row,
+                                           int64_t f, uint32_t (&s)[32]) {
+  const bool full = f + 32 <= a.out;   // (the same for the warp)
+  float v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(s[i]);
+  if (bias) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(bias + i);
+      v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+    }
+  }
+  if (a.relu) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = relu_nan(v[i]);
+  }
+  if (a.dtype == AGN_PREC_MX4) {
     uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float4 v = p[i];
-      const uint32_t x = max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu);
-      const uint32_t y = max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu);
-      amax = max(amax, max(x, y));
+    for (int i = 0; i < 32; ++i) {
+      if (!full && f + i >= a.out) v[i] = 0.f;
+      amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
     }
     const uint32_t code = mx_scale_code(amax);
     const float inv = mx_inverse(code);
     uint32_t q[4] = {0, 0, 0, 0};
     if (code != 255) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 v = p[i];
-        q[i >> 1] |= (mx_pair(v.x * inv, v.y * inv) | mx_pair(v.z * inv, v.w * inv) << 8) << (16 * (i & 1));
-      }
+      for (int i = 0; i < 16; ++i)
+        q[i >> 2] |= mx_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * (i & 3));
     }
-    if (lane < n) {
-      if (f0 < a.out)
-        AGN_ST(reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.y) + r * mx_row_bytes(a.out) + kb * 16),
-               make_uint4(q[0], q[1], q[2], q[3]));
-      if ((kb >> 2) < a.y_tiles_k)
-        AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
-    }
+    if (!row) return;
+    const int64_t kb = f / kMxBlock;
+    if (f < a.out)
+      AGN_ST(reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.y) + r * mx_row_bytes(a.out) + kb * 16),
+             make_uint4(q[0], q[1], q[2], q[3]));
+    AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
+  } else if (!row) {
     return;
-  }
-  if (a.vec && f0 + 32 <= a.out) {
-    if (a.dtype == AGN_PREC_BF16) {
+  } else if (a.dtype == AGN_PREC_BF16) {
+    bf16* p = static_cast<bf16*>(a.y) + r * a.ldy + f;
+    if (full && a.vec) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int row = 8 * g + (lane >> 2), f = 8 * (lane & 3);
-        const float4 u = *reinterpret_cast<const float4*>(t + row * kPairPad + f);
-        const float4 v = *reinterpret_cast<const float4*>(t + row * kPairPad + f + 4);
-        const __nv_bfloat162 o[4] = {__floats2bfloat162_rn(u.x, u.y), __floats2bfloat162_rn(u.z, u.w),
-                                     __floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-        if (row < n)
-          AGN_ST(reinterpret_cast<uint4*>(static_cast<bf16*>(a.y) + (r0 + row) * a.ldy + f0 + f),
-                 *reinterpret_cast<const uint4*>(o));
+      for (int i = 0; i < 32; i += 16) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const __nv_bfloat162 o = __floats2bfloat162_rn(v[i + 2 * j], v[i + 2 * j + 1]);
+          w[j] = *reinterpret_cast<const uint32_t*>(&o);
+        }
+        store32(p + i, w, a.vec == 2);
       }
     } else {
 #pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const int row = 4 * g + (lane >> 3), f = 4 * (lane & 7);
-        const float4 v = *reinterpret_cast<const float4*>(t + row * kPairPad + f);
-        if (row < n)
-          AGN_ST(reinterpret_cast<float4*>(static_cast<float*>(a.y) + (r0 + row) * a.ldy + f0 + f), v);
-      }
+      for (int i = 0; i < 32; ++i)
+        if (f + i < a.out) AGN_ST(p + i, __float2bfloat16_rn(v[i]));
     }
-    return;
-  }
-  if (f0 + lane >= a.out) return;   // rows that are not aligned, or the last features: one by one
-  for (int row = 0; row < n; ++row) {
-    const float v = t[row * kPairPad + lane];
-    const int64_t at = (r0 + row) * a.ldy + f0 + lane;
-    if (a.dtype == AGN_PREC_BF16) AGN_ST(static_cast<bf16*>(a.y) + at, __float2bfloat16_rn(v));
-    else AGN_ST(static_cast<float*>(a.y) + at, v);
+  } else {
+    float* p = static_cast<float*>(a.y) + r * a.ldy + f;
+    if (full && a.vec) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[i + j]);
+        store32(p + i, w, a.vec == 2);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (f + i < a.out) AGN_ST(p + i, v[i]);
+    }
   }
 }
 
@@ -449,8 +482,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  float* staged = reinterpret_cast<float*>(smem + kPairRing);
-  uint64_t* full = reinterpret_cast<uint64_t*>(staged + 8 * kPairStaged);   // codes of both CTAs (first CTA's)
+  float* biases = reinterpret_cast<float*>(smem + kPairStages * kPairStage);   // [finishing warp][128]
+  uint64_t* full = reinterpret_cast<uint64_t*>(biases + 8 * 128);   // codes of both CTAs (first CTA's)
   uint64_t* empty = full + kPairStages;
   uint64_t* scales_in = empty + kPairStages;        // this CTA's scales in shared memory
   uint64_t* scales_up = scales_in + kPairStages;    // both CTAs' in TMEM (first CTA's)
@@ -496,7 +529,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   if (warp == 4 && lane == 0) {
     int it = 0;
     for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
-      const int f = (t % tiles_f) * 256 + 128 * cta, n = (t / tiles_f) * 256;
+      const int f = (t % tiles_f) * 256, n = (t / tiles_f) * 256 + 128 * cta;
       for (int kt = 0; kt < KT; ++kt, ++it) {
         const int s = it % kPairStages;
         if (it >= kPairStages &&
@@ -507,11 +540,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         uint8_t* st = smem + s * kPairStage;
         const uint32_t bar = tc::map_cluster(&full[s], 0);
         tc::mbar_arrive_expect_tx(&scales_in[s], 3 * kSfBytes);
-        tc::tma_load_3d(st + 2 * kPairHalf, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
-        tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
+        tc::tma_load_3d(st + 2 * kPairHalf, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
+        tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
         if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
-        tc::tma_load_2d_pair(st, &tmW, bar, kt * 128, f);
-        tc::tma_load_2d_pair(st + kPairHalf, &tmX, bar, kt * 128, n + 128 * cta);
+        tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
+        tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, f + 128 * cta);
       }
     }
     if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
@@ -531,21 +564,21 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], (it / kPairStages) & 1, abort_flag));
         if (!ok) break;
         const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
-        uint32_t w[8], x[16];
+        uint32_t x[8], w[16];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const uint4 v = src[32 * q];
-          w[4 * q] = v.x; w[4 * q + 1] = v.y; w[4 * q + 2] = v.z; w[4 * q + 3] = v.w;
+          x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint4 u = src[64 * (1 + h) + 32 * q];
-            x[8 * q + 4 * h] = u.x; x[8 * q + 4 * h + 1] = u.y;
-            x[8 * q + 4 * h + 2] = u.z; x[8 * q + 4 * h + 3] = u.w;
+            w[8 * q + 4 * h] = u.x; w[8 * q + 4 * h + 1] = u.y;
+            w[8 * q + 4 * h + 2] = u.z; w[8 * q + 4 * h + 3] = u.w;
           }
         }
         const uint32_t col = tmem + quadrant + kPairSf + (uint32_t)s * kPairSfCols;
-        tc::tmem_st_32x32b_x8(col, w);
-        tc::tmem_st_32x32b_x16(col + 8, x);
+        tc::tmem_st_32x32b_x8(col, x);
+        tc::tmem_st_32x32b_x16(col + 8, w);
         tc::tmem_st_wait();
         tc::tc_fence_before();
         __syncwarp();
@@ -591,14 +624,24 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   } else if (warp >= 8) {
     const int q = warp & 3, half = (warp - 8) >> 2;
     const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
-    float* stage = staged + (warp - 8) * kPairStaged;
+    float* bias = biases + 128 * (warp - 8);
+    // 4-bit outputs: blocks past the row's last in its last scale tile are written too
+    const int64_t end = a.dtype == AGN_PREC_MX4 ? a.y_tiles_k * 128 : a.out;
     bool ok = true;
     int done = 0;
     for (int t = pair; t < tiles; t += pairs, ++done) {
-      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * cta + 32 * q;
-      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * half;
-      const bool live = f0 + lane < a.out;
-      const float b = a.bias && live ? AGN_LD(a.bias + f0 + lane) : 0.f;
+      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * half;
+      const int64_t r = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q + lane;
+      if (a.bias) {   // (on its way while the sums are)
+        float b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          b[i] = f0 + lane + 32 * i < a.out ? AGN_LD(a.bias + f0 + lane + 32 * i) : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
+        __syncwarp();
+      }
       ok = ok && wait_pair<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
       ok = __all_sync(0xffffffffu, ok);
       tc::tc_fence_after();
@@ -607,7 +650,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         if (a.err) atomicExch(a.err, 1);
       }
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {   // 64 columns (rows of y) at a time
+      for (int h = 0; h < 2; ++h) {   // 64 features at a time
         uint32_t v[2][32];
         if (ok) {
           const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half + 64 * h);
@@ -619,20 +662,14 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             __syncwarp();
             if (lane == 0) tc::mbar_arrive_relaxed(empty_at);
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 64; ++i) v[i / 32][i % 32] = 0x7fc00000u;
         }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const int64_t rc = r0 + 64 * h + 32 * c;
-          if (rc >= a.rows) break;   // (warp-uniform)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float x = ok ? __uint_as_float(v[c][i]) + b : NAN;
-            if (a.relu && x <= 0.f) x = 0.f;
-            stage[i * kPairPad + lane] = live ? x : 0.f;
-          }
-          __syncwarp();
-          store_staged(a, stage, rc, (int)min((int64_t)32, a.rows - rc), f0, lane);
-          __syncwarp();
+          const int64_t f = f0 + 64 * h + 32 * c;
+          if (f < end) finish_row(a, a.bias ? bias + 64 * h + 32 * c : nullptr, r, r < a.rows, f, v[c]);
         }
       }
     }
@@ -650,8 +687,8 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStr
   AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, rb, m.rows, rb, 128));
   // the scales: words of a tile, tiles along K, tiles of rows
   AGN_TRY(make_tmap_u32_3d(&tws, m.w_scales, kMxTileBytes / 4, a.tiles_k,
-                           ceil_div(m.out, kMxTileRows), 2, 1));
-  AGN_TRY(make_tmap_u32_3d(&txs, m.x_scales, kMxTileBytes / 4, a.tiles_k, a.row_tiles, 2, 2));
+                           ceil_div(m.out, kMxTileRows), 2, 2));
+  AGN_TRY(make_tmap_u32_3d(&txs, m.x_scales, kMxTileBytes / 4, a.tiles_k, a.row_tiles, 2, 1));
   auto kern = mx4_linear_pair_kernel;
   AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)kPairSmem));
@@ -679,8 +716,8 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.y_scales = static_cast<uint8_t*>(m.y_scales);
   a.y_tiles_k = mx_tiles_k(m.out);
   a.err = m.err;
-  a.vec = m.dtype != AGN_PREC_MX4 && m.ldy * (int64_t)dtype_size(m.dtype) % 16 == 0 &&
-          reinterpret_cast<uintptr_t>(m.y) % 16 == 0;
+  const uint64_t rows_at = reinterpret_cast<uintptr_t>(m.y) | (uint64_t)m.ldy * dtype_size(m.dtype);
+  a.vec = m.dtype == AGN_PREC_MX4 ? 0 : rows_at % 32 == 0 ? 2 : rows_at % 16 == 0 ? 1 : 0;
   const int sms = current_sms();
   if (m.rows > 256 && m.out > 128 && ceil_div(m.out, 256) * ceil_div(m.rows, 256) * 4 >= sms)
     return launch_pair(m, a, sms, st);
