@@ -339,9 +339,9 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
 //         its lane quadrant): tcgen05.cp takes 97 clocks for 512 bytes, six of them a stage,
 //         and little of it beside the MMAs (four MMAs 513 clocks, with six copies 860)
 //   5     issues the MMAs (first CTA)
-//   8-15  finish: 64 columns at a time into registers, bias, ReLU, rounding, stores
+//   8-15  finish: their 128 columns into registers at once, bias, ReLU, rounding, stores
 // A second accumulator would leave no TMEM columns for the scales: the next tile's
-// MMAs start once the last 64 columns are in registers.
+// MMAs start once the sums are in registers.
 constexpr int kPairThreads = 512;
 constexpr int kPairStages = 6;
 constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows or features
@@ -526,33 +526,58 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  if (warp == 4 && lane == 0) {
-    int it = 0;
-    for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
-      const int f = (t % tiles_f) * 256, n = (t / tiles_f) * 256 + 128 * cta;
-      for (int kt = 0; kt < KT; ++kt, ++it) {
-        const int s = it % kPairStages;
-        if (it >= kPairStages &&
-            !wait_pair<false>(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
-          *abort_flag = 1;
-          break;
-        }
-        uint8_t* st = smem + s * kPairStage;
-        const uint32_t bar = tc::map_cluster(&full[s], 0);
-        tc::mbar_arrive_expect_tx(&scales_in[s], 3 * kSfBytes);
-        tc::tma_load_3d(st + 2 * kPairHalf, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
-        tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
-        if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
-        tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
-        tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, f + 128 * cta);
+  // The finishing warps hold 128 sums a thread: 2 x 128 threads x (72 + 184) registers
+  // are the launch's 512 x 128.
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int q = warp & 3, half = (warp - 8) >> 2;
+    const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
+    float* bias = biases + 128 * (warp - 8);
+    // 4-bit outputs: blocks past the row's last in its last scale tile are written too
+    const int64_t end = a.dtype == AGN_PREC_MX4 ? a.y_tiles_k * 128 : a.out;
+    bool ok = true;
+    int done = 0;
+    for (int t = pair; t < tiles; t += pairs, ++done) {
+      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * half;
+      const int64_t r = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q + lane;
+      if (a.bias) {   // (on its way while the sums are)
+        float b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          b[i] = f0 + lane + 32 * i < a.out ? AGN_LD(a.bias + f0 + lane + 32 * i) : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
+        __syncwarp();
+      }
+      ok = ok && wait_pair<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
+      ok = __all_sync(0xffffffffu, ok);
+      tc::tc_fence_after();
+      if (!ok && lane == 0) {
+        *abort_flag = 1;
+        if (a.err) atomicExch(a.err, 1);
+      }
+      uint32_t v[4][32];
+      if (ok) {
+        const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc::tmem_ld_32x32b_x32(col + 32 * c, v[c]);
+        tc::tmem_ld_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_relaxed(empty_at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0x7fc00000u;
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int64_t f = f0 + 32 * c;
+        if (f < end) finish_row(a, a.bias ? bias + 32 * c : nullptr, r, r < a.rows, f, v[c]);
       }
     }
-    if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
-      for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j) {
-        tc::mbar_wait_bounded(&scales_in[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
-        if (cta == 0) tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
-      }
   } else if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // a stage's scales: lane l holds words j (rows 32 j + l) of every tile; the
     // stage was loaded again only after the MMAs that read its TMEM columns
     const uint32_t quadrant = (uint32_t)(32 * warp) << 16;
@@ -586,91 +611,68 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
-  } else if (warp == 5 && lane == 0 && cta == 0) {
-    int it = 0, done = 0;
-    for (int t = pair; t < tiles; t += pairs, ++done) {
-      if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
-      for (int kt = 0; kt < KT && !*abort_flag; ++kt, ++it) {
-        const int s = it % kPairStages;
-        if (!wait_pair<true>(&scales_up[s], (it / kPairStages) & 1, abort_flag) ||
-            !wait_pair<false>(&full[s], (it / kPairStages) & 1, abort_flag)) {
-          *abort_flag = 1;
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 4 && lane == 0) {
+      int it = 0;
+      for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
+        const int f = (t % tiles_f) * 256, n = (t / tiles_f) * 256 + 128 * cta;
+        for (int kt = 0; kt < KT; ++kt, ++it) {
+          const int s = it % kPairStages;
+          if (it >= kPairStages &&
+              !wait_pair<false>(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
+            *abort_flag = 1;
+            break;
+          }
+          uint8_t* st = smem + s * kPairStage;
+          const uint32_t bar = tc::map_cluster(&full[s], 0);
+          tc::mbar_arrive_expect_tx(&scales_in[s], 3 * kSfBytes);
+          tc::tma_load_3d(st + 2 * kPairHalf, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
+          tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
+          if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
+          tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
+          tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, f + 128 * cta);
+        }
+      }
+      if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
+        for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j) {
+          tc::mbar_wait_bounded(&scales_in[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+          if (cta == 0) tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+        }
+    } else if (warp == 5 && lane == 0 && cta == 0) {
+      int it = 0, done = 0;
+      for (int t = pair; t < tiles; t += pairs, ++done) {
+        if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
+        for (int kt = 0; kt < KT && !*abort_flag; ++kt, ++it) {
+          const int s = it % kPairStages;
+          if (!wait_pair<true>(&scales_up[s], (it / kPairStages) & 1, abort_flag) ||
+              !wait_pair<false>(&full[s], (it / kPairStages) & 1, abort_flag)) {
+            *abort_flag = 1;
+            break;
+          }
+          tc::tc_fence_after();
+          const uint32_t sa = tc::smem_u32(smem + s * kPairStage), sb = sa + kPairHalf;
+          const uint32_t sf = tmem + kPairSf + (uint32_t)s * kPairSfCols;
+          const int steps = min(4, a.k_steps - 4 * kt);
+  #pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= steps) break;
+            const int q = kk >> 1;
+            tc::mma_mxf4_pair(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
+                              tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
+                              (kk & 1) ? tc::idesc_mxf4(256, 256, 2) : tc::idesc_mxf4(256, 256, 0),
+                              sf + 4 * q, sf + 8 + 8 * q, (kt | kk) != 0);
+          }
+          tc::mma_commit_pair(&empty[s]);
+        }
+        if (*abort_flag) {
+          // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
+          // end before any memory goes
+          tc::mma_commit_pair(drained);
+          tc::mbar_wait_bounded(drained, 0, kWaitNs);
           break;
         }
-        tc::tc_fence_after();
-        const uint32_t sa = tc::smem_u32(smem + s * kPairStage), sb = sa + kPairHalf;
-        const uint32_t sf = tmem + kPairSf + (uint32_t)s * kPairSfCols;
-        const int steps = min(4, a.k_steps - 4 * kt);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          if (kk >= steps) break;
-          const int q = kk >> 1;
-          tc::mma_mxf4_pair(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
-                            tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
-                            (kk & 1) ? tc::idesc_mxf4(256, 256, 2) : tc::idesc_mxf4(256, 256, 0),
-                            sf + 4 * q, sf + 8 + 8 * q, (kt | kk) != 0);
-        }
-        tc::mma_commit_pair(&empty[s]);
-      }
-      if (*abort_flag) {
-        // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
-        // end before any memory goes
-        tc::mma_commit_pair(drained);
-        tc::mbar_wait_bounded(drained, 0, kWaitNs);
-        break;
-      }
-      tc::mma_commit_pair(sums_full);
-    }
-  } else if (warp >= 8) {
-    const int q = warp & 3, half = (warp - 8) >> 2;
-    const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
-    float* bias = biases + 128 * (warp - 8);
-    // 4-bit outputs: blocks past the row's last in its last scale tile are written too
-    const int64_t end = a.dtype == AGN_PREC_MX4 ? a.y_tiles_k * 128 : a.out;
-    bool ok = true;
-    int done = 0;
-    for (int t = pair; t < tiles; t += pairs, ++done) {
-      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * half;
-      const int64_t r = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q + lane;
-      if (a.bias) {   // (on its way while the sums are)
-        float b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          b[i] = f0 + lane + 32 * i < a.out ? AGN_LD(a.bias + f0 + lane + 32 * i) : 0.f;
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
-        __syncwarp();
-      }
-      ok = ok && wait_pair<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
-      tc::tc_fence_after();
-      if (!ok && lane == 0) {
-        *abort_flag = 1;
-        if (a.err) atomicExch(a.err, 1);
-      }
-#pragma unroll 1
-      for (int h = 0; h < 2; ++h) {   // 64 features at a time
-        uint32_t v[2][32];
-        if (ok) {
-          const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half + 64 * h);
-          tc::tmem_ld_32x32b_x32(col, v[0]);
-          tc::tmem_ld_32x32b_x32(col + 32, v[1]);
-          tc::tmem_ld_wait();
-          if (h == 1) {
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive_relaxed(empty_at);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 64; ++i) v[i / 32][i % 32] = 0x7fc00000u;
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int64_t f = f0 + 64 * h + 32 * c;
-          if (f < end) finish_row(a, a.bias ? bias + 64 * h + 32 * c : nullptr, r, r < a.rows, f, v[c]);
-        }
+        tc::mma_commit_pair(sums_full);
       }
     }
   }
