@@ -483,11 +483,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
   float* biases = reinterpret_cast<float*>(smem + kPairStages * kPairStage);   // [finishing warp][128]
-  uint64_t* full = reinterpret_cast<uint64_t*>(biases + 8 * 128);   // codes of both CTAs (first CTA's)
+  // first CTA's: both CTAs' codes in shared memory and scales in TMEM
+  uint64_t* full = reinterpret_cast<uint64_t*>(biases + 8 * 128);
   uint64_t* empty = full + kPairStages;
   uint64_t* scales_in = empty + kPairStages;        // this CTA's scales in shared memory
-  uint64_t* scales_up = scales_in + kPairStages;    // both CTAs' in TMEM (first CTA's)
-  uint64_t* sums_full = scales_up + kPairStages;
+  uint64_t* sums_full = scales_in + kPairStages;
   uint64_t* sums_empty = sums_full + 1;             // (first CTA's)
   uint64_t* drained = sums_empty + 1;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drained + 1);
@@ -500,10 +500,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kPairStages; ++s) {
-      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&full[s], 1 + 8);    // the loads, and four scale warps of each CTA
       tc::mbar_init(&empty[s], 1);
       tc::mbar_init(&scales_in[s], 1);
-      tc::mbar_init(&scales_up[s], 8);   // four warps of each CTA
     }
     tc::mbar_init(sums_full, 1);
     tc::mbar_init(sums_empty, 16);       // the finishing warps of both CTAs
@@ -581,12 +580,13 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     // a stage's scales: lane l holds words j (rows 32 j + l) of every tile; the
     // stage was loaded again only after the MMAs that read its TMEM columns
     const uint32_t quadrant = (uint32_t)(32 * warp) << 16;
-    int it = 0;
+    const uint32_t full0 = tc::map_cluster(full, 0);
+    int s = 0;
+    uint32_t phase = 0;
     bool ok = true;
     for (int t = pair; t < tiles && ok; t += pairs) {
-      for (int kt = 0; kt < KT; ++kt, ++it) {
-        const int s = it % kPairStages;
-        ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], (it / kPairStages) & 1, abort_flag));
+      for (int kt = 0; kt < KT; ++kt) {
+        ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], phase, abort_flag));
         if (!ok) break;
         const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
         uint32_t x[8], w[16];
@@ -607,63 +607,80 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         tc::tmem_st_wait();
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive_relaxed(tc::map_cluster(&scales_up[s], 0));
+        if (lane == 0) tc::mbar_arrive_relaxed(full0 + 8u * (uint32_t)s);
+        if (++s == kPairStages) s = 0, phase ^= 1;
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 4 && lane == 0) {
-      int it = 0;
+      const uint32_t full0 = tc::map_cluster(full, 0);
+      int s = 0, n_armed = 0;
+      uint32_t phase = 1;   // (the first round finds every stage free)
       for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
         const int f = (t % tiles_f) * 256, n = (t / tiles_f) * 256 + 128 * cta;
-        for (int kt = 0; kt < KT; ++kt, ++it) {
-          const int s = it % kPairStages;
-          if (it >= kPairStages &&
-              !wait_pair<false>(&empty[s], ((it / kPairStages) - 1) & 1, abort_flag)) {
+        for (int kt = 0; kt < KT; ++kt) {
+          if (!wait_pair<false>(&empty[s], phase, abort_flag)) {
             *abort_flag = 1;
             break;
           }
           uint8_t* st = smem + s * kPairStage;
-          const uint32_t bar = tc::map_cluster(&full[s], 0);
+          const uint32_t bar = full0 + 8u * (uint32_t)s;
           tc::mbar_arrive_expect_tx(&scales_in[s], 3 * kSfBytes);
           tc::tma_load_3d(st + 2 * kPairHalf, &tmXs, &scales_in[s], 0, 2 * kt, n >> 7);
           tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
           if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
           tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
           tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, f + 128 * cta);
+          n_armed = min(n_armed + 1, kPairStages);
+          if (++s == kPairStages) s = 0, phase ^= 1;
         }
       }
       if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
-        for (int j = it - 1; j >= 0 && j >= it - kPairStages; --j) {
-          tc::mbar_wait_bounded(&scales_in[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
-          if (cta == 0) tc::mbar_wait_bounded(&full[j % kPairStages], (j / kPairStages) & 1, kWaitNs);
+        for (; n_armed > 0; --n_armed) {
+          if (--s < 0) s = kPairStages - 1, phase ^= 1;
+          // (armed in the round whose empty wait had `phase`: it completes the other one)
+          tc::mbar_wait_bounded(&scales_in[s], phase ^ 1, kWaitNs);
+          if (cta == 0) tc::mbar_wait_bounded(&full[s], phase ^ 1, kWaitNs);
         }
     } else if (warp == 5 && lane == 0 && cta == 0) {
-      int it = 0, done = 0;
+      // An MMA is issued in about the time that it takes, and few wait in line: what this
+      // thread does between them is tensor time lost unless it is short (836 clocks
+      // a stage with two barriers waited on in turn and the descriptors made anew, 513
+      // for the MMAs alone).  So: one barrier a stage, asked for the next stage
+      // between this stage's MMAs, descriptors by addition.
+      const uint64_t da0 = tc::smem_desc_sw128(tc::smem_u32(smem), 16, 1024);
+      constexpr uint64_t kToB = kPairHalf >> 4;
+      uint64_t da = da0;
+      uint32_t sf = tmem + kPairSf;
+      int s = 0, done = 0;
+      uint32_t phase = 0;
+      bool ready = false;
       for (int t = pair; t < tiles; t += pairs, ++done) {
         if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
-        for (int kt = 0; kt < KT && !*abort_flag; ++kt, ++it) {
-          const int s = it % kPairStages;
-          if (!wait_pair<true>(&scales_up[s], (it / kPairStages) & 1, abort_flag) ||
-              !wait_pair<false>(&full[s], (it / kPairStages) & 1, abort_flag)) {
+        for (int left = a.k_steps; left > 0; left -= 4) {
+          if (!ready && !wait_pair<false>(&full[s], phase, abort_flag)) {
             *abort_flag = 1;
             break;
           }
           tc::tc_fence_after();
-          const uint32_t sa = tc::smem_u32(smem + s * kPairStage), sb = sa + kPairHalf;
-          const uint32_t sf = tmem + kPairSf + (uint32_t)s * kPairSfCols;
-          const int steps = min(4, a.k_steps - 4 * kt);
-  #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            if (kk >= steps) break;
-            const int q = kk >> 1;
-            tc::mma_mxf4_pair(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
-                              tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
-                              (kk & 1) ? tc::idesc_mxf4(256, 256, 2) : tc::idesc_mxf4(256, 256, 0),
-                              sf + 4 * q, sf + 8 + 8 * q, (kt | kk) != 0);
-          }
-          tc::mma_commit_pair(&empty[s]);
+          const bool first = left == a.k_steps;
+          tc::mma_mxf4_pair(tmem, da, da + kToB, tc::idesc_mxf4(256, 256, 0), sf, sf + 8, !first);
+          if (left > 1)
+            tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, tc::idesc_mxf4(256, 256, 2), sf, sf + 8, 1);
+          uint64_t* const mine = &empty[s];
+          const uint64_t d = da + 4;
+          const uint32_t sf1 = sf;
+          da += kPairStage >> 4;
+          sf += kPairSfCols;
+          if (++s == kPairStages) s = 0, phase ^= 1, da = da0, sf = tmem + kPairSf;
+          ready = tc::mbar_test_wait(&full[s], phase);
+          if (left > 2)
+            tc::mma_mxf4_pair(tmem, d, d + kToB, tc::idesc_mxf4(256, 256, 0), sf1 + 4, sf1 + 16, 1);
+          if (left > 3)
+            tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, tc::idesc_mxf4(256, 256, 2), sf1 + 4, sf1 + 16, 1);
+          tc::mma_commit_pair(mine);
         }
         if (*abort_flag) {
           // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
