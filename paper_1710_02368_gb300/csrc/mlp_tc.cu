@@ -1308,6 +1308,32 @@ Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint6
   return encode(map, 2, base, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1);
 }
 
+Status make_tmap_store_2d(CUtensorMap* map, const void* base, int esize, uint64_t inner,
+                          uint64_t rows, uint64_t row_stride_elems, uint32_t box_inner,
+                          uint32_t box_rows) {
+  AGN_TRY(tc_init());
+  const uint64_t stride = row_stride_elems * esize;
+  if ((reinterpret_cast<uintptr_t>(base) | stride | inner * esize) & 15)
+    return Status::Err(AGN_E_UNSUPPORTED, "tensor map of stores not in 16-byte pieces");
+#ifdef AGN_BOUNDS_CHECK
+  if (!bounds_host_ok(base, (rows - 1) * stride + inner * esize))
+    return Status::Err(AGN_E_BOUNDS, "bounds-checked build: a tensor map beyond a known buffer");
+#endif
+  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride};
+  const cuuint32_t box[2] = {box_inner, box_rows}, estr[2] = {1, 1};
+  const CUresult r = g_encode(
+      map,
+      esize == 4   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+      : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                   : CU_TENSOR_MAP_DATA_TYPE_UINT8,
+      2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      box_inner * esize == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS)
+    return Status::Err(AGN_E_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string(r));
+  return Status::Ok();
+}
+
 Status make_tmap_u32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                         uint64_t batch, uint32_t box_rows, uint32_t box_batch) {
   cuuint64_t dims[3] = {inner, rows, batch};

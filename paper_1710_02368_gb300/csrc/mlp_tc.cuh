@@ -143,6 +143,12 @@ Status make_tmap_f32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint
 // Bytes in rows (inner and row_stride multiples of 16), boxes of 128 bytes, 128-byte swizzle.
 Status make_tmap_u8_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                        uint64_t row_stride, uint32_t box_rows);
+// Output of tensor stores: elements of esize (4: fp32, 2: bf16, 1: bytes), rows and base
+// 16-byte aligned, inner whole 16-byte pieces (the store unit's), boxes of 128-byte rows (128-byte swizzle) or 64-byte ones
+// (64-byte swizzle).
+Status make_tmap_store_2d(CUtensorMap* map, const void* base, int esize, uint64_t inner,
+                          uint64_t rows, uint64_t row_stride_elems, uint32_t box_inner,
+                          uint32_t box_rows);
 // Contiguous 32-bit words [batch][rows][inner], boxes of whole rows, no swizzle.
 Status make_tmap_u32_3d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows,
                         uint64_t batch, uint32_t box_rows, uint32_t box_batch);

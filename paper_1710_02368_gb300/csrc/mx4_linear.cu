@@ -59,7 +59,9 @@ struct LinearArgs {
   int split;                // CTAs of a cluster, along K
   const float* bias;
   int relu, dtype;
-  int vec;                  // rows of y start 16-byte aligned (1), 32-byte (2)
+  int vec;                  // rows of y start 16-byte aligned
+  int64_t bulk_out;         // features that bulk stores may write: whole 16-byte pieces of
+                            // aligned rows (4-bit output: all)
   void* y;
   int64_t ldy;
   uint8_t* y_scales;
@@ -329,24 +331,23 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
 // Two SMs share a tile of 256 rows x 256 features (tcgen05 cta_group::2): each
 // holds its 128 rows and half of the features, 64 bytes of operands a clock of MMA
 // time where a CTA alone would need 96, and the L2 gives an SM about 64.  Here the
-// rows are the MMA's M: a lane holds a row's consecutive features, which it
-// stores 32 bytes at a time and which are whole blocks of a 4-bit output; nothing
-// passes through shared memory, whose bandwidth the MMAs and the loads use up
-// (128 of 128 bytes a clock at the full rate).  One
-// pair for every two SMs walks over the tiles; roles by warp:
+// rows are the MMA's M: a lane holds a row's consecutive features, whole blocks of
+// a 4-bit output.  One pair for every two SMs walks over the tiles; roles by warp:
 //   4     loads: codes complete on the first CTA's barriers, each CTA's scales on its own
 //   0-3   bring a stage's scales from shared memory into TMEM (tcgen05.st, each warp
 //         its lane quadrant): tcgen05.cp takes 97 clocks for 512 bytes, six of them a stage,
 //         and little of it beside the MMAs (four MMAs 513 clocks, with six copies 860)
 //   5     issues the MMAs (first CTA)
-//   8-15  finish: their 128 columns into registers at once, bias, ReLU, rounding, stores
+//   8-15  finish: their 128 columns into registers at once, bias, ReLU, rounding, bulk
+//         stores from shared memory
 // A second accumulator would leave no TMEM columns for the scales: the next tile's
 // MMAs start once the sums are in registers.
 constexpr int kPairThreads = 512;
-constexpr int kPairStages = 6;
+constexpr int kPairStages = 5;
+constexpr int kPairStaged = 4096;                          // a finishing warp's tile of outputs
 constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows or features
 constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // x, w, scales of 128 rows and 256 features
-constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 8 * 512 + 1024 + 512;   // + biases
+constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 8 * (kPairStaged + 512) + 1024 + 512;
 static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448, "shared memory");
 constexpr uint32_t kPairSf = 256, kPairSfCols = 24;        // a stage's scales in TMEM: x's 8, w's 16
 static_assert(kPairSf + kPairStages * kPairSfCols <= 512, "TMEM");
@@ -381,27 +382,9 @@ __device__ __forceinline__ float relu_nan(float x) {   // max(x, 0), NaN stays
   return r;
 }
 
-// 32 bytes of a row in one store (the address 32-byte aligned) or two (16).
-__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8], bool whole) {
-  if (!AGN_BOUNDS_OK(p, 32)) {
-    AGN_BOUNDS_FAIL(p);
-  } else if (whole) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]),
-                 "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-  } else {
-    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-  }
-}
-
-// Features f .. f + 31 of row r from their sums: bias (theirs, in shared memory; null:
-// none), ReLU, rounding, store.  `row`: the row exists.  f < out (4-bit outputs: or
-// in its last scale tile).
-__device__ __forceinline__ void finish_row(const LinearArgs& a, const float* bias, int64_t r, bool row,
-                                           int64_t f, uint32_t (&s)[32]) {
-  const bool full = f + 32 <= a.out;   // (the same for the warp)
-  float v[32];
+// Bias (32 values in shared memory, or null) and ReLU on a row's 32 consecutive sums.
+__device__ __forceinline__ void activate(const LinearArgs& a, const float* bias, uint32_t (&s)[32],
+                                         float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(s[i]);
   if (bias) {
@@ -415,74 +398,135 @@ __device__ __forceinline__ void finish_row(const LinearArgs& a, const float* bia
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = relu_nan(v[i]);
   }
-  if (a.dtype == AGN_PREC_MX4) {
-    uint32_t amax = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (!full && f + i >= a.out) v[i] = 0.f;
-      amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+}
+
+// 16-byte piece c of a lane's row in a staged tile of rows of kRow bytes, swizzled as
+// the output's tensor map says (128: by row mod 8, 64: by row / 2 mod 4): eight lanes
+// write eight different bank groups.
+template <int kRow>
+__device__ __forceinline__ uint4* staged_at(uint8_t* tile, int lane, int c) {
+  const int sw = kRow == 128 ? lane & 7 : (lane >> 1) & 3;
+  return reinterpret_cast<uint4*>(tile + lane * kRow + ((c ^ sw) << 4));
+}
+
+// A warp's 32 rows x 128 features of one tile to y by bulk stores from its staged tile
+// (4 KB): a store instruction of 32 rows takes the load/store unit about 64 clocks
+// whatever its width, a bulk store none.  kOut: AGN_PREC_*.
+template <int kOut>
+__device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMap* tmY, uint8_t* tile,
+                                           const float* bias, int64_t r0, int64_t f0, int lane,
+                                           uint32_t (&s)[4][32]) {
+  auto reuse = [&] {   // the bulk stores have read the tile
+    if (lane == 0) tc::bulk_wait_read();
+    __syncwarp();
+  };
+  auto send = [&](int x) {
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tc::tma_store_2d(tmY, tile, x, (int)r0);
+      tc::bulk_commit();
     }
-    const uint32_t code = mx_scale_code(amax);
-    const float inv = mx_inverse(code);
-    uint32_t q[4] = {0, 0, 0, 0};
-    if (code != 255) {
+  };
+  if (kOut == AGN_PREC_MX4) {
+    uint32_t word = 0;
+    reuse();
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        q[i >> 2] |= mx_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * (i & 3));
-    }
-    if (!row) return;
-    const int64_t kb = f / kMxBlock;
-    if (f < a.out)
-      AGN_ST(reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.y) + r * mx_row_bytes(a.out) + kb * 16),
-             make_uint4(q[0], q[1], q[2], q[3]));
-    AGN_ST(a.y_scales + mx_scale_at(r, kb, a.y_tiles_k), (uint8_t)code);
-  } else if (!row) {
-    return;
-  } else if (a.dtype == AGN_PREC_BF16) {
-    bf16* p = static_cast<bf16*>(a.y) + r * a.ldy + f;
-    if (full && a.vec) {
+    for (int c = 0; c < 4; ++c) {   // a block each
+      float v[32];
+      activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
+      uint32_t amax = 0;
+      const int n = (int)max((int64_t)0, min((int64_t)32, a.out - f0 - 32 * c));   // (warp-uniform)
+      if (n < 32) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 16) {
-        uint32_t w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const __nv_bfloat162 o = __floats2bfloat162_rn(v[i + 2 * j], v[i + 2 * j + 1]);
-          w[j] = *reinterpret_cast<const uint32_t*>(&o);
-        }
-        store32(p + i, w, a.vec == 2);
+        for (int i = 0; i < 32; ++i)
+          if (i >= n) v[i] = 0.f;
       }
-    } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (f + i < a.out) AGN_ST(p + i, __float2bfloat16_rn(v[i]));
+      for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+      const uint32_t code = mx_scale_code(amax);
+      const float inv = mx_inverse(code);
+      uint32_t q[4] = {0, 0, 0, 0};
+      if (code != 255) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          q[i >> 2] |= mx_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * (i & 3));
+      }
+      word |= code << (8 * c);
+      *staged_at<64>(tile, lane, c) = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+    send((int)(f0 / 2));
+    if (r0 + lane < a.rows)
+      AGN_ST(reinterpret_cast<uint32_t*>(a.y_scales + mx_scale_at(r0 + lane, f0 / kMxBlock, a.y_tiles_k)),
+             word);
+  } else if (kOut == AGN_PREC_BF16) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {   // 64 features: 128 bytes of a row
+      if (f0 + 64 * p >= a.bulk_out) break;
+      reuse();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float v[32];
+        activate(a, bias ? bias + 64 * p + 32 * c : nullptr, s[2 * p + c], v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* u = v + 8 * j;
+          const __nv_bfloat162 o[4] = {__floats2bfloat162_rn(u[0], u[1]), __floats2bfloat162_rn(u[2], u[3]),
+                                       __floats2bfloat162_rn(u[4], u[5]), __floats2bfloat162_rn(u[6], u[7])};
+          *staged_at<128>(tile, lane, 4 * c + j) = *reinterpret_cast<const uint4*>(o);
+        }
+      }
+      send((int)(f0 + 64 * p));
     }
   } else {
-    float* p = static_cast<float*>(a.y) + r * a.ldy + f;
-    if (full && a.vec) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 8) {
-        uint32_t w[8];
+    for (int c = 0; c < 4; ++c) {   // 32 features
+      if (f0 + 32 * c >= a.bulk_out) break;
+      float v[32];
+      activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
+      reuse();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[i + j]);
-        store32(p + i, w, a.vec == 2);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (f + i < a.out) AGN_ST(p + i, v[i]);
+      for (int j = 0; j < 8; ++j)
+        *staged_at<128>(tile, lane, j) =
+            make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
+                       __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+      send((int)(f0 + 32 * c));
     }
   }
 }
 
+// The same one by one, features `from` and up: for rows of y that do not start 16-byte
+// aligned, which bulk stores need, and for the last few of a row, since a bulk store
+// writes pieces of 16 bytes.
+template <int kOut>
+__device__ __forceinline__ void store_elements(const LinearArgs& a, const float* bias, int64_t r,
+                                               int64_t f0, int64_t from, uint32_t (&s)[4][32]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    float v[32];
+    activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int64_t f = f0 + 32 * c + i;
+      if (f < from || f >= a.out || r >= a.rows) continue;
+      if (kOut == AGN_PREC_BF16) AGN_ST(static_cast<bf16*>(a.y) + r * a.ldy + f, __float2bfloat16_rn(v[i]));
+      else AGN_ST(static_cast<float*>(a.y) + r * a.ldy + f, v[i]);
+    }
+  }
+}
+
+template <int kOut>
 __global__ void __launch_bounds__(kPairThreads, 1)
 mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                        const __grid_constant__ CUtensorMap tmWs,
-                       const __grid_constant__ CUtensorMap tmXs, const LinearArgs a, int tiles_f,
+                       const __grid_constant__ CUtensorMap tmXs,
+                       const __grid_constant__ CUtensorMap tmY, const LinearArgs a, int tiles_f,
                        int tiles) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  float* biases = reinterpret_cast<float*>(smem + kPairStages * kPairStage);   // [finishing warp][128]
+  uint8_t* staged = smem + kPairStages * kPairStage;                           // [finishing warp][4 KB]
+  float* biases = reinterpret_cast<float*>(staged + 8 * kPairStaged);          // [finishing warp][128]
   // first CTA's: both CTAs' codes in shared memory and scales in TMEM
   uint64_t* full = reinterpret_cast<uint64_t*>(biases + 8 * 128);
   uint64_t* empty = full + kPairStages;
@@ -532,13 +576,12 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     const int q = warp & 3, half = (warp - 8) >> 2;
     const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
     float* bias = biases + 128 * (warp - 8);
-    // 4-bit outputs: blocks past the row's last in its last scale tile are written too
-    const int64_t end = a.dtype == AGN_PREC_MX4 ? a.y_tiles_k * 128 : a.out;
+    uint8_t* tile = staged + (warp - 8) * kPairStaged;
     bool ok = true;
     int done = 0;
     for (int t = pair; t < tiles; t += pairs, ++done) {
       const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * half;
-      const int64_t r = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q + lane;
+      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q;
       if (a.bias) {   // (on its way while the sums are)
         float b[4];
 #pragma unroll
@@ -569,12 +612,14 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
 #pragma unroll
         for (int i = 0; i < 128; ++i) v[i / 32][i % 32] = 0x7fc00000u;
       }
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int64_t f = f0 + 32 * c;
-        if (f < end) finish_row(a, a.bias ? bias + 32 * c : nullptr, r, r < a.rows, f, v[c]);
+      if (f0 < a.out && r0 < a.rows) {   // (warp-uniform)
+        const float* b = a.bias ? bias : nullptr;
+        if (f0 < a.bulk_out) store_rows<kOut>(a, &tmY, tile, b, r0, f0, lane, v);
+        if (kOut != AGN_PREC_MX4 && f0 + 128 > a.bulk_out && a.out > a.bulk_out)
+          store_elements<kOut>(a, b, r0 + lane, f0, a.bulk_out, v);
       }
     }
+    if (lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
   } else if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // a stage's scales: lane l holds words j (rows 32 j + l) of every tile; the
@@ -699,8 +744,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   if (warp == 5) tc::tmem_dealloc_pair(tmem, 512);
 }
 
+template <int kOut>
 Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStream_t st) {
-  CUtensorMap tw, tx, tws, txs;
+  CUtensorMap tw, tx, tws, txs, ty{};
   const int64_t rb = mx_row_bytes(m.in);
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, rb, m.out, rb, 128));
   AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, rb, m.rows, rb, 128));
@@ -708,13 +754,19 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStr
   AGN_TRY(make_tmap_u32_3d(&tws, m.w_scales, kMxTileBytes / 4, a.tiles_k,
                            ceil_div(m.out, kMxTileRows), 2, 2));
   AGN_TRY(make_tmap_u32_3d(&txs, m.x_scales, kMxTileBytes / 4, a.tiles_k, a.row_tiles, 2, 1));
-  auto kern = mx4_linear_pair_kernel;
+  if (kOut == AGN_PREC_MX4)
+    AGN_TRY(make_tmap_store_2d(&ty, m.y, 1, mx_row_bytes(m.out), m.rows, mx_row_bytes(m.out), 64, 32));
+  else if (a.vec)
+    AGN_TRY(make_tmap_store_2d(&ty, m.y, (int)dtype_size(kOut), a.bulk_out, m.rows, m.ldy,
+                               128 / (int)dtype_size(kOut), 32));
+  auto kern = mx4_linear_pair_kernel<kOut>;
   AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)kPairSmem));
   const int64_t tiles_f = ceil_div(m.out, 256), tiles = tiles_f * ceil_div(m.rows, 256);
   const int64_t pairs = std::min<int64_t>(tiles, sms / 2);
   AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem,
-                                  dim3(2, 1, 1), st, tw, tx, tws, txs, a, (int)tiles_f, (int)tiles));
+                                  dim3(2, 1, 1), st, tw, tx, tws, txs, ty, a, (int)tiles_f,
+                                  (int)tiles));
   AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }
@@ -736,10 +788,15 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.y_tiles_k = mx_tiles_k(m.out);
   a.err = m.err;
   const uint64_t rows_at = reinterpret_cast<uintptr_t>(m.y) | (uint64_t)m.ldy * dtype_size(m.dtype);
-  a.vec = m.dtype == AGN_PREC_MX4 ? 0 : rows_at % 32 == 0 ? 2 : rows_at % 16 == 0 ? 1 : 0;
+  a.vec = m.dtype != AGN_PREC_MX4 && rows_at % 16 == 0;
+  a.bulk_out = m.dtype == AGN_PREC_MX4 ? m.out
+               : a.vec                 ? m.out / (16 / (int64_t)dtype_size(m.dtype)) * (16 / (int64_t)dtype_size(m.dtype))
+                                       : 0;
   const int sms = current_sms();
   if (m.rows > 256 && m.out > 128 && ceil_div(m.out, 256) * ceil_div(m.rows, 256) * 4 >= sms)
-    return launch_pair(m, a, sms, st);
+    return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, sms, st)
+           : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, sms, st)
+                                      : launch_pair<AGN_PREC_MX4>(m, a, sms, st);
   const int bn = m.rows <= 16 ? 16 : m.rows <= 32 ? 32 : m.rows <= 64 ? 64 : m.rows <= 1024 ? 128 : 256;
   const int64_t tiles = ceil_div(m.out, 128) * ceil_div(m.rows, bn);
   const int kt = (a.k_steps + 3) / 4;
