@@ -409,13 +409,13 @@ __device__ __forceinline__ uint4* staged_at(uint8_t* tile, int lane, int c) {
   return reinterpret_cast<uint4*>(tile + lane * kRow + ((c ^ sw) << 4));
 }
 
-// A warp's 32 rows x 128 features of one tile to y by bulk stores from its staged tile
+// A warp's 32 rows x 128 (32 chunks) features of one tile to y by bulk stores from its staged tile
 // (4 KB): a store instruction of 32 rows takes the load/store unit about 64 clocks
 // whatever its width, a bulk store none.  kOut: AGN_PREC_*.
 template <int kOut>
 __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMap* tmY, uint8_t* tile,
-                                           const float* bias, int64_t r0, int64_t f0, int lane,
-                                           uint32_t (&s)[4][32]) {
+                                           const float* bias, int64_t r0, int64_t f0, int chunks,
+                                           int lane, uint32_t (&s)[4][32]) {
   auto reuse = [&] {   // the bulk stores have read the tile
     if (lane == 0) tc::bulk_wait_read();
     __syncwarp();
@@ -462,7 +462,7 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
   } else if (kOut == AGN_PREC_BF16) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {   // 64 features: 128 bytes of a row
-      if (f0 + 64 * p >= a.bulk_out) break;
+      if (2 * p >= chunks || f0 + 64 * p >= a.bulk_out) break;
       reuse();
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -481,7 +481,7 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
   } else {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {   // 32 features
-      if (f0 + 32 * c >= a.bulk_out) break;
+      if (c >= chunks || f0 + 32 * c >= a.bulk_out) break;
       float v[32];
       activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
       reuse();
@@ -500,9 +500,11 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
 // writes pieces of 16 bytes.
 template <int kOut>
 __device__ __forceinline__ void store_elements(const LinearArgs& a, const float* bias, int64_t r,
-                                               int64_t f0, int64_t from, uint32_t (&s)[4][32]) {
+                                               int64_t f0, int chunks, int64_t from,
+                                               uint32_t (&s)[4][32]) {
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
+    if (c >= chunks) break;
     float v[32];
     activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
 #pragma unroll
@@ -515,13 +517,26 @@ __device__ __forceinline__ void store_elements(const LinearArgs& a, const float*
   }
 }
 
+// Unit u of the work: a tile, or (from tile n_whole on) half of one, 128 of its features, so
+// that a last round of few tiles occupies twice the pairs for half the time.
+struct PairUnit {
+  int f, n;      // first feature, first row
+  bool narrow;   // 128 features
+  __device__ __forceinline__ PairUnit(int u, int tiles_f, int n_whole) {
+    narrow = u >= n_whole;
+    const int t = narrow ? n_whole + (u - n_whole) / 2 : u;
+    f = (t % tiles_f) * 256 + (narrow ? ((u - n_whole) & 1) * 128 : 0);
+    n = (t / tiles_f) * 256;
+  }
+};
+
 template <int kOut>
 __global__ void __launch_bounds__(kPairThreads, 1)
 mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                        const __grid_constant__ CUtensorMap tmWs,
                        const __grid_constant__ CUtensorMap tmXs,
                        const __grid_constant__ CUtensorMap tmY, const LinearArgs a, int tiles_f,
-                       int tiles) {
+                       int n_whole, int units) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -579,9 +594,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     uint8_t* tile = staged + (warp - 8) * kPairStaged;
     bool ok = true;
     int done = 0;
-    for (int t = pair; t < tiles; t += pairs, ++done) {
-      const int64_t f0 = (int64_t)(t % tiles_f) * 256 + 128 * half;
-      const int64_t r0 = (int64_t)(t / tiles_f) * 256 + 128 * cta + 32 * q;
+    for (int t = pair; t < units; t += pairs, ++done) {
+      const PairUnit unit(t, tiles_f, n_whole);
+      const int chunks = unit.narrow ? 2 : 4;   // of 32 features
+      const int64_t f0 = unit.f + 32 * chunks * half;
+      const int64_t r0 = (int64_t)unit.n + 128 * cta + 32 * q;
       if (a.bias) {   // (on its way while the sums are)
         float b[4];
 #pragma unroll
@@ -601,9 +618,10 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
       uint32_t v[4][32];
       if (ok) {
-        const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(128 * half);
+        const uint32_t col = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(32 * chunks * half);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tc::tmem_ld_32x32b_x32(col + 32 * c, v[c]);
+        for (int c = 0; c < 4; ++c)
+          if (c < chunks) tc::tmem_ld_32x32b_x32(col + 32 * c, v[c]);
         tc::tmem_ld_wait();
         tc::tc_fence_before();
         __syncwarp();
@@ -614,9 +632,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
       if (f0 < a.out && r0 < a.rows) {   // (warp-uniform)
         const float* b = a.bias ? bias : nullptr;
-        if (f0 < a.bulk_out) store_rows<kOut>(a, &tmY, tile, b, r0, f0, lane, v);
-        if (kOut != AGN_PREC_MX4 && f0 + 128 > a.bulk_out && a.out > a.bulk_out)
-          store_elements<kOut>(a, b, r0 + lane, f0, a.bulk_out, v);
+        if (f0 < a.bulk_out) store_rows<kOut>(a, &tmY, tile, b, r0, f0, chunks, lane, v);
+        if (kOut != AGN_PREC_MX4 && f0 + 32 * chunks > a.bulk_out && a.out > a.bulk_out)
+          store_elements<kOut>(a, b, r0 + lane, f0, chunks, a.bulk_out, v);
       }
     }
     if (lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
@@ -629,7 +647,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int t = pair; t < tiles && ok; t += pairs) {
+    for (int t = pair; t < units && ok; t += pairs) {
       for (int kt = 0; kt < KT; ++kt) {
         ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], phase, abort_flag));
         if (!ok) break;
@@ -663,8 +681,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       const uint32_t full0 = tc::map_cluster(full, 0);
       int s = 0, n_armed = 0;
       uint32_t phase = 1;   // (the first round finds every stage free)
-      for (int t = pair; t < tiles && !*abort_flag; t += pairs) {
-        const int f = (t % tiles_f) * 256, n = (t / tiles_f) * 256 + 128 * cta;
+      for (int t = pair; t < units && !*abort_flag; t += pairs) {
+        const PairUnit unit(t, tiles_f, n_whole);
+        const int f = unit.f, n = unit.n + 128 * cta, fb = f + (unit.narrow ? 64 : 128) * cta;
         for (int kt = 0; kt < KT; ++kt) {
           if (!wait_pair<false>(&empty[s], phase, abort_flag)) {
             *abort_flag = 1;
@@ -677,7 +696,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           tc::tma_load_3d(st + 2 * kPairHalf + kSfBytes, &tmWs, &scales_in[s], 0, 2 * kt, f >> 7);
           if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
           tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
-          tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, f + 128 * cta);
+          tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, fb);
           n_armed = min(n_armed + 1, kPairStages);
           if (++s == kPairStages) s = 0, phase ^= 1;
         }
@@ -702,7 +721,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       int s = 0, done = 0;
       uint32_t phase = 0;
       bool ready = false;
-      for (int t = pair; t < tiles; t += pairs, ++done) {
+      for (int t = pair; t < units; t += pairs, ++done) {
+        const uint32_t id0 = t >= n_whole ? tc::idesc_mxf4(256, 128, 0) : tc::idesc_mxf4(256, 256, 0);
+        const uint32_t id2 = t >= n_whole ? tc::idesc_mxf4(256, 128, 2) : tc::idesc_mxf4(256, 256, 2);
         if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
         for (int left = a.k_steps; left > 0; left -= 4) {
           if (!ready && !wait_pair<false>(&full[s], phase, abort_flag)) {
@@ -711,9 +732,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           }
           tc::tc_fence_after();
           const bool first = left == a.k_steps;
-          tc::mma_mxf4_pair(tmem, da, da + kToB, tc::idesc_mxf4(256, 256, 0), sf, sf + 8, !first);
+          tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, !first);
           if (left > 1)
-            tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, tc::idesc_mxf4(256, 256, 2), sf, sf + 8, 1);
+            tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
           uint64_t* const mine = &empty[s];
           const uint64_t d = da + 4;
           const uint32_t sf1 = sf;
@@ -722,9 +743,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           if (++s == kPairStages) s = 0, phase ^= 1, da = da0, sf = tmem + kPairSf;
           ready = tc::mbar_test_wait(&full[s], phase);
           if (left > 2)
-            tc::mma_mxf4_pair(tmem, d, d + kToB, tc::idesc_mxf4(256, 256, 0), sf1 + 4, sf1 + 16, 1);
+            tc::mma_mxf4_pair(tmem, d, d + kToB, id0, sf1 + 4, sf1 + 16, 1);
           if (left > 3)
-            tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, tc::idesc_mxf4(256, 256, 2), sf1 + 4, sf1 + 16, 1);
+            tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, id2, sf1 + 4, sf1 + 16, 1);
           tc::mma_commit_pair(mine);
         }
         if (*abort_flag) {
@@ -763,10 +784,13 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStr
   AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)kPairSmem));
   const int64_t tiles_f = ceil_div(m.out, 256), tiles = tiles_f * ceil_div(m.rows, 256);
-  const int64_t pairs = std::min<int64_t>(tiles, sms / 2);
+  // the last round in halves where they fit (4-bit outputs: a warp's scales are whole words)
+  const int64_t most = sms / 2, rest = tiles % most;
+  const int64_t halves = kOut != AGN_PREC_MX4 && 2 * rest <= most ? rest : 0;
+  const int64_t units = tiles + halves, pairs = std::min(units, most);
   AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem,
                                   dim3(2, 1, 1), st, tw, tx, tws, txs, ty, a, (int)tiles_f,
-                                  (int)tiles));
+                                  (int)(tiles - halves), (int)units));
   AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }
