@@ -19,6 +19,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "mlp.cuh"
 #include "mlp_tc.cuh"
 #include "mx4.cuh"
@@ -33,22 +35,51 @@ constexpr int kThreads = 256;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int kABytes = 128 * 128;
 constexpr int kSfBytes = 2 * kMxTileBytes; // a stage's scales of 128 rows
-constexpr int kMaxSplit = 8;               // portable cluster size
+
+// Shared memory that keeps every other kernel with TMEM off the SM (the library's take
+// 47 KB and more): CTAs of one launch wait for each other, and one that holds TMEM
+// while it waits for a CTA that another launch's CTA keeps from allocating, and the other
+// way round, would wait for ever.
+constexpr size_t kAlone = 184 * 1024;
 
 template <int BN>
 struct Tile {
   static constexpr int kBBytes = BN * 128;
-  static constexpr int kSfTiles = BN > 128 ? 2 : 1;   // 128-row scale tiles of the rows of x
-  static constexpr int kStageBytes = kABytes + kBBytes + kSfBytes * (1 + kSfTiles);
-  static constexpr int kStages = BN <= 32 ? 8 : BN == 64 ? 7 : BN == 128 ? 6 : 4;
+  static constexpr int kStageBytes = kABytes + kBBytes + 2 * kSfBytes;
+  static constexpr int kStages = BN <= 32 ? 8 : BN == 64 ? 7 : 6;
   static constexpr uint32_t kSfCol = BN < 32 ? 32 : BN;   // first TMEM column of the scales
-  static constexpr uint32_t kCols = kSfCol + 8 + 8 * kSfTiles;
-  static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + 256;
+  static constexpr uint32_t kCols = kSfCol + 16;
+  static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
+  static constexpr size_t kNeeded = (size_t)kStages * kStageBytes + 1024 + 256;
+  static constexpr size_t kSmem = kNeeded < kAlone ? kAlone : kNeeded;
   static_assert(kStageBytes % 1024 == 0, "tiles of the 128-byte swizzle");
   static_assert(kSmem <= 232448, "shared memory");
   static_assert(BN * 128 * 4 <= kStages * kStageBytes, "the sums fit into the ring");
 };
+
+// Bounded waits that give up when another role of the CTA has: kTmem for barriers
+// that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
+template <bool kTmem>
+__device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    uint32_t got;
+    if (kTmem)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    else
+      got = tc::mbar_try_wait(bar, parity);
+    if (got) return true;
+    if ((it & 63) == 0) {
+      const uint64_t now = tc::globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (*abort_flag || now - t0 > kWaitNs) return false;
+    }
+  }
+}
 
 struct LinearArgs {
   const uint8_t *w_scales, *x_scales;
@@ -148,17 +179,17 @@ __device__ __forceinline__ void load_scales(void* dst, const uint8_t* src, uint3
 }
 
 template <int BN>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads)
 mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                   const LinearArgs a) {
   using Cfg = Tile<BN>;
-  constexpr int kStages = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * Cfg::kStageBytes);
-  uint64_t* empty = full + kStages;
-  uint64_t* done = empty + kStages;
+  constexpr int stages = Cfg::kStages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + stages * Cfg::kStageBytes);
+  uint64_t* empty = full + stages;
+  uint64_t* done = empty + stages;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
@@ -169,7 +200,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   const int kt0 = rank * kt_per, KT = min(KT_all, kt0 + kt_per) - kt0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       tc::mbar_init(&full[s], 1);
       tc::mbar_init(&empty[s], 1);
     }
@@ -190,70 +221,75 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   pdl_begin();
 
   if (warp == 0 && lane == 0) {
-    const int64_t xt0 = n0 >> 7;   // first 128-row scale tile of x
-    const int xt = (int)min((int64_t)Cfg::kSfTiles, a.row_tiles - xt0);
-    int kt = 0;
-    for (; kt < KT; ++kt) {
-      const int s = kt % kStages;
-      if (kt >= kStages && !tc::wait_or_abort(&empty[s], ((kt / kStages) - 1) & 1, abort_flag, kWaitNs)) {
+    const int64_t xt = n0 >> 7;   // 128-row scale tile of x
+    int s = 0, armed = 0;
+    uint32_t phase = 1;   // (the first round finds every stage free)
+    for (int kg = kt0; kg < kt0 + KT; ++kg) {   // stages along the whole K
+      if (!wait_mbar<false>(&empty[s], phase, abort_flag)) {
         *abort_flag = 1;
         break;
       }
-      if (*abort_flag) break;
       uint8_t* st = smem + s * Cfg::kStageBytes;
       uint8_t* sf = st + kABytes + Cfg::kBBytes;
-      const int kg = kt0 + kt;   // stage along the whole K
       const uint32_t sfb = (uint32_t)min((int64_t)2, a.tiles_k - 2 * kg) * kMxTileBytes;
-      tc::mbar_arrive_expect_tx(&full[s], kABytes + Cfg::kBBytes + sfb * (1 + xt));
+      tc::mbar_arrive_expect_tx(&full[s], kABytes + Cfg::kBBytes + 2 * sfb);
       tc::tma_load_2d(st, &tmW, &full[s], kg * 128, (int)f0);
       tc::tma_load_2d(st + kABytes, &tmX, &full[s], kg * 128, (int)n0);
       load_scales(sf, a.w_scales + ((int64_t)blockIdx.x * a.tiles_k + 2 * kg) * kMxTileBytes, sfb,
                   &full[s]);
-      for (int t = 0; t < xt; ++t)
-        load_scales(sf + kSfBytes * (1 + t),
-                    a.x_scales + ((xt0 + t) * a.tiles_k + 2 * kg) * kMxTileBytes, sfb, &full[s]);
+      load_scales(sf + kSfBytes, a.x_scales + (xt * a.tiles_k + 2 * kg) * kMxTileBytes, sfb, &full[s]);
+      armed = min(armed + 1, stages);
+      if (++s == stages) s = 0, phase ^= 1;
     }
     if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
-      for (int j = kt - 1; j >= 0 && j >= kt - kStages; --j)
-        tc::mbar_wait_bounded(&full[j % kStages], (j / kStages) & 1, kWaitNs);
+      for (; armed > 0; --armed) {
+        if (--s < 0) s = stages - 1, phase ^= 1;
+        tc::mbar_wait_bounded(&full[s], phase ^ 1, kWaitNs);
+      }
   } else if (warp == 1 && lane == 0) {
+    // (short between the MMAs: see the pairs' kernel)
     const uint32_t sfa = tmem + Cfg::kSfCol, sfb = sfa + 8;
-    const uint32_t shift = (uint32_t)(n0 & 127) / 32;   // BN = 64: the tile's half of 128 rows
-    for (int kt = 0; kt < KT; ++kt) {
-      const int s = kt % kStages;
-      if (!tc::wait_or_abort(&full[s], (kt / kStages) & 1, abort_flag, kWaitNs)) {
+    const uint32_t s0 = tc::smem_u32(smem);
+    const uint64_t da0 = tc::smem_desc_sw128(s0, 16, 1024);
+    const uint64_t ds0 = tc::smem_desc_rows16(s0 + kABytes + Cfg::kBBytes, 128);
+    constexpr uint64_t kToB = kABytes >> 4, kTile = kMxTileBytes >> 4, kToX = kSfBytes >> 4;
+    uint64_t da = da0, ds = ds0;
+    int s = 0;
+    uint32_t phase = 0;
+    bool ready = false;
+    for (int left = min(a.k_steps - 4 * kt0, 4 * KT), first = 1; left > 0; left -= 4, first = 0) {
+      if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
         *abort_flag = 1;
         break;
       }
       tc::tc_fence_after();
-      const uint32_t sa = tc::smem_u32(smem + s * Cfg::kStageBytes), sb = sa + kABytes;
-      const uint32_t ss = sb + Cfg::kBBytes;
-      const int steps = min(4, a.k_steps - 4 * (kt0 + kt));
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {   // scale words: blocks 4 q .. 4 q + 3 of the stage
-        if (2 * q >= steps) break;
-        tc::cp_32x128b_warpx4(sfa + 4 * q, tc::smem_desc_rows16(ss + q * kMxTileBytes, 128));
-#pragma unroll
-        for (int t = 0; t < Cfg::kSfTiles; ++t)
-          tc::cp_32x128b_warpx4(sfb + 4 * (Cfg::kSfTiles * q + t),
-                                tc::smem_desc_rows16(ss + kSfBytes * (1 + t) + q * kMxTileBytes, 128));
+      // scale words: blocks 0-3 of the stage, then 4-7
+      tc::cp_32x128b_warpx4(sfa, ds);
+      tc::cp_32x128b_warpx4(sfb, ds + kToX);
+      if (left > 2) {
+        tc::cp_32x128b_warpx4(sfa + 4, ds + kTile);
+        tc::cp_32x128b_warpx4(sfb + 4, ds + kToX + kTile);
       }
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if (kk >= steps) break;
-        const int q = kk >> 1;
-        tc::mma_mxf4(tmem, tc::smem_desc_sw128(sa + kk * 32, 16, 1024),
-                     tc::smem_desc_sw128(sb + kk * 32, 16, 1024),
-                     (kk & 1) ? tc::idesc_mxf4(128, BN, 2) : tc::idesc_mxf4(128, BN, 0),
-                     sfa + 4 * q, sfb + 4 * Cfg::kSfTiles * q + shift, (kt | kk) != 0);
-      }
-      tc::mma_commit(&empty[s]);
+      tc::mma_mxf4(tmem, da, da + kToB, tc::idesc_mxf4(128, BN, 0), sfa, sfb, !first);
+      if (left > 1)
+        tc::mma_mxf4(tmem, da + 2, da + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa, sfb, 1);
+      uint64_t* const mine = &empty[s];
+      const uint64_t d = da + 4;
+      da += Cfg::kStageBytes >> 4;
+      ds += Cfg::kStageBytes >> 4;
+      if (++s == stages) s = 0, phase ^= 1, da = da0, ds = ds0;
+      ready = tc::mbar_test_wait(&full[s], phase);
+      if (left > 2)
+        tc::mma_mxf4(tmem, d, d + kToB, tc::idesc_mxf4(128, BN, 0), sfa + 4, sfb + 4, 1);
+      if (left > 3)
+        tc::mma_mxf4(tmem, d + 2, d + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa + 4, sfb + 4, 1);
+      tc::mma_commit(mine);
     }
     tc::mma_commit(done);
   }
   __syncwarp();
   const bool ok =
-      __syncthreads_and(tc::wait_or_abort(done, 0, abort_flag, kWaitNs) && !*abort_flag) != 0;
+      __syncthreads_and(wait_mbar<false>(done, 0, abort_flag) && !*abort_flag) != 0;
   tc::tc_fence_after();
   if (!ok && threadIdx.x == 0 && a.err) atomicExch(a.err, 1);
 
@@ -307,19 +343,29 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 }
 
 template <int BN>
-Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
+Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int sms, cudaStream_t st) {
+  using Cfg = Tile<BN>;
+  const dim3 grid0((unsigned)ceil_div(m.out, 128), (unsigned)ceil_div(m.rows, BN));
+  // CTAs along K: one to an SM, clusters of at most 4; of 8 where they are few (16
+  // of them take two rounds: one GPC holds two).  us, clusters of 8, 4, 2: one row of 4096 to
+  // 1000 4.9, 5.6, 7.4; 64 rows of 2048 to 2048 10.3, 5.7, 7.0
+  const int64_t tiles = (int64_t)grid0.x * grid0.y;
+  const int kt = (a.k_steps + 3) / 4;
+  const int64_t most = tiles * 8 <= 96 ? 8 : 4;
+  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({most, kt, sms / tiles}));
+  a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
   CUtensorMap tw, tx;
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, mx_row_bytes(m.in), m.out, mx_row_bytes(m.in), 128));
   AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, mx_row_bytes(m.in), m.rows, mx_row_bytes(m.in), BN));
   auto kern = mx4_linear_kernel<BN>;
-  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)Tile<BN>::kSmem));
-  const dim3 grid((unsigned)ceil_div(m.out, 128), (unsigned)ceil_div(m.rows, BN), (unsigned)a.split);
+  constexpr size_t smem = Cfg::kSmem;
+  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  const dim3 grid(grid0.x, grid0.y, (unsigned)a.split);
   if (a.split > 1)
-    AGN_TRY_CUDA(launch_pdl_cluster(kern, grid, kThreads, Tile<BN>::kSmem,
-                                    dim3(1, 1, (unsigned)a.split), st, tw, tx, a));
+    AGN_TRY_CUDA(launch_pdl_cluster(kern, grid, kThreads, smem, dim3(1, 1, (unsigned)a.split), st, tw,
+                                    tx, a));
   else
-    AGN_TRY_CUDA(launch_pdl(kern, grid, kThreads, Tile<BN>::kSmem, st, tw, tx, a));
+    AGN_TRY_CUDA(launch_pdl(kern, grid, kThreads, smem, st, tw, tx, a));
   AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }
@@ -348,33 +394,9 @@ constexpr int kPairStaged = 4096;                          // a finishing warp's
 constexpr int kPairHalf = 128 * 128;                       // codes of 128 rows or features
 constexpr int kPairStage = 2 * kPairHalf + 3 * kSfBytes;   // x, w, scales of 128 rows and 256 features
 constexpr size_t kPairSmem = (size_t)kPairStages * kPairStage + 8 * (kPairStaged + 512) + 1024 + 512;
-static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448, "shared memory");
+static_assert(kPairStage % 1024 == 0 && kPairSmem <= 232448 && kPairSmem >= kAlone, "shared memory");
 constexpr uint32_t kPairSf = 256, kPairSfCols = 24;        // a stage's scales in TMEM: x's 8, w's 16
 static_assert(kPairSf + kPairStages * kPairSfCols <= 512, "TMEM");
-
-// Bounded waits that give up when another role of the CTA has: kTmem for barriers
-// that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
-template <bool kTmem>
-__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  uint64_t t0 = 0;
-  for (uint32_t it = 1;; ++it) {
-    uint32_t got;
-    if (kTmem)
-      asm volatile(
-          "{\n\t.reg .pred p;\n\t"
-          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-          "selp.u32 %0, 1, 0, p;\n\t}"
-          : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
-    else
-      got = tc::mbar_try_wait(bar, parity);
-    if (got) return true;
-    if ((it & 63) == 0) {
-      const uint64_t now = tc::globaltimer_ns();
-      if (t0 == 0) t0 = now;
-      if (*abort_flag || now - t0 > kWaitNs) return false;
-    }
-  }
-}
 
 __device__ __forceinline__ float relu_nan(float x) {   // max(x, 0), NaN stays
   float r;
@@ -411,7 +433,9 @@ __device__ __forceinline__ uint4* staged_at(uint8_t* tile, int lane, int c) {
 
 // A warp's 32 rows x 128 (32 chunks) features of one tile to y by bulk stores from its staged tile
 // (4 KB): a store instruction of 32 rows takes the load/store unit about 64 clocks
-// whatever its width, a bulk store none.  kOut: AGN_PREC_*.
+// whatever its width, a bulk store none.  Where y's rows are not 16-byte aligned, and
+// where the last features of a row are no whole 16 bytes (the bulk store's pieces), the
+// warp stores the tile row by row.  kOut: AGN_PREC_*.
 template <int kOut>
 __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMap* tmY, uint8_t* tile,
                                            const float* bias, int64_t r0, int64_t f0, int chunks,
@@ -426,6 +450,23 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
     if (lane == 0) {
       tc::tma_store_2d(tmY, tile, x, (int)r0);
       tc::bulk_commit();
+    }
+  };
+  // a tile of kW features from f on, by a bulk store or row by row
+  using T = typename std::conditional<kOut == AGN_PREC_BF16, bf16, float>::type;
+  constexpr int kW = 128 / (int)sizeof(T);
+  auto put = [&](int64_t f) {
+    if (a.bulk_out == a.out || f + kW <= a.bulk_out) return send((int)f);
+    __syncwarp();
+    const int n = (int)min((int64_t)32, a.rows - r0);
+#pragma unroll
+    for (int e = 0; e < kW; e += 32) {
+      const int i = e + lane;   // this lane's feature
+      if (f + i >= a.out) break;
+      T* p = static_cast<T*>(a.y) + r0 * a.ldy + f + i;
+      for (int row = 0; row < n; ++row, p += a.ldy)
+        AGN_ST(p, *reinterpret_cast<const T*>(tile + row * 128 + (((i * (int)sizeof(T) >> 4) ^ (row & 7)) << 4) +
+                                              (i * (int)sizeof(T) & 15)));
     }
   };
   if (kOut == AGN_PREC_MX4) {
@@ -462,7 +503,7 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
   } else if (kOut == AGN_PREC_BF16) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {   // 64 features: 128 bytes of a row
-      if (2 * p >= chunks || f0 + 64 * p >= a.bulk_out) break;
+      if (2 * p >= chunks || f0 + 64 * p >= a.out) break;
       reuse();
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -476,12 +517,12 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
           *staged_at<128>(tile, lane, 4 * c + j) = *reinterpret_cast<const uint4*>(o);
         }
       }
-      send((int)(f0 + 64 * p));
+      put(f0 + 64 * p);
     }
   } else {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {   // 32 features
-      if (c >= chunks || f0 + 32 * c >= a.bulk_out) break;
+      if (c >= chunks || f0 + 32 * c >= a.out) break;
       float v[32];
       activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
       reuse();
@@ -490,29 +531,7 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
         *staged_at<128>(tile, lane, j) =
             make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
                        __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
-      send((int)(f0 + 32 * c));
-    }
-  }
-}
-
-// The same one by one, features `from` and up: for rows of y that do not start 16-byte
-// aligned, which bulk stores need, and for the last few of a row, since a bulk store
-// writes pieces of 16 bytes.
-template <int kOut>
-__device__ __forceinline__ void store_elements(const LinearArgs& a, const float* bias, int64_t r,
-                                               int64_t f0, int chunks, int64_t from,
-                                               uint32_t (&s)[4][32]) {
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (c >= chunks) break;
-    float v[32];
-    activate(a, bias ? bias + 32 * c : nullptr, s[c], v);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int64_t f = f0 + 32 * c + i;
-      if (f < from || f >= a.out || r >= a.rows) continue;
-      if (kOut == AGN_PREC_BF16) AGN_ST(static_cast<bf16*>(a.y) + r * a.ldy + f, __float2bfloat16_rn(v[i]));
-      else AGN_ST(static_cast<float*>(a.y) + r * a.ldy + f, v[i]);
+      put(f0 + 32 * c);
     }
   }
 }
@@ -609,7 +628,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
         __syncwarp();
       }
-      ok = ok && wait_pair<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
+      ok = ok && wait_mbar<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
       ok = __all_sync(0xffffffffu, ok);
       tc::tc_fence_after();
       if (!ok && lane == 0) {
@@ -632,9 +651,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
       if (f0 < a.out && r0 < a.rows) {   // (warp-uniform)
         const float* b = a.bias ? bias : nullptr;
-        if (f0 < a.bulk_out) store_rows<kOut>(a, &tmY, tile, b, r0, f0, chunks, lane, v);
-        if (kOut != AGN_PREC_MX4 && f0 + 32 * chunks > a.bulk_out && a.out > a.bulk_out)
-          store_elements<kOut>(a, b, r0 + lane, f0, chunks, a.bulk_out, v);
+        store_rows<kOut>(a, &tmY, tile, b, r0, f0, chunks, lane, v);
       }
     }
     if (lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
@@ -649,7 +666,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     bool ok = true;
     for (int t = pair; t < units && ok; t += pairs) {
       for (int kt = 0; kt < KT; ++kt) {
-        ok = __all_sync(0xffffffffu, wait_pair<false>(&scales_in[s], phase, abort_flag));
+        ok = __all_sync(0xffffffffu, wait_mbar<false>(&scales_in[s], phase, abort_flag));
         if (!ok) break;
         const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
         uint32_t x[8], w[16];
@@ -685,7 +702,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         const PairUnit unit(t, tiles_f, n_whole);
         const int f = unit.f, n = unit.n + 128 * cta, fb = f + (unit.narrow ? 64 : 128) * cta;
         for (int kt = 0; kt < KT; ++kt) {
-          if (!wait_pair<false>(&empty[s], phase, abort_flag)) {
+          if (!wait_mbar<false>(&empty[s], phase, abort_flag)) {
             *abort_flag = 1;
             break;
           }
@@ -724,9 +741,9 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       for (int t = pair; t < units; t += pairs, ++done) {
         const uint32_t id0 = t >= n_whole ? tc::idesc_mxf4(256, 128, 0) : tc::idesc_mxf4(256, 256, 0);
         const uint32_t id2 = t >= n_whole ? tc::idesc_mxf4(256, 128, 2) : tc::idesc_mxf4(256, 256, 2);
-        if (done > 0 && !wait_pair<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
+        if (done > 0 && !wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
         for (int left = a.k_steps; left > 0; left -= 4) {
-          if (!ready && !wait_pair<false>(&full[s], phase, abort_flag)) {
+          if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
             *abort_flag = 1;
             break;
           }
@@ -777,7 +794,7 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStr
   AGN_TRY(make_tmap_u32_3d(&txs, m.x_scales, kMxTileBytes / 4, a.tiles_k, a.row_tiles, 2, 1));
   if (kOut == AGN_PREC_MX4)
     AGN_TRY(make_tmap_store_2d(&ty, m.y, 1, mx_row_bytes(m.out), m.rows, mx_row_bytes(m.out), 64, 32));
-  else if (a.vec)
+  else if (a.bulk_out > 0)
     AGN_TRY(make_tmap_store_2d(&ty, m.y, (int)dtype_size(kOut), a.bulk_out, m.rows, m.ldy,
                                128 / (int)dtype_size(kOut), 32));
   auto kern = mx4_linear_pair_kernel<kOut>;
@@ -817,22 +834,17 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
                : a.vec                 ? m.out / (16 / (int64_t)dtype_size(m.dtype)) * (16 / (int64_t)dtype_size(m.dtype))
                                        : 0;
   const int sms = current_sms();
-  if (m.rows > 256 && m.out > 128 && ceil_div(m.out, 256) * ceil_div(m.rows, 256) * 4 >= sms)
+  // Tiles of 256 x 256 by pairs of SMs from 257 rows on (us, pairs and 128-column tiles: 512 rows of
+  // 4096 to 4096 11.3 and 13.4, 1024 12.2 and 25.6, 10000 of 784 to 128 8.2 and 7.6; 200 of 4096
+  // to 1000 10.5 and 7.7), else the narrowest columns that hold the rows.
+  if (m.rows > 256)
     return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, sms, st)
            : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, sms, st)
                                       : launch_pair<AGN_PREC_MX4>(m, a, sms, st);
-  const int bn = m.rows <= 16 ? 16 : m.rows <= 32 ? 32 : m.rows <= 64 ? 64 : m.rows <= 1024 ? 128 : 256;
-  const int64_t tiles = ceil_div(m.out, 128) * ceil_div(m.rows, bn);
-  const int kt = (a.k_steps + 3) / 4;
-  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, kt, sms / tiles}));
-  a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
-  switch (bn) {
-    case 16: return launch_linear<16>(m, a, st);
-    case 32: return launch_linear<32>(m, a, st);
-    case 64: return launch_linear<64>(m, a, st);
-    case 128: return launch_linear<128>(m, a, st);
-    default: return launch_linear<256>(m, a, st);
-  }
+  return m.rows <= 16   ? launch_linear<16>(m, a, sms, st)
+         : m.rows <= 32 ? launch_linear<32>(m, a, sms, st)
+         : m.rows <= 64 ? launch_linear<64>(m, a, sms, st)
+                        : launch_linear<128>(m, a, sms, st);
 }
 
 namespace {
