@@ -603,10 +603,10 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  // The finishing warps hold 128 sums a thread: 2 x 128 threads x (72 + 184) registers
+  // The finishing warps hold 128 sums a thread: 2 x 128 threads x (48 + 208) registers
   // are the launch's 512 x 128.
   if (warp >= 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int q = warp & 3, half = (warp - 8) >> 2;
     const uint32_t empty_at = tc::map_cluster(sums_empty, 0);
     float* bias = biases + 128 * (warp - 8);
@@ -656,7 +656,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     }
     if (lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
   } else if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     // a stage's scales: lane l holds words j (rows 32 j + l) of every tile; the
     // stage was loaded again only after the MMAs that read its TMEM columns
     const uint32_t quadrant = (uint32_t)(32 * warp) << 16;
@@ -693,7 +693,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     }
     if (!ok && lane == 0) *abort_flag = 1;
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 4 && lane == 0) {
       const uint32_t full0 = tc::map_cluster(full, 0);
       int s = 0, n_armed = 0;
@@ -739,32 +739,34 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       uint32_t phase = 0;
       bool ready = false;
       for (int t = pair; t < units; t += pairs, ++done) {
-        const uint32_t id0 = t >= n_whole ? tc::idesc_mxf4(256, 128, 0) : tc::idesc_mxf4(256, 256, 0);
-        const uint32_t id2 = t >= n_whole ? tc::idesc_mxf4(256, 128, 2) : tc::idesc_mxf4(256, 256, 2);
         if (done > 0 && !wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
-        for (int left = a.k_steps; left > 0; left -= 4) {
-          if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
-            *abort_flag = 1;
-            break;
+        // (N a constant: the instruction descriptor is then one too)
+        auto mainloop = [&](auto columns) {
+          constexpr uint32_t id0 = tc::idesc_mxf4(256, decltype(columns)::value, 0);
+          constexpr uint32_t id2 = tc::idesc_mxf4(256, decltype(columns)::value, 2);
+          for (int left = a.k_steps; left > 0; left -= 4) {
+            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
+              *abort_flag = 1;
+              break;
+            }
+            tc::tc_fence_after();
+            const bool first = left == a.k_steps;
+            tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, !first);
+            if (left > 1) tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
+            uint64_t* const mine = &empty[s];
+            const uint64_t d = da + 4;
+            const uint32_t sf1 = sf;
+            da += kPairStage >> 4;
+            sf += kPairSfCols;
+            if (++s == kPairStages) s = 0, phase ^= 1, da = da0, sf = tmem + kPairSf;
+            ready = tc::mbar_test_wait(&full[s], phase);
+            if (left > 2) tc::mma_mxf4_pair(tmem, d, d + kToB, id0, sf1 + 4, sf1 + 16, 1);
+            if (left > 3) tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, id2, sf1 + 4, sf1 + 16, 1);
+            tc::mma_commit_pair(mine);
           }
-          tc::tc_fence_after();
-          const bool first = left == a.k_steps;
-          tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, !first);
-          if (left > 1)
-            tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
-          uint64_t* const mine = &empty[s];
-          const uint64_t d = da + 4;
-          const uint32_t sf1 = sf;
-          da += kPairStage >> 4;
-          sf += kPairSfCols;
-          if (++s == kPairStages) s = 0, phase ^= 1, da = da0, sf = tmem + kPairSf;
-          ready = tc::mbar_test_wait(&full[s], phase);
-          if (left > 2)
-            tc::mma_mxf4_pair(tmem, d, d + kToB, id0, sf1 + 4, sf1 + 16, 1);
-          if (left > 3)
-            tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, id2, sf1 + 4, sf1 + 16, 1);
-          tc::mma_commit_pair(mine);
-        }
+        };
+        if (t >= n_whole) mainloop(std::integral_constant<int, 128>());
+        else mainloop(std::integral_constant<int, 256>());
         if (*abort_flag) {
           // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
           // end before any memory goes
