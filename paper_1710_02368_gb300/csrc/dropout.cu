@@ -26,9 +26,12 @@ namespace agn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;      // rows of a thread whose loads are in flight together
-constexpr int kBlocksPerSm = 4;
-constexpr int kSumTxShift = 3;  // with sums: tiles of at most 8 units (128 bytes of a row)
+// Resident blocks of an SM and rows of a thread whose loads are in flight together, for one
+// input matrix or two and without or with column sums (more rows spill).  16384 x 4096 bf16,
+// us: two matrices 65 with (4, 2), 67 with (3, 3); with sums 82 and 74.
+constexpr int blocks_per_sm(bool two, bool sums) { return two && sums ? 3 : 4; }
+constexpr int unroll(bool two, bool sums) { return two ? (sums ? 3 : 2) : 4; }
+constexpr int kMaxUnits = 32;   // 16-byte units of a row in a block's tile
 
 struct DropArgs {
   const void* x;          // forward: input; backward: the layer's input (ReLU), or null
@@ -42,7 +45,7 @@ struct DropArgs {
   uint32_t t16;           // T << 16
   float scale;
   int relu, vec;          // vec: every row of every matrix starts 16-byte aligned
-  int tx_shift;           // log2 of the threads along a row
+  int tile_units;         // units of 16 bytes of a row in a block's tile: a thread each
   // hidden layers of a training run (kHidden): matrices [slots][rows][cols]
   const int* slot_worker;
   const long long* slot_t0;
@@ -64,8 +67,24 @@ __device__ __forceinline__ uint4 load16(const T* p, bool full, int n) {
   return q;
 }
 template <typename T>
-__device__ __forceinline__ float element(const uint4& q, int i) {
-  return static_cast<float>(reinterpret_cast<const T*>(&q)[i]);
+__device__ __forceinline__ float2 element2(const uint4& q, int i) {   // elements i and i + 1
+  const T* e = reinterpret_cast<const T*>(&q);
+  return make_float2(static_cast<float>(e[i]), static_cast<float>(e[i + 1]));
+}
+// Two fp32 operations of one instruction, each rounded to nearest.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
 }
 template <typename T>
 __device__ __forceinline__ void store16(T* p, bool full, int n, const float (&v)[16 / sizeof(T)]) {
@@ -82,36 +101,27 @@ __device__ __forceinline__ void store16(T* p, bool full, int n, const float (&v)
   }
 }
 
-// The keep mask of V consecutive elements from the draws of their groups of
-// four: number i0 of the stream, and i0 + 1 for V = 8.  The upper half of a word
-// compares as it is (u >= T iff word >= T << 16), the lower half shifted up.
-template <int V>
-__device__ __forceinline__ uint32_t keep_mask(uint64_t key, uint64_t i0, uint32_t t16) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int g = 0; g < V / 4; ++g) {
-    const uint64_t d = gen::draw(key, i0 + g);
-    const uint32_t w[2] = {(uint32_t)d, (uint32_t)(d >> 32)};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      m |= (w[h] << 16) >= t16 ? 1u << (4 * g + 2 * h) : 0u;
-      m |= w[h] >= t16 ? 2u << (4 * g + 2 * h) : 0u;
-    }
-  }
-  return m;
+// Whether element e of a draw's four is kept.  The upper half of a word compares as
+// it is (u >= T iff word >= T << 16), the lower half shifted up.
+__device__ __forceinline__ bool kept(uint64_t d, int e, uint32_t t16) {
+  const uint32_t w = (uint32_t)(e & 2 ? d >> 32 : d);
+  return (e & 1 ? w : w << 16) >= t16;
 }
 
-// A block: tiles of 2^tx_shift units of 16 bytes along the row (blockIdx.x) by
+// A block: tiles of tile_units units of 16 bytes along the row (blockIdx.x) by
 // rows_per_block rows (blockIdx.y); a thread keeps its columns (the bias stays
 // in registers) and steps down the rows.
-template <typename T, bool kBackward, bool kHidden>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) dropout_kernel(const DropArgs a) {
-  constexpr int V = 16 / sizeof(T);
+// kTwo: two input matrices (forward: x and the residual; backward: dy and the ReLU's x).
+// kSums: backward with the bias's gradient.
+template <typename T, bool kBackward, bool kTwo, bool kSums, bool kHidden = false>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_kernel(const DropArgs a) {
+  constexpr int V = 16 / sizeof(T), kUnroll = kHidden ? 2 : unroll(kTwo, kSums);
+  constexpr bool kReadX = !kBackward || kTwo, kReadExtra = kBackward || kTwo;
   pdl_begin();
-  const int tx = threadIdx.x & ((1 << a.tx_shift) - 1), ty = threadIdx.x >> a.tx_shift;
-  const int nty = kThreads >> a.tx_shift;
-  const int64_t c = (((int64_t)blockIdx.x << a.tx_shift) + tx) * V;
-  const int n = c < a.cols ? (int)min((int64_t)V, a.cols - c) : 0;   // elements of this thread
+  const int w = a.tile_units, ty = threadIdx.x / w, tx = threadIdx.x % w;
+  const int nty = kThreads / w;   // (threads past w nty have no rows)
+  const int64_t c = ((int64_t)blockIdx.x * w + tx) * V;
+  const int n = c < a.cols && ty < nty ? (int)min((int64_t)V, a.cols - c) : 0;   // its elements
   const bool full = a.vec && n == V;
   const int64_t r0 = blockIdx.y * a.rows_per_block;
   const int64_t r1 = min(a.rows, r0 + a.rows_per_block);
@@ -140,35 +150,54 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) dropout_kernel(const D
     sum[e] = 0.f;
   }
   if (n > 0) {
+    uint64_t z = key + (first + (uint64_t)(r0 + ty) * groups + 1) * gen::kG;
+    const uint64_t z_step = (uint64_t)nty * groups * gen::kG;
     for (int64_t r = r0 + ty; r < r1; r += (int64_t)kUnroll * nty) {
       uint4 v[kUnroll], q[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t ru = r + (int64_t)u * nty;
         if (ru >= r1) break;
-        if (!kBackward || a.relu) v[u] = load16(x + ru * a.ldx + c, full, n);
-        if (kBackward || extra) q[u] = load16(extra + ru * a.lde + c, full, n);
+        if (kReadX) v[u] = load16(x + ru * a.ldx + c, full, n);
+        if (kReadExtra) q[u] = load16(extra + ru * a.lde + c, full, n);
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t ru = r + (int64_t)u * nty;
         if (ru >= r1) break;
-        const uint32_t keep = keep_mask<V>(key, first + (uint64_t)ru * groups, a.t16);
+        uint64_t d[V / 4];   // draw(key, i) = mix(key + (i + 1) G), from z by addition
+#pragma unroll
+        for (int g = 0; g < V / 4; ++g) d[g] = gen::mix(z + (uint64_t)g * gen::kG);
+        z += z_step;
         float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          bool k = (keep >> e) & 1;
+        for (int e = 0; e < V; e += 2) {   // two at a time: packed products and sums
+          const float2 xv = kReadX ? element2<T>(v[u], e) : make_float2(0.f, 0.f);
+          const float2 ev = kReadExtra ? element2<T>(q[u], e) : make_float2(0.f, 0.f);
+          const float2 be = make_float2(b[e], b[e + 1]);
+          const bool k0 = kept(d[e / 4], e & 3, a.t16), k1 = kept(d[e / 4], (e & 3) + 1, a.t16);
+          float2 t;
           if (kBackward) {
+            t = mul2(ev, make_float2(a.scale, a.scale));
             // (a value that is not a number passes, forward and backward)
-            if (a.relu) k = k && !(__fadd_rn(element<T>(v[u], e), b[e]) <= 0.f);
-            o[e] = k ? __fmul_rn(element<T>(q[u], e), a.scale) : 0.f;
-            sum[e] += o[e];
+            const float2 p = kTwo ? add2(xv, be) : make_float2(1.f, 1.f);
+            t.x = k0 && !(p.x <= 0.f) ? t.x : 0.f;
+            t.y = k1 && !(p.y <= 0.f) ? t.y : 0.f;
+            if (kSums) {
+              const float2 sv = add2(make_float2(sum[e], sum[e + 1]), t);
+              sum[e] = sv.x;
+              sum[e + 1] = sv.y;
+            }
           } else {
-            float t = a.bias ? __fadd_rn(element<T>(v[u], e), b[e]) : element<T>(v[u], e);
-            if (a.relu && t <= 0.f) t = 0.f;
-            o[e] = k ? __fmul_rn(t, a.scale) : 0.f;
-            if (extra) o[e] = __fadd_rn(o[e], element<T>(q[u], e));
+            t = a.bias ? add2(xv, be) : xv;
+            if (a.relu) t = make_float2(t.x <= 0.f ? 0.f : t.x, t.y <= 0.f ? 0.f : t.y);
+            t = mul2(t, make_float2(a.scale, a.scale));
+            t.x = k0 ? t.x : 0.f;
+            t.y = k1 ? t.y : 0.f;
+            if (kTwo) t = add2(t, ev);
           }
+          o[e] = t.x;
+          o[e + 1] = t.y;
         }
         store16(y + ru * a.ldy + c, full, n, o);
         if (kHidden && a.pieces) {
@@ -186,15 +215,17 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) dropout_kernel(const D
       }
     }
   }
-  if (kBackward && a.dbias) {
+  if constexpr (kSums) {
     // db of the block's columns: the threads of a column in order, then the
     // cluster's blocks (all the rows of these columns) in rank order through
     // distributed shared memory: no workspace, no atomics, the same bits each time
     __shared__ float part[kThreads * V];
-    __shared__ float col[V << kSumTxShift];
-    const int width = V << a.tx_shift;
+    __shared__ float col[V * kMaxUnits];
+    const int width = V * w;
+    if (ty < nty) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) part[ty * width + tx * V + e] = sum[e];
+      for (int e = 0; e < V; ++e) part[ty * width + tx * V + e] = sum[e];
+    }
     __syncthreads();
     for (int j = threadIdx.x; j < width; j += kThreads) {
       float s = 0.f;
@@ -204,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) dropout_kernel(const D
     cluster_sync();
     const int ranks = gridDim.y;
     for (int j = threadIdx.x; j < width; j += kThreads) {
-      const int64_t cj = ((int64_t)blockIdx.x << a.tx_shift) * V + j;
+      const int64_t cj = (int64_t)blockIdx.x * width + j;
       if (j % ranks != (int)blockIdx.y || cj >= a.cols) continue;
       float s = 0.f;
       for (int k = 0; k < ranks; ++k) s += ld_cluster(col + j, k);
@@ -214,23 +245,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) dropout_kernel(const D
   }
 }
 
-// Threads along a row: a power of two up to `most`, the largest that wastes at
-// most a sixteenth of the threads on columns past the end, else the least wasteful.
-int pick_tx_shift(int64_t units, int most) {
-  int best = 0;
-  int64_t best_pad = units;
-  for (int s = most; s >= 0; --s) {
-    const int64_t pad = round_up(units, (int64_t)1 << s);
-    if (pad * 16 <= units * 17) return s;
-    if (s == most || pad < best_pad) {
-      best = s;
-      best_pad = pad;
-    }
-  }
-  return best;
-}
-
 constexpr int kMaxCluster = 8;
+
+template <typename T>
+struct Two {};   // (max_clusters' tag of the kernel with two inputs)
 
 template <typename T>
 Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
@@ -238,30 +256,52 @@ Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
   const int sms = current_sms();
   const int64_t units = ceil_div(a.cols, V);
   const bool sums = backward && a.dbias;
-  a.tx_shift = pick_tx_shift(units, sums ? kSumTxShift : 5);
-  const int64_t tiles = ceil_div(units, (int64_t)1 << a.tx_shift);
-  const int nty = kThreads >> a.tx_shift;
-  // one wave of resident blocks; with sums, all the rows of a column tile in a cluster
-  const int64_t most = sums ? kMaxCluster
-                            : std::max<int64_t>(1, (int64_t)sms * kBlocksPerSm / (tiles * slots));
-  int64_t blocks = std::min<int64_t>(std::min<int64_t>(most, 65535),
-                                     std::max<int64_t>(1, ceil_div(a.rows, nty)));
-  a.rows_per_block = std::max<int64_t>(1, ceil_div(a.rows, blocks));
-  if (!sums) blocks = std::max<int64_t>(1, ceil_div(a.rows, a.rows_per_block));
-  const dim3 grid((unsigned)tiles, (unsigned)blocks, (unsigned)slots);
-  if (a.slot_worker) {
-    auto k = dropout_kernel<T, false, true>;
-    AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
-  } else if (!backward) {
-    auto k = dropout_kernel<T, false, false>;
-    AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
-  } else if (!sums) {
-    auto k = dropout_kernel<T, true, false>;
-    AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
+  const bool two = backward ? a.x != nullptr : a.extra != nullptr;
+  const int64_t fit = std::max<int64_t>(1, (int64_t)sms * blocks_per_sm(two, sums) / slots);   // resident blocks
+  int64_t tiles = 0, blocks = 0;
+  if (!sums) {
+    // wide tiles, and as many blocks down the rows as are resident
+    int best = 1;
+    for (int w = 2; w <= kMaxUnits; w *= 2)
+      if (round_up(units, w) * 16 <= round_up(units, best) * 17) best = w;
+    a.tile_units = best;
+    tiles = ceil_div(units, best);
+    blocks = std::min<int64_t>(std::max<int64_t>(1, fit / tiles), ceil_div(a.rows, kThreads / best));
+    a.rows_per_block = ceil_div(a.rows, blocks);
+    blocks = ceil_div(a.rows, a.rows_per_block);
   } else {
-    auto k = dropout_kernel<T, true, false>;
-    AGN_TRY_CUDA(launch_pdl_cluster(k, grid, kThreads, 0, dim3(1, grid.y, 1), st, a));
+    // A cluster has all the rows of its tile.  The kernel is as much bound by instructions
+    // as by memory, so what counts is how many of the resident blocks have work, in one
+    // round: the width (whole 32-byte sectors) and the cluster with the most, the widest of
+    // about equals (16384 x 4096 bf16 at four blocks an SM: 64 tiles of 8 units, clusters of 8, 512
+    // of 608 blocks, 78 us; 86 of 6 units and clusters of 7, 602 blocks but two rounds, 102 us).
+    double most = 0.0;
+    for (int w = 16; w >= 2; w -= 2) {
+      const int64_t t = ceil_div(units, w);
+      int64_t c = std::min<int64_t>(kMaxCluster, std::max<int64_t>(1, ceil_div(a.rows, kThreads / w)));
+      while (c > 1 && (two ? max_clusters<Two<T>>(dropout_kernel<T, true, true, true>, kThreads, 0, (int)c)
+                           : max_clusters<T>(dropout_kernel<T, true, false, true>, kThreads, 0, (int)c)) < t)
+        --c;
+      const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
+      if (used > most * 1.02) {
+        most = used;
+        a.tile_units = w;
+        tiles = t;
+        blocks = c;
+      }
+    }
+    a.rows_per_block = std::max<int64_t>(1, ceil_div(a.rows, blocks));
   }
+  const dim3 grid((unsigned)tiles, (unsigned)blocks, (unsigned)slots);
+  auto k = a.slot_worker ? dropout_kernel<T, false, false, false, true>
+           : sums        ? (a.x ? dropout_kernel<T, true, true, true> : dropout_kernel<T, true, false, true>)
+           : backward    ? (a.x ? dropout_kernel<T, true, true, false> : dropout_kernel<T, true, false, false>)
+           : a.extra     ? dropout_kernel<T, false, true, false>
+                         : dropout_kernel<T, false, false, false>;
+  if (sums)
+    AGN_TRY_CUDA(launch_pdl_cluster(k, grid, kThreads, 0, dim3(1, grid.y, 1), st, a));
+  else
+    AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
   AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }

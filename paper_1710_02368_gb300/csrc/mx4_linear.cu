@@ -343,23 +343,23 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 }
 
 template <int BN>
-Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int sms, cudaStream_t st) {
+Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
   using Cfg = Tile<BN>;
   const dim3 grid0((unsigned)ceil_div(m.out, 128), (unsigned)ceil_div(m.rows, BN));
-  // CTAs along K: one to an SM, clusters of at most 4; of 8 where they are few (16
-  // of them take two rounds: one GPC holds two).  us, clusters of 8, 4, 2: one row of 4096 to
-  // 1000 4.9, 5.6, 7.4; 64 rows of 2048 to 2048 10.3, 5.7, 7.0
+  // CTAs along K: the most whose clusters are all resident (us, clusters of 8, 4, 2: one row of
+  // 4096 to 1000, 8 tiles, 4.9, 5.6, 7.4; 64 rows of 2048 to 2048, 16 tiles, two rounds of
+  // clusters of 8, 10.3, 5.7, 7.0)
+  auto kern = mx4_linear_kernel<BN>;
+  constexpr size_t smem = Cfg::kSmem;
+  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   const int64_t tiles = (int64_t)grid0.x * grid0.y;
   const int kt = (a.k_steps + 3) / 4;
-  const int64_t most = tiles * 8 <= 96 ? 8 : 4;
-  a.split = (int)std::max<int64_t>(1, std::min<int64_t>({most, kt, sms / tiles}));
+  a.split = std::min(8, kt);
+  while (a.split > 1 && max_clusters<Cfg>(kern, kThreads, smem, a.split) < tiles) --a.split;
   a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
   CUtensorMap tw, tx;
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, mx_row_bytes(m.in), m.out, mx_row_bytes(m.in), 128));
   AGN_TRY(make_tmap_u8_2d(&tx, m.x_codes, mx_row_bytes(m.in), m.rows, mx_row_bytes(m.in), BN));
-  auto kern = mx4_linear_kernel<BN>;
-  constexpr size_t smem = Cfg::kSmem;
-  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   const dim3 grid(grid0.x, grid0.y, (unsigned)a.split);
   if (a.split > 1)
     AGN_TRY_CUDA(launch_pdl_cluster(kern, grid, kThreads, smem, dim3(1, 1, (unsigned)a.split), st, tw,
@@ -843,10 +843,10 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
     return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, sms, st)
            : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, sms, st)
                                       : launch_pair<AGN_PREC_MX4>(m, a, sms, st);
-  return m.rows <= 16   ? launch_linear<16>(m, a, sms, st)
-         : m.rows <= 32 ? launch_linear<32>(m, a, sms, st)
-         : m.rows <= 64 ? launch_linear<64>(m, a, sms, st)
-                        : launch_linear<128>(m, a, sms, st);
+  return m.rows <= 16   ? launch_linear<16>(m, a, st)
+         : m.rows <= 32 ? launch_linear<32>(m, a, st)
+         : m.rows <= 64 ? launch_linear<64>(m, a, st)
+                        : launch_linear<128>(m, a, st);
 }
 
 namespace {

@@ -108,6 +108,37 @@ inline int current_sms() {
   return n;
 }
 
+// Clusters of c blocks (along y; 1 <= c <= 8) of this kernel that are resident at once on
+// the current device: fewer blocks than single ones, since a cluster stays within a GPC (a block to an
+// SM: 152 single ones, 36 clusters of four, 15 of eight).  Asked once for each Tag and device.
+template <typename Tag, typename... KArgs>
+int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c) {
+  constexpr int kMax = 64;
+  static std::atomic<int> known[kMax][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMax || c < 1 || c > 8) return 1;
+  int n = known[dev][c].load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1, (unsigned)c, 1);
+    cfg.blockDim = threads;
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1;
+    attr[0].val.clusterDim.y = (unsigned)c;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = 1;
+    }
+    known[dev][c].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 // launch_pdl with clusters of `cluster` blocks.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl_cluster(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
