@@ -7,9 +7,10 @@
 // A block with an infinity or a NaN has no scale that could say so for one
 // element: its scale is NaN, and so is every value of it.
 //
-// One pass: four lanes hold a block (8 elements each, 16 or 32 bytes a lane), its
-// largest magnitude by two shuffles; sixteen lanes write four blocks' codes (64
-// bytes) and the four scales as one word of a scale tile.  Bound by memory.
+// One pass.  A lane holds 32 bytes of a row (16 bf16 or 8 fp32 elements), two or four
+// lanes a block, whose largest magnitude goes between them by shuffles; the lanes
+// of four blocks write their codes (64 bytes) and the four scales as one word of a
+// scale tile.  Bound by memory in fp32, by the conversions as much in bf16.
 #include "mx4.cuh"
 #include "ops.cuh"
 
@@ -18,9 +19,18 @@ namespace agn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
-constexpr int kLane = 8;        // elements of a lane
-constexpr int kWordLanes = 16;  // lanes of a scale word: 128 elements
+// Rows of a thread whose loads are in flight together, quantising and back, and resident
+// blocks of an SM.  us, 16384 x 4096 fp32 and bf16, 10000 x 784 fp32: quantising 50, 30, 8.4
+// (rows 4 and blocks 6: 49, 30, 9.7; 2 and 6: 59, 33, 9.5), back 50, 29, 8.7 (2 and 6: 54, 32, 9.9).
+constexpr int kQuantRows = 2, kBackRows = 8, kBlocksPerSm = 8;
+
+// Elements of a lane, its lanes of a block and of four blocks (a scale word).
+template <typename T>
+struct Lanes {
+  static constexpr int kElems = 32 / (int)sizeof(T);
+  static constexpr int kBlock = kMxBlock / kElems;
+  static constexpr int kWord = 4 * kBlock;
+};
 
 struct MxArgs {
   const void* x;
@@ -30,86 +40,123 @@ struct MxArgs {
   int64_t rows, cols, ld;
   int64_t row_bytes, tiles_k;
   int64_t rows_per_block;
-  int vec;              // rows of x (y) start 16-byte aligned
-  int tx_shift;         // log2 of the lanes along a row (>= 4)
+  int vec;              // rows of x (y) start 16-byte aligned (1), 32-byte (2)
+  int tx_shift;         // log2 of the lanes along a row (>= those of a word)
 };
 
-struct Eight {
-  float v[kLane];
-};
-
+// 32 bytes of a row as they are: one load (vec 2: 32-byte aligned), two (vec 1), or the n
+// valid elements (vec 0).
 template <typename T>
-struct Raw {
-  uint4 q[sizeof(T) * kLane / 16];
+struct __align__(32) Raw {
+  uint4 q[2];
 };
-
 template <typename T>
-__device__ __forceinline__ Raw<T> load8(const T* p, bool full, int n) {
+__device__ __forceinline__ Raw<T> load32(const T* p, int vec, int n) {
   Raw<T> r;
-  constexpr int Q = sizeof(T) * kLane / 16;
-  if (full) {
-#pragma unroll
-    for (int i = 0; i < Q; ++i) r.q[i] = AGN_LD(reinterpret_cast<const uint4*>(p) + i);
+  if (vec == 2) {
+    if (AGN_BOUNDS_OK(p, 32)) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r.q[0].x), "=r"(r.q[0].y), "=r"(r.q[0].z), "=r"(r.q[0].w), "=r"(r.q[1].x),
+                     "=r"(r.q[1].y), "=r"(r.q[1].z), "=r"(r.q[1].w)
+                   : "l"(p));
+    } else {
+      AGN_BOUNDS_FAIL(p);
+      r.q[0] = r.q[1] = make_uint4(0, 0, 0, 0);
+    }
+  } else if (vec == 1) {
+    r.q[0] = AGN_LD(reinterpret_cast<const uint4*>(p));
+    r.q[1] = AGN_LD(reinterpret_cast<const uint4*>(p) + 1);
   } else {
+    r.q[0] = r.q[1] = make_uint4(0, 0, 0, 0);
     T* e = reinterpret_cast<T*>(&r);
 #pragma unroll
-    for (int i = 0; i < Q; ++i) r.q[i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < kLane; ++i)
+    for (int i = 0; i < Lanes<T>::kElems; ++i)
       if (i < n) e[i] = AGN_LD(p + i);
   }
   return r;
 }
 
 template <typename T>
+__device__ __forceinline__ void store32(T* p, int vec, const Raw<T>& r) {
+  if (vec == 2) {
+    if (AGN_BOUNDS_OK(p, 32))
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r.q[0].x),
+                   "r"(r.q[0].y), "r"(r.q[0].z), "r"(r.q[0].w), "r"(r.q[1].x), "r"(r.q[1].y),
+                   "r"(r.q[1].z), "r"(r.q[1].w)
+                   : "memory");
+    else
+      AGN_BOUNDS_FAIL(p);
+  } else {
+    AGN_ST(reinterpret_cast<uint4*>(p), r.q[0]);
+    AGN_ST(reinterpret_cast<uint4*>(p) + 1, r.q[1]);
+  }
+}
+
+// The bits of the largest magnitude as a float (a NaN is above infinity).
+__device__ __forceinline__ uint32_t largest(const Raw<float>& r) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ uint32_t largest(const Raw<bf16>& r) {   // two halves at a time
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+  return max(m & 0xffff0000u, m << 16);
+}
+
+template <typename T>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(const MxArgs a) {
+  using L = Lanes<T>;
+  constexpr int kUnroll = kQuantRows;
   pdl_begin();
   const int tx = threadIdx.x & ((1 << a.tx_shift) - 1), ty = threadIdx.x >> a.tx_shift;
   const int nty = kThreads >> a.tx_shift;
-  const int64_t unit = ((int64_t)blockIdx.x << a.tx_shift) + tx;   // 8 columns
-  const int64_t c = unit * kLane, kq = unit / kWordLanes;          // and its scale word
+  const int64_t unit = ((int64_t)blockIdx.x << a.tx_shift) + tx;   // a lane's 32 bytes
+  const int64_t c = unit * L::kElems, kq = unit / L::kWord;        // and its scale word
   const int64_t r0 = blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-  const int n = c < a.cols ? (int)min((int64_t)kLane, a.cols - c) : 0;
-  const bool full = a.vec && n == kLane;
-  const T* x = static_cast<const T*>(a.x);
-  // a whole warp has the same rows or not: the shuffles below stay within groups of 16
-  // lanes, whose lanes share a row
-  const uint32_t group = 0xffffu << (threadIdx.x & 16);
+  const int n = c < a.cols ? (int)min((int64_t)L::kElems, a.cols - c) : 0;
+  const int vec = n == L::kElems ? a.vec : 0;
+  const bool in_row = c / 2 < a.row_bytes, leads = tx % L::kWord == 0 && kq < a.tiles_k;
+  const T* x = static_cast<const T*>(a.x) + (r0 + ty) * a.ld + c;
+  uint8_t* codes = a.codes + (r0 + ty) * a.row_bytes + c / 2;
+  // the shuffles stay within the lanes of a scale word, which share a row
+  const uint32_t group = ((1u << L::kWord) - 1) << (threadIdx.x & 31 & ~(L::kWord - 1));
   for (int64_t r = r0 + ty; r < r1; r += (int64_t)kUnroll * nty) {
     Raw<T> raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t ru = r + (int64_t)u * nty;
-      if (ru < r1) raw[u] = load8(x + ru * a.ld + c, full, n);
-    }
+    for (int u = 0; u < kUnroll; ++u)
+      if (r + (int64_t)u * nty < r1) raw[u] = load32(x + (int64_t)u * nty * a.ld, vec, n);
+    x += (int64_t)kUnroll * nty * a.ld;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kUnroll; ++u, codes += nty * a.row_bytes) {
       const int64_t ru = r + (int64_t)u * nty;
       if (ru >= r1) break;
-      const T* e = reinterpret_cast<const T*>(&raw[u]);
-      float v[kLane];
-      uint32_t amax = 0;
+      uint32_t amax = largest(raw[u]);
 #pragma unroll
-      for (int i = 0; i < kLane; ++i) {
-        v[i] = static_cast<float>(e[i]);
-        amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);   // (NaN is above infinity)
-      }
-      amax = max(amax, __shfl_xor_sync(group, amax, 1));
-      amax = max(amax, __shfl_xor_sync(group, amax, 2));
+      for (int o = 1; o < L::kBlock; o <<= 1) amax = max(amax, __shfl_xor_sync(group, amax, o));
       const uint32_t code = mx_scale_code(amax);
       const float inv = mx_inverse(code);
-      uint32_t q = 0;
-      if (code != 255) {
+      const T* e = reinterpret_cast<const T*>(&raw[u]);
+      uint32_t q[L::kElems / 8];
 #pragma unroll
-        for (int i = 0; i < kLane / 2; ++i)
-          q |= mx_pair(__fmul_rn(v[2 * i], inv), __fmul_rn(v[2 * i + 1], inv)) << (8 * i);
+      for (int i = 0; i < L::kElems / 8; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(static_cast<float>(e[8 * i + j]), inv);
+        q[i] = code == 255 ? 0u : mx_pack8(v);
       }
-      if (unit * 4 < a.row_bytes)
-        AGN_ST(reinterpret_cast<uint32_t*>(a.codes + ru * a.row_bytes) + unit, q);
-      uint32_t word = code << (8 * ((tx >> 2) & 3));   // (blocks past the row: code 0)
-      word |= __shfl_xor_sync(group, word, 4);
-      word |= __shfl_xor_sync(group, word, 8);
-      if ((tx & 15) == 0 && kq < a.tiles_k)
+      if (in_row) {
+        if constexpr (L::kElems == 16) AGN_ST(reinterpret_cast<uint2*>(codes), make_uint2(q[0], q[1]));
+        else AGN_ST(reinterpret_cast<uint32_t*>(codes), q[0]);
+      }
+      uint32_t word = code << (8 * (tx / L::kBlock % 4));   // (blocks past the row: code 0)
+      word |= __shfl_xor_sync(group, word, L::kBlock);
+      word |= __shfl_xor_sync(group, word, 2 * L::kBlock);
+      if (leads)
         AGN_ST(reinterpret_cast<uint32_t*>(a.scales + mx_scale_at(ru, 4 * kq, a.tiles_k)), word);
     }
   }
@@ -117,56 +164,87 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(const MxArgs a) 
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(const MxArgs a) {
+  using L = Lanes<T>;
+  constexpr int kUnroll = kBackRows;
   pdl_begin();
   const int tx = threadIdx.x & ((1 << a.tx_shift) - 1), ty = threadIdx.x >> a.tx_shift;
   const int nty = kThreads >> a.tx_shift;
   const int64_t unit = ((int64_t)blockIdx.x << a.tx_shift) + tx;
-  const int64_t c = unit * kLane;
+  const int64_t c = unit * L::kElems;
   const int64_t r0 = blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
-  const int n = c < a.cols ? (int)min((int64_t)kLane, a.cols - c) : 0;
-  if (n == 0) return;
-  const bool full = a.vec && n == kLane;
-  T* y = static_cast<T*>(a.y);
+  const bool in_row = c / 2 < a.row_bytes;
+  const bool full = a.vec && c + L::kElems <= a.cols;
+  const uint32_t group = ((1u << L::kWord) - 1) << (threadIdx.x & 31 & ~(L::kWord - 1));
+  T* y = static_cast<T*>(a.y) + (r0 + ty) * a.ld;
   for (int64_t r = r0 + ty; r < r1; r += (int64_t)kUnroll * nty) {
-    uint32_t q[kUnroll], s[kUnroll];
+    uint32_t q[kUnroll][L::kElems / 8], s[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int64_t ru = r + (int64_t)u * nty;
-      if (ru >= r1) break;
-      q[u] = AGN_LD(reinterpret_cast<const uint32_t*>(a.codes + ru * a.row_bytes) + unit);
-      s[u] = AGN_LD(a.scales + mx_scale_at(ru, unit >> 2, a.tiles_k));
+      s[u] = 0;
+#pragma unroll
+      for (int i = 0; i < L::kElems / 8; ++i) q[u][i] = 0;
+      if (ru >= r1 || !in_row) continue;
+      const uint8_t* p = a.codes + ru * a.row_bytes + c / 2;
+      if constexpr (L::kElems == 16) {
+        const uint2 v = AGN_LD(reinterpret_cast<const uint2*>(p));
+        q[u][0] = v.x;
+        q[u][1] = v.y;
+      } else {
+        q[u][0] = AGN_LD(reinterpret_cast<const uint32_t*>(p));
+      }
+      s[u] = AGN_LD(a.scales + mx_scale_at(ru, c / kMxBlock, a.tiles_k));
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t ru = r + (int64_t)u * nty;
-      if (ru >= r1) break;
+    for (int u = 0; u < kUnroll; ++u, y += nty * a.ld) {
+      if (r + (int64_t)u * nty >= r1) break;
       const float scale = mx_scale_value(s[u]);
-      Raw<T> out;
-      T* e = reinterpret_cast<T*>(&out);
+      if (a.vec) {
+        Raw<T> out;
+        T* e = reinterpret_cast<T*>(&out);
 #pragma unroll
-      for (int i = 0; i < kLane; ++i)
-        e[i] = static_cast<T>(__fmul_rn(mx_element((q[u] >> (4 * i)) & 15u), scale));
-      T* p = y + ru * a.ld + c;
-      if (full) {
+        for (int i = 0; i < L::kElems / 8; ++i) {
+          float v[8];
+          mx_unpack8(q[u][i], v);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) * kLane / 16); ++i)
-          AGN_ST(reinterpret_cast<uint4*>(p) + i, out.q[i]);
+          for (int j = 0; j < 8; ++j) e[8 * i + j] = static_cast<T>(__fmul_rn(v[j], scale));
+        }
+        if (full) {
+          store32(y + c, a.vec, out);
+        } else {
+#pragma unroll
+          for (int i = 0; i < L::kElems; ++i)
+            if (c + i < a.cols) AGN_ST(y + c + i, e[i]);
+        }
       } else {
+        // rows that are not aligned: the lanes of a word pass their codes on so that each store
+        // is of consecutive elements, kWord j + lane of the word's 128
+        const int lane = tx % L::kWord;
+        T* p = y + c - (int64_t)lane * L::kElems;
+        const int64_t left = a.cols - (c - (int64_t)lane * L::kElems);
 #pragma unroll
-        for (int i = 0; i < kLane; ++i)
-          if (i < n) AGN_ST(p + i, e[i]);
+        for (int j = 0; j < L::kElems; ++j) {
+          const int e = L::kWord * j + lane, src = e / L::kElems, at = e % L::kElems;
+          const float by = __shfl_sync(group, scale, src, L::kWord);
+          uint32_t w = __shfl_sync(group, q[u][0], src, L::kWord);
+          if constexpr (L::kElems == 16) {
+            const uint32_t w1 = __shfl_sync(group, q[u][1], src, L::kWord);
+            if (at >= 8) w = w1;
+          }
+          if (e < left) AGN_ST(p + e, static_cast<T>(__fmul_rn(mx_element((w >> (4 * (at & 7))) & 15u), by)));
+        }
       }
     }
   }
 }
 
-// Blocks of 2^tx_shift lanes along a row (16 to 256, what leaves the fewest idle) by
+// Blocks of 2^tx_shift lanes along a row (a word's to 256, what leaves the fewest idle) by
 // rows_per_block rows, one wave of resident blocks.
-dim3 geometry(MxArgs* a) {
-  const int64_t units = a->tiles_k * kWordLanes;
-  int best = 4;
+dim3 geometry(MxArgs* a, int word_shift) {
+  const int64_t units = a->tiles_k << word_shift;
+  int best = word_shift;
   int64_t pad = INT64_MAX;
-  for (int s = 8; s >= 4; --s) {
+  for (int s = 8; s >= word_shift; --s) {
     const int64_t p = round_up(units, (int64_t)1 << s);
     if (p < pad) {
       best = s;
@@ -175,15 +253,16 @@ dim3 geometry(MxArgs* a) {
   }
   a->tx_shift = best;
   const int64_t tiles = ceil_div(units, (int64_t)1 << best), nty = kThreads >> best;
-  const int64_t most = std::max<int64_t>(1, (int64_t)current_sms() * 6 / tiles);
+  const int64_t most = std::max<int64_t>(1, (int64_t)current_sms() * kBlocksPerSm / tiles);
   int64_t blocks = std::min<int64_t>(std::min<int64_t>(most, 65535), ceil_div(a->rows, nty));
   a->rows_per_block = ceil_div(a->rows, blocks);
   blocks = ceil_div(a->rows, a->rows_per_block);
   return dim3((unsigned)tiles, (unsigned)blocks);
 }
 
-bool rows_aligned(const void* p, int64_t ld, size_t es) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (size_t)ld * es % 16 == 0;
+int row_alignment(const void* p, int64_t ld, size_t es) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(p) | (uint64_t)ld * es;
+  return at % 32 == 0 ? 2 : at % 16 == 0 ? 1 : 0;
 }
 
 // Quantise (y null) or dequantise (x null).
@@ -197,8 +276,8 @@ Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, i
   a.row_bytes = mx_row_bytes(cols);
   a.tiles_k = mx_tiles_k(cols);
   const bool f32 = dtype == AGN_PREC_FP32;
-  a.vec = rows_aligned(x ? x : y, ld, f32 ? 4 : 2);
-  const dim3 grid = geometry(&a);
+  a.vec = row_alignment(x ? x : y, ld, f32 ? 4 : 2);
+  const dim3 grid = geometry(&a, f32 ? 4 : 3);
   auto k = x ? (f32 ? mx4_quantize_kernel<float> : mx4_quantize_kernel<bf16>)
              : (f32 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>);
   AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));

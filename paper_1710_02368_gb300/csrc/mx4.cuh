@@ -1,6 +1,8 @@
 // Microscaled 4-bit matrices (mx4.cu, mx4_linear.cu; layout in include/agn.h).
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 
 namespace agn {
@@ -39,15 +41,38 @@ __device__ __forceinline__ float mx_inverse(uint32_t code) {
 __device__ __forceinline__ float mx_scale_value(uint32_t code) {
   return __uint_as_float(code == 255 ? 0x7fc00000u : code == 0 ? 0x00400000u : code << 23);
 }
-// Two floats to E2M1 codes, round to nearest even, saturating at 6: lo in the low nibble.
-__device__ __forceinline__ uint32_t mx_pair(float lo, float hi) {
+// Eight floats to E2M1 codes, round to nearest even, saturating at 6: v[0] in the low nibble.
+__device__ __forceinline__ uint32_t mx_pack8(const float (&v)[8]) {
   uint32_t r;
-  asm("{\n\t.reg .b8 t;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
-      "cvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
   return r;
 }
-// E2M1's magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6 (twice them, a nibble each).
+// The values of eight codes.
+__device__ __forceinline__ void mx_unpack8(uint32_t q, float (&v)[8]) {
+  uint32_t h[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(q));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
+
+// The value of one code: E2M1's magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6 from twice them, a nibble each.
 __device__ __forceinline__ float mx_element(uint32_t code) {
   const float v = 0.5f * (float)((0xC8643210u >> (4 * (code & 7))) & 15u);
   return code & 8 ? -v : v;

@@ -130,8 +130,8 @@ __device__ __forceinline__ void finish(const LinearArgs& a, int64_t r, int64_t f
     for (int o = 1; o < 8; o <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     const uint32_t code = mx_scale_code(amax);
     const float inv = mx_inverse(code);
-    uint32_t q = code == 255 ? 0u
-                             : mx_pair(v[0] * inv, v[1] * inv) | mx_pair(v[2] * inv, v[3] * inv) << 8;
+    const float u[8] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, 0.f, 0.f, 0.f, 0.f};
+    const uint32_t q = code == 255 ? 0u : mx_pack8(u) & 0xffffu;
     const uint32_t hi = __shfl_down_sync(0xffffffffu, q, 1);
     const int lane = threadIdx.x & 31;
     const int64_t row_bytes = mx_row_bytes(a.out);
@@ -490,8 +490,12 @@ __device__ __forceinline__ void store_rows(const LinearArgs& a, const CUtensorMa
       uint32_t q[4] = {0, 0, 0, 0};
       if (code != 255) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          q[i >> 2] |= mx_pair(v[2 * i] * inv, v[2 * i + 1] * inv) << (8 * (i & 3));
+        for (int i = 0; i < 4; ++i) {
+          float u[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u[j] = v[8 * i + j] * inv;
+          q[i] = mx_pack8(u);
+        }
       }
       word |= code << (8 * c);
       *staged_at<64>(tile, lane, c) = make_uint4(q[0], q[1], q[2], q[3]);
