@@ -442,8 +442,8 @@ int agn_commit_pull_noalloc(float* theta_c, float* acc, float* replicas, void* r
  *   ldx, ldr, ldy: row strides in elements, >= cols (ldr unused without a
  *               residual); rows that start on 16-byte boundaries are faster;
  *   y         : may be x or the residual itself with the same stride (in place);
- *               any other overlap is AGN_E_INVALID.  Bytes between the rows are
- *               left alone.
+ *               any other overlap (of the bytes from a matrix's first element to its
+ *               last) is AGN_E_INVALID.  Bytes between the rows are left alone.
  *   p         : in [0, 1).  rows or cols 0: nothing to do.
  * This call and the ones after it queue their work on `stream` and return
  * without waiting; they allocate nothing, keep nothing between calls, may be
@@ -507,8 +507,8 @@ int agn_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int6
 /*
  * A layer on microscaled operands, on the tensor cores:
  *     y[r][f] = act(sum_k x[r][k] w[f][k] + bias[f]),  act = ReLU with relu, else none
- * x [rows][in] and w [out][in] in 4-bit form, fp32 sums, any rows >= 0, in >= 1,
- * out >= 1 (below 2^31 - 256).  A NaN passes the ReLU.
+ * x [rows][in] and w [out][in] in 4-bit form, fp32 sums; rows >= 0 and out >= 1
+ * below 2^31 - 256, in 1 .. 2^28.  A NaN passes the ReLU.
  *   y     : dtype AGN_PREC_FP32 or AGN_PREC_BF16: device [rows][ldy], ldy >= out, rounded
  *           once from the fp32 value.  AGN_PREC_MX4: y and y_scales are the codes
  *           and scales of a [rows][out] matrix, quantised from the fp32 values as
@@ -517,7 +517,7 @@ int agn_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int6
  *   err   : device int32, NULL = none: set to 1 (never cleared) when a bounded wait of the kernel
  *           gave up (2 s); the values that it could not compute are NaN.
  * The order of the sums depends on the sizes alone: equal calls give equal bits.
- * Errors: AGN_E_INVALID, AGN_E_UNSUPPORTED (more than 16776960 rows), AGN_E_CUDA.
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
  */
 int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_codes,
                    const void* w_scales, const float* bias, int64_t rows, int64_t in, int64_t out,

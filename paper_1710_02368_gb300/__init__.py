@@ -298,7 +298,10 @@ def _addr(x):
     """A device pointer argument (a tensor or an int) as ctypes takes it."""
     if x is None:
         return None
-    return x.data_ptr() if hasattr(x, "data_ptr") else int(x)
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return int(x)
 
 
 _U64 = (1 << 64) - 1

@@ -302,7 +302,6 @@ Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
     AGN_TRY_CUDA(launch_pdl_cluster(k, grid, kThreads, 0, dim3(1, grid.y, 1), st, a));
   else
     AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
-  AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }
 

@@ -281,7 +281,6 @@ Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, i
   auto k = x ? (f32 ? mx4_quantize_kernel<float> : mx4_quantize_kernel<bf16>)
              : (f32 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>);
   AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
-  AGN_TRY_CUDA(cudaGetLastError());
   return Status::Ok();
 }
 

@@ -160,12 +160,15 @@ cudaError_t launch_pdl_cluster(void (*kern)(KArgs...), dim3 grid, dim3 block, si
   return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
 }
 
-// Runs an entry point's body: its status as the C code, the message kept.
+// Runs an entry point's body: its status as the C code, the message kept (and
+// the runtime's last error cleared, which a later launch check of the caller's
+// would take for its own).
 template <typename F>
 int guarded(F&& body) {
   Status s;
   try {
     s = body();
+    if (s.code == AGN_E_CUDA || s.code == AGN_E_OOM) cudaGetLastError();
     if (!s.ok()) set_global_error(s.msg);
   } catch (const std::exception&) {
     s.code = AGN_E_OOM;

@@ -71,7 +71,7 @@ def test_dequantize_refuses(agn):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(rows=-1), dict(inner=0), dict(out=0), dict(inner=1 << 31), dict(out=(1 << 31) - 1),
+    dict(rows=-1), dict(inner=0), dict(out=0), dict(inner=(1 << 28) + 1), dict(out=(1 << 31) - 1), dict(rows=(1 << 31) - 1),
     dict(dtype=5), dict(ldy=99), dict(x_codes=None), dict(w_scales=None), dict(y=None),
     dict(dtype=2), dict(x_codes=X + 4), dict(w_scales=W + 4), dict(y=X + 16), dict(err=Z),
     dict(bias=Z + 2), dict(dtype=2, y_scales=Z), dict(dtype=2, y_scales=3 * Z + 4),
