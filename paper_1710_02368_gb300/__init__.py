@@ -44,7 +44,7 @@ def library_path() -> str:
 
 
 def _L():
-    return _lib.load()
+    return _lib._LIB or _lib.load()
 
 
 def _check(rc: int, handle=None):
@@ -312,20 +312,24 @@ def agn_dropout(x, y, dtype, rows, cols, p, seed, offset=0, bias=None, residual=
     """y = dropout(act(x + bias)) + residual on device buffers; row strides
     default to cols.  The mask is a function of (p, seed, offset) and the
     element's place (include/agn.h)."""
-    _check(_L().agn_dropout(_addr(x), _addr(bias), _addr(residual), _addr(y), dtype, bool(relu),
-                            rows, cols, cols if ldx is None else ldx, cols if ldr is None else ldr,
-                            cols if ldy is None else ldy, p, seed & _U64, offset & _U64,
-                            _addr(stream)))
+    rc = _L().agn_dropout(_addr(x), _addr(bias), _addr(residual), _addr(y), dtype, bool(relu), rows,
+                          cols, cols if ldx is None else ldx, cols if ldr is None else ldr,
+                          cols if ldy is None else ldy, p, seed & _U64, offset & _U64,
+                          _addr(stream))
+    if rc:
+        _check(rc)
 
 
 def agn_dropout_backward(dy, dx, dtype, rows, cols, p, seed, offset=0, x=None, bias=None,
                          dbias=None, relu=0, lddy=None, ldx=None, lddx=None, stream=None):
     """Gradient of agn_dropout with the same (p, seed, offset): dx, and dbias [cols]
     (fp32) when given.  With relu, x and bias are the forward call's."""
-    _check(_L().agn_dropout_backward(_addr(dy), _addr(x), _addr(bias), _addr(dx), _addr(dbias),
-                                     dtype, bool(relu), rows, cols, cols if lddy is None else lddy,
-                                     cols if ldx is None else ldx, cols if lddx is None else lddx,
-                                     p, seed & _U64, offset & _U64, _addr(stream)))
+    rc = _L().agn_dropout_backward(_addr(dy), _addr(x), _addr(bias), _addr(dx), _addr(dbias), dtype,
+                                   bool(relu), rows, cols, cols if lddy is None else lddy,
+                                   cols if ldx is None else ldx, cols if lddx is None else lddx, p,
+                                   seed & _U64, offset & _U64, _addr(stream))
+    if rc:
+        _check(rc)
 
 
 def agn_mx4_bytes(rows, cols):
@@ -336,23 +340,29 @@ def agn_mx4_bytes(rows, cols):
 
 
 def agn_mx4_quantize(x, dtype, rows, cols, codes, scales, ldx=None, stream=None):
-    _check(_L().agn_mx4_quantize(_addr(x), dtype, rows, cols, cols if ldx is None else ldx,
-                                 _addr(codes), _addr(scales), _addr(stream)))
+    rc = _L().agn_mx4_quantize(_addr(x), dtype, rows, cols, cols if ldx is None else ldx,
+                               _addr(codes), _addr(scales), _addr(stream))
+    if rc:
+        _check(rc)
 
 
 def agn_mx4_dequantize(codes, scales, rows, cols, y, dtype, ldy=None, stream=None):
-    _check(_L().agn_mx4_dequantize(_addr(codes), _addr(scales), rows, cols, _addr(y), dtype,
-                                   cols if ldy is None else ldy, _addr(stream)))
+    rc = _L().agn_mx4_dequantize(_addr(codes), _addr(scales), rows, cols, _addr(y), dtype,
+                                 cols if ldy is None else ldy, _addr(stream))
+    if rc:
+        _check(rc)
 
 
 def agn_mx4_linear(x_codes, x_scales, w_codes, w_scales, rows, inner, out, y, dtype, bias=None,
                    relu=0, ldy=None, y_scales=None, err=None, stream=None):
     """y [rows][out] = act(x w^T + bias) on 4-bit x [rows][inner] and w [out][inner];
     dtype AGN_PREC_MX4: y and y_scales receive 4-bit rows."""
-    _check(_L().agn_mx4_linear(_addr(x_codes), _addr(x_scales), _addr(w_codes), _addr(w_scales),
-                               _addr(bias), rows, inner, out, bool(relu), _addr(y), dtype,
-                               out if ldy is None else ldy, _addr(y_scales), _addr(err),
-                               _addr(stream)))
+    rc = _L().agn_mx4_linear(_addr(x_codes), _addr(x_scales), _addr(w_codes), _addr(w_scales),
+                             _addr(bias), rows, inner, out, bool(relu), _addr(y), dtype,
+                             out if ldy is None else ldy, _addr(y_scales), _addr(err),
+                             _addr(stream))
+    if rc:
+        _check(rc)
 
 
 class AGN:

@@ -253,7 +253,7 @@ struct Two {};   // (max_clusters' tag of the kernel with two inputs)
 template <typename T>
 Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const int sms = current_sms();
+  const int dev = current_device(), sms = device_sms(dev);
   const int64_t units = ceil_div(a.cols, V);
   const bool sums = backward && a.dbias;
   const bool two = backward ? a.x != nullptr : a.extra != nullptr;
@@ -279,8 +279,8 @@ Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
     for (int w = 16; w >= 2; w -= 2) {
       const int64_t t = ceil_div(units, w);
       int64_t c = std::min<int64_t>(kMaxCluster, std::max<int64_t>(1, ceil_div(a.rows, kThreads / w)));
-      while (c > 1 && (two ? max_clusters<Two<T>>(dropout_kernel<T, true, true, true>, kThreads, 0, (int)c)
-                           : max_clusters<T>(dropout_kernel<T, true, false, true>, kThreads, 0, (int)c)) < t)
+      while (c > 1 && (two ? max_clusters<Two<T>>(dropout_kernel<T, true, true, true>, kThreads, 0, (int)c, dev)
+                           : max_clusters<T>(dropout_kernel<T, true, false, true>, kThreads, 0, (int)c, dev)) < t)
         --c;
       const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
       if (used > most * 1.02) {

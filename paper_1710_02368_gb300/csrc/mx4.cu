@@ -253,7 +253,7 @@ dim3 geometry(MxArgs* a, int word_shift) {
   }
   a->tx_shift = best;
   const int64_t tiles = ceil_div(units, (int64_t)1 << best), nty = kThreads >> best;
-  const int64_t most = std::max<int64_t>(1, (int64_t)current_sms() * kBlocksPerSm / tiles);
+  const int64_t most = std::max<int64_t>(1, (int64_t)device_sms(current_device()) * kBlocksPerSm / tiles);
   int64_t blocks = std::min<int64_t>(std::min<int64_t>(most, 65535), ceil_div(a->rows, nty));
   a->rows_per_block = ceil_div(a->rows, blocks);
   blocks = ceil_div(a->rows, a->rows_per_block);

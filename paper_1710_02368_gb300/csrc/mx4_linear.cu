@@ -343,7 +343,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 }
 
 template <int BN>
-Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
+Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int dev, cudaStream_t st) {
   using Cfg = Tile<BN>;
   const dim3 grid0((unsigned)ceil_div(m.out, 128), (unsigned)ceil_div(m.rows, BN));
   // CTAs along K: the most whose clusters are all resident (us, clusters of 8, 4, 2: one row of
@@ -351,11 +351,11 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, cudaStream_t st) {
   // clusters of 8, 10.3, 5.7, 7.0)
   auto kern = mx4_linear_kernel<BN>;
   constexpr size_t smem = Cfg::kSmem;
-  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  AGN_TRY_CUDA(allow_smem<Cfg>(kern, smem, dev));
   const int64_t tiles = (int64_t)grid0.x * grid0.y;
   const int kt = (a.k_steps + 3) / 4;
   a.split = std::min(8, kt);
-  while (a.split > 1 && max_clusters<Cfg>(kern, kThreads, smem, a.split) < tiles) --a.split;
+  while (a.split > 1 && max_clusters<Cfg>(kern, kThreads, smem, a.split, dev) < tiles) --a.split;
   a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
   CUtensorMap tw, tx;
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, mx_row_bytes(m.in), m.out, mx_row_bytes(m.in), 128));
@@ -788,7 +788,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
 }
 
 template <int kOut>
-Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStream_t st) {
+Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int dev, cudaStream_t st) {
   CUtensorMap tw, tx, tws, txs, ty{};
   const int64_t rb = mx_row_bytes(m.in);
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, rb, m.out, rb, 128));
@@ -803,11 +803,10 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int sms, cudaStr
     AGN_TRY(make_tmap_store_2d(&ty, m.y, (int)dtype_size(kOut), a.bulk_out, m.rows, m.ldy,
                                128 / (int)dtype_size(kOut), 32));
   auto kern = mx4_linear_pair_kernel<kOut>;
-  AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)kPairSmem));
+  AGN_TRY_CUDA((allow_smem<std::integral_constant<int, kOut>>(kern, kPairSmem, dev)));
   const int64_t tiles_f = ceil_div(m.out, 256), tiles = tiles_f * ceil_div(m.rows, 256);
   // the last round in halves where they fit (4-bit outputs: a warp's scales are whole words)
-  const int64_t most = sms / 2, rest = tiles % most;
+  const int64_t most = device_sms(dev) / 2, rest = tiles % most;
   const int64_t halves = kOut != AGN_PREC_MX4 && 2 * rest <= most ? rest : 0;
   const int64_t units = tiles + halves, pairs = std::min(units, most);
   AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem,
@@ -837,18 +836,18 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.bulk_out = m.dtype == AGN_PREC_MX4 ? m.out
                : a.vec                 ? m.out / (16 / (int64_t)dtype_size(m.dtype)) * (16 / (int64_t)dtype_size(m.dtype))
                                        : 0;
-  const int sms = current_sms();
+  const int dev = current_device();
   // Tiles of 256 x 256 by pairs of SMs from 257 rows on (us, pairs and 128-column tiles: 512 rows of
   // 4096 to 4096 11.3 and 13.4, 1024 12.2 and 25.6, 10000 of 784 to 128 8.2 and 7.6; 200 of 4096
   // to 1000 10.5 and 7.7), else the narrowest columns that hold the rows.
   if (m.rows > 256)
-    return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, sms, st)
-           : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, sms, st)
-                                      : launch_pair<AGN_PREC_MX4>(m, a, sms, st);
-  return m.rows <= 16   ? launch_linear<16>(m, a, st)
-         : m.rows <= 32 ? launch_linear<32>(m, a, st)
-         : m.rows <= 64 ? launch_linear<64>(m, a, st)
-                        : launch_linear<128>(m, a, st);
+    return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, dev, st)
+           : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, dev, st)
+                                      : launch_pair<AGN_PREC_MX4>(m, a, dev, st);
+  return m.rows <= 16   ? launch_linear<16>(m, a, dev, st)
+         : m.rows <= 32 ? launch_linear<32>(m, a, dev, st)
+         : m.rows <= 64 ? launch_linear<64>(m, a, dev, st)
+                        : launch_linear<128>(m, a, dev, st);
 }
 
 namespace {

@@ -93,30 +93,44 @@ struct KnownBuffers {
   }
 };
 
-// SMs of the current device (asked once for each device).
-inline int current_sms() {
-  constexpr int kMax = 64;
-  static std::atomic<int> sms[kMax];
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMax) return 152;
-  n = sms[dev].load(std::memory_order_relaxed);
+// What is asked of a device once: by its ordinal, the current device's in these calls.
+constexpr int kMaxDevices = 64;
+
+inline int current_device() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : kMaxDevices;
+}
+
+inline int device_sms(int dev) {
+  static std::atomic<int> known[kMaxDevices + 1];
+  int n = known[dev].load(std::memory_order_relaxed);
   if (n == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+    if (dev == kMaxDevices ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
       n = 152;
-    sms[dev].store(n, std::memory_order_relaxed);
+    known[dev].store(n, std::memory_order_relaxed);
   }
   return n;
+}
+
+// Lets a kernel have `smem` bytes of dynamic shared memory (a Tag for each kernel).
+template <typename Tag, typename... KArgs>
+cudaError_t allow_smem(void (*kern)(KArgs...), size_t smem, int dev) {
+  static std::atomic<int> done[kMaxDevices + 1];
+  if (dev < kMaxDevices && done[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+  const cudaError_t e =
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess) done[dev].store(1, std::memory_order_relaxed);
+  return e;
 }
 
 // Clusters of c blocks (along y; 1 <= c <= 8) of this kernel that are resident at once on
 // the current device: fewer blocks than single ones, since a cluster stays within a GPC (a block to an
 // SM: 152 single ones, 36 clusters of four, 15 of eight).  Asked once for each Tag and device.
 template <typename Tag, typename... KArgs>
-int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c) {
-  constexpr int kMax = 64;
-  static std::atomic<int> known[kMax][9];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMax || c < 1 || c > 8) return 1;
+int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c, int dev) {
+  static std::atomic<int> known[kMaxDevices + 1][9];
+  if (c < 1 || c > 8) return 1;
   int n = known[dev][c].load(std::memory_order_relaxed);
   if (n == 0) {
     cudaLaunchConfig_t cfg = {};
