@@ -730,10 +730,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         }
     } else if (warp == 5 && lane == 0 && cta == 0) {
       // An MMA is issued in about the time that it takes, and few wait in line: what this
-      // thread does between them is tensor time lost unless it is short (836 clocks
-      // a stage with two barriers waited on in turn and the descriptors made anew, 513
-      // for the MMAs alone).  So: one barrier a stage, asked for the next stage
-      // between this stage's MMAs, descriptors by addition.
+      // thread does between them is tensor time lost unless it is short.  So: one barrier
+      // a stage, asked for the next stage between this stage's MMAs, descriptors by addition
+      // or constant, whole stages without a test (clocks a stage: 836 with two barriers
+      // waited on in turn and the descriptors made anew, 646 with tests of the last stage's
+      // length, now 588; 513 for the MMAs alone).
       const uint64_t da0 = tc::smem_desc_sw128(tc::smem_u32(smem), 16, 1024);
       constexpr uint64_t kToB = kPairHalf >> 4;
       uint64_t da = da0;
@@ -747,25 +748,42 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         auto mainloop = [&](auto columns) {
           constexpr uint32_t id0 = tc::idesc_mxf4(256, decltype(columns)::value, 0);
           constexpr uint32_t id2 = tc::idesc_mxf4(256, decltype(columns)::value, 2);
-          for (int left = a.k_steps; left > 0; left -= 4) {
-            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
-              *abort_flag = 1;
-              break;
-            }
-            tc::tc_fence_after();
-            const bool first = left == a.k_steps;
-            tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, !first);
-            if (left > 1) tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
-            uint64_t* const mine = &empty[s];
-            const uint64_t d = da + 4;
-            const uint32_t sf1 = sf;
+          uint32_t acc = 0;   // the tile's first MMA overwrites
+          auto next = [&] {
             da += kPairStage >> 4;
             sf += kPairSfCols;
             if (++s == kPairStages) s = 0, phase ^= 1, da = da0, sf = tmem + kPairSf;
             ready = tc::mbar_test_wait(&full[s], phase);
-            if (left > 2) tc::mma_mxf4_pair(tmem, d, d + kToB, id0, sf1 + 4, sf1 + 16, 1);
-            if (left > 3) tc::mma_mxf4_pair(tmem, d + 2, d + kToB + 2, id2, sf1 + 4, sf1 + 16, 1);
+            acc = 1;
+          };
+          int left = a.k_steps;
+          for (; left >= 4; left -= 4) {   // whole stages
+            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
+              *abort_flag = 1;
+              return;
+            }
+            tc::tc_fence_after();
+            tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, acc);
+            tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
+            tc::mma_mxf4_pair(tmem, da + 4, da + kToB + 4, id0, sf + 4, sf + 16, 1);
+            uint64_t* const mine = &empty[s];
+            const uint64_t d = da + 6;
+            const uint32_t f = sf;
+            next();
+            tc::mma_mxf4_pair(tmem, d, d + kToB, id2, f + 4, f + 16, 1);
             tc::mma_commit_pair(mine);
+          }
+          if (left > 0) {
+            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
+              *abort_flag = 1;
+              return;
+            }
+            tc::tc_fence_after();
+            tc::mma_mxf4_pair(tmem, da, da + kToB, id0, sf, sf + 8, acc);
+            if (left > 1) tc::mma_mxf4_pair(tmem, da + 2, da + kToB + 2, id2, sf, sf + 8, 1);
+            if (left > 2) tc::mma_mxf4_pair(tmem, da + 4, da + kToB + 4, id0, sf + 4, sf + 16, 1);
+            tc::mma_commit_pair(&empty[s]);
+            next();
           }
         };
         if (t >= n_whole) mainloop(std::integral_constant<int, 128>());
