@@ -4,9 +4,10 @@
 // tcgen05.mma kind::mxf4 (products of E2M1 values scaled by both blocks'
 // powers of two, f32 sums in TMEM), output fp32, bf16 or 4-bit codes again.
 //
-// The features are the MMA's M (128 TMEM lanes), the rows of x its N (BN
-// columns): few rows take narrow tiles that read each weight once, and a lane's
-// features are contiguous in every output row.  A stage is 256 k: 128-byte rows
+// Few rows, one CTA a tile: the features are the MMA's M (128 TMEM lanes), the rows
+// of x its N (BN columns), so that narrow tiles read each weight once and a lane's
+// features are contiguous in every output row.  (Many rows: see the pairs of CTAs
+// below.)  A stage is 256 k: 128-byte rows
 // of codes (TMA, 128-byte swizzle) and two scale tiles of 512 bytes (bulk copies;
 // the scales are stored as the tensor core wants them), copied to TMEM by the
 // thread that issues the MMAs.  K past the last element costs nothing: codes and
@@ -374,10 +375,9 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int dev, cudaStream_t
 // ---------------------------------------------------------------------------
 
 // Two SMs share a tile of 256 rows x 256 features (tcgen05 cta_group::2): each
-// holds its 128 rows and half of the features, 64 bytes of operands a clock of MMA
-// time where a CTA alone would need 96, and the L2 gives an SM about 64.  Here the
-// rows are the MMA's M: a lane holds a row's consecutive features, whole blocks of
-// a 4-bit output.  One pair for every two SMs walks over the tiles; roles by warp:
+// loads its 128 rows and half of the features, 64 bytes a clock of MMA time where a CTA
+// alone would load 96.  Here the rows are the MMA's M: a lane holds a row's
+// consecutive features, whole blocks of a 4-bit output.  One pair for every two SMs walks over the tiles; roles by warp:
 //   4     loads: codes complete on the first CTA's barriers, each CTA's scales on its own
 //   0-3   bring a stage's scales from shared memory into TMEM (tcgen05.st, each warp
 //         its lane quadrant): tcgen05.cp takes 97 clocks for 512 bytes, six of them a stage,
@@ -799,6 +799,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       }
     }
   }
+  __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
   cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers

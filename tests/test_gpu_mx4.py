@@ -217,6 +217,110 @@ def test_four_bit_output(agn, torch, rows, inner, out):
         assert torch.equal(c, c2) and torch.equal(s, s2)
 
 
+def test_random_shapes(agn, torch):
+    """Codes at random with scales within a factor of four: every sum is exact in fp32, at any shape, stride,
+    start and type of the output."""
+    rng = np.random.default_rng(11)
+    for i in range(90):
+        rows, inner, out = (int(round(np.exp(rng.uniform(0, np.log(hi))))) for hi in (900, 900, 700))
+        if i % 6 == 0:
+            rows, out = rows + 700, out + 300   # pairs of CTAs, and several tiles
+        m = []
+        for r in (rows, out):
+            nb = R.blocks(inner)
+            code = rng.integers(0, 16, (r, nb * 32)).astype(np.uint8)
+            code[:, inner:] = 0
+            scale = rng.integers(126, 129, (r, nb)).astype(np.uint8)
+            c, s = R.mx4_pack(code, scale)
+            s = s.copy()
+            s[padding(r, inner)[2].ravel()] = 0xFF
+            m.append((torch.tensor(c.reshape(-1), device="cuda"), torch.tensor(s, device="cuda"),
+                      R.mx4_values(code, scale)[:, :inner]))
+        dtype, relu, ldy, start = int(rng.integers(2)), int(rng.integers(2)), out + int(rng.integers(9)), int(rng.integers(9))
+        if i % 3 == 0:
+            ldy, start = (out + 15) // 8 * 8, 0
+        buf = torch.full((start + rows * ldy + 8,), 7.0, device="cuda").to(dt(torch, dtype))
+        y = buf[start:start + rows * ldy].view(rows, ldy)
+        agn.agn_mx4_linear(*m[0][:2], *m[1][:2], rows, inner, out, y, dtype, relu=relu, ldy=ldy)
+        want = m[0][2] @ m[1][2].T
+        want = torch.tensor(np.maximum(want, 0) if relu else want, dtype=torch.float32).to(dt(torch, dtype)).double().numpy()
+        got = y[:, :out].double().cpu().numpy()
+        assert np.array_equal(got, want), (rows, inner, out, dtype, ldy, start)
+        y[:, :out] = 7.0
+        assert torch.all(buf == 7.0), (rows, inner, out, dtype, ldy, start)
+
+
+def test_first_calls_in_a_capture(agn, torch):
+    """A process whose first calls are captured ones: what a device is asked once is asked then."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch, paper_1710_02368_gb300 as agn
+def mat(r, c): return tuple(torch.zeros(n, dtype=torch.uint8, device="cuda") for n in agn.agn_mx4_bytes(r, c))
+x, y, db = torch.randn(600, 300, device="cuda"), torch.empty(600, 300, device="cuda"), torch.empty(300, device="cuda")
+q, w = mat(600, 300), mat(200, 300)
+z, z1 = torch.empty(600, 200, device="cuda"), torch.empty(5, 200, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    s = torch.cuda.current_stream().cuda_stream
+    agn.agn_dropout(x, y, 0, 600, 300, 0.5, 1, relu=1, stream=s)
+    agn.agn_dropout_backward(y, y, 0, 600, 300, 0.5, 1, x=x, relu=1, dbias=db, stream=s)
+    agn.agn_mx4_quantize(x, 0, 600, 300, *q, stream=s)
+    agn.agn_mx4_quantize(x, 0, 200, 300, *w, stream=s)
+    agn.agn_mx4_linear(*q, *w, 600, 300, 200, z, 0, stream=s)
+    agn.agn_mx4_linear(*q, *w, 5, 300, 200, z1, 0, stream=s)
+g.replay(); torch.cuda.synchronize()
+a, b, c = z.clone(), z1.clone(), db.clone()
+agn.agn_mx4_linear(*q, *w, 600, 300, 200, z, 0)
+agn.agn_mx4_linear(*q, *w, 5, 300, 200, z1, 0)
+agn.agn_dropout(x, y, 0, 600, 300, 0.5, 1, relu=1)
+agn.agn_dropout_backward(y, y, 0, 600, 300, 0.5, 1, x=x, relu=1, dbias=db)
+assert torch.equal(a, z) and torch.equal(b, z1) and torch.equal(c, db) and float(a.abs().sum()) > 0
+print("same")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+def test_two_threads(agn, torch):
+    """Calls from two host threads, each on its own stream and buffers."""
+    import threading
+    rows, dims = 500, (300, 200)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    xs = [torch.randn(rows, dims[0], generator=g, device="cuda") for _ in range(2)]
+    w = quantize(agn, torch, torch.randn(dims[1], dims[0], generator=g, device="cuda"))
+    bufs = [(buffers(agn, torch, rows, dims[0]), torch.empty(rows, dims[1], device="cuda")) for _ in range(2)]
+    want = []
+    for i in range(2):
+        q = quantize(agn, torch, xs[i])
+        want.append(linear(agn, torch, q, w, rows, *dims))
+    torch.cuda.synchronize()
+    streams, failed = [torch.cuda.Stream() for _ in range(2)], []
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            for _ in range(200):
+                agn.agn_mx4_quantize(xs[i], 0, rows, dims[0], *bufs[i][0], stream=streams[i].cuda_stream)
+                agn.agn_mx4_linear(*bufs[i][0], *w, rows, *dims, bufs[i][1], 0, stream=streams[i].cuda_stream)
+                try:
+                    agn.agn_mx4_linear(*bufs[i][0], *w, -1 - i, *dims, bufs[i][1], 0)
+                except agn.AGNError as e:
+                    assert e.code == agn.AGN_E_INVALID
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+    ts = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in ts]
+    [t.join() for t in ts]
+    torch.cuda.synchronize()
+    assert not failed
+    for i in range(2):
+        assert torch.equal(bufs[i][1], want[i])
+
+
 def test_not_finite(agn, torch):
     """A NaN block of a row makes that row NaN and no other; of a feature, that column; through the ReLU
     and into a 4-bit output."""

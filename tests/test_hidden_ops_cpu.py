@@ -84,6 +84,21 @@ def test_linear_refuses(agn, bad):
     refused(agn, lambda: agn.agn_mx4_linear(**a))
 
 
+@pytest.mark.parametrize("kw,code", [(dict(dropout=1.0), "INVALID"), (dict(dropout=-0.1), "INVALID"),
+                                     (dict(dropout=float("nan")), "INVALID"), (dict(eval_mx4=1), "INVALID"),
+                                     (dict(eval_mx4=1, n_eval=4, dims=(8, 4)), "UNSUPPORTED")], ids=str)
+def test_create_refuses(agn, kw, code):
+    kw = dict(kw)
+    dims = kw.pop("dims", (8, 8, 4))
+    with pytest.raises(agn.AGNError) as e:
+        agn.AGN(dims, 2, 1, 0.1, 1, **kw)
+    assert e.value.name == "AGN_E_" + code
+
+
+def test_evaluate_mx4_refuses_a_null_handle(agn):
+    assert agn._lib.load().agn_evaluate_mx4(None, None, None, None, 0) == agn.AGN_E_INVALID
+
+
 def test_nothing_to_do_touches_nothing(agn):
     agn.agn_dropout(None, None, 0, 0, 8, 0.5, 1)
     agn.agn_dropout(None, None, 1, 8, 0, 0.5, 1)
