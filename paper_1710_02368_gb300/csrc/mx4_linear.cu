@@ -254,6 +254,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     const uint64_t da0 = tc::smem_desc_sw128(s0, 16, 1024);
     const uint64_t ds0 = tc::smem_desc_rows16(s0 + kABytes + Cfg::kBBytes, 128);
     constexpr uint64_t kToB = kABytes >> 4, kTile = kMxTileBytes >> 4, kToX = kSfBytes >> 4;
+    const uint32_t sfx = sfb + (uint32_t)(n0 & 127) / 32;   // this tile's rows of the 128 (BN = 64)
     uint64_t da = da0, ds = ds0;
     int s = 0;
     uint32_t phase = 0;
@@ -271,9 +272,9 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         tc::cp_32x128b_warpx4(sfa + 4, ds + kTile);
         tc::cp_32x128b_warpx4(sfb + 4, ds + kToX + kTile);
       }
-      tc::mma_mxf4(tmem, da, da + kToB, tc::idesc_mxf4(128, BN, 0), sfa, sfb, !first);
+      tc::mma_mxf4(tmem, da, da + kToB, tc::idesc_mxf4(128, BN, 0), sfa, sfx, !first);
       if (left > 1)
-        tc::mma_mxf4(tmem, da + 2, da + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa, sfb, 1);
+        tc::mma_mxf4(tmem, da + 2, da + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa, sfx, 1);
       uint64_t* const mine = &empty[s];
       const uint64_t d = da + 4;
       da += Cfg::kStageBytes >> 4;
@@ -281,9 +282,9 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       if (++s == stages) s = 0, phase ^= 1, da = da0, ds = ds0;
       ready = tc::mbar_test_wait(&full[s], phase);
       if (left > 2)
-        tc::mma_mxf4(tmem, d, d + kToB, tc::idesc_mxf4(128, BN, 0), sfa + 4, sfb + 4, 1);
+        tc::mma_mxf4(tmem, d, d + kToB, tc::idesc_mxf4(128, BN, 0), sfa + 4, sfx + 4, 1);
       if (left > 3)
-        tc::mma_mxf4(tmem, d + 2, d + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa + 4, sfb + 4, 1);
+        tc::mma_mxf4(tmem, d + 2, d + kToB + 2, tc::idesc_mxf4(128, BN, 2), sfa + 4, sfx + 4, 1);
       tc::mma_commit(mine);
     }
     tc::mma_commit(done);
@@ -856,17 +857,21 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
                : a.vec                 ? m.out / (16 / (int64_t)dtype_size(m.dtype)) * (16 / (int64_t)dtype_size(m.dtype))
                                        : 0;
   const int dev = current_device();
-  // Tiles of 256 x 256 by pairs of SMs from 257 rows on (us, pairs and 128-column tiles: 512 rows of
-  // 4096 to 4096 11.3 and 13.4, 1024 12.2 and 25.6, 10000 of 784 to 128 8.2 and 7.6; 200 of 4096
-  // to 1000 10.5 and 7.7), else the narrowest columns that hold the rows.
-  if (m.rows > 256)
-    return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, dev, st)
-           : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, dev, st)
-                                      : launch_pair<AGN_PREC_MX4>(m, a, dev, st);
-  return m.rows <= 16   ? launch_linear<16>(m, a, dev, st)
-         : m.rows <= 32 ? launch_linear<32>(m, a, dev, st)
-         : m.rows <= 64 ? launch_linear<64>(m, a, dev, st)
-                        : launch_linear<128>(m, a, dev, st);
+  // One tile of rows while it holds them all.  More: tiles of 64 rows while K can be split
+  // over four CTAs for each, pairs of CTAs from 257 rows, or from 129 with 64 tiles of 128 x
+  // 128, else tiles of 128.  us with 64, 128, pairs: 200 rows of 1000 to 1000 5.3, 6.1, 6.4; 1024
+  // of 784 to 128 5.2, 6.4, 6.5; 128 of 4096 to 4096 8.9, 8.0, 9.8; 200 of 4096 to 4096 10.9, 10.5,
+  // 9.8; 300 of 4096 to 4096 20.1, 12.3, 10.2.
+  if (m.rows <= 16) return launch_linear<16>(m, a, dev, st);
+  if (m.rows <= 32) return launch_linear<32>(m, a, dev, st);
+  const int64_t tiles_f = ceil_div(m.out, 128);
+  if (m.rows <= 64 || tiles_f * ceil_div(m.rows, 64) <=
+                          max_clusters<Tile<64>>(mx4_linear_kernel<64>, kThreads, Tile<64>::kSmem, 4, dev))
+    return launch_linear<64>(m, a, dev, st);
+  if (m.rows <= 128 || (m.rows <= 256 && 2 * tiles_f < 64)) return launch_linear<128>(m, a, dev, st);
+  return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, dev, st)
+         : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, dev, st)
+                                    : launch_pair<AGN_PREC_MX4>(m, a, dev, st);
 }
 
 namespace {
