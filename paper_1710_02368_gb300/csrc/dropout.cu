@@ -33,6 +33,9 @@ constexpr int blocks_per_sm(bool two, bool sums) { return two && sums ? 3 : 4; }
 constexpr int unroll(bool two, bool sums) { return two ? (sums ? 3 : 2) : 4; }
 constexpr int kMaxUnits = 32;   // 16-byte units of a row in a block's tile
 
+// How the rows of the call's matrices lie to 16-byte boundaries.
+enum Rows { kOther, kAligned, kAlike };
+
 struct DropArgs {
   const void* x;          // forward: input; backward: the layer's input (ReLU), or null
   const float* bias;      // [cols] or null
@@ -44,7 +47,10 @@ struct DropArgs {
   uint64_t key, offset;
   uint32_t t16;           // T << 16
   float scale;
-  int relu, vec;          // vec: every row of every matrix starts 16-byte aligned
+  int relu;
+  // Rows::kAligned, kAlike (every matrix's row r starts `start` + r ldy elements past a 16-byte
+  // boundary, modulo 16 bytes), kOther
+  int layout, start;
   int tile_units;         // units of 16 bytes of a row in a block's tile: a thread each
   // hidden layers of a training run (kHidden): matrices [slots][rows][cols]
   const int* slot_worker;
@@ -54,16 +60,16 @@ struct DropArgs {
   int64_t plane;
 };
 
-// 16 bytes of a row, as they are: from aligned memory in one load, else the n
-// valid elements one by one.
+// 16 bytes of a row, as they are: from aligned memory in one load, else the
+// valid elements lo .. n - 1 one by one.
 template <typename T>
-__device__ __forceinline__ uint4 load16(const T* p, bool full, int n) {
+__device__ __forceinline__ uint4 load16(const T* p, bool full, int lo, int n) {
   if (full) return AGN_LD(reinterpret_cast<const uint4*>(p));
   uint4 q = make_uint4(0, 0, 0, 0);
   T* e = reinterpret_cast<T*>(&q);
 #pragma unroll
   for (int i = 0; i < (int)(16 / sizeof(T)); ++i)
-    if (i < n) e[i] = AGN_LD(p + i);
+    if (i >= lo && i < n) e[i] = AGN_LD(p + i);
   return q;
 }
 template <typename T>
@@ -87,7 +93,8 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return r;
 }
 template <typename T>
-__device__ __forceinline__ void store16(T* p, bool full, int n, const float (&v)[16 / sizeof(T)]) {
+__device__ __forceinline__ void store16(T* p, bool full, int lo, int n,
+                                        const float (&v)[16 / sizeof(T)]) {
   uint4 q;
   T* e = reinterpret_cast<T*>(&q);
 #pragma unroll
@@ -97,7 +104,7 @@ __device__ __forceinline__ void store16(T* p, bool full, int n, const float (&v)
   } else {
 #pragma unroll
     for (int i = 0; i < (int)(16 / sizeof(T)); ++i)
-      if (i < n) AGN_ST(p + i, e[i]);
+      if (i >= lo && i < n) AGN_ST(p + i, e[i]);
   }
 }
 
@@ -113,18 +120,35 @@ __device__ __forceinline__ bool kept(uint64_t d, int e, uint32_t t16) {
 // in registers) and steps down the rows.
 // kTwo: two input matrices (forward: x and the residual; backward: dy and the ReLU's x).
 // kSums: backward with the bias's gradient.
-template <typename T, bool kBackward, bool kTwo, bool kSums, bool kHidden = false>
+// kShift: rows that are not aligned, but all alike (Rows::kAlike).  A thread's 16 bytes
+// are aligned ones, so its columns start up to 16 bytes before the tile's; its rows are a
+// multiple of 8 apart and start at the same place, so they are the same columns all the way down.
+// With column sums a tile has a unit less than its threads: the last reads the unit that
+// the next tile's first reads and stores, and each sums the columns of its own tile (so the output
+// is no input here).  Against elements one by one, us: 19620 x 287 bf16 9.9 for 27.5, with ReLU and
+// sums 39 for 73; 16384 x 4095 bf16 94 for 160 (aligned 4096: 51, two draws for this one's three);
+// 2865 x 3183 fp32 12.2 for 12.0, with sums 14.2 for 21.0.
+template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_kernel(const DropArgs a) {
   constexpr int V = 16 / sizeof(T), kUnroll = kHidden ? 2 : unroll(kTwo, kSums);
   constexpr bool kReadX = !kBackward || kTwo, kReadExtra = kBackward || kTwo;
   pdl_begin();
   const int w = a.tile_units, ty = threadIdx.x / w, tx = threadIdx.x % w;
   const int nty = kThreads / w;   // (threads past w nty have no rows)
-  const int64_t c = ((int64_t)blockIdx.x * w + tx) * V;
-  const int n = c < a.cols && ty < nty ? (int)min((int64_t)V, a.cols - c) : 0;   // its elements
-  const bool full = a.vec && n == V;
+  constexpr bool kShared = kShift && kSums;   // the last unit is the next tile's too
+  const int own = (kShared ? w - 1 : w) * V;  // columns of a tile
   const int64_t r0 = blockIdx.y * a.rows_per_block;
   const int64_t r1 = min(a.rows, r0 + a.rows_per_block);
+  const int64_t tile0 = (int64_t)blockIdx.x * own;
+  // row t of the block starts so many elements past a boundary
+  auto past = [&](int t) { return (int)((a.start + (uint32_t)(r0 + t) * (uint32_t)a.ldy) & (V - 1)); };
+  const int m = kShift ? past(ty) : 0;
+  const int64_t c = tile0 + tx * V - m;
+  // this thread's elements: lo .. n - 1
+  const int lo = kShift && c < 0 ? m : 0;
+  const bool last = kShared && tx == w - 1 && blockIdx.x + 1 < gridDim.x;
+  const int n = ty < nty && c + lo < a.cols && !(last && m == 0) ? (int)min((int64_t)V, a.cols - c) : 0;
+  const bool full = (kShift || a.layout == kAligned) && lo == 0 && n == V;
   const uint64_t groups = (uint64_t)((a.cols + 3) / 4);
   const T* x = static_cast<const T*>(a.x);
   const T* extra = static_cast<const T*>(a.extra);
@@ -142,11 +166,12 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
     y += z * a.rows * a.ldy;
     piece0 = z * a.rows * a.ldy;
   }
-  first += (uint64_t)c / 4;
+  first += (uint64_t)(c >> 2);
+  const int skip = (int)(c & 3);   // (kShift: elements of the first draw before this thread's)
   float b[V], sum[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    b[e] = a.bias && e < n ? AGN_LD(a.bias + c + e) : 0.f;
+    b[e] = a.bias && e >= lo && e < n ? AGN_LD(a.bias + c + e) : 0.f;
     sum[e] = 0.f;
   }
   if (n > 0) {
@@ -158,8 +183,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t ru = r + (int64_t)u * nty;
         if (ru >= r1) break;
-        if (kReadX) v[u] = load16(x + ru * a.ldx + c, full, n);
-        if (kReadExtra) q[u] = load16(extra + ru * a.lde + c, full, n);
+        if (kReadX) v[u] = load16(x + ru * a.ldx + c, full, lo, n);
+        if (kReadExtra) q[u] = load16(extra + ru * a.lde + c, full, lo, n);
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -168,6 +193,24 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
         uint64_t d[V / 4];   // draw(key, i) = mix(key + (i + 1) G), from z by addition
 #pragma unroll
         for (int g = 0; g < V / 4; ++g) d[g] = gen::mix(z + (uint64_t)g * gen::kG);
+        if (kShift) {   // 16 skip bits off the front, the rest from one more draw
+          const uint64_t more = gen::mix(z + (uint64_t)(V / 4) * gen::kG);
+          uint32_t s[V / 2 + 2];
+#pragma unroll
+          for (int g = 0; g <= V / 4; ++g) {
+            const uint64_t f = g < V / 4 ? d[g < V / 4 ? g : 0] : more;
+            s[2 * g] = (uint32_t)f;
+            s[2 * g + 1] = (uint32_t)(f >> 32);
+          }
+#pragma unroll
+          for (int i = 0; i <= V / 2; ++i) s[i] = skip & 2 ? s[i + 1] : s[i];
+#pragma unroll
+          for (int g = 0; g < V / 4; ++g) {
+            const uint32_t l = __funnelshift_r(s[2 * g], s[2 * g + 1], 16 * (skip & 1));
+            const uint32_t h = __funnelshift_r(s[2 * g + 1], s[2 * g + 2], 16 * (skip & 1));
+            d[g] = (uint64_t)h << 32 | l;
+          }
+        }
         z += z_step;
         float o[V];
 #pragma unroll
@@ -199,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
           o[e] = t.x;
           o[e + 1] = t.y;
         }
-        store16(y + ru * a.ldy + c, full, n, o);
+        if (!last) store16(y + ru * a.ldy + c, full, lo, n, o);
         if (kHidden && a.pieces) {
           bf16* pp = a.pieces + piece0 + ru * a.ldy + c;
 #pragma unroll
@@ -227,15 +270,15 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
       for (int e = 0; e < V; ++e) part[ty * width + tx * V + e] = sum[e];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < width; j += kThreads) {
+    for (int j = threadIdx.x; j < own; j += kThreads) {
       float s = 0.f;
-      for (int t = 0; t < nty; ++t) s += part[t * width + j];
+      for (int t = 0; t < nty; ++t) s += part[t * width + j + (kShift ? past(t) : 0)];
       col[j] = s;
     }
     cluster_sync();
     const int ranks = gridDim.y;
-    for (int j = threadIdx.x; j < width; j += kThreads) {
-      const int64_t cj = (int64_t)blockIdx.x * width + j;
+    for (int j = threadIdx.x; j < own; j += kThreads) {
+      const int64_t cj = tile0 + j;
       if (j % ranks != (int)blockIdx.y || cj >= a.cols) continue;
       float s = 0.f;
       for (int k = 0; k < ranks; ++k) s += ld_cluster(col + j, k);
@@ -247,19 +290,17 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
 
 constexpr int kMaxCluster = 8;
 
-template <typename T>
-struct Two {};   // (max_clusters' tag of the kernel with two inputs)
-
-template <typename T>
-Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
+// The launch of one instantiation: tiles, rows and clusters.
+template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
+Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const int dev = current_device(), sms = device_sms(dev);
-  const int64_t units = ceil_div(a.cols, V);
-  const bool sums = backward && a.dbias;
-  const bool two = backward ? a.x != nullptr : a.extra != nullptr;
-  const int64_t fit = std::max<int64_t>(1, (int64_t)sms * blocks_per_sm(two, sums) / slots);   // resident blocks
+  auto kern = dropout_kernel<T, kBackward, kTwo, kSums, kShift, kHidden>;
+  const int dev = current_device();
+  const int64_t units = ceil_div(a.cols, V) + (kShift && !kSums ? 1 : 0);   // (a part at each end)
+  const int64_t fit =   // resident blocks
+      std::max<int64_t>(1, (int64_t)device_sms(dev) * blocks_per_sm(kTwo, kSums) / slots);
   int64_t tiles = 0, blocks = 0;
-  if (!sums) {
+  if (!kSums) {
     // wide tiles, and as many blocks down the rows as are resident
     int best = 1;
     for (int w = 2; w <= kMaxUnits; w *= 2)
@@ -272,16 +313,16 @@ Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
   } else {
     // A cluster has all the rows of its tile.  The kernel is as much bound by instructions
     // as by memory, so what counts is how many of the resident blocks have work, in one
-    // round: the width (whole 32-byte sectors) and the cluster with the most, the widest of
-    // about equals (16384 x 4096 bf16 at four blocks an SM: 64 tiles of 8 units, clusters of 8, 512
-    // of 608 blocks, 78 us; 86 of 6 units and clusters of 7, 602 blocks but two rounds, 102 us).
+    // round: the width (whole 32-byte sectors; shifted rows: powers of two) and the cluster
+    // with the most, the widest of about equals (16384 x 4096 bf16 at four blocks an SM: 64 tiles
+    // of 8 units, clusters of 8, 512 of 608 blocks, 78 us; 86 of 6 units and clusters of 7, 602
+    // blocks but two rounds, 102 us).
     double most = 0.0;
-    for (int w = 16; w >= 2; w -= 2) {
-      const int64_t t = ceil_div(units, w);
+    for (int w = 16; w >= 2; w = kShift ? w / 2 : w - 2) {
+      const int64_t t = ceil_div(units, kShift ? w - 1 : w);
       int64_t c = std::min<int64_t>(kMaxCluster, std::max<int64_t>(1, ceil_div(a.rows, kThreads / w)));
-      while (c > 1 && (two ? max_clusters<Two<T>>(dropout_kernel<T, true, true, true>, kThreads, 0, (int)c, dev)
-                           : max_clusters<T>(dropout_kernel<T, true, false, true>, kThreads, 0, (int)c, dev)) < t)
-        --c;
+      struct Tag {};
+      while (c > 1 && max_clusters<Tag>(kern, kThreads, 0, (int)c, dev) < t) --c;
       const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
       if (used > most * 1.02) {
         most = used;
@@ -293,21 +334,31 @@ Status launch_dropout(DropArgs a, bool backward, int slots, cudaStream_t st) {
     a.rows_per_block = std::max<int64_t>(1, ceil_div(a.rows, blocks));
   }
   const dim3 grid((unsigned)tiles, (unsigned)blocks, (unsigned)slots);
-  auto k = a.slot_worker ? dropout_kernel<T, false, false, false, true>
-           : sums        ? (a.x ? dropout_kernel<T, true, true, true> : dropout_kernel<T, true, false, true>)
-           : backward    ? (a.x ? dropout_kernel<T, true, true, false> : dropout_kernel<T, true, false, false>)
-           : a.extra     ? dropout_kernel<T, false, true, false>
-                         : dropout_kernel<T, false, false, false>;
-  if (sums)
-    AGN_TRY_CUDA(launch_pdl_cluster(k, grid, kThreads, 0, dim3(1, grid.y, 1), st, a));
+  if (kSums)
+    AGN_TRY_CUDA(launch_pdl_cluster(kern, grid, kThreads, 0, dim3(1, grid.y, 1), st, a));
   else
-    AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
+    AGN_TRY_CUDA(launch_pdl(kern, grid, kThreads, 0, st, a));
   return Status::Ok();
 }
 
-Status run_dropout(DropArgs a, bool backward, int dtype, int slots, cudaStream_t st) {
-  return dtype == AGN_PREC_FP32 ? launch_dropout<float>(a, backward, slots, st)
-                                : launch_dropout<bf16>(a, backward, slots, st);
+template <typename T, bool kBackward, bool kTwo, bool kSums>
+Status launch_rows(const DropArgs& a, cudaStream_t st) {
+  return a.layout == kAlike ? launch_kernel<T, kBackward, kTwo, kSums, true>(a, 1, st)
+                            : launch_kernel<T, kBackward, kTwo, kSums, false>(a, 1, st);
+}
+
+template <typename T>
+Status launch_dropout(const DropArgs& a, bool backward, cudaStream_t st) {
+  if (!backward)
+    return a.extra ? launch_rows<T, false, true, false>(a, st) : launch_rows<T, false, false, false>(a, st);
+  if (a.dbias)
+    return a.x ? launch_rows<T, true, true, true>(a, st) : launch_rows<T, true, false, true>(a, st);
+  return a.x ? launch_rows<T, true, true, false>(a, st) : launch_rows<T, true, false, false>(a, st);
+}
+
+Status run_dropout(const DropArgs& a, bool backward, int dtype, cudaStream_t st) {
+  return dtype == AGN_PREC_FP32 ? launch_dropout<float>(a, backward, st)
+                                : launch_dropout<bf16>(a, backward, st);
 }
 
 Status set_probability(double p, DropArgs* a) {
@@ -318,8 +369,15 @@ Status set_probability(double p, DropArgs* a) {
   return Status::Ok();
 }
 
-bool rows_aligned(const void* p, int64_t ld, size_t es) {
-  return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && (size_t)ld * es % 16 == 0);
+// The layout of up to three matrices (null: none); the last is the output.
+void set_layout(DropArgs* a, const void* p0, int64_t ld0, const void* p1, int64_t ld1, const void* y,
+                int64_t ldy, size_t es) {
+  auto at = [&](const void* p) { return (int)(reinterpret_cast<uintptr_t>(p) % 16 / es); };
+  auto step = [&](int64_t ld) { return (int)((uint64_t)ld * es % 16 / es); };
+  const bool alike = (!p0 || (at(p0) == at(y) && step(ld0) == step(ldy))) &&
+                     (!p1 || (at(p1) == at(y) && step(ld1) == step(ldy)));
+  a->start = at(y);
+  a->layout = !alike ? kOther : at(y) == 0 && step(ldy) == 0 ? kAligned : kAlike;
 }
 
 Status forward(const void* x, const float* bias, const void* residual, void* y, int dtype,
@@ -348,10 +406,10 @@ Status forward(const void* x, const float* bias, const void* residual, void* y, 
   a.key = gen::key(seed, gen::kDropout);
   a.offset = offset;
   a.relu = relu != 0;
-  a.vec = rows_aligned(x, ldx, es) && rows_aligned(y, ldy, es) && rows_aligned(residual, ldr, es);
+  set_layout(&a, x, ldx, residual, ldr, y, ldy, es);
   KnownBuffers known({bx, bb, br, by});
   AGN_TRY(bounds_upload(st));
-  AGN_TRY(run_dropout(a, false, dtype, 1, st));
+  AGN_TRY(run_dropout(a, false, dtype, st));
   return bounds_collect(st);
 }
 
@@ -384,10 +442,11 @@ Status backward(const void* dy, const void* x, const float* bias, void* dx, floa
   a.key = gen::key(seed, gen::kDropout);
   a.offset = offset;
   a.relu = relu != 0;
-  a.vec = rows_aligned(x, ldx, es) && rows_aligned(dx, lddx, es) && rows_aligned(dy, lddy, es);
+  set_layout(&a, x, ldx, dy, lddy, dx, lddx, es);
+  if (a.layout == kAlike && dbias && (dx == dy || dx == x)) a.layout = kOther;   // (kShift)
   KnownBuffers known({bg, bx, bb, bo, bs});
   AGN_TRY(bounds_upload(st));
-  AGN_TRY(run_dropout(a, true, dtype, 1, st));
+  AGN_TRY(run_dropout(a, true, dtype, st));
   return bounds_collect(st);
 }
 
@@ -408,11 +467,12 @@ Status dropout_hidden(const HiddenDropArgs& h, int slots, cudaStream_t st) {
   a.x = h.H; a.y = h.H;
   a.rows = h.m; a.cols = h.d; a.ldx = h.d; a.ldy = h.d;
   a.key = gen::key(h.seed, gen::kDropout);
-  a.vec = rows_aligned(h.H, h.d, sizeof(T));
+  set_layout(&a, nullptr, 0, nullptr, 0, h.H, h.d, sizeof(T));
+  if (a.layout == kAlike) a.layout = kOther;   // (small: one by one)
   a.slot_worker = h.slot_worker; a.slot_t0 = h.slot_t0;
   a.step = h.step; a.layers = h.layers; a.layer = h.layer;
   a.pieces = h.pieces; a.plane = h.plane;
-  return launch_dropout<T>(a, false, slots, st);
+  return launch_kernel<T, false, false, false, false, true>(a, slots, st);
 }
 template Status dropout_hidden<float>(const HiddenDropArgs&, int, cudaStream_t);
 template Status dropout_hidden<bf16>(const HiddenDropArgs&, int, cudaStream_t);

@@ -128,6 +128,51 @@ def test_strides_and_alignment(agn, torch, dtype, ldx, ldr, ldy, start):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,cols,ld,start", [(1, 9, 9, 5), (70, 3, 5, 1), (211, 24, 24, 3), (530, 63, 67, 2), (1030, 287, 287, 0),
+                                                (95, 1001, 1002, 7), (64, 260, 264, 4), (2050, 121, 125, 6)])
+@pytest.mark.parametrize("two,sums", [(0, 0), (1, 0), (0, 1), (1, 1)])
+def test_rows_that_start_alike_but_unaligned(agn, torch, dtype, rows, cols, ld, start, two, sums):
+    """Every matrix's rows lie the same way to 16 bytes; what is between and around the rows stays."""
+    rng = np.random.default_rng(rows + cols)
+    p, seed, offset = 0.4, 77, 5
+    _, a = strided(torch, dtype, rows, ld, start, rng)
+    _, b = strided(torch, dtype, rows, ld, start, rng)
+    buf, y = strided(torch, dtype, rows, ld, start, rng, fill=7.0)
+    bias = torch.tensor(rng.standard_normal(cols), dtype=torch.float32, device="cuda")
+    live = R.keep_mask(rows, cols, p, seed, offset)
+    x, other = f64(a)[:, :cols], f64(b)[:, :cols]
+    if sums:   # backward: dy a, the ReLU's input b
+        db = torch.full((cols + 2,), 7.0, device="cuda")
+        agn.agn_dropout_backward(a, y, dtype, rows, cols, p, seed, offset, x=b if two else None, bias=bias if two else None,
+                                 dbias=db[1:], relu=two, lddy=ld, ldx=ld, lddx=ld)
+        if two:
+            live = live & (other + f64(bias) > 0)
+        want = np.where(live, x * R.gain(p), 0.0)
+        tol = 1.01 * (2 * 2.0 ** -24 + HALF[dtype]) * np.abs(want)
+        # as in test_backward
+        check(f64(db)[1:-1], want.sum(0), 1.01 * (rows + 1) * 2.0 ** -24 * np.abs(want).sum(0) + 1e-45)
+        assert db[0] == 7 and db[-1] == 7
+    else:
+        agn.agn_dropout(a, y, dtype, rows, cols, p, seed, offset, bias=bias, residual=b if two else None, relu=1,
+                        ldx=ld, ldr=ld, ldy=ld)
+        t = np.where(live, np.maximum(x + f64(bias), 0) * R.gain(p), 0.0)
+        want = t + (other if two else 0.0)
+        # as in test_forward
+        term = 3 * 2.0 ** -24 * np.abs(t)
+        tol = 1.01 * (term + 2.0 ** -24 * np.abs(want) + HALF[dtype] * (np.abs(want) + term)) + 1e-45
+    check(f64(y)[:, :cols], want, tol)
+    if sums:   # in place: the same bits
+        c, db2 = a.clone(), torch.empty_like(db[1:])
+        agn.agn_dropout_backward(a, a, dtype, rows, cols, p, seed, offset, x=b if two else None, bias=bias if two else None,
+                                 dbias=db2, relu=two, lddy=ld, ldx=ld, lddx=ld)
+        assert torch.equal(a[:, :cols], y[:, :cols]) and torch.equal(a[:, cols:], c[:, cols:])
+        check(f64(db2)[:-1], want.sum(0), 1.01 * (rows + 1) * 2.0 ** -24 * np.abs(want).sum(0) + 1e-45)
+    rest = f64(buf)
+    rest[start:start + rows * ld].reshape(rows, ld)[:, :cols] = 7.0
+    assert np.all(rest == 7.0)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 def test_in_place(agn, torch, dtype):
     rng = np.random.default_rng(6)
     x = torch.tensor(rng.standard_normal((65, 133)), device="cuda").to(dt(torch, dtype))
