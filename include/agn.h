@@ -440,7 +440,8 @@ int agn_commit_pull_noalloc(float* theta_c, float* acc, float* replicas, void* r
  *   dtype     : AGN_PREC_FP32 or AGN_PREC_BF16, of x, residual and y;
  *   bias      : device fp32 [cols], NULL = none;  residual: NULL = none;
  *   ldx, ldr, ldy: row strides in elements, >= cols (ldr unused without a
- *               residual); rows that start on 16-byte boundaries are faster;
+ *               residual); rows that start on 16-byte boundaries are fastest, rows that
+ *               start equally far past one in every matrix next;
  *   y         : may be x or the residual itself with the same stride (in place);
  *               any other overlap (of the bytes from a matrix's first element to its
  *               last) is AGN_E_INVALID.  Bytes between the rows are left alone.

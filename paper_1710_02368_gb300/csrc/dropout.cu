@@ -126,7 +126,7 @@ __device__ __forceinline__ bool kept(uint64_t d, int e, uint32_t t16) {
 // With column sums a tile has a unit less than its threads: the last reads the unit that
 // the next tile's first reads and stores, and each sums the columns of its own tile (so the output
 // is no input here).  Against elements one by one, us: 19620 x 287 bf16 9.9 for 27.5, with ReLU and
-// sums 39 for 73; 16384 x 4095 bf16 94 for 160 (aligned 4096: 51, two draws for this one's three);
+// sums 29 for 73; 16384 x 4095 bf16 94 for 160 (aligned 4096: 51, two draws for this one's three);
 // 2865 x 3183 fp32 12.2 for 12.0, with sums 14.2 for 21.0.
 template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_kernel(const DropArgs a) {
@@ -288,7 +288,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
   }
 }
 
-constexpr int kMaxCluster = 8;
+// Blocks of a cluster: the portable eight, and more where a thread has so many rows (see
+// launch_kernel).
+constexpr int kMaxCluster = 8, kWideCluster = 16, kWideRows = 16;
 
 // The launch of one instantiation: tiles, rows and clusters.
 template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
@@ -313,22 +315,30 @@ Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
   } else {
     // A cluster has all the rows of its tile.  The kernel is as much bound by instructions
     // as by memory, so what counts is how many of the resident blocks have work, in one
-    // round: the width (whole 32-byte sectors; shifted rows: powers of two) and the cluster
-    // with the most, the widest of about equals (16384 x 4096 bf16 at four blocks an SM: 64 tiles
-    // of 8 units, clusters of 8, 512 of 608 blocks, 78 us; 86 of 6 units and clusters of 7, 602
-    // blocks but two rounds, 102 us).
+    // round: the width (whole 32-byte sectors but for a row of one unit; shifted rows: powers of
+    // two) and the cluster with the most, the widest of about equals (16384 x 4096 bf16 at four
+    // blocks an SM: 64 tiles of 8 units, clusters of 8, 512 of 608 blocks, 78 us; 86 of 6 units and
+    // clusters of 7, 602 blocks but two rounds, 102 us).  Where that leaves a quarter idle,
+    // clusters of up to 16, if threads have kWideRows rows or more of eight blocks (us, 8 and 16:
+    // 65536 x 64 bf16 28 and 16, 16384 x 32 fp32 7.5 and 5.3; 2048 x 1000 fp32, 8 rows, 6.1 and
+    // 6.5; 16384 x 4096 bf16 without ReLU, 512 blocks with 8, 52.5 and 54.1).
     double most = 0.0;
-    for (int w = 16; w >= 2; w = kShift ? w / 2 : w - 2) {
-      const int64_t t = ceil_div(units, kShift ? w - 1 : w);
-      int64_t c = std::min<int64_t>(kMaxCluster, std::max<int64_t>(1, ceil_div(a.rows, kThreads / w)));
-      struct Tag {};
-      while (c > 1 && max_clusters<Tag>(kern, kThreads, 0, (int)c, dev) < t) --c;
-      const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
-      if (used > most * 1.02) {
-        most = used;
-        a.tile_units = w;
-        tiles = t;
-        blocks = c;
+    const int narrowest = kShift || units > 1 ? 2 : 1;
+    for (int widest : {kMaxCluster, kWideCluster}) {
+      if (4 * most > 3 * (double)fit) break;
+      for (int w = 16; w >= narrowest; w = kShift || w == 2 ? w / 2 : w - 2) {
+        const int64_t t = ceil_div(units, kShift ? w - 1 : w), nty = kThreads / w;
+        if (widest == kWideCluster && a.rows < kMaxCluster * kWideRows * nty) continue;
+        int64_t c = std::min<int64_t>(widest, std::max<int64_t>(1, ceil_div(a.rows, nty)));
+        struct Tag {};
+        while (c > 1 && max_clusters<Tag>(kern, kThreads, 0, (int)c, dev) < t) --c;
+        const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
+        if (used > most * 1.02) {
+          most = used;
+          a.tile_units = w;
+          tiles = t;
+          blocks = c;
+        }
       }
     }
     a.rows_per_block = std::max<int64_t>(1, ceil_div(a.rows, blocks));

@@ -124,15 +124,16 @@ cudaError_t allow_smem(void (*kern)(KArgs...), size_t smem, int dev) {
   return e;
 }
 
-// Clusters of c blocks (along y; 1 <= c <= 8) of this kernel that are resident at once on
-// the current device: fewer blocks than single ones, since a cluster stays within a GPC (a block to an
-// SM: 152 single ones, 36 clusters of four, 15 of eight).  Asked once for each Tag and device.
+// Clusters of c blocks (along y; more than the portable 8 are allowed for the kernel first)
+// of this kernel that are resident at once on the current device: fewer blocks than single ones,
+// since a cluster stays within a GPC (a block to an SM: 152 single ones, 36 clusters of four, 15 of
+// eight); 0 where they cannot be.  Asked once for each Tag and device.
 template <typename Tag, typename... KArgs>
 int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c, int dev) {
-  static std::atomic<int> known[kMaxDevices + 1][9];
-  if (c < 1 || c > 8) return 1;
-  int n = known[dev][c].load(std::memory_order_relaxed);
-  if (n == 0) {
+  static std::atomic<int> known[kMaxDevices + 1][17];   // + 1
+  if (c < 1 || c > 16) return 0;
+  int n = known[dev][c].load(std::memory_order_relaxed) - 1;
+  if (n < 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(1, (unsigned)c, 1);
     cfg.blockDim = threads;
@@ -146,11 +147,13 @@ int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c, int de
     cfg.numAttrs = 1;
     if ((smem > 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                           (int)smem) != cudaSuccess) ||
+        (c > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+                      cudaSuccess) ||
         cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
       cudaGetLastError();
-      n = 1;
+      n = c > 8 ? 0 : 1;
     }
-    known[dev][c].store(n, std::memory_order_relaxed);
+    known[dev][c].store(n + 1, std::memory_order_relaxed);
   }
   return n;
 }

@@ -100,6 +100,14 @@ def test_backward(agn, torch, dtype, rows, cols, relu, sums):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,cols", [(40000, 8), (33001, 4), (20011, 16), (17000, 33), (65536, 2)])
+@pytest.mark.parametrize("relu", [0, 1])
+def test_sums_of_tall_matrices(agn, torch, dtype, rows, cols, relu):
+    """Wide clusters down the rows."""
+    test_backward(agn, torch, dtype, rows, cols, relu, 1)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("ldx,ldr,ldy,start", [(20, 20, 20, 0), (21, 17, 19, 0), (24, 24, 24, 1), (17, 32, 24, 3)])
 def test_strides_and_alignment(agn, torch, dtype, ldx, ldr, ldy, start):
     rng = np.random.default_rng(5)
