@@ -19,10 +19,11 @@ namespace agn {
 namespace {
 
 constexpr int kThreads = 256;
-// Rows of a thread whose loads are in flight together, quantising and back, and resident
-// blocks of an SM.  us, 16384 x 4096 fp32 and bf16, 10000 x 784 fp32: quantising 50, 30, 8.4
-// (rows 4 and blocks 6: 49, 30, 9.7; 2 and 6: 59, 33, 9.5), back 50, 29, 8.7 (2 and 6: 54, 32, 9.9).
-constexpr int kQuantRows = 2, kBackRows = 8, kBlocksPerSm = 8;
+// Rows of a thread whose loads are in flight together, quantising, back, and back into rows that
+// are not aligned (two, four, eight: 65536 x 100 bf16 11.0, 11.2, 14.1), and resident blocks of an
+// SM.  us, 16384 x 4096 fp32 and bf16, 10000 x 784 fp32: quantising 50, 30, 8.4
+// (rows 4 and blocks 6: 49, 30, 9.7; 2 and 6: 59, 33, 9.5), back 49, 28, 8.7 (2 and 6: 54, 32, 9.9).
+constexpr int kQuantRows = 2, kBackRows = 8, kShiftRows = 2, kBlocksPerSm = 8;
 
 // Elements of a lane, its lanes of a block and of four blocks (a scale word).
 template <typename T>
@@ -40,20 +41,42 @@ struct MxArgs {
   int64_t rows, cols, ld;
   int64_t row_bytes, tiles_k;
   int64_t rows_per_block;
-  int vec;              // rows of x (y) start 16-byte aligned (1), 32-byte (2)
+  int vec;              // rows of x (y) start 16-byte aligned (1), 32-byte (2), neither (0)
+  const void* x_end;    // past x's last element
   int tx_shift;         // log2 of the lanes along a row (>= those of a word)
 };
 
-// 32 bytes of a row as they are: one load (vec 2: 32-byte aligned), two (vec 1), or the n
-// valid elements (vec 0).
+// 32 bytes of a row as they are: one load (vec 2: 32-byte aligned), two (vec 1), the 48 aligned
+// bytes that hold them (vec 0, 48 bytes within the matrix begin .. end), or the n valid elements.
 template <typename T>
 struct __align__(32) Raw {
   uint4 q[2];
 };
-template <typename T>
-__device__ __forceinline__ Raw<T> load32(const T* p, int vec, int n) {
+template <typename T, bool kShift>
+__device__ __forceinline__ Raw<T> load32(const T* p, int vec, int n, const void* begin,
+                                         const void* end) {
   Raw<T> r;
-  if (vec == 2) {
+  const uint32_t past = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15;
+  const char* from = reinterpret_cast<const char*>(p) - past;
+  const bool whole = n == Lanes<T>::kElems;
+  if (kShift && whole && from >= begin && from + 48 <= end) {
+    uint32_t w[12];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(from) + i);
+      w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 10; ++i) w[i] = past & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 9; ++i) w[i] = past & 4 ? w[i + 1] : w[i];
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (past & 2));
+    }
+    r.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    r.q[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  } else if (!kShift && whole && vec == 2) {
     if (AGN_BOUNDS_OK(p, 32)) {
       asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(r.q[0].x), "=r"(r.q[0].y), "=r"(r.q[0].z), "=r"(r.q[0].w), "=r"(r.q[1].x),
@@ -63,7 +86,7 @@ __device__ __forceinline__ Raw<T> load32(const T* p, int vec, int n) {
       AGN_BOUNDS_FAIL(p);
       r.q[0] = r.q[1] = make_uint4(0, 0, 0, 0);
     }
-  } else if (vec == 1) {
+  } else if (!kShift && whole && vec == 1) {
     r.q[0] = AGN_LD(reinterpret_cast<const uint4*>(p));
     r.q[1] = AGN_LD(reinterpret_cast<const uint4*>(p) + 1);
   } else {
@@ -108,7 +131,8 @@ __device__ __forceinline__ uint32_t largest(const Raw<bf16>& r) {   // two halve
   return max(m & 0xffff0000u, m << 16);
 }
 
-template <typename T>
+// kShift: rows that are not 16-byte aligned (16384 x 4095 bf16 44 us, with single elements 70).
+template <typename T, bool kShift>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(const MxArgs a) {
   using L = Lanes<T>;
   constexpr int kUnroll = kQuantRows;
@@ -119,7 +143,6 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(const MxArgs a) 
   const int64_t c = unit * L::kElems, kq = unit / L::kWord;        // and its scale word
   const int64_t r0 = blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const int n = c < a.cols ? (int)min((int64_t)L::kElems, a.cols - c) : 0;
-  const int vec = n == L::kElems ? a.vec : 0;
   const bool in_row = c / 2 < a.row_bytes, leads = tx % L::kWord == 0 && kq < a.tiles_k;
   const T* x = static_cast<const T*>(a.x) + (r0 + ty) * a.ld + c;
   uint8_t* codes = a.codes + (r0 + ty) * a.row_bytes + c / 2;
@@ -129,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(const MxArgs a) 
     Raw<T> raw[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-      if (r + (int64_t)u * nty < r1) raw[u] = load32(x + (int64_t)u * nty * a.ld, vec, n);
+      if (r + (int64_t)u * nty < r1) raw[u] = load32<T, kShift>(x + (int64_t)u * nty * a.ld, a.vec, n, a.x, a.x_end);
     x += (int64_t)kUnroll * nty * a.ld;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u, codes += nty * a.row_bytes) {
@@ -173,8 +196,7 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(const MxArgs a
   const int64_t c = unit * L::kElems;
   const int64_t r0 = blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const bool in_row = c / 2 < a.row_bytes;
-  const bool full = a.vec && c + L::kElems <= a.cols;
-  const uint32_t group = ((1u << L::kWord) - 1) << (threadIdx.x & 31 & ~(L::kWord - 1));
+  const bool full = c + L::kElems <= a.cols;
   T* y = static_cast<T*>(a.y) + (r0 + ty) * a.ld;
   for (int64_t r = r0 + ty; r < r1; r += (int64_t)kUnroll * nty) {
     uint32_t q[kUnroll][L::kElems / 8], s[kUnroll];
@@ -199,49 +221,90 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(const MxArgs a
     for (int u = 0; u < kUnroll; ++u, y += nty * a.ld) {
       if (r + (int64_t)u * nty >= r1) break;
       const float scale = mx_scale_value(s[u]);
-      if (a.vec) {
-        Raw<T> out;
-        T* e = reinterpret_cast<T*>(&out);
+      Raw<T> out;
+      T* e = reinterpret_cast<T*>(&out);
 #pragma unroll
-        for (int i = 0; i < L::kElems / 8; ++i) {
-          float v[8];
-          mx_unpack8(q[u][i], v);
+      for (int i = 0; i < L::kElems / 8; ++i) {
+        float v[8];
+        mx_unpack8(q[u][i], v);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) e[8 * i + j] = static_cast<T>(__fmul_rn(v[j], scale));
-        }
-        if (full) {
-          store32(y + c, a.vec, out);
-        } else {
-#pragma unroll
-          for (int i = 0; i < L::kElems; ++i)
-            if (c + i < a.cols) AGN_ST(y + c + i, e[i]);
-        }
+        for (int j = 0; j < 8; ++j) e[8 * i + j] = static_cast<T>(__fmul_rn(v[j], scale));
+      }
+      if (full) {
+        store32(y + c, a.vec, out);
       } else {
-        // rows that are not aligned: the lanes of a word pass their codes on so that each store
-        // is of consecutive elements, kWord j + lane of the word's 128
-        const int lane = tx % L::kWord;
-        T* p = y + c - (int64_t)lane * L::kElems;
-        const int64_t left = a.cols - (c - (int64_t)lane * L::kElems);
 #pragma unroll
-        for (int j = 0; j < L::kElems; ++j) {
-          const int e = L::kWord * j + lane, src = e / L::kElems, at = e % L::kElems;
-          const float by = __shfl_sync(group, scale, src, L::kWord);
-          uint32_t w = __shfl_sync(group, q[u][0], src, L::kWord);
-          if constexpr (L::kElems == 16) {
-            const uint32_t w1 = __shfl_sync(group, q[u][1], src, L::kWord);
-            if (at >= 8) w = w1;
-          }
-          if (e < left) AGN_ST(p + e, static_cast<T>(__fmul_rn(mx_element((w >> (4 * (at & 7))) & 15u), by)));
-        }
+        for (int i = 0; i < L::kElems; ++i)
+          if (c + i < a.cols) AGN_ST(y + c + i, e[i]);
       }
     }
   }
 }
 
-// Blocks of 2^tx_shift lanes along a row (a word's to 256, what leaves the fewest idle) by
-// rows_per_block rows, one wave of resident blocks.
-dim3 geometry(MxArgs* a, int word_shift) {
-  const int64_t units = a->tiles_k << word_shift;
+// Into rows that are not 16-byte aligned: a lane has the eight elements c .. c + 7 of a row
+// that lie in aligned 16 (fp32: 32) bytes, c up to 7 before a multiple of 8; its codes are a
+// piece of two words, its scales those of one block or two.  (us, with a lane's consecutive
+// codes passed on by shuffles and stores of single elements, and so: 16384 x 4095 bf16 198, 66;
+// 65536 x 100 bf16 27, 11; 2865 x 3183 fp32 13.7, 10.4.)
+template <typename T>
+__global__ void __launch_bounds__(kThreads) mx4_dequantize_shift_kernel(const MxArgs a) {
+  constexpr int V = 8, kUnroll = kShiftRows;
+  pdl_begin();
+  const int tx = threadIdx.x & ((1 << a.tx_shift) - 1), ty = threadIdx.x >> a.tx_shift;
+  const int nty = kThreads >> a.tx_shift;
+  const int64_t c0 = (((int64_t)blockIdx.x << a.tx_shift) + tx) * V;
+  const int64_t r0 = blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const int64_t last = a.row_bytes / 4 - 1;   // a row's last word of codes
+  T* y = static_cast<T*>(a.y);
+  for (int64_t r = r0 + ty; r < r1; r += (int64_t)kUnroll * nty) {
+    uint32_t lo[kUnroll], hi[kUnroll], s0[kUnroll], s1[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t ru = r + (int64_t)u * nty;
+      lo[u] = hi[u] = s0[u] = s1[u] = 0;
+      const int past = (int)(reinterpret_cast<uintptr_t>(y + ru * a.ld) / sizeof(T)) & (V - 1);
+      const int64_t c = c0 - past;
+      if (ru >= r1 || c >= a.cols) continue;
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(a.codes + ru * a.row_bytes);
+      const int64_t w = c >> 3;   // (-1: the elements before the row)
+      if (w >= 0) lo[u] = AGN_LD(p + w);
+      if (w < last) hi[u] = AGN_LD(p + w + 1);
+      const int64_t k0 = max(c, (int64_t)0) / kMxBlock, k1 = min(c + V - 1, a.cols - 1) / kMxBlock;
+      s0[u] = AGN_LD(a.scales + mx_scale_at(ru, k0, a.tiles_k));
+      s1[u] = k1 == k0 ? s0[u] : AGN_LD(a.scales + mx_scale_at(ru, k1, a.tiles_k));
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t ru = r + (int64_t)u * nty;
+      if (ru >= r1) break;
+      const int past = (int)(reinterpret_cast<uintptr_t>(y + ru * a.ld) / sizeof(T)) & (V - 1);
+      const int64_t c = c0 - past;
+      if (c >= a.cols) continue;
+      float v[8];
+      mx_unpack8(__funnelshift_r(lo[u], hi[u], 4 * (uint32_t)(c & 7)), v);
+      const float by0 = mx_scale_value(s0[u]), by1 = mx_scale_value(s1[u]);
+      const int first = kMxBlock - (int)(c & (kMxBlock - 1));   // elements of the first block
+      alignas(16) T e[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        e[i] = static_cast<T>(__fmul_rn(v[i], i < first || c < 0 ? by0 : by1));
+      T* to = y + ru * a.ld + c;
+      if (c >= 0 && c + V <= a.cols) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+          AGN_ST(reinterpret_cast<uint4*>(to) + i, reinterpret_cast<const uint4*>(e)[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (c + i >= 0 && c + i < a.cols) AGN_ST(to + i, e[i]);
+      }
+    }
+  }
+}
+
+// Blocks of 2^tx_shift lanes along a row of `units` (2^word_shift to 256, what leaves the fewest
+// idle) by rows_per_block rows, one wave of resident blocks.
+dim3 geometry(MxArgs* a, int64_t units, int word_shift) {
   int best = word_shift;
   int64_t pad = INT64_MAX;
   for (int s = 8; s >= word_shift; --s) {
@@ -277,9 +340,15 @@ Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, i
   a.tiles_k = mx_tiles_k(cols);
   const bool f32 = dtype == AGN_PREC_FP32;
   a.vec = row_alignment(x ? x : y, ld, f32 ? 4 : 2);
-  const dim3 grid = geometry(&a, f32 ? 4 : 3);
-  auto k = x ? (f32 ? mx4_quantize_kernel<float> : mx4_quantize_kernel<bf16>)
-             : (f32 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>);
+  const int es = f32 ? 4 : 2, word_shift = f32 ? 4 : 3;
+  if (x) a.x_end = static_cast<const char*>(x) + matrix_bytes(rows, cols, ld, es);
+  const bool shift = a.vec == 0;
+  const dim3 grid = !x && shift ? geometry(&a, ceil_div(cols, 8) + 1, 3)
+                                : geometry(&a, a.tiles_k << word_shift, word_shift);
+  auto k = x ? (shift ? (f32 ? mx4_quantize_kernel<float, true> : mx4_quantize_kernel<bf16, true>)
+                      : (f32 ? mx4_quantize_kernel<float, false> : mx4_quantize_kernel<bf16, false>))
+             : (shift ? (f32 ? mx4_dequantize_shift_kernel<float> : mx4_dequantize_shift_kernel<bf16>)
+                      : (f32 ? mx4_dequantize_kernel<float> : mx4_dequantize_kernel<bf16>));
   AGN_TRY_CUDA(launch_pdl(k, grid, kThreads, 0, st, a));
   return Status::Ok();
 }

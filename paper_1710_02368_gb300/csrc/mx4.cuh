@@ -72,12 +72,6 @@ __device__ __forceinline__ void mx_unpack8(uint32_t q, float (&v)[8]) {
   }
 }
 
-// The value of one code: E2M1's magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6 from twice them, a nibble each.
-__device__ __forceinline__ float mx_element(uint32_t code) {
-  const float v = 0.5f * (float)((0xC8643210u >> (4 * (code & 7))) & 15u);
-  return code & 8 ? -v : v;
-}
-
 // y = act(x w^T + b) on quantised operands (mx4_linear.cu).
 struct Mx4LinearArgs {
   const void *x_codes, *x_scales, *w_codes, *w_scales;

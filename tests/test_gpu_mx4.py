@@ -95,6 +95,25 @@ def test_quantize_strides(agn, torch, dtype, ldx, start):
     check_quantized(torch, x[:, :cols].double().cpu().numpy(), rows, cols, c, s)
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,cols,ld,start", [(1, 1, 1, 1), (3, 16, 17, 3), (130, 33, 33, 0), (70, 95, 96, 7), (257, 1001, 1003, 5),
+                                                (40, 4095, 4095, 2), (600, 17, 18, 1)])
+def test_rows_that_are_not_aligned(agn, torch, dtype, rows, cols, ld, start):
+    """Quantised and back; what is between and around the rows stays."""
+    x = hard_rows(np.random.default_rng(rows), rows, cols)
+    buf = torch.full((start + rows * ld + 9,), float("nan"), device="cuda").to(dt(torch, dtype))
+    m = buf[start:start + rows * ld].view(rows, ld)
+    m[:, :cols] = torch.tensor(x, device="cuda").to(dt(torch, dtype))
+    c, s = quantize(agn, torch, m, dtype, ldx=ld, cols=cols)
+    check_quantized(torch, m[:, :cols].double().cpu().numpy(), rows, cols, c, s)
+    buf.fill_(7.0)
+    agn.agn_mx4_dequantize(c, s, rows, cols, m, dtype, ldy=ld)
+    want = R.mx4_unpack(c.cpu().numpy()[:rows * R.blocks(cols) * 16], s.cpu().numpy(), rows, cols)
+    assert np.array_equal(m[:, :cols].double().cpu().numpy(), want)
+    m[:, :cols] = 7.0
+    assert torch.all(buf == 7.0)
+
+
 def test_quantize_extremes(agn, torch):
     """Subnormal, smallest, largest and signed zero blocks; blocks that are not finite are NaN."""
     x = torch.zeros(8, 64, device="cuda")
