@@ -388,12 +388,12 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int dev, cudaStream_t
 //         stores from shared memory
 // A second accumulator would leave no TMEM columns for the scales: the next tile's
 // MMAs start once the sums are in registers.
-// What bounds it: a stage is 36 KB written to shared memory by the loads, 32 KB read by the
-// MMAs and 12 KB by the scale warps, 630 clocks at 128 bytes a clock, which long sums come to
-// (16384 x 4096 x 4096 to bf16 94 us, 5.8 PFLOP/s; 8192^3 161 us, 6.8), and 1340 clocks between
-// two tiles, 940 of them for the reads of 256 columns of TMEM.  Four stages and two tiles
-// of outputs a finishing warp: 102 us.  Short sums (10000 x 1000 x 1000 to fp32, 13 us) wait for the
-// stores of their outputs (3.8 TB/s over the kernel, 6.9 within a round).
+// What bounds it: a stage of four MMAs takes 603 clocks over long sums (513 for the MMAs alone; the
+// scale warps' reads cost nothing), the issuing thread's work between them, and 1340 clocks pass
+// between two tiles, 940 of them for the reads of 256 columns of TMEM (16384 x 4096 x 4096 to
+// bf16 94 us, 5.8 PFLOP/s; 8192^3 161 us, 6.8).  Four stages and two tiles of outputs a
+// finishing warp: 102 us.  Short sums (10000 x 1000 x 1000 to fp32, 13 us) wait for the stores of
+// their outputs (3.8 TB/s over the kernel, 6.9 within a round).
 constexpr int kPairThreads = 512;
 constexpr int kPairStages = 5;
 constexpr int kPairStaged = 4096;                          // a finishing warp's tile of outputs
@@ -741,7 +741,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       // a stage, asked for the next stage between this stage's MMAs, descriptors by addition
       // or constant, whole stages without a test (clocks a stage: 836 with two barriers
       // waited on in turn and the descriptors made anew, 646 with tests of the last stage's
-      // length, now 588; 513 for the MMAs alone).
+      // length, now 588-603; 513 for the MMAs alone; by the whole warp, one lane issuing, 650).
       const uint64_t da0 = tc::smem_desc_sw128(tc::smem_u32(smem), 16, 1024);
       constexpr uint64_t kToB = kPairHalf >> 4;
       uint64_t da = da0;
