@@ -125,9 +125,9 @@ __device__ __forceinline__ bool kept(uint64_t d, int e, uint32_t t16) {
 // multiple of 8 apart and start at the same place, so they are the same columns all the way down.
 // With column sums a tile has a unit less than its threads: the last reads the unit that
 // the next tile's first reads and stores, and each sums the columns of its own tile (so the output
-// is no input here).  Against elements one by one, us: 19620 x 287 bf16 9.9 for 27.5, with ReLU and
-// sums 29 for 73; 16384 x 4095 bf16 94 for 160 (aligned 4096: 51, two draws for this one's three);
-// 2865 x 3183 fp32 12.2 for 12.0, with sums 14.2 for 21.0.
+// is no input here).  Against elements one by one, us: 19620 x 287 bf16 8.3 for 27.5, with ReLU and
+// sums 22 for 72; 16384 x 4095 bf16 73 for 160 (aligned 4096: 51, two draws for this one's three),
+// with ReLU and sums 94 for 247 (72); 2865 x 3183 fp32 12.4 for 12.0, with sums 14.5 for 21.0.
 template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_kernel(const DropArgs a) {
   constexpr int V = 16 / sizeof(T), kUnroll = kHidden ? 2 : unroll(kTwo, kSums);
@@ -183,8 +183,14 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t ru = r + (int64_t)u * nty;
         if (ru >= r1) break;
-        if (kReadX) v[u] = load16(x + ru * a.ldx + c, full, lo, n);
-        if (kReadExtra) q[u] = load16(extra + ru * a.lde + c, full, lo, n);
+        // (kShift: a unit at a row's end is read whole where it lies in the matrix; single
+        // elements made the blocks at the ends the last by far: 16384 x 4095 bf16 with ReLU and sums 203 us, so 94)
+        auto whole = [&](int64_t ld) {
+          const int64_t at = ru * ld + c;
+          return full || (kShift && at >= 0 && at + V <= (a.rows - 1) * ld + a.cols);
+        };
+        if (kReadX) v[u] = load16(x + ru * a.ldx + c, whole(a.ldx), lo, n);
+        if (kReadExtra) q[u] = load16(extra + ru * a.lde + c, whole(a.lde), lo, n);
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -314,11 +320,12 @@ Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
     blocks = ceil_div(a.rows, a.rows_per_block);
   } else {
     // A cluster has all the rows of its tile.  The kernel is as much bound by instructions
-    // as by memory, so what counts is how many of the resident blocks have work, in one
-    // round: the width (whole 32-byte sectors but for a row of one unit; shifted rows: powers of
+    // as by memory, so what counts is how many of the resident blocks have work, over the
+    // rounds: the width (whole 32-byte sectors but for a row of one unit; shifted rows: powers of
     // two) and the cluster with the most, the widest of about equals (16384 x 4096 bf16 at four
     // blocks an SM: 64 tiles of 8 units, clusters of 8, 512 of 608 blocks, 78 us; 86 of 6 units and
-    // clusters of 7, 602 blocks but two rounds, 102 us).  Where that leaves a quarter idle,
+    // clusters of 7, 602 blocks but two rounds, 102 us; 7197 x 6736 fp32: 842 tiles of 2 units in
+    // two rounds 86, 106 of 16 and clusters of 5 66).  Where that leaves a quarter idle,
     // clusters of up to 16, if threads have kWideRows rows or more of eight blocks (us, 8 and 16:
     // 65536 x 64 bf16 28 and 16, 16384 x 32 fp32 7.5 and 5.3; 2048 x 1000 fp32, 8 rows, 6.1 and
     // 6.5; 16384 x 4096 bf16 without ReLU, 512 blocks with 8, 52.5 and 54.1).
@@ -332,7 +339,7 @@ Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
         int64_t c = std::min<int64_t>(widest, std::max<int64_t>(1, ceil_div(a.rows, nty)));
         struct Tag {};
         while (c > 1 && max_clusters<Tag>(kern, kThreads, 0, (int)c, dev) < t) --c;
-        const double used = (double)std::min(t * c, fit) * units / (double)(t * w);
+        const double used = (double)(t * c) / ceil_div(t * c, fit) * units / (double)(t * w);
         if (used > most * 1.02) {
           most = used;
           a.tile_units = w;
