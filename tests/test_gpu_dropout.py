@@ -299,3 +299,27 @@ def test_offsets_past_32_bits(agn, torch):
     assert np.array_equal(tail, want)
     del x
     torch.cuda.empty_cache()
+
+
+def test_wide_clusters_first_called_in_a_capture():
+    """A process whose first call is a captured one that needs clusters of more than eight blocks."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_1710_02368_gb300 as agn
+x, y = torch.randn(40000, 8, device="cuda"), torch.empty(40000, 8, device="cuda")
+db, again = torch.empty(8, device="cuda"), torch.empty(8, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    agn.agn_dropout_backward(x, y, 0, 40000, 8, 0.5, 1, dbias=db, stream=torch.cuda.current_stream().cuda_stream)
+g.replay(); torch.cuda.synchronize()
+z = y.clone()
+agn.agn_dropout_backward(x, y, 0, 40000, 8, 0.5, 1, dbias=again)
+assert torch.equal(db, again) and torch.equal(y, z) and float(db.abs().sum()) > 0
+print("same")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
