@@ -177,11 +177,11 @@ struct agn_handle {
   // accumulator elided: `acc` holds each worker's theta at its last pull and
   // a commit adds (theta_k - theta_pull) scaled by 1/lambda (or 1/(tau+1), 1)
   bool elide = false;
-  // Adam as the local optimizer: raw gradients go to grad, the moments m, v
-  // persist per worker, the accumulator (if kept) sums the steps
   // dropout of the hidden layers (0: none) and the scale of what it keeps
   double dropout = 0.0;
   float drop_scale = 1.f;
+  // Adam as the local optimizer: raw gradients go to grad, the moments m, v
+  // persist per worker, the accumulator (if kept) sums the steps
   bool adam = false;
   float beta1 = 0.9f, beta2 = 0.999f, eps = 1e-8f;
   float* grad = nullptr;      // [n][P_pad]
