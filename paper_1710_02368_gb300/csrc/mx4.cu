@@ -20,10 +20,15 @@ namespace {
 
 constexpr int kThreads = 256;
 // Rows of a thread whose loads are in flight together, quantising, back, and back into rows that
-// are not aligned (two, four, eight: 65536 x 100 bf16 11.0, 11.2, 14.1), and resident blocks of an
-// SM.  us, 16384 x 4096 fp32 and bf16, 10000 x 784 fp32: quantising 50, 30, 8.4
-// (rows 4 and blocks 6: 49, 30, 9.7; 2 and 6: 59, 33, 9.5), back 49, 28, 8.7 (2 and 6: 54, 32, 9.9).
-constexpr int kQuantRows = 2, kBackRows = 8, kShiftRows = 2, kBlocksPerSm = 8;
+// are not aligned, and blocks of a launch for each SM.  Quantising: as many as are resident with
+// the kernel's registers.  Back: more rows in flight are better in the largest matrices only.  us, new
+// inputs each time, 10000 x 784 fp32, 4096 x 4096 bf16, 16384 x 4096 bf16 and fp32: quantising
+// 8.0, 9.4, 29.2, 48.3 (eight blocks: 8.7, 9.7, 29.4, 49.7; three: 10.4, 10.6, 34.5, 60.3); back 7.2,
+// 7.9, 28.9, 51.9 (eight rows: 8.4, 8.9, 27.8, 49.6; four blocks: 7.2, 8.4, 31.0, 53.1).  Not
+// aligned, two, four, eight rows, 65536 x 100 bf16: 11.0, 11.2, 14.1.
+constexpr int kQuantRows = 2, kBackRows = 4, kShiftRows = 2;
+constexpr int quant_blocks(bool f32) { return f32 ? 5 : 4; }
+constexpr int kBackBlocks = 8;
 
 // Elements of a lane, its lanes of a block and of four blocks (a scale word).
 template <typename T>
@@ -304,7 +309,7 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_shift_kernel(const Mx
 
 // Blocks of 2^tx_shift lanes along a row of `units` (2^word_shift to 256, what leaves the fewest
 // idle) by rows_per_block rows, one wave of resident blocks.
-dim3 geometry(MxArgs* a, int64_t units, int word_shift) {
+dim3 geometry(MxArgs* a, int64_t units, int word_shift, int blocks_per_sm) {
   int best = word_shift;
   int64_t pad = INT64_MAX;
   for (int s = 8; s >= word_shift; --s) {
@@ -316,7 +321,7 @@ dim3 geometry(MxArgs* a, int64_t units, int word_shift) {
   }
   a->tx_shift = best;
   const int64_t tiles = ceil_div(units, (int64_t)1 << best), nty = kThreads >> best;
-  const int64_t most = std::max<int64_t>(1, (int64_t)device_sms(current_device()) * kBlocksPerSm / tiles);
+  const int64_t most = std::max<int64_t>(1, (int64_t)device_sms(current_device()) * blocks_per_sm / tiles);
   int64_t blocks = std::min<int64_t>(std::min<int64_t>(most, 65535), ceil_div(a->rows, nty));
   a->rows_per_block = ceil_div(a->rows, blocks);
   blocks = ceil_div(a->rows, a->rows_per_block);
@@ -343,8 +348,9 @@ Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, i
   const int es = f32 ? 4 : 2, word_shift = f32 ? 4 : 3;
   if (x) a.x_end = static_cast<const char*>(x) + matrix_bytes(rows, cols, ld, es);
   const bool shift = a.vec == 0;
-  const dim3 grid = !x && shift ? geometry(&a, ceil_div(cols, 8) + 1, 3)
-                                : geometry(&a, a.tiles_k << word_shift, word_shift);
+  const dim3 grid = !x && shift ? geometry(&a, ceil_div(cols, 8) + 1, 3, kBackBlocks)
+                                : geometry(&a, a.tiles_k << word_shift, word_shift,
+                                           x ? quant_blocks(f32) : kBackBlocks);
   auto k = x ? (shift ? (f32 ? mx4_quantize_kernel<float, true> : mx4_quantize_kernel<bf16, true>)
                       : (f32 ? mx4_quantize_kernel<float, false> : mx4_quantize_kernel<bf16, false>))
              : (shift ? (f32 ? mx4_dequantize_shift_kernel<float> : mx4_dequantize_shift_kernel<bf16>)
