@@ -303,10 +303,12 @@ template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool k
 Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
   constexpr int V = 16 / sizeof(T);
   auto kern = dropout_kernel<T, kBackward, kTwo, kSums, kShift, kHidden>;
-  const int dev = current_device();
+  int dev = 0, sms = 0;
+  AGN_TRY(current_device(&dev));
+  AGN_TRY(device_sms(dev, &sms));
   const int64_t units = ceil_div(a.cols, V) + (kShift && !kSums ? 1 : 0);   // (a part at each end)
   const int64_t fit =   // resident blocks
-      std::max<int64_t>(1, (int64_t)device_sms(dev) * blocks_per_sm(kTwo, kSums) / slots);
+      std::max<int64_t>(1, (int64_t)sms * blocks_per_sm(kTwo, kSums) / slots);
   int64_t tiles = 0, blocks = 0;
   if (!kSums) {
     // wide tiles, and as many blocks down the rows as are resident
@@ -338,7 +340,11 @@ Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
         if (widest == kWideCluster && a.rows < kMaxCluster * kWideRows * nty) continue;
         int64_t c = std::min<int64_t>(widest, std::max<int64_t>(1, ceil_div(a.rows, nty)));
         struct Tag {};
-        while (c > 1 && max_clusters<Tag>(kern, kThreads, 0, (int)c, dev) < t) --c;
+        for (; c > 1; --c) {
+          int resident = 0;
+          AGN_TRY(max_clusters<Tag>(kern, kThreads, 0, (int)c, dev, &resident));
+          if (resident >= t) break;
+        }
         const double used = (double)(t * c) / ceil_div(t * c, fit) * units / (double)(t * w);
         if (used > most * 1.02) {
           most = used;

@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_shift_kernel(const Mx
 
 // Blocks of 2^tx_shift lanes along a row of `units` (2^word_shift to 256, what leaves the fewest
 // idle) by rows_per_block rows, one wave of resident blocks.
-dim3 geometry(MxArgs* a, int64_t units, int word_shift, int blocks_per_sm) {
+dim3 geometry(MxArgs* a, int64_t units, int word_shift, int64_t resident) {
   int best = word_shift;
   int64_t pad = INT64_MAX;
   for (int s = 8; s >= word_shift; --s) {
@@ -321,7 +321,7 @@ dim3 geometry(MxArgs* a, int64_t units, int word_shift, int blocks_per_sm) {
   }
   a->tx_shift = best;
   const int64_t tiles = ceil_div(units, (int64_t)1 << best), nty = kThreads >> best;
-  const int64_t most = std::max<int64_t>(1, (int64_t)device_sms(current_device()) * blocks_per_sm / tiles);
+  const int64_t most = std::max<int64_t>(1, resident / tiles);
   int64_t blocks = std::min<int64_t>(std::min<int64_t>(most, 65535), ceil_div(a->rows, nty));
   a->rows_per_block = ceil_div(a->rows, blocks);
   blocks = ceil_div(a->rows, a->rows_per_block);
@@ -348,9 +348,12 @@ Status launch_mx(const void* x, void* y, void* codes, void* scales, int dtype, i
   const int es = f32 ? 4 : 2, word_shift = f32 ? 4 : 3;
   if (x) a.x_end = static_cast<const char*>(x) + matrix_bytes(rows, cols, ld, es);
   const bool shift = a.vec == 0;
-  const dim3 grid = !x && shift ? geometry(&a, ceil_div(cols, 8) + 1, 3, kBackBlocks)
-                                : geometry(&a, a.tiles_k << word_shift, word_shift,
-                                           x ? quant_blocks(f32) : kBackBlocks);
+  int dev = 0, sms = 0;
+  AGN_TRY(current_device(&dev));
+  AGN_TRY(device_sms(dev, &sms));
+  const int64_t resident = (int64_t)sms * (x ? quant_blocks(f32) : kBackBlocks);
+  const dim3 grid = !x && shift ? geometry(&a, ceil_div(cols, 8) + 1, 3, resident)
+                                : geometry(&a, a.tiles_k << word_shift, word_shift, resident);
   auto k = x ? (shift ? (f32 ? mx4_quantize_kernel<float, true> : mx4_quantize_kernel<bf16, true>)
                       : (f32 ? mx4_quantize_kernel<float, false> : mx4_quantize_kernel<bf16, false>))
              : (shift ? (f32 ? mx4_dequantize_shift_kernel<float> : mx4_dequantize_shift_kernel<bf16>)

@@ -357,7 +357,11 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int dev, cudaStream_t
   const int64_t tiles = (int64_t)grid0.x * grid0.y;
   const int kt = (a.k_steps + 3) / 4;
   a.split = std::min(8, kt);
-  while (a.split > 1 && max_clusters<Cfg>(kern, kThreads, smem, a.split, dev) < tiles) --a.split;
+  for (; a.split > 1; --a.split) {
+    int resident = 0;
+    AGN_TRY(max_clusters<Cfg>(kern, kThreads, smem, a.split, dev, &resident));
+    if (resident >= tiles) break;
+  }
   a.split = (int)ceil_div(kt, ceil_div(kt, a.split));   // no empty rank
   CUtensorMap tw, tx;
   AGN_TRY(make_tmap_u8_2d(&tw, m.w_codes, mx_row_bytes(m.in), m.out, mx_row_bytes(m.in), 128));
@@ -832,7 +836,9 @@ Status launch_pair(const Mx4LinearArgs& m, const LinearArgs& a, int dev, cudaStr
   AGN_TRY_CUDA((allow_smem<std::integral_constant<int, kOut>>(kern, kPairSmem, dev)));
   const int64_t tiles_f = ceil_div(m.out, 256), tiles = tiles_f * ceil_div(m.rows, 256);
   // the last round in halves where they fit (4-bit outputs: a warp's scales are whole words)
-  const int64_t most = device_sms(dev) / 2, rest = tiles % most;
+  int sms = 0;
+  AGN_TRY(device_sms(dev, &sms));
+  const int64_t most = std::max(1, sms / 2), rest = tiles % most;
   const int64_t halves = kOut != AGN_PREC_MX4 && 2 * rest <= most ? rest : 0;
   const int64_t units = tiles + halves, pairs = std::min(units, most);
   AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem,
@@ -862,7 +868,8 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.bulk_out = m.dtype == AGN_PREC_MX4 ? m.out
                : a.vec                 ? m.out / (16 / (int64_t)dtype_size(m.dtype)) * (16 / (int64_t)dtype_size(m.dtype))
                                        : 0;
-  const int dev = current_device();
+  int dev = 0, fours = 0;
+  AGN_TRY(current_device(&dev));
   // One tile of rows while it holds them all.  More: tiles of 64 rows while K can be split
   // over four CTAs for each, pairs of CTAs from 257 rows, or from 129 with 64 tiles of 128 x
   // 128, else tiles of 128.  us with 64, 128, pairs: 200 rows of 1000 to 1000 5.3, 6.1, 6.4; 1024
@@ -871,9 +878,9 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   if (m.rows <= 16) return launch_linear<16>(m, a, dev, st);
   if (m.rows <= 32) return launch_linear<32>(m, a, dev, st);
   const int64_t tiles_f = ceil_div(m.out, 128);
-  if (m.rows <= 64 || tiles_f * ceil_div(m.rows, 64) <=
-                          max_clusters<Tile<64>>(mx4_linear_kernel<64>, kThreads, Tile<64>::kSmem, 4, dev))
-    return launch_linear<64>(m, a, dev, st);
+  if (m.rows <= 64) return launch_linear<64>(m, a, dev, st);
+  AGN_TRY(max_clusters<Tile<64>>(mx4_linear_kernel<64>, kThreads, Tile<64>::kSmem, 4, dev, &fours));
+  if (tiles_f * ceil_div(m.rows, 64) <= fours) return launch_linear<64>(m, a, dev, st);
   if (m.rows <= 128 || (m.rows <= 256 && 2 * tiles_f < 64)) return launch_linear<128>(m, a, dev, st);
   return m.dtype == AGN_PREC_FP32   ? launch_pair<AGN_PREC_FP32>(m, a, dev, st)
          : m.dtype == AGN_PREC_BF16 ? launch_pair<AGN_PREC_BF16>(m, a, dev, st)

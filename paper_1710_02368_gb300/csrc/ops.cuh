@@ -93,69 +93,64 @@ struct KnownBuffers {
   }
 };
 
-// What is asked of a device once: by its ordinal, the current device's in these calls.
-constexpr int kMaxDevices = 64;
+// What is asked of a device is asked once and kept by its ordinal (the current device's in these
+// calls), but for an answer that is an error: the call returns it and the next one asks again.
+// (A stand-in would decide clusters, and with them the order of sums, for every later call.)
+constexpr int kMaxDevices = 64;   // ordinals from here on are asked every time
 
-inline int current_device() {
-  int dev = 0;
-  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : kMaxDevices;
+inline bool kept_device(int dev) { return dev >= 0 && dev < kMaxDevices; }
+
+inline Status current_device(int* dev) {
+  AGN_TRY_CUDA(cudaGetDevice(dev));
+  return Status::Ok();
 }
 
-inline int device_sms(int dev) {
-  static std::atomic<int> known[kMaxDevices + 1];
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (dev == kMaxDevices ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-      n = 152;
-    known[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
+inline Status device_sms(int dev, int* sms) {
+  static std::atomic<int> known[kMaxDevices];
+  if (kept_device(dev) && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return Status::Ok();
+  AGN_TRY_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  if (*sms < 1) return Status::Err(AGN_E_CUDA, "the device reports no multiprocessors");
+  if (kept_device(dev)) known[dev].store(*sms, std::memory_order_relaxed);
+  return Status::Ok();
 }
 
 // Lets a kernel have `smem` bytes of dynamic shared memory (a Tag for each kernel).
 template <typename Tag, typename... KArgs>
 cudaError_t allow_smem(void (*kern)(KArgs...), size_t smem, int dev) {
-  static std::atomic<int> done[kMaxDevices + 1];
-  if (dev < kMaxDevices && done[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+  static std::atomic<int> done[kMaxDevices];
+  if (kept_device(dev) && done[dev].load(std::memory_order_relaxed)) return cudaSuccess;
   const cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) done[dev].store(1, std::memory_order_relaxed);
+  if (e == cudaSuccess && kept_device(dev)) done[dev].store(1, std::memory_order_relaxed);
   return e;
 }
 
-// Clusters of c blocks (along y; more than the portable 8 are allowed for the kernel first)
-// of this kernel that are resident at once on the current device: fewer blocks than single ones,
-// since a cluster stays within a GPC (a block to an SM: 152 single ones, 36 clusters of four, 15 of
-// eight); 0 where they cannot be.  Asked once for each Tag and device.
+// *n: clusters of c blocks, 2 to 16 (along y; more than the portable 8 are allowed for the kernel
+// first), of this kernel that are resident at once on the current device: fewer blocks than single
+// ones, since a cluster stays within a GPC (a block to an SM: 152 single ones, 36 clusters of four,
+// 15 of eight); 0 where they cannot be.  Kept for each Tag and device.
 template <typename Tag, typename... KArgs>
-int max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c, int dev) {
-  static std::atomic<int> known[kMaxDevices + 1][17];   // + 1
-  if (c < 1 || c > 16) return 0;
-  int n = known[dev][c].load(std::memory_order_relaxed) - 1;
-  if (n < 0) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1, (unsigned)c, 1);
-    cfg.blockDim = threads;
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1;
-    attr[0].val.clusterDim.y = (unsigned)c;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if ((smem > 0 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                          (int)smem) != cudaSuccess) ||
-        (c > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
-                      cudaSuccess) ||
-        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
-      cudaGetLastError();
-      n = c > 8 ? 0 : 1;
-    }
-    known[dev][c].store(n + 1, std::memory_order_relaxed);
-  }
-  return n;
+Status max_clusters(void (*kern)(KArgs...), int threads, size_t smem, int c, int dev, int* n) {
+  static std::atomic<int> known[kMaxDevices][17];   // + 1
+  if (c < 2 || c > 16) return Status::Err(AGN_E_INVALID, "clusters have 2 to 16 blocks");
+  if (kept_device(dev) && (*n = known[dev][c].load(std::memory_order_relaxed) - 1) >= 0) return Status::Ok();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1, (unsigned)c, 1);
+  cfg.blockDim = threads;
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1;
+  attr[0].val.clusterDim.y = (unsigned)c;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (smem > 0)
+    AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  if (c > 8) AGN_TRY_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  AGN_TRY_CUDA(cudaOccupancyMaxActiveClusters(n, kern, &cfg));
+  if (kept_device(dev)) known[dev][c].store(*n + 1, std::memory_order_relaxed);
+  return Status::Ok();
 }
 
 // launch_pdl with clusters of `cluster` blocks.
