@@ -1220,6 +1220,23 @@ Status launch_tc(const CUtensorMap& a, const CUtensorMap& b, const TcArgs& args,
 
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 
+// A host thread whose first use of CUDA this is has a device but no context yet, which the driver
+// wants: it gets the device's.
+CUresult encode_tiled(CUtensorMap* map, CUtensorMapDataType type, int rank, void* base,
+                      const cuuint64_t* dims, const cuuint64_t* strides_bytes, const cuuint32_t* box,
+                      const cuuint32_t* estr, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion l2) {
+  auto call = [&] {
+    return g_encode(map, type, (cuuint32_t)rank, base, dims, strides_bytes, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, l2, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  const CUresult r = call();
+  int dev = 0;
+  if (r != CUDA_ERROR_INVALID_CONTEXT || cudaGetDevice(&dev) != cudaSuccess ||
+      cudaSetDevice(dev) != cudaSuccess)
+    return r;
+  return call();
+}
+
 Status encode(CUtensorMap* map, int rank, const void* base, const cuuint64_t* dims,
               const cuuint64_t* strides_bytes, const cuuint32_t* box,
               CUtensorMapDataType dtype = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, int esize = 2,
@@ -1244,9 +1261,8 @@ Status encode(CUtensorMap* map, int rank, const void* base, const cuuint64_t* di
   }
 #endif
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  CUresult r = g_encode(map, dtype, rank, const_cast<void*>(base), dims, strides_bytes, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = encode_tiled(map, dtype, rank, const_cast<void*>(base), dims, strides_bytes, box,
+                                  estr, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
   if (r != CUDA_SUCCESS)
     return Status::Err(AGN_E_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string(r));
   return Status::Ok();
@@ -1321,14 +1337,14 @@ Status make_tmap_store_2d(CUtensorMap* map, const void* base, int esize, uint64_
 #endif
   const cuuint64_t dims[2] = {inner, rows}, strides[1] = {stride};
   const cuuint32_t box[2] = {box_inner, box_rows}, estr[2] = {1, 1};
-  const CUresult r = g_encode(
+  const CUresult r = encode_tiled(
       map,
       esize == 4   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
       : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                    : CU_TENSOR_MAP_DATA_TYPE_UINT8,
-      2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      2, const_cast<void*>(base), dims, strides, box, estr,
       box_inner * esize == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      CU_TENSOR_MAP_L2_PROMOTION_NONE);
   if (r != CUDA_SUCCESS)
     return Status::Err(AGN_E_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string(r));
   return Status::Ok();
