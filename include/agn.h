@@ -535,9 +535,20 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
  * split-K rank withhold_rank of every split-K launch skip its arrival on the
  * tile counter, so that the ranks waiting for it give up after wait_ns
  * (-1 = none).  After a run that timed out, the handle's results are not
- * valid: destroy it.  Errors: AGN_E_INVALID.
+ * valid: destroy it.  agn_evaluate_mx4's products take both as the next call does.
+ * Errors: AGN_E_INVALID.
  */
 int agn_debug_waits(agn_handle* h, int64_t wait_ns, int32_t withhold_rank);
+
+/*
+ * The same for the calling thread's later agn_mx4_linear calls: wait_ns > 0 bounds
+ * the waits of a product's CTA for each other by that (0 = the default, 2 s; those for
+ * copies in flight after one gave up keep 2 s); withhold_rank >= 0 makes the CTAs
+ * of that rank, along K or in a pair, leave out the last load of their first tile and all
+ * after it, so that what waits for it gives up: NaN values and *err = 1 (-1 = none).
+ * Errors: AGN_E_INVALID.
+ */
+int agn_debug_linear_waits(int64_t wait_ns, int32_t withhold_rank);
 
 /*
  * Fill the inputs of the standalone commit workload on the device with the

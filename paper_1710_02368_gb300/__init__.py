@@ -26,7 +26,7 @@ __all__ = [
     "agn_last_run_stats", "agn_profile", "agn_kernel_stats", "agn_generate_inputs", "agn_export_inputs", "agn_last_error",
     "agn_destroy", "agn_make_schedule", "agn_plan_waves", "agn_commit_pull",
     "agn_commit_pull_noalloc",
-    "agn_fill_commit_inputs", "agn_debug_waits", "agn_dropout", "agn_dropout_backward",
+    "agn_fill_commit_inputs", "agn_debug_waits", "agn_debug_linear_waits", "agn_dropout", "agn_dropout_backward",
     "agn_evaluate_mx4", "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
     "library_path",
 ]
@@ -287,6 +287,12 @@ def agn_debug_waits(h, wait_ns, withhold_rank=-1):
     """Test hook: bound the device waits of later runs by wait_ns (0 = 2 s) and
     make one split-K rank withhold its arrival (-1 = none)."""
     _check(_L().agn_debug_waits(h, int(wait_ns), int(withhold_rank)), h)
+
+
+def agn_debug_linear_waits(wait_ns, withhold_rank=-1):
+    """Test hook: the bounded waits of this thread's agn_mx4_linear calls (0 = default
+    limit) and the rank that leaves a load out (-1 = none)."""
+    _check(_L().agn_debug_linear_waits(int(wait_ns), int(withhold_rank)))
 
 
 def agn_fill_commit_inputs(theta_c, acc, replicas, P, ld, n, seed, stream=None):

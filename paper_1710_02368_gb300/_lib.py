@@ -132,6 +132,7 @@ SIGNATURES = {
     "agn_mx4_linear": (C.c_int, [_PTR] * 5 + [C.c_int64] * 3 + [C.c_int32, _PTR, C.c_int32,
                                                                 C.c_int64, _PTR, _PTR, _PTR]),
     "agn_debug_waits": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32]),
+    "agn_debug_linear_waits": (C.c_int, [C.c_int64, C.c_int32]),
     "agn_fill_commit_inputs": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                          C.c_int64, C.c_int32, C.c_uint64, C.c_void_p]),
 }

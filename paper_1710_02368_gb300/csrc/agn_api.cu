@@ -1905,6 +1905,8 @@ Status eval_chunk_mx4(agn_handle* h, int64_t r0, int rows) {
     a.y_scales = last ? nullptr : h->h4[(l + 1) % 2].scales;
     a.ldy = h->dims[l];
     a.err = h->flag + 1;
+    a.wait_ns = h->dbg_wait_ns;
+    a.withhold = h->dbg_withhold;
     AGN_TRY(agn::mx4_linear(a, h->stream));
   }
   if (C <= agn::kHeadMaxClasses && K % 4 == 0)

@@ -83,6 +83,11 @@ struct Mx4LinearArgs {
   int64_t ldy;
   void* y_scales;         // AGN_PREC_MX4
   int* err;               // set to 1 when a bounded wait gives up (null: none)
+  // Test hook (agn_debug_waits, agn_debug_linear_waits): wait_ns > 0 is the limit of the waits
+  // for each other instead of 2 s; withhold = r + 1: CTA r along K, or of each pair, leaves the last
+  // stage of its first tile and all after it out (0 = none).
+  uint64_t wait_ns;
+  int withhold;
 };
 // The launches alone (the entry points check their arguments first).
 Status mx4_linear(const Mx4LinearArgs& a, cudaStream_t st);

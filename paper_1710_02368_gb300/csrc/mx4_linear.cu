@@ -16,7 +16,8 @@
 // adding the others' in rank order through distributed shared memory (no
 // workspace, no atomics, the same bits each time).
 // Every wait on an mbarrier is bounded (2 s): a tile that gives up is stored as
-// NaN and sets *err.
+// NaN and sets *err.  Whoever gives up, each stage that was armed is waited for (with a
+// limit of its own) before its memory is used again or its CTA ends.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -61,7 +62,8 @@ struct Tile {
 // Bounded waits that give up when another role of the CTA has: kTmem for barriers
 // that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
 template <bool kTmem>
-__device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                          uint64_t limit_ns) {
   uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
     uint32_t got;
@@ -77,7 +79,7 @@ __device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volati
     if ((it & 63) == 0) {
       const uint64_t now = tc::globaltimer_ns();
       if (t0 == 0) t0 = now;
-      if (*abort_flag || now - t0 > kWaitNs) return false;
+      if (*abort_flag || now - t0 > limit_ns) return false;
     }
   }
 }
@@ -99,6 +101,8 @@ struct LinearArgs {
   uint8_t* y_scales;
   int64_t y_tiles_k;
   int* err;
+  uint64_t wait_ns;         // limit of the roles' waits
+  int withhold;             // test hook: rank r = withhold - 1 leaves out a stage (0: none)
 };
 
 __device__ __forceinline__ float4 ld_cluster4(const float* p, uint32_t rank) {
@@ -221,12 +225,14 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
+  int armed = 0;   // (loading thread) stages
   if (warp == 0 && lane == 0) {
     const int64_t xt = n0 >> 7;   // 128-row scale tile of x
-    int s = 0, armed = 0;
+    int s = 0;
     uint32_t phase = 1;   // (the first round finds every stage free)
-    for (int kg = kt0; kg < kt0 + KT; ++kg) {   // stages along the whole K
-      if (!wait_mbar<false>(&empty[s], phase, abort_flag)) {
+    const int kt1 = kt0 + KT - (a.withhold == rank + 1 ? 1 : 0);
+    for (int kg = kt0; kg < kt1; ++kg) {   // stages along the whole K
+      if (!wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
         *abort_flag = 1;
         break;
       }
@@ -239,14 +245,9 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       load_scales(sf, a.w_scales + ((int64_t)blockIdx.x * a.tiles_k + 2 * kg) * kMxTileBytes, sfb,
                   &full[s]);
       load_scales(sf + kSfBytes, a.x_scales + (xt * a.tiles_k + 2 * kg) * kMxTileBytes, sfb, &full[s]);
-      armed = min(armed + 1, stages);
+      ++armed;
       if (++s == stages) s = 0, phase ^= 1;
     }
-    if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
-      for (; armed > 0; --armed) {
-        if (--s < 0) s = stages - 1, phase ^= 1;
-        tc::mbar_wait_bounded(&full[s], phase ^ 1, kWaitNs);
-      }
   } else if (warp == 1 && lane == 0) {
     // (short between the MMAs: see the pairs' kernel)
     const uint32_t sfa = tmem + Cfg::kSfCol, sfb = sfa + 8;
@@ -260,7 +261,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     uint32_t phase = 0;
     bool ready = false;
     for (int left = min(a.k_steps - 4 * kt0, 4 * KT), first = 1; left > 0; left -= 4, first = 0) {
-      if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
+      if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
         *abort_flag = 1;
         break;
       }
@@ -291,9 +292,17 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   }
   __syncwarp();
   const bool ok =
-      __syncthreads_and(wait_mbar<false>(done, 0, abort_flag) && !*abort_flag) != 0;
+      __syncthreads_and(wait_mbar<false>(done, 0, abort_flag, a.wait_ns) && !*abort_flag) != 0;
+  if (!ok) {   // every copy has landed and every MMA is done before the ring is written over
+    if (threadIdx.x == 0) {
+      for (int i = max(0, armed - stages); i < armed; ++i)
+        tc::mbar_wait_bounded(&full[i % stages], (uint32_t)(i / stages) & 1, kWaitNs);
+      tc::mbar_wait_bounded(done, 0, kWaitNs);
+      if (a.err) atomicExch(a.err, 1);
+    }
+    __syncthreads();
+  }
   tc::tc_fence_after();
-  if (!ok && threadIdx.x == 0 && a.err) atomicExch(a.err, 1);
 
   // the sums to shared memory (the ring is free): [column][128 features]
   float* sums = reinterpret_cast<float*>(smem);
@@ -563,6 +572,45 @@ struct PairUnit {
   }
 };
 
+// A role that gives up says so in both CTAs: whatever it leaves out, the other's would wait for.
+__device__ __forceinline__ void give_up(volatile int* abort_flag) {
+#pragma unroll
+  for (uint32_t r = 0; r < 2; ++r)
+    asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(
+                     tc::map_cluster(const_cast<int*>(abort_flag), r)), "r"(1)
+                 : "memory");
+}
+
+// Stages, from the launch's first, that a CTA's loading thread armed and whose scales each of its
+// scale warps brought to TMEM.
+struct PairStages {
+  int64_t loaded, scaled[4];
+};
+__device__ __forceinline__ int64_t ld_cluster64(const int64_t* p, uint32_t rank) {
+  int64_t v;
+  asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(tc::map_cluster(p, rank)) : "memory");
+  return v;
+}
+
+// After a role gave up and all have ended (one thread of each CTA, none of them left at work): wait for
+// the copies of the last stages, each CTA's scales on its own barriers and both CTAs' codes on the
+// first's, where what will not come any more (the loads of the CTA that armed fewer stages,
+// the arrivals of scale warps) is made up for: a stage's phase then ends when its copies have landed.
+__device__ __forceinline__ void land(uint64_t* full, uint64_t* scales_in, const PairStages* done, int cta) {
+  for (int64_t i = max((int64_t)0, done->loaded - kPairStages); i < done->loaded; ++i)
+    tc::mbar_wait_bounded(&scales_in[i % kPairStages], (uint32_t)(i / kPairStages) & 1, kWaitNs);
+  if (cta != 0) return;
+  const int64_t n0 = done->loaded, n1 = ld_cluster64(&done->loaded, 1), n = max(n0, n1);
+  for (int64_t i = max((int64_t)0, n - kPairStages); i < n; ++i) {
+    uint64_t* const bar = &full[i % kPairStages];
+    if (i >= n0) tc::mbar_arrive_expect_tx(bar, 2 * kPairHalf);      // (the second CTA's codes alone)
+    else if (i >= n1) tc::mbar_complete_tx(bar, 2 * kPairHalf);
+    for (uint32_t w = 0; w < 8; ++w)
+      if (i >= ld_cluster64(&done->scaled[w & 3], w >> 2)) tc::mbar_arrive(bar);
+    tc::mbar_wait_bounded(bar, (uint32_t)(i / kPairStages) & 1, kWaitNs);
+  }
+}
+
 template <int kOut>
 __global__ void __launch_bounds__(kPairThreads, 1)
 mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
@@ -582,7 +630,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
   uint64_t* sums_full = scales_in + kPairStages;
   uint64_t* sums_empty = sums_full + 1;             // (first CTA's)
   uint64_t* drained = sums_empty + 1;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drained + 1);
+  PairStages* stages_done = reinterpret_cast<PairStages*>(drained + 1);
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(stages_done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -642,11 +691,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
         __syncwarp();
       }
-      ok = ok && wait_mbar<true>(sums_full, done & 1, abort_flag) && !*abort_flag;
+      ok = ok && wait_mbar<true>(sums_full, done & 1, abort_flag, a.wait_ns) && !*abort_flag;
       ok = __all_sync(0xffffffffu, ok);
       tc::tc_fence_after();
       if (!ok && lane == 0) {
-        *abort_flag = 1;
+        give_up(abort_flag);
         if (a.err) atomicExch(a.err, 1);
       }
       uint32_t v[4][32];
@@ -678,9 +727,10 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int t = pair; t < units && ok; t += pairs) {
-      for (int kt = 0; kt < KT; ++kt) {
-        ok = __all_sync(0xffffffffu, wait_mbar<false>(&scales_in[s], phase, abort_flag));
+    int t = pair, kt = 0;
+    for (; t < units; t += pairs) {
+      for (kt = 0; kt < KT; ++kt) {
+        ok = __all_sync(0xffffffffu, wait_mbar<false>(&scales_in[s], phase, abort_flag, a.wait_ns));
         if (!ok) break;
         const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
         uint32_t x[8], w[16];
@@ -704,20 +754,26 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         if (lane == 0) tc::mbar_arrive_relaxed(full0 + 8u * (uint32_t)s);
         if (++s == kPairStages) s = 0, phase ^= 1;
       }
+      if (!ok) break;
     }
-    if (!ok && lane == 0) *abort_flag = 1;
+    if (lane == 0) {
+      stages_done->scaled[warp] = (int64_t)((t - pair) / pairs) * KT + (ok ? 0 : kt);
+      if (!ok) give_up(abort_flag);
+    }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 4 && lane == 0) {
       const uint32_t full0 = tc::map_cluster(full, 0);
-      int s = 0, n_armed = 0;
+      int s = 0;
+      int64_t loaded = 0;
+      const int64_t stop = a.withhold == cta + 1 ? KT - 1 : INT64_MAX;
       uint32_t phase = 1;   // (the first round finds every stage free)
-      for (int t = pair; t < units && !*abort_flag; t += pairs) {
+      for (int t = pair; t < units && loaded < stop && !*abort_flag; t += pairs) {
         const PairUnit unit(t, tiles_f, n_whole);
         const int f = unit.f, n = unit.n + 128 * cta, fb = f + (unit.narrow ? 64 : 128) * cta;
-        for (int kt = 0; kt < KT; ++kt) {
-          if (!wait_mbar<false>(&empty[s], phase, abort_flag)) {
-            *abort_flag = 1;
+        for (int kt = 0; kt < KT && loaded < stop; ++kt) {
+          if (!wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
+            give_up(abort_flag);
             break;
           }
           uint8_t* st = smem + s * kPairStage;
@@ -728,17 +784,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], 4 * kPairHalf);
           tc::tma_load_2d_pair(st, &tmX, bar, kt * 128, n);
           tc::tma_load_2d_pair(st + kPairHalf, &tmW, bar, kt * 128, fb);
-          n_armed = min(n_armed + 1, kPairStages);
+          ++loaded;
           if (++s == kPairStages) s = 0, phase ^= 1;
         }
       }
-      if (*abort_flag)   // wait (bounded) for the copies of the stages armed last
-        for (; n_armed > 0; --n_armed) {
-          if (--s < 0) s = kPairStages - 1, phase ^= 1;
-          // (armed in the round whose empty wait had `phase`: it completes the other one)
-          tc::mbar_wait_bounded(&scales_in[s], phase ^ 1, kWaitNs);
-          if (cta == 0) tc::mbar_wait_bounded(&full[s], phase ^ 1, kWaitNs);
-        }
+      stages_done->loaded = loaded;
     } else if (warp == 5 && lane == 0 && cta == 0) {
       // An MMA is issued in about the time that it takes, and few wait in line: what this
       // thread does between them is tensor time lost unless it is short.  So: one barrier
@@ -754,7 +804,10 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       uint32_t phase = 0;
       bool ready = false;
       for (int t = pair; t < units; t += pairs, ++done) {
-        if (done > 0 && !wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag)) *abort_flag = 1;
+        if (done > 0 && !wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag, a.wait_ns)) {
+          give_up(abort_flag);   // (the sums of the tile before may still be read)
+          break;
+        }
         // (N a constant: the instruction descriptor is then one too)
         auto mainloop = [&](auto columns) {
           constexpr uint32_t id0 = tc::idesc_mxf4(256, decltype(columns)::value, 0);
@@ -769,8 +822,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           };
           int left = a.k_steps;
           for (; left >= 4; left -= 4) {   // whole stages
-            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
-              *abort_flag = 1;
+            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+              give_up(abort_flag);
               return;
             }
             tc::tc_fence_after();
@@ -785,8 +838,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             tc::mma_commit_pair(mine);
           }
           if (left > 0) {
-            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag)) {
-              *abort_flag = 1;
+            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+              give_up(abort_flag);
               return;
             }
             tc::tc_fence_after();
@@ -799,21 +852,22 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         };
         if (t >= n_whole) mainloop(std::integral_constant<int, 128>());
         else mainloop(std::integral_constant<int, 256>());
-        if (*abort_flag) {
-          // no sums: the finishing warps of both CTAs give up (2 s); the MMAs in flight
-          // end before any memory goes
-          tc::mma_commit_pair(drained);
-          tc::mbar_wait_bounded(drained, 0, kWaitNs);
-          break;
-        }
+        if (*abort_flag) break;   // no sums: the finishing warps of both CTAs give up
         tc::mma_commit_pair(sums_full);
       }
+      tc::mma_commit_pair(drained);
     }
   }
   __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
+  // the MMA thread's last commit: no MMA is in flight, and none of its arrivals here
+  if (warp == 5 && lane == 0) tc::mbar_wait_bounded(drained, 0, kWaitNs);
   cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers
+  if (*abort_flag) {   // (the same in both CTAs: nobody is left who could set it)
+    if (threadIdx.x == 256) land(full, scales_in, stages_done, cta);
+    cluster_sync();
+  }
   if (warp == 5) tc::tmem_dealloc_pair(tmem, 512);
 }
 
@@ -863,6 +917,8 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
   a.y_scales = static_cast<uint8_t*>(m.y_scales);
   a.y_tiles_k = mx_tiles_k(m.out);
   a.err = m.err;
+  a.wait_ns = m.wait_ns ? m.wait_ns : kWaitNs;
+  a.withhold = m.withhold;
   const uint64_t rows_at = reinterpret_cast<uintptr_t>(m.y) | (uint64_t)m.ldy * dtype_size(m.dtype);
   a.vec = m.dtype != AGN_PREC_MX4 && rows_at % 16 == 0;
   a.bulk_out = m.dtype == AGN_PREC_MX4 ? m.out
@@ -888,6 +944,10 @@ Status mx4_linear(const Mx4LinearArgs& m, cudaStream_t st) {
 }
 
 namespace {
+
+// agn_debug_linear_waits: of the calling thread's calls
+thread_local uint64_t t_wait_ns = 0;
+thread_local int t_withhold = 0;
 
 Status linear_call(const Mx4LinearArgs& m, cudaStream_t st) {
   const bool mx = m.dtype == AGN_PREC_MX4;
@@ -940,6 +1000,18 @@ extern "C" int agn_mx4_linear(const void* x_codes, const void* x_scales, const v
     m.relu = relu;
     m.y = y; m.dtype = dtype; m.ldy = ldy; m.y_scales = y_scales;
     m.err = err;
+    m.wait_ns = agn::t_wait_ns;
+    m.withhold = agn::t_withhold;
     return agn::linear_call(m, static_cast<cudaStream_t>(stream));
+  });
+}
+
+extern "C" int agn_debug_linear_waits(int64_t wait_ns, int32_t withhold_rank) {
+  return agn::guarded([&] {
+    if (wait_ns < 0 || wait_ns > 2000000000ll || withhold_rank < -1 || withhold_rank > 65534)
+      return agn::Status::Err(AGN_E_INVALID, "wait_ns must be in [0, 2e9], withhold_rank >= -1");
+    agn::t_wait_ns = (uint64_t)wait_ns;
+    agn::t_withhold = withhold_rank + 1;
+    return agn::Status::Ok();
   });
 }
