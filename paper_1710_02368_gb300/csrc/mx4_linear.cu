@@ -90,10 +90,12 @@ struct LinearArgs {
   int64_t tiles_k;          // scale tiles along K
   int64_t row_tiles;        // 128-row scale tiles of x
   int k_steps;              // ceil(in / 64)
-  int split;                // CTAs of a cluster, along K
+  uint16_t split;           // CTAs of a cluster, along K
+  uint16_t withhold;        // test hook: rank r = withhold - 1 leaves out a stage (0: none)
   const float* bias;
   int relu, dtype;
   int vec;                  // rows of y start 16-byte aligned
+  uint32_t wait_ns;         // limit of the roles' waits
   int64_t bulk_out;         // features that bulk stores may write: whole 16-byte pieces of
                             // aligned rows (4-bit output: all)
   void* y;
@@ -101,9 +103,10 @@ struct LinearArgs {
   uint8_t* y_scales;
   int64_t y_tiles_k;
   int* err;
-  uint64_t wait_ns;         // limit of the roles' waits
-  int withhold;             // test hook: rank r = withhold - 1 leaves out a stage (0: none)
 };
+// (With 144 bytes the one-CTA kernel was compiled to 40 registers, not 48, and took longer: 128 rows
+// of 4096 to 4096 9.3 us for 8.3, 37 of 784 to 1000 4.7 for 4.2.)
+static_assert(sizeof(LinearArgs) == 128, "kernel arguments");
 
 __device__ __forceinline__ float4 ld_cluster4(const float* p, uint32_t rank) {
   const uint32_t own = tc::smem_u32(p);
@@ -225,10 +228,9 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  int armed = 0;   // (loading thread) stages
   if (warp == 0 && lane == 0) {
     const int64_t xt = n0 >> 7;   // 128-row scale tile of x
-    int s = 0;
+    int s = 0, armed = 0;
     uint32_t phase = 1;   // (the first round finds every stage free)
     const int kt1 = kt0 + KT - (a.withhold == rank + 1 ? 1 : 0);
     for (int kg = kt0; kg < kt1; ++kg) {   // stages along the whole K
@@ -245,8 +247,14 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       load_scales(sf, a.w_scales + ((int64_t)blockIdx.x * a.tiles_k + 2 * kg) * kMxTileBytes, sfb,
                   &full[s]);
       load_scales(sf + kSfBytes, a.x_scales + (xt * a.tiles_k + 2 * kg) * kMxTileBytes, sfb, &full[s]);
-      ++armed;
+      armed = min(armed + 1, stages);
       if (++s == stages) s = 0, phase ^= 1;
+    }
+    // Nobody passes the barrier below while copies are in flight: the stages armed last are waited for,
+    // for as long as the others' waits can last and 2 s more.
+    for (; armed > 0; --armed) {
+      if (--s < 0) s = stages - 1, phase ^= 1;
+      tc::mbar_wait_bounded(&full[s], phase ^ 1, 2 * kWaitNs);
     }
   } else if (warp == 1 && lane == 0) {
     // (short between the MMAs: see the pairs' kernel)
@@ -289,20 +297,13 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       tc::mma_commit(mine);
     }
     tc::mma_commit(done);
+    tc::mbar_wait_bounded(done, 0, kWaitNs);   // (nor while MMAs are)
   }
   __syncwarp();
   const bool ok =
       __syncthreads_and(wait_mbar<false>(done, 0, abort_flag, a.wait_ns) && !*abort_flag) != 0;
-  if (!ok) {   // every copy has landed and every MMA is done before the ring is written over
-    if (threadIdx.x == 0) {
-      for (int i = max(0, armed - stages); i < armed; ++i)
-        tc::mbar_wait_bounded(&full[i % stages], (uint32_t)(i / stages) & 1, kWaitNs);
-      tc::mbar_wait_bounded(done, 0, kWaitNs);
-      if (a.err) atomicExch(a.err, 1);
-    }
-    __syncthreads();
-  }
   tc::tc_fence_after();
+  if (!ok && threadIdx.x == 0 && a.err) atomicExch(a.err, 1);
 
   // the sums to shared memory (the ring is free): [column][128 features]
   float* sums = reinterpret_cast<float*>(smem);
@@ -582,32 +583,33 @@ __device__ __forceinline__ void give_up(volatile int* abort_flag) {
 }
 
 // Stages, from the launch's first, that a CTA's loading thread armed and whose scales each of its
-// scale warps brought to TMEM.
+// scale warps brought to TMEM (far from 2^31: operands that fill the memory make 10^8).
 struct PairStages {
-  int64_t loaded, scaled[4];
+  int loaded, scaled[4];
 };
-__device__ __forceinline__ int64_t ld_cluster64(const int64_t* p, uint32_t rank) {
-  int64_t v;
-  asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(tc::map_cluster(p, rank)) : "memory");
+__device__ __forceinline__ int ld_cluster_int(const int* p, uint32_t rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(tc::map_cluster(p, rank)) : "memory");
   return v;
 }
 
-// After a role gave up and all have ended (one thread of each CTA, none of them left at work): wait for
-// the copies of the last stages, each CTA's scales on its own barriers and both CTAs' codes on the
-// first's, where what will not come any more (the loads of the CTA that armed fewer stages,
-// the arrivals of scale warps) is made up for: a stage's phase then ends when its copies have landed.
+// After a role gave up and all have ended (one thread of each CTA): wait for the copies of the last
+// stages, each CTA's scales on its own barriers and both CTAs' codes on the first's, where what
+// will not come any more (the loads of the CTA that armed fewer stages, the arrivals of scale warps)
+// is made up for: a stage's phase then ends when its copies have landed.
 __device__ __forceinline__ void land(uint64_t* full, uint64_t* scales_in, const PairStages* done, int cta) {
-  for (int64_t i = max((int64_t)0, done->loaded - kPairStages); i < done->loaded; ++i)
-    tc::mbar_wait_bounded(&scales_in[i % kPairStages], (uint32_t)(i / kPairStages) & 1, kWaitNs);
-  if (cta != 0) return;
-  const int64_t n0 = done->loaded, n1 = ld_cluster64(&done->loaded, 1), n = max(n0, n1);
-  for (int64_t i = max((int64_t)0, n - kPairStages); i < n; ++i) {
-    uint64_t* const bar = &full[i % kPairStages];
-    if (i >= n0) tc::mbar_arrive_expect_tx(bar, 2 * kPairHalf);      // (the second CTA's codes alone)
-    else if (i >= n1) tc::mbar_complete_tx(bar, 2 * kPairHalf);
+  const int n0 = done->loaded, n1 = cta == 0 ? ld_cluster_int(&done->loaded, 1) : 0, n = max(n0, n1);
+#pragma unroll 1
+  for (int i = max(0, n - kPairStages); i < n; ++i) {
+    const uint32_t s = (uint32_t)i % kPairStages, parity = (uint32_t)i / kPairStages & 1;
+    if (i < n0) tc::mbar_wait_bounded(&scales_in[s], parity, kWaitNs);
+    if (cta != 0) continue;
+    if (i >= n0) tc::mbar_arrive_expect_tx(&full[s], 2 * kPairHalf);   // (the second CTA's codes alone)
+    else if (i >= n1) tc::mbar_complete_tx(&full[s], 2 * kPairHalf);
+#pragma unroll 1
     for (uint32_t w = 0; w < 8; ++w)
-      if (i >= ld_cluster64(&done->scaled[w & 3], w >> 2)) tc::mbar_arrive(bar);
-    tc::mbar_wait_bounded(bar, (uint32_t)(i / kPairStages) & 1, kWaitNs);
+      if (i >= ld_cluster_int(&done->scaled[w & 3], w >> 2)) tc::mbar_arrive(&full[s]);
+    tc::mbar_wait_bounded(&full[s], parity, kWaitNs);
   }
 }
 
@@ -757,7 +759,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       if (!ok) break;
     }
     if (lane == 0) {
-      stages_done->scaled[warp] = (int64_t)((t - pair) / pairs) * KT + (ok ? 0 : kt);
+      stages_done->scaled[warp] = (t - pair) / pairs * KT + (ok ? 0 : kt);
       if (!ok) give_up(abort_flag);
     }
   } else {
@@ -765,8 +767,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     if (warp == 4 && lane == 0) {
       const uint32_t full0 = tc::map_cluster(full, 0);
       int s = 0;
-      int64_t loaded = 0;
-      const int64_t stop = a.withhold == cta + 1 ? KT - 1 : INT64_MAX;
+      int loaded = 0;
+      const int stop = a.withhold == cta + 1 ? KT - 1 : INT32_MAX;
       uint32_t phase = 1;   // (the first round finds every stage free)
       for (int t = pair; t < units && loaded < stop && !*abort_flag; t += pairs) {
         const PairUnit unit(t, tiles_f, n_whole);
@@ -855,17 +857,18 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         if (*abort_flag) break;   // no sums: the finishing warps of both CTAs give up
         tc::mma_commit_pair(sums_full);
       }
-      tc::mma_commit_pair(drained);
     }
   }
   __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
-  // the MMA thread's last commit: no MMA is in flight, and none of its arrivals here
-  if (warp == 5 && lane == 0) tc::mbar_wait_bounded(drained, 0, kWaitNs);
   cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers
-  if (*abort_flag) {   // (the same in both CTAs: nobody is left who could set it)
-    if (threadIdx.x == 256) land(full, scales_in, stages_done, cta);
+  if (__builtin_expect(*abort_flag, 0)) {   // (the same in both CTAs: nobody is left who could set it)
+    if (warp == 5 && lane == 0) {
+      if (cta == 0) tc::mma_commit_pair(drained);   // (the thread that issued the MMAs)
+      tc::mbar_wait_bounded(drained, 0, kWaitNs);
+      land(full, scales_in, stages_done, cta);
+    }
     cluster_sync();
   }
   if (warp == 5) tc::tmem_dealloc_pair(tmem, 512);
