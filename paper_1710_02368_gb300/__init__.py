@@ -10,6 +10,7 @@ the library's CUDA kernels; without the built library the calls raise.
 from __future__ import annotations
 
 import ctypes as C
+from operator import index
 
 import numpy as np
 
@@ -320,7 +321,7 @@ def agn_dropout(x, y, dtype, rows, cols, p, seed, offset=0, bias=None, residual=
     element's place (include/agn.h)."""
     rc = _L().agn_dropout(_addr(x), _addr(bias), _addr(residual), _addr(y), dtype, bool(relu), rows,
                           cols, cols if ldx is None else ldx, cols if ldr is None else ldr,
-                          cols if ldy is None else ldy, p, seed & _U64, offset & _U64,
+                          cols if ldy is None else ldy, p, index(seed) & _U64, index(offset) & _U64,
                           _addr(stream))
     if rc:
         _check(rc)
@@ -333,7 +334,7 @@ def agn_dropout_backward(dy, dx, dtype, rows, cols, p, seed, offset=0, x=None, b
     rc = _L().agn_dropout_backward(_addr(dy), _addr(x), _addr(bias), _addr(dx), _addr(dbias), dtype,
                                    bool(relu), rows, cols, cols if lddy is None else lddy,
                                    cols if ldx is None else ldx, cols if lddx is None else lddx, p,
-                                   seed & _U64, offset & _U64, _addr(stream))
+                                   index(seed) & _U64, index(offset) & _U64, _addr(stream))
     if rc:
         _check(rc)
 
