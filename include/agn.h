@@ -460,8 +460,10 @@ int agn_dropout(const void* x, const float* bias, const void* residual, void* y,
  * Gradient of agn_dropout: from dy = dL/dy,
  *     dx = keep(r, c) and not (relu and x + bias <= 0) ? dy * scale : 0
  * (rounded once to dtype) with the mask of (p, seed, offset), computed anew, and
- *     dbias[c] = sum_r of dx[r][c] before its rounding, fp32, in a fixed order
- * (the same bits each time).  The residual's gradient is dy itself.
+ *     dbias[c] = sum_r of dx[r][c] before its rounding, fp32.  Equal calls give equal
+ * bits; the order of the sums depends on the sizes, on how the rows lie to 16-byte
+ * boundaries, on whether dx is an input, and on the device (its resident clusters).
+ * The residual's gradient is dy itself.
  *   x, bias   : the forward call's, read only with relu (bias NULL = none there);
  *   dx        : may be dy or x itself with the same stride;
  *   dbias     : device fp32 [cols], NULL = not wanted; with rows = 0 it is zeroed.
@@ -517,7 +519,8 @@ int agn_mx4_dequantize(const void* codes, const void* scales, int64_t rows, int6
  *   bias  : device fp32 [out], NULL = none.
  *   err   : device int32, NULL = none: set to 1 (never cleared) when a bounded wait of the kernel
  *           gave up (2 s); the values that it could not compute are NaN.
- * The order of the sums depends on the sizes alone: equal calls give equal bits.
+ * Equal calls give equal bits; the order of the sums depends on the sizes and on the
+ * device (its resident clusters).
  * Errors: AGN_E_INVALID, AGN_E_CUDA.
  */
 int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_codes,

@@ -324,10 +324,11 @@ Status launch_kernel(DropArgs a, int slots, cudaStream_t st) {
     // A cluster has all the rows of its tile.  The kernel is as much bound by instructions
     // as by memory, so what counts is how many of the resident blocks have work, over the
     // rounds: the width (whole 32-byte sectors but for a row of one unit; shifted rows: powers of
-    // two) and the cluster with the most, the widest of about equals (16384 x 4096 bf16 at four
-    // blocks an SM: 64 tiles of 8 units, clusters of 8, 512 of 608 blocks, 78 us; 86 of 6 units and
-    // clusters of 7, 602 blocks but two rounds, 102 us; 7197 x 6736 fp32: 842 tiles of 2 units in
-    // two rounds 86, 106 of 16 and clusters of 5 66).  Where that leaves a quarter idle,
+    // two) and the cluster with the most, the widest of about equals (16384 x 4096 bf16 with ReLU,
+    // three blocks an SM: 86 tiles of 6 units, clusters of 5, 430 of 456 blocks, 73 us; 64 of 8, clusters
+    // of 6, 384 blocks 79, clusters of 7, 448 blocks but two rounds (59 clusters are resident) 103;
+    // 128 of 4, clusters of 3 77; 7197 x 6736 fp32: 842 tiles of 2 units in two rounds 86, 106 of
+    // 16 and clusters of 5 66).  Where that leaves a quarter idle,
     // clusters of up to 16, if threads have kWideRows rows or more of eight blocks (us, 8 and 16:
     // 65536 x 64 bf16 28 and 16, 16384 x 32 fp32 7.5 and 5.3; 2048 x 1000 fp32, 8 rows, 6.1 and
     // 6.5; 16384 x 4096 bf16 without ReLU, 512 blocks with 8, 52.5 and 54.1).

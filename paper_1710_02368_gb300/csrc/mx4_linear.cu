@@ -400,14 +400,20 @@ Status launch_linear(const Mx4LinearArgs& m, LinearArgs a, int dev, cudaStream_t
 //   5     issues the MMAs (first CTA)
 //   8-15  finish: their 128 columns into registers at once, bias, ReLU, rounding, bulk
 //         stores from shared memory
-// A second accumulator would leave no TMEM columns for the scales: the next tile's
-// MMAs start once the sums are in registers.
-// What bounds it: a stage of four MMAs takes 603 clocks over long sums (513 for the MMAs alone; the
-// scale warps' reads cost nothing), the issuing thread's work between them, and 1340 clocks pass
-// between two tiles, 940 of them for the reads of 256 columns of TMEM (16384 x 4096 x 4096 to
-// bf16 94 us, 5.8 PFLOP/s; 8192^3 161 us, 6.8).  Four stages and two tiles of outputs a
-// finishing warp: 102 us.  Short sums (10000 x 1000 x 1000 to fp32, 13 us) wait for the stores of
-// their outputs (3.8 TB/s over the kernel, 6.9 within a round).
+// A second accumulator of 256 columns would leave no TMEM columns for the scales: the next
+// tile's MMAs start once the sums are in registers.
+// What bounds it, in clocks of a pair with most units (clock64 and globaltimer in a copy of the
+// kernel; the SMs run at 1.87 to 1.91 GHz under it, whatever the samples of 2.07 say):
+//   16384 x 4096 x 4096 to bf16, 176 thousand, 93 us (5.9 PFLOP/s): 3.5 to the first stage, 143 for 13
+//   units of 16 stages and a half one, 10.7 waiting for loads, 14.5 for the sums to leave TMEM (1100
+//   a unit, 940 of them a finishing warp's reads of its 128 columns), 2.3 to finish the last
+//   unit, 2.4 until its stores are done.  The pairs end within 6 us of each other.
+//   A stage of four MMAs takes 660 clocks there and 620 where a unit has 32 stages (8192^3, 160 us,
+//   6.9 PFLOP/s); 513 are the MMAs' own, the rest the issuing thread's work between them (the scale
+//   warps' reads cost nothing).  Four stages and two tiles of outputs a finishing warp: 102 us.
+//   10000 x 1000 x 1000 to fp32, 24 thousand, 13 us: 3.1 to the first stage; 60 pairs of two units end at 19,
+//   16 with a half one more at 23; 2.5 of each until the last stores are done.  The outputs leave at
+//   3.1 TB/s over the kernel.
 constexpr int kPairThreads = 512;
 constexpr int kPairStages = 5;
 constexpr int kPairStaged = 4096;                          // a finishing warp's tile of outputs
@@ -797,7 +803,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       // a stage, asked for the next stage between this stage's MMAs, descriptors by addition
       // or constant, whole stages without a test (clocks a stage: 836 with two barriers
       // waited on in turn and the descriptors made anew, 646 with tests of the last stage's
-      // length, now 588-603; 513 for the MMAs alone; by the whole warp, one lane issuing, 650).
+      // length, now 588-603 from stage to stage; 513 for the MMAs alone; by the whole warp, one lane issuing, 650).
       const uint64_t da0 = tc::smem_desc_sw128(tc::smem_u32(smem), 16, 1024);
       constexpr uint64_t kToB = kPairHalf >> 4;
       uint64_t da = da0;
