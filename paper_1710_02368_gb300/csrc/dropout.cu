@@ -127,7 +127,7 @@ __device__ __forceinline__ bool kept(uint64_t d, int e, uint32_t t16) {
 // the next tile's first reads and stores, and each sums the columns of its own tile (so the output
 // is no input here).  Against elements one by one, us: 19620 x 287 bf16 8.3 for 27.5, with ReLU and
 // sums 22 for 72; 16384 x 4095 bf16 73 for 160 (aligned 4096: 51, two draws for this one's three),
-// with ReLU and sums 94 for 247 (72); 2865 x 3183 fp32 12.4 for 12.0, with sums 14.5 for 21.0.
+// with ReLU and sums 97 for 247 (73); 2865 x 3183 fp32 12.4 for 12.0, with sums 14.5 for 21.0.
 template <typename T, bool kBackward, bool kTwo, bool kSums, bool kShift, bool kHidden = false>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_kernel(const DropArgs a) {
   constexpr int V = 16 / sizeof(T), kUnroll = kHidden ? 2 : unroll(kTwo, kSums);
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(kTwo, kSums)) dropout_
         const int64_t ru = r + (int64_t)u * nty;
         if (ru >= r1) break;
         // (kShift: a unit at a row's end is read whole where it lies in the matrix; single
-        // elements made the blocks at the ends the last by far: 16384 x 4095 bf16 with ReLU and sums 203 us, so 94)
+        // elements made the blocks at the ends the last by far: 16384 x 4095 bf16 with ReLU and sums 203 us, so 97)
         auto whole = [&](int64_t ld) {
           const int64_t at = ru * ld + c;
           return full || (kShift && at >= 0 && at + V <= (a.rows - 1) * ld + a.cols);
