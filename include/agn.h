@@ -529,6 +529,86 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
                    void* stream);
 
 /*
+ * AdamW over the tensors of a model (decoupled weight decay), and the norm of their
+ * gradients.  A plan names the tensors' buffers once; every step is then one launch.
+ * With t = step, for each element of a tensor, each operation rounded to fp32:
+ *     g = grad scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) (g g);  r = sqrt(v);
+ *     param = param (1 - lr weight_decay) - (lr / (1 - b1^t)) (m / (r / sqrt(1 - b2^t) + eps));
+ *     copy = bf16(param)
+ * state_bits 32: m and v are fp32 [n].  state_bits 8: m holds codes of m, v codes of
+ * r (v is then r r), a byte each, and m_scale and v_scale a byte for 32 consecutive elements
+ * of the tensor ([ceil(n / 32)]).  A scale byte E is 2^(E - 127) (0 is 0, so zeroed states are zeros);
+ * a code of m is a sign (bit 7), 4 bits of exponent x and 3 of mantissa f, of r 4 and 4 bits: the
+ * scale times (1 + f / 2^b) 2^(x - 15), with x = 0 f / 2^b 2^-14, b = 3 or 4.  The scale
+ * is the least power of two that brings the block's largest magnitude to 2 - 2^-b or below (E in 1 .. 253).
+ * Values are rounded up or down at random, in proportion (a step changes v by 1/1000
+ * of it where b2 = 0.999, less than half a code: to the nearest it would never move): up
+ * where the fraction between both codes plus (16 bits + 1/2) / 65536 reaches 1, never from r > 0 to 0.
+ * The bits are the library's splitmix64 generator's: number offset + (draws of the
+ * tensors before, ceil(n / 2) each) + floor(i / 2) (mod 2^64) of stream 9 of `seed` for element i, its low (i even)
+ * or high half, 16 bits for m below 16 for r.  A step uses sum ceil(n / 2) numbers: add that
+ * to offset after each.
+ */
+typedef struct agn_optim agn_optim;
+typedef struct agn_optim_tensor {
+  float* param;          /* device fp32 [n]; NULL in every tensor: gradients alone (norm) */
+  const void* grad;      /* device [n] of grad_dtype */
+  void* m;               /* device fp32 or codes [n] */
+  void* v;
+  uint8_t* m_scale;      /* state_bits 8 */
+  uint8_t* v_scale;
+  void* copy;            /* device bf16 [n], NULL = none */
+  int64_t n;             /* elements, 0 .. 2^40 */
+  int32_t grad_dtype;    /* AGN_PREC_FP32 or AGN_PREC_BF16 */
+  int32_t reserved;      /* 0 */
+  double weight_decay;   /* >= 0 */
+} agn_optim_tensor;
+
+/*
+ * The plan of a list of tensors on the current device.  It keeps the buffers' addresses:
+ * they stay the caller's and valid as long as the plan is used; what a step writes
+ * may overlap nothing else of the plan (AGN_E_INVALID), gradients may be the same memory.  Any alignment
+ * of their element; 32-byte boundaries (16 of bf16, 8 of codes) are fastest.  It
+ * allocates device memory and waits for the copy of the list: not in a stream capture.
+ * Errors: AGN_E_INVALID, AGN_E_OOM, AGN_E_CUDA.
+ */
+int agn_optim_create(const agn_optim_tensor* tensors, int32_t n_tensors, int32_t state_bits,
+                     agn_optim** out);
+/* Waits for the device (as cudaFree does) and frees the plan; NULL is nothing. */
+void agn_optim_destroy(agn_optim* plan);
+
+/*
+ * norm[0] = sqrt(sum of all gradients' squares) and scale[0] = the factor that clips it: max_norm /
+ * norm where norm > max_norm (> 0, infinity: none), else 1; NaN where the norm is not finite.  Device fp32,
+ * either may be NULL.  Squares are fp32 (a gradient from 1.8e19 up gives an infinite norm, one
+ * below 1e-23 counts as 0), sums fp32 of 64 at most, then 64-bit; equal calls on a device give equal bits.  The
+ * plan has one scratch array for it: order the norms of a plan on one stream, or by events.
+ * Queued on `stream`, may be captured; so is agn_optim_adamw.
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_optim_grad_norm(agn_optim* plan, double max_norm, float* norm, float* scale, void* stream);
+
+/*
+ * One step.  scale: device fp32 [1], read when the step runs (agn_optim_grad_norm's, or a loss
+ * scale's inverse), NULL = 1; where it is not finite, nothing changes.  A captured call keeps its lr,
+ * step, seed and offset.  Element by element: a NaN or infinity without scale goes into the
+ * states (8 bits: the largest codes).
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_optim_adamw(agn_optim* plan, double lr, int64_t step, double beta1, double beta2, double eps,
+                    const float* scale, uint64_t seed, uint64_t offset, void* stream);
+
+/*
+ * The values of 8-bit states: m_out [n] from m and its scales, r_out [n] (= sqrt(v)) from v and its
+ * scales, either NULL, in AGN_PREC_FP32 or AGN_PREC_BF16 (exact, but where a value lies below the dtype's
+ * normal ones).  No outputs, or n = 0: nothing to do.
+ * Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_adamw_dequantize(const uint8_t* m, const uint8_t* m_scale, const uint8_t* v,
+                         const uint8_t* v_scale, int64_t n, void* m_out, void* r_out, int32_t dtype,
+                         void* stream);
+
+/*
  * Test hook of the failure path of the bounded device waits (the paper has no
  * counterpart).  The tensor-core GEMMs' split-K exchange and the fused output
  * layer wait, on the device, for the other CTAs of their launch; every such

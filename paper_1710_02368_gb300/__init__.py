@@ -29,7 +29,8 @@ __all__ = [
     "agn_commit_pull_noalloc",
     "agn_fill_commit_inputs", "agn_debug_waits", "agn_debug_linear_waits", "agn_dropout", "agn_dropout_backward",
     "agn_evaluate_mx4", "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
-    "library_path",
+    "agn_optim_create", "agn_optim_destroy", "agn_optim_grad_norm", "agn_optim_adamw",
+    "agn_adamw_dequantize", "AGNOptim", "library_path",
 ]
 
 
@@ -370,6 +371,91 @@ def agn_mx4_linear(x_codes, x_scales, w_codes, w_scales, rows, inner, out, y, dt
                              _addr(stream))
     if rc:
         _check(rc)
+
+
+def agn_optim_create(tensors, state_bits=32):
+    """The plan (an opaque handle) of a list of dicts: n, grad, grad_dtype, and for steps param,
+    m, v, with 8-bit states m_scale and v_scale; copy and weight_decay where wanted."""
+    arr = (_lib.agn_optim_tensor * max(1, len(tensors)))()
+    for a, t in zip(arr, tensors):
+        unknown = set(t) - {f[0] for f in a._fields_}
+        if unknown:
+            raise ValueError(f"unknown keys of a tensor: {sorted(unknown)}")
+        for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy"):
+            setattr(a, k, _addr(t.get(k)))
+        a.n, a.grad_dtype = index(t["n"]), index(t.get("grad_dtype", AGN_PREC_FP32))
+        a.weight_decay = float(t.get("weight_decay", 0.0))
+    h = C.c_void_p()
+    _check(_L().agn_optim_create(arr, len(tensors), state_bits, C.byref(h)))
+    return h
+
+
+def agn_optim_destroy(plan):
+    if plan:
+        _L().agn_optim_destroy(plan)
+
+
+def agn_optim_grad_norm(plan, max_norm, norm=None, scale=None, stream=None):
+    """The norm of a plan's gradients and the factor that clips it (device fp32 [1] each)."""
+    rc = _L().agn_optim_grad_norm(plan, max_norm, _addr(norm), _addr(scale), _addr(stream))
+    if rc:
+        _check(rc)
+
+
+def agn_optim_adamw(plan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, scale=None, seed=0, offset=0,
+                    stream=None):
+    """One AdamW step of a plan (include/agn.h has the formulas and the 8-bit states)."""
+    rc = _L().agn_optim_adamw(plan, lr, step, beta1, beta2, eps, _addr(scale), index(seed) & _U64,
+                              index(offset) & _U64, _addr(stream))
+    if rc:
+        _check(rc)
+
+
+def agn_adamw_dequantize(m, m_scale, v, v_scale, n, m_out, r_out, dtype, stream=None):
+    """The values of 8-bit states: m and r = sqrt(v)."""
+    rc = _L().agn_adamw_dequantize(_addr(m), _addr(m_scale), _addr(v), _addr(v_scale), n, _addr(m_out),
+                                   _addr(r_out), dtype, _addr(stream))
+    if rc:
+        _check(rc)
+
+
+class AGNOptim:
+    """Owning wrapper of one plan of the optimizer (agn_optim_create's arguments); it keeps the tensors
+    that it was given."""
+
+    def __init__(self, tensors, state_bits=32):
+        self.h = None
+        self.tensors = [dict(t) for t in tensors]
+        self.h = agn_optim_create(self.tensors, state_bits)
+
+    @property
+    def draws(self):
+        """What a step with 8-bit states adds to the generator's offset."""
+        return sum((index(t["n"]) + 1) // 2 for t in self.tensors)
+
+    def grad_norm(self, max_norm, norm=None, scale=None, stream=None):
+        agn_optim_grad_norm(self.h, max_norm, norm, scale, stream)
+
+    def adamw(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, scale=None, seed=0, offset=0,
+              stream=None):
+        agn_optim_adamw(self.h, lr, step, beta1, beta2, eps, scale, seed, offset, stream)
+
+    def close(self):
+        if self.h:
+            agn_optim_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
 
 
 class AGN:

@@ -78,6 +78,15 @@ class agn_options(C.Structure):
     ]
 
 
+class agn_optim_tensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", C.c_int64),
+        ("grad_dtype", C.c_int32),
+        ("reserved", C.c_int32),
+        ("weight_decay", C.c_double),
+    ]
+
+
 _PTR = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _I64P = C.POINTER(C.c_int64)
@@ -131,6 +140,13 @@ SIGNATURES = {
                                      _PTR]),
     "agn_mx4_linear": (C.c_int, [_PTR] * 5 + [C.c_int64] * 3 + [C.c_int32, _PTR, C.c_int32,
                                                                 C.c_int64, _PTR, _PTR, _PTR]),
+    "agn_optim_create": (C.c_int, [C.POINTER(agn_optim_tensor), C.c_int32, C.c_int32,
+                                   C.POINTER(C.c_void_p)]),
+    "agn_optim_destroy": (None, [_PTR]),
+    "agn_optim_grad_norm": (C.c_int, [_PTR, C.c_double, _PTR, _PTR, _PTR]),
+    "agn_optim_adamw": (C.c_int, [_PTR, C.c_double, C.c_int64] + [C.c_double] * 3 +
+                        [_PTR, C.c_uint64, C.c_uint64, _PTR]),
+    "agn_adamw_dequantize": (C.c_int, [_PTR] * 4 + [C.c_int64, _PTR, _PTR, C.c_int32, _PTR]),
     "agn_debug_waits": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32]),
     "agn_debug_linear_waits": (C.c_int, [C.c_int64, C.c_int32]),
     "agn_fill_commit_inputs": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,

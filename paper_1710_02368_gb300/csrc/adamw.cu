@@ -1,0 +1,636 @@
+// AdamW over many tensors in one launch (decoupled weight decay), with 32-bit states or
+// with 8-bit ones, and the norm of all gradients with the factor that clips it (formulas and
+// the 8-bit form in include/agn.h).
+//
+// Every pass is bound by its bytes: an element with 32-bit states moves 28 (fp32 gradient) or
+// 26 bytes (bf16), with 8-bit states 16 or 14 and 1/8 for the scales, 2 more with the copy.  The
+// tensors are cut into pieces of 2048 elements, a list of which lies on the device, so that many
+// small tensors and a few large ones are the same launch; a block of 256 threads takes pieces in turn,
+// a thread eight consecutive elements: 32 bytes a load or store of fp32.  Four lanes are a
+// block of 32 elements with one scale: its largest value is two shuffles.
+// Each operation of a state is rounded to fp32 by itself (no fused multiply-add), so that
+// the codes of the 8-bit form do not depend on how a compiler contracts.
+#include <cfloat>
+#include <cmath>
+#include <memory>
+#include <vector>
+
+#include "common.cuh"
+#include "generator.cuh"
+#include "ops.cuh"
+
+namespace agn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 8;                       // elements of a thread
+constexpr int kPiece = kThreads * kPer;
+constexpr int kBlock = 32;                    // elements that share a scale
+constexpr int kMantM = 3, kMantR = 4;         // mantissa bits of the codes of m and sqrt(v)
+constexpr int kMostGrid = 4096;               // blocks of the norm's first pass
+
+// A tensor as the kernels see it.
+struct Tensor {
+  float* param;
+  const void* grad;
+  void *m, *v;
+  uint8_t *ms, *vs;
+  bf16* copy;
+  int64_t n;
+  uint64_t first;    // draws of the tensors before it
+  double decay;
+  int32_t bf16_grad;
+  int32_t wide;      // every buffer takes its widest loads and stores
+};
+struct Piece {
+  int32_t tensor, index;
+};
+
+struct StepArgs {
+  const Tensor* tensors;
+  const Piece* pieces;
+  int n_pieces;
+  float b1, ob1, b2, ob2, eps, rc2, size;   // rc2 = 1 / sqrt(1 - beta2^t), size = lr / (1 - beta1^t)
+  double lr;
+  const float* scale;
+  uint64_t key, offset;
+};
+
+__device__ __forceinline__ void load8(const float* p, int n, bool wide, float (&x)[8]) {
+  if (wide && n == 8) {
+    if (AGN_BOUNDS_OK(p, 32)) {
+      asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]),
+                     "=f"(x[7])
+                   : "l"(p));
+    } else {
+      AGN_BOUNDS_FAIL(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? AGN_LD(p + i) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, bool wide, const float (&x)[8]) {
+  if (wide && n == 8) {
+    if (AGN_BOUNDS_OK(p, 32)) {
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]),
+                   "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                   : "memory");
+    } else {
+      AGN_BOUNDS_FAIL(p);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) AGN_ST(p + i, x[i]);
+  }
+}
+__device__ __forceinline__ void load8(const bf16* p, int n, bool wide, float (&x)[8]) {
+  if (wide && n == 8) {
+    const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? __bfloat162float(AGN_LD(p + i)) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(bf16* p, int n, bool wide, const float (&x)[8]) {
+  if (wide && n == 8) {
+    const __nv_bfloat162 o[4] = {__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3]),
+                                 __floats2bfloat162_rn(x[4], x[5]), __floats2bfloat162_rn(x[6], x[7])};
+    AGN_ST(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(o));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) AGN_ST(p + i, __float2bfloat16_rn(x[i]));
+  }
+}
+__device__ __forceinline__ uint2 load8_codes(const uint8_t* p, int n, bool wide) {
+  if (wide && n == 8) return AGN_LD(reinterpret_cast<const uint2*>(p));
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) w[i >> 2] |= (uint32_t)AGN_LD(p + i) << (8 * (i & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store8_codes(uint8_t* p, int n, bool wide, const uint32_t (&c)[8]) {
+  if (wide && n == 8) {
+    AGN_ST(reinterpret_cast<uint2*>(p), make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
+                                                   c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) AGN_ST(p + i, (uint8_t)c[i]);
+  }
+}
+__device__ __forceinline__ uint32_t code_at(uint2 q, int i) {
+  return ((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 255u;
+}
+
+// The magnitude of a code: its exponent and mantissa lie where a float's do, 112 exponents lower
+// (so a code with exponent 0 is a subnormal float, its product with 2^112 exact).
+template <int kMant>
+__device__ __forceinline__ float decode(uint32_t code, float scale) {
+  return __fmul_rn(__fmul_rn(__uint_as_float(code << (23 - kMant)), 0x1p112f), scale);
+}
+__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e << 23); }
+
+// The scale of a block whose largest magnitude has the bits `top`: the power of two that brings it
+// into [1, 2 - 2^-kMant], the largest code's value.
+template <int kMant>
+__device__ __forceinline__ uint32_t scale_code(uint32_t top) {
+  return min(max((top + ((1u << (23 - kMant)) - 1)) >> 23, 1u), 253u);
+}
+// The code of x >= 0: up to the next one where the fraction left and (bits + 1/2) / 65536 reach one.
+template <int kMant>
+__device__ __forceinline__ uint32_t encode(float x, float inverse, uint32_t bits) {
+  const float u = __fmul_rn(__fmul_rn(x, inverse), 0x1p-112f);
+  constexpr int shift = 23 - kMant;
+  return min((__float_as_uint(u) + (bits << (shift - 16)) + (1u << (shift - 17))) >> shift,
+             (16u << kMant) - 1);
+}
+
+template <int kBits>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const StepArgs a) {
+  pdl_begin();
+  float s = 1.f;
+  if (a.scale) {
+    s = AGN_LD(a.scale);
+    if (!(fabsf(s) <= FLT_MAX)) return;
+  }
+  for (int c = blockIdx.x; c < a.n_pieces; c += gridDim.x) {
+    const Piece piece = AGN_LD(a.pieces + c);
+    const Tensor t = AGN_LD(a.tensors + piece.tensor);
+    const int64_t e = (int64_t)piece.index * kPiece + threadIdx.x * kPer;
+    const int n = (int)max((int64_t)0, min((int64_t)kPer, t.n - e));
+    const bool wide = t.wide;
+    float g[8], p[8], m[8], v[8];
+    uint2 qm = make_uint2(0, 0), qv = make_uint2(0, 0);
+    float sm = 0.f, sv = 0.f;
+    if (n > 0) {
+      if (t.bf16_grad) load8(static_cast<const bf16*>(t.grad) + e, n, wide, g);
+      else load8(static_cast<const float*>(t.grad) + e, n, wide, g);
+      load8(t.param + e, n, wide, p);
+      if (kBits == 8) {
+        qm = load8_codes(static_cast<const uint8_t*>(t.m) + e, n, wide);
+        qv = load8_codes(static_cast<const uint8_t*>(t.v) + e, n, wide);
+        sm = scale_value(AGN_LD(t.ms + e / kBlock));
+        sv = scale_value(AGN_LD(t.vs + e / kBlock));
+      } else {
+        load8(static_cast<const float*>(t.m) + e, n, wide, m);
+        load8(static_cast<const float*>(t.v) + e, n, wide, v);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = p[i] = m[i] = v[i] = 0.f;
+    }
+    const float keep = (float)__dsub_rn(1.0, __dmul_rn(a.lr, t.decay));
+    float r[8];
+    uint32_t top_m = 0, top_r = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float gi = a.scale ? __fmul_rn(g[i], s) : g[i];
+      if (kBits == 8) {
+        const uint32_t cm = code_at(qm, i);
+        m[i] = decode<kMantM>(cm & 127u, sm);
+        m[i] = cm & 128u ? -m[i] : m[i];
+        const float root = decode<kMantR>(code_at(qv, i), sv);
+        v[i] = __fmul_rn(root, root);
+      }
+      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(gi, a.ob1));
+      v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(gi, gi), a.ob2));
+      r[i] = __fsqrt_rn(v[i]);
+      const float q = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(r[i], a.rc2), a.eps));
+      p[i] = __fsub_rn(__fmul_rn(p[i], keep), __fmul_rn(q, a.size));
+      if (kBits == 8) {
+        if (i >= n) m[i] = r[i] = 0.f;
+        top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu);
+        top_r = max(top_r, __float_as_uint(r[i]) & 0x7fffffffu);
+      }
+    }
+    if (kBits == 8) {
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        top_m = max(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
+        top_r = max(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
+      }
+      const uint32_t em = scale_code<kMantM>(top_m), er = scale_code<kMantR>(top_r);
+      const float im = scale_value(254u - em), ir = scale_value(254u - er);
+      const uint64_t d0 = a.key + (a.offset + t.first + (uint64_t)(e / 2) + 1) * gen::kG;
+      uint32_t cm[8], cr[8];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {   // a draw for two elements: 16 bits for m, 16 for sqrt(v)
+        const uint64_t d = gen::mix(d0 + (uint64_t)h * gen::kG);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int i = 2 * h + k;
+          const uint32_t w = (uint32_t)(d >> (32 * k));
+          cm[i] = encode<kMantM>(fabsf(m[i]), im, w & 0xffffu) | (__float_as_uint(m[i]) >> 31) << 7;
+          cr[i] = encode<kMantR>(r[i], ir, w >> 16);
+          if (r[i] > 0.f) cr[i] = max(cr[i], 1u);   // m / eps would follow
+        }
+      }
+      if (n > 0) {
+        store8_codes(static_cast<uint8_t*>(t.m) + e, n, wide, cm);
+        store8_codes(static_cast<uint8_t*>(t.v) + e, n, wide, cr);
+        if ((threadIdx.x & 3) == 0) {
+          AGN_ST(t.ms + e / kBlock, (uint8_t)em);
+          AGN_ST(t.vs + e / kBlock, (uint8_t)er);
+        }
+      }
+    } else if (n > 0) {
+      store8(static_cast<float*>(t.m) + e, n, wide, m);
+      store8(static_cast<float*>(t.v) + e, n, wide, v);
+    }
+    if (n > 0) {
+      store8(t.param + e, n, wide, p);
+      if (t.copy) store8(t.copy + e, n, wide, p);
+    }
+  }
+}
+
+// Squares in fp32, a thread's sums of up to 64 of them, then doubles: per block, then over the
+// blocks in order.
+__global__ void __launch_bounds__(kThreads)
+norm_kernel(const Tensor* tensors, const Piece* pieces, int n_pieces, double* partials) {
+  pdl_begin();
+  double sum = 0.0;
+  float part = 0.f;
+  int held = 0;
+  for (int c = blockIdx.x; c < n_pieces; c += gridDim.x) {
+    const Piece piece = AGN_LD(pieces + c);
+    const Tensor* t = tensors + piece.tensor;
+    const int64_t e = (int64_t)piece.index * kPiece + threadIdx.x * kPer;
+    const int n = (int)max((int64_t)0, min((int64_t)kPer, AGN_LD(&t->n) - e));
+    if (n <= 0) continue;
+    const void* grad = AGN_LD(&t->grad);
+    const bool wide = AGN_LD(&t->wide);
+    float g[8];
+    if (AGN_LD(&t->bf16_grad)) load8(static_cast<const bf16*>(grad) + e, n, wide, g);
+    else load8(static_cast<const float*>(grad) + e, n, wide, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part = fmaf(g[i], g[i], part);
+    if (++held == 8) {
+      sum += (double)part;
+      part = 0.f;
+      held = 0;
+    }
+  }
+  sum += (double)part;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  __shared__ double warps[kThreads / 32];
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 32; ++w) sum += warps[w];
+    AGN_ST(partials + blockIdx.x, sum);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads)
+norm_finish_kernel(const double* partials, int n, double max_norm, float* norm, float* scale) {
+  pdl_begin();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < n; i += kThreads) sum += AGN_LD(partials + i);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  __shared__ double warps[kThreads / 32];
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 32; ++w) sum += warps[w];
+    const float total = (float)sqrt(sum), most = (float)max_norm;
+    if (norm) AGN_ST(norm, total);
+    if (scale)
+      AGN_ST(scale, !(total <= FLT_MAX) ? __uint_as_float(0x7fc00000u) : total > most ? __fdiv_rn(most, total) : 1.f);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+dequantize_kernel(const uint8_t* m, const uint8_t* ms, const uint8_t* v, const uint8_t* vs, int64_t n,
+                  T* m_out, T* r_out, bool wide) {
+  pdl_begin();
+  const int64_t step = (int64_t)gridDim.x * kPiece;
+  for (int64_t e = (int64_t)blockIdx.x * kPiece + threadIdx.x * kPer; e < n; e += step) {
+    const int k = (int)min((int64_t)kPer, n - e);
+    float x[8];
+    if (m_out) {
+      const uint2 q = load8_codes(m + e, k, wide);
+      const float s = scale_value(AGN_LD(ms + e / kBlock));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t c = code_at(q, i);
+        x[i] = decode<kMantM>(c & 127u, s);
+        x[i] = c & 128u ? -x[i] : x[i];
+      }
+      store8(m_out + e, k, wide, x);
+    }
+    if (r_out) {
+      const uint2 q = load8_codes(v + e, k, wide);
+      const float s = scale_value(AGN_LD(vs + e / kBlock));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = decode<kMantR>(code_at(q, i), s);
+      store8(r_out + e, k, wide, x);
+    }
+  }
+}
+
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+}  // namespace
+
+AGN_BOUNDS_UNIT(adamw)
+
+}  // namespace agn
+
+struct agn_optim {
+  int device = 0, bits = 32;
+  bool has_param = false;
+  int64_t tensors = 0;
+  int pieces = 0, norm_grid = 0;
+  agn::Tensor* d_tensors = nullptr;
+  agn::Piece* d_pieces = nullptr;
+  double* d_partials = nullptr;
+  std::vector<agn::CallBuffer> buffers;   // every buffer of the tensors (the bounds-checked build's)
+  // the bytes of all buffers and of those that a step writes: intervals apart and in order
+  std::vector<std::pair<uintptr_t, uintptr_t>> all, written;
+  ~agn_optim() {
+    cudaFree(d_tensors);
+    cudaFree(d_pieces);
+    cudaFree(d_partials);
+  }
+};
+
+namespace agn {
+namespace {
+
+// Bounds-checked build: a plan's buffers and tables are known while a call lasts.
+struct KnownPlan {
+  std::vector<const void*> p;
+  void add(const void* q, size_t bytes) {
+    if (!q || !bytes) return;
+    bounds_add(q, bytes);
+    p.push_back(q);
+  }
+  explicit KnownPlan(const agn_optim& o) {
+#ifdef AGN_BOUNDS_CHECK
+    for (const CallBuffer& b : o.buffers) add(b.p, b.bytes);
+    // (tables are not a caller's: the checker's self-test does not shorten them)
+    add(o.d_tensors, (size_t)o.tensors * sizeof(Tensor) + 256);
+    add(o.d_pieces, (size_t)o.pieces * sizeof(Piece) + 256);
+    add(o.d_partials, (size_t)o.norm_grid * sizeof(double) + 256);
+#else
+    (void)o;
+#endif
+  }
+  ~KnownPlan() {
+    for (const void* q : p) bounds_remove(q);
+  }
+};
+
+Status optim_create(const agn_optim_tensor* ts, int32_t n_tensors, int32_t bits, agn_optim** out) {
+  if (!out) return Status::Err(AGN_E_INVALID, "null pointer");
+  *out = nullptr;
+  if (bits != 32 && bits != 8) return Status::Err(AGN_E_INVALID, "state_bits must be 32 or 8");
+  if (n_tensors < 0 || (n_tensors > 0 && !ts)) return Status::Err(AGN_E_INVALID, "bad tensor list");
+  std::unique_ptr<agn_optim> o(new agn_optim);
+  o->bits = bits;
+  o->has_param = n_tensors > 0 && ts[0].param;
+  std::vector<Tensor> host;
+  std::vector<Piece> pieces;
+  struct Range {
+    uintptr_t lo, hi;
+    bool written;
+    int tensor;
+  };
+  std::vector<Range> ranges;
+  uint64_t first = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const agn_optim_tensor& t = ts[i];
+    const std::string name = "tensor " + std::to_string(i);
+    const size_t gs = dtype_size(t.grad_dtype);
+    if (!gs) return Status::Err(AGN_E_INVALID, name + ": unknown grad_dtype");
+    if (t.n < 0 || t.n > (int64_t)1 << 40) return Status::Err(AGN_E_INVALID, name + ": n must be in [0, 2^40]");
+    if (!(t.weight_decay >= 0.0 && t.weight_decay <= 1e30))
+      return Status::Err(AGN_E_INVALID, name + ": weight_decay must be finite and >= 0");
+    if ((t.param != nullptr) != o->has_param)
+      return Status::Err(AGN_E_INVALID, name + ": all tensors have a param or none has");
+    if (t.n > 0) {
+      if (!t.grad) return Status::Err(AGN_E_INVALID, name + ": null grad");
+      if (t.param && (!t.m || !t.v || (bits == 8 && (!t.m_scale || !t.v_scale))))
+        return Status::Err(AGN_E_INVALID, name + ": null state");
+    }
+    const size_t n = (size_t)t.n, nb = (n + kBlock - 1) / kBlock, ss = bits == 8 ? 1 : 4;
+    const bool p = t.param != nullptr;
+    const CallBuffer bufs[7] = {{"grad", t.grad, n * gs, gs},
+                                {"param", t.param, n * 4, 4},
+                                {"m", p ? t.m : nullptr, n * ss, ss},
+                                {"v", p ? t.v : nullptr, n * ss, ss},
+                                {"m_scale", p && bits == 8 ? t.m_scale : nullptr, nb, 1},
+                                {"v_scale", p && bits == 8 ? t.v_scale : nullptr, nb, 1},
+                                {"copy", p ? t.copy : nullptr, n * 2, 2}};
+    Tensor d{};
+    d.param = t.param; d.grad = t.grad; d.m = t.m; d.v = t.v;
+    d.ms = t.m_scale; d.vs = t.v_scale;
+    d.copy = p ? static_cast<bf16*>(t.copy) : nullptr;
+    d.n = t.n;
+    d.first = first;
+    d.decay = t.weight_decay;
+    d.bf16_grad = t.grad_dtype == AGN_PREC_BF16;
+    d.wide = aligned(t.grad, 8 * gs) && (!p || (aligned(t.param, 32) && aligned(t.m, 8 * ss) &&
+                                                aligned(t.v, 8 * ss) && aligned(t.copy, 16)));
+    for (int k = 0; k < 7; ++k) {
+      if (!bufs[k].p || !bufs[k].bytes) continue;
+      if (reinterpret_cast<uintptr_t>(bufs[k].p) % bufs[k].align != 0)
+        return Status::Err(AGN_E_INVALID, name + ": " + bufs[k].name + " is not aligned");
+      const uintptr_t lo = reinterpret_cast<uintptr_t>(bufs[k].p);
+      ranges.push_back({lo, lo + bufs[k].bytes, k > 0, i});
+      o->buffers.push_back(bufs[k]);
+    }
+    first += (uint64_t)(t.n + 1) / 2;
+    const int64_t count = ceil_div(t.n, kPiece);
+    if ((int64_t)pieces.size() + count > INT32_MAX / 2)
+      return Status::Err(AGN_E_INVALID, "too many elements for one plan");
+    for (int64_t k = 0; k < count; ++k) pieces.push_back({i, (int32_t)k});
+    host.push_back(d);
+  }
+  // What is written overlaps nothing (gradients may be the same memory).
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  uintptr_t end = 0, end_written = 0;
+  auto join = [](std::vector<std::pair<uintptr_t, uintptr_t>>& to, const Range& r) {
+    if (!to.empty() && r.lo <= to.back().second) to.back().second = std::max(to.back().second, r.hi);
+    else to.push_back({r.lo, r.hi});
+  };
+  for (const Range& r : ranges) {
+    if ((r.written && r.lo < end) || r.lo < end_written)
+      return Status::Err(AGN_E_INVALID, "tensor " + std::to_string(r.tensor) + ": a buffer overlaps another one");
+    join(o->all, r);
+    if (r.written) join(o->written, r);
+    end = std::max(end, r.hi);
+    if (r.written) end_written = std::max(end_written, r.hi);
+  }
+  AGN_TRY(current_device(&o->device));
+  for (const CallBuffer& b : o->buffers) AGN_TRY(check_buffers({b}));
+  int sms = 0;
+  AGN_TRY(device_sms(o->device, &sms));
+  o->tensors = (int64_t)host.size();
+  o->pieces = (int)pieces.size();
+  o->norm_grid = std::max(1, std::min({o->pieces, kMostGrid, 8 * sms}));
+  AGN_TRY_CUDA(cudaMalloc(&o->d_tensors, host.size() * sizeof(Tensor) + 256));
+  AGN_TRY_CUDA(cudaMalloc(&o->d_pieces, pieces.size() * sizeof(Piece) + 256));
+  AGN_TRY_CUDA(cudaMalloc(&o->d_partials, (size_t)o->norm_grid * sizeof(double) + 256));
+  if (!host.empty())
+    AGN_TRY_CUDA(cudaMemcpy(o->d_tensors, host.data(), host.size() * sizeof(Tensor), cudaMemcpyHostToDevice));
+  if (!pieces.empty())
+    AGN_TRY_CUDA(cudaMemcpy(o->d_pieces, pieces.data(), pieces.size() * sizeof(Piece), cudaMemcpyHostToDevice));
+  // (a copy from pageable memory may still be under way when it returns; later work of streams that
+  // do not wait for the default one must find it done)
+  AGN_TRY_CUDA(cudaStreamSynchronize(nullptr));
+  *out = o.release();
+  return Status::Ok();
+}
+
+// A call's own buffer shares no bytes with the plan's.
+Status check_apart(const CallBuffer& b, const std::vector<std::pair<uintptr_t, uintptr_t>>& of) {
+  if (!b.p || !b.bytes) return Status::Ok();
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(b.p);
+  const auto next = std::upper_bound(of.begin(), of.end(), std::make_pair(lo, UINTPTR_MAX));
+  if ((next != of.end() && next->first < lo + b.bytes) || (next != of.begin() && std::prev(next)->second > lo))
+    return Status::Err(AGN_E_INVALID, std::string(b.name) + " overlaps a tensor's buffer");
+  return Status::Ok();
+}
+
+Status plan_device(const agn_optim* o) {
+  if (!o) return Status::Err(AGN_E_INVALID, "null plan");
+  int dev = 0;
+  AGN_TRY(current_device(&dev));
+  if (dev != o->device) return Status::Err(AGN_E_INVALID, "the plan belongs to another device than the current one");
+  return Status::Ok();
+}
+
+Status optim_norm(agn_optim* o, double max_norm, float* norm, float* scale, cudaStream_t st) {
+  if (!(max_norm > 0.0)) return Status::Err(AGN_E_INVALID, "max_norm must be > 0");
+  if (!norm && !scale) return Status::Err(AGN_E_INVALID, "null pointer");
+  const CallBuffer nb{"norm", norm, norm ? sizeof(float) : 0, 4}, sb{"scale", scale, scale ? sizeof(float) : 0, 4};
+  AGN_TRY(check_apart(nb, {sb}));
+  AGN_TRY(plan_device(o));
+  AGN_TRY(check_apart(nb, o->all));
+  AGN_TRY(check_apart(sb, o->all));
+  AGN_TRY(check_buffers({nb, sb}));
+  KnownPlan plan(*o);
+  KnownBuffers known({nb, sb});
+  AGN_TRY(bounds_upload(st));
+  AGN_TRY_CUDA(launch_pdl(norm_kernel, dim3((unsigned)o->norm_grid), dim3(kThreads), 0, st,
+                          (const Tensor*)o->d_tensors, (const Piece*)o->d_pieces, o->pieces, o->d_partials));
+  AGN_TRY_CUDA(launch_pdl(norm_finish_kernel, dim3(1), dim3(kThreads), 0, st, (const double*)o->d_partials,
+                          o->norm_grid, max_norm, norm, scale));
+  return bounds_collect(st);
+}
+
+Status optim_step(agn_optim* o, double lr, int64_t step, double beta1, double beta2, double eps,
+                  const float* scale, uint64_t seed, uint64_t offset, cudaStream_t st) {
+  auto below_one = [](double b) { return b >= 0.0 && b < 1.0; };
+  if (!(std::fabs(lr) <= 1e30) || step < 1 || !below_one(beta1) || !below_one(beta2) || !(eps >= 0.0 && eps <= 1e30))
+    return Status::Err(AGN_E_INVALID,
+                       "need a finite lr, step >= 1, beta1 and beta2 in [0, 1), eps >= 0");
+  const CallBuffer sb{"scale", scale, scale ? sizeof(float) : 0, 4};
+  AGN_TRY(plan_device(o));
+  if (!o->has_param && o->tensors > 0) return Status::Err(AGN_E_INVALID, "the plan has gradients alone");
+  AGN_TRY(check_apart(sb, o->written));
+  AGN_TRY(check_buffers({sb}));
+  if (o->pieces == 0) return Status::Ok();
+  StepArgs a{};
+  a.tensors = o->d_tensors;
+  a.pieces = o->d_pieces;
+  a.n_pieces = o->pieces;
+  a.b1 = (float)beta1; a.ob1 = (float)(1.0 - beta1);
+  a.b2 = (float)beta2; a.ob2 = (float)(1.0 - beta2);
+  a.eps = (float)eps;
+  a.rc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  a.size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+  a.lr = lr;
+  a.scale = scale;
+  a.key = gen::key(seed, gen::kOptimState);
+  a.offset = offset;
+  int sms = 0;
+  AGN_TRY(device_sms(o->device, &sms));
+  KnownPlan plan(*o);
+  KnownBuffers known({sb});
+  AGN_TRY(bounds_upload(st));
+  const dim3 grid((unsigned)std::min(o->pieces, 8 * sms));
+  if (o->bits == 8) AGN_TRY_CUDA(launch_pdl(adamw_kernel<8>, grid, dim3(kThreads), 0, st, a));
+  else AGN_TRY_CUDA(launch_pdl(adamw_kernel<32>, grid, dim3(kThreads), 0, st, a));
+  return bounds_collect(st);
+}
+
+Status dequantize(const uint8_t* m, const uint8_t* ms, const uint8_t* v, const uint8_t* vs, int64_t n,
+                  void* m_out, void* r_out, int32_t dtype, cudaStream_t st) {
+  const size_t es = dtype_size(dtype);
+  if (!es) return Status::Err(AGN_E_INVALID, "unknown dtype");
+  if (n < 0 || n > (int64_t)1 << 48) return Status::Err(AGN_E_INVALID, "n must be in [0, 2^48]");
+  if (n == 0 || (!m_out && !r_out)) return Status::Ok();
+  if ((m_out && (!m || !ms)) || (r_out && (!v || !vs))) return Status::Err(AGN_E_INVALID, "null pointer");
+  const size_t nb = (size_t)ceil_div(n, kBlock);
+  const CallBuffer cm{"m", m_out ? m : nullptr, (size_t)n, 1}, sm{"m_scale", m_out ? ms : nullptr, nb, 1},
+      cv{"v", r_out ? v : nullptr, (size_t)n, 1}, sv{"v_scale", r_out ? vs : nullptr, nb, 1},
+      om{"m_out", m_out, m_out ? (size_t)n * es : 0, es}, orr{"r_out", r_out, r_out ? (size_t)n * es : 0, es};
+  AGN_TRY(check_apart(om, {cm, sm, cv, sv, orr}));
+  AGN_TRY(check_apart(orr, {cm, sm, cv, sv}));
+  AGN_TRY(check_buffers({cm, sm, cv, sv, om, orr}));
+  KnownBuffers known({cm, sm, cv, sv, om, orr});
+  AGN_TRY(bounds_upload(st));
+  int dev = 0, sms = 0;
+  AGN_TRY(current_device(&dev));
+  AGN_TRY(device_sms(dev, &sms));
+  const bool wide = aligned(m, 8) && aligned(v, 8) && aligned(m_out, 8 * es) && aligned(r_out, 8 * es);
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, kPiece), 16 * (int64_t)sms));
+  if (dtype == AGN_PREC_FP32)
+    AGN_TRY_CUDA(launch_pdl(dequantize_kernel<float>, grid, dim3(kThreads), 0, st, m, ms, v, vs, n,
+                            static_cast<float*>(m_out), static_cast<float*>(r_out), wide));
+  else
+    AGN_TRY_CUDA(launch_pdl(dequantize_kernel<bf16>, grid, dim3(kThreads), 0, st, m, ms, v, vs, n,
+                            static_cast<bf16*>(m_out), static_cast<bf16*>(r_out), wide));
+  return bounds_collect(st);
+}
+
+}  // namespace
+}  // namespace agn
+
+extern "C" int agn_optim_create(const agn_optim_tensor* tensors, int32_t n_tensors, int32_t state_bits,
+                                agn_optim** out) {
+  return agn::guarded([&] { return agn::optim_create(tensors, n_tensors, state_bits, out); });
+}
+
+extern "C" int agn_optim_grad_norm(agn_optim* plan, double max_norm, float* norm, float* scale, void* stream) {
+  return agn::guarded(
+      [&] { return agn::optim_norm(plan, max_norm, norm, scale, static_cast<cudaStream_t>(stream)); });
+}
+
+extern "C" int agn_optim_adamw(agn_optim* plan, double lr, int64_t step, double beta1, double beta2,
+                               double eps, const float* scale, uint64_t seed, uint64_t offset, void* stream) {
+  return agn::guarded([&] {
+    return agn::optim_step(plan, lr, step, beta1, beta2, eps, scale, seed, offset,
+                           static_cast<cudaStream_t>(stream));
+  });
+}
+
+extern "C" void agn_optim_destroy(agn_optim* plan) { delete plan; }
+
+extern "C" int agn_adamw_dequantize(const uint8_t* m, const uint8_t* m_scale, const uint8_t* v,
+                                    const uint8_t* v_scale, int64_t n, void* m_out, void* r_out,
+                                    int32_t dtype, void* stream) {
+  return agn::guarded([&] {
+    return agn::dequantize(m, m_scale, v, v_scale, n, m_out, r_out, dtype, static_cast<cudaStream_t>(stream));
+  });
+}

@@ -36,6 +36,7 @@ enum Stream : uint64_t {
   kCommitTheta = 6,
   kCommitOrder = 7,
   kDropout = 8,
+  kOptimState = 9,
 };
 
 AGN_HD uint64_t mix(uint64_t z) {

@@ -59,31 +59,6 @@ struct Tile {
   static_assert(BN * 128 * 4 <= kStages * kStageBytes, "the sums fit into the ring");
 };
 
-// Bounded waits that give up when another role of the CTA has: kTmem for barriers
-// that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
-template <bool kTmem>
-__device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
-                                          uint64_t limit_ns) {
-  uint64_t t0 = 0;
-  for (uint32_t it = 1;; ++it) {
-    uint32_t got;
-    if (kTmem)
-      asm volatile(
-          "{\n\t.reg .pred p;\n\t"
-          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-          "selp.u32 %0, 1, 0, p;\n\t}"
-          : "=r"(got) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
-    else
-      got = tc::mbar_try_wait(bar, parity);
-    if (got) return true;
-    if ((it & 63) == 0) {
-      const uint64_t now = tc::globaltimer_ns();
-      if (t0 == 0) t0 = now;
-      if (*abort_flag || now - t0 > limit_ns) return false;
-    }
-  }
-}
-
 struct LinearArgs {
   const uint8_t *w_scales, *x_scales;
   int64_t rows, out;
@@ -234,7 +209,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     uint32_t phase = 1;   // (the first round finds every stage free)
     const int kt1 = kt0 + KT - (a.withhold == rank + 1 ? 1 : 0);
     for (int kg = kt0; kg < kt1; ++kg) {   // stages along the whole K
-      if (!wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
+      if (!tc::wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
         *abort_flag = 1;
         break;
       }
@@ -269,7 +244,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     uint32_t phase = 0;
     bool ready = false;
     for (int left = min(a.k_steps - 4 * kt0, 4 * KT), first = 1; left > 0; left -= 4, first = 0) {
-      if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+      if (!ready && !tc::wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
         *abort_flag = 1;
         break;
       }
@@ -301,7 +276,7 @@ mx4_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   }
   __syncwarp();
   const bool ok =
-      __syncthreads_and(wait_mbar<false>(done, 0, abort_flag, a.wait_ns) && !*abort_flag) != 0;
+      __syncthreads_and(tc::wait_mbar<false>(done, 0, abort_flag, a.wait_ns) && !*abort_flag) != 0;
   tc::tc_fence_after();
   if (!ok && threadIdx.x == 0 && a.err) atomicExch(a.err, 1);
 
@@ -579,32 +554,17 @@ struct PairUnit {
   }
 };
 
-// A role that gives up says so in both CTAs: whatever it leaves out, the other's would wait for.
-__device__ __forceinline__ void give_up(volatile int* abort_flag) {
-#pragma unroll
-  for (uint32_t r = 0; r < 2; ++r)
-    asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(
-                     tc::map_cluster(const_cast<int*>(abort_flag), r)), "r"(1)
-                 : "memory");
-}
-
 // Stages, from the launch's first, that a CTA's loading thread armed and whose scales each of its
 // scale warps brought to TMEM (far from 2^31: operands that fill the memory make 10^8).
 struct PairStages {
   int loaded, scaled[4];
 };
-__device__ __forceinline__ int ld_cluster_int(const int* p, uint32_t rank) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(tc::map_cluster(p, rank)) : "memory");
-  return v;
-}
-
 // After a role gave up and all have ended (one thread of each CTA): wait for the copies of the last
 // stages, each CTA's scales on its own barriers and both CTAs' codes on the first's, where what
 // will not come any more (the loads of the CTA that armed fewer stages, the arrivals of scale warps)
 // is made up for: a stage's phase then ends when its copies have landed.
 __device__ __forceinline__ void land(uint64_t* full, uint64_t* scales_in, const PairStages* done, int cta) {
-  const int n0 = done->loaded, n1 = cta == 0 ? ld_cluster_int(&done->loaded, 1) : 0, n = max(n0, n1);
+  const int n0 = done->loaded, n1 = cta == 0 ? tc::ld_cluster_int(&done->loaded, 1) : 0, n = max(n0, n1);
 #pragma unroll 1
   for (int i = max(0, n - kPairStages); i < n; ++i) {
     const uint32_t s = (uint32_t)i % kPairStages, parity = (uint32_t)i / kPairStages & 1;
@@ -614,7 +574,7 @@ __device__ __forceinline__ void land(uint64_t* full, uint64_t* scales_in, const 
     else if (i >= n1) tc::mbar_complete_tx(&full[s], 2 * kPairHalf);
 #pragma unroll 1
     for (uint32_t w = 0; w < 8; ++w)
-      if (i >= ld_cluster_int(&done->scaled[w & 3], w >> 2)) tc::mbar_arrive(&full[s]);
+      if (i >= tc::ld_cluster_int(&done->scaled[w & 3], w >> 2)) tc::mbar_arrive(&full[s]);
     tc::mbar_wait_bounded(&full[s], parity, kWaitNs);
   }
 }
@@ -699,11 +659,11 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         for (int i = 0; i < 4; ++i) bias[lane + 32 * i] = b[i];
         __syncwarp();
       }
-      ok = ok && wait_mbar<true>(sums_full, done & 1, abort_flag, a.wait_ns) && !*abort_flag;
+      ok = ok && tc::wait_mbar<true>(sums_full, done & 1, abort_flag, a.wait_ns) && !*abort_flag;
       ok = __all_sync(0xffffffffu, ok);
       tc::tc_fence_after();
       if (!ok && lane == 0) {
-        give_up(abort_flag);
+        tc::give_up(abort_flag);
         if (a.err) atomicExch(a.err, 1);
       }
       uint32_t v[4][32];
@@ -738,7 +698,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     int t = pair, kt = 0;
     for (; t < units; t += pairs) {
       for (kt = 0; kt < KT; ++kt) {
-        ok = __all_sync(0xffffffffu, wait_mbar<false>(&scales_in[s], phase, abort_flag, a.wait_ns));
+        ok = __all_sync(0xffffffffu, tc::wait_mbar<false>(&scales_in[s], phase, abort_flag, a.wait_ns));
         if (!ok) break;
         const uint4* src = reinterpret_cast<const uint4*>(smem + s * kPairStage + 2 * kPairHalf) + lane;
         uint32_t x[8], w[16];
@@ -766,7 +726,7 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     }
     if (lane == 0) {
       stages_done->scaled[warp] = (t - pair) / pairs * KT + (ok ? 0 : kt);
-      if (!ok) give_up(abort_flag);
+      if (!ok) tc::give_up(abort_flag);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
@@ -780,8 +740,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
         const PairUnit unit(t, tiles_f, n_whole);
         const int f = unit.f, n = unit.n + 128 * cta, fb = f + (unit.narrow ? 64 : 128) * cta;
         for (int kt = 0; kt < KT && loaded < stop; ++kt) {
-          if (!wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
-            give_up(abort_flag);
+          if (!tc::wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
+            tc::give_up(abort_flag);
             break;
           }
           uint8_t* st = smem + s * kPairStage;
@@ -812,8 +772,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
       uint32_t phase = 0;
       bool ready = false;
       for (int t = pair; t < units; t += pairs, ++done) {
-        if (done > 0 && !wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag, a.wait_ns)) {
-          give_up(abort_flag);   // (the sums of the tile before may still be read)
+        if (done > 0 && !tc::wait_mbar<true>(sums_empty, (done - 1) & 1, abort_flag, a.wait_ns)) {
+          tc::give_up(abort_flag);   // (the sums of the tile before may still be read)
           break;
         }
         // (N a constant: the instruction descriptor is then one too)
@@ -830,8 +790,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
           };
           int left = a.k_steps;
           for (; left >= 4; left -= 4) {   // whole stages
-            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
-              give_up(abort_flag);
+            if (!ready && !tc::wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+              tc::give_up(abort_flag);
               return;
             }
             tc::tc_fence_after();
@@ -846,8 +806,8 @@ mx4_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             tc::mma_commit_pair(mine);
           }
           if (left > 0) {
-            if (!ready && !wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
-              give_up(abort_flag);
+            if (!ready && !tc::wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+              tc::give_up(abort_flag);
               return;
             }
             tc::tc_fence_after();

@@ -126,12 +126,24 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* src, 
       "r"(smem_u32(src)), "r"(x), "r"(y)
       : "memory");
 }
+// The same, adding to what is there (f32), at the L2.
+__device__ __forceinline__ void tma_add_2d(const void* tmap, const void* src, int x, int y) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(tmap)),
+      "r"(smem_u32(src)), "r"(x), "r"(y)
+      : "memory");
+}
 __device__ __forceinline__ void bulk_commit() {
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 // Every bulk group of this thread has read its source / is complete.
 __device__ __forceinline__ void bulk_wait_read() {
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+// All but the last bulk group of this thread have read their sources.
+__device__ __forceinline__ void bulk_wait_read_1() {
+  asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
 }
 __device__ __forceinline__ void bulk_wait() {
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -324,12 +336,71 @@ __device__ __forceinline__ void tma_load_2d_pair(void* dst, const void* tmap, ui
       "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y)
       : "memory");
 }
+__device__ __forceinline__ void tma_load_3d_pair(void* dst, const void* tmap, uint32_t bar, int x,
+                                                 int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+// mma_bf16 by a pair of CTAs: M = 256, the first CTA's 128 rows and the second's; each
+// holds half of B's columns.
+__device__ __forceinline__ void mma_bf16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                              uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // Arrive on a barrier of the cluster (its shared::cluster address).  Relaxed: it
 // orders TMEM accesses alone, with tcgen05.fence::before_thread_sync before it and
 // ::after_thread_sync after the wait (a release at cluster scope costs about 1000 clocks).
 __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
                : "memory");
+}
+
+// Bounded waits that give up when another role of the CTA has: kTmem for barriers
+// that order TMEM accesses alone (relaxed, with a tcgen05 fence after it).
+template <bool kTmem>
+__device__ __forceinline__ bool wait_mbar(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                          uint64_t limit_ns) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    uint32_t got;
+    if (kTmem)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(got) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    else
+      got = mbar_try_wait(bar, parity);
+    if (got) return true;
+    if ((it & 63) == 0) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (*abort_flag || now - t0 > limit_ns) return false;
+    }
+  }
+}
+
+// A role that gives up says so in both CTAs: whatever it leaves out, the other's would wait for.
+__device__ __forceinline__ void give_up(volatile int* abort_flag) {
+#pragma unroll
+  for (uint32_t r = 0; r < 2; ++r)
+    asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(
+                     map_cluster(const_cast<int*>(abort_flag), r)), "r"(1)
+                 : "memory");
+}
+
+__device__ __forceinline__ int ld_cluster_int(const int* p, uint32_t rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(map_cluster(p, rank)) : "memory");
+  return v;
 }
 
 // Arrive on `bar` once every tcgen05.mma issued so far by this thread completes.
