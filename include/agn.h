@@ -529,6 +529,50 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
                    void* stream);
 
 /*
+ * The output layer and its softmax cross-entropy over many classes in one call, the logits kept
+ * nowhere (the head of agn_run's nets has up to a few classes; the paper has no counterpart):
+ *     z[r][c] = sum_k x[r][k] w[c][k] + bias[c];  lse[r] = log sum_c exp z[r][c];
+ *     loss[r] = lse[r] - z[r][labels[r]]
+ * A row whose label is not in 0 .. classes - 1 is left out: loss = lse = 0, and its x may
+ * hold anything.  A class with a bias of minus infinity takes no part; where no class does,
+ * lse is minus infinity and loss infinity.  A logit that is NaN or plus infinity makes them NaN.
+ *   x       : device [rows][inner], w: device [classes][inner], both of dtype (AGN_PREC_FP32, whose products
+ *             are those of three exact bf16 pieces, or AGN_PREC_BF16; sums fp32), rows one after the other,
+ *             16-byte aligned;
+ *   bias    : device fp32 [classes], NULL = none;  labels: device int32 [rows];
+ *   loss, lse: device fp32 [rows];
+ *   work    : device scratch, 256-byte aligned, of at least agn_linear_ce_bytes(...) bytes (backward 0); it
+ *             holds nothing between calls, and calls that may run at the same time need one each;
+ *   err     : device int32, NULL = none: set to 1 (never cleared) when a bounded wait gave up (2 s); values that
+ *             could not be computed are NaN.
+ * rows 0 .. 2^28, inner 1 .. 2^20, classes 1 .. 2^28.  bf16 rows of a multiple of 8 elements are read as
+ * they are, others are copied first.  Equal calls give equal bits.  Queued on `stream`, may be captured.
+ * agn_linear_ce_bytes needs no GPU.  Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_linear_ce_bytes(int64_t rows, int64_t inner, int64_t classes, int32_t dtype, int32_t backward,
+                        int64_t* bytes);
+int agn_linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int32_t dtype,
+                  int64_t rows, int64_t inner, int64_t classes, float* loss, float* lse, void* work,
+                  int64_t work_bytes, int32_t* err, void* stream);
+
+/*
+ * Its gradients, from lse alone: with a = scale (dloss + dlse), b = scale dloss of the row,
+ *     p[r][c] = a exp(z[r][c] - lse[r]) - b [c = labels[r]];
+ *     dx = p w (dtype), dw = p^T x (dtype), dbias[c] = sum_r p[r][c] (fp32)
+ * p is computed anew for a piece of the classes at a time; for dx and dw it is rounded to bf16 (AGN_PREC_FP32: three
+ * pieces).  Rows left out have dx = 0 and no part in the sums, nor have rows whose lse is minus infinity.
+ *   lse     : agn_linear_ce's;  dloss, dlse: device fp32 [rows], the gradients of loss (NULL: 1)
+ *             and lse (NULL: 0);  scale: a factor of both (1 / rows: of the mean loss);
+ *   dx, dw  : 16-byte aligned, dx like x, dw like w, dbias [classes]; NULL = not wanted;
+ *   work    : as above, agn_linear_ce_bytes(..., backward 1).
+ * rows 0: dw and dbias are zeroed.  Errors: AGN_E_INVALID, AGN_E_CUDA.
+ */
+int agn_linear_ce_backward(const void* x, const void* w, const float* bias, const int32_t* labels,
+                           const float* lse, const float* dloss, const float* dlse, double scale, int32_t dtype,
+                           int64_t rows, int64_t inner, int64_t classes, void* dx, void* dw, float* dbias, void* work,
+                           int64_t work_bytes, int32_t* err, void* stream);
+
+/*
  * AdamW over the tensors of a model (decoupled weight decay), and the norm of their
  * gradients.  A plan names the tensors' buffers once; every step is then one launch.
  * With t = step, for each element of a tensor, each operation rounded to fp32:
@@ -632,6 +676,10 @@ int agn_debug_waits(agn_handle* h, int64_t wait_ns, int32_t withhold_rank);
  * Errors: AGN_E_INVALID.
  */
 int agn_debug_linear_waits(int64_t wait_ns, int32_t withhold_rank);
+
+/* The same for the products of the calling thread's later agn_linear_ce and agn_linear_ce_backward calls
+ * (withhold_rank 0 or 1: that CTA of each pair, 0 also where a CTA works alone). */
+int agn_debug_linear_ce_waits(int64_t wait_ns, int32_t withhold_rank);
 
 /*
  * Fill the inputs of the standalone commit workload on the device with the

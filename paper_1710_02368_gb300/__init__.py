@@ -29,6 +29,7 @@ __all__ = [
     "agn_commit_pull_noalloc",
     "agn_fill_commit_inputs", "agn_debug_waits", "agn_debug_linear_waits", "agn_dropout", "agn_dropout_backward",
     "agn_evaluate_mx4", "agn_mx4_bytes", "agn_mx4_quantize", "agn_mx4_dequantize", "agn_mx4_linear",
+    "agn_linear_ce_bytes", "agn_linear_ce", "agn_linear_ce_backward", "agn_debug_linear_ce_waits",
     "agn_optim_create", "agn_optim_destroy", "agn_optim_grad_norm", "agn_optim_adamw",
     "agn_adamw_dequantize", "AGNOptim", "library_path",
 ]
@@ -371,6 +372,40 @@ def agn_mx4_linear(x_codes, x_scales, w_codes, w_scales, rows, inner, out, y, dt
                              _addr(stream))
     if rc:
         _check(rc)
+
+
+def agn_linear_ce_bytes(rows, inner, classes, dtype, backward=0):
+    """Bytes of scratch of agn_linear_ce (backward: of agn_linear_ce_backward)."""
+    n = C.c_int64()
+    _check(_L().agn_linear_ce_bytes(rows, inner, classes, dtype, bool(backward), C.byref(n)))
+    return n.value
+
+
+def agn_linear_ce(x, w, labels, dtype, rows, inner, classes, loss, lse, work, work_bytes, bias=None,
+                  err=None, stream=None):
+    """Softmax cross-entropy of x [rows][inner] w [classes][inner]^T + bias on device buffers: loss and
+    lse [rows]."""
+    rc = _L().agn_linear_ce(_addr(x), _addr(w), _addr(bias), _addr(labels), dtype, rows, inner, classes,
+                            _addr(loss), _addr(lse), _addr(work), work_bytes, _addr(err), _addr(stream))
+    if rc:
+        _check(rc)
+
+
+def agn_linear_ce_backward(x, w, labels, lse, dtype, rows, inner, classes, work, work_bytes, dx=None,
+                           dw=None, dbias=None, bias=None, dloss=None, dlse=None, scale=1.0, err=None,
+                           stream=None):
+    """Gradients of agn_linear_ce: dx, dw, dbias, those that are given."""
+    rc = _L().agn_linear_ce_backward(_addr(x), _addr(w), _addr(bias), _addr(labels), _addr(lse),
+                                     _addr(dloss), _addr(dlse), scale, dtype, rows, inner, classes,
+                                     _addr(dx), _addr(dw), _addr(dbias), _addr(work), work_bytes,
+                                     _addr(err), _addr(stream))
+    if rc:
+        _check(rc)
+
+
+def agn_debug_linear_ce_waits(wait_ns, withhold_rank=-1):
+    """Test hook: agn_debug_linear_waits for this thread's agn_linear_ce calls."""
+    _check(_L().agn_debug_linear_ce_waits(int(wait_ns), int(withhold_rank)))
 
 
 def agn_optim_create(tensors, state_bits=32):

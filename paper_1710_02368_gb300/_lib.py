@@ -140,6 +140,12 @@ SIGNATURES = {
                                      _PTR]),
     "agn_mx4_linear": (C.c_int, [_PTR] * 5 + [C.c_int64] * 3 + [C.c_int32, _PTR, C.c_int32,
                                                                 C.c_int64, _PTR, _PTR, _PTR]),
+    "agn_linear_ce_bytes": (C.c_int, [C.c_int64] * 3 + [C.c_int32] * 2 + [_I64P]),
+    "agn_linear_ce": (C.c_int, [_PTR] * 4 + [C.c_int32] + [C.c_int64] * 3 + [_PTR] * 3 +
+                      [C.c_int64, _PTR, _PTR]),
+    "agn_linear_ce_backward": (C.c_int, [_PTR] * 7 + [C.c_double, C.c_int32] + [C.c_int64] * 3 +
+                               [_PTR] * 4 + [C.c_int64, _PTR, _PTR]),
+    "agn_debug_linear_ce_waits": (C.c_int, [C.c_int64, C.c_int32]),
     "agn_optim_create": (C.c_int, [C.POINTER(agn_optim_tensor), C.c_int32, C.c_int32,
                                    C.POINTER(C.c_void_p)]),
     "agn_optim_destroy": (None, [_PTR]),

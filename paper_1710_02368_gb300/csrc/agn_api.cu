@@ -85,6 +85,8 @@ AGN_BOUNDS_DECL(dropout)
 AGN_BOUNDS_DECL(mx4)
 AGN_BOUNDS_DECL(mx4_linear)
 AGN_BOUNDS_DECL(adamw)
+AGN_BOUNDS_DECL(linear_ce)
+AGN_BOUNDS_DECL(linear_ce_gemm)
 #undef AGN_BOUNDS_DECL
 
 namespace {
@@ -139,7 +141,8 @@ Status bounds_upload(cudaStream_t st) {
   using SetFn = cudaError_t (*)(const BoundsTable&, cudaStream_t);
   for (SetFn f : {bounds_set_commit, bounds_set_eval, bounds_set_head, bounds_set_simt,
                   bounds_set_tc, bounds_set_dw, bounds_set_optim, bounds_set_dropout,
-                  bounds_set_mx4, bounds_set_mx4_linear, bounds_set_adamw})
+                  bounds_set_mx4, bounds_set_mx4_linear, bounds_set_adamw, bounds_set_linear_ce,
+                  bounds_set_linear_ce_gemm})
     AGN_TRY_CUDA(f(t, st));
   return Status::Ok();
 }
@@ -150,7 +153,8 @@ Status bounds_collect(cudaStream_t st) {
   unsigned long long total = 0;
   for (GetFn f : {bounds_get_commit, bounds_get_eval, bounds_get_head, bounds_get_simt,
                   bounds_get_tc, bounds_get_dw, bounds_get_optim, bounds_get_dropout,
-                  bounds_get_mx4, bounds_get_mx4_linear, bounds_get_adamw}) {
+                  bounds_get_mx4, bounds_get_mx4_linear, bounds_get_adamw, bounds_get_linear_ce,
+                  bounds_get_linear_ce_gemm}) {
     unsigned long long a = 0;
     unsigned int c = 0;
     AGN_TRY_CUDA(f(&a, &c, st));

@@ -1,0 +1,830 @@
+// Softmax cross-entropy of a linear layer over many classes, and its gradients, without
+// the logits in memory (formulas in include/agn.h).
+//
+// Forward: one product x w^T whose epilogue keeps (maximum, sum of exponentials) of each row and
+// half a tile of columns, 16 bytes for 256 logits; a small kernel joins them.  Backward, from the rows'
+// lse alone: the product again, its epilogue turns logits into p, the gradient with respect
+// to them (bf16, fp32 as three bf16 pieces), for a piece of the classes at a time; then dw = p^T x
+// and dx += p w of the piece.  Pieces keep p's buffer at 128 MB.
+// Rows without a label cost nothing and may hold anything: the rows with one are counted and, where
+// some are missing, gathered on the device; all sizes that depend on it are read there.
+// Small problems (few rows, w in a few 10 KB) take two plain kernels instead: a warp a row.
+#include "linear_ce.cuh"
+
+#include <cfloat>
+#include <cmath>
+
+#include "mlp_tc.cuh"
+#include "ops.cuh"
+
+namespace agn {
+namespace ce {
+
+namespace {
+
+constexpr int kSms = 152;                       // what splits along K are made for
+constexpr int64_t kPieceBytes = 128ll << 20;    // of p
+constexpr int64_t kPackBytes = 96ll << 20;      // of w's pieces (they stay in the L2)
+constexpr int64_t kPartBytes = 64ll << 20;      // of a product's sums by ranges along K
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Sizes {
+  int64_t rows, inner, classes;
+  int prec;
+};
+
+// How a product is cut.
+struct Cut {
+  int ctas, bn;
+  int64_t tiles;
+};
+
+Cut cut(int64_t M, int64_t N, int planes, bool b_mn) {
+  Cut c;
+  c.ctas = M > 128 ? 2 : 1;
+  const int64_t tm = ceil_div(M, 128 * c.ctas);
+  const int64_t at_once = kSms / c.ctas;
+  const int most = planes > 1 || c.ctas == 1 ? 128 : 256, least = b_mn && c.ctas == 2 ? 128 : 64;
+  // the fewest rounds of tiles by their cost: a narrower tile does less work a byte
+  double best = 0;
+  for (int bn = most; bn >= least; bn /= 2) {
+    const double rounds = (double)ceil_div(tm * ceil_div(N, bn), at_once);
+    const double cost = rounds * (bn + (bn == 256 ? 0 : 16));
+    if (bn == most || cost < best) {
+      best = cost;
+      c.bn = bn;
+    }
+  }
+  c.tiles = tm * ceil_div(N, c.bn);
+  return c;
+}
+
+int cut_k(const Cut& c, int64_t M, int64_t N, int64_t K, int products) {
+  const int64_t free = kSms / c.ctas / std::max<int64_t>(1, c.tiles);
+  const int64_t steps = ceil_div(K, 64) * products;
+  int64_t s = std::min<int64_t>({free, steps / 16, ceil_div(K, 64), 64});
+  const int64_t bytes = round_up(M, 256) * round_up(N, 256) * 4;
+  s = std::min(s, kPartBytes / bytes);
+  return (int)std::max<int64_t>(1, s);
+}
+
+bool small(const Sizes& s) { return s.rows <= 512 && s.inner * s.classes <= 32768 && s.classes <= 2048; }
+
+struct Layout {
+  int planes, products;
+  int64_t kp;              // x's and w's row stride where they are packed
+  bool direct;             // bf16 rows that the copy engine reads as they are
+  int64_t rows_pad, piece; // classes of a piece (a multiple of 256, but for one piece of all)
+  int64_t pieces, ldp;     // p's row stride
+  Cut z, dx, dw;
+  int dx_splits, dw_splits;
+  bool dx_part;
+  int64_t halves;          // forward: partial (maximum, sum) of a row
+  size_t idx, live, x, w, ms, zlab, p, db, dxs, dws, bytes;
+};
+
+Layout layout(const Sizes& s, bool backward) {
+  Layout l{};
+  l.planes = s.prec == AGN_PREC_FP32 ? 3 : 1;
+  l.products = l.planes == 3 ? 6 : 1;
+  l.kp = round_up(s.inner, 8);
+  l.direct = l.planes == 1 && s.inner % 8 == 0;
+  l.rows_pad = round_up(s.rows, 256);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (size_t)round_up((int64_t)bytes, 1024);
+    return here;
+  };
+  if (small(s)) {
+    if (backward) l.p = take((size_t)s.rows * s.classes * 4);
+    l.bytes = std::max<size_t>(at, 1024);
+    return l;
+  }
+  int64_t most = s.classes;
+  auto limit = [&](int64_t bytes, int64_t each) { most = std::min(most, std::max<int64_t>(1024, bytes / each / 256 * 256)); };
+  if (backward) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
+  if (!l.direct) limit(kPackBytes, l.kp * 2 * l.planes);
+  limit((int64_t)1 << 29, std::max<int64_t>(1, l.rows_pad / 16384));   // tiles of a launch
+  l.piece = most;
+  l.pieces = ceil_div(s.classes, l.piece);
+  l.ldp = round_up(l.piece, 64);
+  l.z = cut(s.rows, l.piece, l.planes, false);
+  l.live = take(4);
+  l.idx = take((size_t)l.rows_pad * 4);
+  l.x = take((size_t)l.planes * l.rows_pad * l.kp * 2);
+  if (!l.direct) l.w = take((size_t)l.planes * l.piece * l.kp * 2);
+  if (!backward) {
+    l.halves = 2 * (ceil_div(l.piece, l.z.bn) * (l.pieces - 1) +
+                    ceil_div(s.classes - (l.pieces - 1) * l.piece, l.z.bn));
+    l.ms = take((size_t)l.halves * l.rows_pad * 8);
+    l.zlab = take((size_t)l.rows_pad * 4);
+  } else {
+    l.p = take((size_t)l.planes * l.rows_pad * l.ldp * 2);
+    l.db = take((size_t)(l.rows_pad / 32) * l.ldp * 4);
+    l.dx = cut(s.rows, s.inner, l.planes, true);
+    l.dx_splits = cut_k(l.dx, s.rows, s.inner, l.piece, l.products);
+    l.dx_part = l.pieces > 1 || l.dx_splits > 1;
+    if (l.dx_part) l.dxs = take((size_t)l.dx_splits * l.rows_pad * round_up(s.inner, 64) * 4);
+    l.dw = cut(l.piece, s.inner, l.planes, true);
+    l.dw_splits = cut_k(l.dw, l.piece, s.inner, s.rows, l.products);
+    if (l.dw_splits > 1)
+      l.dws = take((size_t)l.dw_splits * round_up(l.piece, 256) * round_up(s.inner, 64) * 4);
+  }
+  l.bytes = at;
+  return l;
+}
+
+// ------------------------------------------------------------------ kernels
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void from_float(float* p, float v) { AGN_ST(p, v); }
+__device__ __forceinline__ void from_float(bf16* p, float v) { AGN_ST(p, __float2bfloat16_rn(v)); }
+
+// The places of the rows with a label, in order, and their number: one block, 8 rows a thread at a time.
+__global__ void __launch_bounds__(1024) rows_kernel(const int* labels, int rows, int classes, int* idx, int* live) {
+  pdl_begin();
+  __shared__ int sums[33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int base = 0;
+  for (int r0 = 0; r0 < rows; r0 += 8192) {
+    const int first = r0 + 8 * threadIdx.x;
+    uint32_t mask = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (first + i < rows && has_label(AGN_LD(labels + first + i), classes)) mask |= 1u << i;
+    const int n = __popc(mask);
+    int before = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += v;
+    }
+    if (lane == 31) sums[warp] = before;
+    __syncthreads();
+    if (warp == 0) {
+      int v = sums[lane], all = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int w = __shfl_up_sync(0xffffffffu, all, o);
+        if (lane >= o) all += w;
+      }
+      sums[lane] = all - v;
+      if (lane == 31) sums[32] = all;
+    }
+    __syncthreads();
+    int to = base + sums[warp] + before - n;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (mask >> i & 1) AGN_ST(idx + to++, first + i);
+    base += sums[32];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) AGN_ST(live, base);
+}
+
+// Rows of src as bf16 (fp32: three pieces) with zeros up to the stride, eight columns a thread.  idx
+// (x): the rows with a label, then zeros up to a multiple of 64 rows; nothing where the copy engine
+// reads src itself (direct) and no row is missing.  dx: its rows without a label are zeroed.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+pack_kernel(const T* src, int64_t rows, int inner, const int* idx, const int* live_p, bool direct, bf16* dst,
+            int64_t ld, int64_t plane, const int* labels, int classes, T* dx) {
+  pdl_begin();
+  const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+  const int groups = (int)(ld / 8);
+  int64_t live = rows, out_rows = rows;
+  if (idx) {
+    live = AGN_LD(live_p);
+    out_rows = (live + 63) / 64 * 64;
+    if (live < rows && dx) {
+      for (int64_t i = first; i < rows * groups; i += step) {
+        const int64_t r = i / groups;
+        if (has_label(AGN_LD(labels + r), classes)) continue;
+        const int c = (int)(i - r * groups) * 8;
+        for (int k = c; k < min(c + 8, inner); ++k) from_float(dx + r * inner + k, 0.f);
+      }
+    }
+    if (direct && live == rows) return;
+  }
+  const bool vec = inner % 8 == 0;   // (src is 16-byte aligned)
+  for (int64_t i = first; i < out_rows * groups; i += step) {
+    const int64_t r = i / groups;
+    const int c = (int)(i - r * groups) * 8;
+    float v[8];
+    if (r >= live) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    } else {
+      const T* p = src + (idx ? (int64_t)AGN_LD(idx + r) : r) * inner + c;
+      if (vec) {
+        constexpr int n = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 8 / n; ++j) {
+          const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(p) + j);
+          const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+          for (int k = 0; k < n; ++k) v[j * n + k] = to_float(e[k]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + k < inner ? to_float(AGN_LD(p + k)) : 0.f;
+      }
+    }
+    bf16 q[3][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (sizeof(T) == 4) split3(v[k], q[0][k], q[1][k], q[2][k]);
+      else q[0][k] = __float2bfloat16_rn(v[k]);
+    }
+#pragma unroll
+    for (int j = 0; j < (sizeof(T) == 4 ? 3 : 1); ++j)
+      AGN_ST(reinterpret_cast<uint4*>(dst + j * plane + r * ld + c), *reinterpret_cast<const uint4*>(q[j]));
+  }
+}
+
+// lse and loss from the partial maxima and sums: 32 rows a block, its warps share a row's partials.
+__global__ void __launch_bounds__(1024)
+join_kernel(const float2* ms, int halves, int64_t rows_pad, const float* zlab, const int* labels, int classes,
+            int rows, const int* idx, const int* live_p, float* loss, float* lse) {
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int live = AGN_LD(live_p);
+  const int row = blockIdx.x * 32 + lane;
+  __shared__ float2 part[32][32];
+  float m = -INFINITY, s = 0.f;
+  if (row < live) {
+    for (int j = warp; j < halves; j += warps) {
+      const float2 v = AGN_LD(ms + (int64_t)j * rows_pad + row);
+      const float most = fmaxf(m, v.x), from = most == -INFINITY ? 0.f : most;
+      s = s * exp2f((m - from) * kLog2e) + v.y * exp2f((v.x - from) * kLog2e);
+      m = most;
+    }
+  }
+  part[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp != 0) return;
+  for (int j = 1; j < warps; ++j) {
+    const float2 v = part[j][lane];
+    const float most = fmaxf(m, v.x), from = most == -INFINITY ? 0.f : most;
+    s = s * exp2f((m - from) * kLog2e) + v.y * exp2f((v.x - from) * kLog2e);
+    m = most;
+  }
+  if (row < live) {
+    const int at = AGN_LD(idx + row);
+    const float total = m == -INFINITY && s == 0.f ? -INFINITY : m + logf(s);
+    AGN_ST(lse + at, total);
+    AGN_ST(loss + at, total == -INFINITY ? INFINITY : total - AGN_LD(zlab + row));
+  }
+  if (row < rows && !has_label(AGN_LD(labels + row), classes)) {
+    AGN_ST(lse + row, 0.f);
+    AGN_ST(loss + row, 0.f);
+  }
+}
+
+// dbias[c] = the sums of 32 rows each, in order: 32 columns a block, its warps share them.
+__global__ void __launch_bounds__(1024)
+columns_kernel(const float* db, int64_t ld, int cols, const int* live_p, float* out) {
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int blocks = (AGN_LD(live_p) + 31) / 32, c = blockIdx.x * 32 + lane;
+  __shared__ float part[32][33];
+  float s = 0.f;
+  if (c < cols)
+    for (int b = warp; b < blocks; b += warps) s += AGN_LD(db + b * ld + c);
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || c >= cols) return;
+  for (int j = 1; j < warps; ++j) s += part[j][lane];
+  AGN_ST(out + c, s);
+}
+
+// out[idx[m]][n] = the sum of the ranges' sums, in order (idx null: row m).
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+ranges_kernel(const float* part, int splits, int64_t plane, int64_t ld, int64_t rows, int cols, const int* idx,
+              const int* live_p, T* out, bool vec) {
+  pdl_begin();
+  const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+  const int groups = (cols + 3) / 4;
+  if (idx) rows = AGN_LD(live_p);
+  for (int64_t i = first; i < rows * groups; i += step) {
+    const int64_t r = i / groups;
+    const int c = (int)(i - r * groups) * 4;
+    const float* p = part + r * ld + c;
+    float4 s = AGN_LD(reinterpret_cast<const float4*>(p));
+    for (int k = 1; k < splits; ++k) {
+      const float4 v = AGN_LD(reinterpret_cast<const float4*>(p + k * plane));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const int64_t to = (idx ? (int64_t)AGN_LD(idx + r) : r) * cols + c;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    if (vec && c + 4 <= cols) {
+      if (sizeof(T) == 4) {
+        AGN_ST(reinterpret_cast<float4*>(out + to), s);
+      } else {
+        const __nv_bfloat162 o[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+        AGN_ST(reinterpret_cast<uint2*>(out + to), *reinterpret_cast<const uint2*>(o));
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < cols) from_float(out + to + k, v[k]);
+    }
+  }
+}
+
+// ---- small problems: a warp a row, fp32 arithmetic
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The logits of four classes from c on (every lane gets them).
+template <typename T>
+__device__ __forceinline__ void logits4(const T* x, const T* w, const float* bias, int inner, int classes, int c,
+                                        int lane, float (&z)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) z[j] = 0.f;
+  for (int k = lane; k < inner; k += 32) {
+    const float xv = to_float(AGN_LD(x + k));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      z[j] = fmaf(xv, to_float(AGN_LD(w + (int64_t)min(c + j, classes - 1) * inner + k)), z[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    z[j] = warp_sum(z[j]);
+    z[j] = c + j < classes ? z[j] + (bias ? AGN_LD(bias + c + j) : 0.f) : -INFINITY;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64)
+small_loss_kernel(const T* x, const T* w, const float* bias, const int* labels, int rows, int inner, int classes,
+                  float* loss, float* lse) {
+  pdl_begin();
+  const int lane = threadIdx.x & 31, row = blockIdx.x * 2 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int label = AGN_LD(labels + row);
+  float total = 0.f, l = 0.f;
+  if (has_label(label, classes)) {
+    float m = -INFINITY, s = 0.f, zl = 0.f;
+    for (int c = 0; c < classes; c += 4) {
+      float z[4];
+      logits4(x + (int64_t)row * inner, w, bias, inner, classes, c, lane, z);
+      float most = m;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        most = fmaxf(most, z[j]);
+        if (c + j == label) zl = z[j];
+      }
+      const float from = most == -INFINITY ? 0.f : most;
+      s *= exp2f((m - from) * kLog2e);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += exp2f((z[j] - from) * kLog2e);
+      m = most;
+    }
+    total = m == -INFINITY && s == 0.f ? -INFINITY : m + logf(s);
+    l = total == -INFINITY ? INFINITY : total - zl;
+  }
+  if (lane == 0) {
+    AGN_ST(lse + row, total);
+    AGN_ST(loss + row, l);
+  }
+}
+
+// p [rows][classes] (fp32) and dx.
+template <typename T>
+__global__ void __launch_bounds__(64)
+small_rows_kernel(const T* x, const T* w, const float* bias, const int* labels, const float* lse, const float* dloss,
+                  const float* dlse, float scale, int rows, int inner, int classes, float* p, T* dx) {
+  pdl_begin();
+  extern __shared__ float shared_p[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 2 + warp;
+  if (row >= rows) return;
+  float* mine = shared_p + warp * classes;
+  const int label = AGN_LD(labels + row);
+  const bool known = has_label(label, classes);
+  float total = 0.f, fa = 0.f, fb = 0.f;
+  if (known) {
+    total = AGN_LD(lse + row);
+    const float dl = dloss ? AGN_LD(dloss + row) : 1.f;
+    fb = scale * dl;
+    fa = dlse ? scale * (dl + AGN_LD(dlse + row)) : fb;
+  }
+  const bool live = known && total != -INFINITY;
+  for (int c = 0; c < classes; c += 4) {
+    float z[4];
+    if (live) logits4(x + (int64_t)row * inner, w, bias, inner, classes, c, lane, z);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v = 0.f;
+      if (live) {
+        v = fa * exp2f((z[j] - total) * kLog2e);
+        if (c + j == label) v -= fb;
+      }
+      if (lane == j && c + j < classes) mine[c + j] = v;
+    }
+  }
+  __syncwarp();
+  for (int c = lane; c < classes; c += 32) AGN_ST(p + (int64_t)row * classes + c, mine[c]);
+  if (!dx) return;
+  for (int k = lane; k < inner; k += 32) {
+    float s = 0.f;
+    if (live)
+      for (int c = 0; c < classes; ++c) s = fmaf(mine[c], to_float(AGN_LD(w + (int64_t)c * inner + k)), s);
+    from_float(dx + (int64_t)row * inner + k, s);
+  }
+}
+
+// dw and dbias: 32 columns of a class a block, its warps share the rows.  (Column `inner`: the bias.)
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+small_columns_kernel(const float* p, const T* x, const int* labels, int rows, int inner, int classes, T* dw,
+                     float* dbias) {
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kThreads / 32;
+  const int c = blockIdx.x, k = blockIdx.y * 32 + lane;
+  __shared__ float part[kThreads / 32][33];
+  float s = 0.f;
+  if (k <= inner)
+    for (int r = warp; r < rows; r += warps) {
+      if (!has_label(AGN_LD(labels + r), classes)) continue;
+      const float v = AGN_LD(p + (int64_t)r * classes + c);
+      s = k < inner ? fmaf(v, to_float(AGN_LD(x + (int64_t)r * inner + k)), s) : s + v;
+    }
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || k > inner) return;
+  for (int j = 1; j < warps; ++j) s += part[j][lane];
+  if (k < inner) {
+    if (dw) from_float(dw + (int64_t)c * inner + k, s);
+  } else if (dbias) {
+    AGN_ST(dbias + c, s);
+  }
+}
+
+// ------------------------------------------------------------------ calls
+
+struct Call {
+  const void *x, *w;
+  const float* bias;
+  const int* labels;
+  Sizes s;
+  float *loss, *lse_out;                       // forward
+  const float *lse, *dloss, *dlse;             // backward
+  float scale;
+  void *dx, *dw;
+  float* dbias;
+  uint8_t* work;
+  int64_t work_bytes;
+  int* err;
+  uint64_t wait_ns;
+  int withhold;
+};
+
+template <typename... A>
+Status run(void (*kern)(A...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+  AGN_TRY_CUDA(launch_pdl(kern, grid, dim3((unsigned)threads), smem, st, args...));
+  return Status::Ok();
+}
+
+unsigned grid_for(int64_t items, int per) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, per), 8 * kSms)); }
+
+template <typename T>
+Status small_forward(const Call& c, cudaStream_t st) {
+  return run(small_loss_kernel<T>, dim3((unsigned)ceil_div(c.s.rows, 2)), 64, 0, st, static_cast<const T*>(c.x),
+             static_cast<const T*>(c.w), c.bias, c.labels, (int)c.s.rows, (int)c.s.inner, (int)c.s.classes, c.loss,
+             c.lse_out);
+}
+
+template <typename T>
+Status small_backward(const Call& c, const Layout& l, cudaStream_t st) {
+  float* p = reinterpret_cast<float*>(c.work + l.p);
+  const int rows = (int)c.s.rows, inner = (int)c.s.inner, classes = (int)c.s.classes;
+  AGN_TRY(run(small_rows_kernel<T>, dim3((unsigned)ceil_div(rows, 2)), 64, (size_t)classes * 8, st,
+              static_cast<const T*>(c.x), static_cast<const T*>(c.w), c.bias, c.labels, c.lse, c.dloss, c.dlse,
+              c.scale, rows, inner, classes, p, static_cast<T*>(c.dx)));
+  if (!c.dw && !c.dbias) return Status::Ok();
+  return run(small_columns_kernel<T>, dim3((unsigned)classes, (unsigned)ceil_div(inner + 1, 32)), kThreads, 0, st,
+             (const float*)p, static_cast<const T*>(c.x), c.labels, rows, inner, classes, static_cast<T*>(c.dw),
+             c.dbias);
+}
+
+// Rows of x that have a label: counted, and packed (or gathered where some are missing).
+template <typename T>
+Status prepare_rows(const Call& c, const Layout& l, cudaStream_t st) {
+  int* idx = reinterpret_cast<int*>(c.work + l.idx);
+  int* live = reinterpret_cast<int*>(c.work + l.live);
+  AGN_TRY(run(rows_kernel, dim3(1), 1024, 0, st, c.labels, (int)c.s.rows, (int)c.s.classes, idx, live));
+  return run(pack_kernel<T>, dim3(grid_for(l.rows_pad * (l.kp / 8), kThreads)), kThreads, 0, st,
+             static_cast<const T*>(c.x), c.s.rows, (int)c.s.inner, (const int*)idx, (const int*)live, l.direct,
+             reinterpret_cast<bf16*>(c.work + l.x), l.kp, l.rows_pad * l.kp, c.labels, (int)c.s.classes,
+             static_cast<T*>(c.dx));
+}
+
+// Rows c0 .. c0 + n - 1 of w as bf16 rows or pieces, where they are not read as they are.
+template <typename T>
+Status prepare_w(const Call& c, const Layout& l, int64_t c0, int64_t n, cudaStream_t st) {
+  if (l.direct) return Status::Ok();
+  return run(pack_kernel<T>, dim3(grid_for(n * (l.kp / 8), kThreads)), kThreads, 0, st,
+             static_cast<const T*>(c.w) + c0 * c.s.inner, n, (int)c.s.inner, (const int*)nullptr,
+             (const int*)nullptr, false, reinterpret_cast<bf16*>(c.work + l.w), l.kp, l.piece * l.kp,
+             (const int*)nullptr, 0, (T*)nullptr);
+}
+
+// x as an operand: as it is and gathered, or packed alone.
+Status x_maps(const Call& c, const Layout& l, uint32_t box_inner, uint32_t box_rows, CUtensorMap* own, CUtensorMap* alt) {
+  const void* packed = c.work + l.x;
+  AGN_TRY(make_tmap_bf16_3d(alt, packed, l.kp, l.rows_pad, l.planes, l.kp, l.rows_pad * l.kp, box_inner, box_rows));
+  if (!l.direct) {
+    *own = *alt;
+    return Status::Ok();
+  }
+  return make_tmap_bf16_3d(own, c.x, c.s.inner, c.s.rows, 1, c.s.inner, c.s.rows * c.s.inner, box_inner, box_rows);
+}
+
+// Rows c0 .. c0 + n - 1 of w as an operand.
+Status w_map(const Call& c, const Layout& l, int64_t c0, int64_t n, uint32_t box_inner, uint32_t box_rows,
+             CUtensorMap* m) {
+  if (l.direct)
+    return make_tmap_bf16_3d(m, static_cast<const bf16*>(c.w) + c0 * c.s.inner, c.s.inner, n, 1, c.s.inner,
+                             n * c.s.inner, box_inner, box_rows);
+  return make_tmap_bf16_3d(m, c.work + l.w, l.kp, n, l.planes, l.kp, l.piece * l.kp, box_inner, box_rows);
+}
+
+GemmArgs common_args(const Call& c, const Layout& l) {
+  GemmArgs a{};
+  a.live = reinterpret_cast<const int*>(c.work + l.live);
+  a.idx = reinterpret_cast<const int*>(c.work + l.idx);
+  a.rows = (int)c.s.rows;
+  a.products = l.products;
+  a.splits = 1;
+  a.err = c.err;
+  a.wait_ns = (uint32_t)c.wait_ns;
+  a.withhold = c.withhold;
+  return a;
+}
+
+// The product of the logits of classes c0 .. c0 + n - 1.
+GemmArgs logit_args(const Call& c, const Layout& l, int64_t c0, int64_t n) {
+  GemmArgs a = common_args(c, l);
+  a.M = (int)c.s.rows; a.N = (int)n; a.K = (int)l.kp;
+  a.alt = l.direct ? 1 : 0;
+  a.bn = l.z.bn;
+  a.bias = c.bias;
+  a.labels = c.labels;
+  a.class0 = (int)c0; a.classes = (int)c.s.classes;
+  a.rows_pad = l.rows_pad;
+  return a;
+}
+
+template <typename T>
+Status forward(const Call& c, const Layout& l, cudaStream_t st) {
+  AGN_TRY(prepare_rows<T>(c, l, st));
+  float2* ms = reinterpret_cast<float2*>(c.work + l.ms);
+  float* zlab = reinterpret_cast<float*>(c.work + l.zlab);
+  CUtensorMap tx, txa, tw;
+  AGN_TRY(x_maps(c, l, 64, 128, &tx, &txa));
+  const int64_t tm = ceil_div(c.s.rows, 128 * l.z.ctas);
+  int64_t half = 0;
+  for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
+    const int64_t n = std::min(l.piece, c.s.classes - c0);
+    AGN_TRY(prepare_w<T>(c, l, c0, n, st));
+    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &tw));
+    GemmArgs a = logit_args(c, l, c0, n);
+    a.ms = ms + half * l.rows_pad;
+    a.zlab = zlab;
+    AGN_TRY(gemm(l.z.ctas, kLse, tx, tw, txa, tx, a, (int)std::min<int64_t>(INT32_MAX, tm * ceil_div(n, l.z.bn)), st));
+    half += 2 * ceil_div(n, l.z.bn);
+  }
+  const int warps = (int)std::min<int64_t>(32, std::max<int64_t>(1, half / 4));
+  return run(join_kernel, dim3((unsigned)ceil_div(c.s.rows, 32)), 32 * warps, 0, st, (const float2*)ms, (int)half,
+             l.rows_pad, (const float*)zlab, c.labels, (int)c.s.classes, (int)c.s.rows,
+             (const int*)(c.work + l.idx), (const int*)(c.work + l.live), c.loss, c.lse_out);
+}
+
+template <typename T>
+Status sum_ranges(const float* part, int splits, int64_t plane, int64_t ld, int64_t rows, int64_t cols, const int* idx,
+                  const int* live, T* out, cudaStream_t st) {
+  const bool vec = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
+  return run(ranges_kernel<T>, dim3(grid_for(rows * ceil_div(cols, 4), kThreads)), kThreads, 0, st, part, splits,
+             plane, ld, rows, (int)cols, idx, live, out, vec);
+}
+
+template <typename T>
+Status backward(const Call& c, const Layout& l, cudaStream_t st) {
+  constexpr int es = (int)sizeof(T);
+  const int64_t rows = c.s.rows, inner = c.s.inner;
+  const int* idx = reinterpret_cast<const int*>(c.work + l.idx);
+  const int* live = reinterpret_cast<const int*>(c.work + l.live);
+  AGN_TRY(prepare_rows<T>(c, l, st));
+  bf16* p = reinterpret_cast<bf16*>(c.work + l.p);
+  float* db = reinterpret_cast<float*>(c.work + l.db);
+  const int64_t p_plane = l.rows_pad * l.ldp, ldn = round_up(inner, 64), dw_rows = round_up(l.piece, 256);
+  CUtensorMap tx, txa, txm, txma, tp_store, tp_k, tp_m, tc;
+  AGN_TRY(x_maps(c, l, 64, 128, &tx, &txa));
+  AGN_TRY(x_maps(c, l, 64, 64, &txm, &txma));
+  AGN_TRY(make_tmap_store_2d(&tp_store, p, 2, l.ldp, l.planes * l.rows_pad, l.ldp, 32, 32));
+  AGN_TRY(make_tmap_bf16_3d(&tp_k, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 128));
+  AGN_TRY(make_tmap_bf16_3d(&tp_m, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 64));
+  const bool rows16 = inner * es % 16 == 0;
+  for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
+    const int64_t n = std::min(l.piece, c.s.classes - c0);
+    AGN_TRY(prepare_w<T>(c, l, c0, n, st));
+    CUtensorMap tw;
+    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &tw));
+    GemmArgs a = logit_args(c, l, c0, n);
+    a.lse = c.lse; a.dloss = c.dloss; a.dlse = c.dlse; a.scale = c.scale;
+    a.p_plane = (int)l.rows_pad;
+    a.db = c.dbias ? db : nullptr;
+    a.ld_db = l.ldp;
+    AGN_TRY(gemm(l.z.ctas, kGrad, tx, tw, txa, tp_store, a,
+                 (int)(ceil_div(rows, 128 * l.z.ctas) * ceil_div(n, l.z.bn)), st));
+    if (c.dbias)
+      AGN_TRY(run(columns_kernel, dim3((unsigned)ceil_div(n, 32)),
+                  32 * (int)std::min<int64_t>(32, l.rows_pad / 128), 0, st, (const float*)db, l.ldp, (int)n, live,
+                  c.dbias + c0));
+    if (c.dw) {   // [n][inner] = p^T x
+      T* dw = static_cast<T*>(c.dw) + c0 * inner;
+      GemmArgs d = common_args(c, l);
+      d.M = (int)n; d.N = (int)inner; d.K = (int)rows;
+      d.live_is = 1;
+      d.alt = l.direct ? 2 : 0;
+      d.bn = l.dw.bn;
+      d.a_mn = d.b_mn = 1;
+      d.splits = l.dw_splits;
+      d.out = dw; d.ldo = inner; d.dtype = c.s.prec;
+      tc = tp_store;   // (not read)
+      if (l.dw_splits > 1) {
+        d.part = 1;
+        d.part_rows = (int)dw_rows;
+        AGN_TRY(make_tmap_store_2d(&tc, c.work + l.dws, 4, ldn, l.dw_splits * dw_rows, ldn, 32, 32));
+      } else if (rows16) {
+        d.tma_out = 1;
+        AGN_TRY(make_tmap_store_2d(&tc, dw, es, inner, n, inner, 32, 32));
+      }
+      const int64_t tiles = ceil_div(n, 128 * l.dw.ctas) * ceil_div(inner, l.dw.bn);
+      AGN_TRY(gemm(l.dw.ctas, kOut, tp_m, txm, txma, tc, d, (int)(tiles * d.splits), st));
+      if (l.dw_splits > 1)
+        AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dws), l.dw_splits, dw_rows * ldn, ldn, n,
+                           inner, (const int*)nullptr, (const int*)nullptr, dw, st));
+    }
+    if (c.dx) {   // [rows][inner] += p w
+      GemmArgs d = common_args(c, l);
+      d.M = (int)rows; d.N = (int)inner; d.K = (int)n;
+      d.bn = l.dx.bn;
+      d.b_mn = 1;
+      d.splits = l.dx_splits;
+      d.out = c.dx; d.ldo = inner; d.dtype = c.s.prec;
+      d.scatter = 1;
+      CUtensorMap twm;
+      AGN_TRY(w_map(c, l, c0, n, 64, 64, &twm));
+      tc = tp_store;
+      if (l.dx_part) {
+        d.part = c0 == 0 ? 1 : 2;
+        d.part_rows = (int)l.rows_pad;
+        AGN_TRY(make_tmap_store_2d(&tc, c.work + l.dxs, 4, ldn, l.dx_splits * l.rows_pad, ldn, 32, 32));
+      } else if (rows16) {
+        d.tma_out = 1;
+        AGN_TRY(make_tmap_store_2d(&tc, c.dx, es, inner, rows, inner, 32, 32));
+      }
+      const int64_t tiles = ceil_div(rows, 128 * l.dx.ctas) * ceil_div(inner, l.dx.bn);
+      AGN_TRY(gemm(l.dx.ctas, kOut, tp_k, twm, twm, tc, d, (int)(tiles * d.splits), st));
+    }
+  }
+  if (c.dx && l.dx_part)
+    AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dxs), l.dx_splits, l.rows_pad * ldn, ldn, rows,
+                       inner, idx, live, static_cast<T*>(c.dx), st));
+  return Status::Ok();
+}
+
+Status check_sizes(const Sizes& s) {
+  if (!dtype_size(s.prec)) return Status::Err(AGN_E_INVALID, "unknown dtype");
+  if (s.rows < 0 || s.rows > 1 << 28 || s.inner < 1 || s.inner > 1 << 20 || s.classes < 1 || s.classes > 1 << 28)
+    return Status::Err(AGN_E_INVALID, "need 0 <= rows <= 2^28, 1 <= inner <= 2^20, 1 <= classes <= 2^28");
+  return Status::Ok();
+}
+
+Status call(Call& c, bool backward_call, cudaStream_t st) {
+  AGN_TRY(check_sizes(c.s));
+  const size_t es = dtype_size(c.s.prec);
+  const int64_t rows = c.s.rows, inner = c.s.inner, classes = c.s.classes;
+  const size_t xb = (size_t)rows * inner * es, wb = (size_t)classes * inner * es, rb = (size_t)rows * 4,
+               cb = (size_t)classes * 4;
+  const Layout l = layout(c.s, backward_call);
+  if (rows > 0) {
+    if (!c.x || !c.w || !c.labels || (backward_call ? !c.lse : !c.loss || !c.lse_out))
+      return Status::Err(AGN_E_INVALID, "null pointer");
+    if (!c.work || c.work_bytes < (int64_t)l.bytes)
+      return Status::Err(AGN_E_INVALID, "work needs " + std::to_string(l.bytes) + " bytes");
+  }
+  const CallBuffer x{"x", c.x, xb, 16}, w{"w", c.w, wb, 16}, bias{"bias", c.bias, c.bias ? cb : 0, 4},
+      labels{"labels", c.labels, rb, 4}, lse{"lse", backward_call ? c.lse : c.lse_out, rb, 4},
+      loss{"loss", c.loss, c.loss ? rb : 0, 4}, dloss{"dloss", c.dloss, c.dloss ? rb : 0, 4},
+      dlse{"dlse", c.dlse, c.dlse ? rb : 0, 4}, dx{"dx", c.dx, c.dx ? xb : 0, 16}, dw{"dw", c.dw, c.dw ? wb : 0, 16},
+      dbias{"dbias", c.dbias, c.dbias ? cb : 0, 4}, work{"work", rows > 0 ? c.work : nullptr, l.bytes, 256},
+      err{"err", c.err, c.err ? 4u : 0u, 4};
+  AGN_TRY(check_apart(work, {x, w, bias, labels, lse, loss, dloss, dlse, dx, dw, dbias, err}));
+  if (backward_call) {
+    AGN_TRY(check_apart(dx, {x, w, bias, labels, lse, dloss, dlse, dw, dbias, err}));
+    AGN_TRY(check_apart(dw, {x, w, bias, labels, lse, dloss, dlse, dbias, err}));
+    AGN_TRY(check_apart(dbias, {x, w, bias, labels, lse, dloss, dlse, err}));
+    AGN_TRY(check_apart(err, {x, w, bias, labels, lse, dloss, dlse}));
+  } else {
+    AGN_TRY(check_apart(loss, {x, w, bias, labels, lse, err}));
+    AGN_TRY(check_apart(lse, {x, w, bias, labels, err}));
+    AGN_TRY(check_apart(err, {x, w, bias, labels}));
+  }
+  if (rows == 0) {   // no rows: the sums over them are zero
+    AGN_TRY(check_buffers({dw, dbias}));
+    if (c.dw) AGN_TRY_CUDA(cudaMemsetAsync(c.dw, 0, wb, st));
+    if (c.dbias) AGN_TRY_CUDA(cudaMemsetAsync(c.dbias, 0, cb, st));
+    return Status::Ok();
+  }
+  AGN_TRY(check_buffers({x, w, bias, labels, lse, loss, dloss, dlse, dx, dw, dbias, work, err}));
+  KnownBuffers known({x, w, bias, labels, lse, loss, dloss, dlse});
+  KnownBuffers known2({dx, dw, dbias, work, err});
+  AGN_TRY(bounds_upload(st));
+  const bool fp32 = c.s.prec == AGN_PREC_FP32;
+  if (!backward_call) {
+    if (small(c.s)) AGN_TRY(fp32 ? small_forward<float>(c, st) : small_forward<bf16>(c, st));
+    else AGN_TRY(fp32 ? forward<float>(c, l, st) : forward<bf16>(c, l, st));
+  } else if (c.dx || c.dw || c.dbias) {
+    if (small(c.s)) AGN_TRY(fp32 ? small_backward<float>(c, l, st) : small_backward<bf16>(c, l, st));
+    else AGN_TRY(fp32 ? backward<float>(c, l, st) : backward<bf16>(c, l, st));
+  }
+  return bounds_collect(st);
+}
+
+// agn_debug_linear_ce_waits: of the calling thread's calls
+thread_local uint64_t t_wait_ns = 0;
+thread_local int t_withhold = 0;
+
+}  // namespace
+}  // namespace ce
+
+AGN_BOUNDS_UNIT(linear_ce)
+
+}  // namespace agn
+
+extern "C" int agn_linear_ce_bytes(int64_t rows, int64_t inner, int64_t classes, int32_t dtype, int32_t backward,
+                                   int64_t* bytes) {
+  return agn::guarded([&] {
+    const agn::ce::Sizes s{rows, inner, classes, dtype};
+    if (!bytes) return agn::Status::Err(AGN_E_INVALID, "null pointer");
+    AGN_TRY(agn::ce::check_sizes(s));
+    *bytes = (int64_t)agn::ce::layout(s, backward != 0).bytes;
+    return agn::Status::Ok();
+  });
+}
+
+extern "C" int agn_linear_ce(const void* x, const void* w, const float* bias, const int32_t* labels, int32_t dtype,
+                             int64_t rows, int64_t inner, int64_t classes, float* loss, float* lse, void* work,
+                             int64_t work_bytes, int32_t* err, void* stream) {
+  return agn::guarded([&] {
+    agn::ce::Call c{};
+    c.x = x; c.w = w; c.bias = bias; c.labels = labels;
+    c.s = {rows, inner, classes, dtype};
+    c.loss = loss; c.lse_out = lse;
+    c.work = static_cast<uint8_t*>(work); c.work_bytes = work_bytes;
+    c.err = err;
+    c.wait_ns = agn::ce::t_wait_ns; c.withhold = agn::ce::t_withhold;
+    return agn::ce::call(c, false, static_cast<cudaStream_t>(stream));
+  });
+}
+
+extern "C" int agn_linear_ce_backward(const void* x, const void* w, const float* bias, const int32_t* labels,
+                                      const float* lse, const float* dloss, const float* dlse, double scale,
+                                      int32_t dtype, int64_t rows, int64_t inner, int64_t classes, void* dx, void* dw,
+                                      float* dbias, void* work, int64_t work_bytes, int32_t* err, void* stream) {
+  return agn::guarded([&] {
+    agn::ce::Call c{};
+    c.x = x; c.w = w; c.bias = bias; c.labels = labels;
+    c.s = {rows, inner, classes, dtype};
+    c.lse = lse; c.dloss = dloss; c.dlse = dlse;
+    c.scale = (float)scale;
+    c.dx = dx; c.dw = dw; c.dbias = dbias;
+    c.work = static_cast<uint8_t*>(work); c.work_bytes = work_bytes;
+    c.err = err;
+    c.wait_ns = agn::ce::t_wait_ns; c.withhold = agn::ce::t_withhold;
+    return agn::ce::call(c, true, static_cast<cudaStream_t>(stream));
+  });
+}
+
+extern "C" int agn_debug_linear_ce_waits(int64_t wait_ns, int32_t withhold_rank) {
+  return agn::guarded([&] {
+    if (wait_ns < 0 || wait_ns > 2000000000ll || withhold_rank < -1 || withhold_rank > 1)
+      return agn::Status::Err(AGN_E_INVALID, "wait_ns must be in [0, 2e9], withhold_rank -1, 0 or 1");
+    agn::ce::t_wait_ns = (uint64_t)wait_ns;
+    agn::ce::t_withhold = withhold_rank + 1;
+    return agn::Status::Ok();
+  });
+}

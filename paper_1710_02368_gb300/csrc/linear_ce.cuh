@@ -1,0 +1,62 @@
+// The output layer's softmax cross-entropy over many classes without keeping the
+// logits (linear_ce.cu: entry points and small kernels; linear_ce_gemm.cuh: the products).
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+
+namespace agn {
+namespace ce {
+
+enum Epilogue {
+  kLse = 0,    // each row's maximum and sum of exponentials over a tile's columns
+  kGrad = 1,   // p, the gradient with respect to the logits, and its column sums
+  kOut = 2,    // the product itself
+};
+
+// One product of [M][K] and [N][K] operands.  Coordinates are elements; rows of x are
+// those with a label, in order (`live` of them, `idx` their places).
+struct GemmArgs {
+  int M, N, K;              // M (live_is 0) or K (live_is 1) is a bound where live is given
+  const int* live;          // device, null: M and K as they are
+  int live_is;
+  int rows;                 // rows of x in all: live < rows means that x was gathered
+  int alt;                  // 1 (2): A (B) comes from tmAlt where x was gathered
+  int bn;                   // columns of a tile
+  int a_mn, b_mn;           // operand stored [K][M] ([K][N]) instead
+  int b_k0, b_n0;           // where B's rows of this product start along K, along N
+  int products;             // 1, or 6 of three bf16 pieces (planes)
+  int splits;               // ranges along K, each with sums of its own (kOut)
+  int* err;
+  uint32_t wait_ns;
+  int withhold;             // test hook: CTA withhold - 1 of a tile leaves out its last stage and all after
+  const int* idx;           // [live] places of the rows
+  // kLse, kGrad
+  const float* bias;        // [classes] or null
+  const int* labels;        // [rows]
+  int class0, classes;      // first class of this product, classes in all
+  float2* ms;               // kLse: [2 N / bn][rows_pad] (maximum, sum)
+  int64_t rows_pad;
+  float* zlab;              // kLse: [rows_pad] the label's logit
+  const float *lse, *dloss, *dlse;   // kGrad, by place
+  float scale;
+  int p_plane;              // kGrad: rows from piece to piece of p
+  float* db;                // kGrad: [rows_pad / 32][ld_db] column sums of 32 rows, or null
+  int64_t ld_db;
+  // kOut
+  void* out;                // [M][ldo] of dtype, rows at idx[m] where live < rows and scatter
+  int dtype;
+  int64_t ldo;
+  int scatter;
+  int tma_out;              // tmC is valid for `out`
+  int part;                 // 0: to out; 1, 2: tmC is fp32 sums [splits][part_rows], stored, added
+  int part_rows;
+};
+
+// ctas: 1 or 2 (pairs).  Queues the launch on the current device.
+Status gemm(int ctas, int epilogue, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt,
+            const CUtensorMap& c, const GemmArgs& args, int max_units, cudaStream_t st);
+
+}  // namespace ce
+}  // namespace agn

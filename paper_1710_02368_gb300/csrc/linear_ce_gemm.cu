@@ -1,0 +1,579 @@
+// The three products of the output layer's loss on the tensor cores (tcgen05 kind::f16, f32
+// sums in TMEM), with what follows each in its epilogue:
+//   logits z = x w^T (K along both operands' rows): kLse leaves (max, sum of exponentials) of
+//     each row and half a tile, kGrad writes p = a softmax - b [label] in bf16 and sums its columns;
+//   dx = p w and dw = p^T x (kOut): operands stored the other way round are read so (the MMA
+//     takes either major), nothing is transposed in memory.
+// fp32 operands are three exact bf16 pieces (planes): six products of pieces, the first in one
+// accumulator and the five smaller ones in another.
+// One CTA a tile of 128 rows, or a pair (cta_group::2) a tile of 256, each CTA loading its 128 rows
+// of A and half of B's: 64 bytes a clock of MMA time instead of 96 with 256 columns.  Persistent:
+// a CTA (pair) walks over tiles in bands of eight along M, so that what runs at a time shares operands
+// in the L2.  Roles by warp: 0 loads (TMA, 128-byte swizzle), 1 issues the MMAs, 4-11 finish, two
+// accumulators in turn, so that a tile's epilogue runs beside the next one's MMAs.
+// Every wait is bounded (2 s); whoever gives up says so to all roles, what could not be computed
+// is NaN, *err is 1, and stages in flight are waited for before the CTA ends.
+#include "linear_ce.cuh"
+#include "ops.cuh"
+#include "tc_ptx.cuh"
+
+namespace agn {
+namespace ce {
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr int kBK = 64;                   // k of a stage: 128-byte rows
+constexpr int kABytes = 128 * 128;        // 128 rows (or columns) of a stage
+constexpr int kBox = 64 * 128;            // an operand stored along M or N: boxes of 64 x 64 k
+constexpr int kRing = 160 * 1024;
+constexpr int kMaxStages = 8;
+constexpr int kStaged = 4096;             // a finishing warp's tile of outputs
+constexpr size_t kSmem = 1024 + kRing + 8 * (kStaged + 512) + 512;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Geometry {
+  int M, N, K, tiles_n, tiles, units, kt_per, KT;
+  bool gathered;
+};
+
+template <int kCtas>
+__device__ __forceinline__ Geometry geometry(const GemmArgs& a) {
+  Geometry g;
+  g.M = a.M; g.N = a.N; g.K = a.K;
+  g.gathered = false;
+  if (a.live) {
+    const int live = min(AGN_LD(a.live), a.rows);
+    g.gathered = live < a.rows;
+    if (a.live_is) g.K = live;
+    else g.M = live;
+  }
+  g.tiles_n = (g.N + a.bn - 1) / a.bn;
+  g.tiles = (g.M + 128 * kCtas - 1) / (128 * kCtas) * g.tiles_n;
+  g.units = g.tiles * a.splits;
+  g.KT = (g.K + kBK - 1) / kBK;
+  g.kt_per = (g.KT + a.splits - 1) / a.splits;
+  return g;
+}
+
+// Tile (in units of a tile) and range along K of unit u: bands of eight tiles along M.
+struct Unit {
+  int m, n, split, kt0, kt;
+  __device__ __forceinline__ Unit(const Geometry& g, int splits, int u) {
+    split = u % splits;
+    const int t = u / splits, tiles_m = g.tiles / g.tiles_n;
+    const int band = t / (8 * g.tiles_n), m0 = band * 8, gm = min(8, tiles_m - m0);
+    const int r = t - m0 * g.tiles_n;
+    m = m0 + r % gm;
+    n = r / gm;
+    kt0 = min(g.KT, split * g.kt_per);
+    kt = min(g.KT, kt0 + g.kt_per) - kt0;
+  }
+};
+
+// Pieces of A and B of product q: the largest first, which has an accumulator of its own.
+__device__ __forceinline__ int piece_a(int q) { return (0x201100 >> (4 * q)) & 15; }
+__device__ __forceinline__ int piece_b(int q) { return (0x021010 >> (4 * q)) & 15; }
+
+// 16-byte piece c of row `row` of a staged tile of rows of kRow bytes, swizzled as its tensor map says.
+template <int kRow>
+__device__ __forceinline__ uint8_t* staged_at(uint8_t* tile, int row, int c) {
+  const int sw = kRow == 128 ? row & 7 : (row >> 1) & 3;
+  return tile + row * kRow + ((c ^ sw) << 4);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Lane l gets the sum over the warp's lanes of v[l]: halves are exchanged and added.
+__device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
+#pragma unroll
+  for (int h = 16; h > 0; h >>= 1) {
+#pragma unroll
+    for (int j = 0; j < h; ++j) {
+      const float send = lane & h ? v[j] : v[j + h], keep = lane & h ? v[j + h] : v[j];
+      v[j] = keep + __shfl_xor_sync(0xffffffffu, send, h);
+    }
+  }
+  return v[0];
+}
+
+// A finishing warp's 32 rows x 32 columns to memory from its staged tile: by bulk stores where a
+// tensor map allows it, else row by row.
+struct Writer {
+  const CUtensorMap* map;
+  uint8_t* tile;
+  int lane;
+  uint32_t slot;   // 2 KB halves of the tile in turn
+
+  __device__ __forceinline__ void send(uint8_t* src, int x, int y, bool add) {
+    tc::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if (add) tc::tma_add_2d(map, src, x, y);
+      else tc::tma_store_2d(map, src, x, y);
+      tc::bulk_commit();
+    }
+  }
+  // 16 words of 2 bf16 a lane
+  __device__ __forceinline__ void stage_bf16(uint8_t* to, const uint32_t (&w)[16]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint4*>(staged_at<64>(to, lane, j)) =
+          make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  }
+  __device__ __forceinline__ void put_bf16(const uint32_t (&w)[16], int x, int y) {
+    if (lane == 0) tc::bulk_wait_read_1();
+    __syncwarp();
+    uint8_t* to = tile + 2048 * slot;
+    slot ^= 1;
+    stage_bf16(to, w);
+    send(to, x, y, false);
+  }
+  __device__ __forceinline__ void stage_fp32(const float (&v)[32]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<float4*>(staged_at<128>(tile, lane, j)) =
+          make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  }
+  __device__ __forceinline__ void put_fp32(const float (&v)[32], int x, int y, bool add) {
+    if (lane == 0) tc::bulk_wait_read();
+    __syncwarp();
+    stage_fp32(v);
+    send(tile, x, y, add);
+  }
+  // rows 0 .. n - 1 to out + at[row] * ldo: columns 0 .. cols - 1; `at` of row l is lane l's
+  template <typename T>
+  __device__ __forceinline__ void put_rows(const float (&v)[32], T* out, int64_t at, int n, int cols) {
+    constexpr int kRow = 32 * (int)sizeof(T), kVec = 16 / (int)sizeof(T), kLanes = 32 / kVec;
+    __syncwarp();
+    if (sizeof(T) == 4) {
+      stage_fp32(v);
+    } else {
+      uint32_t w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+      stage_bf16(tile, w);
+    }
+    __syncwarp();
+    // (the same for the warp: its rows' places differ by whole rows)
+    const bool vec = cols == 32 && __all_sync(0xffffffffu, (reinterpret_cast<uintptr_t>(out + at) & 15) == 0);
+    if (vec) {
+      const int piece = lane % kLanes;
+#pragma unroll 1
+      for (int r0 = 0; r0 < 32; r0 += kVec) {
+        const int row = r0 + lane / kLanes;
+        const int64_t to = __shfl_sync(0xffffffffu, at, row);
+        if (row < n)
+          AGN_ST(reinterpret_cast<uint4*>(out + to + piece * kVec),
+                 *reinterpret_cast<const uint4*>(staged_at<kRow>(tile, row, piece)));
+      }
+    } else {
+#pragma unroll 1
+      for (int row = 0; row < n; ++row) {
+        const int64_t to = __shfl_sync(0xffffffffu, at, row);
+        if (lane < cols)
+          AGN_ST(out + to + lane, *reinterpret_cast<const T*>(staged_at<kRow>(tile, row, lane / kVec) +
+                                                              lane % kVec * sizeof(T)));
+      }
+    }
+  }
+};
+
+// After a role gave up and all have ended: wait for the copies of the last stages, where what will not
+// come any more (the loads of the CTA that armed fewer stages) is made up for.
+template <int kCtas>
+__device__ __forceinline__ void land(uint64_t* full, const int* loaded, int stages, uint32_t bytes) {
+  const int n0 = *loaded, n1 = kCtas == 2 ? tc::ld_cluster_int(loaded, 1) : n0, n = max(n0, n1);
+#pragma unroll 1
+  for (int i = max(0, n - stages); i < n; ++i) {
+    uint64_t* bar = &full[i % stages];
+    if (i >= n0) tc::mbar_arrive_expect_tx(bar, bytes);   // (the second CTA's copies alone)
+    else if (i >= n1) tc::mbar_complete_tx(bar, bytes);
+    tc::mbar_wait_bounded(bar, (uint32_t)(i / stages) & 1, kWaitNs);
+  }
+}
+
+template <int kCtas, int kEpi>
+__global__ void __launch_bounds__(kThreads, 1)
+ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+               const __grid_constant__ CUtensorMap tmAlt, const __grid_constant__ CUtensorMap tmC,
+               const GemmArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* staged = ring + kRing;                                          // [finishing warp][4 KB]
+  float* biases = reinterpret_cast<float*>(staged + 8 * kStaged);          // [finishing warp][128]
+  uint64_t* full = reinterpret_cast<uint64_t*>(biases + 8 * 128);          // (first CTA's: both CTAs' operands)
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* acc_full = empty + kMaxStages;
+  uint64_t* acc_empty = acc_full + 2;                                      // (first CTA's)
+  uint64_t* drained = acc_empty + 2;
+  int* loaded_out = reinterpret_cast<int*>(drained + 1);
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(loaded_out + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = kCtas == 2 ? (int)cluster_rank() : 0;
+  const int group = blockIdx.x / kCtas, groups = gridDim.x / kCtas;
+  const int nb = a.bn / kCtas;
+  const uint32_t stage = kABytes + nb * 128;
+  const int stages = min(kMaxStages, (int)(kRing / stage));
+
+  auto stop_all = [&] {
+    if (kCtas == 2) tc::give_up(abort_flag);
+    else *abort_flag = 1;
+  };
+  auto commit = [&](uint64_t* bar) {
+    if (kCtas == 2) tc::mma_commit_pair(bar);
+    else tc::mma_commit(bar);
+  };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(&acc_full[b], 1);
+      tc::mbar_init(&acc_empty[b], 8 * kCtas);
+    }
+    tc::mbar_init(drained, 1);
+    *loaded_out = 0;
+    *abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (warp == 2) {
+    if (kCtas == 2) {
+      tc::tmem_alloc_pair(tmem_holder, 512);
+      tc::tmem_relinquish_pair();
+    } else {
+      tc::tmem_alloc(tmem_holder, 512);
+      tc::tmem_relinquish();
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (kCtas == 2) cluster_sync();
+  tc::tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  pdl_begin();
+
+  const Geometry g = geometry<kCtas>(a);
+  const uint32_t acc_cols = a.products > 1 ? 2 * a.bn : a.bn;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const CUtensorMap* pa = g.gathered && a.alt == 1 ? &tmAlt : &tmA;
+      const CUtensorMap* pb = g.gathered && a.alt == 2 ? &tmAlt : &tmB;
+      const uint32_t full0 = kCtas == 2 ? tc::map_cluster(full, 0) : 0;
+      int s = 0, loaded = 0, stop = INT32_MAX;
+      uint32_t phase = 1;   // (the first round finds every stage free)
+      bool ok = true;
+      for (int u = group; ok && u < g.units; u += groups) {
+        const Unit t(g, a.splits, u);
+        const int m = (t.m * kCtas + cta) * 128, n = t.n * a.bn + cta * nb;
+        if (a.withhold == cta + 1) stop = max(0, t.kt * a.products - 1);
+        for (int kt = t.kt0; ok && kt < t.kt0 + t.kt; ++kt) {
+          for (int q = 0; q < a.products; ++q) {
+            if (loaded >= stop) {
+              ok = false;
+              break;
+            }
+            if (!tc::wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
+              stop_all();
+              ok = false;
+              break;
+            }
+            uint8_t* st = ring + s * stage;
+            auto load = [&](uint8_t* dst, const CUtensorMap* map, int x, int y, int z) {
+              if (kCtas == 2) tc::tma_load_3d_pair(dst, map, full0 + 8u * (uint32_t)s, x, y, z);
+              else tc::tma_load_3d(dst, map, &full[s], x, y, z);
+            };
+            if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], kCtas * stage);
+            const int za = piece_a(q), zb = piece_b(q), k = kt * kBK;
+            if (a.a_mn) {
+              load(st, pa, m, k, za);
+              load(st + kBox, pa, m + 64, k, za);
+            } else {
+              load(st, pa, k, m, za);
+            }
+            if (a.b_mn) {
+              for (int j = 0; j < nb; j += 64)
+                load(st + kABytes + j * 128, pb, n + j, k + a.b_k0, zb);
+            } else {
+              load(st + kABytes, pb, k, n + a.b_n0, zb);
+            }
+            ++loaded;
+            if (++s == stages) s = 0, phase ^= 1;
+          }
+        }
+      }
+      *loaded_out = loaded;
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && cta == 0) {
+      const uint32_t idesc = tc::idesc_bf16_f32(128 * kCtas, a.bn, a.a_mn, a.b_mn);
+      const uint32_t r0 = tc::smem_u32(ring);
+      const uint64_t da0 = tc::smem_desc_sw128(r0, a.a_mn ? kBox : 16, 1024);
+      const uint64_t db0 = tc::smem_desc_sw128(r0 + kABytes, a.b_mn ? kBox : 16, 1024);
+      const uint64_t ka = (a.a_mn ? 2048 : 32) >> 4, kb = (a.b_mn ? 2048 : 32) >> 4;   // 16 k
+      uint64_t da = da0, db = db0;
+      int s = 0, done = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int u = group; u < g.units; u += groups, ++done) {
+        const Unit t(g, a.splits, u);
+        const int buf = done & 1;
+        if (done >= 2 && !tc::wait_mbar<true>(&acc_empty[buf], ((done >> 1) - 1) & 1, abort_flag, a.wait_ns)) {
+          stop_all();
+          break;
+        }
+        tc::tc_fence_after();
+        const uint32_t d0 = tmem + buf * acc_cols;
+        for (int kt = 0; ok && kt < t.kt; ++kt) {
+          for (int q = 0; q < a.products; ++q) {
+            if (!tc::wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
+              stop_all();
+              ok = false;
+              break;
+            }
+            tc::tc_fence_after();
+            const uint32_t d = d0 + (q > 0 ? a.bn : 0);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint32_t acc = kk > 0 || kt > 0 || q > 1;
+              if (kCtas == 2) tc::mma_bf16_pair(d, da + kk * ka, db + kk * kb, idesc, acc);
+              else tc::mma_bf16(d, da + kk * ka, db + kk * kb, idesc, acc);
+            }
+            commit(&empty[s]);
+            da += stage >> 4;
+            db += stage >> 4;
+            if (++s == stages) s = 0, phase ^= 1, da = da0, db = db0;
+          }
+        }
+        if (!ok || *abort_flag) break;   // no sums: the finishing warps give up
+        commit(&acc_full[buf]);
+      }
+    }
+  } else if (warp >= 4) {
+    const int e = warp - 4, quad = warp & 3, half = e >> 2, chunks = a.bn / 64;   // of 32 columns
+    float* bias = biases + 128 * e;
+    const uint32_t empty0 = kCtas == 2 ? tc::map_cluster(acc_empty, 0) : tc::smem_u32(acc_empty);
+    Writer out{&tmC, staged + e * kStaged, lane, 0};
+    bool ok = true;
+    int done = 0;
+    for (int u = group; u < g.units; u += groups, ++done) {
+      const Unit t(g, a.splits, u);
+      const int buf = done & 1;
+      const int row0 = (t.m * kCtas + cta) * 128 + 32 * quad, row = row0 + lane;
+      const int col0 = t.n * a.bn + half * 32 * chunks;
+      const bool live = row < g.M;
+      // what the row needs, on its way while the sums are
+      int label = -1;
+      float lse = 0.f, fa = 0.f, fb = 0.f;
+      if (kEpi != kOut) {
+        if (live) {
+          const int at = AGN_LD(a.idx + row);
+          label = AGN_LD(a.labels + at) - a.class0 - col0;
+          if (kEpi == kGrad) {
+            lse = AGN_LD(a.lse + at);
+            const float dl = a.dloss ? AGN_LD(a.dloss + at) : 1.f;
+            fb = a.scale * dl;
+            fa = a.dlse ? a.scale * (dl + AGN_LD(a.dlse + at)) : fb;
+          }
+        }
+        __syncwarp();
+        for (int i = lane; i < 32 * chunks; i += 32) {
+          const int c = a.class0 + col0 + i;
+          bias[i] = col0 + i >= g.N ? -INFINITY : a.bias ? AGN_LD(a.bias + c) : 0.f;
+        }
+        __syncwarp();
+      }
+      ok = ok && tc::wait_mbar<true>(&acc_full[buf], (done >> 1) & 1, abort_flag, a.wait_ns) && !*abort_flag;
+      ok = __all_sync(0xffffffffu, ok);
+      tc::tc_fence_after();
+      if (!ok && lane == 0) {
+        stop_all();
+        if (a.err) atomicExch(a.err, 1);
+      }
+      float top = -INFINITY, sum = 0.f;
+      const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + buf * acc_cols + half * 32 * chunks;
+#pragma unroll 1
+      for (int ch = 0; ch < chunks; ++ch) {
+        const int col = col0 + 32 * ch;   // (of this product)
+        float v[32];
+        if (ok) {
+          uint32_t r[32];
+          tc::tmem_ld_32x32b_x32(acc + 32 * ch, r);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+          if (a.products > 1) {
+            tc::tmem_ld_32x32b_x32(acc + a.bn + 32 * ch, r);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r[i]);
+          }
+          if (t.kt == 0) {   // nothing was summed
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fc00000u);
+        }
+        if (ch + 1 == chunks && ok) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive_relaxed(empty0 + 8u * (uint32_t)buf);
+        }
+        if (kEpi != kOut) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(bias + 32 * ch + i);
+            v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+          }
+        }
+        const uint32_t hit = (uint32_t)(label - 32 * ch);   // < 32: the label's column is here
+        if (kEpi == kLse) {
+          if (hit < 32) {
+            float z = v[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) z = hit == i ? v[i] : z;
+            AGN_ST(a.zlab + row, z);
+          }
+          float most = top;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]);
+          const float from = most == -INFINITY ? 0.f : most;
+          float s0 = sum * exp2f((top - from) * kLog2e), s1 = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            s0 += exp2f((v[i] - from) * kLog2e);
+            s1 += exp2f((v[i + 1] - from) * kLog2e);
+          }
+          sum = s0 + s1;
+          top = most;
+        } else if (kEpi == kGrad) {
+          const bool dead = !live || lse == -INFINITY;   // (no class that is not masked: no gradient)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float p = fa * exp2f((v[i] - lse) * kLog2e);
+            if (hit == i) p -= fb;
+            v[i] = dead ? 0.f : p;
+          }
+          for (int q = 0; q < (a.products > 1 ? 3 : 1); ++q) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              if (q == 0) {
+                w[i] = pack2(v[2 * i], v[2 * i + 1]);
+              } else {   // what the pieces before left
+                float x[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  bf16 p0, p1, p2;
+                  split3(v[2 * i + k], p0, p1, p2);
+                  x[k] = __bfloat162float(q == 1 ? p1 : p2);
+                }
+                w[i] = pack2(x[0], x[1]);
+              }
+            }
+            out.put_bf16(w, col, q * a.p_plane + row0);
+          }
+          if (a.db && row0 < g.M) {
+            const float s = column_sums(v, lane);
+            if (col + lane < g.N) AGN_ST(a.db + (int64_t)(row0 >> 5) * a.ld_db + col + lane, s);
+          }
+        } else {
+          if (row0 >= g.M || col >= g.N) continue;   // (warp-uniform)
+          if (a.part) {
+            out.put_fp32(v, col, t.split * a.part_rows + row0, a.part == 2);
+          } else if (a.tma_out && !(a.scatter && g.gathered)) {
+            if (a.dtype == AGN_PREC_BF16) {
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+              out.put_bf16(w, col, row0);
+            } else {
+              out.put_fp32(v, col, row0, false);
+            }
+          } else {
+            const int n = min(32, g.M - row0), cols = min(32, g.N - col);
+            const int64_t place = live ? (a.scatter ? AGN_LD(a.idx + row) : row) : 0;
+            const int64_t at = place * a.ldo + col;
+            if (a.dtype == AGN_PREC_BF16) out.put_rows(v, static_cast<bf16*>(a.out), at, n, cols);
+            else out.put_rows(v, static_cast<float*>(a.out), at, n, cols);
+          }
+        }
+      }
+      if (kEpi == kLse && live)
+        AGN_ST(a.ms + (int64_t)(2 * t.n + half) * a.rows_pad + row, make_float2(top, sum));
+    }
+    if (kEpi != kLse && lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
+  }
+  __syncwarp();
+  tc::tc_fence_before();
+  __syncthreads();
+  if (kCtas == 2) cluster_sync();   // no CTA leaves while the other reads its memory or signals its barriers
+  if (__builtin_expect(*abort_flag, 0)) {   // (the same in both CTAs: nobody is left who could set it)
+    if (warp == 1 && lane == 0) {
+      if (cta == 0) {
+        commit(drained);   // (the thread that issued the MMAs)
+        tc::mbar_wait_bounded(drained, 0, kWaitNs);
+        land<kCtas>(full, loaded_out, stages, stage);
+      } else {
+        tc::mbar_wait_bounded(drained, 0, kWaitNs);
+      }
+    }
+    __syncthreads();
+    if (kCtas == 2) cluster_sync();
+  }
+  if (warp == 2) {
+    if (kCtas == 2) tc::tmem_dealloc_pair(tmem, 512);
+    else tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int kCtas, int kEpi>
+Status launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& talt, const CUtensorMap& tc,
+              const GemmArgs& a, int max_units, cudaStream_t st) {
+  struct Tag {};
+  auto kern = ce_gemm_kernel<kCtas, kEpi>;
+  int dev = 0, sms = 0;
+  AGN_TRY(current_device(&dev));
+  AGN_TRY(device_sms(dev, &sms));
+  AGN_TRY_CUDA(allow_smem<Tag>(kern, kSmem, dev));
+  const int groups = std::max(1, std::min(max_units, sms / kCtas));
+  if (kCtas == 2)
+    AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * groups)), dim3(kThreads), kSmem, dim3(2, 1, 1), st,
+                                    ta, tb, talt, tc, a));
+  else
+    AGN_TRY_CUDA(launch_pdl(kern, dim3((unsigned)groups), dim3(kThreads), kSmem, st, ta, tb, talt, tc, a));
+  return Status::Ok();
+}
+
+}  // namespace
+
+Status gemm(int ctas, int epilogue, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt,
+            const CUtensorMap& c, const GemmArgs& args, int max_units, cudaStream_t st) {
+  GemmArgs g = args;
+  if (!g.wait_ns) g.wait_ns = (uint32_t)kWaitNs;
+  if (ctas == 2) {
+    if (epilogue == kLse) return launch<2, kLse>(a, b, alt, c, g, max_units, st);
+    if (epilogue == kGrad) return launch<2, kGrad>(a, b, alt, c, g, max_units, st);
+    return launch<2, kOut>(a, b, alt, c, g, max_units, st);
+  }
+  if (epilogue == kLse) return launch<1, kLse>(a, b, alt, c, g, max_units, st);
+  if (epilogue == kGrad) return launch<1, kGrad>(a, b, alt, c, g, max_units, st);
+  return launch<1, kOut>(a, b, alt, c, g, max_units, st);
+}
+
+}  // namespace ce
+
+AGN_BOUNDS_UNIT(linear_ce_gemm)
+
+}  // namespace agn
