@@ -33,51 +33,80 @@ struct Sizes {
   int prec;
 };
 
-// How a product is cut.
+// How one or two products of a launch are cut.
 struct Cut {
   int ctas, bn;
-  int64_t tiles;
+  int64_t tiles[2];
+  int splits[2];
+};
+struct Extents {
+  int64_t M, N, K;
 };
 
-Cut cut(int64_t M, int64_t N, int planes, bool b_mn) {
-  Cut c;
-  c.ctas = M > 128 ? 2 : 1;
-  const int64_t tm = ceil_div(M, 128 * c.ctas);
-  const int64_t at_once = kSms / c.ctas;
-  const int most = planes > 1 || c.ctas == 1 ? 128 : 256, least = b_mn && c.ctas == 2 ? 128 : 64;
-  // the fewest rounds of tiles by their cost: a narrower tile does less work a byte
-  double best = 0;
-  for (int bn = most; bn >= least; bn /= 2) {
-    const double rounds = (double)ceil_div(tm * ceil_div(N, bn), at_once);
-    const double cost = rounds * (bn + (bn == 256 ? 0 : 16));
-    if (bn == most || cost < best) {
-      best = cost;
-      c.bn = bn;
-    }
-  }
-  c.tiles = tm * ceil_div(N, c.bn);
-  return c;
+// Clocks of a tile's 64 k: the MMAs at 4096 multiply-adds a clock and SM, or its operands at 64 bytes a
+// clock from the L2 (fp32: six products of three pieces each).
+double step_clocks(int ctas, int bn, int planes, int64_t a_box) {
+  const double mma = bn * 2.0 * (planes == 3 ? 6 : 1), load = (a_box * 128 + bn / ctas * 128) / 64.0 * planes;
+  return std::max(mma, load);
 }
 
-int cut_k(const Cut& c, int64_t M, int64_t N, int64_t K, int products) {
-  const int64_t free = kSms / c.ctas / std::max<int64_t>(1, c.tiles);
-  const int64_t steps = ceil_div(K, 64) * products;
-  int64_t s = std::min<int64_t>({free, steps / 16, ceil_div(K, 64), 64});
-  const int64_t bytes = round_up(M, 256) * round_up(N, 256) * 4;
-  s = std::min(s, kPartBytes / bytes);
-  return (int)std::max<int64_t>(1, s);
+// Tile width by the estimated time: rounds of tiles over the SMs, or B's bytes from memory (24 a clock and
+// SM) if that is more.  Of products cut along K also the ranges: as many as even out the work, where
+// that saves more than the pass over their sums costs.
+Cut cut(int ctas, int planes, bool b_mn, int a_box, const Extents* e, int n, bool ranges) {
+  Cut best{};
+  double best_time = 0;
+  const int64_t at_once = kSms / ctas;
+  const int least = b_mn && ctas == 2 ? 128 : 64;
+  for (int bn = planes > 1 ? 128 : 256; bn >= least; bn /= 2) {
+    Cut c{};
+    c.ctas = ctas;
+    c.bn = bn;
+    const double step = step_clocks(ctas, bn, planes, a_box);
+    double steps = 0, bytes = 0;
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) {
+      c.tiles[i] = ceil_div(e[i].M, 128 * ctas) * ceil_div(e[i].N, bn);
+      c.splits[i] = 1;
+      tiles += c.tiles[i];
+      steps += (double)c.tiles[i] * ceil_div(e[i].K, 64);
+      bytes += (double)ceil_div(e[i].N, bn) * bn * ceil_div(e[i].K, 64) * 128 * planes;
+    }
+    const double share = std::max(1.0, steps / at_once);   // of a CTA
+    double longest = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t kt = ceil_div(e[i].K, 64);
+      if (ranges && (kt - share) * step > 12000) {
+        const int64_t sums = round_up(e[i].M, 256) * round_up(e[i].N, 64) * 4;
+        const int64_t s = std::min({(int64_t)std::ceil(kt / std::max(share, 4000 / step)), kPartBytes / sums, (int64_t)64});
+        c.splits[i] = (int)std::max<int64_t>(1, s);
+      }
+      longest = std::max(longest, (double)ceil_div(kt, c.splits[i]));
+    }
+    const double rounds = n == 1 && c.splits[0] == 1 ? (double)ceil_div(tiles, at_once) * ceil_div(e[0].K, 64)
+                                                     : std::max(share, longest);
+    const double time = std::max(rounds * step, bytes / (24.0 * kSms)) + 1500.0 * tiles / at_once;
+    if (best.bn == 0 || time < best_time) {
+      best = c;
+      best_time = time;
+    }
+  }
+  return best;
 }
 
 bool small(const Sizes& s) { return s.rows <= 512 && s.inner * s.classes <= 32768 && s.classes <= 2048; }
 
 struct Layout {
-  int planes, products;
-  int64_t kp;              // x's and w's row stride where they are packed
+  int planes;
+  int64_t kp;              // x's and w's row stride where they are packed (whole 128 bytes)
   bool direct;             // bf16 rows that the copy engine reads as they are
   int64_t rows_pad, piece; // classes of a piece (a multiple of 256, but for one piece of all)
   int64_t pieces, ldp;     // p's row stride
-  Cut z, dx, dw;
-  int dx_splits, dw_splits;
+  Cut z;
+  int a_box;               // rows of x in a box of the logits' product
+  bool both;               // dw and dx are one launch
+  Cut grads[2];            // dw, dx (both: the first alone, with two products)
+  int dw_splits, dx_splits;
   bool dx_part;
   int64_t halves;          // forward: partial (maximum, sum) of a row
   size_t idx, live, x, w, ms, zlab, p, db, dxs, dws, bytes;
@@ -86,8 +115,7 @@ struct Layout {
 Layout layout(const Sizes& s, bool backward) {
   Layout l{};
   l.planes = s.prec == AGN_PREC_FP32 ? 3 : 1;
-  l.products = l.planes == 3 ? 6 : 1;
-  l.kp = round_up(s.inner, 8);
+  l.kp = round_up(s.inner, 64);
   l.direct = l.planes == 1 && s.inner % 8 == 0;
   l.rows_pad = round_up(s.rows, 256);
   size_t at = 0;
@@ -109,7 +137,9 @@ Layout layout(const Sizes& s, bool backward) {
   l.piece = most;
   l.pieces = ceil_div(s.classes, l.piece);
   l.ldp = round_up(l.piece, 64);
-  l.z = cut(s.rows, l.piece, l.planes, false);
+  l.a_box = (int)std::min<int64_t>(128, round_up(s.rows, 8));
+  const Extents ez{s.rows, l.piece, s.inner};
+  l.z = cut(s.rows > 128 ? 2 : 1, l.planes, false, l.a_box, &ez, 1, false);
   l.live = take(4);
   l.idx = take((size_t)l.rows_pad * 4);
   l.x = take((size_t)l.planes * l.rows_pad * l.kp * 2);
@@ -122,12 +152,15 @@ Layout layout(const Sizes& s, bool backward) {
   } else {
     l.p = take((size_t)l.planes * l.rows_pad * l.ldp * 2);
     l.db = take((size_t)(l.rows_pad / 32) * l.ldp * 4);
-    l.dx = cut(s.rows, s.inner, l.planes, true);
-    l.dx_splits = cut_k(l.dx, s.rows, s.inner, l.piece, l.products);
+    const Extents e[2] = {{l.piece, s.inner, s.rows}, {s.rows, s.inner, l.piece}};   // dw, dx
+    const int dw_ctas = l.piece > 128 ? 2 : 1, dx_ctas = l.z.ctas;
+    l.both = dw_ctas == dx_ctas;
+    l.grads[0] = cut(dw_ctas, l.planes, true, 128, e, l.both ? 2 : 1, true);
+    if (!l.both) l.grads[1] = cut(dx_ctas, l.planes, true, 128, e + 1, 1, true);
+    l.dw_splits = l.grads[0].splits[0];
+    l.dx_splits = l.both ? l.grads[0].splits[1] : l.grads[1].splits[0];
     l.dx_part = l.pieces > 1 || l.dx_splits > 1;
     if (l.dx_part) l.dxs = take((size_t)l.dx_splits * l.rows_pad * round_up(s.inner, 64) * 4);
-    l.dw = cut(l.piece, s.inner, l.planes, true);
-    l.dw_splits = cut_k(l.dw, l.piece, s.inner, s.rows, l.products);
     if (l.dw_splits > 1)
       l.dws = take((size_t)l.dw_splits * round_up(l.piece, 256) * round_up(s.inner, 64) * 4);
   }
@@ -187,96 +220,186 @@ __global__ void __launch_bounds__(1024) rows_kernel(const int* labels, int rows,
   if (threadIdx.x == 0) AGN_ST(live, base);
 }
 
-// Rows of src as bf16 (fp32: three pieces) with zeros up to the stride, eight columns a thread.  idx
-// (x): the rows with a label, then zeros up to a multiple of 64 rows; nothing where the copy engine
-// reads src itself (direct) and no row is missing.  dx: its rows without a label are zeroed.
+// Eight columns from c on of a row of `inner` elements (null: zeros) to dst, as bf16 or three pieces.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
-pack_kernel(const T* src, int64_t rows, int inner, const int* idx, const int* live_p, bool direct, bf16* dst,
-            int64_t ld, int64_t plane, const int* labels, int classes, T* dx) {
-  pdl_begin();
-  const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
-  const int groups = (int)(ld / 8);
-  int64_t live = rows, out_rows = rows;
-  if (idx) {
-    live = AGN_LD(live_p);
-    out_rows = (live + 63) / 64 * 64;
-    if (live < rows && dx) {
-      for (int64_t i = first; i < rows * groups; i += step) {
-        const int64_t r = i / groups;
-        if (has_label(AGN_LD(labels + r), classes)) continue;
-        const int c = (int)(i - r * groups) * 8;
-        for (int k = c; k < min(c + 8, inner); ++k) from_float(dx + r * inner + k, 0.f);
-      }
+__device__ __forceinline__ void pack8(const T* row, int inner, int c, bf16* dst, int64_t plane) {
+  float v[8];
+  if (row && inner % 8 == 0 && c < inner) {   // (rows are 16-byte aligned then)
+    constexpr int n = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int j = 0; j < 8 / n; ++j) {
+      const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(row + c) + j);
+      const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+      for (int k = 0; k < n; ++k) v[j * n + k] = to_float(e[k]);
     }
-    if (direct && live == rows) return;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = row && c + k < inner ? to_float(AGN_LD(row + c + k)) : 0.f;
   }
-  const bool vec = inner % 8 == 0;   // (src is 16-byte aligned)
-  for (int64_t i = first; i < out_rows * groups; i += step) {
+  bf16 q[3][8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (sizeof(T) == 4) split3(v[k], q[0][k], q[1][k], q[2][k]);
+    else q[0][k] = __float2bfloat16_rn(v[k]);
+  }
+#pragma unroll
+  for (int j = 0; j < (sizeof(T) == 4 ? 3 : 1); ++j)
+    AGN_ST(reinterpret_cast<uint4*>(dst + j * plane + c), *reinterpret_cast<const uint4*>(q[j]));
+}
+
+// A matrix to be packed: rows with zeros up to the stride.
+template <typename T>
+struct Pack {
+  const T* src;
+  int64_t rows;
+  int inner;
+  bf16* dst;
+  int64_t ld, plane;
+};
+
+template <typename T>
+__device__ __forceinline__ void pack_rows(const Pack<T>& p, int64_t first, int64_t step) {
+  const int groups = (int)(p.ld / 8);
+  for (int64_t i = first; i < p.rows * groups; i += step) {
     const int64_t r = i / groups;
-    const int c = (int)(i - r * groups) * 8;
-    float v[8];
-    if (r >= live) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = 0.f;
-    } else {
-      const T* p = src + (idx ? (int64_t)AGN_LD(idx + r) : r) * inner + c;
-      if (vec) {
-        constexpr int n = 16 / (int)sizeof(T);
-#pragma unroll
-        for (int j = 0; j < 8 / n; ++j) {
-          const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(p) + j);
-          const T* e = reinterpret_cast<const T*>(&q);
-#pragma unroll
-          for (int k = 0; k < n; ++k) v[j * n + k] = to_float(e[k]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = c + k < inner ? to_float(AGN_LD(p + k)) : 0.f;
-      }
-    }
-    bf16 q[3][8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (sizeof(T) == 4) split3(v[k], q[0][k], q[1][k], q[2][k]);
-      else q[0][k] = __float2bfloat16_rn(v[k]);
-    }
-#pragma unroll
-    for (int j = 0; j < (sizeof(T) == 4 ? 3 : 1); ++j)
-      AGN_ST(reinterpret_cast<uint4*>(dst + j * plane + r * ld + c), *reinterpret_cast<const uint4*>(q[j]));
+    pack8(p.src + r * p.inner, p.inner, (int)(i - r * groups) * 8, p.dst + r * p.ld, p.plane);
   }
 }
 
-// lse and loss from the partial maxima and sums: 32 rows a block, its warps share a row's partials.
-__global__ void __launch_bounds__(1024)
-join_kernel(const float2* ms, int halves, int64_t rows_pad, const float* zlab, const int* labels, int classes,
-            int rows, const int* idx, const int* live_p, float* loss, float* lse) {
+template <typename T>
+__global__ void __launch_bounds__(kThreads) pack_kernel(const Pack<T> p) {
   pdl_begin();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  pack_rows(p, (int64_t)blockIdx.x * blockDim.x + threadIdx.x, (int64_t)gridDim.x * blockDim.x);
+}
+
+// x's rows with a label to consecutive rows (and zeros up to a multiple of 64 rows); nothing where the copy
+// engine reads x itself (direct) and no row is missing.  dx: its rows without a label are zeroed.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+gather_kernel(const Pack<T> x, bool direct, const int* idx, const int* live_p, const int* labels, int classes, T* dx) {
+  pdl_begin();
+  const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+  const int groups = (int)(x.ld / 8);
+  const int64_t live = AGN_LD(live_p), out_rows = (live + 63) / 64 * 64;
+  if (live < x.rows && dx) {
+    for (int64_t i = first; i < x.rows * x.inner; i += step)
+      if (!has_label(AGN_LD(labels + i / x.inner), classes)) from_float(dx + i, 0.f);
+  }
+  if (direct && live == x.rows) return;
+  for (int64_t i = first; i < out_rows * groups; i += step) {
+    const int64_t r = i / groups;
+    pack8(r < live ? x.src + (int64_t)AGN_LD(idx + r) * x.inner : nullptr, x.inner, (int)(i - r * groups) * 8,
+          x.dst + r * x.ld, x.plane);
+  }
+}
+
+// rows_kernel, gather_kernel and w's packing in one launch for up to kMostRows rows: a block has a range of
+// rows, and each counts all labels, so that none waits for another (16384 labels: 1 us).
+constexpr int kMostRows = 32768, kRangeRows = 256;
+template <typename T>
+__global__ void __launch_bounds__(1024)
+prepare_kernel(const Pack<T> x, const Pack<T> w, bool direct, int range, const int* labels, int classes, int* idx,
+               int* live_p, T* dx) {
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rows = (int)x.rows, r0 = min(rows, (int)blockIdx.x * range), r1 = min(rows, r0 + range);
+  __shared__ int counts[2][32];
+  __shared__ int list[kRangeRows], first_of[kRangeRows / 32];
+  __shared__ bool known[kRangeRows];
+  int all = 0, before = 0;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < rows; i += 1024) {
+    const int n = has_label(AGN_LD(labels + i), classes);
+    all += n;
+    before += i < r0 ? n : 0;
+  }
+  all = __reduce_add_sync(0xffffffffu, all);
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) counts[0][warp] = all, counts[1][warp] = before;
+  const int mine = r0 + (int)threadIdx.x;
+  bool has = false;
+  uint32_t ballot = 0;
+  if (warp < kRangeRows / 32) {
+    has = mine < r1 && has_label(AGN_LD(labels + mine), classes);
+    ballot = __ballot_sync(0xffffffffu, has);
+    if (lane == 0) first_of[warp] = __popc(ballot);
+    known[threadIdx.x] = has;
+  }
+  __syncthreads();
+  all = __reduce_add_sync(0xffffffffu, counts[0][lane]);
+  before = __reduce_add_sync(0xffffffffu, counts[1][lane]);
+  int n = 0;   // of this range
+#pragma unroll
+  for (int k = 0; k < kRangeRows / 32; ++k) {
+    if (k == warp && has) {
+      const int at = n + __popc(ballot & ((1u << lane) - 1));
+      list[at] = mine;
+      AGN_ST(idx + before + at, mine);
+    }
+    n += first_of[k];
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) AGN_ST(live_p, all);
+  __syncthreads();
+  const int groups = (int)(x.ld / 8);
+  if (!direct || all < rows) {
+    for (int i = threadIdx.x; i < n * groups; i += 1024) {
+      const int r = i / groups;
+      pack8(x.src + (int64_t)list[r] * x.inner, x.inner, (i - r * groups) * 8, x.dst + (int64_t)(before + r) * x.ld,
+            x.plane);
+    }
+    for (int r = all + blockIdx.x; r < (all + 63) / 64 * 64; r += gridDim.x)
+      for (int i = threadIdx.x; i < groups; i += 1024) pack8((const T*)nullptr, x.inner, i * 8, x.dst + (int64_t)r * x.ld, x.plane);
+  }
+  if (dx && all < rows) {
+    for (int i = threadIdx.x; i < (r1 - r0) * x.inner; i += 1024)
+      if (!known[i / x.inner]) from_float(dx + (int64_t)r0 * x.inner + i, 0.f);
+  }
+  if (w.src) pack_rows(w, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024);
+}
+
+// (maximum, sum of exponentials) of two sets of values.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;
+  return make_float2(most, a.y * exp2f((a.x - from) * kLog2e) + b.y * exp2f((b.x - from) * kLog2e));
+}
+
+// lse and loss from the partial maxima and sums: a warp a row, or where there are few rows a block.
+__global__ void __launch_bounds__(kThreads)
+join_kernel(const float2* ms, int halves, int64_t ld, int rows_a_block, const float* zlab, const int* labels,
+            int classes, int rows, const int* idx, const int* live_p, float* loss, float* lse) {
+  pdl_begin();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int live = AGN_LD(live_p);
-  const int row = blockIdx.x * 32 + lane;
-  __shared__ float2 part[32][32];
-  float m = -INFINITY, s = 0.f;
+  const int shared_by = kThreads / 32 / rows_a_block;   // warps of a row
+  const int row = blockIdx.x * rows_a_block + warp / shared_by, part = warp % shared_by;
+  float2 v = make_float2(-INFINITY, 0.f);
   if (row < live) {
-    for (int j = warp; j < halves; j += warps) {
-      const float2 v = AGN_LD(ms + (int64_t)j * rows_pad + row);
-      const float most = fmaxf(m, v.x), from = most == -INFINITY ? 0.f : most;
-      s = s * exp2f((m - from) * kLog2e) + v.y * exp2f((v.x - from) * kLog2e);
-      m = most;
+    const float2* p = ms + (int64_t)row * ld;
+    for (int j = part * 32 + lane; j < halves; j += 4 * 32 * shared_by) {
+      float2 q[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int at = j + k * 32 * shared_by;
+        q[k] = at < halves ? AGN_LD(p + at) : make_float2(-INFINITY, 0.f);
+      }
+      v = join(v, join(join(q[0], q[1]), join(q[2], q[3])));
     }
   }
-  part[warp][lane] = make_float2(m, s);
-  __syncthreads();
-  if (warp != 0) return;
-  for (int j = 1; j < warps; ++j) {
-    const float2 v = part[j][lane];
-    const float most = fmaxf(m, v.x), from = most == -INFINITY ? 0.f : most;
-    s = s * exp2f((m - from) * kLog2e) + v.y * exp2f((v.x - from) * kLog2e);
-    m = most;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+  if (shared_by > 1) {   // (the same for all: a block a row)
+    __shared__ float2 parts[kThreads / 32];
+    if (lane == 0) parts[warp] = v;
+    __syncthreads();
+    if (part != 0) return;
+    for (int j = 1; j < shared_by; ++j) v = join(v, parts[warp + j]);
   }
+  if (lane != 0) return;
   if (row < live) {
     const int at = AGN_LD(idx + row);
-    const float total = m == -INFINITY && s == 0.f ? -INFINITY : m + logf(s);
+    const float total = v.x == -INFINITY && v.y == 0.f ? -INFINITY : v.x + logf(v.y);
     AGN_ST(lse + at, total);
     AGN_ST(loss + at, total == -INFINITY ? INFINITY : total - AGN_LD(zlab + row));
   }
@@ -518,26 +641,39 @@ Status small_backward(const Call& c, const Layout& l, cudaStream_t st) {
              c.dbias);
 }
 
-// Rows of x that have a label: counted, and packed (or gathered where some are missing).
 template <typename T>
-Status prepare_rows(const Call& c, const Layout& l, cudaStream_t st) {
-  int* idx = reinterpret_cast<int*>(c.work + l.idx);
-  int* live = reinterpret_cast<int*>(c.work + l.live);
-  AGN_TRY(run(rows_kernel, dim3(1), 1024, 0, st, c.labels, (int)c.s.rows, (int)c.s.classes, idx, live));
-  return run(pack_kernel<T>, dim3(grid_for(l.rows_pad * (l.kp / 8), kThreads)), kThreads, 0, st,
-             static_cast<const T*>(c.x), c.s.rows, (int)c.s.inner, (const int*)idx, (const int*)live, l.direct,
-             reinterpret_cast<bf16*>(c.work + l.x), l.kp, l.rows_pad * l.kp, c.labels, (int)c.s.classes,
-             static_cast<T*>(c.dx));
+Pack<T> w_pack(const Call& c, const Layout& l, int64_t c0, int64_t n) {
+  return Pack<T>{static_cast<const T*>(c.w) + c0 * c.s.inner, n, (int)c.s.inner,
+                 reinterpret_cast<bf16*>(c.work + l.w), l.kp, l.piece * l.kp};
 }
 
 // Rows c0 .. c0 + n - 1 of w as bf16 rows or pieces, where they are not read as they are.
 template <typename T>
 Status prepare_w(const Call& c, const Layout& l, int64_t c0, int64_t n, cudaStream_t st) {
   if (l.direct) return Status::Ok();
-  return run(pack_kernel<T>, dim3(grid_for(n * (l.kp / 8), kThreads)), kThreads, 0, st,
-             static_cast<const T*>(c.w) + c0 * c.s.inner, n, (int)c.s.inner, (const int*)nullptr,
-             (const int*)nullptr, false, reinterpret_cast<bf16*>(c.work + l.w), l.kp, l.piece * l.kp,
-             (const int*)nullptr, 0, (T*)nullptr);
+  return run(pack_kernel<T>, dim3(grid_for(n * (l.kp / 8), kThreads)), kThreads, 0, st, w_pack<T>(c, l, c0, n));
+}
+
+// Rows of x that have a label: counted, and packed (or gathered where some are missing); the first piece
+// of w.
+template <typename T>
+Status prepare(const Call& c, const Layout& l, cudaStream_t st) {
+  int* idx = reinterpret_cast<int*>(c.work + l.idx);
+  int* live = reinterpret_cast<int*>(c.work + l.live);
+  const Pack<T> x{static_cast<const T*>(c.x), c.s.rows, (int)c.s.inner, reinterpret_cast<bf16*>(c.work + l.x), l.kp,
+                  l.rows_pad * l.kp};
+  const int64_t n = std::min(l.piece, c.s.classes);
+  if (c.s.rows <= kMostRows) {
+    const Pack<T> w = l.direct ? Pack<T>{} : w_pack<T>(c, l, 0, n);
+    const int64_t items = (l.direct ? 0 : n * l.kp / 8192) + ceil_div(c.s.rows, 4);
+    const int64_t grid = std::max(std::min<int64_t>(kSms, items), ceil_div(c.s.rows, kRangeRows));
+    return run(prepare_kernel<T>, dim3((unsigned)grid), 1024, 0, st, x, w, l.direct, (int)ceil_div(c.s.rows, grid),
+               c.labels, (int)c.s.classes, idx, live, static_cast<T*>(c.dx));
+  }
+  AGN_TRY(run(rows_kernel, dim3(1), 1024, 0, st, c.labels, (int)c.s.rows, (int)c.s.classes, idx, live));
+  AGN_TRY(run(gather_kernel<T>, dim3(grid_for(l.rows_pad * (l.kp / 8), kThreads)), kThreads, 0, st, x, l.direct,
+              (const int*)idx, (const int*)live, c.labels, (int)c.s.classes, static_cast<T*>(c.dx)));
+  return prepare_w<T>(c, l, 0, n, st);
 }
 
 // x as an operand: as it is and gathered, or packed alone.
@@ -565,7 +701,8 @@ GemmArgs common_args(const Call& c, const Layout& l) {
   a.live = reinterpret_cast<const int*>(c.work + l.live);
   a.idx = reinterpret_cast<const int*>(c.work + l.idx);
   a.rows = (int)c.s.rows;
-  a.products = l.products;
+  a.planes = l.planes;
+  a.a_box = 128;
   a.splits = 1;
   a.err = c.err;
   a.wait_ns = (uint32_t)c.wait_ns;
@@ -576,38 +713,45 @@ GemmArgs common_args(const Call& c, const Layout& l) {
 // The product of the logits of classes c0 .. c0 + n - 1.
 GemmArgs logit_args(const Call& c, const Layout& l, int64_t c0, int64_t n) {
   GemmArgs a = common_args(c, l);
-  a.M = (int)c.s.rows; a.N = (int)n; a.K = (int)l.kp;
+  a.M = (int)c.s.rows; a.N = (int)n; a.K = (int)c.s.inner;
   a.alt = l.direct ? 1 : 0;
   a.bn = l.z.bn;
+  a.a_box = l.a_box;
   a.bias = c.bias;
   a.labels = c.labels;
   a.class0 = (int)c0; a.classes = (int)c.s.classes;
-  a.rows_pad = l.rows_pad;
   return a;
+}
+
+int64_t logit_units(const Call& c, const Layout& l, int64_t n) {
+  return ceil_div(c.s.rows, 128 * l.z.ctas) * ceil_div(n, l.z.bn);
 }
 
 template <typename T>
 Status forward(const Call& c, const Layout& l, cudaStream_t st) {
-  AGN_TRY(prepare_rows<T>(c, l, st));
+  AGN_TRY(prepare<T>(c, l, st));
   float2* ms = reinterpret_cast<float2*>(c.work + l.ms);
   float* zlab = reinterpret_cast<float*>(c.work + l.zlab);
-  CUtensorMap tx, txa, tw;
-  AGN_TRY(x_maps(c, l, 64, 128, &tx, &txa));
-  const int64_t tm = ceil_div(c.s.rows, 128 * l.z.ctas);
+  GemmLaunch g{};
+  g.n = 1;
+  GemmMaps& maps = g.maps[0];
+  AGN_TRY(x_maps(c, l, 64, l.a_box, &maps.a, &maps.alt));
   int64_t half = 0;
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
-    AGN_TRY(prepare_w<T>(c, l, c0, n, st));
-    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &tw));
-    GemmArgs a = logit_args(c, l, c0, n);
-    a.ms = ms + half * l.rows_pad;
-    a.zlab = zlab;
-    AGN_TRY(gemm(l.z.ctas, kLse, tx, tw, txa, tx, a, (int)std::min<int64_t>(INT32_MAX, tm * ceil_div(n, l.z.bn)), st));
+    if (c0 > 0) AGN_TRY(prepare_w<T>(c, l, c0, n, st));
+    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &maps.b));
+    g.args[0] = logit_args(c, l, c0, n);
+    g.args[0].ms = ms;
+    g.args[0].ld_ms = l.halves;
+    g.args[0].ms0 = (int)half;
+    g.args[0].zlab = zlab;
+    AGN_TRY(gemm(l.z.ctas, kLse, g, logit_units(c, l, n), st));
     half += 2 * ceil_div(n, l.z.bn);
   }
-  const int warps = (int)std::min<int64_t>(32, std::max<int64_t>(1, half / 4));
-  return run(join_kernel, dim3((unsigned)ceil_div(c.s.rows, 32)), 32 * warps, 0, st, (const float2*)ms, (int)half,
-             l.rows_pad, (const float*)zlab, c.labels, (int)c.s.classes, (int)c.s.rows,
+  const int rows_a_block = c.s.rows >= 4 * kSms || half <= 64 ? 8 : 1;
+  return run(join_kernel, dim3((unsigned)ceil_div(c.s.rows, rows_a_block)), kThreads, 0, st, (const float2*)ms,
+             (int)half, l.halves, rows_a_block, (const float*)zlab, c.labels, (int)c.s.classes, (int)c.s.rows,
              (const int*)(c.work + l.idx), (const int*)(c.work + l.live), c.loss, c.lse_out);
 }
 
@@ -625,80 +769,88 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
   const int64_t rows = c.s.rows, inner = c.s.inner;
   const int* idx = reinterpret_cast<const int*>(c.work + l.idx);
   const int* live = reinterpret_cast<const int*>(c.work + l.live);
-  AGN_TRY(prepare_rows<T>(c, l, st));
+  AGN_TRY(prepare<T>(c, l, st));
   bf16* p = reinterpret_cast<bf16*>(c.work + l.p);
   float* db = reinterpret_cast<float*>(c.work + l.db);
   const int64_t p_plane = l.rows_pad * l.ldp, ldn = round_up(inner, 64), dw_rows = round_up(l.piece, 256);
-  CUtensorMap tx, txa, txm, txma, tp_store, tp_k, tp_m, tc;
-  AGN_TRY(x_maps(c, l, 64, 128, &tx, &txa));
-  AGN_TRY(x_maps(c, l, 64, 64, &txm, &txma));
-  AGN_TRY(make_tmap_store_2d(&tp_store, p, 2, l.ldp, l.planes * l.rows_pad, l.ldp, 32, 32));
-  AGN_TRY(make_tmap_bf16_3d(&tp_k, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 128));
-  AGN_TRY(make_tmap_bf16_3d(&tp_m, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 64));
+  GemmLaunch z{}, dw{}, dx{};
+  z.n = dw.n = dx.n = 1;
+  AGN_TRY(x_maps(c, l, 64, l.a_box, &z.maps[0].a, &z.maps[0].alt));
+  AGN_TRY(make_tmap_store_2d(&z.maps[0].c, p, 2, l.ldp, l.planes * l.rows_pad, l.ldp, 32, 32));
+  AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].a, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 64));
+  AGN_TRY(x_maps(c, l, 64, 64, &dw.maps[0].b, &dw.maps[0].alt));
+  AGN_TRY(make_tmap_bf16_3d(&dx.maps[0].a, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 128));
   const bool rows16 = inner * es % 16 == 0;
+  const Cut &cw = l.grads[0], &cx = l.both ? l.grads[0] : l.grads[1];
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
-    AGN_TRY(prepare_w<T>(c, l, c0, n, st));
-    CUtensorMap tw;
-    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &tw));
-    GemmArgs a = logit_args(c, l, c0, n);
+    if (c0 > 0) AGN_TRY(prepare_w<T>(c, l, c0, n, st));
+    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &z.maps[0].b));
+    GemmArgs& a = z.args[0];
+    a = logit_args(c, l, c0, n);
     a.lse = c.lse; a.dloss = c.dloss; a.dlse = c.dlse; a.scale = c.scale;
     a.p_plane = (int)l.rows_pad;
     a.db = c.dbias ? db : nullptr;
     a.ld_db = l.ldp;
-    AGN_TRY(gemm(l.z.ctas, kGrad, tx, tw, txa, tp_store, a,
-                 (int)(ceil_div(rows, 128 * l.z.ctas) * ceil_div(n, l.z.bn)), st));
+    AGN_TRY(gemm(l.z.ctas, kGrad, z, logit_units(c, l, n), st));
     if (c.dbias)
       AGN_TRY(run(columns_kernel, dim3((unsigned)ceil_div(n, 32)),
                   32 * (int)std::min<int64_t>(32, l.rows_pad / 128), 0, st, (const float*)db, l.ldp, (int)n, live,
                   c.dbias + c0));
+    T* dw_out = static_cast<T*>(c.dw) + c0 * inner;
+    int64_t dw_units = 0, dx_units = 0;
     if (c.dw) {   // [n][inner] = p^T x
-      T* dw = static_cast<T*>(c.dw) + c0 * inner;
-      GemmArgs d = common_args(c, l);
+      GemmArgs& d = dw.args[0];
+      d = common_args(c, l);
       d.M = (int)n; d.N = (int)inner; d.K = (int)rows;
       d.live_is = 1;
       d.alt = l.direct ? 2 : 0;
-      d.bn = l.dw.bn;
+      d.bn = cw.bn;
       d.a_mn = d.b_mn = 1;
       d.splits = l.dw_splits;
-      d.out = dw; d.ldo = inner; d.dtype = c.s.prec;
-      tc = tp_store;   // (not read)
+      d.out = dw_out; d.ldo = inner; d.dtype = c.s.prec;
       if (l.dw_splits > 1) {
         d.part = 1;
         d.part_rows = (int)dw_rows;
-        AGN_TRY(make_tmap_store_2d(&tc, c.work + l.dws, 4, ldn, l.dw_splits * dw_rows, ldn, 32, 32));
+        AGN_TRY(make_tmap_store_2d(&dw.maps[0].c, c.work + l.dws, 4, ldn, l.dw_splits * dw_rows, ldn, 32, 32));
       } else if (rows16) {
         d.tma_out = 1;
-        AGN_TRY(make_tmap_store_2d(&tc, dw, es, inner, n, inner, 32, 32));
+        AGN_TRY(make_tmap_store_2d(&dw.maps[0].c, dw_out, es, inner, n, inner, 32, 32));
       }
-      const int64_t tiles = ceil_div(n, 128 * l.dw.ctas) * ceil_div(inner, l.dw.bn);
-      AGN_TRY(gemm(l.dw.ctas, kOut, tp_m, txm, txma, tc, d, (int)(tiles * d.splits), st));
-      if (l.dw_splits > 1)
-        AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dws), l.dw_splits, dw_rows * ldn, ldn, n,
-                           inner, (const int*)nullptr, (const int*)nullptr, dw, st));
+      dw_units = ceil_div(n, 128 * cw.ctas) * ceil_div(inner, cw.bn) * d.splits;
     }
     if (c.dx) {   // [rows][inner] += p w
-      GemmArgs d = common_args(c, l);
+      GemmArgs& d = dx.args[0];
+      d = common_args(c, l);
       d.M = (int)rows; d.N = (int)inner; d.K = (int)n;
-      d.bn = l.dx.bn;
+      d.bn = cx.bn;
       d.b_mn = 1;
       d.splits = l.dx_splits;
       d.out = c.dx; d.ldo = inner; d.dtype = c.s.prec;
       d.scatter = 1;
-      CUtensorMap twm;
-      AGN_TRY(w_map(c, l, c0, n, 64, 64, &twm));
-      tc = tp_store;
+      AGN_TRY(w_map(c, l, c0, n, 64, 64, &dx.maps[0].b));
       if (l.dx_part) {
         d.part = c0 == 0 ? 1 : 2;
         d.part_rows = (int)l.rows_pad;
-        AGN_TRY(make_tmap_store_2d(&tc, c.work + l.dxs, 4, ldn, l.dx_splits * l.rows_pad, ldn, 32, 32));
+        AGN_TRY(make_tmap_store_2d(&dx.maps[0].c, c.work + l.dxs, 4, ldn, l.dx_splits * l.rows_pad, ldn, 32, 32));
       } else if (rows16) {
         d.tma_out = 1;
-        AGN_TRY(make_tmap_store_2d(&tc, c.dx, es, inner, rows, inner, 32, 32));
+        AGN_TRY(make_tmap_store_2d(&dx.maps[0].c, c.dx, es, inner, rows, inner, 32, 32));
       }
-      const int64_t tiles = ceil_div(rows, 128 * l.dx.ctas) * ceil_div(inner, l.dx.bn);
-      AGN_TRY(gemm(l.dx.ctas, kOut, tp_k, twm, twm, tc, d, (int)(tiles * d.splits), st));
+      dx_units = ceil_div(rows, 128 * cx.ctas) * ceil_div(inner, cx.bn) * d.splits;
     }
+    if (c.dw && c.dx && l.both) {
+      dw.n = 2;
+      dw.maps[1] = dx.maps[0];
+      dw.args[1] = dx.args[0];
+      AGN_TRY(gemm(cw.ctas, kOut, dw, dw_units + dx_units, st));
+    } else {
+      if (c.dw) AGN_TRY(gemm(cw.ctas, kOut, dw, dw_units, st));
+      if (c.dx) AGN_TRY(gemm(cx.ctas, kOut, dx, dx_units, st));
+    }
+    if (c.dw && l.dw_splits > 1)
+      AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dws), l.dw_splits, dw_rows * ldn, ldn, n, inner,
+                         (const int*)nullptr, (const int*)nullptr, dw_out, st));
   }
   if (c.dx && l.dx_part)
     AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dxs), l.dx_splits, l.rows_pad * ldn, ldn, rows,

@@ -26,7 +26,8 @@ struct GemmArgs {
   int bn;                   // columns of a tile
   int a_mn, b_mn;           // operand stored [K][M] ([K][N]) instead
   int b_k0, b_n0;           // where B's rows of this product start along K, along N
-  int products;             // 1, or 6 of three bf16 pieces (planes)
+  int planes;               // 1, or 3 bf16 pieces of fp32 operands: six products
+  int a_box;                // rows of A's boxes (128, fewer where M is less; its box is 64 along M with a_mn)
   int splits;               // ranges along K, each with sums of its own (kOut)
   int* err;
   uint32_t wait_ns;
@@ -36,8 +37,9 @@ struct GemmArgs {
   const float* bias;        // [classes] or null
   const int* labels;        // [rows]
   int class0, classes;      // first class of this product, classes in all
-  float2* ms;               // kLse: [2 N / bn][rows_pad] (maximum, sum)
-  int64_t rows_pad;
+  float2* ms;               // kLse: [rows_pad][ld_ms], from column ms0 on 2 N / bn (maximum, sum)
+  int64_t ld_ms;
+  int ms0;
   float* zlab;              // kLse: [rows_pad] the label's logit
   const float *lse, *dloss, *dlse;   // kGrad, by place
   float scale;
@@ -54,9 +56,19 @@ struct GemmArgs {
   int part_rows;
 };
 
-// ctas: 1 or 2 (pairs).  Queues the launch on the current device.
-Status gemm(int ctas, int epilogue, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt,
-            const CUtensorMap& c, const GemmArgs& args, int max_units, cudaStream_t st);
+struct GemmMaps {
+  CUtensorMap a, b, alt, c;
+};
+
+// A launch: one product, or (kOut) two with the same bn, planes and a_box, whose tiles one grid shares.
+struct GemmLaunch {
+  GemmMaps maps[2];
+  GemmArgs args[2];
+  int n;
+};
+
+// ctas: 1 or 2 (pairs); max_units: tiles times ranges along K, at most.  On the current device.
+Status gemm(int ctas, int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st);
 
 }  // namespace ce
 }  // namespace agn

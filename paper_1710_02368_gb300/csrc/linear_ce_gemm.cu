@@ -5,7 +5,9 @@
 //   dx = p w and dw = p^T x (kOut): operands stored the other way round are read so (the MMA
 //     takes either major), nothing is transposed in memory.
 // fp32 operands are three exact bf16 pieces (planes): six products of pieces, the first in one
-// accumulator and the five smaller ones in another.
+// accumulator and the five smaller ones in another.  The tensor cores cut what they add to an
+// accumulator off below its last bit, always towards zero, so these sums are taken over 256 k at
+// a time and added in registers, rounded (one accumulator over K = 50000: 1.5e-5 of dx off).
 // One CTA a tile of 128 rows, or a pair (cta_group::2) a tile of 256, each CTA loading its 128 rows
 // of A and half of B's: 64 bytes a clock of MMA time instead of 96 with 256 columns.  Persistent:
 // a CTA (pair) walks over tiles in bands of eight along M, so that what runs at a time shares operands
@@ -25,10 +27,10 @@ namespace {
 constexpr int kThreads = 384;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int kBK = 64;                   // k of a stage: 128-byte rows
-constexpr int kABytes = 128 * 128;        // 128 rows (or columns) of a stage
 constexpr int kBox = 64 * 128;            // an operand stored along M or N: boxes of 64 x 64 k
-constexpr int kRing = 160 * 1024;
-constexpr int kMaxStages = 8;
+constexpr int kRing = 176 * 1024;
+constexpr int kMaxStages = 16;
+constexpr int kPartK = 4;                 // fp32: stages' k of a sum in TMEM
 constexpr int kStaged = 4096;             // a finishing warp's tile of outputs
 constexpr size_t kSmem = 1024 + kRing + 8 * (kStaged + 512) + 512;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -71,10 +73,6 @@ struct Unit {
     kt = min(g.KT, kt0 + g.kt_per) - kt0;
   }
 };
-
-// Pieces of A and B of product q: the largest first, which has an accumulator of its own.
-__device__ __forceinline__ int piece_a(int q) { return (0x201100 >> (4 * q)) & 15; }
-__device__ __forceinline__ int piece_b(int q) { return (0x021010 >> (4 * q)) & 15; }
 
 // 16-byte piece c of row `row` of a staged tile of rows of kRow bytes, swizzled as its tensor map says.
 template <int kRow>
@@ -197,11 +195,8 @@ __device__ __forceinline__ void land(uint64_t* full, const int* loaded, int stag
   }
 }
 
-template <int kCtas, int kEpi>
-__global__ void __launch_bounds__(kThreads, 1)
-ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-               const __grid_constant__ CUtensorMap tmAlt, const __grid_constant__ CUtensorMap tmC,
-               const GemmArgs a) {
+template <int kCtas, int kEpi, int kPlanes>
+__global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ GemmLaunch launch) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staged = ring + kRing;                                          // [finishing warp][4 KB]
@@ -218,9 +213,11 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = kCtas == 2 ? (int)cluster_rank() : 0;
   const int group = blockIdx.x / kCtas, groups = gridDim.x / kCtas;
-  const int nb = a.bn / kCtas;
-  const uint32_t stage = kABytes + nb * 128;
+  const int bn = launch.args[0].bn, nb = bn / kCtas;
+  // (A's rows past its box are whatever follows in shared memory: rows of sums that nobody reads)
+  const uint32_t a_bytes = launch.args[0].a_box * 128, stage = a_bytes + nb * 128;
   const int stages = min(kMaxStages, (int)(kRing / stage));
+  const uint32_t wait_ns = launch.args[0].wait_ns;
 
   auto stop_all = [&] {
     if (kCtas == 2) tc::give_up(abort_flag);
@@ -261,50 +258,67 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  const Geometry g = geometry<kCtas>(a);
-  const uint32_t acc_cols = a.products > 1 ? 2 * a.bn : a.bn;
+  const Geometry g0 = geometry<kCtas>(launch.args[0]);
+  Geometry g1 = g0;
+  int units = g0.units;
+  if (kEpi == kOut && launch.n == 2) {
+    g1 = geometry<kCtas>(launch.args[1]);
+    units += g1.units;
+  }
+  constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
+  const uint32_t acc_cols = kSets * bn;
+  // Which product unit u belongs to.
+  auto which = [&](int u) { return kEpi == kOut && u >= g0.units ? 1 : 0; };
+  auto unit_of = [&](int u, int p) {
+    return p ? Unit(g1, launch.args[1].splits, u - g0.units) : Unit(g0, launch.args[0].splits, u);
+  };
 
   if (warp == 0) {
     if (lane == 0) {
-      const CUtensorMap* pa = g.gathered && a.alt == 1 ? &tmAlt : &tmA;
-      const CUtensorMap* pb = g.gathered && a.alt == 2 ? &tmAlt : &tmB;
       const uint32_t full0 = kCtas == 2 ? tc::map_cluster(full, 0) : 0;
       int s = 0, loaded = 0, stop = INT32_MAX;
       uint32_t phase = 1;   // (the first round finds every stage free)
       bool ok = true;
-      for (int u = group; ok && u < g.units; u += groups) {
-        const Unit t(g, a.splits, u);
-        const int m = (t.m * kCtas + cta) * 128, n = t.n * a.bn + cta * nb;
-        if (a.withhold == cta + 1) stop = max(0, t.kt * a.products - 1);
+      for (int u = group; ok && u < units; u += groups) {
+        const int p = which(u);
+        const GemmArgs& a = launch.args[p];
+        const bool gathered = p ? g1.gathered : g0.gathered;
+        const CUtensorMap* pa = gathered && a.alt == 1 ? &launch.maps[p].alt : &launch.maps[p].a;
+        const CUtensorMap* pb = gathered && a.alt == 2 ? &launch.maps[p].alt : &launch.maps[p].b;
+        const Unit t = unit_of(u, p);
+        const int m = (t.m * kCtas + cta) * 128, n = t.n * bn + cta * nb;
+        const bool a_mn = a.a_mn, b_mn = a.b_mn;
+        const int b_k0 = a.b_k0, b_n0 = a.b_n0;
+        if (a.withhold == cta + 1) stop = max(0, t.kt * kPlanes - 1);
         for (int kt = t.kt0; ok && kt < t.kt0 + t.kt; ++kt) {
-          for (int q = 0; q < a.products; ++q) {
+#pragma unroll 1
+          for (int z = 0; z < kPlanes; ++z) {
             if (loaded >= stop) {
               ok = false;
               break;
             }
-            if (!tc::wait_mbar<false>(&empty[s], phase, abort_flag, a.wait_ns)) {
+            if (!tc::wait_mbar<false>(&empty[s], phase, abort_flag, wait_ns)) {
               stop_all();
               ok = false;
               break;
             }
             uint8_t* st = ring + s * stage;
-            auto load = [&](uint8_t* dst, const CUtensorMap* map, int x, int y, int z) {
+            auto load = [&](uint8_t* dst, const CUtensorMap* map, int x, int y) {
               if (kCtas == 2) tc::tma_load_3d_pair(dst, map, full0 + 8u * (uint32_t)s, x, y, z);
               else tc::tma_load_3d(dst, map, &full[s], x, y, z);
             };
             if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], kCtas * stage);
-            const int za = piece_a(q), zb = piece_b(q), k = kt * kBK;
-            if (a.a_mn) {
-              load(st, pa, m, k, za);
-              load(st + kBox, pa, m + 64, k, za);
+            const int k = kt * kBK;
+            if (a_mn) {
+              load(st, pa, m, k);
+              load(st + kBox, pa, m + 64, k);
             } else {
-              load(st, pa, k, m, za);
+              load(st, pa, k, m);
             }
-            if (a.b_mn) {
-              for (int j = 0; j < nb; j += 64)
-                load(st + kABytes + j * 128, pb, n + j, k + a.b_k0, zb);
+            if (b_mn) {
+              for (int j = 0; j < nb; j += 64) load(st + a_bytes + j * 128, pb, n + j, k + b_k0);
             } else {
-              load(st + kABytes, pb, k, n + a.b_n0, zb);
+              load(st + a_bytes, pb, k, n + b_n0);
             }
             ++loaded;
             if (++s == stages) s = 0, phase ^= 1;
@@ -315,61 +329,99 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     }
   } else if (warp == 1) {
     if (lane == 0 && cta == 0) {
-      const uint32_t idesc = tc::idesc_bf16_f32(128 * kCtas, a.bn, a.a_mn, a.b_mn);
       const uint32_t r0 = tc::smem_u32(ring);
-      const uint64_t da0 = tc::smem_desc_sw128(r0, a.a_mn ? kBox : 16, 1024);
-      const uint64_t db0 = tc::smem_desc_sw128(r0 + kABytes, a.b_mn ? kBox : 16, 1024);
-      const uint64_t ka = (a.a_mn ? 2048 : 32) >> 4, kb = (a.b_mn ? 2048 : 32) >> 4;   // 16 k
-      uint64_t da = da0, db = db0;
-      int s = 0, done = 0;
+      const uint32_t step = stage >> 4;
+      int s = 0, done = 0;   // (done: sums, from the launch's first)
       uint32_t phase = 0;
       bool ok = true;
-      for (int u = group; u < g.units; u += groups, ++done) {
-        const Unit t(g, a.splits, u);
-        const int buf = done & 1;
-        if (done >= 2 && !tc::wait_mbar<true>(&acc_empty[buf], ((done >> 1) - 1) & 1, abort_flag, a.wait_ns)) {
-          stop_all();
-          break;
-        }
-        tc::tc_fence_after();
-        const uint32_t d0 = tmem + buf * acc_cols;
-        for (int kt = 0; ok && kt < t.kt; ++kt) {
-          for (int q = 0; q < a.products; ++q) {
-            if (!tc::wait_mbar<false>(&full[s], phase, abort_flag, a.wait_ns)) {
-              stop_all();
-              ok = false;
-              break;
-            }
-            tc::tc_fence_after();
-            const uint32_t d = d0 + (q > 0 ? a.bn : 0);
+      for (int u = group; ok && u < units; u += groups) {
+        const int p = which(u);
+        const GemmArgs& a = launch.args[p];
+        const Unit t = unit_of(u, p);
+        const bool a_mn = a.a_mn, b_mn = a.b_mn;
+        const uint32_t idesc = tc::idesc_bf16_f32(128 * kCtas, bn, a_mn, b_mn);
+        const uint64_t da0 = tc::smem_desc_sw128(r0, a_mn ? kBox : 16, 1024);
+        const uint64_t db0 = tc::smem_desc_sw128(r0 + a_bytes, b_mn ? kBox : 16, 1024);
+        const uint64_t ka = (a_mn ? 2048 : 32) >> 4, kb = (b_mn ? 2048 : 32) >> 4;   // 16 k
+        // 64 k of A in slot i times B in slot j
+        auto product = [&](uint32_t d, int i, int j, bool first) {
+          const uint64_t da = da0 + (uint64_t)(i * step), db = db0 + (uint64_t)(j * step);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const uint32_t acc = kk > 0 || kt > 0 || q > 1;
-              if (kCtas == 2) tc::mma_bf16_pair(d, da + kk * ka, db + kk * kb, idesc, acc);
-              else tc::mma_bf16(d, da + kk * ka, db + kk * kb, idesc, acc);
-            }
-            commit(&empty[s]);
-            da += stage >> 4;
-            db += stage >> 4;
-            if (++s == stages) s = 0, phase ^= 1, da = da0, db = db0;
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kCtas == 2) tc::mma_bf16_pair(d, da + kk * ka, db + kk * kb, idesc, kk > 0 || !first);
+            else tc::mma_bf16(d, da + kk * ka, db + kk * kb, idesc, kk > 0 || !first);
           }
-        }
-        if (!ok || *abort_flag) break;   // no sums: the finishing warps give up
-        commit(&acc_full[buf]);
+        };
+        auto arrived = [&](int i, uint32_t ph) {
+          ok = ok && tc::wait_mbar<false>(&full[i], ph, abort_flag, wait_ns);
+          tc::tc_fence_after();
+          return ok;
+        };
+        auto next = [&] {
+          if (++s == stages) s = 0, phase ^= 1;
+        };
+        int kt = 0;
+        do {   // a sum (of nothing: announced as it is)
+          const int buf = done & 1;
+          if (done >= 2 && !tc::wait_mbar<true>(&acc_empty[buf], ((done >> 1) - 1) & 1, abort_flag, wait_ns)) {
+            ok = false;
+            break;
+          }
+          tc::tc_fence_after();
+          const uint32_t d = tmem + buf * acc_cols;
+          const int end = kPlanes == 3 ? min(t.kt, kt + kPartK) : t.kt;
+          for (bool first = true; kt < end; ++kt, first = false) {
+            if (kPlanes == 1) {
+              if (!arrived(s, phase)) break;
+              product(d, s, s, first);
+              commit(&empty[s]);
+              next();
+            } else {   // pieces 0, 1, 2 as they come; a slot is free with the last product that reads it
+              const int s0 = s;
+              if (!arrived(s0, phase)) break;
+              product(d, s0, s0, first);
+              next();
+              const int s1 = s;
+              if (!arrived(s1, phase)) break;
+              product(d + bn, s0, s1, first);
+              product(d + bn, s1, s0, false);
+              product(d + bn, s1, s1, false);
+              commit(&empty[s1]);
+              next();
+              const int s2 = s;
+              if (!arrived(s2, phase)) break;
+              product(d + bn, s0, s2, false);
+              product(d + bn, s2, s0, false);
+              commit(&empty[s0]);
+              commit(&empty[s2]);
+              next();
+            }
+          }
+          if (!ok || *abort_flag) {
+            ok = false;   // no sums: the finishing warps give up
+            break;
+          }
+          commit(&acc_full[buf]);
+          ++done;
+        } while (kt < t.kt);
       }
+      if (!ok) stop_all();
     }
   } else if (warp >= 4) {
-    const int e = warp - 4, quad = warp & 3, half = e >> 2, chunks = a.bn / 64;   // of 32 columns
+    const int e = warp - 4, quad = warp & 3, half = e >> 2, chunks = bn / 64;   // of 32 columns
     float* bias = biases + 128 * e;
     const uint32_t empty0 = kCtas == 2 ? tc::map_cluster(acc_empty, 0) : tc::smem_u32(acc_empty);
-    Writer out{&tmC, staged + e * kStaged, lane, 0};
+    Writer out{nullptr, staged + e * kStaged, lane, 0};
     bool ok = true;
     int done = 0;
-    for (int u = group; u < g.units; u += groups, ++done) {
-      const Unit t(g, a.splits, u);
-      const int buf = done & 1;
+    for (int u = group; u < units; u += groups) {
+      const int p = which(u);
+      const GemmArgs& a = launch.args[p];
+      const Geometry& g = p ? g1 : g0;
+      const Unit t = unit_of(u, p);
+      out.map = &launch.maps[p].c;
       const int row0 = (t.m * kCtas + cta) * 128 + 32 * quad, row = row0 + lane;
-      const int col0 = t.n * a.bn + half * 32 * chunks;
+      const int col0 = t.n * bn + half * 32 * chunks;
       const bool live = row < g.M;
       // what the row needs, on its way while the sums are
       int label = -1;
@@ -392,44 +444,29 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         __syncwarp();
       }
-      ok = ok && tc::wait_mbar<true>(&acc_full[buf], (done >> 1) & 1, abort_flag, a.wait_ns) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
-      tc::tc_fence_after();
-      if (!ok && lane == 0) {
-        stop_all();
-        if (a.err) atomicExch(a.err, 1);
-      }
       float top = -INFINITY, sum = 0.f;
-      const uint32_t acc = tmem + ((uint32_t)(32 * quad) << 16) + buf * acc_cols + half * 32 * chunks;
-#pragma unroll 1
-      for (int ch = 0; ch < chunks; ++ch) {
+
+      // The sums in buffer `buf` are there (or will not come).
+      auto wait_sums = [&](int buf) {
+        ok = ok && tc::wait_mbar<true>(&acc_full[buf], (done >> 1) & 1, abort_flag, wait_ns) && !*abort_flag;
+        ok = __all_sync(0xffffffffu, ok);
+        tc::tc_fence_after();
+        if (!ok && lane == 0) {
+          stop_all();
+          if (a.err) atomicExch(a.err, 1);
+        }
+      };
+      auto free_sums = [&](int buf) {
+        if (!ok) return;
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_relaxed(empty0 + 8u * (uint32_t)buf);
+      };
+      const uint32_t at0 = tmem + ((uint32_t)(32 * quad) << 16) + half * 32 * chunks;
+
+      // 32 columns of sums of this row
+      auto finish = [&](int ch, float (&v)[32]) {
         const int col = col0 + 32 * ch;   // (of this product)
-        float v[32];
-        if (ok) {
-          uint32_t r[32];
-          tc::tmem_ld_32x32b_x32(acc + 32 * ch, r);
-          tc::tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-          if (a.products > 1) {
-            tc::tmem_ld_32x32b_x32(acc + a.bn + 32 * ch, r);
-            tc::tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r[i]);
-          }
-          if (t.kt == 0) {   // nothing was summed
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = 0.f;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7fc00000u);
-        }
-        if (ch + 1 == chunks && ok) {
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive_relaxed(empty0 + 8u * (uint32_t)buf);
-        }
         if (kEpi != kOut) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
@@ -461,15 +498,16 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           const bool dead = !live || lse == -INFINITY;   // (no class that is not masked: no gradient)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            float p = fa * exp2f((v[i] - lse) * kLog2e);
-            if (hit == i) p -= fb;
-            v[i] = dead ? 0.f : p;
+            float q = fa * exp2f((v[i] - lse) * kLog2e);
+            if (hit == i) q -= fb;
+            v[i] = dead ? 0.f : q;
           }
-          for (int q = 0; q < (a.products > 1 ? 3 : 1); ++q) {
+#pragma unroll
+          for (int z = 0; z < kPlanes; ++z) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              if (q == 0) {
+              if (z == 0) {
                 w[i] = pack2(v[2 * i], v[2 * i + 1]);
               } else {   // what the pieces before left
                 float x[2];
@@ -477,19 +515,19 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 for (int k = 0; k < 2; ++k) {
                   bf16 p0, p1, p2;
                   split3(v[2 * i + k], p0, p1, p2);
-                  x[k] = __bfloat162float(q == 1 ? p1 : p2);
+                  x[k] = __bfloat162float(z == 1 ? p1 : p2);
                 }
                 w[i] = pack2(x[0], x[1]);
               }
             }
-            out.put_bf16(w, col, q * a.p_plane + row0);
+            out.put_bf16(w, col, z * a.p_plane + row0);
           }
           if (a.db && row0 < g.M) {
             const float s = column_sums(v, lane);
             if (col + lane < g.N) AGN_ST(a.db + (int64_t)(row0 >> 5) * a.ld_db + col + lane, s);
           }
         } else {
-          if (row0 >= g.M || col >= g.N) continue;   // (warp-uniform)
+          if (row0 >= g.M || col >= g.N) return;   // (warp-uniform)
           if (a.part) {
             out.put_fp32(v, col, t.split * a.part_rows + row0, a.part == 2);
           } else if (a.tma_out && !(a.scatter && g.gathered)) {
@@ -509,9 +547,59 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             else out.put_rows(v, static_cast<float*>(a.out), at, n, cols);
           }
         }
+      };
+
+      const uint32_t none = 0x7fc00000u;   // what could not be computed
+      if (kPlanes == 1) {
+        const int buf = done & 1;
+        wait_sums(buf);
+#pragma unroll 1
+        for (int ch = 0; ch < chunks; ++ch) {
+          uint32_t r[32];
+          float v[32];
+          if (ok) {
+            tc::tmem_ld_32x32b_x32(at0 + buf * acc_cols + 32 * ch, r);
+            tc::tmem_ld_wait();
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(!ok ? none : t.kt == 0 ? 0u : r[i]);
+          if (ch + 1 == chunks) free_sums(buf);
+          finish(ch, v);
+        }
+        ++done;
+      } else {
+        float v[2][32];   // (64 columns at most)
+#pragma unroll
+        for (int i = 0; i < 64; ++i) v[i / 32][i % 32] = 0.f;
+        int kt = 0;
+        do {
+          const int buf = done & 1;
+          wait_sums(buf);
+#pragma unroll
+          for (int ch = 0; ch < 2; ++ch) {
+            if (ch >= chunks) break;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {   // 16 columns of a set at a time
+              uint32_t r[16];
+              if (ok) {
+                tc::tmem_ld_32x32b_x16(at0 + buf * acc_cols + (h >> 1) * bn + 32 * ch + 16 * (h & 1), r);
+                tc::tmem_ld_wait();
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                v[ch][16 * (h & 1) + i] += __uint_as_float(!ok ? none : t.kt == 0 ? 0u : r[i]);
+            }
+          }
+          free_sums(buf);
+          ++done;
+          kt += kPartK;
+        } while (kt < t.kt);
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch)
+          if (ch < chunks) finish(ch, v[ch]);
       }
       if (kEpi == kLse && live)
-        AGN_ST(a.ms + (int64_t)(2 * t.n + half) * a.rows_pad + row, make_float2(top, sum));
+        AGN_ST(a.ms + (int64_t)row * a.ld_ms + a.ms0 + 2 * t.n + half, make_float2(top, sum));
     }
     if (kEpi != kLse && lane == 0) tc::bulk_wait();   // the last stores are done before the kernel is
   }
@@ -538,38 +626,38 @@ ce_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   }
 }
 
-template <int kCtas, int kEpi>
-Status launch(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& talt, const CUtensorMap& tc,
-              const GemmArgs& a, int max_units, cudaStream_t st) {
+template <int kCtas, int kEpi, int kPlanes>
+Status queue(const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
   struct Tag {};
-  auto kern = ce_gemm_kernel<kCtas, kEpi>;
+  auto kern = ce_gemm_kernel<kCtas, kEpi, kPlanes>;
   int dev = 0, sms = 0;
   AGN_TRY(current_device(&dev));
   AGN_TRY(device_sms(dev, &sms));
   AGN_TRY_CUDA(allow_smem<Tag>(kern, kSmem, dev));
-  const int groups = std::max(1, std::min(max_units, sms / kCtas));
+  const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>(max_units, sms / kCtas));
   if (kCtas == 2)
-    AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3((unsigned)(2 * groups)), dim3(kThreads), kSmem, dim3(2, 1, 1), st,
-                                    ta, tb, talt, tc, a));
+    AGN_TRY_CUDA(launch_pdl_cluster(kern, dim3(2 * groups), dim3(kThreads), kSmem, dim3(2, 1, 1), st, g));
   else
-    AGN_TRY_CUDA(launch_pdl(kern, dim3((unsigned)groups), dim3(kThreads), kSmem, st, ta, tb, talt, tc, a));
+    AGN_TRY_CUDA(launch_pdl(kern, dim3(groups), dim3(kThreads), kSmem, st, g));
   return Status::Ok();
+}
+
+template <int kCtas, int kPlanes>
+Status queue_for(int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
+  if (epilogue == kLse) return queue<kCtas, kLse, kPlanes>(g, max_units, st);
+  if (epilogue == kGrad) return queue<kCtas, kGrad, kPlanes>(g, max_units, st);
+  return queue<kCtas, kOut, kPlanes>(g, max_units, st);
 }
 
 }  // namespace
 
-Status gemm(int ctas, int epilogue, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& alt,
-            const CUtensorMap& c, const GemmArgs& args, int max_units, cudaStream_t st) {
-  GemmArgs g = args;
-  if (!g.wait_ns) g.wait_ns = (uint32_t)kWaitNs;
-  if (ctas == 2) {
-    if (epilogue == kLse) return launch<2, kLse>(a, b, alt, c, g, max_units, st);
-    if (epilogue == kGrad) return launch<2, kGrad>(a, b, alt, c, g, max_units, st);
-    return launch<2, kOut>(a, b, alt, c, g, max_units, st);
-  }
-  if (epilogue == kLse) return launch<1, kLse>(a, b, alt, c, g, max_units, st);
-  if (epilogue == kGrad) return launch<1, kGrad>(a, b, alt, c, g, max_units, st);
-  return launch<1, kOut>(a, b, alt, c, g, max_units, st);
+Status gemm(int ctas, int epilogue, const GemmLaunch& launch, int64_t max_units, cudaStream_t st) {
+  GemmLaunch g = launch;
+  for (GemmArgs& a : g.args)
+    if (!a.wait_ns) a.wait_ns = (uint32_t)kWaitNs;
+  if (g.args[0].planes == 3)
+    return ctas == 2 ? queue_for<2, 3>(epilogue, g, max_units, st) : queue_for<1, 3>(epilogue, g, max_units, st);
+  return ctas == 2 ? queue_for<2, 1>(epilogue, g, max_units, st) : queue_for<1, 1>(epilogue, g, max_units, st);
 }
 
 }  // namespace ce
