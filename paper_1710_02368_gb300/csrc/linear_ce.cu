@@ -108,6 +108,7 @@ struct Layout {
   Cut grads[2];            // dw, dx (both: the first alone, with two products)
   int dw_splits, dx_splits;
   bool dx_part;
+  bool few;
   int64_t halves;          // forward: partial (maximum, sum) of a row
   size_t idx, live, x, w, ms, zlab, p, db, dxs, dws, bytes;
 };
@@ -127,6 +128,19 @@ Layout layout(const Sizes& s, bool backward) {
   if (small(s)) {
     if (backward) l.p = take((size_t)s.rows * s.classes * 4);
     l.bytes = std::max<size_t>(at, 1024);
+    return l;
+  }
+  if (few(s.rows, s.prec, backward)) {
+    l.few = true;
+    l.halves = few_blocks(s.classes);
+    if (!backward) {
+      l.ms = take((size_t)s.rows * l.halves * 8);
+      l.zlab = take((size_t)s.rows * 4);
+    } else {
+      l.p = take((size_t)s.classes * few_rows(s.rows) * 4);
+      l.dxs = take((size_t)few_cut(s.inner, s.classes, s.prec == AGN_PREC_FP32 ? 4 : 2).parts * s.rows * l.kp * 4);
+    }
+    l.bytes = at;
     return l;
   }
   int64_t most = s.classes;
@@ -364,13 +378,14 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(most, a.y * exp2f((a.x - from) * kLog2e) + b.y * exp2f((b.x - from) * kLog2e));
 }
 
-// lse and loss from the partial maxima and sums: a warp a row, or where there are few rows a block.
+// lse and loss from the partial maxima and sums: a warp a row, or where there are few rows a block.  idx
+// null: no row was moved.
 __global__ void __launch_bounds__(kThreads)
 join_kernel(const float2* ms, int halves, int64_t ld, int rows_a_block, const float* zlab, const int* labels,
             int classes, int rows, const int* idx, const int* live_p, float* loss, float* lse) {
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int live = AGN_LD(live_p);
+  const int live = idx ? AGN_LD(live_p) : rows;
   const int shared_by = kThreads / 32 / rows_a_block;   // warps of a row
   const int row = blockIdx.x * rows_a_block + warp / shared_by, part = warp % shared_by;
   float2 v = make_float2(-INFINITY, 0.f);
@@ -397,8 +412,8 @@ join_kernel(const float2* ms, int halves, int64_t ld, int rows_a_block, const fl
     for (int j = 1; j < shared_by; ++j) v = join(v, parts[warp + j]);
   }
   if (lane != 0) return;
-  if (row < live) {
-    const int at = AGN_LD(idx + row);
+  if (row < live && (idx || has_label(AGN_LD(labels + row), classes))) {
+    const int at = idx ? AGN_LD(idx + row) : row;
     const float total = v.x == -INFINITY && v.y == 0.f ? -INFINITY : v.x + logf(v.y);
     AGN_ST(lse + at, total);
     AGN_ST(loss + at, total == -INFINITY ? INFINITY : total - AGN_LD(zlab + row));
@@ -727,6 +742,30 @@ int64_t logit_units(const Call& c, const Layout& l, int64_t n) {
   return ceil_div(c.s.rows, 128 * l.z.ctas) * ceil_div(n, l.z.bn);
 }
 
+Status join_rows(const Call& c, const float2* ms, int64_t halves, const float* zlab, const int* idx, const int* live,
+                 cudaStream_t st) {
+  const int rows_a_block = c.s.rows >= 4 * kSms || halves <= 64 ? 8 : 1;
+  return run(join_kernel, dim3((unsigned)ceil_div(c.s.rows, rows_a_block)), kThreads, 0, st, ms, (int)halves, halves,
+             rows_a_block, zlab, c.labels, (int)c.s.classes, (int)c.s.rows, idx, live, c.loss, c.lse_out);
+}
+
+Status run_few(const Call& c, const Layout& l, bool backward_call, cudaStream_t st) {
+  FewArgs a{};
+  a.x = c.x; a.w = c.w; a.bias = c.bias; a.labels = c.labels;
+  a.rows = (int)c.s.rows; a.inner = (int)c.s.inner; a.classes = (int)c.s.classes;
+  a.ms = reinterpret_cast<float2*>(c.work + l.ms);
+  a.zlab = reinterpret_cast<float*>(c.work + l.zlab);
+  a.lse = c.lse; a.dloss = c.dloss; a.dlse = c.dlse;
+  a.scale = c.scale;
+  a.p = reinterpret_cast<float*>(c.work + l.p);
+  a.dx = c.dx; a.dw = c.dw; a.dbias = c.dbias;
+  a.dx_parts = c.dx ? reinterpret_cast<float*>(c.work + l.dxs) : nullptr;
+  a.ld_parts = l.kp;
+  AGN_TRY(few(a, c.s.prec, backward_call, st));
+  if (backward_call) return Status::Ok();
+  return join_rows(c, a.ms, l.halves, a.zlab, nullptr, nullptr, st);
+}
+
 template <typename T>
 Status forward(const Call& c, const Layout& l, cudaStream_t st) {
   AGN_TRY(prepare<T>(c, l, st));
@@ -749,10 +788,8 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
     AGN_TRY(gemm(l.z.ctas, kLse, g, logit_units(c, l, n), st));
     half += 2 * ceil_div(n, l.z.bn);
   }
-  const int rows_a_block = c.s.rows >= 4 * kSms || half <= 64 ? 8 : 1;
-  return run(join_kernel, dim3((unsigned)ceil_div(c.s.rows, rows_a_block)), kThreads, 0, st, (const float2*)ms,
-             (int)half, l.halves, rows_a_block, (const float*)zlab, c.labels, (int)c.s.classes, (int)c.s.rows,
-             (const int*)(c.work + l.idx), (const int*)(c.work + l.live), c.loss, c.lse_out);
+  return join_rows(c, ms, half, zlab, reinterpret_cast<const int*>(c.work + l.idx),
+                   reinterpret_cast<const int*>(c.work + l.live), st);
 }
 
 template <typename T>
@@ -908,9 +945,11 @@ Status call(Call& c, bool backward_call, cudaStream_t st) {
   const bool fp32 = c.s.prec == AGN_PREC_FP32;
   if (!backward_call) {
     if (small(c.s)) AGN_TRY(fp32 ? small_forward<float>(c, st) : small_forward<bf16>(c, st));
+    else if (l.few) AGN_TRY(run_few(c, l, false, st));
     else AGN_TRY(fp32 ? forward<float>(c, l, st) : forward<bf16>(c, l, st));
   } else if (c.dx || c.dw || c.dbias) {
     if (small(c.s)) AGN_TRY(fp32 ? small_backward<float>(c, l, st) : small_backward<bf16>(c, l, st));
+    else if (l.few) AGN_TRY(run_few(c, l, true, st));
     else AGN_TRY(fp32 ? backward<float>(c, l, st) : backward<bf16>(c, l, st));
   }
   return bounds_collect(st);

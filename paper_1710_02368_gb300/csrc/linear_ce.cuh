@@ -70,5 +70,48 @@ struct GemmLaunch {
 // ctas: 1 or 2 (pairs); max_units: tiles times ranges along K, at most.  On the current device.
 Status gemm(int ctas, int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st);
 
+// A few rows (linear_ce_few.cu): up to 16 of fp32; of bf16 up to 4, backward (us for 8 and 16 rows of fp32,
+// 4096 and 2048 to 32000 and 50000 classes, against three pieces on the tensor cores: 98 for 802, 203 for
+// 430, gradients 284 for 1387, 460 for 908; bf16, 4096 to 32000: one row 47 for 49, gradients of 4 rows 151
+// for 203, of 8 242 for 204).
+struct FewArgs {
+  const void *x, *w;
+  const float* bias;
+  const int* labels;
+  int rows, inner, classes;
+  float2* ms;               // forward: [rows][few_blocks] (maximum, sum)
+  float* zlab;              // [rows]
+  const float *lse, *dloss, *dlse;   // backward
+  float scale;
+  float* p;                 // [classes][few_rows]
+  void *dx, *dw;
+  float* dbias;
+  float* dx_parts;          // [parts][rows][ld_parts], null: no dx
+  int64_t ld_parts;
+};
+constexpr int kFewSms = 152;   // what grids are made for
+constexpr int few_rows(int64_t rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+constexpr bool few(int64_t rows, int dtype, bool backward) {
+  return rows <= (dtype == AGN_PREC_FP32 ? 16 : backward ? 4 : 0);
+}
+// Blocks of the dot products: a warp takes four classes at a time.
+constexpr int64_t few_blocks(int64_t classes) { return std::min<int64_t>(kFewSms, (classes + 63) / 64); }
+// Blocks of the outer products: `along` threads along the columns of 16 bytes, ranges of classes.
+struct FewCut {
+  int along, parts;
+  int64_t blocks_k, blocks_c;
+};
+inline FewCut few_cut(int64_t inner, int64_t classes, int es) {
+  const int64_t columns = (inner * es + 15) / 16;
+  FewCut c;
+  c.along = (int)std::min<int64_t>(256, (columns + 31) / 32 * 32);
+  c.blocks_k = (columns + c.along - 1) / c.along;
+  const int64_t at_once = 256 / c.along;
+  c.blocks_c = std::max<int64_t>(1, std::min<int64_t>(kFewSms * 2 / c.blocks_k, (classes + 16 * at_once - 1) / (16 * at_once)));
+  c.parts = (int)(c.blocks_c * at_once);
+  return c;
+}
+Status few(const FewArgs& a, int dtype, bool backward, cudaStream_t st);
+
 }  // namespace ce
 }  // namespace agn

@@ -267,10 +267,29 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   }
   constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
   const uint32_t acc_cols = kSets * bn;
-  // Which product unit u belongs to.
-  auto which = [&](int u) { return kEpi == kOut && u >= g0.units ? 1 : 0; };
-  auto unit_of = [&](int u, int p) {
-    return p ? Unit(g1, launch.args[1].splits, u - g0.units) : Unit(g0, launch.args[0].splits, u);
+  // Unit i of this CTA (pair): of product p, number u.  One product: in turn.  Two: the longer units first, in
+  // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time.
+  const bool two = kEpi == kOut && launch.n == 2;
+  const int longer = two && g1.kt_per > g0.kt_per ? 1 : 0;
+  const int n_long = longer ? g1.units : g0.units, n_short = units - n_long;
+  const int more = n_long % groups;   // CTAs with one more long unit
+  const int ahead = two && more ? (longer ? g1.kt_per : g0.kt_per) / max(1, longer ? g0.kt_per : g1.kt_per) : 0;
+  const int mine = n_long / groups + (group < more ? 1 : 0);
+  struct Place {
+    int p, u;   // u < 0: no more
+  };
+  auto place = [&](int i) {
+    if (i < mine) return Place{longer, i * groups + group};
+    int j = i - mine, u = -1;
+    if (group >= more) {
+      if (j < ahead) u = j * (groups - more) + group - more;
+      else j -= ahead;
+    }
+    if (u < 0) u = ahead * (groups - more) + j * groups + group;
+    return Place{1 - longer, u < n_short ? u : -1};
+  };
+  auto unit_of = [&](Place at) {
+    return at.p ? Unit(g1, launch.args[1].splits, at.u) : Unit(g0, launch.args[0].splits, at.u);
   };
 
   if (warp == 0) {
@@ -279,13 +298,15 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       int s = 0, loaded = 0, stop = INT32_MAX;
       uint32_t phase = 1;   // (the first round finds every stage free)
       bool ok = true;
-      for (int u = group; ok && u < units; u += groups) {
-        const int p = which(u);
+      for (int i = 0; ok; ++i) {
+        const Place at = place(i);
+        if (at.u < 0) break;
+        const int p = at.p;
         const GemmArgs& a = launch.args[p];
         const bool gathered = p ? g1.gathered : g0.gathered;
         const CUtensorMap* pa = gathered && a.alt == 1 ? &launch.maps[p].alt : &launch.maps[p].a;
         const CUtensorMap* pb = gathered && a.alt == 2 ? &launch.maps[p].alt : &launch.maps[p].b;
-        const Unit t = unit_of(u, p);
+        const Unit t = unit_of(at);
         const int m = (t.m * kCtas + cta) * 128, n = t.n * bn + cta * nb;
         const bool a_mn = a.a_mn, b_mn = a.b_mn;
         const int b_k0 = a.b_k0, b_n0 = a.b_n0;
@@ -334,10 +355,12 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       int s = 0, done = 0;   // (done: sums, from the launch's first)
       uint32_t phase = 0;
       bool ok = true;
-      for (int u = group; ok && u < units; u += groups) {
-        const int p = which(u);
+      for (int i = 0; ok; ++i) {
+        const Place at = place(i);
+        if (at.u < 0) break;
+        const int p = at.p;
         const GemmArgs& a = launch.args[p];
-        const Unit t = unit_of(u, p);
+        const Unit t = unit_of(at);
         const bool a_mn = a.a_mn, b_mn = a.b_mn;
         const uint32_t idesc = tc::idesc_bf16_f32(128 * kCtas, bn, a_mn, b_mn);
         const uint64_t da0 = tc::smem_desc_sw128(r0, a_mn ? kBox : 16, 1024);
@@ -414,11 +437,13 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     Writer out{nullptr, staged + e * kStaged, lane, 0};
     bool ok = true;
     int done = 0;
-    for (int u = group; u < units; u += groups) {
-      const int p = which(u);
+    for (int i = 0;; ++i) {
+      const Place at = place(i);
+      if (at.u < 0) break;
+      const int p = at.p;
       const GemmArgs& a = launch.args[p];
       const Geometry& g = p ? g1 : g0;
-      const Unit t = unit_of(u, p);
+      const Unit t = unit_of(at);
       out.map = &launch.maps[p].c;
       const int row0 = (t.m * kCtas + cta) * 128 + 32 * quad, row = row0 + lane;
       const int col0 = t.n * bn + half * 32 * chunks;

@@ -83,7 +83,9 @@ def check(agn, x, w, b, labels, dtype, scale=1.0, dloss=None, dlse=None):
 
 SIZES = [(1, 16, 2), (1, 1, 1), (33, 100, 10), (32, 128, 10), (512, 33, 60),        # plain kernels
          (513, 64, 100), (600, 1, 3), (257, 64, 257), (130, 72, 1000),              # pairs
-         (1, 4096, 3001), (100, 80, 5000), (128, 1000, 999), (5, 8, 70000),         # a CTA a tile
+         (1, 4096, 3001), (2, 100, 2000), (3, 1000, 777), (8, 520, 999), (7, 35, 4001),   # few rows
+         (9, 2048, 515), (16, 1600, 301), (16, 4100, 100), (15, 33, 5000), (12, 8, 70000),
+         (100, 80, 5000), (128, 1000, 999), (17, 8, 70000), (20, 4096, 640),              # a CTA a tile
          (777, 1000, 1500), (300, 130, 700), (1000, 257, 515),                      # ragged, packed rows
          (4096, 200, 10), (64, 64, 20000), (16000, 40, 5)]                          # ranges along K
 
@@ -96,7 +98,7 @@ def test_sizes(agn, rows, inner, classes, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,inner,classes", [(70, 30, 20), (700, 96, 333), (1300, 100, 130), (90, 64, 3000)])
+@pytest.mark.parametrize("rows,inner,classes", [(70, 30, 20), (7, 80, 3000), (16, 50, 900), (700, 96, 333), (1300, 100, 130), (90, 64, 3000)])
 @pytest.mark.parametrize("ignored", [0.3, 0.97, 1.0])
 def test_rows_left_out(agn, rows, inner, classes, ignored, dtype):
     """They hold NaN and infinities and touch nothing; their dx is zero."""
@@ -129,7 +131,7 @@ def check_masked(agn, x, w, b, labels, dtype, out, dloss, dlse):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,inner,classes", [(40, 24, 30), (700, 64, 300)])
+@pytest.mark.parametrize("rows,inner,classes", [(40, 24, 30), (8, 64, 900), (700, 64, 300)])
 def test_masked_classes(agn, rows, inner, classes, dtype):
     """Classes with a bias of minus infinity (some of them labels, then the loss is infinite) and all of them."""
     x, w, b, labels = make(rows, inner, classes, dtype, masked=classes // 3)
@@ -145,7 +147,7 @@ def test_masked_classes(agn, rows, inner, classes, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("rows,inner,classes", [(40, 24, 30), (700, 64, 300)])
+@pytest.mark.parametrize("rows,inner,classes", [(40, 24, 30), (8, 64, 900), (700, 64, 300)])
 def test_rows_that_are_not_finite(agn, rows, inner, classes, dtype):
     """A NaN row that has a label is NaN; the other rows' losses and dx are what they are without it."""
     x, w, b, labels = make(rows, inner, classes, dtype)
@@ -171,7 +173,7 @@ def test_pieces_of_the_classes(agn, dtype, rows, ignored):
 
 @pytest.mark.parametrize("dtype", [0, 1])
 def test_outputs_not_wanted(agn, dtype):
-    for size in ((40, 24, 30), (700, 64, 300)):
+    for size in ((40, 24, 30), (6, 64, 900), (700, 64, 300)):
         x, w, b, labels = make(*size, dtype)
         _, lse = forward(agn, x, w, b, labels, dtype)
         full = backward(agn, x, w, b, labels, lse, dtype)
@@ -182,7 +184,7 @@ def test_outputs_not_wanted(agn, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
-@pytest.mark.parametrize("size", [(40, 24, 30), (700, 64, 3000), (90, 200, 900), (3000, 264, 24)])
+@pytest.mark.parametrize("size", [(40, 24, 30), (7, 70, 3000), (700, 64, 3000), (90, 200, 900), (3000, 264, 24)])
 def test_equal_calls_give_equal_bits_and_stay_inside(agn, size, dtype):
     """Also in a workspace with other contents; what lies around the buffers stays as it was."""
     rows, inner, classes = size
