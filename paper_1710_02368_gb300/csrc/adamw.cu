@@ -406,7 +406,7 @@ Status optim_create(const agn_optim_tensor* ts, int32_t n_tensors, int32_t bits,
   if (n_tensors < 0 || (n_tensors > 0 && !ts)) return Status::Err(AGN_E_INVALID, "bad tensor list");
   std::unique_ptr<agn_optim> o(new agn_optim);
   o->bits = bits;
-  o->has_param = n_tensors > 0 && ts[0].param;
+  bool any = false;   // (an empty tensor's addresses may be null)
   std::vector<Tensor> host;
   std::vector<Piece> pieces;
   struct Range {
@@ -424,9 +424,11 @@ Status optim_create(const agn_optim_tensor* ts, int32_t n_tensors, int32_t bits,
     if (t.n < 0 || t.n > (int64_t)1 << 40) return Status::Err(AGN_E_INVALID, name + ": n must be in [0, 2^40]");
     if (!(t.weight_decay >= 0.0 && t.weight_decay <= 1e30))
       return Status::Err(AGN_E_INVALID, name + ": weight_decay must be finite and >= 0");
-    if ((t.param != nullptr) != o->has_param)
-      return Status::Err(AGN_E_INVALID, name + ": all tensors have a param or none has");
     if (t.n > 0) {
+      if (!any) o->has_param = t.param != nullptr;
+      any = true;
+      if ((t.param != nullptr) != o->has_param)
+        return Status::Err(AGN_E_INVALID, name + ": all tensors have a param or none has");
       if (!t.grad) return Status::Err(AGN_E_INVALID, name + ": null grad");
       if (t.param && (!t.m || !t.v || (bits == 8 && (!t.m_scale || !t.v_scale))))
         return Status::Err(AGN_E_INVALID, name + ": null state");
@@ -546,7 +548,7 @@ Status optim_step(agn_optim* o, double lr, int64_t step, double beta1, double be
                        "need a finite lr, step >= 1, beta1 and beta2 in [0, 1), eps >= 0");
   const CallBuffer sb{"scale", scale, scale ? sizeof(float) : 0, 4};
   AGN_TRY(plan_device(o));
-  if (!o->has_param && o->tensors > 0) return Status::Err(AGN_E_INVALID, "the plan has gradients alone");
+  if (!o->has_param && o->pieces > 0) return Status::Err(AGN_E_INVALID, "the plan has gradients alone");
   AGN_TRY(check_apart(sb, o->written));
   AGN_TRY(check_buffers({sb}));
   if (o->pieces == 0) return Status::Ok();

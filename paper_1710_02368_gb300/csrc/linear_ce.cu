@@ -933,6 +933,7 @@ Status call(Call& c, bool backward_call, cudaStream_t st) {
     AGN_TRY(check_apart(err, {x, w, bias, labels}));
   }
   if (rows == 0) {   // no rows: the sums over them are zero
+    if (!c.dw && !c.dbias) return Status::Ok();
     AGN_TRY(check_buffers({dw, dbias}));
     if (c.dw) AGN_TRY_CUDA(cudaMemsetAsync(c.dw, 0, wb, st));
     if (c.dbias) AGN_TRY_CUDA(cudaMemsetAsync(c.dbias, 0, cb, st));
