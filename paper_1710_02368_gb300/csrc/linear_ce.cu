@@ -38,58 +38,73 @@ struct Cut {
   int ctas, bn;
   int64_t tiles[2];
   int splits[2];
+  double time;   // estimated clocks
 };
 struct Extents {
   int64_t M, N, K;
+  bool b_mn;
 };
 
-// Clocks of a tile's 64 k: the MMAs at 4096 multiply-adds a clock and SM, or its operands at 64 bytes a
-// clock from the L2 (fp32: six products of three pieces each).
-double step_clocks(int ctas, int bn, int planes, int64_t a_box) {
-  const double mma = bn * 2.0 * (planes == 3 ? 6 : 1), load = (a_box * 128 + bn / ctas * 128) / 64.0 * planes;
-  return std::max(mma, load);
+// Clocks of a tile's 64 k: the MMAs at 4096 multiply-adds a clock and SM, its operands at 64 bytes a clock
+// from the L2, or shared memory at 128: what arrives, and what the MMAs read (B stored along N twice).
+// fp32: six products of three pieces each.
+double step_clocks(int ctas, int bn, int planes, int64_t a_box, bool b_mn) {
+  const int products = planes == 3 ? 6 : 1;
+  const double mma = bn * 2.0 * products, in = (a_box * 128 + bn / ctas * 128) * planes;
+  const double read = (128 * 128 + bn / ctas * 128 * (b_mn ? 2 : 1)) * products;
+  return std::max({mma, in / 64.0, (in + read) / 128.0});
 }
 
 // Tile width by the estimated time: rounds of tiles over the SMs, or B's bytes from memory (24 a clock and
 // SM) if that is more.  Of products cut along K also the ranges: as many as even out the work, where
-// that saves more than the pass over their sums costs.
-Cut cut(int ctas, int planes, bool b_mn, int a_box, const Extents* e, int n, bool ranges) {
+// that saves more than the pass over their sums costs.  A tile takes its epilogue's time at least, 14 clocks
+// a column.
+Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges) {
   Cut best{};
-  double best_time = 0;
   const int64_t at_once = kSms / ctas;
-  const int least = b_mn && ctas == 2 ? 128 : 64;
+  int least = 64;   // (a box is 64 columns of an operand stored along N)
+  for (int i = 0; i < n; ++i)
+    if (e[i].b_mn && ctas == 2) least = 128;
   for (int bn = planes > 1 ? 128 : 256; bn >= least; bn /= 2) {
     Cut c{};
     c.ctas = ctas;
     c.bn = bn;
-    const double step = step_clocks(ctas, bn, planes, a_box);
+    double step = 0;
+    for (int i = 0; i < n; ++i) step = std::max(step, step_clocks(ctas, bn, planes, a_box, e[i].b_mn));
     double steps = 0, bytes = 0;
-    int64_t tiles = 0;
+    int64_t tiles = 0, kt[2], most[2];
     for (int i = 0; i < n; ++i) {
       c.tiles[i] = ceil_div(e[i].M, 128 * ctas) * ceil_div(e[i].N, bn);
       c.splits[i] = 1;
+      kt[i] = ceil_div(e[i].K, 64);
+      most[i] = ranges ? std::min({kPartBytes / (round_up(e[i].M, 256) * round_up(e[i].N, 256) * 4), (int64_t)64,
+                                   ceil_div((int64_t)std::ceil(kt[i] * step), 4000)})
+                       : 1;
       tiles += c.tiles[i];
-      steps += (double)c.tiles[i] * ceil_div(e[i].K, 64);
-      bytes += (double)ceil_div(e[i].N, bn) * bn * ceil_div(e[i].K, 64) * 128 * planes;
+      steps += c.tiles[i] * std::max((double)kt[i], bn * 14 / step);
+      bytes += (double)ceil_div(e[i].N, bn) * bn * kt[i] * 128 * planes;
     }
-    const double share = std::max(1.0, steps / at_once);   // of a CTA
-    double longest = 0;
-    for (int i = 0; i < n; ++i) {
-      const int64_t kt = ceil_div(e[i].K, 64);
-      if (ranges && (kt - share) * step > 12000) {
-        const int64_t sums = round_up(e[i].M, 256) * round_up(e[i].N, 64) * 4;
-        const int64_t s = std::min({(int64_t)std::ceil(kt / std::max(share, 4000 / step)), kPartBytes / sums, (int64_t)64});
-        c.splits[i] = (int)std::max<int64_t>(1, s);
+    double rounds = 0, more = 0;   // steps one after the other, clocks of passes over sums
+    if (n == 1) {
+      const double pass = 8000 + (double)e[0].M * e[0].N * 4 / (24.0 * kSms);
+      auto after = [&](int64_t k) {
+        return ceil_div(tiles * k, at_once) * std::max((double)ceil_div(kt[0], k), bn * 14 / step);
+      };
+      rounds = after(1);
+      for (int64_t k = 2; k <= most[0]; ++k) {
+        const double r = after(k);
+        if (r * step + pass * (1 + 0.1 * k) < rounds * step + more)
+          rounds = r, more = pass * (1 + 0.1 * k), c.splits[0] = (int)k;
       }
-      longest = std::max(longest, (double)ceil_div(kt, c.splits[i]));
+    } else {
+      rounds = std::max(1.0, steps / at_once);   // a CTA's share
+      for (int i = 0; i < n; ++i)
+        if ((kt[i] - rounds) * step > 12000)
+          c.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>(most[i], (int64_t)std::ceil(kt[i] / rounds)));
+      for (int i = 0; i < n; ++i) rounds = std::max(rounds, (double)ceil_div(kt[i], c.splits[i]));
     }
-    const double rounds = n == 1 && c.splits[0] == 1 ? (double)ceil_div(tiles, at_once) * ceil_div(e[0].K, 64)
-                                                     : std::max(share, longest);
-    const double time = std::max(rounds * step, bytes / (24.0 * kSms)) + 1500.0 * tiles / at_once;
-    if (best.bn == 0 || time < best_time) {
-      best = c;
-      best_time = time;
-    }
+    c.time = std::max(rounds * step, bytes / (24.0 * kSms)) + more + 500.0 * tiles / at_once;
+    if (best.bn == 0 || c.time < best.time) best = c;
   }
   return best;
 }
@@ -108,9 +123,10 @@ struct Layout {
   Cut grads[2];            // dw, dx (both: the first alone, with two products)
   int dw_splits, dx_splits;
   bool dx_part;
+  bool x_t;                // dw reads x laid out along its rows
   bool few;
   int64_t halves;          // forward: partial (maximum, sum) of a row
-  size_t idx, live, x, w, ms, zlab, p, db, dxs, dws, bytes;
+  size_t idx, live, x, xt, w, ms, zlab, p, db, dxs, dws, bytes;
 };
 
 Layout layout(const Sizes& s, bool backward) {
@@ -148,12 +164,23 @@ Layout layout(const Sizes& s, bool backward) {
   if (backward) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
   if (!l.direct) limit(kPackBytes, l.kp * 2 * l.planes);
   limit((int64_t)1 << 29, std::max<int64_t>(1, l.rows_pad / 16384));   // tiles of a launch
+  l.pieces = ceil_div(s.classes, most);
+  l.a_box = (int)std::min<int64_t>(128, round_up(s.rows, 8));
+  auto logits = [&](int64_t n) {
+    const Extents e{s.rows, n, s.inner, false};
+    return cut(s.rows > 128 ? 2 : 1, l.planes, l.a_box, &e, 1, false);
+  };
   l.piece = most;
+  if (l.pieces > 1) {   // pieces alike, or as large as they may be and one of the rest
+    const int64_t alike = std::min(most, round_up(ceil_div(s.classes, l.pieces), 256));
+    auto time = [&](int64_t n) {
+      return (double)(s.classes / n) * logits(n).time + (s.classes % n ? logits(s.classes % n).time : 0);
+    };
+    if (time(alike) < time(most)) l.piece = alike;
+  }
   l.pieces = ceil_div(s.classes, l.piece);
   l.ldp = round_up(l.piece, 64);
-  l.a_box = (int)std::min<int64_t>(128, round_up(s.rows, 8));
-  const Extents ez{s.rows, l.piece, s.inner};
-  l.z = cut(s.rows > 128 ? 2 : 1, l.planes, false, l.a_box, &ez, 1, false);
+  l.z = logits(l.piece);
   l.live = take(4);
   l.idx = take((size_t)l.rows_pad * 4);
   l.x = take((size_t)l.planes * l.rows_pad * l.kp * 2);
@@ -166,11 +193,18 @@ Layout layout(const Sizes& s, bool backward) {
   } else {
     l.p = take((size_t)l.planes * l.rows_pad * l.ldp * 2);
     l.db = take((size_t)(l.rows_pad / 32) * l.ldp * 4);
-    const Extents e[2] = {{l.piece, s.inner, s.rows}, {s.rows, s.inner, l.piece}};   // dw, dx
-    const int dw_ctas = l.piece > 128 ? 2 : 1, dx_ctas = l.z.ctas;
-    l.both = dw_ctas == dx_ctas;
-    l.grads[0] = cut(dw_ctas, l.planes, true, 128, e, l.both ? 2 : 1, true);
-    if (!l.both) l.grads[1] = cut(dx_ctas, l.planes, true, 128, e + 1, 1, true);
+    // x along its rows, for dw, where the products' gain (us, a fifth of their time) is more than a pass over x
+    const double elements = (double)s.rows * s.inner;
+    l.x_t = elements * s.classes * (l.planes == 3 ? 14e-10 : 2.3e-10) > elements * (l.planes == 3 ? 1.5e-6 : 0.6e-6) + 2.5;
+    if (l.x_t) l.xt = take((size_t)l.planes * round_up(s.inner, 64) * l.rows_pad * 2);
+    const Extents e[2] = {{l.piece, s.inner, s.rows, !l.x_t}, {s.inner, s.rows, l.piece, false}};   // dw, dx (transposed)
+    const int dw_ctas = l.piece > 128 ? 2 : 1, dx_ctas = s.inner > 128 ? 2 : 1;
+    for (int i = 0; i < 2; ++i) l.grads[i] = cut(i ? dx_ctas : dw_ctas, l.planes, 128, e + i, 1, true);
+    if (dw_ctas == dx_ctas) {   // one launch, where one width suits both
+      const Cut c = cut(dw_ctas, l.planes, 128, e, 2, true);
+      l.both = c.time < l.grads[0].time + l.grads[1].time + 4000;
+      if (l.both) l.grads[0] = c;
+    }
     l.dw_splits = l.grads[0].splits[0];
     l.dx_splits = l.both ? l.grads[0].splits[1] : l.grads[1].splits[0];
     l.dx_part = l.pieces > 1 || l.dx_splits > 1;
@@ -370,6 +404,45 @@ prepare_kernel(const Pack<T> x, const Pack<T> w, bool direct, int range, const i
       if (!known[i / x.inner]) from_float(dx + (int64_t)r0 * x.inner + i, 0.f);
   }
   if (w.src) pack_rows(w, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024);
+}
+
+// dst [inner][ld] = x's rows with a label along their columns (zeros up to a multiple of 64 rows), tiles of
+// 64 x 64 elements through shared memory.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+transpose_kernel(const T* x, int inner, const int* idx, const int* live_p, bf16* dst, int64_t ld, int64_t plane) {
+  pdl_begin();
+  constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+  __shared__ bf16 tile[kPlanes][64][66];   // [column][row]
+  const int live = AGN_LD(live_p), tiles_r = (live + 63) / 64, tiles_c = (inner + 63) / 64;
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  for (int64_t t = blockIdx.x; t < (int64_t)tiles_r * tiles_c; t += gridDim.x) {
+    const int r0 = (int)(t / tiles_c) * 64, c0 = (int)(t % tiles_c) * 64;
+    __syncthreads();
+#pragma unroll 4
+    for (int r = ty; r < 64; r += 4) {
+      float v = 0.f;
+      if (r0 + r < live && c0 + tx < inner) v = to_float(AGN_LD(x + (int64_t)AGN_LD(idx + r0 + r) * inner + c0 + tx));
+      bf16 q[3];
+      if (kPlanes == 3) split3(v, q[0], q[1], q[2]);
+      else q[0] = __float2bfloat16_rn(v);
+#pragma unroll
+      for (int p = 0; p < kPlanes; ++p) tile[p][tx][r] = q[p];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p)
+#pragma unroll 2
+      for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {   // 8 rows a thread
+        const int c = i >> 3, r = (i & 7) * 8;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(&tile[p][c][r + 2 * k]);
+        if (c0 + c < inner)
+          AGN_ST(reinterpret_cast<uint4*>(dst + p * plane + (int64_t)(c0 + c) * ld + r0 + r),
+                 make_uint4(w[0], w[1], w[2], w[3]));
+      }
+  }
 }
 
 // (maximum, sum of exponentials) of two sets of values.
@@ -815,10 +888,18 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
   AGN_TRY(x_maps(c, l, 64, l.a_box, &z.maps[0].a, &z.maps[0].alt));
   AGN_TRY(make_tmap_store_2d(&z.maps[0].c, p, 2, l.ldp, l.planes * l.rows_pad, l.ldp, 32, 32));
   AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].a, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 64));
-  AGN_TRY(x_maps(c, l, 64, 64, &dw.maps[0].b, &dw.maps[0].alt));
-  AGN_TRY(make_tmap_bf16_3d(&dx.maps[0].a, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 128));
-  const bool rows16 = inner * es % 16 == 0;
   const Cut &cw = l.grads[0], &cx = l.both ? l.grads[0] : l.grads[1];
+  if (!l.x_t) {
+    AGN_TRY(x_maps(c, l, 64, 64, &dw.maps[0].b, &dw.maps[0].alt));
+  } else if (c.dw) {
+    bf16* xt = reinterpret_cast<bf16*>(c.work + l.xt);
+    const int64_t plane = round_up(inner, 64) * l.rows_pad;
+    AGN_TRY(run(transpose_kernel<T>, dim3(grid_for(l.rows_pad / 64 * ceil_div(inner, 64), 1)), kThreads, 0, st,
+                static_cast<const T*>(c.x), (int)inner, idx, live, xt, l.rows_pad, plane));
+    AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].b, xt, l.rows_pad, inner, l.planes, l.rows_pad, plane, 64, cw.bn / cw.ctas));
+  }
+  AGN_TRY(make_tmap_bf16_3d(&dx.maps[0].b, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, cx.bn / cx.ctas));
+  const bool rows16 = inner * es % 16 == 0;
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
     if (c0 > 0) AGN_TRY(prepare_w<T>(c, l, c0, n, st));
@@ -841,9 +922,10 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       d = common_args(c, l);
       d.M = (int)n; d.N = (int)inner; d.K = (int)rows;
       d.live_is = 1;
-      d.alt = l.direct ? 2 : 0;
+      d.alt = l.direct && !l.x_t ? 2 : 0;
       d.bn = cw.bn;
-      d.a_mn = d.b_mn = 1;
+      d.a_mn = 1;
+      d.b_mn = !l.x_t;
       d.splits = l.dw_splits;
       d.out = dw_out; d.ldo = inner; d.dtype = c.s.prec;
       if (l.dw_splits > 1) {
@@ -856,16 +938,18 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       }
       dw_units = ceil_div(n, 128 * cw.ctas) * ceil_div(inner, cw.bn) * d.splits;
     }
-    if (c.dx) {   // [rows][inner] += p w
+    if (c.dx) {   // [rows][inner] += p w, as w^T p^T
       GemmArgs& d = dx.args[0];
       d = common_args(c, l);
-      d.M = (int)rows; d.N = (int)inner; d.K = (int)n;
+      d.M = (int)inner; d.N = (int)rows; d.K = (int)n;
+      d.live_is = 2;
+      d.transposed = 1;
       d.bn = cx.bn;
-      d.b_mn = 1;
+      d.a_mn = 1;
       d.splits = l.dx_splits;
       d.out = c.dx; d.ldo = inner; d.dtype = c.s.prec;
       d.scatter = 1;
-      AGN_TRY(w_map(c, l, c0, n, 64, 64, &dx.maps[0].b));
+      AGN_TRY(w_map(c, l, c0, n, 64, 64, &dx.maps[0].a));
       if (l.dx_part) {
         d.part = c0 == 0 ? 1 : 2;
         d.part_rows = (int)l.rows_pad;
@@ -874,7 +958,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
         d.tma_out = 1;
         AGN_TRY(make_tmap_store_2d(&dx.maps[0].c, c.dx, es, inner, rows, inner, 32, 32));
       }
-      dx_units = ceil_div(rows, 128 * cx.ctas) * ceil_div(inner, cx.bn) * d.splits;
+      dx_units = ceil_div(inner, 128 * cx.ctas) * ceil_div(rows, cx.bn) * d.splits;
     }
     if (c.dw && c.dx && l.both) {
       dw.n = 2;

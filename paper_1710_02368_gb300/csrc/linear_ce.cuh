@@ -18,8 +18,8 @@ enum Epilogue {
 // One product of [M][K] and [N][K] operands.  Coordinates are elements; rows of x are
 // those with a label, in order (`live` of them, `idx` their places).
 struct GemmArgs {
-  int M, N, K;              // M (live_is 0) or K (live_is 1) is a bound where live is given
-  const int* live;          // device, null: M and K as they are
+  int M, N, K;              // M (live_is 0), K (1) or N (2) is a bound where live is given
+  const int* live;          // device, null: as they are
   int live_is;
   int rows;                 // rows of x in all: live < rows means that x was gathered
   int alt;                  // 1 (2): A (B) comes from tmAlt where x was gathered
@@ -47,6 +47,7 @@ struct GemmArgs {
   float* db;                // kGrad: [rows_pad / 32][ld_db] column sums of 32 rows, or null
   int64_t ld_db;
   // kOut
+  int transposed;           // the output is [N][M] (whose rows `out`, `scatter` and `part_rows` speak of)
   void* out;                // [M][ldo] of dtype, rows at idx[m] where live < rows and scatter
   int dtype;
   int64_t ldo;

@@ -2,8 +2,10 @@
 // sums in TMEM), with what follows each in its epilogue:
 //   logits z = x w^T (K along both operands' rows): kLse leaves (max, sum of exponentials) of
 //     each row and half a tile, kGrad writes p = a softmax - b [label] in bf16 and sums its columns;
-//   dx = p w and dw = p^T x (kOut): operands stored the other way round are read so (the MMA
-//     takes either major), nothing is transposed in memory.
+//   dw = p^T x and dx = p w (kOut): the MMA takes operands stored along M or N (MN-major) too, but
+//     B's so stored cost it: 256 x 256 tiles of 8192 x 8192 x 4096 1.25 times the clocks, A's none (B's reads
+//     of shared memory, it seems, twice as many).  So dx is made as w^T p^T, p in B's place as it lies,
+//     and leaves transposed, and x is laid out along its rows for dw where that pays.
 // fp32 operands are three exact bf16 pieces (planes): six products of pieces, the first in one
 // accumulator and the five smaller ones in another.  The tensor cores cut what they add to an
 // accumulator off below its last bit, always towards zero, so these sums are taken over 256 k at
@@ -48,8 +50,9 @@ __device__ __forceinline__ Geometry geometry(const GemmArgs& a) {
   if (a.live) {
     const int live = min(AGN_LD(a.live), a.rows);
     g.gathered = live < a.rows;
-    if (a.live_is) g.K = live;
-    else g.M = live;
+    if (a.live_is == 0) g.M = live;
+    else if (a.live_is == 1) g.K = live;
+    else g.N = live;
   }
   g.tiles_n = (g.N + a.bn - 1) / a.bn;
   g.tiles = (g.M + 128 * kCtas - 1) / (128 * kCtas) * g.tiles_n;
@@ -123,6 +126,29 @@ struct Writer {
       *reinterpret_cast<uint4*>(staged_at<64>(to, lane, j)) =
           make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
   }
+  // the tile's rows are the 32 columns, its columns the lanes
+  template <typename T>
+  __device__ __forceinline__ void stage_transposed(uint8_t* to, const float (&v)[32]) {
+    constexpr int kRow = 32 * (int)sizeof(T), kVec = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      uint8_t* p = staged_at<kRow>(to, i, lane / kVec) + lane % kVec * sizeof(T);
+      if (sizeof(T) == 4) *reinterpret_cast<float*>(p) = v[i];
+      else *reinterpret_cast<bf16*>(p) = __float2bfloat16_rn(v[i]);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void put_transposed(const float (&v)[32], int x, int y, bool add) {
+    if (lane == 0) {
+      if (sizeof(T) == 4) tc::bulk_wait_read();
+      else tc::bulk_wait_read_1();
+    }
+    __syncwarp();
+    uint8_t* to = sizeof(T) == 4 ? tile : tile + 2048 * slot;
+    slot ^= 1;
+    stage_transposed<T>(to, v);
+    send(to, x, y, add);
+  }
   __device__ __forceinline__ void put_bf16(const uint32_t (&w)[16], int x, int y) {
     if (lane == 0) tc::bulk_wait_read_1();
     __syncwarp();
@@ -145,10 +171,13 @@ struct Writer {
   }
   // rows 0 .. n - 1 to out + at[row] * ldo: columns 0 .. cols - 1; `at` of row l is lane l's
   template <typename T>
-  __device__ __forceinline__ void put_rows(const float (&v)[32], T* out, int64_t at, int n, int cols) {
+  __device__ __forceinline__ void put_rows(const float (&v)[32], T* out, int64_t at, int n, int cols,
+                                           bool transposed) {
     constexpr int kRow = 32 * (int)sizeof(T), kVec = 16 / (int)sizeof(T), kLanes = 32 / kVec;
     __syncwarp();
-    if (sizeof(T) == 4) {
+    if (transposed) {
+      stage_transposed<T>(tile, v);
+    } else if (sizeof(T) == 4) {
       stage_fp32(v);
     } else {
       uint32_t w[16];
@@ -258,23 +287,22 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   const uint32_t tmem = *tmem_holder;
   pdl_begin();
 
-  const Geometry g0 = geometry<kCtas>(launch.args[0]);
-  Geometry g1 = g0;
-  int units = g0.units;
-  if (kEpi == kOut && launch.n == 2) {
-    g1 = geometry<kCtas>(launch.args[1]);
-    units += g1.units;
-  }
+  __shared__ Geometry geo[2];
+  if (threadIdx.x < 2 && (int)threadIdx.x < launch.n) geo[threadIdx.x] = geometry<kCtas>(launch.args[threadIdx.x]);
+  __syncthreads();
   constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
   const uint32_t acc_cols = kSets * bn;
   // Unit i of this CTA (pair): of product p, number u.  One product: in turn.  Two: the longer units first, in
-  // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time.
+  // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time, and are
+  // the first when the rest is given out in turn.
   const bool two = kEpi == kOut && launch.n == 2;
-  const int longer = two && g1.kt_per > g0.kt_per ? 1 : 0;
-  const int n_long = longer ? g1.units : g0.units, n_short = units - n_long;
+  const int longer = two && geo[1].kt_per > geo[0].kt_per ? 1 : 0;
+  const int n_long = geo[longer].units, n_short = two ? geo[1 - longer].units : 0;
   const int more = n_long % groups;   // CTAs with one more long unit
-  const int ahead = two && more ? (longer ? g1.kt_per : g0.kt_per) / max(1, longer ? g0.kt_per : g1.kt_per) : 0;
+  constexpr int kBeside = kPlanes == 3 ? 3 : 6;   // a unit's time beside its stages, in stages
+  const int ahead = two && more ? (geo[longer].kt_per + kBeside) / (geo[1 - longer].kt_per + kBeside) : 0;
   const int mine = n_long / groups + (group < more ? 1 : 0);
+  const int rank = group >= more ? group - more : group - more + groups;
   struct Place {
     int p, u;   // u < 0: no more
   };
@@ -282,15 +310,13 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     if (i < mine) return Place{longer, i * groups + group};
     int j = i - mine, u = -1;
     if (group >= more) {
-      if (j < ahead) u = j * (groups - more) + group - more;
+      if (j < ahead) u = j * (groups - more) + rank;
       else j -= ahead;
     }
-    if (u < 0) u = ahead * (groups - more) + j * groups + group;
+    if (u < 0) u = ahead * (groups - more) + j * groups + rank;
     return Place{1 - longer, u < n_short ? u : -1};
   };
-  auto unit_of = [&](Place at) {
-    return at.p ? Unit(g1, launch.args[1].splits, at.u) : Unit(g0, launch.args[0].splits, at.u);
-  };
+  auto unit_of = [&](Place at) { return Unit(geo[at.p], launch.args[at.p].splits, at.u); };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -303,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         if (at.u < 0) break;
         const int p = at.p;
         const GemmArgs& a = launch.args[p];
-        const bool gathered = p ? g1.gathered : g0.gathered;
+        const bool gathered = geo[p].gathered;
         const CUtensorMap* pa = gathered && a.alt == 1 ? &launch.maps[p].alt : &launch.maps[p].a;
         const CUtensorMap* pb = gathered && a.alt == 2 ? &launch.maps[p].alt : &launch.maps[p].b;
         const Unit t = unit_of(at);
@@ -442,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       if (at.u < 0) break;
       const int p = at.p;
       const GemmArgs& a = launch.args[p];
-      const Geometry& g = p ? g1 : g0;
+      const Geometry& g = geo[p];
       const Unit t = unit_of(at);
       out.map = &launch.maps[p].c;
       const int row0 = (t.m * kCtas + cta) * 128 + 32 * quad, row = row0 + lane;
@@ -553,23 +579,32 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
           }
         } else {
           if (row0 >= g.M || col >= g.N) return;   // (warp-uniform)
+          const bool flip = a.transposed;
+          const int x0 = flip ? row0 : col, y0 = flip ? col : row0;   // the output's column and row
           if (a.part) {
-            out.put_fp32(v, col, t.split * a.part_rows + row0, a.part == 2);
+            if (flip) out.put_transposed<float>(v, x0, t.split * a.part_rows + y0, a.part == 2);
+            else out.put_fp32(v, x0, t.split * a.part_rows + y0, a.part == 2);
           } else if (a.tma_out && !(a.scatter && g.gathered)) {
             if (a.dtype == AGN_PREC_BF16) {
-              uint32_t w[16];
+              if (flip) {
+                out.put_transposed<bf16>(v, x0, y0, false);
+              } else {
+                uint32_t w[16];
 #pragma unroll
-              for (int i = 0; i < 16; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
-              out.put_bf16(w, col, row0);
+                for (int i = 0; i < 16; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+                out.put_bf16(w, x0, y0);
+              }
+            } else if (flip) {
+              out.put_transposed<float>(v, x0, y0, false);
             } else {
-              out.put_fp32(v, col, row0, false);
+              out.put_fp32(v, x0, y0, false);
             }
           } else {
-            const int n = min(32, g.M - row0), cols = min(32, g.N - col);
-            const int64_t place = live ? (a.scatter ? AGN_LD(a.idx + row) : row) : 0;
-            const int64_t at = place * a.ldo + col;
-            if (a.dtype == AGN_PREC_BF16) out.put_rows(v, static_cast<bf16*>(a.out), at, n, cols);
-            else out.put_rows(v, static_cast<float*>(a.out), at, n, cols);
+            const int n = min(32, (flip ? g.N : g.M) - y0), cols = min(32, (flip ? g.M : g.N) - x0);
+            const int y = y0 + min(lane, n - 1);
+            const int64_t to = (int64_t)(a.scatter ? AGN_LD(a.idx + y) : y) * a.ldo + x0;
+            if (a.dtype == AGN_PREC_BF16) out.put_rows(v, static_cast<bf16*>(a.out), to, n, cols, flip);
+            else out.put_rows(v, static_cast<float*>(a.out), to, n, cols, flip);
           }
         }
       };
