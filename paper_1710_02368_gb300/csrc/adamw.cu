@@ -13,6 +13,7 @@
 #include <cfloat>
 #include <cmath>
 #include <memory>
+#include <type_traits>
 #include <vector>
 
 #include "common.cuh"
@@ -57,8 +58,9 @@ struct StepArgs {
   uint64_t key, offset;
 };
 
+// Eight elements at p: in one piece (wide: aligned, and all there), or the first n one by one.
 __device__ __forceinline__ void load8(const float* p, int n, bool wide, float (&x)[8]) {
-  if (wide && n == 8) {
+  if (wide) {
     if (AGN_BOUNDS_OK(p, 32)) {
       asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]),
@@ -75,7 +77,7 @@ __device__ __forceinline__ void load8(const float* p, int n, bool wide, float (&
   }
 }
 __device__ __forceinline__ void store8(float* p, int n, bool wide, const float (&x)[8]) {
-  if (wide && n == 8) {
+  if (wide) {
     if (AGN_BOUNDS_OK(p, 32)) {
       asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]),
                    "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
@@ -89,22 +91,8 @@ __device__ __forceinline__ void store8(float* p, int n, bool wide, const float (
       if (i < n) AGN_ST(p + i, x[i]);
   }
 }
-__device__ __forceinline__ void load8(const bf16* p, int n, bool wide, float (&x)[8]) {
-  if (wide && n == 8) {
-    const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? __bfloat162float(AGN_LD(p + i)) : 0.f;
-  }
-}
 __device__ __forceinline__ void store8(bf16* p, int n, bool wide, const float (&x)[8]) {
-  if (wide && n == 8) {
+  if (wide) {
     const __nv_bfloat162 o[4] = {__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3]),
                                  __floats2bfloat162_rn(x[4], x[5]), __floats2bfloat162_rn(x[6], x[7])};
     AGN_ST(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(o));
@@ -114,8 +102,39 @@ __device__ __forceinline__ void store8(bf16* p, int n, bool wide, const float (&
       if (i < n) AGN_ST(p + i, __float2bfloat16_rn(x[i]));
   }
 }
+// Eight gradients as they lie, and their values: apart, so that what is loaded beside them is under way before
+// anything waits for them.
+template <typename T>
+struct Raw {
+  uint32_t w[sizeof(T) == 4 ? 8 : 4];
+};
+__device__ __forceinline__ void load8(const float* p, int n, bool wide, Raw<float>& r) {
+  float x[8];
+  load8(p, n, wide, x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(x[i]);
+}
+__device__ __forceinline__ void load8(const bf16* p, int n, bool wide, Raw<bf16>& r) {
+  if (wide) {
+    const uint4 q = AGN_LD(reinterpret_cast<const uint4*>(p));
+    r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = 2 * i < n ? AGN_LD(reinterpret_cast<const uint16_t*>(p) + 2 * i) : 0;
+      const uint32_t hi = 2 * i + 1 < n ? AGN_LD(reinterpret_cast<const uint16_t*>(p) + 2 * i + 1) : 0;
+      r.w[i] = hi << 16 | lo;
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw<T>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    x[i] = __uint_as_float(sizeof(T) == 4 ? r.w[i % (sizeof(r.w) / 4)] : i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+}
 __device__ __forceinline__ uint2 load8_codes(const uint8_t* p, int n, bool wide) {
-  if (wide && n == 8) return AGN_LD(reinterpret_cast<const uint2*>(p));
+  if (wide) return AGN_LD(reinterpret_cast<const uint2*>(p));
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -123,26 +142,32 @@ __device__ __forceinline__ uint2 load8_codes(const uint8_t* p, int n, bool wide)
   return make_uint2(w[0], w[1]);
 }
 __device__ __forceinline__ void store8_codes(uint8_t* p, int n, bool wide, const uint32_t (&c)[8]) {
-  if (wide && n == 8) {
-    AGN_ST(reinterpret_cast<uint2*>(p), make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
-                                                   c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24));
+  if (wide) {
+    auto four = [&](int i) {   // their low bytes
+      return __byte_perm(__byte_perm(c[i], c[i + 1], 0x0040), __byte_perm(c[i + 2], c[i + 3], 0x0040), 0x5410);
+    };
+    AGN_ST(reinterpret_cast<uint2*>(p), make_uint2(four(0), four(4)));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) AGN_ST(p + i, (uint8_t)c[i]);
   }
 }
+// Code i of eight, in the upper byte (the lower ones are 0).
 __device__ __forceinline__ uint32_t code_at(uint2 q, int i) {
-  return ((i < 4 ? q.x : q.y) >> (8 * (i & 3))) & 255u;
+  return __byte_perm(i < 4 ? q.x : q.y, 0, (i & 3) << 12 | 0x444);
 }
 
-// The magnitude of a code: its exponent and mantissa lie where a float's do, 112 exponents lower
-// (so a code with exponent 0 is a subnormal float, its product with 2^112 exact).
-template <int kMant>
+// The magnitude of a code (in the upper byte): its exponent and mantissa lie where a float's do, 112
+// exponents lower (so a code with exponent 0 is a subnormal float, its product with 2^112 exact).  kOnce:
+// `scale` has the factor 2^112 in it, which fits scales up to 2^15.
+template <int kMant, bool kOnce>
 __device__ __forceinline__ float decode(uint32_t code, float scale) {
-  return __fmul_rn(__fmul_rn(__uint_as_float(code << (23 - kMant)), 0x1p112f), scale);
+  const float u = __uint_as_float(code >> (kMant + 1));
+  return kOnce ? __fmul_rn(u, scale) : __fmul_rn(__fmul_rn(u, 0x1p112f), scale);
 }
 __device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e << 23); }
+constexpr uint32_t kOnceMost = 141;   // scale bytes whose factors with 2^112 and 2^-112 are floats
 
 // The scale of a block whose largest magnitude has the bits `top`: the power of two that brings it
 // into [1, 2 - 2^-kMant], the largest code's value.
@@ -150,95 +175,107 @@ template <int kMant>
 __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
   return min(max((top + ((1u << (23 - kMant)) - 1)) >> 23, 1u), 253u);
 }
-// The code of x >= 0: up to the next one where the fraction left and (bits + 1/2) / 65536 reach one.
-template <int kMant>
+// The code of x >= 0: up to the next one where the fraction left and (bits + 1/2) / 65536 reach one.  kOnce:
+// `inverse` has the factor 2^-112 in it, and no value is above the largest code's.
+template <int kMant, bool kOnce>
 __device__ __forceinline__ uint32_t encode(float x, float inverse, uint32_t bits) {
-  const float u = __fmul_rn(__fmul_rn(x, inverse), 0x1p-112f);
+  const float u = kOnce ? __fmul_rn(x, inverse) : __fmul_rn(__fmul_rn(x, inverse), 0x1p-112f);
   constexpr int shift = 23 - kMant;
-  return min((__float_as_uint(u) + (bits << (shift - 16)) + (1u << (shift - 17))) >> shift,
-             (16u << kMant) - 1);
+  const uint32_t code = (__float_as_uint(u) + (bits << (shift - 16)) + (1u << (shift - 17))) >> shift;
+  return kOnce ? code : min(code, (16u << kMant) - 1);
 }
 
-template <int kBits>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const StepArgs a) {
-  pdl_begin();
-  float s = 1.f;
-  if (a.scale) {
-    s = AGN_LD(a.scale);
-    if (!(fabsf(s) <= FLT_MAX)) return;
-  }
-  for (int c = blockIdx.x; c < a.n_pieces; c += gridDim.x) {
-    const Piece piece = AGN_LD(a.pieces + c);
-    const Tensor t = AGN_LD(a.tensors + piece.tensor);
-    const int64_t e = (int64_t)piece.index * kPiece + threadIdx.x * kPer;
+// m, sqrt(v) and the parameter after the step; v is given and left as sqrt(v)'s square (8 bits) or itself.
+__device__ __forceinline__ void step_one(const StepArgs& a, float g, float keep, float& p, float& m, float& v, float& r) {
+  m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.ob1));
+  v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.ob2));
+  r = __fsqrt_rn(v);
+  const float q = __fdividef(m, __fadd_rn(__fmul_rn(r, a.rc2), a.eps));
+  p = __fsub_rn(__fmul_rn(p, keep), __fmul_rn(q, a.size));
+}
+
+// Pieces `index` to `end` - 1 of a tensor.
+template <int kBits, typename G>
+__device__ __forceinline__ void step_pieces(const StepArgs& a, const Tensor& t, float s, int64_t index, int64_t end) {
+  const float keep = (float)__dsub_rn(1.0, __dmul_rn(a.lr, t.decay));
+  for (; index < end; ++index) {
+    const int64_t e = index * kPiece + threadIdx.x * kPer;
     const int n = (int)max((int64_t)0, min((int64_t)kPer, t.n - e));
-    const bool wide = t.wide;
+    const bool wide = t.wide && n == kPer;
+    // (what is not there is loaded as zeros, whose states and codes are zeros)
     float g[8], p[8], m[8], v[8];
-    uint2 qm = make_uint2(0, 0), qv = make_uint2(0, 0);
-    float sm = 0.f, sv = 0.f;
-    if (n > 0) {
-      if (t.bf16_grad) load8(static_cast<const bf16*>(t.grad) + e, n, wide, g);
-      else load8(static_cast<const float*>(t.grad) + e, n, wide, g);
-      load8(t.param + e, n, wide, p);
-      if (kBits == 8) {
-        qm = load8_codes(static_cast<const uint8_t*>(t.m) + e, n, wide);
-        qv = load8_codes(static_cast<const uint8_t*>(t.v) + e, n, wide);
-        sm = scale_value(AGN_LD(t.ms + e / kBlock));
-        sv = scale_value(AGN_LD(t.vs + e / kBlock));
-      } else {
-        load8(static_cast<const float*>(t.m) + e, n, wide, m);
-        load8(static_cast<const float*>(t.v) + e, n, wide, v);
+    Raw<G> raw;
+    uint2 qm, qv;
+    uint32_t em = 0, er = 0;
+    load8(static_cast<const G*>(t.grad) + e, n, wide, raw);
+    load8(t.param + e, n, wide, p);
+    if (kBits == 8) {
+      qm = load8_codes(static_cast<const uint8_t*>(t.m) + e, n, wide);
+      qv = load8_codes(static_cast<const uint8_t*>(t.v) + e, n, wide);
+      if (n > 0) {
+        em = AGN_LD(t.ms + e / kBlock);
+        er = AGN_LD(t.vs + e / kBlock);
       }
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = p[i] = m[i] = v[i] = 0.f;
+      load8(static_cast<const float*>(t.m) + e, n, wide, m);
+      load8(static_cast<const float*>(t.v) + e, n, wide, v);
     }
-    const float keep = (float)__dsub_rn(1.0, __dmul_rn(a.lr, t.decay));
-    float r[8];
-    uint32_t top_m = 0, top_r = 0;
+    unpack8(raw, g);
+    if (a.scale) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float gi = a.scale ? __fmul_rn(g[i], s) : g[i];
-      if (kBits == 8) {
-        const uint32_t cm = code_at(qm, i);
-        m[i] = decode<kMantM>(cm & 127u, sm);
-        m[i] = cm & 128u ? -m[i] : m[i];
-        const float root = decode<kMantR>(code_at(qv, i), sv);
-        v[i] = __fmul_rn(root, root);
-      }
-      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(gi, a.ob1));
-      v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(gi, gi), a.ob2));
-      r[i] = __fsqrt_rn(v[i]);
-      const float q = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(r[i], a.rc2), a.eps));
-      p[i] = __fsub_rn(__fmul_rn(p[i], keep), __fmul_rn(q, a.size));
-      if (kBits == 8) {
-        if (i >= n) m[i] = r[i] = 0.f;
+      for (int i = 0; i < 8; ++i) g[i] = __fmul_rn(g[i], s);
+    }
+    float r[8];
+    if (kBits == 8) {
+      auto values = [&](auto once) {
+        constexpr bool kOnce = decltype(once)::value;
+        const float sm = scale_value(kOnce && em ? em + 112 : em), sr = scale_value(kOnce && er ? er + 112 : er);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t cm = code_at(qm, i);
+          m[i] = __uint_as_float(__float_as_uint(decode<kMantM, kOnce>(cm & 0x7f000000u, sm)) | (cm & 0x80000000u));
+          const float root = decode<kMantR, kOnce>(code_at(qv, i), sr);
+          v[i] = __fmul_rn(root, root);
+        }
+      };
+      if (__any_sync(0xffffffffu, max(em, er) > kOnceMost)) values(std::false_type());
+      else values(std::true_type());
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) step_one(a, g[i], keep, p[i], m[i], v[i], r[i]);
+    if (kBits == 8) {
+      uint32_t top_m = 0, top_r = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
         top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu);
         top_r = max(top_r, __float_as_uint(r[i]) & 0x7fffffffu);
       }
-    }
-    if (kBits == 8) {
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1) {
         top_m = max(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
         top_r = max(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
       }
-      const uint32_t em = scale_code<kMantM>(top_m), er = scale_code<kMantR>(top_r);
-      const float im = scale_value(254u - em), ir = scale_value(254u - er);
+      em = scale_code<kMantM>(top_m), er = scale_code<kMantR>(top_r);
       const uint64_t d0 = a.key + (a.offset + t.first + (uint64_t)(e / 2) + 1) * gen::kG;
       uint32_t cm[8], cr[8];
+      auto codes = [&](auto once) {
+        constexpr bool kOnce = decltype(once)::value;
+        const float im = scale_value((kOnce ? 142u : 254u) - em), ir = scale_value((kOnce ? 142u : 254u) - er);
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {   // a draw for two elements: 16 bits for m, 16 for sqrt(v)
-        const uint64_t d = gen::mix(d0 + (uint64_t)h * gen::kG);
+        for (int h = 0; h < 4; ++h) {   // a draw for two elements: 16 bits for m, 16 for sqrt(v)
+          const uint64_t d = gen::mix(d0 + (uint64_t)h * gen::kG);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int i = 2 * h + k;
-          const uint32_t w = (uint32_t)(d >> (32 * k));
-          cm[i] = encode<kMantM>(fabsf(m[i]), im, w & 0xffffu) | (__float_as_uint(m[i]) >> 31) << 7;
-          cr[i] = encode<kMantR>(r[i], ir, w >> 16);
-          if (r[i] > 0.f) cr[i] = max(cr[i], 1u);   // m / eps would follow
+          for (int k = 0; k < 2; ++k) {
+            const int i = 2 * h + k;
+            const uint32_t w = (uint32_t)(d >> (32 * k));
+            cm[i] = encode<kMantM, kOnce>(fabsf(m[i]), im, w & 0xffffu) | (__float_as_uint(m[i]) >> 24 & 0x80u);
+            cr[i] = encode<kMantR, kOnce>(r[i], ir, w >> 16);
+            if (r[i] > 0.f) cr[i] = max(cr[i], 1u);   // m / eps would follow
+          }
         }
-      }
+      };
+      if (__any_sync(0xffffffffu, max(em, er) > kOnceMost)) codes(std::false_type());
+      else codes(std::true_type());
       if (n > 0) {
         store8_codes(static_cast<uint8_t*>(t.m) + e, n, wide, cm);
         store8_codes(static_cast<uint8_t*>(t.v) + e, n, wide, cr);
@@ -258,57 +295,101 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const StepArgs a) {
   }
 }
 
-// Squares in fp32, a thread's sums of up to 64 of them, then doubles: per block, then over the
-// blocks in order.
-__global__ void __launch_bounds__(kThreads)
-norm_kernel(const Tensor* tensors, const Piece* pieces, int n_pieces, double* partials) {
+template <int kBits>
+__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const StepArgs a) {
   pdl_begin();
-  double sum = 0.0;
-  float part = 0.f;
-  int held = 0;
-  for (int c = blockIdx.x; c < n_pieces; c += gridDim.x) {
-    const Piece piece = AGN_LD(pieces + c);
-    const Tensor* t = tensors + piece.tensor;
-    const int64_t e = (int64_t)piece.index * kPiece + threadIdx.x * kPer;
-    const int n = (int)max((int64_t)0, min((int64_t)kPer, AGN_LD(&t->n) - e));
-    if (n <= 0) continue;
-    const void* grad = AGN_LD(&t->grad);
-    const bool wide = AGN_LD(&t->wide);
-    float g[8];
-    if (AGN_LD(&t->bf16_grad)) load8(static_cast<const bf16*>(grad) + e, n, wide, g);
-    else load8(static_cast<const float*>(grad) + e, n, wide, g);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) part = fmaf(g[i], g[i], part);
-    if (++held == 8) {
-      sum += (double)part;
-      part = 0.f;
-      held = 0;
-    }
+  float s = 1.f;
+  if (a.scale) {
+    s = AGN_LD(a.scale);
+    if (!(fabsf(s) <= FLT_MAX)) return;
   }
-  sum += (double)part;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  __shared__ double warps[kThreads / 32];
-  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 32; ++w) sum += warps[w];
-    AGN_ST(partials + blockIdx.x, sum);
+  // A block's pieces are consecutive, and a tensor's among them a run that needs no look at the list.
+  const int last = (int)((int64_t)a.n_pieces * (blockIdx.x + 1) / gridDim.x);
+  for (int c = (int)((int64_t)a.n_pieces * blockIdx.x / gridDim.x); c < last;) {
+    const Piece piece = AGN_LD(a.pieces + c);
+    const Tensor t = AGN_LD(a.tensors + piece.tensor);
+    const int64_t end = min((int64_t)piece.index + last - c, (t.n + kPiece - 1) / kPiece);
+    if (t.bf16_grad) step_pieces<kBits, bf16>(a, t, s, piece.index, end);
+    else step_pieces<kBits, float>(a, t, s, piece.index, end);
+    c += (int)(end - piece.index);
   }
 }
 
+// Squares and a thread's sums of up to 32 of them in fp32, those with the rounding's remainder carried along;
+// a warp's 32 in fp32, the rest in 64 bits (an SM adds few of those: sums of threads took most of the time).
+constexpr int kNormPieces = 4;   // in flight
 __global__ void __launch_bounds__(kThreads)
-norm_finish_kernel(const double* partials, int n, double max_norm, float* norm, float* scale) {
+norm_kernel(const Tensor* tensors, const Piece* pieces, int n_pieces, double* partials) {
   pdl_begin();
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < n; i += kThreads) sum += AGN_LD(partials + i);
+  float sum = 0.f, rest = 0.f;
+  auto add = [&](float part) {   // (Knuth's two-sum)
+    const float both = __fadd_rn(sum, part), back = __fsub_rn(both, sum);
+    rest = __fadd_rn(rest, __fadd_rn(__fsub_rn(sum, __fsub_rn(both, back)), __fsub_rn(part, back)));
+    sum = both;
+  };
+  auto squares = [&](auto kind, const Tensor& t, int64_t index, int64_t end) {
+    using G = decltype(kind);
+    const G* grad = static_cast<const G*>(t.grad);
+    // whole pieces, four in flight; then one by one
+    const int64_t whole = t.wide ? min(end, t.n / kPiece) : 0;
+    for (; index + kNormPieces <= whole; index += kNormPieces) {
+      const int64_t e = index * kPiece + threadIdx.x * kPer;
+      Raw<G> raw[kNormPieces];
+#pragma unroll
+      for (int k = 0; k < kNormPieces; ++k) load8(grad + e + k * kPiece, kPer, true, raw[k]);
+      float part = 0.f;
+#pragma unroll
+      for (int k = 0; k < kNormPieces; ++k) {
+        float g[8];
+        unpack8(raw[k], g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part = fmaf(g[i], g[i], part);
+      }
+      add(part);
+    }
+    for (; index < end; ++index) {
+      const int64_t e = index * kPiece + threadIdx.x * kPer;
+      const int n = (int)max((int64_t)0, min((int64_t)kPer, t.n - e));
+      if (n <= 0) continue;
+      Raw<G> raw;
+      load8(grad + e, n, t.wide && n == kPer, raw);
+      float g[8], part = 0.f;
+      unpack8(raw, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part = fmaf(g[i], g[i], part);
+      add(part);
+    }
+  };
+  const int last = (int)((int64_t)n_pieces * (blockIdx.x + 1) / gridDim.x);
+  for (int c = (int)((int64_t)n_pieces * blockIdx.x / gridDim.x); c < last;) {
+    const Piece piece = AGN_LD(pieces + c);
+    const Tensor t = AGN_LD(tensors + piece.tensor);
+    const int64_t end = min((int64_t)piece.index + last - c, (t.n + kPiece - 1) / kPiece);
+    if (t.bf16_grad) squares(bf16(), t, piece.index, end);
+    else squares(float(), t, piece.index, end);
+    c += (int)(end - piece.index);
+  }
+  if (fabsf(sum) <= FLT_MAX) sum += rest;   // (an infinite sum's remainder is NaN)
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  __shared__ double warps[kThreads / 32];
+  __shared__ float warps[kThreads / 32];
   if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 32; ++w) sum += warps[w];
+    double all = warps[0];
+    for (int w = 1; w < kThreads / 32; ++w) all += (double)warps[w];
+    AGN_ST(partials + blockIdx.x, all);
+  }
+}
+
+__global__ void __launch_bounds__(32)
+norm_finish_kernel(const double* partials, int n, double max_norm, float* norm, float* scale) {
+  pdl_begin();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < n; i += 32) sum += AGN_LD(partials + i);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (threadIdx.x == 0) {
     const float total = (float)sqrt(sum), most = (float)max_norm;
     if (norm) AGN_ST(norm, total);
     if (scale)
@@ -324,24 +405,24 @@ dequantize_kernel(const uint8_t* m, const uint8_t* ms, const uint8_t* v, const u
   const int64_t step = (int64_t)gridDim.x * kPiece;
   for (int64_t e = (int64_t)blockIdx.x * kPiece + threadIdx.x * kPer; e < n; e += step) {
     const int k = (int)min((int64_t)kPer, n - e);
+    const bool whole = wide && k == kPer;
     float x[8];
     if (m_out) {
-      const uint2 q = load8_codes(m + e, k, wide);
+      const uint2 q = load8_codes(m + e, k, whole);
       const float s = scale_value(AGN_LD(ms + e / kBlock));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t c = code_at(q, i);
-        x[i] = decode<kMantM>(c & 127u, s);
-        x[i] = c & 128u ? -x[i] : x[i];
+        x[i] = __uint_as_float(__float_as_uint(decode<kMantM, false>(c & 0x7f000000u, s)) | (c & 0x80000000u));
       }
-      store8(m_out + e, k, wide, x);
+      store8(m_out + e, k, whole, x);
     }
     if (r_out) {
-      const uint2 q = load8_codes(v + e, k, wide);
+      const uint2 q = load8_codes(v + e, k, whole);
       const float s = scale_value(AGN_LD(vs + e / kBlock));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = decode<kMantR>(code_at(q, i), s);
-      store8(r_out + e, k, wide, x);
+      for (int i = 0; i < 8; ++i) x[i] = decode<kMantR, false>(code_at(q, i), s);
+      store8(r_out + e, k, whole, x);
     }
   }
 }
@@ -378,13 +459,13 @@ namespace {
 // Bounds-checked build: a plan's buffers and tables are known while a call lasts.
 struct KnownPlan {
   std::vector<const void*> p;
-  void add(const void* q, size_t bytes) {
-    if (!q || !bytes) return;
-    bounds_add(q, bytes);
-    p.push_back(q);
-  }
   explicit KnownPlan(const agn_optim& o) {
 #ifdef AGN_BOUNDS_CHECK
+    auto add = [&](const void* q, size_t bytes) {
+      if (!q || !bytes) return;
+      bounds_add(q, bytes);
+      p.push_back(q);
+    };
     for (const CallBuffer& b : o.buffers) add(b.p, b.bytes);
     // (tables are not a caller's: the checker's self-test does not shorten them)
     add(o.d_tensors, (size_t)o.tensors * sizeof(Tensor) + 256);
@@ -488,7 +569,7 @@ Status optim_create(const agn_optim_tensor* ts, int32_t n_tensors, int32_t bits,
   AGN_TRY(device_sms(o->device, &sms));
   o->tensors = (int64_t)host.size();
   o->pieces = (int)pieces.size();
-  o->norm_grid = std::max(1, std::min({o->pieces, kMostGrid, 8 * sms}));
+  o->norm_grid = std::max(1, std::min({(int)ceil_div(o->pieces, kNormPieces), kMostGrid, 4 * sms}));
   AGN_TRY_CUDA(cudaMalloc(&o->d_tensors, host.size() * sizeof(Tensor) + 256));
   AGN_TRY_CUDA(cudaMalloc(&o->d_pieces, pieces.size() * sizeof(Piece) + 256));
   AGN_TRY_CUDA(cudaMalloc(&o->d_partials, (size_t)o->norm_grid * sizeof(double) + 256));
@@ -535,7 +616,7 @@ Status optim_norm(agn_optim* o, double max_norm, float* norm, float* scale, cuda
   AGN_TRY(bounds_upload(st));
   AGN_TRY_CUDA(launch_pdl(norm_kernel, dim3((unsigned)o->norm_grid), dim3(kThreads), 0, st,
                           (const Tensor*)o->d_tensors, (const Piece*)o->d_pieces, o->pieces, o->d_partials));
-  AGN_TRY_CUDA(launch_pdl(norm_finish_kernel, dim3(1), dim3(kThreads), 0, st, (const double*)o->d_partials,
+  AGN_TRY_CUDA(launch_pdl(norm_finish_kernel, dim3(1), dim3(32), 0, st, (const double*)o->d_partials,
                           o->norm_grid, max_norm, norm, scale));
   return bounds_collect(st);
 }
