@@ -85,7 +85,7 @@ def test_host_memory_is_refused(agn, call):
 
 @pytest.mark.parametrize("dtype", [0, 1])
 def test_scratch(agn, dtype):
-    """It grows with the sizes' smooth parts only: p's buffer is bounded, no logits are kept."""
+    """x packed (backward twice: along its rows too), dx's sums, and p's bounded buffer: no logits are kept."""
     for k in (0, 1):
         with pytest.raises(agn.AGNError):
             agn.agn_linear_ce_bytes(-1, 8, 8, dtype, k)
@@ -98,7 +98,7 @@ def test_scratch(agn, dtype):
         packed = x * (rows + 256) * (inner + 64) + (100 * MB if dtype == 0 else 0)
         logits = rows * classes
         assert fwd <= packed + logits / 8 + 16 * rows + pad
-        assert bwd <= packed + dx * (rows + 256) * (inner + 64) + max(130 * MB, (rows + 256) * 1024 * es * 1.5) * 1.25 + 65 * MB + pad
+        assert bwd <= packed + x * (rows + 256) * (inner + 64) + dx * (rows + 256) * (inner + 64) + max(130 * MB, (rows + 256) * 1024 * es * 1.5) * 1.25 + 65 * MB + pad
     assert agn._lib.load().agn_linear_ce_bytes(1, 1, 1, 0, 0, None) == agn.AGN_E_INVALID
 
 
