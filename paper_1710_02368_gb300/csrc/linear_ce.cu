@@ -497,56 +497,86 @@ join_kernel(const float2* ms, int halves, int64_t ld, int rows_a_block, const fl
   }
 }
 
-// dbias[c] = the sums of 32 rows each, in order: 32 columns a block, its warps share them.
-__global__ void __launch_bounds__(1024)
-columns_kernel(const float* db, int64_t ld, int cols, const int* live_p, float* out) {
-  pdl_begin();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int blocks = (AGN_LD(live_p) + 31) / 32, c = blockIdx.x * 32 + lane;
-  __shared__ float part[32][33];
-  float s = 0.f;
-  if (c < cols)
-    for (int b = warp; b < blocks; b += warps) s += AGN_LD(db + b * ld + c);
-  part[warp][lane] = s;
-  __syncthreads();
-  if (warp != 0 || c >= cols) return;
-  for (int j = 1; j < warps; ++j) s += part[j][lane];
-  AGN_ST(out + c, s);
-}
-
-// out[idx[m]][n] = the sum of the ranges' sums, in order (idx null: row m).
+// What a piece leaves to be added up, a launch for all of it.
+constexpr int kSumThreads = 1024;   // (16384 rows have 512 sums of 32 a column: 8 warps took 3 us more)
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
-ranges_kernel(const float* part, int splits, int64_t plane, int64_t ld, int64_t rows, int cols, const int* idx,
-              const int* live_p, T* out, bool vec) {
-  pdl_begin();
-  const int64_t first = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
-  const int groups = (cols + 3) / 4;
-  if (idx) rows = AGN_LD(live_p);
-  for (int64_t i = first; i < rows * groups; i += step) {
+struct Ranges {   // out[idx[m]][n] = the sum of the ranges' sums, in order (idx null: row m)
+  const float* part;
+  int splits;
+  int64_t plane, ld, rows;
+  int cols;
+  const int* idx;
+  T* out;
+  bool vec;
+  int blocks;     // of the launch
+};
+struct Columns {  // out[c] = the sums of 32 rows each, in order
+  const float* db;
+  int64_t ld;
+  int cols;
+  float* out;
+  int blocks;
+};
+
+template <typename T>
+__device__ __forceinline__ void sum_ranges(const Ranges<T>& a, int block, int live) {
+  const int64_t rows = a.idx ? live : a.rows;
+  const int groups = (a.cols + 3) / 4;
+  const int64_t step = (int64_t)a.blocks * kSumThreads;
+  for (int64_t i = (int64_t)block * kSumThreads + threadIdx.x; i < rows * groups; i += step) {
     const int64_t r = i / groups;
     const int c = (int)(i - r * groups) * 4;
-    const float* p = part + r * ld + c;
+    const float* p = a.part + r * a.ld + c;
     float4 s = AGN_LD(reinterpret_cast<const float4*>(p));
-    for (int k = 1; k < splits; ++k) {
-      const float4 v = AGN_LD(reinterpret_cast<const float4*>(p + k * plane));
+#pragma unroll 4
+    for (int k = 1; k < a.splits; ++k) {
+      const float4 v = AGN_LD(reinterpret_cast<const float4*>(p + k * a.plane));
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
-    const int64_t to = (idx ? (int64_t)AGN_LD(idx + r) : r) * cols + c;
+    const int64_t to = (a.idx ? (int64_t)AGN_LD(a.idx + r) : r) * a.cols + c;
     const float v[4] = {s.x, s.y, s.z, s.w};
-    if (vec && c + 4 <= cols) {
+    if (a.vec && c + 4 <= a.cols) {
       if (sizeof(T) == 4) {
-        AGN_ST(reinterpret_cast<float4*>(out + to), s);
+        AGN_ST(reinterpret_cast<float4*>(a.out + to), s);
       } else {
         const __nv_bfloat162 o[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
-        AGN_ST(reinterpret_cast<uint2*>(out + to), *reinterpret_cast<const uint2*>(o));
+        AGN_ST(reinterpret_cast<uint2*>(a.out + to), *reinterpret_cast<const uint2*>(o));
       }
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (c + k < cols) from_float(out + to + k, v[k]);
+        if (c + k < a.cols) from_float(a.out + to + k, v[k]);
     }
   }
+}
+
+// 32 columns a block, whose warps share the blocks of rows.
+__device__ __forceinline__ void sum_columns(const Columns& a, int block, int live) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kSumThreads / 32;
+  const int blocks = (live + 31) / 32, c = block * 32 + lane;
+  __shared__ float part[kSumThreads / 32][33];
+  float s = 0.f;
+  if (c < a.cols) {
+#pragma unroll 4
+    for (int b = warp; b < blocks; b += warps) s += AGN_LD(a.db + b * a.ld + c);
+  }
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || c >= a.cols) return;
+  for (int j = 1; j < warps; ++j) s += part[j][lane];
+  AGN_ST(a.out + c, s);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSumThreads)
+sums_kernel(const Columns db, const Ranges<T> dw, const Ranges<T> dx, const int* live_p) {
+  pdl_begin();
+  const int live = AGN_LD(live_p);
+  int block = blockIdx.x;
+  if (block < db.blocks) return sum_columns(db, block, live);
+  block -= db.blocks;
+  if (block < dw.blocks) return sum_ranges(dw, block, live);
+  sum_ranges(dx, block - dw.blocks, live);
 }
 
 // ---- small problems: a warp a row, fp32 arithmetic
@@ -866,11 +896,10 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
 }
 
 template <typename T>
-Status sum_ranges(const float* part, int splits, int64_t plane, int64_t ld, int64_t rows, int64_t cols, const int* idx,
-                  const int* live, T* out, cudaStream_t st) {
+Ranges<T> ranges(const void* part, int splits, int64_t plane, int64_t ld, int64_t rows, int64_t cols, const int* idx, T* out) {
   const bool vec = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
-  return run(ranges_kernel<T>, dim3(grid_for(rows * ceil_div(cols, 4), kThreads)), kThreads, 0, st, part, splits,
-             plane, ld, rows, (int)cols, idx, live, out, vec);
+  return {static_cast<const float*>(part), splits, plane, ld, rows, (int)cols, idx, out, vec,
+          (int)grid_for(rows * ceil_div(cols, 4), kSumThreads)};
 }
 
 template <typename T>
@@ -911,10 +940,6 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
     a.db = c.dbias ? db : nullptr;
     a.ld_db = l.ldp;
     AGN_TRY(gemm(l.z.ctas, kGrad, z, logit_units(c, l, n), st));
-    if (c.dbias)
-      AGN_TRY(run(columns_kernel, dim3((unsigned)ceil_div(n, 32)),
-                  32 * (int)std::min<int64_t>(32, l.rows_pad / 128), 0, st, (const float*)db, l.ldp, (int)n, live,
-                  c.dbias + c0));
     T* dw_out = static_cast<T*>(c.dw) + c0 * inner;
     int64_t dw_units = 0, dx_units = 0;
     if (c.dw) {   // [n][inner] = p^T x
@@ -969,13 +994,16 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       if (c.dw) AGN_TRY(gemm(cw.ctas, kOut, dw, dw_units, st));
       if (c.dx) AGN_TRY(gemm(cx.ctas, kOut, dx, dx_units, st));
     }
+    Columns columns{};
+    Ranges<T> rw{}, rx{};
+    if (c.dbias) columns = {db, l.ldp, (int)n, c.dbias + c0, (int)ceil_div(n, 32)};
     if (c.dw && l.dw_splits > 1)
-      AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dws), l.dw_splits, dw_rows * ldn, ldn, n, inner,
-                         (const int*)nullptr, (const int*)nullptr, dw_out, st));
+      rw = ranges<T>(c.work + l.dws, l.dw_splits, dw_rows * ldn, ldn, n, inner, nullptr, dw_out);
+    if (c.dx && l.dx_part && c0 + n == c.s.classes)
+      rx = ranges<T>(c.work + l.dxs, l.dx_splits, l.rows_pad * ldn, ldn, rows, inner, idx, static_cast<T*>(c.dx));
+    const int blocks = columns.blocks + rw.blocks + rx.blocks;
+    if (blocks > 0) AGN_TRY(run(sums_kernel<T>, dim3((unsigned)blocks), kSumThreads, 0, st, columns, rw, rx, live));
   }
-  if (c.dx && l.dx_part)
-    AGN_TRY(sum_ranges(reinterpret_cast<const float*>(c.work + l.dxs), l.dx_splits, l.rows_pad * ldn, ldn, rows,
-                       inner, idx, live, static_cast<T*>(c.dx), st));
   return Status::Ok();
 }
 
