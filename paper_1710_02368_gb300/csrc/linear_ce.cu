@@ -871,7 +871,9 @@ Status run_few(const Call& c, const Layout& l, bool backward_call, cudaStream_t 
 
 template <typename T>
 Status forward(const Call& c, const Layout& l, cudaStream_t st) {
-  AGN_TRY(prepare<T>(c, l, st));
+  // One tile of rows is read as it is: rows without a label cost nothing more and are their own alone (3 us).
+  const bool as_is = l.direct && c.s.rows <= 128;
+  if (!as_is) AGN_TRY(prepare<T>(c, l, st));
   float2* ms = reinterpret_cast<float2*>(c.work + l.ms);
   float* zlab = reinterpret_cast<float*>(c.work + l.zlab);
   GemmLaunch g{};
@@ -888,10 +890,14 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
     g.args[0].ld_ms = l.halves;
     g.args[0].ms0 = (int)half;
     g.args[0].zlab = zlab;
+    if (as_is) {
+      g.args[0].live = nullptr;
+      g.args[0].idx = nullptr;
+    }
     AGN_TRY(gemm(l.z.ctas, kLse, g, logit_units(c, l, n), st));
     half += 2 * ceil_div(n, l.z.bn);
   }
-  return join_rows(c, ms, half, zlab, reinterpret_cast<const int*>(c.work + l.idx),
+  return join_rows(c, ms, half, zlab, as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.idx),
                    reinterpret_cast<const int*>(c.work + l.live), st);
 }
 

@@ -32,7 +32,7 @@ struct GemmArgs {
   int* err;
   uint32_t wait_ns;
   int withhold;             // test hook: CTA withhold - 1 of a tile leaves out its last stage and all after
-  const int* idx;           // [live] places of the rows
+  const int* idx;           // [live] places of the rows, null: their own
   // kLse, kGrad
   const float* bias;        // [classes] or null
   const int* labels;        // [rows]

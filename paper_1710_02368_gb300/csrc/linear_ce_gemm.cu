@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       float lse = 0.f, fa = 0.f, fb = 0.f;
       if (kEpi != kOut) {
         if (live) {
-          const int at = AGN_LD(a.idx + row);
+          const int at = a.idx ? AGN_LD(a.idx + row) : row;
           label = AGN_LD(a.labels + at) - a.class0 - col0;
           if (kEpi == kGrad) {
             lse = AGN_LD(a.lse + at);
