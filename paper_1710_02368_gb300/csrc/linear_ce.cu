@@ -415,19 +415,40 @@ transpose_kernel(const T* x, int inner, const int* idx, const int* live_p, bf16*
   constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
   __shared__ bf16 tile[kPlanes][64][66];   // [column][row]
   const int live = AGN_LD(live_p), tiles_r = (live + 63) / 64, tiles_c = (inner + 63) / 64;
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  constexpr int kVec = 16 / (int)sizeof(T), kPieces = 64 / kVec;   // 16 bytes of a row a thread
+  const bool vec = inner % kVec == 0;
   for (int64_t t = blockIdx.x; t < (int64_t)tiles_r * tiles_c; t += gridDim.x) {
     const int r0 = (int)(t / tiles_c) * 64, c0 = (int)(t % tiles_c) * 64;
     __syncthreads();
-#pragma unroll 4
-    for (int r = ty; r < 64; r += 4) {
-      float v = 0.f;
-      if (r0 + r < live && c0 + tx < inner) v = to_float(AGN_LD(x + (int64_t)AGN_LD(idx + r0 + r) * inner + c0 + tx));
-      bf16 q[3];
-      if (kPlanes == 3) split3(v, q[0], q[1], q[2]);
-      else q[0] = __float2bfloat16_rn(v);
+    uint4 raw[kPieces / 4];
 #pragma unroll
-      for (int p = 0; p < kPlanes; ++p) tile[p][tx][r] = q[p];
+    for (int j = 0; j < kPieces / 4; ++j) {
+      const int i = j * kThreads + threadIdx.x, r = i / kPieces, c = i % kPieces * kVec;
+      alignas(16) T e[kVec] = {};
+      if (r0 + r < live && c0 + c < inner) {
+        const T* p = x + (int64_t)AGN_LD(idx + r0 + r) * inner + c0 + c;
+        if (vec) {
+          *reinterpret_cast<uint4*>(e) = AGN_LD(reinterpret_cast<const uint4*>(p));
+        } else {
+          for (int k = 0; k < kVec; ++k)
+            if (c0 + c + k < inner) e[k] = AGN_LD(p + k);
+        }
+      }
+      raw[j] = *reinterpret_cast<const uint4*>(e);
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces / 4; ++j) {
+      const int i = j * kThreads + threadIdx.x, r = i / kPieces, c = i % kPieces * kVec;
+      const T* e = reinterpret_cast<const T*>(&raw[j]);
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        const float v = to_float(e[k]);
+        bf16 q[3];
+        if (kPlanes == 3) split3(v, q[0], q[1], q[2]);
+        else q[0] = __float2bfloat16_rn(v);
+#pragma unroll
+        for (int p = 0; p < kPlanes; ++p) tile[p][c + k][r] = q[p];
+      }
     }
     __syncthreads();
 #pragma unroll
