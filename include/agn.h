@@ -546,7 +546,9 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
  *   err     : device int32, NULL = none: set to 1 (never cleared) when a bounded wait gave up (2 s); values that
  *             could not be computed are NaN.
  * rows 0 .. 2^28, inner 1 .. 2^20, classes 1 .. 2^28.  bf16 rows of a multiple of 8 elements are read as
- * they are, others are copied first.  Equal calls give equal bits.  Queued on `stream`, may be captured.
+ * they are, others are copied first.  No output, nor work, shares bytes with another buffer.  Equal calls
+ * give equal bits.  Queued on `stream`, may be captured.  fp32 values of 3.39e38 and more, and infinities, have
+ * no pieces and give NaN.
  * agn_linear_ce_bytes needs no GPU.  Errors: AGN_E_INVALID, AGN_E_CUDA.
  */
 int agn_linear_ce_bytes(int64_t rows, int64_t inner, int64_t classes, int32_t dtype, int32_t backward,

@@ -172,6 +172,18 @@ def test_pieces_of_the_classes(agn, dtype, rows, ignored):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("inner", [16, 13])
+@pytest.mark.parametrize("ignored", [0.0, 0.4])
+def test_more_rows_than_one_launch_prepares(agn, dtype, inner, ignored):
+    rows = 40_001
+    x, w, b, labels = make(rows, inner, 37, dtype, ignored=ignored)
+    out = (labels < 0) | (labels >= 37)
+    x[out] = math.nan
+    _, _, got = check(agn, x, w, b, labels, dtype, scale=1.0 / rows)
+    assert torch.all(got["dx"][out] == 0)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 def test_outputs_not_wanted(agn, dtype):
     for size in ((40, 24, 30), (6, 64, 900), (700, 64, 300)):
         x, w, b, labels = make(*size, dtype)
