@@ -8,7 +8,7 @@
 // and dx += p w of the piece.  Pieces keep p's buffer at 128 MB.
 // Rows without a label cost nothing and may hold anything: the rows with one are counted and, where
 // some are missing, gathered on the device; all sizes that depend on it are read there.
-// Small problems (few rows, w in a few 10 KB) take two plain kernels instead: a warp a row.
+// Small problems (w in a few 10 KB) take plain kernels instead: a block a row.
 #include "linear_ce.cuh"
 
 #include <cfloat>
@@ -109,7 +109,15 @@ Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges) {
   return best;
 }
 
-bool small(const Sizes& s) { return s.rows <= 512 && s.inner * s.classes <= 32768 && s.classes <= 2048; }
+// Plain kernels for small problems, where their estimated time (us: every row reads all of w from the L2, short
+// rows a class a thread) is less than that of the products, whose launches and k steps are one after the other.
+bool small(const Sizes& s, bool backward) {
+  if (s.rows > 1024 || s.classes > 4096 || s.inner * s.classes > 32768) return false;
+  const double each = (double)s.rows * s.inner * s.classes / (s.inner <= 64 ? 0.65e6 : 1.9e6);
+  const double step = s.prec == AGN_PREC_FP32 ? 1.2 : 0.35, k = (double)ceil_div(s.inner, 64);
+  if (!backward) return 3 + each < 8 + step * std::min(k, 12.0);
+  return 5 + 2 * each + s.rows / 32 * 0.2 < 16 + step * std::min(k + (double)(std::max(s.rows, s.classes) / 64), 24.0);
+}
 
 struct Layout {
   int planes;
@@ -118,15 +126,17 @@ struct Layout {
   int64_t rows_pad, piece; // classes of a piece (a multiple of 256, but for one piece of all)
   int64_t pieces, ldp;     // p's row stride
   Cut z;
+  int z_splits;            // more than 1: the logits by ranges of K, in scratch (few tiles with a long K)
+  int64_t ldz;
   int a_box;               // rows of x in a box of the logits' product
   bool both;               // dw and dx are one launch
   Cut grads[2];            // dw, dx (both: the first alone, with two products)
   int dw_splits, dx_splits;
   bool dx_part;
   bool x_t;                // dw reads x laid out along its rows
-  bool few;
+  bool small, few;
   int64_t halves;          // forward: partial (maximum, sum) of a row
-  size_t idx, live, x, xt, w, ms, zlab, p, db, dxs, dws, bytes;
+  size_t idx, live, x, xt, w, zs, ms, zlab, p, db, dxs, dws, bytes;
 };
 
 Layout layout(const Sizes& s, bool backward) {
@@ -141,7 +151,8 @@ Layout layout(const Sizes& s, bool backward) {
     at += (size_t)round_up((int64_t)bytes, 1024);
     return here;
   };
-  if (small(s)) {
+  if (small(s, backward)) {
+    l.small = true;
     if (backward) l.p = take((size_t)s.rows * s.classes * 4);
     l.bytes = std::max<size_t>(at, 1024);
     return l;
@@ -181,10 +192,20 @@ Layout layout(const Sizes& s, bool backward) {
   l.pieces = ceil_div(s.classes, l.piece);
   l.ldp = round_up(l.piece, 64);
   l.z = logits(l.piece);
+  l.z_splits = 1;
+  if (l.pieces == 1) {
+    const Extents e{s.rows, s.classes, s.inner, false};
+    const Cut c = cut(s.rows > 128 ? 2 : 1, l.planes, l.a_box, &e, 1, true);
+    if (c.splits[0] > 1 && c.time < l.z.time) l.z = c, l.z_splits = c.splits[0];
+  }
   l.live = take(4);
   l.idx = take((size_t)l.rows_pad * 4);
   l.x = take((size_t)l.planes * l.rows_pad * l.kp * 2);
   if (!l.direct) l.w = take((size_t)l.planes * l.piece * l.kp * 2);
+  if (l.z_splits > 1) {
+    l.ldz = round_up(s.classes, 64);
+    l.zs = take((size_t)l.z_splits * l.rows_pad * l.ldz * 4);
+  }
   if (!backward) {
     l.halves = 2 * (ceil_div(l.piece, l.z.bn) * (l.pieces - 1) +
                     ceil_div(s.classes - (l.pieces - 1) * l.piece, l.z.bn));
@@ -518,6 +539,124 @@ join_kernel(const float2* ms, int halves, int64_t ld, int rows_a_block, const fl
   }
 }
 
+// ---- logits that lie in scratch as sums of ranges along K
+
+struct Logits {
+  const float* z;           // [splits][rows_pad][ld]
+  int splits;
+  int64_t plane, ld;
+  const float* bias;
+  const int* labels;
+  int classes, rows;
+  const int *idx, *live;    // null: rows are where they were
+};
+
+// Four logits from class c on of row r (past the last class: minus infinity).
+__device__ __forceinline__ void logits4(const Logits& a, int64_t r, int c, float (&v)[4]) {
+  const float* p = a.z + r * a.ld + c;
+  float4 s = AGN_LD(reinterpret_cast<const float4*>(p));
+#pragma unroll 4
+  for (int k = 1; k < a.splits; ++k) {
+    const float4 q = AGN_LD(reinterpret_cast<const float4*>(p + k * a.plane));
+    s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+  }
+  v[0] = s.x; v[1] = s.y; v[2] = s.z; v[3] = s.w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    v[j] = c + j < a.classes ? v[j] + (a.bias ? AGN_LD(a.bias + c + j) : 0.f) : -INFINITY;
+}
+
+// lse and loss, a block a row.
+__global__ void __launch_bounds__(kThreads) logits_loss_kernel(const Logits a, float* loss, float* lse) {
+  pdl_begin();
+  __shared__ float2 parts[kThreads / 32];
+  __shared__ float picked;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
+  const bool own = has_label(AGN_LD(a.labels + row), a.classes);
+  if (threadIdx.x == 0 && !own) {
+    AGN_ST(lse + row, 0.f);
+    AGN_ST(loss + row, 0.f);
+  }
+  if (a.idx ? row >= AGN_LD(a.live) : !own) return;   // (the same for the block)
+  const int at = a.idx ? AGN_LD(a.idx + row) : row, label = AGN_LD(a.labels + at);
+  float2 v = make_float2(-INFINITY, 0.f);
+  for (int c = threadIdx.x * 4; c < a.classes; c += kThreads * 4) {
+    float z[4];
+    logits4(a, row, c, z);
+    float most = v.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      most = fmaxf(most, z[j]);
+      if (c + j == label) picked = z[j];
+    }
+    const float from = most == -INFINITY ? 0.f : most;
+    v.y *= exp2f((v.x - from) * kLog2e);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.y += exp2f((z[j] - from) * kLog2e);
+    v.x = most;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+  if (lane == 0) parts[warp] = v;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int j = 1; j < kThreads / 32; ++j) v = join(v, parts[j]);
+  const float total = v.x == -INFINITY && v.y == 0.f ? -INFINITY : v.x + logf(v.y);
+  AGN_ST(lse + at, total);
+  AGN_ST(loss + at, total == -INFINITY ? INFINITY : total - picked);
+}
+
+// p and its sums over 32 rows: 32 rows x 64 columns a block, eight columns a thread.
+template <int kPlanes>
+__global__ void __launch_bounds__(kThreads)
+logits_grad_kernel(const Logits a, const float* lse, const float* dloss, const float* dlse, float scale, bf16* p,
+                   int64_t ldp, int64_t plane, float* db) {
+  pdl_begin();
+  __shared__ float sums[32][65];
+  const int live = AGN_LD(a.live);
+  const int row0 = blockIdx.y * 32, row = row0 + (threadIdx.x >> 3), c0 = blockIdx.x * 64, c = c0 + (threadIdx.x & 7) * 8;
+  if (row0 >= (live + 63) / 64 * 64) return;   // (rows up to a multiple of 64 are zeros)
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  if (row < live && c < a.classes) {
+    const int at = AGN_LD(a.idx + row), label = AGN_LD(a.labels + at);
+    const float total = AGN_LD(lse + at), dl = dloss ? AGN_LD(dloss + at) : 1.f, fb = scale * dl;
+    const float fa = dlse ? scale * (dl + AGN_LD(dlse + at)) : fb;
+    if (total != -INFINITY) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float z[4];
+        logits4(a, row, c + 4 * h, z);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[4 * h + j] = fa * exp2f((z[j] - total) * kLog2e);
+          if (c + 4 * h + j == label) v[4 * h + j] -= fb;
+        }
+      }
+    }
+  }
+  bf16 q[3][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (kPlanes == 3) split3(v[i], q[0][i], q[1][i], q[2][i]);
+    else q[0][i] = __float2bfloat16_rn(v[i]);
+    sums[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + i] = v[i];
+  }
+#pragma unroll
+  for (int k = 0; k < kPlanes; ++k)
+    AGN_ST(reinterpret_cast<uint4*>(p + k * plane + row * ldp + c), *reinterpret_cast<const uint4*>(q[k]));
+  if (!db) return;
+  __syncthreads();
+  if (threadIdx.x < 64 && c0 + (int)threadIdx.x < a.classes && row0 < live) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r) s += sums[r][threadIdx.x];
+    AGN_ST(db + (int64_t)blockIdx.y * ldp + c0 + threadIdx.x, s);
+  }
+}
+
 // What a piece leaves to be added up, a launch for all of it.
 constexpr int kSumThreads = 1024;   // (16384 rows have 512 sums of 32 a column: 8 warps took 3 us more)
 template <typename T>
@@ -600,128 +739,188 @@ sums_kernel(const Columns db, const Ranges<T> dw, const Ranges<T> dx, const int*
   sum_ranges(dx, block - dw.blocks, live);
 }
 
-// ---- small problems: a warp a row, fp32 arithmetic
+// ---- small problems: a block a row, fp32 arithmetic
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
 
-// The logits of four classes from c on (every lane gets them).
+// A row's logits into shared memory z [classes]: short rows a class a thread, with x [64] in shared memory
+// too, others four classes a warp, 16 bytes a lane where rows are aligned.
 template <typename T>
-__device__ __forceinline__ void logits4(const T* x, const T* w, const float* bias, int inner, int classes, int c,
-                                        int lane, float (&z)[4]) {
+__device__ __forceinline__ void logits(const T* x, const T* w, const float* bias, int inner, int classes, float* xs,
+                                       float* z) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (inner <= 64) {
+    if ((int)threadIdx.x < inner) xs[threadIdx.x] = to_float(AGN_LD(x + threadIdx.x));
+    __syncthreads();
+    for (int c = threadIdx.x; c < classes; c += kThreads) {
+      const T* p = w + c * inner;
+      float s = 0.f;
+#pragma unroll 8
+      for (int k = 0; k < inner; ++k) s = fmaf(xs[k], to_float(AGN_LD(p + k)), s);
+      z[c] = s + (bias ? AGN_LD(bias + c) : 0.f);
+    }
+  } else {
+    constexpr int n = 16 / (int)sizeof(T);
+    for (int c = 4 * warp; c < classes; c += 4 * (kThreads / 32)) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const T* rows[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) z[j] = 0.f;
-  for (int k = lane; k < inner; k += 32) {
-    const float xv = to_float(AGN_LD(x + k));
+      for (int j = 0; j < 4; ++j) rows[j] = w + min(c + j, classes - 1) * inner;
+      if (inner % n == 0) {
+#pragma unroll 2
+        for (int k = lane * n; k < inner; k += 32 * n) {
+          const uint4 xq = AGN_LD(reinterpret_cast<const uint4*>(x + k));
+          const T* xe = reinterpret_cast<const T*>(&xq);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      z[j] = fmaf(xv, to_float(AGN_LD(w + (int64_t)min(c + j, classes - 1) * inner + k)), z[j]);
+          for (int j = 0; j < 4; ++j) {
+            const uint4 wq = AGN_LD(reinterpret_cast<const uint4*>(rows[j] + k));
+            const T* we = reinterpret_cast<const T*>(&wq);
+#pragma unroll
+            for (int e = 0; e < n; ++e) s[j] = fmaf(to_float(xe[e]), to_float(we[e]), s[j]);
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int k = lane; k < inner; k += 32) {
+          const float xv = to_float(AGN_LD(x + k));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] = fmaf(xv, to_float(AGN_LD(rows[j] + k)), s[j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[j] = warp_sum(s[j]);
+        if (lane == 0 && c + j < classes) z[c + j] = s[j] + (bias ? AGN_LD(bias + c + j) : 0.f);
+      }
+    }
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    z[j] = warp_sum(z[j]);
-    z[j] = c + j < classes ? z[j] + (bias ? AGN_LD(bias + c + j) : 0.f) : -INFINITY;
-  }
+  __syncthreads();
 }
 
 template <typename T>
-__global__ void __launch_bounds__(64)
-small_loss_kernel(const T* x, const T* w, const float* bias, const int* labels, int rows, int inner, int classes,
-                  float* loss, float* lse) {
+__global__ void __launch_bounds__(kThreads)
+small_loss_kernel(const T* x, const T* w, const float* bias, const int* labels, int inner, int classes, float* loss,
+                  float* lse) {
   pdl_begin();
-  const int lane = threadIdx.x & 31, row = blockIdx.x * 2 + (threadIdx.x >> 5);
-  if (row >= rows) return;
+  extern __shared__ float z[];
+  __shared__ float xs[64], warps[kThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
   const int label = AGN_LD(labels + row);
-  float total = 0.f, l = 0.f;
-  if (has_label(label, classes)) {
-    float m = -INFINITY, s = 0.f, zl = 0.f;
-    for (int c = 0; c < classes; c += 4) {
-      float z[4];
-      logits4(x + (int64_t)row * inner, w, bias, inner, classes, c, lane, z);
-      float most = m;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        most = fmaxf(most, z[j]);
-        if (c + j == label) zl = z[j];
-      }
-      const float from = most == -INFINITY ? 0.f : most;
-      s *= exp2f((m - from) * kLog2e);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s += exp2f((z[j] - from) * kLog2e);
-      m = most;
+  if (!has_label(label, classes)) {   // (the same for the block)
+    if (threadIdx.x == 0) {
+      AGN_ST(lse + row, 0.f);
+      AGN_ST(loss + row, 0.f);
     }
-    total = m == -INFINITY && s == 0.f ? -INFINITY : m + logf(s);
-    l = total == -INFINITY ? INFINITY : total - zl;
+    return;
   }
-  if (lane == 0) {
+  logits(x + (int64_t)row * inner, w, bias, inner, classes, xs, z);
+  float most = -INFINITY;
+  for (int c = threadIdx.x; c < classes; c += kThreads) most = fmaxf(most, z[c]);
+  most = warp_max(most);
+  if (lane == 0) warps[warp] = most;
+  __syncthreads();
+  for (int j = 0; j < kThreads / 32; ++j) most = fmaxf(most, warps[j]);
+  const float from = most == -INFINITY ? 0.f : most;
+  float s = 0.f;
+  for (int c = threadIdx.x; c < classes; c += kThreads) s += exp2f((z[c] - from) * kLog2e);
+  s = warp_sum(s);
+  __syncthreads();
+  if (lane == 0) warps[warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int j = 1; j < kThreads / 32; ++j) s += warps[j];
+    const float total = most == -INFINITY && s == 0.f ? -INFINITY : most + logf(s);
     AGN_ST(lse + row, total);
-    AGN_ST(loss + row, l);
+    AGN_ST(loss + row, total == -INFINITY ? INFINITY : total - z[label]);
   }
 }
 
 // p [rows][classes] (fp32) and dx.
 template <typename T>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kThreads)
 small_rows_kernel(const T* x, const T* w, const float* bias, const int* labels, const float* lse, const float* dloss,
-                  const float* dlse, float scale, int rows, int inner, int classes, float* p, T* dx) {
+                  const float* dlse, float scale, int inner, int classes, float* p, T* dx) {
   pdl_begin();
-  extern __shared__ float shared_p[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 2 + warp;
-  if (row >= rows) return;
-  float* mine = shared_p + warp * classes;
+  extern __shared__ float z[];
+  __shared__ float xs[64], part[kThreads / 32][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
   const int label = AGN_LD(labels + row);
-  const bool known = has_label(label, classes);
-  float total = 0.f, fa = 0.f, fb = 0.f;
-  if (known) {
-    total = AGN_LD(lse + row);
+  const bool known = has_label(label, classes);   // (the same for the block)
+  const float total = known ? AGN_LD(lse + row) : 0.f;
+  const bool live = known && total != -INFINITY;
+  float fa = 0.f, fb = 0.f;
+  if (live) {
     const float dl = dloss ? AGN_LD(dloss + row) : 1.f;
     fb = scale * dl;
     fa = dlse ? scale * (dl + AGN_LD(dlse + row)) : fb;
+    logits(x + (int64_t)row * inner, w, bias, inner, classes, xs, z);
   }
-  const bool live = known && total != -INFINITY;
-  for (int c = 0; c < classes; c += 4) {
-    float z[4];
-    if (live) logits4(x + (int64_t)row * inner, w, bias, inner, classes, c, lane, z);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v = 0.f;
-      if (live) {
-        v = fa * exp2f((z[j] - total) * kLog2e);
-        if (c + j == label) v -= fb;
-      }
-      if (lane == j && c + j < classes) mine[c + j] = v;
+  for (int c = threadIdx.x; c < classes; c += kThreads) {
+    float v = 0.f;
+    if (live) {
+      v = fa * exp2f((z[c] - total) * kLog2e);
+      if (c == label) v -= fb;
     }
+    z[c] = v;
+    AGN_ST(p + (int64_t)row * classes + c, v);
   }
-  __syncwarp();
-  for (int c = lane; c < classes; c += 32) AGN_ST(p + (int64_t)row * classes + c, mine[c]);
+  __syncthreads();
   if (!dx) return;
-  for (int k = lane; k < inner; k += 32) {
-    float s = 0.f;
-    if (live)
-      for (int c = 0; c < classes; ++c) s = fmaf(mine[c], to_float(AGN_LD(w + (int64_t)c * inner + k)), s);
-    from_float(dx + (int64_t)row * inner + k, s);
+  T* out = dx + (int64_t)row * inner;
+  if (classes <= 64 || inner >= kThreads) {   // a column a thread
+    for (int k = threadIdx.x; k < inner; k += kThreads) {
+      float s = 0.f;
+      if (live) {
+#pragma unroll 8
+        for (int c = 0; c < classes; ++c) s = fmaf(z[c], to_float(AGN_LD(w + c * inner + k)), s);
+      }
+      from_float(out + k, s);
+    }
+  } else {   // 32 columns at a time, whose classes the warps share
+    for (int k0 = 0; k0 < inner; k0 += 32) {
+      const int k = min(k0 + lane, inner - 1);
+      float s = 0.f;
+      if (live) {
+#pragma unroll 8
+        for (int c = warp; c < classes; c += kThreads / 32) s = fmaf(z[c], to_float(AGN_LD(w + c * inner + k)), s);
+      }
+      part[warp][lane] = s;
+      __syncthreads();
+      if (warp == 0 && k0 + lane < inner) {
+        for (int j = 1; j < kThreads / 32; ++j) s += part[j][lane];
+        from_float(out + k, s);
+      }
+      __syncthreads();
+    }
   }
 }
 
 // dw and dbias: 32 columns of a class a block, its warps share the rows.  (Column `inner`: the bias.)
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(1024)
 small_columns_kernel(const float* p, const T* x, const int* labels, int rows, int inner, int classes, T* dw,
                      float* dbias) {
   pdl_begin();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kThreads / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int c = blockIdx.x, k = blockIdx.y * 32 + lane;
-  __shared__ float part[kThreads / 32][33];
+  __shared__ float part[32][33];
   float s = 0.f;
-  if (k <= inner)
-    for (int r = warp; r < rows; r += warps) {
-      if (!has_label(AGN_LD(labels + r), classes)) continue;
-      const float v = AGN_LD(p + (int64_t)r * classes + c);
-      s = k < inner ? fmaf(v, to_float(AGN_LD(x + (int64_t)r * inner + k)), s) : s + v;
-    }
+  const int at = min(k, inner - 1);
+#pragma unroll 4
+  for (int r = warp; r < rows; r += warps) {
+    const bool known = has_label(AGN_LD(labels + r), classes);
+    const float v = AGN_LD(p + (int64_t)r * classes + c), xv = to_float(AGN_LD(x + (int64_t)r * inner + at));
+    s = fmaf(v, !known ? 0.f : k < inner ? xv : 1.f, s);
+  }
   part[warp][lane] = s;
   __syncthreads();
   if (warp != 0 || k > inner) return;
@@ -762,20 +961,21 @@ unsigned grid_for(int64_t items, int per) { return (unsigned)std::max<int64_t>(1
 
 template <typename T>
 Status small_forward(const Call& c, cudaStream_t st) {
-  return run(small_loss_kernel<T>, dim3((unsigned)ceil_div(c.s.rows, 2)), 64, 0, st, static_cast<const T*>(c.x),
-             static_cast<const T*>(c.w), c.bias, c.labels, (int)c.s.rows, (int)c.s.inner, (int)c.s.classes, c.loss,
-             c.lse_out);
+  return run(small_loss_kernel<T>, dim3((unsigned)c.s.rows), kThreads, (size_t)c.s.classes * 4, st,
+             static_cast<const T*>(c.x), static_cast<const T*>(c.w), c.bias, c.labels, (int)c.s.inner,
+             (int)c.s.classes, c.loss, c.lse_out);
 }
 
 template <typename T>
 Status small_backward(const Call& c, const Layout& l, cudaStream_t st) {
   float* p = reinterpret_cast<float*>(c.work + l.p);
   const int rows = (int)c.s.rows, inner = (int)c.s.inner, classes = (int)c.s.classes;
-  AGN_TRY(run(small_rows_kernel<T>, dim3((unsigned)ceil_div(rows, 2)), 64, (size_t)classes * 8, st,
+  AGN_TRY(run(small_rows_kernel<T>, dim3((unsigned)rows), kThreads, (size_t)classes * 4, st,
               static_cast<const T*>(c.x), static_cast<const T*>(c.w), c.bias, c.labels, c.lse, c.dloss, c.dlse,
-              c.scale, rows, inner, classes, p, static_cast<T*>(c.dx)));
+              c.scale, inner, classes, p, static_cast<T*>(c.dx)));
   if (!c.dw && !c.dbias) return Status::Ok();
-  return run(small_columns_kernel<T>, dim3((unsigned)classes, (unsigned)ceil_div(inner + 1, 32)), kThreads, 0, st,
+  return run(small_columns_kernel<T>, dim3((unsigned)classes, (unsigned)ceil_div(inner + 1, 32)),
+             rows > 128 ? 1024 : 256, 0, st,
              (const float*)p, static_cast<const T*>(c.x), c.labels, rows, inner, classes, static_cast<T*>(c.dw),
              c.dbias);
 }
@@ -890,6 +1090,24 @@ Status run_few(const Call& c, const Layout& l, bool backward_call, cudaStream_t 
   return join_rows(c, a.ms, l.halves, a.zlab, nullptr, nullptr, st);
 }
 
+// The logits' product by ranges of K into scratch.
+Status logit_ranges(const Call& c, const Layout& l, GemmLaunch& g, bool as_is, cudaStream_t st, Logits* out) {
+  float* zs = reinterpret_cast<float*>(c.work + l.zs);
+  AGN_TRY(w_map(c, l, 0, c.s.classes, 64, l.z.bn / l.z.ctas, &g.maps[0].b));
+  AGN_TRY(make_tmap_store_2d(&g.maps[0].c, zs, 4, l.ldz, l.z_splits * l.rows_pad, l.ldz, 32, 32));
+  GemmArgs& a = g.args[0];
+  a = logit_args(c, l, 0, c.s.classes);
+  a.splits = l.z_splits;
+  a.part = 1;
+  a.part_rows = (int)l.rows_pad;
+  if (as_is) a.live = nullptr;
+  AGN_TRY(gemm(l.z.ctas, kOut, g, logit_units(c, l, c.s.classes) * l.z_splits, st));
+  *out = Logits{zs, l.z_splits, l.rows_pad * l.ldz, l.ldz, c.bias, c.labels, (int)c.s.classes, (int)c.s.rows,
+                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.idx),
+                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.live)};
+  return Status::Ok();
+}
+
 template <typename T>
 Status forward(const Call& c, const Layout& l, cudaStream_t st) {
   // One tile of rows is read as it is: rows without a label cost nothing more and are their own alone (3 us).
@@ -901,6 +1119,11 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
   g.n = 1;
   GemmMaps& maps = g.maps[0];
   AGN_TRY(x_maps(c, l, 64, l.a_box, &maps.a, &maps.alt));
+  if (l.z_splits > 1) {
+    Logits z;
+    AGN_TRY(logit_ranges(c, l, g, as_is, st, &z));
+    return run(logits_loss_kernel, dim3((unsigned)c.s.rows), kThreads, 0, st, z, c.loss, c.lse_out);
+  }
   int64_t half = 0;
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
@@ -959,14 +1182,21 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
     if (c0 > 0) AGN_TRY(prepare_w<T>(c, l, c0, n, st));
-    AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &z.maps[0].b));
-    GemmArgs& a = z.args[0];
-    a = logit_args(c, l, c0, n);
-    a.lse = c.lse; a.dloss = c.dloss; a.dlse = c.dlse; a.scale = c.scale;
-    a.p_plane = (int)l.rows_pad;
-    a.db = c.dbias ? db : nullptr;
-    a.ld_db = l.ldp;
-    AGN_TRY(gemm(l.z.ctas, kGrad, z, logit_units(c, l, n), st));
+    if (l.z_splits > 1) {
+      Logits a;
+      AGN_TRY(logit_ranges(c, l, z, false, st, &a));
+      AGN_TRY(run(logits_grad_kernel<sizeof(T) == 4 ? 3 : 1>, dim3((unsigned)(l.ldp / 64), (unsigned)(l.rows_pad / 32)),
+                  kThreads, 0, st, a, c.lse, c.dloss, c.dlse, c.scale, p, l.ldp, p_plane, c.dbias ? db : nullptr));
+    } else {
+      AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &z.maps[0].b));
+      GemmArgs& a = z.args[0];
+      a = logit_args(c, l, c0, n);
+      a.lse = c.lse; a.dloss = c.dloss; a.dlse = c.dlse; a.scale = c.scale;
+      a.p_plane = (int)l.rows_pad;
+      a.db = c.dbias ? db : nullptr;
+      a.ld_db = l.ldp;
+      AGN_TRY(gemm(l.z.ctas, kGrad, z, logit_units(c, l, n), st));
+    }
     T* dw_out = static_cast<T*>(c.dw) + c0 * inner;
     int64_t dw_units = 0, dx_units = 0;
     if (c.dw) {   // [n][inner] = p^T x
@@ -1084,11 +1314,11 @@ Status call(Call& c, bool backward_call, cudaStream_t st) {
   AGN_TRY(bounds_upload(st));
   const bool fp32 = c.s.prec == AGN_PREC_FP32;
   if (!backward_call) {
-    if (small(c.s)) AGN_TRY(fp32 ? small_forward<float>(c, st) : small_forward<bf16>(c, st));
+    if (l.small) AGN_TRY(fp32 ? small_forward<float>(c, st) : small_forward<bf16>(c, st));
     else if (l.few) AGN_TRY(run_few(c, l, false, st));
     else AGN_TRY(fp32 ? forward<float>(c, l, st) : forward<bf16>(c, l, st));
   } else if (c.dx || c.dw || c.dbias) {
-    if (small(c.s)) AGN_TRY(fp32 ? small_backward<float>(c, l, st) : small_backward<bf16>(c, l, st));
+    if (l.small) AGN_TRY(fp32 ? small_backward<float>(c, l, st) : small_backward<bf16>(c, l, st));
     else if (l.few) AGN_TRY(run_few(c, l, true, st));
     else AGN_TRY(fp32 ? backward<float>(c, l, st) : backward<bf16>(c, l, st));
   }

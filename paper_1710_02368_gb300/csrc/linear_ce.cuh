@@ -95,8 +95,8 @@ constexpr int few_rows(int64_t rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : ro
 constexpr bool few(int64_t rows, int dtype, bool backward) {
   return rows <= (dtype == AGN_PREC_FP32 ? 16 : backward ? 4 : 0);
 }
-// Blocks of the dot products: a warp takes four classes at a time.
-constexpr int64_t few_blocks(int64_t classes) { return std::min<int64_t>(kFewSms, (classes + 63) / 64); }
+// Blocks of the dot products: a warp, or several, takes four classes at a time.
+constexpr int64_t few_blocks(int64_t classes) { return std::min<int64_t>(kFewSms, (classes + 3) / 4); }
 // Blocks of the outer products: `along` threads along the columns of 16 bytes, ranges of classes.
 struct FewCut {
   int along, parts;

@@ -23,12 +23,15 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kDotThreads = 512;
-constexpr int kDotWarps = kDotThreads / 32;
 constexpr int kClasses = 4;                 // of a warp at a time
 constexpr int kXFloats = 32 * 1024;         // of x in shared memory
-constexpr int kRing = 3;                    // of a warp's copies: 16 bytes a lane of four classes each
-constexpr size_t kDotRing = (size_t)kDotWarps * kRing * kClasses * 512;
+// Threads of a block of dots (16 rows' sums need 255 registers), and the ring of a warp's copies: 16 bytes a
+// lane of four classes each.
+template <int R>
+struct Dots {
+  static constexpr int threads = R == 16 ? 256 : 512, warps = threads / 32, ring = R == 16 ? 6 : 3;
+  static constexpr size_t ring_bytes = (size_t)warps * ring * kClasses * 512;
+};
 constexpr int kPFloats = 8192;              // of p in shared memory
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -98,15 +101,18 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 
 // R: rows, rounded up to a power of two.
 template <typename T, int R, bool kBackward>
-__global__ void __launch_bounds__(kDotThreads, 1) dots_kernel(const FewArgs a, int chunk, bool wide) {
+__global__ void __launch_bounds__(Dots<R>::threads, 1)
+dots_kernel(const FewArgs a, int chunk, int share, bool wide) {
   pdl_begin();
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int n = Vec<T>::n, V = kClasses * R, kOwn = V >= 32 ? V / 32 : 1;
+  constexpr int kDotThreads = Dots<R>::threads, kDotWarps = Dots<R>::warps, kRing = Dots<R>::ring;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ __align__(16) float shared_sums[kDotWarps][R < 16 ? 32 : 64];   // (and the rows' (maximum, sum) at the end)
   uint4* ring = reinterpret_cast<uint4*>(smem) + warp * (kRing * kClasses * 32) + lane;
   // [R][chunk]; bf16: of eight consecutive columns the first four in a row's first half, the others in its
   // second, so that lanes read consecutive 16 bytes
-  float* xs = reinterpret_cast<float*>(smem + kDotRing);
+  float* xs = reinterpret_cast<float*>(smem + Dots<R>::ring_bytes);
   const T* x = static_cast<const T*>(a.x);
   const T* w = static_cast<const T*>(a.w);
   uint32_t known = 0;   // rows with a label (the others are zeros)
@@ -156,66 +162,107 @@ __global__ void __launch_bounds__(kDotThreads, 1) dots_kernel(const FewArgs a, i
       fa[j] = a.dlse ? a.scale * (dl + AGN_LD(a.dlse + r)) : fb[j];
     }
   }
-  const int groups = (a.classes + kClasses - 1) / kClasses, all = gridDim.x * kDotWarps;
+  // `share` warps of a block take a group of four classes together, a range of its steps each.  Groups go to
+  // the blocks in turn.
+  const int groups = (a.classes + kClasses - 1) / kClasses, teams = kDotWarps / share;
+  const int team = warp / share, mine = warp % share, all = gridDim.x * teams;
   const int rounds = (groups + all - 1) / all;   // (the same for all warps: barriers below)
-  // A warp's work is a sequence of (round, columns) steps of 32 lanes x 16 bytes; copies run kRing - 1 ahead
-  // within a chunk of columns.
+  auto group_of = [&](int round) { return (round * teams + team) * gridDim.x + blockIdx.x; };
+  // A warp's work is a sequence of (round, columns) steps of 32 lanes x 16 bytes; copies run kRing - 1 ahead,
+  // from one group into the next where x lies whole in shared memory, else within a chunk of columns.
+  const int all_steps = (a.inner + 32 * n - 1) / (32 * n), each = (all_steps + share - 1) / share;
+  int ahead_round = 0, ahead_step = mine * each;   // of the next copy
+  uint32_t put = 0, take = 0;                      // slots of the ring
+  auto fetch_at = [&](int c0, int k) {
+    if (k < a.inner) {
+#pragma unroll
+      for (int c = 0; c < kClasses; ++c)
+        copy16(ring + (put * kClasses + c) * 32, w + (int64_t)min(c0 + c, a.classes - 1) * a.inner + k, a.inner - k,
+               wide);
+    }
+    if (++put == kRing) put = 0;
+  };
+  auto fetch_next = [&] {   // (whole)
+    const int end = min(all_steps, (mine + 1) * each);
+    if (ahead_step < end && ahead_round < rounds) {
+      const int group = group_of(ahead_round);
+      if (group < groups) fetch_at(group * kClasses, (ahead_step * 32 + lane) * n);
+      if (++ahead_step == end) ahead_step = mine * each, ++ahead_round;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (whole)
+    for (int i = 0; i < kRing - 1; ++i) fetch_next();
   for (int round = 0; round < rounds; ++round) {
-    const int group = (round * gridDim.x + blockIdx.x) * kDotWarps + warp;
+    const int group = group_of(round);
     const int c0 = group * kClasses;
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    for (int k0 = 0; k0 < a.inner; k0 += chunk) {
-      if (!whole) {
+    // one step: 16 bytes of four classes from the ring, and x's rows
+    auto step_at = [&](int k, int k0) {
+      float wv[kClasses][n];
+#pragma unroll
+      for (int c = 0; c < kClasses; ++c) unpack<T, n>(ring[(take * kClasses + c) * 32], wv[c]);
+      if (++take == kRing) take = 0;
+      if (k >= a.inner) return;
+      const float* xk = xs + (n == 4 ? k - k0 : (k - k0) / 2);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float xv[n];
+#pragma unroll
+        for (int i = 0; i < n; i += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(xk + r * chunk + (i ? chunk / 2 : 0));
+          xv[i] = q.x; xv[i + 1] = q.y; xv[i + 2] = q.z; xv[i + 3] = q.w;
+        }
+#pragma unroll
+        for (int c = 0; c < kClasses; ++c)
+#pragma unroll
+          for (int i = 0; i < n; ++i) acc[c * R + r] = fmaf(wv[c][i], xv[i], acc[c * R + r]);
+      }
+    };
+    if (whole) {
+      if (group < groups) {
+        for (int step = mine * each; step < min(all_steps, (mine + 1) * each); ++step) {
+          fetch_next();
+          asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+          step_at((step * 32 + lane) * n, 0);
+        }
+      }
+    } else {
+      for (int k0 = 0; k0 < a.inner; k0 += chunk) {   // (share is 1)
         __syncthreads();
         load_x(k0);
         __syncthreads();
-      }
-      if (group >= groups) continue;
-      const int end = min(chunk, a.inner - k0), steps = (end + 32 * n - 1) / (32 * n);
-      const T* rows[kClasses];
+        if (group >= groups) continue;
+        const int steps = (min(chunk, a.inner - k0) + 32 * n - 1) / (32 * n);
+        auto fetch = [&](int step) {
+          if (step < steps) fetch_at(c0, k0 + (step * 32 + lane) * n);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        };
 #pragma unroll
-      for (int c = 0; c < kClasses; ++c) rows[c] = w + (int64_t)min(c0 + c, a.classes - 1) * a.inner + k0;
-      auto fetch = [&](int step) {
-        const int k = (step * 32 + lane) * n;
-        if (step < steps && k < end) {
-#pragma unroll
-          for (int c = 0; c < kClasses; ++c)
-            copy16(ring + (step % kRing * kClasses + c) * 32, rows[c] + k, end - k, wide);
+        for (int i = 0; i < kRing - 1; ++i) fetch(i);
+        for (int step = 0; step < steps; ++step) {
+          fetch(step + kRing - 1);
+          asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+          step_at(k0 + (step * 32 + lane) * n, k0);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      };
-#pragma unroll
-      for (int i = 0; i < kRing - 1; ++i) fetch(i);
-      for (int step = 0; step < steps; ++step) {
-        fetch(step + kRing - 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-        const int k = (step * 32 + lane) * n;
-        if (k >= end) continue;
-        float wv[kClasses][n];
-#pragma unroll
-        for (int c = 0; c < kClasses; ++c) unpack<T, n>(ring[(step % kRing * kClasses + c) * 32], wv[c]);
-        const float* xk = xs + (step * 32 + lane) * 4;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          float xv[n];
-#pragma unroll
-          for (int i = 0; i < n; i += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(xk + r * chunk + (i ? chunk / 2 : 0));
-            xv[i] = q.x; xv[i + 1] = q.y; xv[i + 2] = q.z; xv[i + 3] = q.w;
-          }
-#pragma unroll
-          for (int c = 0; c < kClasses; ++c)
-#pragma unroll
-            for (int i = 0; i < n; ++i) acc[c * R + r] = fmaf(wv[c][i], xv[i], acc[c * R + r]);
-        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
       }
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
-    if (group >= groups) continue;
     __syncwarp();
     exchange<V>(acc, lane);
+    if (share > 1) {   // (all warps: rounds are the same)
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) shared_sums[warp][32 * j + lane] = acc[j];
+      __syncthreads();
+      if (mine == 0)
+        for (int k = 1; k < share; ++k)
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j) acc[j] += shared_sums[warp + k][32 * j + lane];
+    }
+    if (group >= groups || mine != 0) continue;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int c = c0 + (v0 + j) / R, r = (v0 + j) % R;
@@ -245,7 +292,8 @@ __global__ void __launch_bounds__(kDotThreads, 1) dots_kernel(const FewArgs a, i
   }
   if constexpr (!kBackward) {
     // rows' (maximum, sum) of this block: over the lanes of a row, then the warps
-    __shared__ float2 parts[kDotWarps][R];
+    __syncthreads();
+    float2(*parts)[R] = reinterpret_cast<float2(*)[R]>(shared_sums);
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       float2 v = ms[j];
@@ -407,10 +455,16 @@ Status dots(const FewArgs& a, cudaStream_t st) {
   int dev = 0;
   AGN_TRY(current_device(&dev));
   const int chunk = (int)std::min<int64_t>(round_up(a.inner, 32 * Vec<T>::n), kXFloats / R / 256 * 256);
-  constexpr size_t most = kDotRing + kXFloats * sizeof(float);
+  constexpr int kDotWarps = Dots<R>::warps;
+  constexpr size_t most = Dots<R>::ring_bytes + kXFloats * sizeof(float);
   AGN_TRY_CUDA(allow_smem<Tag>(kern, most, dev));
-  AGN_TRY_CUDA(launch_pdl(kern, dim3((unsigned)few_blocks(a.classes)), dim3(kDotThreads),
-                          kDotRing + (size_t)R * chunk * 4, st, a, chunk, a.inner % Vec<T>::n == 0));
+  // warps of a group: so many that all have work, a step each at least
+  const int64_t groups = ceil_div(a.classes, kClasses), steps = ceil_div(a.inner, 32 * Vec<T>::n);
+  int share = 1;
+  while (chunk >= a.inner && share < kDotWarps && 2 * share <= steps && groups * share < (int64_t)kFewSms * kDotWarps)
+    share *= 2;
+  AGN_TRY_CUDA(launch_pdl(kern, dim3((unsigned)few_blocks(a.classes)), dim3(Dots<R>::threads),
+                          Dots<R>::ring_bytes + (size_t)R * chunk * 4, st, a, chunk, share, a.inner % Vec<T>::n == 0));
   return Status::Ok();
 }
 
