@@ -52,23 +52,46 @@ double step_clocks(int ctas, int bn, int planes, int64_t a_box, bool b_mn) {
   const int products = planes == 3 ? 6 : 1;
   const double mma = bn * 2.0 * products, in = (a_box * 128 + bn / ctas * 128) * planes;
   const double read = (128 * 128 + bn / ctas * 128 * (b_mn ? 2 : 1)) * products;
-  return std::max({mma, in / 64.0, (in + read) / 128.0});
+  // (fp32 as measured: 128 columns wait for their operands, with B along either side, 256 for sums to be read)
+  if (planes == 3 && bn < 256) return 1.3 * std::max(mma, (in + (128 * 128 + bn / ctas * 128) * products) / 128.0);
+  return std::max({mma, in / 64.0, (in + read) / 128.0}) * (planes == 3 ? 1.1 : 1.0);
+}
+
+// Time of the CTA that ends last, in steps: `n` units of each of two kinds on `at_once` CTAs, the longer ones first
+// and in turn, the others where there is least to do.
+double makespan(int64_t at_once, const int64_t (&n)[2], const double (&cost)[2]) {
+  const int longer = cost[1] > cost[0] ? 1 : 0;
+  const int64_t q = n[longer] / at_once, rest = n[longer] % at_once, others = n[1 - longer];
+  const double low = q * cost[longer], high = low + (rest ? cost[longer] : 0), each = cost[1 - longer];
+  if (others == 0) return high;
+  auto room = [&](double t) {   // for the shorter ones by time t
+    auto fit = [&](double from) { return t < from ? 0 : (int64_t)((t - from) / each + 1e-9); };
+    return rest * fit(high) + (at_once - rest) * fit(low);
+  };
+  double t = std::max(high, low + each * std::floor((double)others / at_once));
+  if (room(high) >= others) t = high;
+  while (room(t) < others) {   // to the next time at which one ends
+    auto next = [&](double from) { return from + (std::floor((t - from) / each + 1e-9) + 1) * each; };
+    t = std::min(next(low), next(high));
+  }
+  return t;
 }
 
 // Tile width by the estimated time: rounds of tiles over the SMs, or B's bytes from memory (24 a clock and
 // SM) if that is more.  Of products cut along K also the ranges: as many as even out the work, where
 // that saves more than the pass over their sums costs.  A tile takes its epilogue's time at least, 14 clocks
-// a column.
-Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges) {
+// a column (fp32's 256, whose sums are read in between, 28).
+Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges, double pass_clocks = 8000) {
   Cut best{};
   const int64_t at_once = kSms / ctas;
   int least = 64;   // (a box is 64 columns of an operand stored along N)
   for (int i = 0; i < n; ++i)
     if (e[i].b_mn && ctas == 2) least = 128;
-  for (int bn = planes > 1 ? 128 : 256; bn >= least; bn /= 2) {
+  for (int bn = planes > 1 && ctas == 1 ? 128 : 256; bn >= least; bn /= 2) {
     Cut c{};
     c.ctas = ctas;
     c.bn = bn;
+    const double finish = bn * (planes == 3 && bn == 256 ? 28 : 14);
     double step = 0;
     for (int i = 0; i < n; ++i) step = std::max(step, step_clocks(ctas, bn, planes, a_box, e[i].b_mn));
     double steps = 0, bytes = 0;
@@ -81,27 +104,42 @@ Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges) {
                                    ceil_div((int64_t)std::ceil(kt[i] * step), 4000)})
                        : 1;
       tiles += c.tiles[i];
-      steps += c.tiles[i] * std::max((double)kt[i], bn * 14 / step);
+      steps += c.tiles[i] * std::max((double)kt[i], finish / step);
       bytes += (double)ceil_div(e[i].N, bn) * bn * kt[i] * 128 * planes;
     }
     double rounds = 0, more = 0;   // steps one after the other, clocks of passes over sums
+    // writing and reading the sums of k ranges
+    auto pass = [&](int i, int64_t k) { return pass_clocks + 250 * k + 2.0 * k * e[i].M * e[i].N * 4 / (24.0 * kSms); };
     if (n == 1) {
-      const double pass = 8000 + (double)e[0].M * e[0].N * 4 / (24.0 * kSms);
       auto after = [&](int64_t k) {
-        return ceil_div(tiles * k, at_once) * std::max((double)ceil_div(kt[0], k), bn * 14 / step);
+        return ceil_div(tiles * k, at_once) * std::max((double)ceil_div(kt[0], k), finish / step);
       };
       rounds = after(1);
       for (int64_t k = 2; k <= most[0]; ++k) {
         const double r = after(k);
-        if (r * step + pass * (1 + 0.1 * k) < rounds * step + more)
-          rounds = r, more = pass * (1 + 0.1 * k), c.splits[0] = (int)k;
+        if (r * step + pass(0, k) < rounds * step + more) rounds = r, more = pass(0, k), c.splits[0] = (int)k;
       }
     } else {
-      rounds = std::max(1.0, steps / at_once);   // a CTA's share
-      for (int i = 0; i < n; ++i)
-        if ((kt[i] - rounds) * step > 12000)
-          c.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>(most[i], (int64_t)std::ceil(kt[i] / rounds)));
-      for (int i = 0; i < n; ++i) rounds = std::max(rounds, (double)ceil_div(kt[i], c.splits[i]));
+      const double share = std::max(1.0, steps / at_once), beside = 0.5;
+      double least_time = 0;
+      for (int j = 0; j < 9; ++j) {   // each uncut, by its share of the work, or twice as often
+        int64_t k[2], units[2];
+        double cost[2], passes = 0;
+        for (int i = 0; i < 2; ++i) {
+          const int often = i ? j / 3 : j % 3;
+          k[i] = often ? std::max<int64_t>(1, std::min<int64_t>(most[i], (int64_t)std::ceil(kt[i] / share) * often)) : 1;
+          units[i] = c.tiles[i] * k[i];
+          cost[i] = std::max((double)ceil_div(kt[i], k[i]), finish / step) + beside;
+          if (k[i] > 1) passes += pass(i, k[i]);
+        }
+        const double r = makespan(at_once, units, cost);
+        if (j == 0 || r * step + passes < least_time) {
+          least_time = r * step + passes;
+          rounds = r;
+          more = passes;
+          for (int i = 0; i < 2; ++i) c.splits[i] = (int)k[i];
+        }
+      }
     }
     c.time = std::max(rounds * step, bytes / (24.0 * kSms)) + more + 500.0 * tiles / at_once;
     if (best.bn == 0 || c.time < best.time) best = c;
@@ -113,10 +151,10 @@ Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges) {
 // rows a class a thread) is less than that of the products, whose launches and k steps are one after the other.
 bool small(const Sizes& s, bool backward) {
   if (s.rows > 1024 || s.classes > 4096 || s.inner * s.classes > 32768) return false;
-  const double each = (double)s.rows * s.inner * s.classes / (s.inner <= 64 ? 0.65e6 : 1.9e6);
+  const double products = (double)s.rows * s.inner * s.classes;
   const double step = s.prec == AGN_PREC_FP32 ? 1.2 : 0.35, k = (double)ceil_div(s.inner, 64);
-  if (!backward) return 3 + each < 8 + step * std::min(k, 12.0);
-  return 5 + 2 * each + s.rows / 32 * 0.2 < 16 + step * std::min(k + (double)(std::max(s.rows, s.classes) / 64), 24.0);
+  if (!backward) return 3 + products / (s.inner <= 64 ? 0.65e6 : 1.9e6) < 8 + step * std::min(k, 12.0);
+  return 5 + products / (s.inner <= 64 ? 0.17e6 : 0.36e6) < 16 + step * std::min(k + (double)(std::max(s.rows, s.classes) / 64), 24.0);
 }
 
 struct Layout {
@@ -195,7 +233,7 @@ Layout layout(const Sizes& s, bool backward) {
   l.z_splits = 1;
   if (l.pieces == 1) {
     const Extents e{s.rows, s.classes, s.inner, false};
-    const Cut c = cut(s.rows > 128 ? 2 : 1, l.planes, l.a_box, &e, 1, true);
+    const Cut c = cut(s.rows > 128 ? 2 : 1, l.planes, l.a_box, &e, 1, true, 2000);
     if (c.splits[0] > 1 && c.time < l.z.time) l.z = c, l.z_splits = c.splits[0];
   }
   l.live = take(4);
@@ -223,7 +261,7 @@ Layout layout(const Sizes& s, bool backward) {
     for (int i = 0; i < 2; ++i) l.grads[i] = cut(i ? dx_ctas : dw_ctas, l.planes, 128, e + i, 1, true);
     if (dw_ctas == dx_ctas) {   // one launch, where one width suits both
       const Cut c = cut(dw_ctas, l.planes, 128, e, 2, true);
-      l.both = c.time < l.grads[0].time + l.grads[1].time + 4000;
+      l.both = c.time < l.grads[0].time + l.grads[1].time + 8000;
       if (l.both) l.grads[0] = c;
     }
     l.dw_splits = l.grads[0].splits[0];

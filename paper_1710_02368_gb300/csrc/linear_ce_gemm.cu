@@ -10,6 +10,8 @@
 // accumulator and the five smaller ones in another.  The tensor cores cut what they add to an
 // accumulator off below its last bit, always towards zero, so these sums are taken over 256 k at
 // a time and added in registers, rounded (one accumulator over K = 50000: 1.5e-5 of dx off).
+// Many fp32 tiles are 256 x 256 as bf16's are, both accumulators then fill TMEM: their sums (512 k) are
+// read between the MMAs, the larger one's first, so that its next products run while the other is read.
 // One CTA a tile of 128 rows, or a pair (cta_group::2) a tile of 256, each CTA loading its 128 rows
 // of A and half of B's: 64 bytes a clock of MMA time instead of 96 with 256 columns.  Persistent:
 // a CTA (pair) walks over tiles in bands of eight along M, so that what runs at a time shares operands
@@ -32,7 +34,7 @@ constexpr int kBK = 64;                   // k of a stage: 128-byte rows
 constexpr int kBox = 64 * 128;            // an operand stored along M or N: boxes of 64 x 64 k
 constexpr int kRing = 176 * 1024;
 constexpr int kMaxStages = 16;
-constexpr int kPartK = 4;                 // fp32: stages' k of a sum in TMEM
+constexpr int kPartK = 4, kPartKWide = 8; // fp32: stages' k of a sum in TMEM
 constexpr int kStaged = 4096;             // a finishing warp's tile of outputs
 constexpr size_t kSmem = 1024 + kRing + 8 * (kStaged + 512) + 512;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -224,7 +226,8 @@ __device__ __forceinline__ void land(uint64_t* full, const int* loaded, int stag
   }
 }
 
-template <int kCtas, int kEpi, int kPlanes>
+// kWide: fp32 tiles of 256 columns.
+template <int kCtas, int kEpi, int kPlanes, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ GemmLaunch launch) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -292,6 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   __syncthreads();
   constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
   const uint32_t acc_cols = kSets * bn;
+  constexpr int kSumK = kWide ? kPartKWide : kPartK;
   // Unit i of this CTA (pair): of product p, number u.  One product: in turn.  Two: the longer units first, in
   // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time, and are
   // the first when the rest is given out in turn.
@@ -318,8 +322,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   };
   auto unit_of = [&](Place at) { return Unit(geo[at.p], launch.args[at.p].splits, at.u); };
 
-  if (warp == 0) {
-    if (lane == 0) {
+  // (kWide: the finishing warps hold 128 sums a thread: 128 x 72 + 256 x 216 registers are the launch's 384 x 168)
+  if (warp < 4) {
+    if (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0 && lane == 0) {
       const uint32_t full0 = kCtas == 2 ? tc::map_cluster(full, 0) : 0;
       int s = 0, loaded = 0, stop = INT32_MAX;
       uint32_t phase = 1;   // (the first round finds every stage free)
@@ -373,9 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         }
       }
       *loaded_out = loaded;
-    }
-  } else if (warp == 1) {
-    if (lane == 0 && cta == 0) {
+    } else if (warp == 1 && lane == 0 && cta == 0) {
       const uint32_t r0 = tc::smem_u32(ring);
       const uint32_t step = stage >> 4;
       int s = 0, done = 0;   // (done: sums, from the launch's first)
@@ -411,14 +415,15 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         };
         int kt = 0;
         do {   // a sum (of nothing: announced as it is)
-          const int buf = done & 1;
-          if (done >= 2 && !tc::wait_mbar<true>(&acc_empty[buf], ((done >> 1) - 1) & 1, abort_flag, wait_ns)) {
-            ok = false;
-            break;
-          }
+          const int buf = kWide ? 0 : done & 1;
+          // (kWide: the larger products' sums have been read; the others' further down)
+          if (kWide ? done >= 1 : done >= 2)
+            ok = tc::wait_mbar<true>(&acc_empty[buf], kWide ? (done - 1) & 1 : ((done >> 1) - 1) & 1, abort_flag,
+                                     wait_ns);
+          if (!ok) break;
           tc::tc_fence_after();
           const uint32_t d = tmem + buf * acc_cols;
-          const int end = kPlanes == 3 ? min(t.kt, kt + kPartK) : t.kt;
+          const int end = kPlanes == 3 ? min(t.kt, kt + kSumK) : t.kt;
           for (bool first = true; kt < end; ++kt, first = false) {
             if (kPlanes == 1) {
               if (!arrived(s, phase)) break;
@@ -432,6 +437,11 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
               next();
               const int s1 = s;
               if (!arrived(s1, phase)) break;
+              if (kWide && first && done >= 1) {
+                ok = tc::wait_mbar<true>(&acc_empty[1], (done - 1) & 1, abort_flag, wait_ns);
+                if (!ok) break;
+                tc::tc_fence_after();
+              }
               product(d + bn, s0, s1, first);
               product(d + bn, s1, s0, false);
               product(d + bn, s1, s1, false);
@@ -456,7 +466,8 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       }
       if (!ok) stop_all();
     }
-  } else if (warp >= 4) {
+  } else {
+    if (kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int e = warp - 4, quad = warp & 3, half = e >> 2, chunks = bn / 64;   // of 32 columns
     float* bias = biases + 128 * e;
     const uint32_t empty0 = kCtas == 2 ? tc::map_cluster(acc_empty, 0) : tc::smem_u32(acc_empty);
@@ -499,7 +510,8 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
 
       // The sums in buffer `buf` are there (or will not come).
       auto wait_sums = [&](int buf) {
-        ok = ok && tc::wait_mbar<true>(&acc_full[buf], (done >> 1) & 1, abort_flag, wait_ns) && !*abort_flag;
+        ok = ok && tc::wait_mbar<true>(&acc_full[buf], kWide ? done & 1 : (done >> 1) & 1, abort_flag, wait_ns) &&
+             !*abort_flag;
         ok = __all_sync(0xffffffffu, ok);
         tc::tc_fence_after();
         if (!ok && lane == 0) {
@@ -628,34 +640,49 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         }
         ++done;
       } else {
-        float v[2][32];   // (64 columns at most)
+        constexpr int kMost = kWide ? 4 : 2;   // chunks
+        float v[kMost][32];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) v[i / 32][i % 32] = 0.f;
+        for (int i = 0; i < 32 * kMost; ++i) v[i / 32][i % 32] = 0.f;
+        // adds one accumulator's columns of a chunk, 16 at a time
+        auto add = [&](uint32_t at, float (&sum)[32]) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[16];
+            if (ok) {
+              tc::tmem_ld_32x32b_x16(at + 16 * h, r);
+              tc::tmem_ld_wait();
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[16 * h + i] += __uint_as_float(!ok ? none : t.kt == 0 ? 0u : r[i]);
+          }
+        };
         int kt = 0;
         do {
-          const int buf = done & 1;
+          const int buf = kWide ? 0 : done & 1;
           wait_sums(buf);
+          const uint32_t at = at0 + buf * acc_cols;
+          if (kWide) {
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            if (ch >= chunks) break;
+            for (int ch = 0; ch < kMost; ++ch) add(at + 32 * ch, v[ch]);
+            free_sums(0);
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {   // 16 columns of a set at a time
-              uint32_t r[16];
-              if (ok) {
-                tc::tmem_ld_32x32b_x16(at0 + buf * acc_cols + (h >> 1) * bn + 32 * ch + 16 * (h & 1), r);
-                tc::tmem_ld_wait();
-              }
+            for (int ch = 0; ch < kMost; ++ch) add(at + bn + 32 * ch, v[ch]);
+            free_sums(1);
+          } else {
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                v[ch][16 * (h & 1) + i] += __uint_as_float(!ok ? none : t.kt == 0 ? 0u : r[i]);
+            for (int ch = 0; ch < kMost; ++ch) {
+              if (ch >= chunks) break;
+              add(at + 32 * ch, v[ch]);
+              add(at + bn + 32 * ch, v[ch]);
             }
+            free_sums(buf);
           }
-          free_sums(buf);
           ++done;
-          kt += kPartK;
+          kt += kSumK;
         } while (kt < t.kt);
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch)
+        for (int ch = 0; ch < kMost; ++ch)
           if (ch < chunks) finish(ch, v[ch]);
       }
       if (kEpi == kLse && live)
@@ -686,10 +713,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   }
 }
 
-template <int kCtas, int kEpi, int kPlanes>
+template <int kCtas, int kEpi, int kPlanes, bool kWide>
 Status queue(const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
   struct Tag {};
-  auto kern = ce_gemm_kernel<kCtas, kEpi, kPlanes>;
+  auto kern = ce_gemm_kernel<kCtas, kEpi, kPlanes, kWide>;
   int dev = 0, sms = 0;
   AGN_TRY(current_device(&dev));
   AGN_TRY(device_sms(dev, &sms));
@@ -702,11 +729,11 @@ Status queue(const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
   return Status::Ok();
 }
 
-template <int kCtas, int kPlanes>
+template <int kCtas, int kPlanes, bool kWide = false>
 Status queue_for(int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
-  if (epilogue == kLse) return queue<kCtas, kLse, kPlanes>(g, max_units, st);
-  if (epilogue == kGrad) return queue<kCtas, kGrad, kPlanes>(g, max_units, st);
-  return queue<kCtas, kOut, kPlanes>(g, max_units, st);
+  if (epilogue == kLse) return queue<kCtas, kLse, kPlanes, kWide>(g, max_units, st);
+  if (epilogue == kGrad) return queue<kCtas, kGrad, kPlanes, kWide>(g, max_units, st);
+  return queue<kCtas, kOut, kPlanes, kWide>(g, max_units, st);
 }
 
 }  // namespace
@@ -715,6 +742,7 @@ Status gemm(int ctas, int epilogue, const GemmLaunch& launch, int64_t max_units,
   GemmLaunch g = launch;
   for (GemmArgs& a : g.args)
     if (!a.wait_ns) a.wait_ns = (uint32_t)kWaitNs;
+  if (g.args[0].planes == 3 && g.args[0].bn == 256) return queue_for<2, 3, true>(epilogue, g, max_units, st);
   if (g.args[0].planes == 3)
     return ctas == 2 ? queue_for<2, 3>(epilogue, g, max_units, st) : queue_for<1, 3>(epilogue, g, max_units, st);
   return ctas == 2 ? queue_for<2, 1>(epilogue, g, max_units, st) : queue_for<1, 1>(epilogue, g, max_units, st);

@@ -87,7 +87,9 @@ SIZES = [(1, 16, 2), (1, 1, 1), (33, 100, 10), (32, 128, 10), (512, 33, 60),    
          (9, 2048, 515), (16, 1600, 301), (16, 4100, 100), (15, 33, 5000), (12, 8, 70000),
          (100, 80, 5000), (128, 1000, 999), (17, 8, 70000), (20, 4096, 640),              # a CTA a tile
          (777, 1000, 1500), (300, 130, 700), (1000, 257, 515),                      # ragged, packed rows
-         (4096, 200, 10), (64, 64, 20000), (16000, 40, 5)]                          # ranges along K
+         (4096, 200, 10), (64, 64, 20000), (16000, 40, 5), (300, 3000, 200),        # ranges along K
+         (60, 5000, 600), (63, 19, 1365), (700, 2100, 15), (2, 5000, 900),
+         (4096, 600, 5000), (5000, 64, 2600), (3001, 1025, 3000)]                   # many tiles
 
 
 @pytest.mark.parametrize("dtype", [0, 1])

@@ -28,7 +28,8 @@ def waits(agn):
 # one CTA a tile: K of one stage and of more than the ring has; pairs: the same, several tiles for each,
 # ranges along K, rows gathered
 SHAPES = [(60, 64, 600, 0.0, [0]), (100, 3000, 130, 0.2, [0]), (200, 64, 700, 0.0, [0, 1]), (300, 3000, 400, 0.3, [0, 1]),
-          (1500, 520, 9000, 0.0, [0, 1]), (9000, 64, 140, 0.1, [0, 1])]
+          (1500, 520, 9000, 0.0, [0, 1]), (9000, 64, 140, 0.1, [0, 1]),
+          (4096, 640, 5000, 0.1, [0, 1])]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
