@@ -211,7 +211,11 @@ Layout layout(const Sizes& s, bool backward) {
   int64_t most = s.classes;
   auto limit = [&](int64_t bytes, int64_t each) { most = std::min(most, std::max<int64_t>(1024, bytes / each / 256 * 256)); };
   if (backward) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
-  if (!l.direct) limit(kPackBytes, l.kp * 2 * l.planes);
+  if (!l.direct) {   // (so many that tiles of few rows still occupy all SMs)
+    const int64_t tm = ceil_div(s.rows, s.rows > 128 ? 256 : 128);
+    const int64_t full = (s.rows > 128 ? kSms / 2 * 128 : kSms * 64) / tm;
+    limit(std::max(kPackBytes, std::min(full * l.kp * 2 * l.planes, 4 * kPackBytes)), l.kp * 2 * l.planes);
+  }
   limit((int64_t)1 << 29, std::max<int64_t>(1, l.rows_pad / 16384));   // tiles of a launch
   l.pieces = ceil_div(s.classes, most);
   l.a_box = (int)std::min<int64_t>(128, round_up(s.rows, 8));

@@ -91,6 +91,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// 2^x; below 2^-126 it is 0 (beside a sum of such that is at least 1, or a probability's gradient)
+__device__ __forceinline__ float exp2_or_0(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Lane l gets the sum over the warp's lanes of v[l]: halves are exchanged and added.
 __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
 #pragma unroll
@@ -545,25 +552,27 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             for (int i = 1; i < 32; ++i) z = hit == i ? v[i] : z;
             AGN_ST(a.zlab + row, z);
           }
-          float most = top;
+          float m[4] = {top, v[1], v[2], v[3]}, s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) most = fmaxf(most, v[i]);
+          for (int i = 0; i < 32; ++i) m[i & 3] = fmaxf(m[i & 3], v[i]);
+          const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
           const float from = most == -INFINITY ? 0.f : most;
-          float s0 = sum * exp2f((top - from) * kLog2e), s1 = 0.f;
+          sum *= exp2_or_0((top - from) * kLog2e);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            s0 += exp2f((v[i] - from) * kLog2e);
-            s1 += exp2f((v[i + 1] - from) * kLog2e);
-          }
-          sum = s0 + s1;
+          for (int i = 0; i < 32; ++i) s[i & 3] += exp2_or_0((v[i] - from) * kLog2e);
+          sum += (s[0] + s[1]) + (s[2] + s[3]);
           top = most;
         } else if (kEpi == kGrad) {
           const bool dead = !live || lse == -INFINITY;   // (no class that is not masked: no gradient)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float q = fa * exp2f((v[i] - lse) * kLog2e);
-            if (hit == i) q -= fb;
-            v[i] = dead ? 0.f : q;
+          for (int i = 0; i < 32; ++i) v[i] = fa * exp2_or_0((v[i] - lse) * kLog2e);
+          if (hit < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = hit == i ? v[i] - fb : v[i];
+          }
+          if (dead) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
 #pragma unroll
           for (int z = 0; z < kPlanes; ++z) {
