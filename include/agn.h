@@ -637,9 +637,9 @@ int agn_optim_grad_norm(agn_optim* plan, double max_norm, float* norm, float* sc
 
 /*
  * One step.  scale: device fp32 [1], read when the step runs (agn_optim_grad_norm's, or a loss
- * scale's inverse), NULL = 1; where it is not finite, nothing changes.  A captured call keeps its lr,
- * step, seed and offset.  Element by element: a NaN or infinity without scale goes into the
- * states (8 bits: the largest codes).
+ * scale's inverse), NULL = 1; where it is not finite, nothing changes.  eps: 0 or a normal fp32
+ * number up to 1e30.  A captured call keeps its lr, step, seed and offset.  Element by element: a
+ * NaN or infinity without scale goes into the states (8 bits: the largest codes).
  * Errors: AGN_E_INVALID, AGN_E_CUDA.
  */
 int agn_optim_adamw(agn_optim* plan, double lr, int64_t step, double beta1, double beta2, double eps,

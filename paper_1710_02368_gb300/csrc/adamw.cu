@@ -738,9 +738,10 @@ Status optim_norm(agn_optim* o, double max_norm, float* norm, float* scale, cuda
 Status optim_step(agn_optim* o, double lr, int64_t step, double beta1, double beta2, double eps,
                   const float* scale, uint64_t seed, uint64_t offset, cudaStream_t st) {
   auto below_one = [](double b) { return b >= 0.0 && b < 1.0; };
-  if (!(std::fabs(lr) <= 1e30) || step < 1 || !below_one(beta1) || !below_one(beta2) || !(eps >= 0.0 && eps <= 1e30))
+  if (!(std::fabs(lr) <= 1e30) || step < 1 || !below_one(beta1) || !below_one(beta2) ||
+      !(eps == 0.0 || (eps >= FLT_MIN && eps <= 1e30)))   // (the quotient takes smaller ones for 0)
     return Status::Err(AGN_E_INVALID,
-                       "need a finite lr, step >= 1, beta1 and beta2 in [0, 1), eps >= 0");
+                       "need a finite lr, step >= 1, beta1 and beta2 in [0, 1), eps 0 or a normal fp32 number >= 0");
   const CallBuffer sb{"scale", scale, scale ? sizeof(float) : 0, 4};
   AGN_TRY(plan_device(o));
   if (!o->has_param && o->pieces > 0) return Status::Err(AGN_E_INVALID, "the plan has gradients alone");

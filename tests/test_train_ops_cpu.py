@@ -137,7 +137,7 @@ def test_plans_refuse_more(agn):
 
 
 @pytest.mark.parametrize("bad", [dict(lr=math.nan), dict(lr=math.inf), dict(step=0), dict(beta1=1.0), dict(beta2=-0.1),
-                                 dict(beta1=math.nan), dict(eps=-1e-8), dict(eps=math.inf)], ids=str)
+                                 dict(beta1=math.nan), dict(eps=-1e-8), dict(eps=math.inf), dict(eps=1e-40)], ids=str)
 def test_steps_refuse(agn, bad):
     a = dict(plan=None, lr=1e-3, step=1, beta1=0.9, beta2=0.999, eps=1e-8)
     a.update(bad)
