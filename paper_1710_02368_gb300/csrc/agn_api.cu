@@ -88,6 +88,7 @@ AGN_BOUNDS_DECL(adamw)
 AGN_BOUNDS_DECL(linear_ce)
 AGN_BOUNDS_DECL(linear_ce_gemm)
 AGN_BOUNDS_DECL(linear_ce_few)
+AGN_BOUNDS_DECL(linear_ce_raw)
 #undef AGN_BOUNDS_DECL
 
 namespace {
@@ -143,7 +144,7 @@ Status bounds_upload(cudaStream_t st) {
   for (SetFn f : {bounds_set_commit, bounds_set_eval, bounds_set_head, bounds_set_simt,
                   bounds_set_tc, bounds_set_dw, bounds_set_optim, bounds_set_dropout,
                   bounds_set_mx4, bounds_set_mx4_linear, bounds_set_adamw, bounds_set_linear_ce,
-                  bounds_set_linear_ce_gemm, bounds_set_linear_ce_few})
+                  bounds_set_linear_ce_gemm, bounds_set_linear_ce_few, bounds_set_linear_ce_raw})
     AGN_TRY_CUDA(f(t, st));
   return Status::Ok();
 }
@@ -155,7 +156,7 @@ Status bounds_collect(cudaStream_t st) {
   for (GetFn f : {bounds_get_commit, bounds_get_eval, bounds_get_head, bounds_get_simt,
                   bounds_get_tc, bounds_get_dw, bounds_get_optim, bounds_get_dropout,
                   bounds_get_mx4, bounds_get_mx4_linear, bounds_get_adamw, bounds_get_linear_ce,
-                  bounds_get_linear_ce_gemm, bounds_get_linear_ce_few}) {
+                  bounds_get_linear_ce_gemm, bounds_get_linear_ce_few, bounds_get_linear_ce_raw}) {
     unsigned long long a = 0;
     unsigned int c = 0;
     AGN_TRY_CUDA(f(&a, &c, st));

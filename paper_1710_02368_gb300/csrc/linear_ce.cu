@@ -157,6 +157,28 @@ bool small(const Sizes& s, bool backward) {
   return 5 + products / (s.inner <= 64 ? 0.17e6 : 0.36e6) < 16 + step * std::min(k + (double)(std::max(s.rows, s.classes) / 64), 24.0);
 }
 
+// Products that read fp32 w as it is, where it is not small (us forward and backward, w packed first in brackets: 56
+// rows of 2392 to 55366 classes 138 and 467 (496 and -), 128 of 4096 to 32000 189 and 550 (502 and 976), 128 of
+// 2048 to 8192 38 and 115 (68 and 126); 128 of 8192 to 300 26 and 58 (24 and 45): its launches are more).
+bool raw(const Sizes& s) {
+  return s.prec == AGN_PREC_FP32 && s.rows <= 128 && s.classes <= 1 << 18 && s.inner * s.classes >= 3 << 20;
+}
+
+// Ranges along K of such a product of M along w's side: by the time of the CTA that ends last and that of a pass
+// over the ranges' sums; each has a step.
+int raw_ranges(int64_t M, int64_t K, int64_t rows) {
+  const int64_t tiles = ceil_div(M, 128), steps = ceil_div(K, 64);
+  const double step = rows <= 64 ? 1800 : 2800;
+  auto time = [&](int64_t k) {
+    return (double)ceil_div(tiles * k, kSms) * ((double)ceil_div(steps, k) * step + 3000) + 250.0 * k +
+           2.0 * (double)k * rows * M * 4 / (24.0 * kSms);
+  };
+  int64_t best = 1;
+  for (int64_t k = 2; k <= std::min<int64_t>({steps, 64, kPartBytes / (round_up(rows, 64) * round_up(M, 64) * 4)}); ++k)
+    if (ceil_div(steps, ceil_div(steps, k)) == k && time(k) < time(best)) best = k;
+  return (int)best;
+}
+
 struct Layout {
   int planes;
   int64_t kp;              // x's and w's row stride where they are packed (whole 128 bytes)
@@ -173,6 +195,7 @@ struct Layout {
   bool dx_part;
   bool x_t;                // dw reads x laid out along its rows
   bool small, few;
+  bool raw;                // w is read as it is by its products (linear_ce_raw.cu), the logits are in scratch
   int64_t halves;          // forward: partial (maximum, sum) of a row
   size_t idx, live, x, xt, w, zs, ms, zlab, p, db, dxs, dws, bytes;
 };
@@ -195,7 +218,7 @@ Layout layout(const Sizes& s, bool backward) {
     l.bytes = std::max<size_t>(at, 1024);
     return l;
   }
-  if (few(s.rows, s.prec, backward)) {
+  if (few(s.rows, s.prec, backward) && !(s.rows > 8 && raw(s))) {
     l.few = true;
     l.halves = few_blocks(s.classes);
     if (!backward) {
@@ -208,10 +231,12 @@ Layout layout(const Sizes& s, bool backward) {
     l.bytes = at;
     return l;
   }
+  l.raw = raw(s);
+  if (l.raw) l.rows_pad = round_up(s.rows, 64);
   int64_t most = s.classes;
   auto limit = [&](int64_t bytes, int64_t each) { most = std::min(most, std::max<int64_t>(1024, bytes / each / 256 * 256)); };
-  if (backward) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
-  if (!l.direct) {   // (so many that tiles of few rows still occupy all SMs)
+  if (backward && !l.raw) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
+  if (!l.direct && !l.raw) {   // (so many that tiles of few rows still occupy all SMs)
     const int64_t tm = ceil_div(s.rows, s.rows > 128 ? 256 : 128);
     const int64_t full = (s.rows > 128 ? kSms / 2 * 128 : kSms * 64) / tm;
     limit(std::max(kPackBytes, std::min(full * l.kp * 2 * l.planes, 4 * kPackBytes)), l.kp * 2 * l.planes);
@@ -235,7 +260,9 @@ Layout layout(const Sizes& s, bool backward) {
   l.ldp = round_up(l.piece, 64);
   l.z = logits(l.piece);
   l.z_splits = 1;
-  if (l.pieces == 1) {
+  if (l.raw) {
+    l.z_splits = raw_ranges(s.classes, s.inner, s.rows);
+  } else if (l.pieces == 1) {
     const Extents e{s.rows, s.classes, s.inner, false};
     const Cut c = cut(s.rows > 128 ? 2 : 1, l.planes, l.a_box, &e, 1, true, 2000);
     if (c.splits[0] > 1 && c.time < l.z.time) l.z = c, l.z_splits = c.splits[0];
@@ -243,8 +270,8 @@ Layout layout(const Sizes& s, bool backward) {
   l.live = take(4);
   l.idx = take((size_t)l.rows_pad * 4);
   l.x = take((size_t)l.planes * l.rows_pad * l.kp * 2);
-  if (!l.direct) l.w = take((size_t)l.planes * l.piece * l.kp * 2);
-  if (l.z_splits > 1) {
+  if (!l.direct && !l.raw) l.w = take((size_t)l.planes * l.piece * l.kp * 2);
+  if (l.z_splits > 1 || l.raw) {
     l.ldz = round_up(s.classes, 64);
     l.zs = take((size_t)l.z_splits * l.rows_pad * l.ldz * 4);
   }
@@ -263,14 +290,14 @@ Layout layout(const Sizes& s, bool backward) {
     const Extents e[2] = {{l.piece, s.inner, s.rows, !l.x_t}, {s.inner, s.rows, l.piece, false}};   // dw, dx (transposed)
     const int dw_ctas = l.piece > 128 ? 2 : 1, dx_ctas = s.inner > 128 ? 2 : 1;
     for (int i = 0; i < 2; ++i) l.grads[i] = cut(i ? dx_ctas : dw_ctas, l.planes, 128, e + i, 1, true);
-    if (dw_ctas == dx_ctas) {   // one launch, where one width suits both
+    if (dw_ctas == dx_ctas && !l.raw) {   // one launch, where one width suits both
       const Cut c = cut(dw_ctas, l.planes, 128, e, 2, true);
       l.both = c.time < l.grads[0].time + l.grads[1].time + 8000;
       if (l.both) l.grads[0] = c;
     }
     l.dw_splits = l.grads[0].splits[0];
-    l.dx_splits = l.both ? l.grads[0].splits[1] : l.grads[1].splits[0];
-    l.dx_part = l.pieces > 1 || l.dx_splits > 1;
+    l.dx_splits = l.raw ? raw_ranges(s.inner, s.classes, s.rows) : l.both ? l.grads[0].splits[1] : l.grads[1].splits[0];
+    l.dx_part = l.pieces > 1 || l.dx_splits > 1 || l.raw;
     if (l.dx_part) l.dxs = take((size_t)l.dx_splits * l.rows_pad * round_up(s.inner, 64) * 4);
     if (l.dw_splits > 1)
       l.dws = take((size_t)l.dw_splits * round_up(l.piece, 256) * round_up(s.inner, 64) * 4);
@@ -608,10 +635,10 @@ __device__ __forceinline__ void logits4(const Logits& a, int64_t r, int c, float
     v[j] = c + j < a.classes ? v[j] + (a.bias ? AGN_LD(a.bias + c + j) : 0.f) : -INFINITY;
 }
 
-// lse and loss, a block a row.
-__global__ void __launch_bounds__(kThreads) logits_loss_kernel(const Logits a, float* loss, float* lse) {
+// lse and loss, a block a row (of many threads where rows are few).
+__global__ void __launch_bounds__(1024) logits_loss_kernel(const Logits a, float* loss, float* lse) {
   pdl_begin();
-  __shared__ float2 parts[kThreads / 32];
+  __shared__ float2 parts[32];
   __shared__ float picked;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
   const bool own = has_label(AGN_LD(a.labels + row), a.classes);
@@ -622,7 +649,7 @@ __global__ void __launch_bounds__(kThreads) logits_loss_kernel(const Logits a, f
   if (a.idx ? row >= AGN_LD(a.live) : !own) return;   // (the same for the block)
   const int at = a.idx ? AGN_LD(a.idx + row) : row, label = AGN_LD(a.labels + at);
   float2 v = make_float2(-INFINITY, 0.f);
-  for (int c = threadIdx.x * 4; c < a.classes; c += kThreads * 4) {
+  for (int c = threadIdx.x * 4; c < a.classes; c += blockDim.x * 4) {
     float z[4];
     logits4(a, row, c, z);
     float most = v.x;
@@ -643,7 +670,7 @@ __global__ void __launch_bounds__(kThreads) logits_loss_kernel(const Logits a, f
   if (lane == 0) parts[warp] = v;
   __syncthreads();
   if (threadIdx.x != 0) return;
-  for (int j = 1; j < kThreads / 32; ++j) v = join(v, parts[j]);
+  for (int j = 1; j < (int)blockDim.x / 32; ++j) v = join(v, parts[j]);
   const float total = v.x == -INFINITY && v.y == 0.f ? -INFINITY : v.x + logf(v.y);
   AGN_ST(lse + at, total);
   AGN_ST(loss + at, total == -INFINITY ? INFINITY : total - picked);
@@ -1031,7 +1058,7 @@ Pack<T> w_pack(const Call& c, const Layout& l, int64_t c0, int64_t n) {
 // Rows c0 .. c0 + n - 1 of w as bf16 rows or pieces, where they are not read as they are.
 template <typename T>
 Status prepare_w(const Call& c, const Layout& l, int64_t c0, int64_t n, cudaStream_t st) {
-  if (l.direct) return Status::Ok();
+  if (l.direct || l.raw) return Status::Ok();
   return run(pack_kernel<T>, dim3(grid_for(n * (l.kp / 8), kThreads)), kThreads, 0, st, w_pack<T>(c, l, c0, n));
 }
 
@@ -1045,8 +1072,9 @@ Status prepare(const Call& c, const Layout& l, cudaStream_t st) {
                   l.rows_pad * l.kp};
   const int64_t n = std::min(l.piece, c.s.classes);
   if (c.s.rows <= kMostRows) {
-    const Pack<T> w = l.direct ? Pack<T>{} : w_pack<T>(c, l, 0, n);
-    const int64_t items = (l.direct ? 0 : n * l.kp / 8192) + ceil_div(c.s.rows, 4);
+    const bool as_is = l.direct || l.raw;
+    const Pack<T> w = as_is ? Pack<T>{} : w_pack<T>(c, l, 0, n);
+    const int64_t items = (as_is ? 0 : n * l.kp / 8192) + ceil_div(c.s.rows, 4);
     const int64_t grid = std::max(std::min<int64_t>(kSms, items), ceil_div(c.s.rows, kRangeRows));
     return run(prepare_kernel<T>, dim3((unsigned)grid), 1024, 0, st, x, w, l.direct, (int)ceil_div(c.s.rows, grid),
                c.labels, (int)c.s.classes, idx, live, static_cast<T*>(c.dx));
@@ -1132,9 +1160,35 @@ Status run_few(const Call& c, const Layout& l, bool backward_call, cudaStream_t 
   return join_rows(c, a.ms, l.halves, a.zlab, nullptr, nullptr, st);
 }
 
-// The logits' product by ranges of K into scratch.
+// out [splits][rows_pad][ld] = x w^T (mn: p w), w read as it is.
+Status raw_product(const Call& c, const Layout& l, bool mn, float* out, int64_t ld, int splits, cudaStream_t st) {
+  RawLaunch r{};
+  if (mn) AGN_TRY(make_tmap_bf16_3d(&r.b, c.work + l.p, l.ldp, l.rows_pad, 3, l.ldp, l.rows_pad * l.ldp, 64, 64));
+  else AGN_TRY(make_tmap_bf16_3d(&r.b, c.work + l.x, l.kp, l.rows_pad, 3, l.kp, l.rows_pad * l.kp, 64, 64));
+  AGN_TRY(make_tmap_store_2d(&r.c, out, 4, ld, splits * l.rows_pad, ld, 32, 32));
+  RawArgs& a = r.args;
+  a.w = static_cast<const float*>(c.w);
+  a.ld = c.s.inner;
+  a.M = (int)(mn ? c.s.inner : c.s.classes);
+  a.K = (int)(mn ? c.s.classes : c.s.inner);
+  a.mn = mn;
+  a.vec = c.s.inner % 4 == 0;
+  a.groups = (int)(l.rows_pad / 64);
+  a.splits = splits;
+  a.part_rows = (int)l.rows_pad;
+  a.err = c.err;
+  a.wait_ns = (uint32_t)c.wait_ns;
+  a.withhold = c.withhold;
+  return raw(r, st);
+}
+
+// The logits into scratch: their product by ranges of K, or with w as it is.
 Status logit_ranges(const Call& c, const Layout& l, GemmLaunch& g, bool as_is, cudaStream_t st, Logits* out) {
   float* zs = reinterpret_cast<float*>(c.work + l.zs);
+  *out = Logits{zs, l.z_splits, l.rows_pad * l.ldz, l.ldz, c.bias, c.labels, (int)c.s.classes, (int)c.s.rows,
+                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.idx),
+                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.live)};
+  if (l.raw) return raw_product(c, l, false, zs, l.ldz, l.z_splits, st);
   AGN_TRY(w_map(c, l, 0, c.s.classes, 64, l.z.bn / l.z.ctas, &g.maps[0].b));
   AGN_TRY(make_tmap_store_2d(&g.maps[0].c, zs, 4, l.ldz, l.z_splits * l.rows_pad, l.ldz, 32, 32));
   GemmArgs& a = g.args[0];
@@ -1143,11 +1197,7 @@ Status logit_ranges(const Call& c, const Layout& l, GemmLaunch& g, bool as_is, c
   a.part = 1;
   a.part_rows = (int)l.rows_pad;
   if (as_is) a.live = nullptr;
-  AGN_TRY(gemm(l.z.ctas, kOut, g, logit_units(c, l, c.s.classes) * l.z_splits, st));
-  *out = Logits{zs, l.z_splits, l.rows_pad * l.ldz, l.ldz, c.bias, c.labels, (int)c.s.classes, (int)c.s.rows,
-                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.idx),
-                as_is ? nullptr : reinterpret_cast<const int*>(c.work + l.live)};
-  return Status::Ok();
+  return gemm(l.z.ctas, kOut, g, logit_units(c, l, c.s.classes) * l.z_splits, st);
 }
 
 template <typename T>
@@ -1161,10 +1211,10 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
   g.n = 1;
   GemmMaps& maps = g.maps[0];
   AGN_TRY(x_maps(c, l, 64, l.a_box, &maps.a, &maps.alt));
-  if (l.z_splits > 1) {
+  if (l.z_splits > 1 || l.raw) {
     Logits z;
     AGN_TRY(logit_ranges(c, l, g, as_is, st, &z));
-    return run(logits_loss_kernel, dim3((unsigned)c.s.rows), kThreads, 0, st, z, c.loss, c.lse_out);
+    return run(logits_loss_kernel, dim3((unsigned)c.s.rows), c.s.rows <= kSms && c.s.classes > 4096 ? 1024 : kThreads, 0, st, z, c.loss, c.lse_out);
   }
   int64_t half = 0;
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
@@ -1224,7 +1274,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
     if (c0 > 0) AGN_TRY(prepare_w<T>(c, l, c0, n, st));
-    if (l.z_splits > 1) {
+    if (l.z_splits > 1 || l.raw) {
       Logits a;
       AGN_TRY(logit_ranges(c, l, z, false, st, &a));
       AGN_TRY(run(logits_grad_kernel<sizeof(T) == 4 ? 3 : 1>, dim3((unsigned)(l.ldp / 64), (unsigned)(l.rows_pad / 32)),
@@ -1262,7 +1312,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       }
       dw_units = ceil_div(n, 128 * cw.ctas) * ceil_div(inner, cw.bn) * d.splits;
     }
-    if (c.dx) {   // [rows][inner] += p w, as w^T p^T
+    if (c.dx && !l.raw) {   // [rows][inner] += p w, as w^T p^T
       GemmArgs& d = dx.args[0];
       d = common_args(c, l);
       d.M = (int)inner; d.N = (int)rows; d.K = (int)n;
@@ -1291,7 +1341,9 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       AGN_TRY(gemm(cw.ctas, kOut, dw, dw_units + dx_units, st));
     } else {
       if (c.dw) AGN_TRY(gemm(cw.ctas, kOut, dw, dw_units, st));
-      if (c.dx) AGN_TRY(gemm(cx.ctas, kOut, dx, dx_units, st));
+      if (c.dx && l.raw)
+        AGN_TRY(raw_product(c, l, true, reinterpret_cast<float*>(c.work + l.dxs), ldn, l.dx_splits, st));
+      else if (c.dx) AGN_TRY(gemm(cx.ctas, kOut, dx, dx_units, st));
     }
     Columns columns{};
     Ranges<T> rw{}, rx{};

@@ -71,6 +71,26 @@ struct GemmLaunch {
 // ctas: 1 or 2 (pairs); max_units: tiles times ranges along K, at most.  On the current device.
 Status gemm(int ctas, int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st);
 
+// A product with w read as it is (linear_ce_raw.cu): out [splits][part_rows][M] = B A^T, fp32, for up to 128 rows of
+// B, three bf16 pieces each.
+struct RawArgs {
+  const float* w;           // (m, k) at w + m ld + k, mn: w + k ld + m
+  int64_t ld;
+  int M, K, mn;
+  int vec;                  // rows of w are 16-byte aligned
+  int groups;               // of 64 rows of B
+  int splits;               // ranges along K, none without a step of 64
+  int part_rows;
+  int* err;
+  uint32_t wait_ns;
+  int withhold;             // as above
+};
+struct RawLaunch {
+  CUtensorMap b, c;         // boxes of 64 k x 64 rows; of 32 x 32 outputs
+  RawArgs args;
+};
+Status raw(const RawLaunch& launch, cudaStream_t st);
+
 // A few rows (linear_ce_few.cu): up to 16 of fp32; of bf16 up to 4, backward (us for 8 and 16 rows of fp32,
 // 4096 and 2048 to 32000 and 50000 classes, against three pieces on the tensor cores: 98 for 802, 203 for
 // 430, gradients 284 for 1387, 460 for 908; bf16, 4096 to 32000: one row 47 for 49, gradients of 4 rows 151

@@ -209,11 +209,18 @@ struct Writer {
       }
     } else {
 #pragma unroll 1
-      for (int row = 0; row < n; ++row) {
-        const int64_t to = __shfl_sync(0xffffffffu, at, row);
-        if (lane < cols)
-          AGN_ST(out + to + lane, *reinterpret_cast<const T*>(staged_at<kRow>(tile, row, lane / kVec) +
-                                                              lane % kVec * sizeof(T)));
+      for (int r0 = 0; r0 < n; r0 += 8) {   // eight under way
+        int64_t to[8];
+        T value[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int row = min(r0 + j, n - 1);
+          to[j] = __shfl_sync(0xffffffffu, at, row);
+          value[j] = *reinterpret_cast<const T*>(staged_at<kRow>(tile, row, lane / kVec) + lane % kVec * sizeof(T));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (r0 + j < n && lane < cols) AGN_ST(out + to[j] + lane, value[j]);
       }
     }
   }
