@@ -2,10 +2,11 @@
 // the logits in memory (formulas in include/agn.h).
 //
 // Forward: one product x w^T whose epilogue keeps (maximum, sum of exponentials) of each row and
-// half a tile of columns, 16 bytes for 256 logits; a small kernel joins them.  Backward, from the rows'
+// half a tile of columns, 16 bytes for 256 logits; a small kernel joins them.  (Where tiles are few, or w is read as
+// it is, the logits are in scratch for once: products by ranges of K.)  Backward, from the rows'
 // lse alone: the product again, its epilogue turns logits into p, the gradient with respect
 // to them (bf16, fp32 as three bf16 pieces), for a piece of the classes at a time; then dw = p^T x
-// and dx += p w of the piece.  Pieces keep p's buffer at 128 MB.
+// and dx += p w of the piece.  Pieces keep p's buffer at 128 MB, w's pieces of fp32 at 96 (384 for few rows).
 // Rows without a label cost nothing and may hold anything: the rows with one are counted and, where
 // some are missing, gathered on the device; all sizes that depend on it are read there.
 // Small problems (w in a few 10 KB) take plain kernels instead: a block a row.

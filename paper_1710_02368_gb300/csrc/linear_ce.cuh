@@ -91,10 +91,9 @@ struct RawLaunch {
 };
 Status raw(const RawLaunch& launch, cudaStream_t st);
 
-// A few rows (linear_ce_few.cu): up to 16 of fp32; of bf16 up to 4, backward (us for 8 and 16 rows of fp32,
-// 4096 and 2048 to 32000 and 50000 classes, against three pieces on the tensor cores: 98 for 802, 203 for
-// 430, gradients 284 for 1387, 460 for 908; bf16, 4096 to 32000: one row 47 for 49, gradients of 4 rows 151
-// for 203, of 8 242 for 204).
+// A few rows (linear_ce_few.cu): up to 8 of fp32, 16 where w is small (linear_ce.cu's raw()); of bf16 up to 4,
+// backward (us for 8 rows of fp32, 4096 to 32000 classes, 90 and 276, 9 rows as the products above 136 and 394, here
+// 167 and 473; bf16, 4096 to 32000: gradients of 4 rows 151 for the tensor cores' 203, of 8 242 for 186).
 struct FewArgs {
   const void *x, *w;
   const float* bias;

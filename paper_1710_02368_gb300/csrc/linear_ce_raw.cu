@@ -7,8 +7,10 @@
 // 64 rows under one another, so that one MMA multiplies a piece of w by all three of them (N = 192): w0 by
 // (x0 x1 x2), w1 by (x0 x1), w2 by x0, three reads of w's pieces where six products would make six.  Three
 // accumulators, largest products first; sums over 256 or 512 k are added in registers (linear_ce_gemm.cu).
-// Bound by w's bytes in principle; shared memory takes 1300 clocks of a step's 1370 that its 32 KB take
-// to come (up to 64 rows), 2100 with 128.
+// Bound by w's bytes and shared memory together: a step's 32 KB come in 1370 clocks of an SM's share of the memory,
+// shared memory moves 168 KB for it (264 KB with more than 64 rows).  56 rows, 2392 to 55366: 117 us, w at 4.5 TB/s; 128
+// rows, 4096 to 32000: 164 us, 3.2 TB/s.  Loads a step further ahead gained nothing; with eight warps
+// that both made pieces and took sums it was 160 and 194.
 // Every wait is bounded as in linear_ce_gemm.cu.
 #include "linear_ce.cuh"
 #include "ops.cuh"
