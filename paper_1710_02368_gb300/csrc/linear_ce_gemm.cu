@@ -34,7 +34,7 @@ constexpr int kBK = 64;                   // k of a stage: 128-byte rows
 constexpr int kBox = 64 * 128;            // an operand stored along M or N: boxes of 64 x 64 k
 constexpr int kRing = 176 * 1024;
 constexpr int kMaxStages = 16;
-constexpr int kPartK = 4, kPartKWide = 8; // fp32: stages' k of a sum in TMEM
+constexpr int kPartK = 4, kPartKWide = 8; // fp32: stages' k of a sum in TMEM, of bf16's losses kPartKWide
 constexpr int kStaged = 4096;             // a finishing warp's tile of outputs
 constexpr size_t kSmem = 1024 + kRing + 8 * (kStaged + 512) + 512;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -240,7 +240,9 @@ __device__ __forceinline__ void land(uint64_t* full, const int* loaded, int stag
   }
 }
 
-// kWide: fp32 tiles of 256 columns.
+// kWide: the finishing warps hold 128 sums a thread: fp32 tiles of 256 columns; bf16's losses of up to 128 rows with K
+// above 1024, whose sums over 512 k are added in registers as fp32's are (one row, K = 4096: the loss is off by 2e-7 of it,
+// by 1.7e-6 with one sum; 47 us for 46.  Pairs of CTAs, which the tensor cores bound, took a tenth longer so).
 template <int kCtas, int kEpi, int kPlanes, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ GemmLaunch launch) {
   extern __shared__ uint8_t smem_raw[];
@@ -309,6 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   __syncthreads();
   constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
   const uint32_t acc_cols = kSets * bn;
+  constexpr bool kOne = kWide && kPlanes == 3;   // one set of sums in TMEM, not two in turn
   constexpr int kSumK = kWide ? kPartKWide : kPartK;
   // Unit i of this CTA (pair): of product p, number u.  One product: in turn.  Two: the longer units first, in
   // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time, and are
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   };
   auto unit_of = [&](Place at) { return Unit(geo[at.p], launch.args[at.p].splits, at.u); };
 
-  // (kWide: the finishing warps hold 128 sums a thread: 128 x 72 + 256 x 216 registers are the launch's 384 x 168)
+  // (kWide: 128 x 72 + 256 x 216 registers are the launch's 384 x 168)
   if (warp < 4) {
     if (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0 && lane == 0) {
@@ -429,15 +432,15 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         };
         int kt = 0;
         do {   // a sum (of nothing: announced as it is)
-          const int buf = kWide ? 0 : done & 1;
-          // (kWide: the larger products' sums have been read; the others' further down)
-          if (kWide ? done >= 1 : done >= 2)
-            ok = tc::wait_mbar<true>(&acc_empty[buf], kWide ? (done - 1) & 1 : ((done >> 1) - 1) & 1, abort_flag,
+          const int buf = kOne ? 0 : done & 1;
+          // (kOne: the larger products' sums have been read; the others' further down)
+          if (kOne ? done >= 1 : done >= 2)
+            ok = tc::wait_mbar<true>(&acc_empty[buf], kOne ? (done - 1) & 1 : ((done >> 1) - 1) & 1, abort_flag,
                                      wait_ns);
           if (!ok) break;
           tc::tc_fence_after();
           const uint32_t d = tmem + buf * acc_cols;
-          const int end = kPlanes == 3 ? min(t.kt, kt + kSumK) : t.kt;
+          const int end = kPlanes == 3 || kWide ? min(t.kt, kt + kSumK) : t.kt;
           for (bool first = true; kt < end; ++kt, first = false) {
             if (kPlanes == 1) {
               if (!arrived(s, phase)) break;
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
               next();
               const int s1 = s;
               if (!arrived(s1, phase)) break;
-              if (kWide && first && done >= 1) {
+              if (kOne && first && done >= 1) {
                 ok = tc::wait_mbar<true>(&acc_empty[1], (done - 1) & 1, abort_flag, wait_ns);
                 if (!ok) break;
                 tc::tc_fence_after();
@@ -524,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
 
       // The sums in buffer `buf` are there (or will not come).
       auto wait_sums = [&](int buf) {
-        ok = ok && tc::wait_mbar<true>(&acc_full[buf], kWide ? done & 1 : (done >> 1) & 1, abort_flag, wait_ns) &&
+        ok = ok && tc::wait_mbar<true>(&acc_full[buf], kOne ? done & 1 : (done >> 1) & 1, abort_flag, wait_ns) &&
              !*abort_flag;
         ok = __all_sync(0xffffffffu, ok);
         tc::tc_fence_after();
@@ -638,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
       };
 
       const uint32_t none = 0x7fc00000u;   // what could not be computed
-      if (kPlanes == 1) {
+      if (kPlanes == 1 && !kWide) {
         const int buf = done & 1;
         wait_sums(buf);
 #pragma unroll 1
@@ -675,10 +678,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         };
         int kt = 0;
         do {
-          const int buf = kWide ? 0 : done & 1;
+          const int buf = kOne ? 0 : done & 1;
           wait_sums(buf);
           const uint32_t at = at0 + buf * acc_cols;
-          if (kWide) {
+          if (kOne) {
 #pragma unroll
             for (int ch = 0; ch < kMost; ++ch) add(at + 32 * ch, v[ch]);
             free_sums(0);
@@ -690,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             for (int ch = 0; ch < kMost; ++ch) {
               if (ch >= chunks) break;
               add(at + 32 * ch, v[ch]);
-              add(at + bn + 32 * ch, v[ch]);
+              if (kPlanes == 3) add(at + bn + 32 * ch, v[ch]);
             }
             free_sums(buf);
           }
@@ -747,7 +750,11 @@ Status queue(const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
 
 template <int kCtas, int kPlanes, bool kWide = false>
 Status queue_for(int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
-  if (epilogue == kLse) return queue<kCtas, kLse, kPlanes, kWide>(g, max_units, st);
+  if (epilogue == kLse) {
+    if (kCtas == 1 && kPlanes == 1 && g.args[0].K > 1024)
+      return queue<kCtas, kLse, kPlanes, kWide || (kCtas == 1 && kPlanes == 1)>(g, max_units, st);
+    return queue<kCtas, kLse, kPlanes, kWide>(g, max_units, st);
+  }
   if (epilogue == kGrad) return queue<kCtas, kGrad, kPlanes, kWide>(g, max_units, st);
   return queue<kCtas, kOut, kPlanes, kWide>(g, max_units, st);
 }
