@@ -728,7 +728,9 @@ logits_grad_kernel(const Logits a, const float* lse, const float* dloss, const f
 }
 
 // What a piece leaves to be added up, a launch for all of it.
-constexpr int kSumThreads = 1024;   // (16384 rows have 512 sums of 32 a column: 8 warps took 3 us more)
+// Threads of a block: many where the sums of a column are (16384 rows have 512 of 32 rows: 8 warps took 3 us more).
+constexpr int kSumThreads = 1024;
+int sum_threads(int64_t rows, bool dbias) { return dbias && rows > 2048 ? kSumThreads : 256; }
 template <typename T>
 struct Ranges {   // out[idx[m]][n] = the sum of the ranges' sums, in order (idx null: row m)
   const float* part;
@@ -752,13 +754,13 @@ template <typename T>
 __device__ __forceinline__ void sum_ranges(const Ranges<T>& a, int block, int live) {
   const int64_t rows = a.idx ? live : a.rows;
   const int groups = (a.cols + 3) / 4;
-  const int64_t step = (int64_t)a.blocks * kSumThreads;
-  for (int64_t i = (int64_t)block * kSumThreads + threadIdx.x; i < rows * groups; i += step) {
+  const int64_t step = (int64_t)a.blocks * blockDim.x;
+  for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < rows * groups; i += step) {
     const int64_t r = i / groups;
     const int c = (int)(i - r * groups) * 4;
     const float* p = a.part + r * a.ld + c;
     float4 s = AGN_LD(reinterpret_cast<const float4*>(p));
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 1; k < a.splits; ++k) {
       const float4 v = AGN_LD(reinterpret_cast<const float4*>(p + k * a.plane));
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -782,7 +784,7 @@ __device__ __forceinline__ void sum_ranges(const Ranges<T>& a, int block, int li
 
 // 32 columns a block, whose warps share the blocks of rows.
 __device__ __forceinline__ void sum_columns(const Columns& a, int block, int live) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kSumThreads / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int blocks = (live + 31) / 32, c = block * 32 + lane;
   __shared__ float part[kSumThreads / 32][33];
   float s = 0.f;
@@ -1239,10 +1241,10 @@ Status forward(const Call& c, const Layout& l, cudaStream_t st) {
 }
 
 template <typename T>
-Ranges<T> ranges(const void* part, int splits, int64_t plane, int64_t ld, int64_t rows, int64_t cols, const int* idx, T* out) {
+Ranges<T> ranges(const void* part, int splits, int64_t plane, int64_t ld, int64_t rows, int64_t cols, const int* idx, T* out, int threads) {
   const bool vec = cols % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0;
   return {static_cast<const float*>(part), splits, plane, ld, rows, (int)cols, idx, out, vec,
-          (int)grid_for(rows * ceil_div(cols, 4), kSumThreads)};
+          (int)grid_for(rows * ceil_div(cols, 4), threads)};
 }
 
 template <typename T>
@@ -1346,15 +1348,18 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
         AGN_TRY(raw_product(c, l, true, reinterpret_cast<float*>(c.work + l.dxs), ldn, l.dx_splits, st));
       else if (c.dx) AGN_TRY(gemm(cx.ctas, kOut, dx, dx_units, st));
     }
+    const int threads = sum_threads(rows, c.dbias);
     Columns columns{};
     Ranges<T> rw{}, rx{};
     if (c.dbias) columns = {db, l.ldp, (int)n, c.dbias + c0, (int)ceil_div(n, 32)};
     if (c.dw && l.dw_splits > 1)
-      rw = ranges<T>(c.work + l.dws, l.dw_splits, dw_rows * ldn, ldn, n, inner, nullptr, dw_out);
+      rw = ranges<T>(c.work + l.dws, l.dw_splits, dw_rows * ldn, ldn, n, inner, nullptr, dw_out,
+                     threads);
     if (c.dx && l.dx_part && c0 + n == c.s.classes)
-      rx = ranges<T>(c.work + l.dxs, l.dx_splits, l.rows_pad * ldn, ldn, rows, inner, idx, static_cast<T*>(c.dx));
+      rx = ranges<T>(c.work + l.dxs, l.dx_splits, l.rows_pad * ldn, ldn, rows, inner, idx, static_cast<T*>(c.dx),
+                     threads);
     const int blocks = columns.blocks + rw.blocks + rx.blocks;
-    if (blocks > 0) AGN_TRY(run(sums_kernel<T>, dim3((unsigned)blocks), kSumThreads, 0, st, columns, rw, rx, live));
+    if (blocks > 0) AGN_TRY(run(sums_kernel<T>, dim3((unsigned)blocks), threads, 0, st, columns, rw, rx, live));
   }
   return Status::Ok();
 }
