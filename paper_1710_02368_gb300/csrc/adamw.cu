@@ -581,7 +581,7 @@ struct KnownPlan {
       p.push_back(q);
     };
     for (const CallBuffer& b : o.buffers) add(b.p, b.bytes);
-    // (tables are not a caller's: the checker's self-test does not shorten them)
+    // (tables are not a caller's: the bounds check's self-test does not shorten them)
     add(o.d_tensors, (size_t)o.tensors * sizeof(Tensor) + 256);
     add(o.d_pieces, (size_t)o.pieces * sizeof(Piece) + 256);
     add(o.d_partials, (size_t)o.norm_grid * sizeof(double) + 256);
