@@ -183,6 +183,7 @@ struct Writer {
   __device__ __forceinline__ void put_rows(const float (&v)[32], T* out, int64_t at, int n, int cols,
                                            bool transposed) {
     constexpr int kRow = 32 * (int)sizeof(T), kVec = 16 / (int)sizeof(T), kLanes = 32 / kVec;
+    if (lane == 0) tc::bulk_wait_read();   // (bulk stores of a joint launch's other product)
     __syncwarp();
     if (transposed) {
       stage_transposed<T>(tile, v);
