@@ -118,7 +118,23 @@ struct Writer {
   uint8_t* tile;
   int lane;
   uint32_t slot;   // 2 KB halves of the tile in turn
+  bool whole = false;   // the last bulk store reads all of the tile
 
+  // Before a half of the tile is overwritten, or all of it: the stores that may still read it have.  (Of halves in
+  // turn all but the last.)
+  __device__ __forceinline__ void wait_half() {
+    if (lane == 0) {
+      if (whole) tc::bulk_wait_read();
+      else tc::bulk_wait_read_1();
+    }
+    whole = false;
+    __syncwarp();
+  }
+  __device__ __forceinline__ void wait_whole() {
+    if (lane == 0) tc::bulk_wait_read();
+    whole = true;
+    __syncwarp();
+  }
   __device__ __forceinline__ void send(uint8_t* src, int x, int y, bool add) {
     tc::fence_proxy_async_smem();
     __syncwarp();
@@ -148,19 +164,15 @@ struct Writer {
   }
   template <typename T>
   __device__ __forceinline__ void put_transposed(const float (&v)[32], int x, int y, bool add) {
-    if (lane == 0) {
-      if (sizeof(T) == 4) tc::bulk_wait_read();
-      else tc::bulk_wait_read_1();
-    }
-    __syncwarp();
+    if (sizeof(T) == 4) wait_whole();
+    else wait_half();
     uint8_t* to = sizeof(T) == 4 ? tile : tile + 2048 * slot;
     slot ^= 1;
     stage_transposed<T>(to, v);
     send(to, x, y, add);
   }
   __device__ __forceinline__ void put_bf16(const uint32_t (&w)[16], int x, int y) {
-    if (lane == 0) tc::bulk_wait_read_1();
-    __syncwarp();
+    wait_half();
     uint8_t* to = tile + 2048 * slot;
     slot ^= 1;
     stage_bf16(to, w);
@@ -173,8 +185,7 @@ struct Writer {
           make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   }
   __device__ __forceinline__ void put_fp32(const float (&v)[32], int x, int y, bool add) {
-    if (lane == 0) tc::bulk_wait_read();
-    __syncwarp();
+    wait_whole();
     stage_fp32(v);
     send(tile, x, y, add);
   }
@@ -183,8 +194,7 @@ struct Writer {
   __device__ __forceinline__ void put_rows(const float (&v)[32], T* out, int64_t at, int n, int cols,
                                            bool transposed) {
     constexpr int kRow = 32 * (int)sizeof(T), kVec = 16 / (int)sizeof(T), kLanes = 32 / kVec;
-    if (lane == 0) tc::bulk_wait_read();   // (bulk stores of a joint launch's other product)
-    __syncwarp();
+    wait_whole();   // (bulk stores of a joint launch's other product)
     if (transposed) {
       stage_transposed<T>(tile, v);
     } else if (sizeof(T) == 4) {

@@ -30,3 +30,12 @@ def joint(agn, rows, inner, classes, dtype, ignored, times=25):
     (300, 1001, 20000, 1, 0.0), (300, 1001, 20000, 1, 0.2), (257, 601, 9000, 0, 0.0), (1500, 333, 5000, 1, 0.0)])
 def test_rows_after_bulk_stores(agn, rows, inner, classes, dtype, ignored):
     joint(agn, rows, inner, classes, dtype, ignored)
+
+
+# bf16 dw by halves of a tile after dx as fp32 sums of ranges or of pieces of the classes; K of few steps, so that
+# its sums are there at once; and the other way round
+@pytest.mark.parametrize("rows,inner,classes,dtype,ignored", [
+    (777, 1000, 10007, 1, 0.0), (256, 2048, 8000, 1, 0.0), (300, 1000, 20000, 1, 0.0), (300, 1000, 20000, 1, 0.3),
+    (256, 520, 30000, 1, 0.0), (9000, 200, 20000, 1, 0.0), (2000, 2048, 300, 1, 0.0), (300, 264, 20000, 0, 0.0)])
+def test_stores_of_both_kinds(agn, rows, inner, classes, dtype, ignored):
+    joint(agn, rows, inner, classes, dtype, ignored)

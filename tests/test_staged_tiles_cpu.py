@@ -4,6 +4,7 @@ source is compiled here for the host with a stand-in for the copy engine that re
 reports a tile that changed in between.  What a tile goes through: the ways out of a launch's products, one
 after the other (of one product in a launch of its own, of two in dw's and dx's joint launch)."""
 
+import itertools
 import os
 import re
 import shutil
@@ -121,3 +122,11 @@ def test_rows_after_bulk_stores(model, way, rows):
     """Rows one by one through a tile that the stores of the product before may still read."""
     for n in (1, 2, 3):
         assert not overwritten(model, way * n + rows + way * n + rows + way)
+
+
+def test_stores_of_all_kinds_in_turn(model):
+    """Half a tile of bf16 after a whole one of fp32 and the other way round, also after rows."""
+    for n in (2, 3, 4):
+        for ways in itertools.product("bfBF", repeat=n):
+            assert not overwritten(model, "".join(ways)), ways
+            assert not overwritten(model, "".join(ways) + "r" + "".join(ways)), ways
