@@ -562,8 +562,9 @@ int agn_linear_ce(const void* x, const void* w, const float* bias, const int32_t
  * Its gradients, from lse alone: with a = scale (dloss + dlse), b = scale dloss of the row,
  *     p[r][c] = a exp(z[r][c] - lse[r]) - b [c = labels[r]];
  *     dx = p w (dtype), dw = p^T x (dtype), dbias[c] = sum_r p[r][c] (fp32)
- * p is computed anew for a piece of the classes at a time; for dx and dw it is rounded to bf16 (AGN_PREC_FP32: three
- * pieces).  Rows left out have dx = 0 and no part in the sums, nor have rows whose lse is minus infinity.
+ * p is computed anew for a piece of the classes at a time; dx and dw take it as two bf16 pieces (2^-17 of it;
+ * AGN_PREC_FP32: three), so that they are rounded to their dtype once; where it is 3.39e38 or more they are NaN.
+ * Rows left out have dx = 0 and no part in the sums, nor have rows whose lse is minus infinity.
  *   lse     : agn_linear_ce's;  dloss, dlse: device fp32 [rows], the gradients of loss (NULL: 1)
  *             and lse (NULL: 0);  scale: a factor of both (1 / rows: of the mean loss);
  *   dx, dw  : 16-byte aligned, dx like x, dw like w, dbias [classes]; NULL = not wanted;

@@ -5,7 +5,7 @@
 // half a tile of columns, 16 bytes for 256 logits; a small kernel joins them.  (Where tiles are few, or w is read as
 // it is, the logits are in scratch for once: products by ranges of K.)  Backward, from the rows'
 // lse alone: the product again, its epilogue turns logits into p, the gradient with respect
-// to them (bf16, fp32 as three bf16 pieces), for a piece of the classes at a time; then dw = p^T x
+// to them (two bf16 pieces, of fp32 operands three), for a piece of the classes at a time; then dw = p^T x
 // and dx += p w of the piece.  Pieces keep p's buffer at 128 MB, w's pieces of fp32 at 96 (384 for few rows).
 // Rows without a label cost nothing and may hold anything: the rows with one are counted and, where
 // some are missing, gathered on the device; all sizes that depend on it are read there.
@@ -24,7 +24,7 @@ namespace ce {
 namespace {
 
 constexpr int kSms = 152;                       // what splits along K are made for
-constexpr int64_t kPieceBytes = 128ll << 20;    // of p
+constexpr int64_t kPieceBytes = 128ll << 20;    // of p's pieces
 constexpr int64_t kPackBytes = 96ll << 20;      // of w's pieces (they stay in the L2)
 constexpr int64_t kPartBytes = 64ll << 20;      // of a product's sums by ranges along K
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -181,7 +181,7 @@ int raw_ranges(int64_t M, int64_t K, int64_t rows) {
 }
 
 struct Layout {
-  int planes;
+  int planes, pieces_p;    // of x and w, of p
   int64_t kp;              // x's and w's row stride where they are packed (whole 128 bytes)
   bool direct;             // bf16 rows that the copy engine reads as they are
   int64_t rows_pad, piece; // classes of a piece (a multiple of 256, but for one piece of all)
@@ -204,6 +204,7 @@ struct Layout {
 Layout layout(const Sizes& s, bool backward) {
   Layout l{};
   l.planes = s.prec == AGN_PREC_FP32 ? 3 : 1;
+  l.pieces_p = p_pieces(l.planes);
   l.kp = round_up(s.inner, 64);
   l.direct = l.planes == 1 && s.inner % 8 == 0;
   l.rows_pad = round_up(s.rows, 256);
@@ -236,7 +237,7 @@ Layout layout(const Sizes& s, bool backward) {
   if (l.raw) l.rows_pad = round_up(s.rows, 64);
   int64_t most = s.classes;
   auto limit = [&](int64_t bytes, int64_t each) { most = std::min(most, std::max<int64_t>(1024, bytes / each / 256 * 256)); };
-  if (backward && !l.raw) limit(kPieceBytes, l.rows_pad * 2 * l.planes);
+  if (backward && !l.raw) limit(kPieceBytes, l.rows_pad * 2 * l.pieces_p);
   if (!l.direct && !l.raw) {   // (so many that tiles of few rows still occupy all SMs)
     const int64_t tm = ceil_div(s.rows, s.rows > 128 ? 256 : 128);
     const int64_t full = (s.rows > 128 ? kSms / 2 * 128 : kSms * 64) / tm;
@@ -282,13 +283,15 @@ Layout layout(const Sizes& s, bool backward) {
     l.ms = take((size_t)l.halves * l.rows_pad * 8);
     l.zlab = take((size_t)l.rows_pad * 4);
   } else {
-    l.p = take((size_t)l.planes * l.rows_pad * l.ldp * 2);
+    l.p = take((size_t)l.pieces_p * l.rows_pad * l.ldp * 2);
     l.db = take((size_t)(l.rows_pad / 32) * l.ldp * 4);
     // x along its rows, for dw, where the products' gain (us, a fifth of their time) is more than a pass over x
     const double elements = (double)s.rows * s.inner;
-    l.x_t = elements * s.classes * (l.planes == 3 ? 14e-10 : 2.3e-10) > elements * (l.planes == 3 ? 1.5e-6 : 0.6e-6) + 2.5;
+    l.x_t = elements * s.classes * (l.planes == 3 ? 14e-10 : 4.6e-10) > elements * (l.planes == 3 ? 1.5e-6 : 0.6e-6) + 2.5;
     if (l.x_t) l.xt = take((size_t)l.planes * round_up(s.inner, 64) * l.rows_pad * 2);
-    const Extents e[2] = {{l.piece, s.inner, s.rows, !l.x_t}, {s.inner, s.rows, l.piece, false}};   // dw, dx (transposed)
+    const int64_t twice = l.planes == 1 ? 2 : 1;   // (steps along K for p's two pieces)
+    const Extents e[2] = {{l.piece, s.inner, twice * round_up(s.rows, 64), !l.x_t},     // dw
+                          {s.inner, s.rows, twice * round_up(l.piece, 64), false}};     // dx (transposed)
     const int dw_ctas = l.piece > 128 ? 2 : 1, dx_ctas = s.inner > 128 ? 2 : 1;
     for (int i = 0; i < 2; ++i) l.grads[i] = cut(i ? dx_ctas : dw_ctas, l.planes, 128, e + i, 1, true);
     if (dw_ctas == dx_ctas && !l.raw) {   // one launch, where one width suits both
@@ -678,7 +681,7 @@ __global__ void __launch_bounds__(1024) logits_loss_kernel(const Logits a, float
 }
 
 // p and its sums over 32 rows: 32 rows x 64 columns a block, eight columns a thread.
-template <int kPlanes>
+template <int kPieces>
 __global__ void __launch_bounds__(kThreads)
 logits_grad_kernel(const Logits a, const float* lse, const float* dloss, const float* dlse, float scale, bf16* p,
                    int64_t ldp, int64_t plane, float* db) {
@@ -710,12 +713,11 @@ logits_grad_kernel(const Logits a, const float* lse, const float* dloss, const f
   bf16 q[3][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (kPlanes == 3) split3(v[i], q[0][i], q[1][i], q[2][i]);
-    else q[0][i] = __float2bfloat16_rn(v[i]);
+    split3(v[i], q[0][i], q[1][i], q[2][i]);
     sums[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + i] = v[i];
   }
 #pragma unroll
-  for (int k = 0; k < kPlanes; ++k)
+  for (int k = 0; k < kPieces; ++k)
     AGN_ST(reinterpret_cast<uint4*>(p + k * plane + row * ldp + c), *reinterpret_cast<const uint4*>(q[k]));
   if (!db) return;
   __syncthreads();
@@ -1260,8 +1262,8 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
   GemmLaunch z{}, dw{}, dx{};
   z.n = dw.n = dx.n = 1;
   AGN_TRY(x_maps(c, l, 64, l.a_box, &z.maps[0].a, &z.maps[0].alt));
-  AGN_TRY(make_tmap_store_2d(&z.maps[0].c, p, 2, l.ldp, l.planes * l.rows_pad, l.ldp, 32, 32));
-  AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].a, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, 64));
+  AGN_TRY(make_tmap_store_2d(&z.maps[0].c, p, 2, l.ldp, l.pieces_p * l.rows_pad, l.ldp, 32, 32));
+  AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].a, p, l.ldp, l.rows_pad, l.pieces_p, l.ldp, p_plane, 64, 64));
   const Cut &cw = l.grads[0], &cx = l.both ? l.grads[0] : l.grads[1];
   if (!l.x_t) {
     AGN_TRY(x_maps(c, l, 64, 64, &dw.maps[0].b, &dw.maps[0].alt));
@@ -1272,7 +1274,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
                 static_cast<const T*>(c.x), (int)inner, idx, live, xt, l.rows_pad, plane));
     AGN_TRY(make_tmap_bf16_3d(&dw.maps[0].b, xt, l.rows_pad, inner, l.planes, l.rows_pad, plane, 64, cw.bn / cw.ctas));
   }
-  AGN_TRY(make_tmap_bf16_3d(&dx.maps[0].b, p, l.ldp, l.rows_pad, l.planes, l.ldp, p_plane, 64, cx.bn / cx.ctas));
+  AGN_TRY(make_tmap_bf16_3d(&dx.maps[0].b, p, l.ldp, l.rows_pad, l.pieces_p, l.ldp, p_plane, 64, cx.bn / cx.ctas));
   const bool rows16 = inner * es % 16 == 0;
   for (int64_t c0 = 0; c0 < c.s.classes; c0 += l.piece) {
     const int64_t n = std::min(l.piece, c.s.classes - c0);
@@ -1280,7 +1282,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
     if (l.z_splits > 1 || l.raw) {
       Logits a;
       AGN_TRY(logit_ranges(c, l, z, false, st, &a));
-      AGN_TRY(run(logits_grad_kernel<sizeof(T) == 4 ? 3 : 1>, dim3((unsigned)(l.ldp / 64), (unsigned)(l.rows_pad / 32)),
+      AGN_TRY(run(logits_grad_kernel<sizeof(T) == 4 ? 3 : 2>, dim3((unsigned)(l.ldp / 64), (unsigned)(l.rows_pad / 32)),
                   kThreads, 0, st, a, c.lse, c.dloss, c.dlse, c.scale, p, l.ldp, p_plane, c.dbias ? db : nullptr));
     } else {
       AGN_TRY(w_map(c, l, c0, n, 64, l.z.bn / l.z.ctas, &z.maps[0].b));
@@ -1299,6 +1301,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       d = common_args(c, l);
       d.M = (int)n; d.N = (int)inner; d.K = (int)rows;
       d.live_is = 1;
+      d.twice = l.planes == 1 ? 1 : 0;
       d.alt = l.direct && !l.x_t ? 2 : 0;
       d.bn = cw.bn;
       d.a_mn = 1;
@@ -1320,6 +1323,7 @@ Status backward(const Call& c, const Layout& l, cudaStream_t st) {
       d = common_args(c, l);
       d.M = (int)inner; d.N = (int)rows; d.K = (int)n;
       d.live_is = 2;
+      d.twice = l.planes == 1 ? 2 : 0;
       d.transposed = 1;
       d.bn = cx.bn;
       d.a_mn = 1;

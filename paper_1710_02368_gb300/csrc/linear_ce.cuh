@@ -15,6 +15,11 @@ enum Epilogue {
   kOut = 2,    // the product itself
 };
 
+// Pieces of p, the gradient with respect to the logits, as the products read it: of bf16 operands two (one would
+// round it, the factor 1 / rows of a mean loss among it, to 2^-8 of it: 777 x 1000 to 10007, dx off by 2.5e-3 of its
+// norm where rounding it alone is 1.7e-3; two hold 2^-17).  Each is a product: dw and dx take twice the MMAs.
+constexpr int p_pieces(int planes) { return planes == 3 ? 3 : 2; }
+
 // One product of [M][K] and [N][K] operands.  Coordinates are elements; rows of x are
 // those with a label, in order (`live` of them, `idx` their places).
 struct GemmArgs {
@@ -27,6 +32,7 @@ struct GemmArgs {
   int a_mn, b_mn;           // operand stored [K][M] ([K][N]) instead
   int b_k0, b_n0;           // where B's rows of this product start along K, along N
   int planes;               // 1, or 3 bf16 pieces of fp32 operands: six products
+  int twice;                // planes 1: 1 (2): A (B) is p in two bf16 pieces, by steps of 64 k in turn
   int a_box;                // rows of A's boxes (128, fewer where M is less; its box is 64 along M with a_mn)
   int splits;               // ranges along K, each with sums of its own (kOut)
   int* err;
@@ -43,7 +49,7 @@ struct GemmArgs {
   float* zlab;              // kLse: [rows_pad] the label's logit
   const float *lse, *dloss, *dlse;   // kGrad, by place
   float scale;
-  int p_plane;              // kGrad: rows from piece to piece of p
+  int p_plane;              // kGrad: rows from piece to piece of p (p_pieces of them)
   float* db;                // kGrad: [rows_pad / 32][ld_db] column sums of 32 rows, or null
   int64_t ld_db;
   // kOut

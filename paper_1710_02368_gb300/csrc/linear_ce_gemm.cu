@@ -1,7 +1,7 @@
 // The three products of the output layer's loss on the tensor cores (tcgen05 kind::f16, f32
 // sums in TMEM), with what follows each in its epilogue:
 //   logits z = x w^T (K along both operands' rows): kLse leaves (max, sum of exponentials) of
-//     each row and half a tile, kGrad writes p = a softmax - b [label] in bf16 and sums its columns;
+//     each row and half a tile, kGrad writes p = a softmax - b [label] in bf16 pieces and sums its columns;
 //   dw = p^T x and dx = p w (kOut): the MMA takes operands stored along M or N (MN-major) too, but
 //     B's so stored cost it: 256 x 256 tiles of 8192 x 8192 x 4096 1.25 times the clocks, A's none (B's reads
 //     of shared memory, it seems, twice as many).  So dx is made as w^T p^T, p in B's place as it lies,
@@ -59,7 +59,7 @@ __device__ __forceinline__ Geometry geometry(const GemmArgs& a) {
   g.tiles_n = (g.N + a.bn - 1) / a.bn;
   g.tiles = (g.M + 128 * kCtas - 1) / (128 * kCtas) * g.tiles_n;
   g.units = g.tiles * a.splits;
-  g.KT = (g.K + kBK - 1) / kBK;
+  g.KT = (g.K + kBK - 1) / kBK * (a.twice ? 2 : 1);
   g.kt_per = (g.KT + a.splits - 1) / a.splits;
   return g;
 }
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         const Unit t = unit_of(at);
         const int m = (t.m * kCtas + cta) * 128, n = t.n * bn + cta * nb;
         const bool a_mn = a.a_mn, b_mn = a.b_mn;
-        const int b_k0 = a.b_k0, b_n0 = a.b_n0;
+        const int b_k0 = a.b_k0, b_n0 = a.b_n0, twice = a.twice;
         if (a.withhold == cta + 1) stop = max(0, t.kt * kPlanes - 1);
         for (int kt = t.kt0; ok && kt < t.kt0 + t.kt; ++kt) {
 #pragma unroll 1
@@ -384,22 +384,23 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
               break;
             }
             uint8_t* st = ring + s * stage;
-            auto load = [&](uint8_t* dst, const CUtensorMap* map, int x, int y) {
-              if (kCtas == 2) tc::tma_load_3d_pair(dst, map, full0 + 8u * (uint32_t)s, x, y, z);
-              else tc::tma_load_3d(dst, map, &full[s], x, y, z);
+            auto load = [&](uint8_t* dst, const CUtensorMap* map, int x, int y, int piece) {
+              if (kCtas == 2) tc::tma_load_3d_pair(dst, map, full0 + 8u * (uint32_t)s, x, y, piece);
+              else tc::tma_load_3d(dst, map, &full[s], x, y, piece);
             };
             if (cta == 0) tc::mbar_arrive_expect_tx(&full[s], kCtas * stage);
-            const int k = kt * kBK;
+            const int k = (twice ? kt >> 1 : kt) * kBK;
+            const int za = twice == 1 ? kt & 1 : z, zb = twice == 2 ? kt & 1 : z;
             if (a_mn) {
-              load(st, pa, m, k);
-              load(st + kBox, pa, m + 64, k);
+              load(st, pa, m, k, za);
+              load(st + kBox, pa, m + 64, k, za);
             } else {
-              load(st, pa, k, m);
+              load(st, pa, k, m, za);
             }
             if (b_mn) {
-              for (int j = 0; j < nb; j += 64) load(st + a_bytes + j * 128, pb, n + j, k + b_k0);
+              for (int j = 0; j < nb; j += 64) load(st + a_bytes + j * 128, pb, n + j, k + b_k0, zb);
             } else {
-              load(st + a_bytes, pb, k, n + b_n0);
+              load(st + a_bytes, pb, k, n + b_n0, zb);
             }
             ++loaded;
             if (++s == stages) s = 0, phase ^= 1;
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
 #pragma unroll
-          for (int z = 0; z < kPlanes; ++z) {
+          for (int z = 0; z < p_pieces(kPlanes); ++z) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {

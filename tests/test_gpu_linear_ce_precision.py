@@ -1,0 +1,39 @@
+"""What the output layer's loss and its gradients keep of their operands, in norms (the bounds of train_ops_ref are
+worst cases of every element and every addition)."""
+
+import math
+
+import pytest
+import torch
+
+import test_gpu_linear_ce as L
+import train_ops_ref as T
+
+pytestmark = pytest.mark.gpu
+agn = L.agn
+
+
+def norm(t):
+    return float(t.double().norm())
+
+
+# pairs of CTAs; rows left out; several pieces of the classes; one CTA a tile; logits by ranges of K in scratch; few rows
+@pytest.mark.parametrize("rows,inner,classes,ignored", [
+    (777, 1000, 10007, 0.3), (300, 264, 1000, 0.0), (600, 1001, 900, 0.0), (11000, 64, 8003, 0.1), (100, 1000, 999, 0.0),
+    (60, 333, 3000, 0.2), (300, 3000, 200, 0.0), (70, 5000, 600, 0.1), (3, 1000, 777, 0.0), (40, 200, 60, 0.0)])
+def test_bf16_gradients_are_rounded_once(agn, rows, inner, classes, ignored):
+    """dx and dw are as far from the 64-bit ones as those rounded to bf16 are: that is 1.7e-3 of the norm (a half step
+    of 2^-8 over mantissas of all sizes), while p in two pieces is off by 2^-17 and logits by some 1e-6: together
+    2 % of that at most, and 5 % are allowed.  (p in one bf16 piece makes it 1.4 times, by the rounding of the scale alone.)"""
+    x, w, b, labels = L.make(rows, inner, classes, 1, ignored=ignored)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    dlse = 1e-2 * torch.randn(rows, generator=g, device="cuda")
+    scale = 1.0 / 777
+    ref = T.linear_ce(x, w, b, labels, None, dlse, scale)
+    _, lse = L.forward(agn, x, w, b, labels, 1)
+    out = L.backward(agn, x, w, b, labels, lse, 1, scale=scale, dlse=dlse)
+    for k in ("dx", "dw"):
+        once = norm(ref[k].bfloat16().double() - ref[k])
+        assert norm(out[k].double() - ref[k]) <= 1.05 * once, k
+    assert norm(out["dbias"].double() - ref["dbias"]) <= 2.0 ** -16 * norm(ref["p_size"].sum(0))
