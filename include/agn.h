@@ -537,9 +537,9 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
  * hold anything.  A class with a bias of minus infinity takes no part; where no class does,
  * lse is minus infinity and loss infinity.  A logit that is NaN or plus infinity makes them NaN.
  *   x       : device [rows][inner], w: device [classes][inner], both of dtype (AGN_PREC_FP32, whose products
- *             are those of three exact bf16 pieces, or AGN_PREC_BF16; sums fp32, in bf16 of more than
- *             128 rows cut off, not rounded, by the tensor cores: 1e-6 of the loss at inner 4096), rows one after the
- *             other, 16-byte aligned;
+ *             are those of three exact bf16 pieces, or AGN_PREC_BF16; sums fp32: the tensor cores cut them off, not
+ *             rounded, up to 512 k, in bf16 of more than 128 rows up to 1024, and those are added rounded),
+ *             rows one after the other, 16-byte aligned;
  *   bias    : device fp32 [classes], NULL = none;  labels: device int32 [rows];
  *   loss, lse: device fp32 [rows];
  *   work    : device scratch, 256-byte aligned, of at least agn_linear_ce_bytes(...) bytes (backward 0); it

@@ -8,8 +8,8 @@
 //     and leaves transposed, and x is laid out along its rows for dw where that pays.
 // fp32 operands are three exact bf16 pieces (planes): six products of pieces, the first in one
 // accumulator and the five smaller ones in another.  The tensor cores cut what they add to an
-// accumulator off below its last bit, always towards zero, so these sums are taken over 256 k at
-// a time and added in registers, rounded (one accumulator over K = 50000: 1.5e-5 of dx off).
+// accumulator off below its last bit, always towards zero, so sums are taken over a part of K at
+// a time (sum_steps) and added in registers, rounded (fp32, one accumulator over K = 50000: 1.5e-5 of dx off).
 // Many fp32 tiles are 256 x 256 as bf16's are, both accumulators then fill TMEM: their sums (512 k) are
 // read between the MMAs, the larger one's first, so that its next products run while the other is read.
 // One CTA a tile of 128 rows, or a pair (cta_group::2) a tile of 256, each CTA loading its 128 rows
@@ -34,7 +34,12 @@ constexpr int kBK = 64;                   // k of a stage: 128-byte rows
 constexpr int kBox = 64 * 128;            // an operand stored along M or N: boxes of 64 x 64 k
 constexpr int kRing = 176 * 1024;
 constexpr int kMaxStages = 16;
-constexpr int kPartK = 4, kPartKWide = 8; // fp32: stages' k of a sum in TMEM, of bf16's losses kPartKWide
+// Stages of a sum in TMEM, where there are more of them the rest is added in registers: fp32 256 k, wide tiles 512; bf16's
+// logits by one CTA 512, by pairs 1024 (by 512 the tensor cores wait for it: 8192 x 4096 to 32768 1252 us, by 1024 1168,
+// one sum 1121); bf16's gradients 8192 k of p's pieces (2e-5 of them, their rounding 2e-3).
+constexpr int sum_steps(int ctas, int epilogue, int planes, bool wide) {
+  return planes == 3 ? (wide ? 8 : 4) : epilogue == kOut ? 128 : ctas == 2 ? 16 : 8;
+}
 constexpr int kStaged = 4096;             // a finishing warp's tile of outputs
 constexpr size_t kSmem = 1024 + kRing + 8 * (kStaged + 512) + 512;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -251,9 +256,8 @@ __device__ __forceinline__ void land(uint64_t* full, const int* loaded, int stag
   }
 }
 
-// kWide: the finishing warps hold 128 sums a thread: fp32 tiles of 256 columns; bf16's losses of up to 128 rows with K
-// above 1024, whose sums over 512 k are added in registers as fp32's are (one row, K = 4096: the loss is off by 2e-7 of it,
-// by 1.7e-6 with one sum; 47 us for 46.  Pairs of CTAs, which the tensor cores bound, took a tenth longer so).
+// kWide: the finishing warps hold 128 sums a thread: fp32 tiles of 256 columns; bf16 with more k than a sum takes
+// (one row, K = 4096: the loss is off by 2e-7 of it, by 1.7e-6 with one sum; K = 65536, sums that only grow: 2e-4).
 template <int kCtas, int kEpi, int kPlanes, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ GemmLaunch launch) {
   extern __shared__ uint8_t smem_raw[];
@@ -323,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
   constexpr uint32_t kSets = kPlanes == 3 ? 2 : 1;   // accumulators of a sum
   const uint32_t acc_cols = kSets * bn;
   constexpr bool kOne = kWide && kPlanes == 3;   // one set of sums in TMEM, not two in turn
-  constexpr int kSumK = kWide ? kPartKWide : kPartK;
+  constexpr int kSumK = sum_steps(kCtas, kEpi, kPlanes, kWide);
   // Unit i of this CTA (pair): of product p, number u.  One product: in turn.  Two: the longer units first, in
   // turn; the CTAs that then have one less begin with as many of the shorter as take that one's time, and are
   // the first when the rest is given out in turn.
@@ -674,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         constexpr int kMost = kWide ? 4 : 2;   // chunks
         float v[kMost][32];
 #pragma unroll
-        for (int i = 0; i < 32 * kMost; ++i) v[i / 32][i % 32] = 0.f;
+        for (int i = 0; i < 32 * kMost; ++i) v[i / 32][i % 32] = -0.f;   // (one sum stays as it is)
         // adds one accumulator's columns of a chunk, 16 at a time
         auto add = [&](uint32_t at, float (&sum)[32]) {
 #pragma unroll
@@ -762,11 +766,7 @@ Status queue(const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
 
 template <int kCtas, int kPlanes, bool kWide = false>
 Status queue_for(int epilogue, const GemmLaunch& g, int64_t max_units, cudaStream_t st) {
-  if (epilogue == kLse) {
-    if (kCtas == 1 && kPlanes == 1 && g.args[0].K > 1024)
-      return queue<kCtas, kLse, kPlanes, kWide || (kCtas == 1 && kPlanes == 1)>(g, max_units, st);
-    return queue<kCtas, kLse, kPlanes, kWide>(g, max_units, st);
-  }
+  if (epilogue == kLse) return queue<kCtas, kLse, kPlanes, kWide>(g, max_units, st);
   if (epilogue == kGrad) return queue<kCtas, kGrad, kPlanes, kWide>(g, max_units, st);
   return queue<kCtas, kOut, kPlanes, kWide>(g, max_units, st);
 }
@@ -777,9 +777,16 @@ Status gemm(int ctas, int epilogue, const GemmLaunch& launch, int64_t max_units,
   GemmLaunch g = launch;
   for (GemmArgs& a : g.args)
     if (!a.wait_ns) a.wait_ns = (uint32_t)kWaitNs;
+  bool wide = false;   // bf16: more than a sum
+  for (int i = 0; i < g.n; ++i) {
+    const int64_t steps = ceil_div(g.args[i].K, kBK) * (g.args[i].twice ? 2 : 1);
+    wide = wide || ceil_div(steps, g.args[i].splits) > std::max(16, sum_steps(ctas, epilogue, 1, true));
+  }
   if (g.args[0].planes == 3 && g.args[0].bn == 256) return queue_for<2, 3, true>(epilogue, g, max_units, st);
   if (g.args[0].planes == 3)
     return ctas == 2 ? queue_for<2, 3>(epilogue, g, max_units, st) : queue_for<1, 3>(epilogue, g, max_units, st);
+  if (wide)
+    return ctas == 2 ? queue_for<2, 1, true>(epilogue, g, max_units, st) : queue_for<1, 1, true>(epilogue, g, max_units, st);
   return ctas == 2 ? queue_for<2, 1>(epilogue, g, max_units, st) : queue_for<1, 1>(epilogue, g, max_units, st);
 }
 

@@ -37,3 +37,25 @@ def test_bf16_gradients_are_rounded_once(agn, rows, inner, classes, ignored):
         once = norm(ref[k].bfloat16().double() - ref[k])
         assert norm(out[k].double() - ref[k]) <= 1.05 * once, k
     assert norm(out["dbias"].double() - ref["dbias"]) <= 2.0 ** -16 * norm(ref["p_size"].sum(0))
+
+
+@pytest.mark.parametrize("rows,classes", [(2048, 9728), (100, 19456)])
+def test_bf16_logits_of_a_long_inner_side(agn, rows, classes):
+    """Sums that only grow, over 65536 k.  A sum in the tensor cores loses two units of 2^-23 of itself at most in
+    each addition (16 products), so sums of 64 additions, of which 64 are rounded, 2 (64 + 8) 2^-23 + 64 2^-24; over
+    all of K it would be some 1e-4.  (All classes have the same logit, so the reference is a product with one vector.)"""
+    inner = 65536
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x = (0.5 + torch.rand(rows, inner, generator=g, device="cuda")).bfloat16()
+    v = ((0.5 + torch.rand(inner, generator=g, device="cuda")) * 2.0 ** -12).bfloat16()
+    w = v.expand(classes, inner).contiguous()
+    labels = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    want = x.double() @ v.double() + math.log(classes)
+    loss, lse = L.forward(agn, x, w, None, labels, 1)
+    assert float(((lse - want) / want).abs().max()) <= 2 * 72 * 2.0 ** -23 + 66 * 2.0 ** -24
+    lse = want.float()   # p is 1 / classes by the same logits
+    db = L.backward(agn, x, w, None, labels, lse, 1, dloss=torch.zeros(rows, device="cuda"),
+                    dlse=torch.ones(rows, device="cuda"), without=("dx", "dw"))["dbias"]
+    # exp of an error of z, 32 or so
+    assert float((db * (classes / rows) - 1).abs().max()) <= 1.1 * float(want.max()) * (2 * 72 * 2.0 ** -23 + 66 * 2.0 ** -24)
