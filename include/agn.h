@@ -589,7 +589,7 @@ int agn_linear_ce_backward(const void* x, const void* w, const float* bias, cons
  * of the tensor ([ceil(n / 32)]).  A scale byte E is 2^(E - 127) (0 is 0, so zeroed states are zeros);
  * a code of m is a sign (bit 7), 4 bits of exponent x and 3 of mantissa f, of r 4 and 4 bits: the
  * scale times (1 + f / 2^b) 2^(x - 15), with x = 0 f / 2^b 2^-14, b = 3 or 4.  The scale
- * is the least power of two that brings the block's largest magnitude to 2 - 2^-b or below (E in 1 .. 253).
+ * is the least power of two that brings the block's largest finite magnitude to 2 - 2^-b or below (E in 1 .. 253).
  * Values are rounded up or down at random, in proportion (a step changes v by 1/1000
  * of it where b2 = 0.999, less than half a code: to the nearest it would never move): up
  * where the fraction between both codes plus (16 bits + 1/2) / 65536 reaches 1, never from r > 0 to 0.
@@ -640,8 +640,9 @@ int agn_optim_grad_norm(agn_optim* plan, double max_norm, float* norm, float* sc
 /*
  * One step.  scale: device fp32 [1], read when the step runs (agn_optim_grad_norm's, or a loss
  * scale's inverse), NULL = 1; where it is not finite, nothing changes.  eps: 0 or a normal fp32
- * number up to 1e30.  A captured call keeps its lr, step, seed and offset.  Element by element: a
- * NaN or infinity without scale goes into the states (8 bits: the largest codes).
+ * number up to 1e30.  A captured call keeps its lr, step, seed and offset.  Element by element: a gradient
+ * that is not finite, or whose square is not, touches no other element; without scale it goes into its states (8
+ * bits: m becomes 0 and the code of r the largest).
  * Errors: AGN_E_INVALID, AGN_E_CUDA.
  */
 int agn_optim_adamw(agn_optim* plan, double lr, int64_t step, double beta1, double beta2, double eps,

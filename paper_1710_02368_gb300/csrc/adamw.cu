@@ -240,18 +240,21 @@ __device__ __forceinline__ void step_eight(const StepArgs& a, const Tensor& t, f
 #pragma unroll
   for (int i = 0; i < 8; ++i) step_one(a, g[i], keep, p[i], m[i], v[i], r[i]);
   if (kBits == 8) {
-    uint32_t top_m = 0, top_r = 0;
+    auto scales = [&](auto finite) {   // finite: of the values that are
+      uint32_t top_m = 0, top_r = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu);
-      top_r = max(top_r, __float_as_uint(r[i]));
-    }
+      for (int i = 0; i < 8; ++i) {
+        top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu);
+        if (!decltype(finite)::value || r[i] <= FLT_MAX) top_r = max(top_r, __float_as_uint(r[i]));
+      }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      top_m = max(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
-      top_r = max(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
-    }
-    em = scale_code<kMantM>(top_m), er = scale_code<kMantR>(top_r);
+      for (int o = 1; o < 4; o <<= 1) {
+        top_m = max(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
+        top_r = max(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
+      }
+      em = scale_code<kMantM>(top_m), er = scale_code<kMantR>(top_r);
+    };
+    scales(std::false_type());
     const uint64_t d0 = a.key + (a.offset + t.first + (uint64_t)(e / 2) + 1) * gen::kG;
     uint32_t cm[8], cr[8];
     auto codes = [&](auto once) {
@@ -272,8 +275,17 @@ __device__ __forceinline__ void step_eight(const StepArgs& a, const Tensor& t, f
         }
       }
     };
-    if (__any_sync(0xffffffffu, max(em, er) > kOnceMost)) codes(std::false_type());
-    else codes(std::true_type());
+    if (__any_sync(0xffffffffu, max(em, er) > kOnceMost)) {
+      // An element whose v is not finite stays out of its block's scales, which would be the largest and leave the
+      // others nothing: its m becomes 0 and its sqrt(v) the largest code.
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (!(r[i] <= FLT_MAX)) m[i] = 0.f;
+      scales(std::true_type());
+      codes(std::false_type());
+    } else {
+      codes(std::true_type());
+    }
     if (n > 0) {
       store8_codes(static_cast<uint8_t*>(t.m) + e, n, wide, cm);
       store8_codes(static_cast<uint8_t*>(t.v) + e, n, wide, cr);
