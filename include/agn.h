@@ -629,8 +629,9 @@ void agn_optim_destroy(agn_optim* plan);
 /*
  * norm[0] = sqrt(sum of all gradients' squares) and scale[0] = the factor that clips it: max_norm /
  * norm where norm > max_norm (> 0, infinity: none), else 1; NaN where the norm is not finite.  Device fp32,
- * either may be NULL.  Squares are fp32 (a gradient from 1.8e19 up gives an infinite norm, one
- * below 1e-23 counts as 0), sums fp32 of 64 at most, then 64-bit; equal calls on a device give equal bits.  The
+ * either may be NULL.  Squares are fp32 (a gradient below 1e-19 loses bits, one below 1e-23 counts as 0), and so are sums of
+ * up to 32 of them, a thread's sum of those, with its remainder, and a warp's 32; the rest is 64-bit, and where fp32 would
+ * overflow all of it.  Equal calls on a device give equal bits.  The
  * plan has one scratch array for it: order the norms of a plan on one stream, or by events.
  * Queued on `stream`, may be captured; so is agn_optim_adamw.
  * Errors: AGN_E_INVALID, AGN_E_CUDA.

@@ -441,8 +441,9 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const StepArgs a) {
   }
 }
 
-// Squares and a thread's sums of up to 32 of them in fp32, those with the rounding's remainder carried along;
-// a warp's 32 in fp32, the rest in 64 bits (an SM adds few of those: sums of threads took most of the time).
+// Squares and sums of up to 32 of them in fp32, a thread's sum of these with the rounding's remainder carried along,
+// a warp's 32 in fp32, the rest in 64 bits (an SM adds few of those: sums of threads took most of the time).  Gradients of
+// 1e18 and more can take that out of fp32's range, though the norm is a number: such a warp reads its gradients once more.
 constexpr int kNormPieces = 4;   // in flight
 __global__ void __launch_bounds__(kThreads)
 norm_kernel(const Tensor* tensors, const Piece* pieces, int n_pieces, double* partials) {
@@ -487,23 +488,47 @@ norm_kernel(const Tensor* tensors, const Piece* pieces, int n_pieces, double* pa
     }
   };
   const int last = (int)((int64_t)n_pieces * (blockIdx.x + 1) / gridDim.x);
-  for (int c = (int)((int64_t)n_pieces * blockIdx.x / gridDim.x); c < last;) {
-    const Piece piece = AGN_LD(pieces + c);
-    const Tensor t = AGN_LD(tensors + piece.tensor);
-    const int64_t end = min((int64_t)piece.index + last - c, (t.n + kPiece - 1) / kPiece);
-    if (t.bf16_grad) squares(bf16(), t, piece.index, end);
-    else squares(float(), t, piece.index, end);
-    c += (int)(end - piece.index);
-  }
+  auto each_run = [&](auto&& f) {
+    for (int c = (int)((int64_t)n_pieces * blockIdx.x / gridDim.x); c < last;) {
+      const Piece piece = AGN_LD(pieces + c);
+      const Tensor t = AGN_LD(tensors + piece.tensor);
+      const int64_t end = min((int64_t)piece.index + last - c, (t.n + kPiece - 1) / kPiece);
+      if (t.bf16_grad) f(bf16(), t, piece.index, end);
+      else f(float(), t, piece.index, end);
+      c += (int)(end - piece.index);
+    }
+  };
+  each_run(squares);
   if (fabsf(sum) <= FLT_MAX) sum += rest;   // (an infinite sum's remainder is NaN)
+  __shared__ double warps[kThreads / 32];
+  if (__any_sync(0xffffffffu, !(sum < 0x1p122f))) {   // a warp whose sum may leave fp32's range: anew in 64 bits
+    double all = 0.0;
+    each_run([&](auto kind, const Tensor& t, int64_t index, int64_t end) {
+      using G = decltype(kind);
+      for (; index < end; ++index) {
+        const int64_t e = index * kPiece + threadIdx.x * kPer;
+        const int n = (int)max((int64_t)0, min((int64_t)kPer, t.n - e));
+        if (n <= 0) continue;
+        Raw<G> raw;
+        load8(static_cast<const G*>(t.grad) + e, n, t.wide && n == kPer, raw);
+        float g[8];
+        unpack8(raw, g);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  __shared__ float warps[kThreads / 32];
-  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
+        for (int i = 0; i < 8; ++i) all = fma((double)g[i], (double)g[i], all);
+      }
+    });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = all;
+  } else {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = (double)sum;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
     double all = warps[0];
-    for (int w = 1; w < kThreads / 32; ++w) all += (double)warps[w];
+    for (int w = 1; w < kThreads / 32; ++w) all += warps[w];
     AGN_ST(partials + blockIdx.x, all);
   }
 }
