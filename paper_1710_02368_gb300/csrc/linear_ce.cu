@@ -784,15 +784,21 @@ __device__ __forceinline__ void sum_ranges(const Ranges<T>& a, int block, int li
   }
 }
 
-// 32 columns a block, whose warps share the blocks of rows.
+// 32 columns a block, whose warps share the blocks of rows; a warp's sum carries what rounding leaves (2^28 rows are
+// 2^18 additions for it; Knuth's two-sum).
 __device__ __forceinline__ void sum_columns(const Columns& a, int block, int live) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   const int blocks = (live + 31) / 32, c = block * 32 + lane;
   __shared__ float part[kSumThreads / 32][33];
-  float s = 0.f;
+  float s = 0.f, rest = 0.f;
   if (c < a.cols) {
 #pragma unroll 4
-    for (int b = warp; b < blocks; b += warps) s += AGN_LD(a.db + b * a.ld + c);
+    for (int b = warp; b < blocks; b += warps) {
+      const float v = AGN_LD(a.db + b * a.ld + c), both = __fadd_rn(s, v), back = __fsub_rn(both, s);
+      rest = __fadd_rn(rest, __fadd_rn(__fsub_rn(s, __fsub_rn(both, back)), __fsub_rn(v, back)));
+      s = both;
+    }
+    if (fabsf(s) <= FLT_MAX) s += rest;   // (an infinite sum's remainder is NaN)
   }
   part[warp][lane] = s;
   __syncthreads();

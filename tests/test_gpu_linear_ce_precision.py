@@ -59,3 +59,19 @@ def test_bf16_logits_of_a_long_inner_side(agn, rows, classes):
                     dlse=torch.ones(rows, device="cuda"), without=("dx", "dw"))["dbias"]
     # exp of an error of z, 32 or so
     assert float((db * (classes / rows) - 1).abs().max()) <= 1.1 * float(want.max()) * (2 * 72 * 2.0 ** -23 + 66 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_bias_gradient_of_very_many_rows(agn, dtype):
+    """Equal terms, which plain fp32 sums round the same way in every addition (1e-5 here): 32 rows are five
+    additions, of a warp's part only the total is rounded, and 32 parts are added."""
+    rows, inner, classes = 1 << 22, 8, 33
+    x = torch.zeros(rows, inner, device="cuda", dtype=L.DT[dtype])
+    w = torch.zeros(classes, inner, device="cuda", dtype=L.DT[dtype])
+    zeros = torch.zeros(rows, device="cuda")
+    labels = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    for term in (2.0 / 3, 0.7, 1.0 + 2.0 ** -20):
+        dlse = torch.full((rows,), term, device="cuda")
+        out = L.backward(agn, x, w, None, labels, zeros, dtype, dloss=zeros, dlse=dlse, without=("dx", "dw"))
+        want = rows * float(dlse[0])   # (z = lse = 0: p is dlse)
+        assert float((out["dbias"].double() / want - 1).abs().max()) <= 40 * 2.0 ** -24
