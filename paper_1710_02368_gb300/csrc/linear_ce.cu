@@ -64,18 +64,14 @@ double makespan(int64_t at_once, const int64_t (&n)[2], const double (&cost)[2])
   const int longer = cost[1] > cost[0] ? 1 : 0;
   const int64_t q = n[longer] / at_once, rest = n[longer] % at_once, others = n[1 - longer];
   const double low = q * cost[longer], high = low + (rest ? cost[longer] : 0), each = cost[1 - longer];
-  if (others == 0) return high;
-  auto room = [&](double t) {   // for the shorter ones by time t
-    auto fit = [&](double from) { return t < from ? 0 : (int64_t)((t - from) / each + 1e-9); };
-    return rest * fit(high) + (at_once - rest) * fit(low);
-  };
-  double t = std::max(high, low + each * std::floor((double)others / at_once));
-  if (room(high) >= others) t = high;
-  while (room(t) < others) {   // to the next time at which one ends
-    auto next = [&](double from) { return from + (std::floor((t - from) / each + 1e-9) + 1) * each; };
-    t = std::min(next(low), next(high));
-  }
-  return t;
+  // By `high` the CTAs that have no longer unit more have done `ahead` of the shorter ones each, and `part` of another.
+  const double apart = rest ? cost[longer] / each : 0;
+  const int64_t ahead = (int64_t)(apart + 1e-9), left = others - (at_once - rest) * ahead;
+  if (left <= 0) return high;
+  // Then all do `late` each; what is still left takes those a part of one first.
+  const double part = std::max(0.0, apart - (double)ahead);
+  const int64_t late = left / at_once, over = left % at_once;
+  return high + ((double)late + (over == 0 ? 0.0 : over <= at_once - rest ? 1.0 - part : 1.0)) * each;
 }
 
 // Tile width by the estimated time: rounds of tiles over the SMs, or B's bytes from memory (24 a clock and
