@@ -310,7 +310,6 @@ Layout layout(const Sizes& s, bool backward) {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void from_float(float* p, float v) { AGN_ST(p, v); }
@@ -554,12 +553,6 @@ transpose_kernel(const T* x, int inner, const int* idx, const int* live_p, bf16*
                  make_uint4(w[0], w[1], w[2], w[3]));
       }
   }
-}
-
-// (maximum, sum of exponentials) of two sets of values.
-__device__ __forceinline__ float2 join(float2 a, float2 b) {
-  const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;
-  return make_float2(most, a.y * exp2f((a.x - from) * kLog2e) + b.y * exp2f((b.x - from) * kLog2e));
 }
 
 // lse and loss from the partial maxima and sums: a warp a row, or where there are few rows a block.  idx

@@ -1,13 +1,25 @@
 // The output layer's softmax cross-entropy over many classes without keeping the
-// logits (linear_ce.cu: entry points and small kernels; linear_ce_gemm.cuh: the products).
+// logits (linear_ce.cu: entry points and small kernels; linear_ce_gemm.cu, linear_ce_raw.cu: the products;
+// linear_ce_few.cu: a few rows).
 #pragma once
 
 #include <cuda.h>
+
+#include <cmath>
 
 #include "common.cuh"
 
 namespace agn {
 namespace ce {
+
+__device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
+
+// (maximum, sum of exponentials) of two sets of values.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  constexpr float kLog2e = 1.44269504088896340736f;
+  const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;
+  return make_float2(most, a.y * exp2f((a.x - from) * kLog2e) + b.y * exp2f((b.x - from) * kLog2e));
+}
 
 enum Epilogue {
   kLse = 0,    // each row's maximum and sum of exponentials over a tile's columns
@@ -30,7 +42,6 @@ struct GemmArgs {
   int alt;                  // 1 (2): A (B) comes from tmAlt where x was gathered
   int bn;                   // columns of a tile
   int a_mn, b_mn;           // operand stored [K][M] ([K][N]) instead
-  int b_k0, b_n0;           // where B's rows of this product start along K, along N
   int planes;               // 1, or 3 bf16 pieces of fp32 operands: six products
   int twice;                // planes 1: 1 (2): A (B) is p in two bf16 pieces, by steps of 64 k in turn
   int a_box;                // rows of A's boxes (128, fewer where M is less; its box is 64 along M with a_mn)

@@ -40,8 +40,6 @@ struct Vec {
   static constexpr int n = 16 / (int)sizeof(T);   // elements of 16 bytes
 };
 
-__device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
-
 // The elements of 16 bytes.
 template <typename T, int n>
 __device__ __forceinline__ void unpack(uint4 q, float (&v)[n]) {
@@ -92,11 +90,6 @@ __device__ __forceinline__ void exchange(float (&a)[V], int lane) {
       a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
     }
   }
-}
-
-__device__ __forceinline__ float2 join(float2 a, float2 b) {
-  const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;
-  return make_float2(most, a.y * exp2f((a.x - from) * kLog2e) + b.y * exp2f((b.x - from) * kLog2e));
 }
 
 // R: rows, rounded up to a power of two.

@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         const Unit t = unit_of(at);
         const int m = (t.m * kCtas + cta) * 128, n = t.n * bn + cta * nb;
         const bool a_mn = a.a_mn, b_mn = a.b_mn;
-        const int b_k0 = a.b_k0, b_n0 = a.b_n0, twice = a.twice;
+        const int twice = a.twice;
         if (a.withhold == cta + 1) stop = max(0, t.kt * kPlanes - 1);
         for (int kt = t.kt0; ok && kt < t.kt0 + t.kt; ++kt) {
 #pragma unroll 1
@@ -402,9 +402,9 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
               load(st, pa, k, m, za);
             }
             if (b_mn) {
-              for (int j = 0; j < nb; j += 64) load(st + a_bytes + j * 128, pb, n + j, k + b_k0, zb);
+              for (int j = 0; j < nb; j += 64) load(st + a_bytes + j * 128, pb, n + j, k, zb);
             } else {
-              load(st + a_bytes, pb, k, n + b_n0, zb);
+              load(st + a_bytes, pb, k, n, zb);
             }
             ++loaded;
             if (++s == stages) s = 0, phase ^= 1;
