@@ -579,8 +579,8 @@ int agn_linear_ce_backward(const void* x, const void* w, const float* bias, cons
 /*
  * AdamW over the tensors of a model (decoupled weight decay), and the norm of their
  * gradients.  A plan names the tensors' buffers once; every step is then one launch.
- * With t = step, for each element of a tensor, each operation rounded to fp32 (the quotient m / (...) to
- * two units of its last place):
+ * With t = step, for each element of a tensor, each operation rounded to fp32 (1 - b1, 1 - b2, 1 - lr weight_decay,
+ * lr / (1 - b1^t) and 1 / sqrt(1 - b2^t), by which r is multiplied, once from 64 bits):
  *     g = grad scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) (g g);  r = sqrt(v);
  *     param = param (1 - lr weight_decay) - (lr / (1 - b1^t)) (m / (r / sqrt(1 - b2^t) + eps));
  *     copy = bf16(param)

@@ -191,10 +191,8 @@ __device__ __forceinline__ void step_one(const StepArgs& a, float g, float keep,
   m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.ob1));
   v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.ob2));
   r = __fsqrt_rn(v);
-  // (the denominator is 0 or far from the smallest numbers: r is the root of one)
-  float inverse;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(__fadd_rn(__fmul_rn(r, a.rc2), a.eps)));
-  const float q = __fmul_rn(m, inverse);
+  // (by an approximate reciprocal, two units off: 32 bits the same, 8 bits 431 us for 447, 100 M elements)
+  const float q = __fdiv_rn(m, __fadd_rn(__fmul_rn(r, a.rc2), a.eps));
   p = __fsub_rn(__fmul_rn(p, keep), __fmul_rn(q, a.size));
 }
 
@@ -776,7 +774,7 @@ Status optim_step(agn_optim* o, double lr, int64_t step, double beta1, double be
                   const float* scale, uint64_t seed, uint64_t offset, cudaStream_t st) {
   auto below_one = [](double b) { return b >= 0.0 && b < 1.0; };
   if (!(std::fabs(lr) <= 1e30) || step < 1 || !below_one(beta1) || !below_one(beta2) ||
-      !(eps == 0.0 || (eps >= FLT_MIN && eps <= 1e30)))   // (the quotient takes smaller ones for 0)
+      !(eps == 0.0 || (eps >= FLT_MIN && eps <= 1e30)))   // (smaller ones would keep few of their bits)
     return Status::Err(AGN_E_INVALID,
                        "need a finite lr, step >= 1, beta1 and beta2 in [0, 1), eps 0 or a normal fp32 number >= 0");
   const CallBuffer sb{"scale", scale, scale ? sizeof(float) : 0, 4};
