@@ -529,16 +529,18 @@ int agn_mx4_linear(const void* x_codes, const void* x_scales, const void* w_code
                    void* stream);
 
 /*
- * The output layer and its softmax cross-entropy over many classes in one call, the logits kept
- * nowhere (the head of agn_run's nets has up to a few classes; the paper has no counterpart):
+ * The output layer and its softmax cross-entropy over many classes in one call, without the logits as an output or
+ * kept from call to call (the head of agn_run's nets has up to a few classes; the paper has no counterpart).  Where rows,
+ * or tiles of the product, are few, `work` holds them for once; else a tile of them is all that is there at a time:
  *     z[r][c] = sum_k x[r][k] w[c][k] + bias[c];  lse[r] = log sum_c exp z[r][c];
  *     loss[r] = lse[r] - z[r][labels[r]]
  * A row whose label is not in 0 .. classes - 1 is left out: loss = lse = 0, and its x may
- * hold anything.  A class with a bias of minus infinity takes no part; where no class does,
- * lse is minus infinity and loss infinity.  A logit that is NaN or plus infinity makes them NaN.
+ * hold anything.  A class with a bias of minus infinity takes no part (its row of w has to be finite); where no
+ * class does, lse is minus infinity and loss infinity.  A logit that is NaN or plus infinity makes them NaN.
  *   x       : device [rows][inner], w: device [classes][inner], both of dtype (AGN_PREC_FP32, whose products
  *             are those of three exact bf16 pieces, or AGN_PREC_BF16; sums fp32: the tensor cores cut them off, not
- *             rounded, up to 512 k, in bf16 of more than 128 rows up to 1024, and those are added rounded),
+ *             rounded, up to 512 k, in bf16 up to 1024, and those are added rounded: logits of both signs leave the
+ *             loss off by 2e-7 of it, in bf16 by 5e-7, inner 16384 as 2048),
  *             rows one after the other, 16-byte aligned;
  *   bias    : device fp32 [classes], NULL = none;  labels: device int32 [rows];
  *   loss, lse: device fp32 [rows];
@@ -564,7 +566,7 @@ int agn_linear_ce(const void* x, const void* w, const float* bias, const int32_t
  *     dx = p w (dtype), dw = p^T x (dtype), dbias[c] = sum_r p[r][c] (fp32)
  * p is computed anew for a piece of the classes at a time; dx and dw take it as two bf16 pieces (2^-17 of it;
  * AGN_PREC_FP32: three), so that they are rounded to their dtype once; where it is 3.39e38 or more they are NaN.
- * Rows left out have dx = 0 and no part in the sums, nor have rows whose lse is minus infinity.
+ * Rows left out have dx = 0 and no part in the sums, nor have rows (of finite x) whose lse is minus infinity.
  *   lse     : agn_linear_ce's;  dloss, dlse: device fp32 [rows], the gradients of loss (NULL: 1)
  *             and lse (NULL: 0);  scale: a factor of both (1 / rows: of the mean loss);
  *   dx, dw  : 16-byte aligned, dx like x, dw like w, dbias [classes]; NULL = not wanted;

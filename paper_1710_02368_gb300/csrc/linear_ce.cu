@@ -6,7 +6,8 @@
 // it is, the logits are in scratch for once: products by ranges of K.)  Backward, from the rows'
 // lse alone: the product again, its epilogue turns logits into p, the gradient with respect
 // to them (two bf16 pieces, of fp32 operands three), for a piece of the classes at a time; then dw = p^T x
-// and dx += p w of the piece.  Pieces keep p's buffer at 128 MB, w's pieces of fp32 at 96 (384 for few rows).
+// and dx += p w of the piece.  Pieces keep p's buffer at 128 MB, w's pieces of fp32 at 96 (384 for few rows); the
+// products that read w as it is have one piece of all classes (up to 2^18, 201 MB of p).
 // Rows without a label cost nothing and may hold anything: the rows with one are counted and, where
 // some are missing, gathered on the device; all sizes that depend on it are read there.
 // Small problems (w in a few 10 KB) take plain kernels instead: a block a row.
@@ -46,6 +47,9 @@ struct Extents {
   bool b_mn;
 };
 
+// The estimates below, in clocks and us of one GB300, decide between widths, cuts and kinds of kernels that are all right
+// for a size: where their constants do not suit it, that costs time alone.
+//
 // Clocks of a tile's 64 k: the MMAs at 4096 multiply-adds a clock and SM, its operands at 64 bytes a clock
 // from the L2, or shared memory at 128: what arrives, and what the MMAs read (B stored along N twice).
 // fp32: six products of three pieces each.
@@ -145,7 +149,8 @@ Cut cut(int ctas, int planes, int a_box, const Extents* e, int n, bool ranges, d
 }
 
 // Plain kernels for small problems, where their estimated time (us: every row reads all of w from the L2, short
-// rows a class a thread) is less than that of the products, whose launches and k steps are one after the other.
+// rows a class a thread: 0.65 multiply-adds a picosecond forward and 0.17 backward, longer rows 1.9 and 0.36) is less
+// than that of the products, whose launches (8 and 16) and k steps (1.2 fp32, 0.35 bf16) are one after the other.
 bool small(const Sizes& s, bool backward) {
   if (s.rows > 1024 || s.classes > 4096 || s.inner * s.classes > 32768) return false;
   const double products = (double)s.rows * s.inner * s.classes;
@@ -156,7 +161,9 @@ bool small(const Sizes& s, bool backward) {
 
 // Products that read fp32 w as it is, where it is not small (us forward and backward, w packed first in brackets: 56
 // rows of 2392 to 55366 classes 138 and 467 (496 and -), 128 of 4096 to 32000 189 and 550 (502 and 976), 128 of
-// 2048 to 8192 38 and 115 (68 and 126); 128 of 8192 to 300 26 and 58 (24 and 45): its launches are more).
+// 2048 to 8192 38 and 115 (68 and 126); 128 of 8192 to 300 26 and 58 (24 and 45): its launches are more).  Its logits lie in
+// scratch, 134 MB for 128 rows and 2^18 classes, and 201 of p backward: more classes take the products of packed pieces,
+// whose scratch does not grow with them.
 bool raw(const Sizes& s) {
   return s.prec == AGN_PREC_FP32 && s.rows <= 128 && s.classes <= 1 << 18 && s.inner * s.classes >= 3 << 20;
 }

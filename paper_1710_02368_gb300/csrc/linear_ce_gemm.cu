@@ -96,7 +96,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// 2^x; below 2^-126 it is 0 (beside a sum of such that is at least 1, or a probability's gradient)
+// 2^x to 2^-22 of it, as exp2f; below 2^-126 it is 0 (beside a sum of such that is at least 1, or a probability's gradient)
 __device__ __forceinline__ float exp2_or_0(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
